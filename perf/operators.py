@@ -268,7 +268,7 @@ def _statistics(x, off, G):
     x = x.view(rows, G, C // G)
     mean = (_graph_sums(x.sum(2), off) / count).float()
     var = _graph_sums(((x - mean[gid][..., None]) ** 2).sum(2), off) / count
-    return mean, (1 / torch.sqrt(var + EPS)).float()
+    return mean.contiguous(), (1 / torch.sqrt(var + EPS)).float().contiguous()
 
 
 def _run_plain(c, s):
