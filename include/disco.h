@@ -29,6 +29,9 @@
  *                       dc_simulate.
  *   dc_train_step       one step of the estimator's supervised training on a batch of
  *                       fused ops with profiled times (Sec. 3.3.3: loss of Eq. (1), Adam).
+ *   dc_dense, dc_graph_norm, dc_keep_rows   the parts of deep estimators one by one, with
+ *                       their gradients: a dense layer with bias, activation and residual,
+ *                       a norm over the rows of each graph, rows kept in 8 bits.
  *
  * Conventions
  *  - Every call returns a dc_status; nothing throws or aborts.
@@ -401,6 +404,121 @@ dc_status dc_train_step(dc_ctx* ctx, const dc_batch* in, const float* target, fl
 /* Copies the current weights to host arrays laid out as for dc_set_weights (DC_F32 contexts).
  * Synchronises `stream`.                                                                       */
 dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* head, void* stream);
+
+/* ---- Operators on the rows of a batch ----
+ *
+ * The parts that layers of deep estimators are made of, on device arrays of the caller: rows of `ld` elements each, in
+ * the storage type of the call (fp32 or bf16, whatever the context's own type is); statistics, biases and the gradients
+ * of vectors are fp32.  Sums are formed in fp32 or more.  The calls take the context for its device and its error text;
+ * none uses its scratch, so calls on different streams may overlap as long as their arrays and workspaces are their
+ * own.  They allocate nothing and do not synchronise, and may be captured into a graph.  Work is enqueued on
+ * `stream`, a stream of the context's device, whatever device is current.  An array of outputs may be null where
+ * the text says so; rows = 0 is allowed.  Limits: rows and graphs fit in int32, in and out are at most 65536,
+ * channels per group at most 1024, channels at most 8192.                                                        */
+typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 3 } dc_activation;
+/* GELU is z (1 + erf(z / sqrt 2)) / 2, SiLU z / (1 + e^-z). */
+
+/* Rows kept in 8 bits for a backward pass.  Per row and 32 columns (the last block may be short): m = max |x|, e = the
+ * smallest integer of [-126, 121] with m <= 127 * 2^e, code = x * 2^-e rounded to nearest even within +-127, and +-1
+ * where x is not zero but would round to it; exponent = e + 127.  The value kept is code * 2^e: off by at most half a step
+ * 2^e, a whole one where |x| is below half of it; its sign is x's.  A block that holds a number that is not finite
+ * has exponent 255 and only NaN.  code [rows, 32 * ceil(cols / 32)] (behind the last column: zeros), exponent
+ * [rows, ceil(cols / 32)].                                                                                          */
+typedef struct {
+  int8_t* code;         /* dev */
+  uint8_t* exponent;    /* dev */
+  int64_t ld_code;      /* elements from row to row, at least 32 * ceil(cols / 32) */
+  int64_t ld_exponent;  /* at least ceil(cols / 32)                                */
+} dc_kept_rows;
+dc_status dc_keep_rows(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                       const dc_kept_rows* out, void* stream);
+dc_status dc_restore_rows(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols, const dc_kept_rows* in, void* x,
+                          int64_t ldx, void* stream);
+
+/* Dense layer: Z = X W + b, Y = act(Z) + R.  With dtype DC_BF16, X, W, R, Y and Z are bf16, each output is rounded once. */
+typedef struct {
+  int32_t dtype, act;   /* dc_dtype, dc_activation                                    */
+  int64_t rows;
+  int32_t in, out;      /* X [rows, in], W [in, out] row-major                        */
+  const void* X;
+  int64_t ldx;
+  const void* W;
+  int64_t ldw;
+  const float* bias;    /* [out] or null                                              */
+  const void* residual; /* R [rows, out] or null; may be the same array as Y          */
+  int64_t ld_residual;
+  void* Z;              /* [rows, out] or null: what the gradient of the activation needs */
+  int64_t ldz;
+  void* Y;              /* [rows, out], not X                                         */
+  int64_t ldy;
+} dc_dense_args;
+dc_status dc_dense(dc_ctx* ctx, const dc_dense_args* args, void* stream);
+
+/* Its gradients: dZ = dY act'(Z); dX = dZ W^T, dW = X^T dZ, db = sum of the rows of dZ (dR is dY).  X is given as rows or
+ * as kept rows.  With DC_BF16, dZ is rounded to bf16 for the products (not for db) and dX and dW are bf16.  The
+ * sums over rows are split and joined in a fixed order: the same call gives the same bits.                           */
+typedef struct {
+  int32_t dtype, act;
+  int64_t rows;
+  int32_t in, out;
+  const void* dY;       /* [rows, out]                                                */
+  int64_t lddy;
+  const void* Z;        /* [rows, out]; not read with DC_ACT_NONE                     */
+  int64_t ldz;
+  const void* X;        /* [rows, in], or null with kept                              */
+  int64_t ldx;
+  const dc_kept_rows* kept;  /* host struct, or null; X is not read then              */
+  const void* W;
+  int64_t ldw;
+  void* dX;             /* [rows, in] or null                                         */
+  int64_t lddx;
+  void* dW;             /* [in, out] or null                                          */
+  int64_t lddw;
+  float* db;            /* [out] or null                                              */
+  void* workspace;      /* dev, dc_dense_backward_bytes() of them, if dW or db        */
+  size_t workspace_bytes;
+} dc_dense_backward_args;
+size_t dc_dense_backward_bytes(const dc_ctx* ctx, int64_t rows, int32_t in, int32_t out);
+dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, void* stream);
+
+/* Norm over the rows of each graph (a group norm whose positions are the rows of a graph), with an activation.  The
+ * channels are in `groups` groups of channels / groups neighbours; per graph and group, over its rows and channels:
+ *   mean, rstd = 1 / sqrt(variance + eps);  y = act(gamma (x - mean) rstd + beta)
+ * A graph without rows has mean 0 and variance 0.  Rows of no graph (before node_off[0], behind node_off[n_graphs]) are
+ * neither read nor written.  A graph whose offsets do not ascend within [0, rows] is left alone, and dc_check
+ * reports DC_ERR_BAD_GRAPH.                                                                                         */
+typedef struct {
+  int32_t dtype, act;
+  int64_t rows;             /* rows of x and y                                            */
+  int32_t n_graphs, channels, groups;
+  float eps;                /* > 0                                                        */
+  const int32_t* node_off;  /* dev [n_graphs + 1]                                         */
+  const void* X;            /* [rows, channels]; backward: null with kept                 */
+  int64_t ldx;
+  const float* gamma;       /* [channels], or null for 1                                  */
+  const float* beta;        /* [channels], or null for 0                                  */
+  float* mean;              /* [n_graphs, groups]: written by the forward, read by the backward */
+  float* rstd;
+  void* Y;                  /* [rows, channels]; may be X                                 */
+  int64_t ldy;
+  /* backward only: u = gamma dY act'(.), xh = (x - mean) rstd,
+   * dX = rstd (u - mean u - xh mean(u xh)) + dres, dgamma = sum dY act'(.) xh, dbeta = sum dY act'(.)  */
+  const dc_kept_rows* kept; /* x as kept rows, or null                                    */
+  const void* dY;
+  int64_t lddy;
+  const void* dres;         /* [rows, channels] or null: the gradient that goes past the norm */
+  int64_t lddres;
+  void* dX;                 /* may be dY or dres                                          */
+  int64_t lddx;
+  float* dgamma;            /* [channels], null together with dbeta                       */
+  float* dbeta;
+  void* workspace;          /* dev, dc_graph_norm_bytes() of them                         */
+  size_t workspace_bytes;
+} dc_graph_norm_args;
+size_t dc_graph_norm_bytes(const dc_ctx* ctx, int64_t rows, int32_t n_graphs, int32_t channels, int32_t groups,
+                           int32_t backward);
+dc_status dc_graph_norm(dc_ctx* ctx, const dc_graph_norm_args* args, void* stream);
+dc_status dc_graph_norm_backward(dc_ctx* ctx, const dc_graph_norm_args* args, void* stream);
 
 /* dc_contract_graphs into context-owned buffers followed by dc_gnn_forward. */
 dc_status dc_eval_candidates(dc_ctx* ctx, int32_t n_cand, const int32_t* cand_graph, const int32_t* cand_off,

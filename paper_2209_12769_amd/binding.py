@@ -32,6 +32,8 @@ DC_AGG_ATTENTION = 1
 DC_KERNELS_SEPARATE_LAYERS = 1
 DC_KERNELS_EVERY_FUSED_OP = 2
 DC_DRAW_DEPENDENCY, DC_DRAW_OP = 0, 1
+DC_ACT_NONE, DC_ACT_RELU, DC_ACT_GELU, DC_ACT_SILU = 0, 1, 2, 3
+ACTIVATIONS = {"none": DC_ACT_NONE, "relu": DC_ACT_RELU, "gelu": DC_ACT_GELU, "silu": DC_ACT_SILU}
 STATUS_NAMES = {0: "DC_OK", 1: "DC_ERR_INVALID_ARG", 2: "DC_ERR_BAD_GRAPH", 3: "DC_ERR_BAD_PARTITION",
                 4: "DC_ERR_CAPACITY", 5: "DC_ERR_OOM", 6: "DC_ERR_HIP", 7: "DC_ERR_UNSUPPORTED"}
 
@@ -65,6 +67,35 @@ class DcSearchResult(C.Structure):
 class DcTrainParams(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("floor", C.c_float), ("max_samples", C.c_int64), ("max_rows", C.c_int64)]
+
+
+class DcKeptRows(C.Structure):
+    _fields_ = [("code", C.c_void_p), ("exponent", C.c_void_p), ("ld_code", C.c_int64), ("ld_exponent", C.c_int64)]
+
+
+class DcDenseArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("n_in", C.c_int32), ("n_out", C.c_int32),
+                ("X", C.c_void_p), ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("Z", C.c_void_p), ("ldz", C.c_int64),
+                ("Y", C.c_void_p), ("ldy", C.c_int64)]
+
+
+class DcDenseBackwardArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("n_in", C.c_int32), ("n_out", C.c_int32),
+                ("dY", C.c_void_p), ("lddy", C.c_int64), ("Z", C.c_void_p), ("ldz", C.c_int64), ("X", C.c_void_p),
+                ("ldx", C.c_int64), ("kept", C.POINTER(DcKeptRows)), ("W", C.c_void_p), ("ldw", C.c_int64),
+                ("dX", C.c_void_p), ("lddx", C.c_int64), ("dW", C.c_void_p), ("lddw", C.c_int64), ("db", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class DcGraphNormArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("n_graphs", C.c_int32),
+                ("channels", C.c_int32), ("groups", C.c_int32), ("eps", C.c_float), ("node_off", C.c_void_p),
+                ("X", C.c_void_p), ("ldx", C.c_int64), ("gamma", C.c_void_p), ("beta", C.c_void_p), ("mean", C.c_void_p),
+                ("rstd", C.c_void_p), ("Y", C.c_void_p), ("ldy", C.c_int64), ("kept", C.POINTER(DcKeptRows)),
+                ("dY", C.c_void_p), ("lddy", C.c_int64), ("dres", C.c_void_p), ("lddres", C.c_int64), ("dX", C.c_void_p),
+                ("lddx", C.c_int64), ("dgamma", C.c_void_p), ("dbeta", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 class DiscoError(RuntimeError):
@@ -116,6 +147,17 @@ def lib():
         L.dc_loss_gradients.argtypes = [vp, C.POINTER(DcBatch), vp, vp, vp, vp, vp]
         L.dc_train_step.argtypes = [vp, C.POINTER(DcBatch), vp, vp, vp]
         L.dc_get_weights.argtypes = [vp, vp, vp, vp, vp]
+        i64, size = C.c_int64, C.c_size_t
+        L.dc_keep_rows.argtypes = [vp, i32, i64, i32, vp, i64, C.POINTER(DcKeptRows), vp]
+        L.dc_restore_rows.argtypes = [vp, i32, i64, i32, C.POINTER(DcKeptRows), vp, i64, vp]
+        L.dc_dense.argtypes = [vp, C.POINTER(DcDenseArgs), vp]
+        L.dc_dense_backward_bytes.argtypes = [vp, i64, i32, i32]
+        L.dc_dense_backward_bytes.restype = size
+        L.dc_dense_backward.argtypes = [vp, C.POINTER(DcDenseBackwardArgs), vp]
+        L.dc_graph_norm_bytes.argtypes = [vp, i64, i32, i32, i32, i32]
+        L.dc_graph_norm_bytes.restype = size
+        L.dc_graph_norm.argtypes = [vp, C.POINTER(DcGraphNormArgs), vp]
+        L.dc_graph_norm_backward.argtypes = [vp, C.POINTER(DcGraphNormArgs), vp]
         L.dc_check.argtypes = [vp, vp]
         L.dc_select_kernels.argtypes = [vp, i32]
         L.dc_last_totals.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64), vp]
@@ -127,7 +169,8 @@ def lib():
                   "dc_gnn_forward", "dc_eval_candidates", "dc_simulate", "dc_check", "dc_last_totals", "dc_profile_begin",
                   "dc_profile_end", "dc_set_profile", "dc_module_times", "dc_cost_candidates", "dc_last_fused_ops",
                   "dc_last_fused_op_repeats", "dc_walked_modules", "dc_search",
-                  "dc_train_begin", "dc_select_kernels", "dc_fused_op_batch", "dc_loss_gradients", "dc_train_step", "dc_get_weights"):
+                  "dc_train_begin", "dc_select_kernels", "dc_fused_op_batch", "dc_loss_gradients", "dc_train_step", "dc_get_weights",
+                  "dc_keep_rows", "dc_restore_rows", "dc_dense", "dc_dense_backward", "dc_graph_norm", "dc_graph_norm_backward"):
             getattr(L, n).restype = i32
         _lib = L
     return _lib
@@ -244,6 +287,38 @@ def dc_get_weights(ctx, W_layers: np.ndarray, b_layers: np.ndarray, head: np.nda
     return lib().dc_get_weights(ctx, W_layers.ctypes.data, b_layers.ctypes.data, head.ctypes.data, stream)
 
 
+def dc_keep_rows(ctx, dtype: int, rows: int, cols: int, x_ptr, ldx: int, out: DcKeptRows, stream: int = 0) -> int:
+    return lib().dc_keep_rows(ctx, dtype, rows, cols, x_ptr, ldx, C.byref(out), stream)
+
+
+def dc_restore_rows(ctx, dtype: int, rows: int, cols: int, kept: DcKeptRows, x_ptr, ldx: int, stream: int = 0) -> int:
+    return lib().dc_restore_rows(ctx, dtype, rows, cols, C.byref(kept), x_ptr, ldx, stream)
+
+
+def dc_dense(ctx, args: DcDenseArgs, stream: int = 0) -> int:
+    return lib().dc_dense(ctx, C.byref(args), stream)
+
+
+def dc_dense_backward_bytes(ctx, rows: int, n_in: int, n_out: int) -> int:
+    return int(lib().dc_dense_backward_bytes(ctx, rows, n_in, n_out))
+
+
+def dc_dense_backward(ctx, args: DcDenseBackwardArgs, stream: int = 0) -> int:
+    return lib().dc_dense_backward(ctx, C.byref(args), stream)
+
+
+def dc_graph_norm_bytes(ctx, rows: int, n_graphs: int, channels: int, groups: int, backward: bool) -> int:
+    return int(lib().dc_graph_norm_bytes(ctx, rows, n_graphs, channels, groups, int(backward)))
+
+
+def dc_graph_norm(ctx, args: DcGraphNormArgs, stream: int = 0) -> int:
+    return lib().dc_graph_norm(ctx, C.byref(args), stream)
+
+
+def dc_graph_norm_backward(ctx, args: DcGraphNormArgs, stream: int = 0) -> int:
+    return lib().dc_graph_norm_backward(ctx, C.byref(args), stream)
+
+
 def dc_check(ctx, stream: int = 0) -> int:
     return lib().dc_check(ctx, stream)
 
@@ -300,6 +375,21 @@ class DeviceBatch:
     Xc: "object"
 
 
+class KeptRows:
+    """Rows kept in 8 bits (see dc_kept_rows): int8 codes and uint8 exponents, device tensors."""
+
+    def __init__(self, code, exponent, cols: int):
+        rows, blocks = int(code.shape[0]), -(-cols // 32)
+        if code.dim() != 2 or exponent.dim() != 2 or code.shape[1] < 32 * blocks or tuple(exponent.shape) != (rows, blocks):
+            raise ValueError(f"kept rows of {cols} columns need codes [rows, {32 * blocks}] and exponents [rows, {blocks}]")
+        self.code, self.exponent, self.cols = code, exponent, cols
+        self.c = DcKeptRows(code.data_ptr(), exponent.data_ptr(), code.stride(0), exponent.stride(0))
+
+    @property
+    def rows(self) -> int:
+        return int(self.code.shape[0])
+
+
 class Evaluator:
     """Owns one dc_ctx.  Methods move pointers across the C ABI; nothing is computed in Python."""
 
@@ -309,6 +399,8 @@ class Evaluator:
         self.torch = torch
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
         self.cfg = DcConfig(F, H, L, DC_BF16 if dtype == "bf16" else DC_F32, max_cand, max_base_nodes,
                             max_base_edges, max_nodes, max_edges,
                             DC_AGG_ATTENTION if agg == "attention" else DC_AGG_MEAN, heads)
@@ -465,6 +557,173 @@ class Evaluator:
             loss = self.torch.empty(1, dtype=self.torch.float32, device=self.device)
         self._ok(dc_train_step(self.ctx, batch.c, target.data_ptr(), loss.data_ptr(), self._stream()), "dc_train_step")
         return loss
+
+    # ---- operators on rows of a batch (device tensors; rows may be apart, columns are neighbours) ----
+    def _matrix(self, x, name: str, cols: Optional[int] = None, rows: Optional[int] = None, dtype=None):
+        """Checks a matrix and returns the elements from row to row."""
+        if x.device != self.device or x.dim() != 2:
+            raise ValueError(f"{name}: need a matrix on {self.device}")
+        if dtype is None:
+            if x.dtype not in (self.torch.float32, self.torch.bfloat16):
+                raise ValueError(f"{name}: need float32 or bfloat16, not {x.dtype}")
+        elif x.dtype != dtype:
+            raise ValueError(f"{name}: need {dtype}, not {x.dtype}")
+        if (cols is not None and x.shape[1] != cols) or (rows is not None and x.shape[0] != rows):
+            raise ValueError(f"{name}: shape {tuple(x.shape)} does not fit")
+        if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
+            raise ValueError(f"{name}: the columns of a row must be neighbours")
+        return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+    def _vector(self, x, name: str, n: int, dtype=None):
+        if x.device != self.device or x.dtype != (dtype or self.torch.float32) or tuple(x.shape) != (n,) or not x.is_contiguous():
+            raise ValueError(f"{name}: need {n} contiguous {dtype or self.torch.float32} on {self.device}")
+        return x.data_ptr()
+
+    def _kept(self, kept: KeptRows, cols: int, rows: int):
+        k = kept
+        if (k.code.device != self.device or k.exponent.device != self.device or k.code.dtype != self.torch.int8
+                or k.exponent.dtype != self.torch.uint8 or k.cols != cols or k.rows != rows or (rows and k.code.stride(1) != 1)
+                or (rows and k.exponent.shape[1] > 1 and k.exponent.stride(1) != 1)):
+            raise ValueError("kept rows do not fit")
+        return C.pointer(DcKeptRows(k.code.data_ptr(), k.exponent.data_ptr(), k.code.stride(0) if rows > 1 else k.code.shape[1],
+                                    k.exponent.stride(0) if rows > 1 else k.exponent.shape[1]))
+
+    @staticmethod
+    def _act(act: str) -> int:
+        if act not in ACTIVATIONS:
+            raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTIVATIONS)}")
+        return ACTIVATIONS[act]
+
+    def _type(self, x) -> int:
+        return DC_BF16 if x.dtype == self.torch.bfloat16 else DC_F32
+
+    def keep_rows(self, x) -> KeptRows:
+        """x [rows, cols] in 8 bits, one power of two per row and 32 columns."""
+        ld, (rows, cols) = self._matrix(x, "x"), x.shape
+        blocks = -(-cols // 32)
+        k = KeptRows(self.torch.empty((rows, 32 * blocks), dtype=self.torch.int8, device=self.device),
+                     self.torch.empty((rows, blocks), dtype=self.torch.uint8, device=self.device), cols)
+        self._ok(dc_keep_rows(self.ctx, self._type(x), rows, cols, x.data_ptr(), ld, self._kept(k, cols, rows).contents,
+                              self._stream()), "dc_keep_rows")
+        return k
+
+    def restore_rows(self, kept: KeptRows, dtype=None, out=None):
+        rows, cols = kept.rows, kept.cols
+        if out is None:
+            out = self.torch.empty((rows, cols), dtype=dtype or self.torch.float32, device=self.device)
+        ld = self._matrix(out, "out", cols, rows, dtype)
+        self._ok(dc_restore_rows(self.ctx, self._type(out), rows, cols, self._kept(kept, cols, rows).contents, out.data_ptr(),
+                                 ld, self._stream()), "dc_restore_rows")
+        return out
+
+    def dense(self, x, w, bias=None, act: str = "none", residual=None, out=None, want_pre: bool = False):
+        """act(x w + bias) + residual; with want_pre also x w + bias, which dense_backward takes as `pre`."""
+        a = DcDenseArgs()
+        a.ldx, (rows, n_in) = self._matrix(x, "x"), x.shape
+        a.ldw, n_out = self._matrix(w, "w", rows=n_in, dtype=x.dtype), int(w.shape[1])
+        if out is None:
+            out = self.torch.empty((rows, n_out), dtype=x.dtype, device=self.device)
+        a.ldy = self._matrix(out, "out", n_out, rows, x.dtype)
+        a.dtype, a.act, a.rows, a.n_in, a.n_out = self._type(x), self._act(act), rows, n_in, n_out
+        a.X, a.W, a.Y = x.data_ptr(), w.data_ptr(), out.data_ptr()
+        if bias is not None:
+            a.bias = self._vector(bias, "bias", n_out)
+        if residual is not None:
+            a.ld_residual = self._matrix(residual, "residual", n_out, rows, x.dtype)
+            a.residual = residual.data_ptr()
+        pre = None
+        if want_pre:
+            pre = self.torch.empty((rows, n_out), dtype=x.dtype, device=self.device)
+            a.Z, a.ldz = pre.data_ptr(), n_out
+        self._ok(dc_dense(self.ctx, a, self._stream()), "dc_dense")
+        return (out, pre) if want_pre else out
+
+    def dense_backward(self, dy, x, w, act: str = "none", pre=None, want=("x", "w", "b")):
+        """Gradients (dx, dw, db) of dense at x, w and bias for the gradient dy at its result; None for those not in
+        `want`.  x: the rows, or KeptRows of them."""
+        torch = self.torch
+        a = DcDenseBackwardArgs()
+        a.lddy, (rows, n_out) = self._matrix(dy, "dy"), dy.shape
+        a.ldw, n_in = self._matrix(w, "w", n_out, dtype=dy.dtype), int(w.shape[0])
+        a.dtype, a.act, a.rows, a.n_in, a.n_out = self._type(dy), self._act(act), rows, n_in, n_out
+        a.dY, a.W = dy.data_ptr(), w.data_ptr()
+        if a.act != DC_ACT_NONE:
+            if pre is None:
+                raise ValueError("pre: the gradient of the activation needs x w + bias")
+            a.ldz, a.Z = self._matrix(pre, "pre", n_out, rows, dy.dtype), pre.data_ptr()
+        if isinstance(x, KeptRows):
+            a.kept = self._kept(x, n_in, rows)
+        else:
+            a.ldx, a.X = self._matrix(x, "x", n_in, rows, dy.dtype), x.data_ptr()
+        dx = torch.empty((rows, n_in), dtype=dy.dtype, device=self.device) if "x" in want else None
+        dw = torch.empty((n_in, n_out), dtype=dy.dtype, device=self.device) if "w" in want else None
+        db = torch.empty(n_out, dtype=torch.float32, device=self.device) if "b" in want else None
+        if dx is not None:
+            a.dX, a.lddx = dx.data_ptr(), n_in
+        if dw is not None:
+            a.dW, a.lddw = dw.data_ptr(), n_out
+        if db is not None:
+            a.db = db.data_ptr()
+        if dw is not None or db is not None:
+            a.workspace_bytes = dc_dense_backward_bytes(self.ctx, rows, n_in, n_out)
+            ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
+            a.workspace = ws.data_ptr()
+        self._ok(dc_dense_backward(self.ctx, a, self._stream()), "dc_dense_backward")
+        return dx, dw, db
+
+    def _norm_args(self, rows: int, channels: int, like, node_off, groups: int, gamma, beta, act: str, backward: bool):
+        a = DcGraphNormArgs()
+        if node_off.dim() != 1 or node_off.numel() < 1:
+            raise ValueError("node_off: need at least one offset")
+        a.n_graphs = node_off.numel() - 1
+        a.node_off = self._vector(node_off, "node_off", a.n_graphs + 1, self.torch.int32)
+        a.dtype, a.act, a.rows, a.channels, a.groups = self._type(like), self._act(act), rows, channels, groups
+        if gamma is not None:
+            a.gamma = self._vector(gamma, "gamma", channels)
+        if beta is not None:
+            a.beta = self._vector(beta, "beta", channels)
+        a.workspace_bytes = dc_graph_norm_bytes(self.ctx, rows, a.n_graphs, channels, groups, backward)
+        ws = self.torch.empty(a.workspace_bytes, dtype=self.torch.uint8, device=self.device) if a.workspace_bytes else None
+        if ws is not None:
+            a.workspace = ws.data_ptr()
+        return a, ws
+
+    def graph_norm(self, x, node_off, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: str = "none", out=None):
+        """(y, mean, rstd): the norm over the rows of each graph and the channels of each group, with an activation.  Rows
+        of no graph are left as they are in `out`."""
+        ldx, (rows, channels) = self._matrix(x, "x"), x.shape
+        if out is None:
+            out = self.torch.empty((rows, channels), dtype=x.dtype, device=self.device)
+        a, ws = self._norm_args(rows, channels, x, node_off, groups, gamma, beta, act, False)
+        a.X, a.ldx, a.Y, a.ldy, a.eps = x.data_ptr(), ldx, out.data_ptr(), self._matrix(out, "out", channels, rows, x.dtype), eps
+        mean = self.torch.empty((a.n_graphs, groups), dtype=self.torch.float32, device=self.device)
+        rstd = self.torch.empty_like(mean)
+        a.mean, a.rstd = mean.data_ptr(), rstd.data_ptr()
+        self._ok(dc_graph_norm(self.ctx, a, self._stream()), "dc_graph_norm")
+        return out, mean, rstd
+
+    def graph_norm_backward(self, dy, x, node_off, groups: int, gamma, beta, mean, rstd, act: str = "none", residual=None,
+                            out=None):
+        """(dx, dgamma, dbeta) for the gradient dy at the result; `residual` is added to dx.  x: the rows, or KeptRows of
+        them; mean, rstd: what graph_norm returned."""
+        lddy, (rows, channels) = self._matrix(dy, "dy"), dy.shape
+        a, ws = self._norm_args(rows, channels, dy, node_off, groups, gamma, beta, act, True)
+        for v, name in ((mean, "mean"), (rstd, "rstd")):
+            if v.device != self.device or v.dtype != self.torch.float32 or tuple(v.shape) != (a.n_graphs, groups) or not v.is_contiguous():
+                raise ValueError(f"{name}: need float32 [{a.n_graphs}, {groups}] on {self.device}")
+        if out is None:
+            out = self.torch.empty((rows, channels), dtype=dy.dtype, device=self.device)
+        if isinstance(x, KeptRows):
+            a.kept = self._kept(x, channels, rows)
+        else:
+            a.ldx, a.X = self._matrix(x, "x", channels, rows, dy.dtype), x.data_ptr()
+        if residual is not None:
+            a.lddres, a.dres = self._matrix(residual, "residual", channels, rows, dy.dtype), residual.data_ptr()
+        grads = self.torch.empty((2, channels), dtype=self.torch.float32, device=self.device)
+        a.dY, a.lddy, a.dX, a.lddx = dy.data_ptr(), lddy, out.data_ptr(), self._matrix(out, "out", channels, rows, dy.dtype)
+        a.mean, a.rstd, a.dgamma, a.dbeta = mean.data_ptr(), rstd.data_ptr(), grads[0].data_ptr(), grads[1].data_ptr()
+        self._ok(dc_graph_norm_backward(self.ctx, a, self._stream()), "dc_graph_norm_backward")
+        return out, grads[0], grads[1]
 
     def get_weights(self):
         """(W_layers, b_layers, head) as host fp32 arrays in the layout of dc_set_weights."""

@@ -9,7 +9,7 @@
 #include <string>
 #include <vector>
 
-#include "common.h"
+#include "operators.h"
 
 using namespace dc;
 
@@ -1362,6 +1362,285 @@ dc_status dc_train_step(dc_ctx* ctx, const dc_batch* in, const float* target, fl
     e = hipGetLastError();
   }
   return e == hipSuccess ? DC_OK : hip_fail(ctx, e, "optimiser step");
+}
+
+// ---------------------------------------------------------------------------
+// operators on the rows of a batch
+// ---------------------------------------------------------------------------
+namespace {
+constexpr long long kRowsMost = 2147483647LL;
+
+// Work goes to the context's device whatever device is current.
+struct OnDevice {
+  int before = -1;
+  bool ok = true;
+  explicit OnDevice(int device) {
+    int now = device;
+    if (hipGetDevice(&now) != hipSuccess) {
+      ok = false;
+    } else if (now != device) {
+      before = now;
+      ok = hipSetDevice(device) == hipSuccess;
+    }
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+bool at(const void* p, int bytes) { return reinterpret_cast<size_t>(p) % (size_t)bytes == 0; }
+
+dc_status shape_check(dc_ctx* ctx, int32_t dtype, int64_t rows) {
+  if (dtype != DC_F32 && dtype != DC_BF16) return fail(ctx, DC_ERR_INVALID_ARG, "dtype must be DC_F32 or DC_BF16");
+  if (rows < 0) return fail(ctx, DC_ERR_INVALID_ARG, "negative rows");
+  if (rows > kRowsMost) return fail(ctx, DC_ERR_UNSUPPORTED, "rows must fit in int32");
+  return DC_OK;
+}
+// An array of rows x cols elements of `bytes` each: there, aligned to an element, rows that do not overlap.
+dc_status array_check(dc_ctx* ctx, const void* p, int64_t ld, int64_t rows, int32_t cols, int bytes, const char* name) {
+  if (rows == 0) return DC_OK;
+  if (!p) return fail(ctx, DC_ERR_INVALID_ARG, std::string("null ") + name);
+  if (!at(p, bytes)) return fail(ctx, DC_ERR_INVALID_ARG, std::string(name) + " is not aligned to its elements");
+  if (ld < cols) return fail(ctx, DC_ERR_INVALID_ARG, std::string(name) + ": rows shorter than their columns");
+  if (ld > (1LL << 40)) return fail(ctx, DC_ERR_UNSUPPORTED, std::string(name) + ": rows too far apart");
+  return DC_OK;
+}
+dc_status kept_check(dc_ctx* ctx, const dc_kept_rows* k, int64_t rows, int32_t cols) {
+  const int nb = (cols + kKeptBlock - 1) / kKeptBlock;
+  dc_status st = array_check(ctx, k->code, k->ld_code, rows, nb * kKeptBlock, 1, "code");
+  if (st != DC_OK) return st;
+  return array_check(ctx, k->exponent, k->ld_exponent, rows, nb, 1, "exponent");
+}
+KeptView kept_view(const dc_kept_rows* k) {
+  KeptView v{};
+  if (k) v = KeptView{reinterpret_cast<const signed char*>(k->code), k->exponent, (long long)k->ld_code, (long long)k->ld_exponent};
+  return v;
+}
+dc_status enqueue_result(dc_ctx* ctx, hipError_t e, const char* what) { return e == hipSuccess ? DC_OK : hip_fail(ctx, e, what); }
+
+dc_status keep_or_restore(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols, const void* src, void* dst, int64_t ldx,
+                          const dc_kept_rows* kept, hipStream_t s) {
+  dc_status st = shape_check(ctx, dtype, rows);
+  if (st != DC_OK) return st;
+  if (!kept) return fail(ctx, DC_ERR_INVALID_ARG, "null kept rows");
+  if (cols < 1 || cols > 65536) return fail(ctx, cols < 1 ? DC_ERR_INVALID_ARG : DC_ERR_UNSUPPORTED, "need 1 to 65536 columns");
+  st = array_check(ctx, src ? src : dst, ldx, rows, cols, dtype == DC_BF16 ? 2 : 4, "x");
+  if (st == DC_OK) st = kept_check(ctx, kept, rows, cols);
+  if (st != DC_OK || rows == 0) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  KeepArgs a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.bf16 = dtype == DC_BF16;
+  a.src = src;
+  a.dst = dst;
+  a.ld = ldx;
+  a.code = reinterpret_cast<signed char*>(kept->code);
+  a.exponent = kept->exponent;
+  a.ld_code = kept->ld_code;
+  a.ld_exponent = kept->ld_exponent;
+  a.n_cu = ctx->n_cu;
+  return enqueue_result(ctx, src ? launch_keep_rows(a, s) : launch_restore_rows(a, s), "kept rows launch");
+}
+
+dc_status dense_shape_check(dc_ctx* ctx, int32_t dtype, int32_t act, int64_t rows, int32_t in, int32_t out) {
+  dc_status st = shape_check(ctx, dtype, rows);
+  if (st != DC_OK) return st;
+  if (act < DC_ACT_NONE || act > DC_ACT_SILU) return fail(ctx, DC_ERR_INVALID_ARG, "unknown activation");
+  if (in < 1 || out < 1) return fail(ctx, DC_ERR_INVALID_ARG, "in and out must be positive");
+  if (in > 65536 || out > 65536) return fail(ctx, DC_ERR_UNSUPPORTED, "in and out must be at most 65536");
+  return DC_OK;
+}
+
+dc_status graph_norm_check(dc_ctx* ctx, const dc_graph_norm_args* a, bool backward, GraphNormArgs* g) {
+  if (!a) return fail(ctx, DC_ERR_INVALID_ARG, "null arguments");
+  dc_status st = shape_check(ctx, a->dtype, a->rows);
+  if (st != DC_OK) return st;
+  if (a->act < DC_ACT_NONE || a->act > DC_ACT_SILU) return fail(ctx, DC_ERR_INVALID_ARG, "unknown activation");
+  if (a->n_graphs < 0 || a->channels < 1 || a->groups < 1 || a->channels % a->groups)
+    return fail(ctx, DC_ERR_INVALID_ARG, "need n_graphs >= 0 and groups that divide the channels");
+  if (a->channels > 8192 || a->channels / a->groups > 1024)
+    return fail(ctx, DC_ERR_UNSUPPORTED, "at most 8192 channels and 1024 per group");
+  if (!backward && !(a->eps > 0.f)) return fail(ctx, DC_ERR_INVALID_ARG, "need eps > 0");
+  const int es = a->dtype == DC_BF16 ? 2 : 4;
+  if (a->n_graphs > 0 && (!a->node_off || !a->mean || !a->rstd)) return fail(ctx, DC_ERR_INVALID_ARG, "null node_off, mean or rstd");
+  if (!at(a->node_off, 4) || !at(a->mean, 4) || !at(a->rstd, 4) || !at(a->gamma, 4) || !at(a->beta, 4) || !at(a->dgamma, 4) ||
+      !at(a->dbeta, 4))
+    return fail(ctx, DC_ERR_INVALID_ARG, "node_off, statistics or vectors are not aligned to their elements");
+  if (backward && a->kept) st = kept_check(ctx, a->kept, a->rows, a->channels);
+  else st = array_check(ctx, a->X, a->ldx, a->rows, a->channels, es, "X");
+  if (st == DC_OK && !backward) st = array_check(ctx, a->Y, a->ldy, a->rows, a->channels, es, "Y");
+  if (st == DC_OK && backward) st = array_check(ctx, a->dY, a->lddy, a->rows, a->channels, es, "dY");
+  if (st == DC_OK && backward) st = array_check(ctx, a->dX, a->lddx, a->rows, a->channels, es, "dX");
+  if (st == DC_OK && backward && a->dres) st = array_check(ctx, a->dres, a->lddres, a->rows, a->channels, es, "dres");
+  if (st != DC_OK) return st;
+  if (backward && !a->dgamma != !a->dbeta) return fail(ctx, DC_ERR_INVALID_ARG, "dgamma and dbeta go together");
+  const size_t need = graph_norm_bytes(a->rows, a->n_graphs, a->channels, a->groups, backward, ctx->n_cu);
+  if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_graph_norm_bytes");
+  if (need > 0 && !at(a->workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+  *g = GraphNormArgs{};
+  g->rows = a->rows;
+  g->n_graphs = a->n_graphs;
+  g->node_off = a->node_off;
+  g->C = a->channels;
+  g->G = a->groups;
+  g->bf16 = a->dtype == DC_BF16;
+  g->act = a->act;
+  g->eps = a->eps;
+  g->X = a->X;
+  g->ldx = a->ldx;
+  g->gamma = a->gamma;
+  g->beta = a->beta;
+  g->mean = a->mean;
+  g->rstd = a->rstd;
+  g->workspace = static_cast<char*>(a->workspace);
+  g->status = ctx->status;
+  g->n_cu = ctx->n_cu;
+  if (!backward) {
+    g->Y = a->Y;
+    g->ldy = a->ldy;
+    return DC_OK;
+  }
+  g->kept = kept_view(a->kept);
+  g->dY = a->dY;
+  g->lddy = a->lddy;
+  g->dRes = a->dres;
+  g->lddres = a->lddres;
+  g->dX = a->dX;
+  g->lddx = a->lddx;
+  g->dgamma = a->dgamma;
+  g->dbeta = a->dbeta;
+  return DC_OK;
+}
+}  // namespace
+
+dc_status dc_keep_rows(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                       const dc_kept_rows* out, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  if (rows > 0 && !x) return fail(ctx, DC_ERR_INVALID_ARG, "null x");
+  return keep_or_restore(ctx, dtype, rows, cols, x, nullptr, ldx, out, static_cast<hipStream_t>(stream));
+}
+
+dc_status dc_restore_rows(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols, const dc_kept_rows* in, void* x,
+                          int64_t ldx, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  return keep_or_restore(ctx, dtype, rows, cols, nullptr, x, ldx, in, static_cast<hipStream_t>(stream));
+}
+
+dc_status dc_dense(dc_ctx* ctx, const dc_dense_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  if (!args) return fail(ctx, DC_ERR_INVALID_ARG, "null arguments");
+  const dc_dense_args& a = *args;
+  dc_status st = dense_shape_check(ctx, a.dtype, a.act, a.rows, a.in, a.out);
+  const int es = a.dtype == DC_BF16 ? 2 : 4;
+  if (st == DC_OK) st = array_check(ctx, a.X, a.ldx, a.rows, a.in, es, "X");
+  if (st == DC_OK) st = array_check(ctx, a.W, a.ldw, a.in, a.out, es, "W");
+  if (st == DC_OK) st = array_check(ctx, a.Y, a.ldy, a.rows, a.out, es, "Y");
+  if (st == DC_OK && a.residual) st = array_check(ctx, a.residual, a.ld_residual, a.rows, a.out, es, "residual");
+  if (st == DC_OK && a.Z) st = array_check(ctx, a.Z, a.ldz, a.rows, a.out, es, "Z");
+  if (st != DC_OK || a.rows == 0) return st;
+  if (!at(a.bias, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "bias is not aligned to its elements");
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  DenseArgs d{};
+  d.rows = a.rows;
+  d.d = a.in;
+  d.nseg = 1;
+  d.N = a.out;
+  d.bf16 = a.dtype == DC_BF16;
+  d.act = a.act;
+  d.X[0] = a.X;
+  d.ldx = a.ldx;
+  d.W = a.W;
+  d.ldw = a.ldw;
+  d.bias = a.bias;
+  d.R = a.residual;
+  d.ldr = a.ld_residual;
+  d.Z = a.Z;
+  d.ldz = a.ldz;
+  d.Y = a.Y;
+  d.ldy = a.ldy;
+  d.n_cu = ctx->n_cu;
+  return enqueue_result(ctx, launch_dense(d, static_cast<hipStream_t>(stream)), "dense layer launch");
+}
+
+size_t dc_dense_backward_bytes(const dc_ctx* ctx, int64_t rows, int32_t in, int32_t out) {
+  if (!ctx || rows < 0 || rows > kRowsMost || in < 1 || out < 1 || in > 65536 || out > 65536) return 0;
+  return dense_back_floats(rows, in, out, ctx->n_cu) * sizeof(float);
+}
+
+dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  if (!args) return fail(ctx, DC_ERR_INVALID_ARG, "null arguments");
+  const dc_dense_backward_args& a = *args;
+  dc_status st = dense_shape_check(ctx, a.dtype, a.act, a.rows, a.in, a.out);
+  const int es = a.dtype == DC_BF16 ? 2 : 4;
+  if (st == DC_OK) st = array_check(ctx, a.dY, a.lddy, a.rows, a.out, es, "dY");
+  if (st == DC_OK && a.act != DC_ACT_NONE) st = array_check(ctx, a.Z, a.ldz, a.rows, a.out, es, "Z");
+  if (st == DC_OK && a.dW) st = a.kept ? kept_check(ctx, a.kept, a.rows, a.in) : array_check(ctx, a.X, a.ldx, a.rows, a.in, es, "X");
+  if (st == DC_OK && a.dW) st = array_check(ctx, a.dW, a.lddw, a.in, a.out, es, "dW");
+  if (st == DC_OK && a.dX) st = array_check(ctx, a.dX, a.lddx, a.rows, a.in, es, "dX");
+  if (st == DC_OK && a.dX) st = array_check(ctx, a.W, a.ldw, a.in, a.out, es, "W");
+  if (st != DC_OK) return st;
+  if (!at(a.db, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "db is not aligned to its elements");
+  if (a.dW || a.db) {
+    if (!a.workspace || a.workspace_bytes < dc_dense_backward_bytes(ctx, a.rows, a.in, a.out))
+      return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_dense_backward_bytes");
+    if (!at(a.workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+  }
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  DenseBackArgs d{};
+  d.rows = a.rows;
+  d.d = a.in;
+  d.nseg = 1;
+  d.N = a.out;
+  d.bf16 = a.dtype == DC_BF16;
+  d.act = a.act;
+  d.dY = a.dY;
+  d.lddy = a.lddy;
+  d.Z = a.act == DC_ACT_NONE ? nullptr : a.Z;
+  d.ldz = a.ldz;
+  d.X[0] = a.X;
+  d.ldx = a.ldx;
+  d.kept = kept_view(a.dW ? a.kept : nullptr);
+  d.W = a.W;
+  d.ldw = a.ldw;
+  d.dX = a.dX;
+  d.lddx = a.lddx;
+  d.dW = a.dW;
+  d.lddw = a.lddw;
+  d.db = a.db;
+  d.workspace = static_cast<float*>(a.workspace);
+  d.n_cu = ctx->n_cu;
+  return enqueue_result(ctx, launch_dense_back(d, static_cast<hipStream_t>(stream)), "dense layer gradient launch");
+}
+
+size_t dc_graph_norm_bytes(const dc_ctx* ctx, int64_t rows, int32_t n_graphs, int32_t channels, int32_t groups, int32_t backward) {
+  if (!ctx || rows < 0 || rows > kRowsMost || n_graphs < 0 || channels < 1 || channels > 8192 || groups < 1 || channels % groups)
+    return 0;
+  return graph_norm_bytes(rows, n_graphs, channels, groups, backward != 0, ctx->n_cu);
+}
+
+dc_status dc_graph_norm(dc_ctx* ctx, const dc_graph_norm_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  GraphNormArgs g;
+  const dc_status st = graph_norm_check(ctx, args, false, &g);
+  if (st != DC_OK || g.n_graphs == 0) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  return enqueue_result(ctx, launch_graph_norm(g, static_cast<hipStream_t>(stream)), "graph norm launch");
+}
+
+dc_status dc_graph_norm_backward(dc_ctx* ctx, const dc_graph_norm_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  GraphNormArgs g;
+  const dc_status st = graph_norm_check(ctx, args, true, &g);
+  if (st != DC_OK) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  return enqueue_result(ctx, launch_graph_norm_back(g, static_cast<hipStream_t>(stream)), "graph norm gradient launch");
 }
 
 dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* head, void* stream) {

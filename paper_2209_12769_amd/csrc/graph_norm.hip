@@ -1,0 +1,701 @@
+// Norm over the rows of each graph with an activation, and its gradient (gfx950): the channels of a row are in G groups
+// of cg = C / G; a statistic runs over a graph's rows and a group's channels, m = rows * cg values.
+//
+//   forward   mu = mean x, v = mean (x - mu)^2, r = 1 / sqrt(v + eps);  y = act(gamma (x - mu) r + beta)
+//   backward  xh = (x - mu) r, dz = dy act'(gamma xh + beta), u = gamma dz, s1 = mean u, s2 = mean u xh;
+//             dx = r (u - s1 - xh s2) [+ dres];  dgamma = sum over rows of dz xh, dbeta = sum of dz
+//
+// Bound by memory, x read once and y written once: a workgroup takes a graph (or a slab of its channels, whole groups and
+// whole cache lines), holds its rows in LDS between the sums and the second pass and reads again only what
+// does not fit.  Sums are formed in 64 bits (v as mean x^2 - mu^2: exact enough for any offset that fp32 values can
+// have next to their spread), three instructions a value, which the loads hide.
+// Graphs longer than a.long_rows would keep one workgroup busy while the others are done: their rows are dealt in chunks
+// to three kernels (sums of a chunk; sums of a graph; second pass), the short graphs' kernel leaves them out.
+#include "operators.h"
+
+namespace dc {
+namespace {
+
+typedef unsigned short u16;
+
+template <typename T, int kV>
+struct alignas(sizeof(T) * kV) Vec {
+  T v[kV];
+};
+struct Kept8 {};       // x as codes
+
+template <typename T, int kV>
+struct Held {          // kV values as they come from memory
+  Vec<T, kV> v;
+};
+template <int kV>
+struct Held<Kept8, kV> {
+  Vec<signed char, kV> v;
+  unsigned char e;
+};
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(u16 x) { return __uint_as_float((unsigned)x << 16); }
+__device__ __forceinline__ void narrow(float x, float& y) { y = x; }
+__device__ __forceinline__ void narrow(float x, u16& y) { y = to_bf16(x); }
+
+struct Norm {
+  GraphNormArgs a;
+  int cg;                  // channels per group
+  int slab;                // channels per slab: whole groups
+  int nslab;
+  int lanes;               // threads per row of a slab: a power of two
+  int held;                // row steps of a thread that stay in LDS
+  long long long_rows;     // graphs with more rows are left to the chunk kernels
+  int chunk_rows;
+  double2* part;           // [chunks + graphs][G] sums of a chunk's rows of a graph
+  float2* means;           // [graphs][G] s1, s2 of the long graphs (backward)
+  float* cols;             // [column blocks][2 C] parts of dgamma | dbeta
+  int col_block0;          // first column block of this launch
+};
+
+template <typename T, int kV>
+__device__ __forceinline__ void hold(Held<T, kV>& h, const Norm& n, long long row, int c) {
+  h.v = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.X) + row * n.a.ldx + c);
+}
+template <int kV>
+__device__ __forceinline__ void hold(Held<Kept8, kV>& h, const Norm& n, long long row, int c) {
+  h.v = *reinterpret_cast<const Vec<signed char, kV>*>(n.a.kept.code + row * n.a.kept.ld_code + c);
+  h.e = n.a.kept.exponent[row * n.a.kept.ld_exponent + c / kKeptBlock];
+}
+template <typename T, int kV>
+__device__ __forceinline__ void values(float (&x)[kV], const Held<T, kV>& h) {
+#pragma unroll
+  for (int k = 0; k < kV; ++k) x[k] = widen(h.v.v[k]);
+}
+template <int kV>
+__device__ __forceinline__ void values(float (&x)[kV], const Held<Kept8, kV>& h) {
+  const float s = kept_scale(h.e);
+#pragma unroll
+  for (int k = 0; k < kV; ++k) x[k] = (float)h.v.v[k] * s;
+}
+
+struct Rows {
+  long long lo, hi;
+  bool ok;
+};
+// The rows of graph g; offsets that do not ascend inside the arrays are reported, and the graph is left alone.
+__device__ __forceinline__ Rows rows_of(const GraphNormArgs& a, int g) {
+  Rows r;
+  r.lo = a.node_off[g];
+  r.hi = a.node_off[g + 1];
+  r.ok = r.lo >= 0 && r.hi >= r.lo && r.hi <= a.rows;
+  if (!r.ok && threadIdx.x == 0) {
+    if (a.stop) atomicCAS(&a.status[0], 0, (int)DC_ERR_BAD_GRAPH);
+    atomicCAS(&a.status[1], 0, (int)DC_ERR_BAD_GRAPH);
+  }
+  return r;
+}
+__device__ __forceinline__ int graphs_of(const GraphNormArgs& a) {
+  return a.n_graphs_dev ? min(a.n_graphs_dev[0], a.n_graphs) : a.n_graphs;
+}
+
+template <int kV>
+struct Affine {
+  float gamma[kV], beta[kV];
+};
+template <int kV>
+__device__ __forceinline__ Affine<kV> affine_at(const GraphNormArgs& a, int c) {
+  Affine<kV> f;
+#pragma unroll
+  for (int k = 0; k < kV; ++k) {
+    f.gamma[k] = a.gamma ? a.gamma[c + k] : 1.f;
+    f.beta[k] = a.beta ? a.beta[c + k] : 0.f;
+  }
+  return f;
+}
+
+template <int kV>
+__device__ __forceinline__ void activate(float (&z)[kV], int act) {
+  switch (act) {
+    case DC_ACT_RELU:
+#pragma unroll
+      for (int k = 0; k < kV; ++k) z[k] = activation(z[k], DC_ACT_RELU);
+      break;
+    case DC_ACT_GELU:
+#pragma unroll
+      for (int k = 0; k < kV; ++k) z[k] = activation(z[k], DC_ACT_GELU);
+      break;
+    case DC_ACT_SILU:
+#pragma unroll
+      for (int k = 0; k < kV; ++k) z[k] = activation(z[k], DC_ACT_SILU);
+      break;
+    default: break;
+  }
+}
+// dy becomes dz.
+template <int kV>
+__device__ __forceinline__ void slope(float (&dy)[kV], const float (&xh)[kV], const Affine<kV>& f, int act) {
+  switch (act) {
+    case DC_ACT_RELU:
+#pragma unroll
+      for (int k = 0; k < kV; ++k) dy[k] *= activation_slope(fmaf(f.gamma[k], xh[k], f.beta[k]), DC_ACT_RELU);
+      break;
+    case DC_ACT_GELU:
+#pragma unroll
+      for (int k = 0; k < kV; ++k) dy[k] *= activation_slope(fmaf(f.gamma[k], xh[k], f.beta[k]), DC_ACT_GELU);
+      break;
+    case DC_ACT_SILU:
+#pragma unroll
+      for (int k = 0; k < kV; ++k) dy[k] *= activation_slope(fmaf(f.gamma[k], xh[k], f.beta[k]), DC_ACT_SILU);
+      break;
+    default: break;
+  }
+}
+
+// What a row's vector adds to the two sums.
+template <bool kBack, int kV>
+__device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x)[kV], float (&dy)[kV], float mu, float r,
+                                         const Affine<kV>& f, int act, float (&dg)[kV], float (&db)[kV]) {
+  if constexpr (!kBack) {
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      const double d = (double)x[k];
+      s1 += d;
+      s2 = fma(d, d, s2);
+    }
+  } else {
+    float xh[kV];
+#pragma unroll
+    for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
+    slope<kV>(dy, xh, f, act);
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      const float u = f.gamma[k] * dy[k];
+      s1 += (double)u;
+      s2 = fma((double)u, (double)xh[k], s2);
+      dg[k] = fmaf(dy[k], xh[k], dg[k]);
+      db[k] += dy[k];
+    }
+  }
+}
+
+// Sums over the workgroup by group.  Threads: `lanes` per row, of which `used` hold one vector each (gv vectors per group);
+// every thread gives its two sums and gets its group's totals.  red: 2 * blockDim.x doubles.
+__device__ __forceinline__ void group_sums(double& s1, double& s2, double2* red, int lanes, int used, int gv) {
+  const int t = threadIdx.x, T = blockDim.x;
+  for (int o = lanes; o < 64; o <<= 1) {               // the rows of a wave
+    s1 += __shfl_xor(s1, o, 64);
+    s2 += __shfl_xor(s2, o, 64);
+  }
+  // one entry per wave (or row, where a row takes several waves) and lane
+  const int width = lanes > 64 ? lanes : 64, parts = T / width, lane = t & (lanes - 1);
+  __syncthreads();                                     // the last totals have been read
+  if (lanes > 64 || (t & 63) < lanes) red[t / width * lanes + lane] = make_double2(s1, s2);
+  __syncthreads();
+  if (parts > 1) {
+    if (t < used) {
+      double2 v = red[t];
+      for (int p = 1; p < parts; ++p) {
+        const double2 w = red[p * lanes + t];
+        v.x += w.x;
+        v.y += w.y;
+      }
+      red[t] = v;
+    }
+    __syncthreads();
+  }
+  if (gv > 1) {
+    if (t < used && t % gv == 0) {
+      double2 v = red[t];
+      for (int i = 1; i < gv; ++i) {
+        const double2 w = red[t + i];
+        v.x += w.x;
+        v.y += w.y;
+      }
+      red[t] = v;
+    }
+    __syncthreads();
+  }
+  const double2 v = red[lane < used ? lane / gv * gv : 0];
+  s1 = v.x;
+  s2 = v.y;
+}
+
+// The second pass of one vector.
+template <typename T, int kV, bool kBack>
+__device__ __forceinline__ void finish(const Norm& n, const float (&x)[kV], float (&dy)[kV], long long row, int c, float mu, float r,
+                                       float s1, float s2, const Affine<kV>& f) {
+  Vec<T, kV> o;
+  float xh[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
+  if constexpr (!kBack) {
+#pragma unroll
+    for (int k = 0; k < kV; ++k) xh[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
+    activate<kV>(xh, n.a.act);
+#pragma unroll
+    for (int k = 0; k < kV; ++k) narrow(xh[k], o.v[k]);
+    *reinterpret_cast<Vec<T, kV>*>(static_cast<T*>(n.a.Y) + row * n.a.ldy + c) = o;
+  } else {
+    slope<kV>(dy, xh, f, n.a.act);
+    Vec<T, kV> add{};
+    if (n.a.dRes) add = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.dRes) + row * n.a.lddres + c);
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      float d = r * (f.gamma[k] * dy[k] - s1 - xh[k] * s2);
+      if (n.a.dRes) d += widen(add.v[k]);
+      narrow(d, o.v[k]);
+    }
+    *reinterpret_cast<Vec<T, kV>*>(static_cast<T*>(n.a.dX) + row * n.a.lddx + c) = o;
+  }
+}
+
+template <typename T, typename X, int kV>
+struct Two {
+  Held<X, kV> x;
+  Vec<T, kV> dy;
+};
+template <typename T, typename X, int kV, bool kBack>
+__device__ __forceinline__ void fetch(Two<T, X, kV>& h, const Norm& n, long long row, int c) {
+  hold<>(h.x, n, row, c);
+  if constexpr (kBack) h.dy = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.dY) + row * n.a.lddy + c);
+}
+template <typename T, typename X, int kV, bool kBack>
+__device__ __forceinline__ void open(float (&x)[kV], float (&dy)[kV], const Two<T, X, kV>& h) {
+  values(x, h.x);
+#pragma unroll
+  for (int k = 0; k < kV; ++k) dy[k] = kBack ? widen(h.dy.v[k]) : 0.f;
+}
+
+// Column sums of the workgroup's rows: dg, db of every thread into cols[block][c], [C + c].
+template <int kV>
+__device__ __forceinline__ void column_sums(const Norm& n, double (&dg)[kV], double (&db)[kV], int lanes, int used, int c, int block,
+                                            double2* red) {
+  const int t = threadIdx.x, T = blockDim.x;
+  for (int o = lanes; o < 64; o <<= 1) {
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      dg[k] += __shfl_xor(dg[k], o, 64);
+      db[k] += __shfl_xor(db[k], o, 64);
+    }
+  }
+  const int width = lanes > 64 ? lanes : 64, parts = T / width, lane = t & (lanes - 1);
+  float* out = n.cols + (size_t)block * 2 * n.a.C;
+#pragma unroll
+  for (int k = 0; k < kV; ++k) {
+    __syncthreads();
+    if (lanes > 64 || (t & 63) < lanes) red[t / width * lanes + lane] = make_double2(dg[k], db[k]);
+    __syncthreads();
+    if (t < used) {
+      double s1 = 0.0, s2 = 0.0;
+      for (int p = 0; p < parts; ++p) {
+        s1 += red[p * lanes + t].x;
+        s2 += red[p * lanes + t].y;
+      }
+      out[c + k] = (float)s1;
+      out[n.a.C + c + k] = (float)s2;
+    }
+  }
+}
+
+// Steps u of a group of kStep row steps from i on: rows first + (i + u) * step below end.
+constexpr int kStep = 4;
+
+// One workgroup per (graph, slab), the slab fixed.  The first n.held row steps of every thread stay in LDS.
+template <typename T, typename X, int kV, int kThreads, bool kBack>
+__global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
+  if (n.a.stop && n.a.stop[0] != 0) return;
+  typedef Two<T, X, kV> Item;
+  extern __shared__ char lds[];
+  double2* red = reinterpret_cast<double2*>(lds);
+  const int slab = blockIdx.x % n.nslab, t = threadIdx.x;
+  Item* mine = reinterpret_cast<Item*>(lds + kThreads * sizeof(double2)) + t;
+  const int c0 = slab * n.slab, width = min(n.slab, n.a.C - c0);
+  const int used = width / kV, lane = t & (n.lanes - 1), rl = t / n.lanes, step = kThreads / n.lanes, gv = n.cg / kV;
+  const bool in = lane < used;
+  const int c = c0 + lane * kV, group = in ? c / n.cg : 0;
+  const Affine<kV> f = affine_at<kV>(n.a, in ? c : c0);
+  double dgs[kV], dbs[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) dgs[k] = dbs[k] = 0.0;
+  const int ng = graphs_of(n.a);
+  for (int g = blockIdx.x / n.nslab; g < ng; g += gridDim.x / n.nslab) {
+    const Rows r = rows_of(n.a, g);
+    if (!r.ok || r.hi - r.lo > n.long_rows) continue;
+    const double m = (double)(r.hi - r.lo) * n.cg;
+    float mu = 0.f, rs = 0.f, s1f = 0.f, s2f = 0.f;
+    if (kBack) {
+      mu = n.a.mean[(size_t)g * n.a.G + group];
+      rs = n.a.rstd[(size_t)g * n.a.G + group];
+    }
+    double s1 = 0.0, s2 = 0.0;
+    float dg[kV], db[kV];
+#pragma unroll
+    for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
+    const long long r0 = r.lo + rl;
+    const int count = in && r0 < r.hi ? (int)((r.hi - r0 + step - 1) / step) : 0;      // row steps of this thread
+    for (int i = 0; i < count; i += kStep) {
+      Item h[kStep];
+#pragma unroll
+      for (int u = 0; u < kStep; ++u)
+        if (i + u < count) fetch<T, X, kV, kBack>(h[u], n, r0 + (long long)(i + u) * step, c);
+#pragma unroll
+      for (int u = 0; u < kStep; ++u)
+        if (i + u < count) {
+          if (i + u < n.held) mine[(i + u) * kThreads] = h[u];
+          float x[kV], dy[kV];
+          open<T, X, kV, kBack>(x, dy, h[u]);
+          add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+        }
+    }
+    group_sums(s1, s2, red, n.lanes, used, gv);
+    if constexpr (!kBack) {
+      const double mean = m > 0 ? s1 / m : 0.0, var = m > 0 ? s2 / m - mean * mean : 0.0;
+      mu = (float)mean;
+      rs = (float)(1.0 / sqrt((var > 0.0 ? var : (var != var ? var : 0.0)) + (double)n.a.eps));
+      if (in && rl == 0 && lane % gv == 0) {
+        n.a.mean[(size_t)g * n.a.G + group] = mu;
+        n.a.rstd[(size_t)g * n.a.G + group] = rs;
+      }
+    } else {
+      s1f = m > 0 ? (float)(s1 / m) : 0.f;
+      s2f = m > 0 ? (float)(s2 / m) : 0.f;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) {
+        dgs[k] += (double)dg[k];
+        dbs[k] += (double)db[k];
+      }
+    }
+    for (int i = 0; i < count; i += kStep) {
+      Item h[kStep];
+#pragma unroll
+      for (int u = 0; u < kStep; ++u)
+        if (i + u < count) {
+          if (i + u < n.held) h[u] = mine[(i + u) * kThreads];
+          else fetch<T, X, kV, kBack>(h[u], n, r0 + (long long)(i + u) * step, c);
+        }
+#pragma unroll
+      for (int u = 0; u < kStep; ++u)
+        if (i + u < count) {
+          float x[kV], dy[kV];
+          open<T, X, kV, kBack>(x, dy, h[u]);
+          finish<T, kV, kBack>(n, x, dy, r0 + (long long)(i + u) * step, c, mu, rs, s1f, s2f, f);
+        }
+    }
+  }
+  if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
+}
+
+// ---- long graphs: rows in chunks ----
+// The last graph that starts at or before row v; offsets that do not ascend give some graph, whose rows are looked at.
+__device__ __forceinline__ int graph_at(const int* off, int ng, long long v) {
+  int lo = 0, hi = ng;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+// A long graph has more rows than a chunk, so that a chunk meets at most two: those of its first and of its last row.
+struct Segment {
+  int g;
+  long long lo, hi;        // rows of the chunk that belong to graph g; lo >= hi: none
+  double m;
+};
+__device__ __forceinline__ Segment segment_of(const Norm& n, int ng, long long chunk, int which) {
+  Segment s{0, 0, 0, 0.0};
+  const long long c0 = chunk * n.chunk_rows;
+  long long c1 = c0 + n.chunk_rows;
+  if (c1 > n.a.rows) c1 = n.a.rows;
+  if (ng <= 0 || c0 >= c1) return s;
+  const int first = graph_at(n.a.node_off, ng, c0), last = graph_at(n.a.node_off, ng, c1 - 1);
+  if (which == 1 && last == first) return s;
+  s.g = which == 0 ? first : last;
+  const Rows r = rows_of(n.a, s.g);
+  if (!r.ok || r.hi - r.lo <= n.long_rows) return s;
+  s.lo = r.lo > c0 ? r.lo : c0;
+  s.hi = r.hi < c1 ? r.hi : c1;
+  s.m = (double)(r.hi - r.lo) * n.cg;
+  return s;
+}
+
+constexpr int kChunkThreads = 1024;
+
+template <typename T, typename X, int kV, bool kBack>
+__global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n) {
+  if (n.a.stop && n.a.stop[0] != 0) return;
+  __shared__ double2 red[kChunkThreads];
+  const int slab = blockIdx.x % n.nslab, t = threadIdx.x;
+  const int c0 = slab * n.slab, width = min(n.slab, n.a.C - c0);
+  const int used = width / kV, lane = t & (n.lanes - 1), rl = t / n.lanes, step = kChunkThreads / n.lanes, gv = n.cg / kV;
+  const bool in = lane < used;
+  const int c = c0 + lane * kV, group = in ? c / n.cg : 0;
+  const Affine<kV> f = affine_at<kV>(n.a, in ? c : c0);
+  double dgs[kV], dbs[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) dgs[k] = dbs[k] = 0.0;
+  const int ng = graphs_of(n.a);
+  const long long nchunk = (n.a.rows + n.chunk_rows - 1) / n.chunk_rows;
+  for (long long chunk = blockIdx.x / n.nslab; chunk < nchunk; chunk += gridDim.x / n.nslab)
+    for (int which = 0; which < 2; ++which) {
+      const Segment seg = segment_of(n, ng, chunk, which);
+      if (seg.lo >= seg.hi) continue;
+      float mu = 0.f, rs = 0.f;
+      if (kBack) {
+        mu = n.a.mean[(size_t)seg.g * n.a.G + group];
+        rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
+      }
+      double s1 = 0.0, s2 = 0.0;
+      float dg[kV], db[kV];
+#pragma unroll
+      for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
+      if (in)
+        for (long long row = seg.lo + rl; row < seg.hi; row += step) {
+          Two<T, X, kV> w;
+          fetch<T, X, kV, kBack>(w, n, row, c);
+          float x[kV], dy[kV];
+          open<T, X, kV, kBack>(x, dy, w);
+          add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+        }
+      group_sums(s1, s2, red, n.lanes, used, gv);
+      if (in && rl == 0 && lane % gv == 0) n.part[(size_t)(chunk + seg.g) * n.a.G + group] = make_double2(s1, s2);
+#pragma unroll
+      for (int k = 0; k < kV; ++k) {
+        dgs[k] += (double)dg[k];
+        dbs[k] += (double)db[k];
+      }
+    }
+  if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
+}
+
+// The sums of a long graph: a wave looks at 64 graphs and takes the long ones of them, one after another, its lanes over the chunks.
+template <bool kBack>
+__global__ __launch_bounds__(256) void long_sums_kernel(const Norm n) {
+  if (n.a.stop && n.a.stop[0] != 0) return;
+  const int ng = graphs_of(n.a), lane = threadIdx.x & 63;
+  const int nw = gridDim.x * 4;
+  for (int g0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; g0 < ng; g0 += nw * 64) {
+    long long lo = 0, hi = 0;
+    if (g0 + lane < ng) {
+      lo = n.a.node_off[g0 + lane];
+      hi = n.a.node_off[g0 + lane + 1];
+    }
+    const bool mine = lo >= 0 && hi <= n.a.rows && hi - lo > n.long_rows;
+    for (unsigned long long todo = __ballot(mine); todo != 0; todo &= todo - 1) {
+      const int l = __ffsll(todo) - 1, g = g0 + l;
+      const long long a = __shfl(lo, l, 64), b = __shfl(hi, l, 64);
+      const long long k0 = a / n.chunk_rows, k1 = (b - 1) / n.chunk_rows;
+      const double m = (double)(b - a) * n.cg;
+      for (int q = 0; q < n.a.G; ++q) {
+        double s1 = 0.0, s2 = 0.0;
+        for (long long k = k0 + lane; k <= k1; k += 64) {
+          const double2 p = n.part[(size_t)(k + g) * n.a.G + q];
+          s1 += p.x;
+          s2 += p.y;
+        }
+        for (int o = 32; o > 0; o >>= 1) {
+          s1 += __shfl_xor(s1, o, 64);
+          s2 += __shfl_xor(s2, o, 64);
+        }
+        if (lane != 0) continue;
+        if (kBack) {
+          n.means[(size_t)g * n.a.G + q] = make_float2((float)(s1 / m), (float)(s2 / m));
+        } else {
+          const double mean = s1 / m, var = s2 / m - mean * mean;
+          n.a.mean[(size_t)g * n.a.G + q] = (float)mean;
+          n.a.rstd[(size_t)g * n.a.G + q] =
+              (float)(1.0 / sqrt((var > 0.0 ? var : (var != var ? var : 0.0)) + (double)n.a.eps));
+        }
+      }
+    }
+  }
+}
+
+template <typename T, typename X, int kV, bool kBack>
+__global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm n) {
+  if (n.a.stop && n.a.stop[0] != 0) return;
+  const int slab = blockIdx.x % n.nslab, t = threadIdx.x;
+  const int c0 = slab * n.slab, width = min(n.slab, n.a.C - c0);
+  const int used = width / kV, lane = t & (n.lanes - 1), rl = t / n.lanes, step = kChunkThreads / n.lanes;
+  if (lane >= used) return;
+  const int c = c0 + lane * kV, group = c / n.cg;
+  const Affine<kV> f = affine_at<kV>(n.a, c);
+  const int ng = graphs_of(n.a);
+  const long long nchunk = (n.a.rows + n.chunk_rows - 1) / n.chunk_rows;
+  for (long long chunk = blockIdx.x / n.nslab; chunk < nchunk; chunk += gridDim.x / n.nslab)
+    for (int which = 0; which < 2; ++which) {
+      const Segment seg = segment_of(n, ng, chunk, which);
+      if (seg.lo >= seg.hi) continue;
+      const float mu = n.a.mean[(size_t)seg.g * n.a.G + group], rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
+      const float2 s = kBack ? n.means[(size_t)seg.g * n.a.G + group] : make_float2(0.f, 0.f);
+      for (long long row = seg.lo + rl; row < seg.hi; row += step) {
+        Two<T, X, kV> w;
+        fetch<T, X, kV, kBack>(w, n, row, c);
+        float x[kV], dy[kV];
+        open<T, X, kV, kBack>(x, dy, w);
+        finish<T, kV, kBack>(n, x, dy, row, c, mu, rs, s.x, s.y, f);
+      }
+    }
+}
+
+// dgamma, dbeta = sums of the column blocks in 64 bits, ascending blocks: a wave per 64 columns' chain would be one round
+// trip per block, so a workgroup takes 16 columns with 16 threads each.
+__global__ __launch_bounds__(256) void column_reduce_kernel(const float* __restrict__ cols, int blocks, int C, float* __restrict__ dgamma,
+                                                            float* __restrict__ dbeta, const int* stop) {
+  if (stop && stop[0] != 0) return;
+  __shared__ double red[16][17];
+  const int j = threadIdx.x & 15, p = threadIdx.x >> 4, c = blockIdx.x * 16 + j;
+  double s = 0.0;
+  if (c < 2 * C)
+    for (int b = p; b < blocks; b += 16) s += (double)cols[(size_t)b * 2 * C + c];
+  red[p][j] = s;
+  __syncthreads();
+  if (p == 0 && c < 2 * C) {
+    double v = 0.0;
+    for (int i = 0; i < 16; ++i) v += red[i][j];
+    if (c < C) dgamma[c] = (float)v;
+    else dbeta[c - C] = (float)v;
+  }
+}
+
+constexpr int kChunkRows = 256;
+struct Plan {
+  int threads, slab, nslab, lanes, held;
+  long long long_rows;
+  bool chunks;             // there may be long graphs
+  int blocks, chunk_blocks;    // column blocks: of the short graphs' kernel, of the chunk kernels
+};
+int pow2_at_least(int x) {
+  int p = 1;
+  while (p < x) p <<= 1;
+  return p;
+}
+// Channels per slab: whole groups, at least a cache line of a row.
+int slab_of(int C, int cg, int es) {
+  const long long s = (long long)((128 / es + cg - 1) / cg) * cg;
+  return s >= C ? C : (int)s;
+}
+int blocks_most(int n_cu) { return n_cu * 8; }
+// LDS for rows of a workgroup of 64, 256 or 1024 threads: eight, three or one of them per CU
+int held_bytes(int threads) { return threads == 64 ? 18 * 1024 : (threads == 256 ? 48 * 1024 : 140 * 1024); }
+
+Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item, int n_cu) {
+  Plan p{};
+  const int cg = C / G;
+  const long long want = rows / (n_graphs > 0 ? n_graphs : 1) * 3 / 2;       // a graph of one and a half times the mean
+  // whole rows and the fewest threads that hold it; else slabs
+  p.slab = C;
+  p.lanes = pow2_at_least((C + v - 1) / v);
+  for (p.threads = 64; p.threads < 1024; p.threads *= 4)
+    if (p.lanes <= p.threads && want <= (long long)held_bytes(p.threads) / (p.threads * item) * (p.threads / p.lanes)) break;
+  if (p.threads == 1024 && (p.lanes > 1024 || want > (long long)held_bytes(1024) / (1024 * item) * (1024 / p.lanes))) {
+    p.slab = slab_of(C, cg, es);
+    p.lanes = pow2_at_least((p.slab + v - 1) / v);
+  }
+  p.held = held_bytes(p.threads) / (p.threads * item);
+  p.nslab = (C + p.slab - 1) / p.slab;
+  // twice what a workgroup would have if all had the same
+  const long long share = 2 * rows * p.nslab / n_cu;
+  p.long_rows = share < 1024 ? 1024 : (share > 4096 ? 4096 : share);
+  p.chunks = rows > p.long_rows;
+  const int most = blocks_most(n_cu) / p.nslab > 0 ? blocks_most(n_cu) / p.nslab : 1;
+  p.blocks = n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most;
+  const long long chunks = (rows + kChunkRows - 1) / kChunkRows;
+  p.chunk_blocks = p.chunks ? (int)(chunks < most ? chunks : most) : 0;
+  return p;
+}
+
+template <typename T, typename X, int kV, int kThreads, bool kBack>
+hipError_t run_short(const Norm& n, int blocks, hipStream_t s) {
+  const size_t bytes = kThreads * sizeof(double2) + (size_t)n.held * kThreads * sizeof(Two<T, X, kV>);
+  auto kernel = graph_norm_kernel<T, X, kV, kThreads, kBack>;
+  if (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kernel, dim3(blocks * n.nslab), dim3(kThreads), bytes, s, n);
+  return hipGetLastError();
+}
+
+template <typename T, typename X, int kV, bool kBack>
+hipError_t run(Norm n, hipStream_t s) {
+  const Plan p = plan_of(n.a.rows, n.a.n_graphs, n.a.C, n.a.G, (int)sizeof(T), kV, (int)sizeof(Two<T, X, kV>), n.a.n_cu);
+  n.slab = p.slab;
+  n.nslab = p.nslab;
+  n.lanes = p.lanes;
+  n.held = p.held;
+  n.long_rows = p.long_rows;
+  n.chunk_rows = kChunkRows;
+  char* w = n.a.workspace;
+  if (p.chunks) {
+    n.part = reinterpret_cast<double2*>(w);
+    w += ((size_t)((n.a.rows + kChunkRows - 1) / kChunkRows) + (size_t)n.a.n_graphs + 1) * n.a.G * sizeof(double2);
+    n.means = reinterpret_cast<float2*>(w);
+    if (kBack) w += (size_t)n.a.n_graphs * n.a.G * sizeof(float2);
+  }
+  n.cols = reinterpret_cast<float*>(w);
+  hipError_t e = p.threads == 64    ? run_short<T, X, kV, 64, kBack>(n, p.blocks, s)
+                 : p.threads == 256 ? run_short<T, X, kV, 256, kBack>(n, p.blocks, s)
+                                    : run_short<T, X, kV, 1024, kBack>(n, p.blocks, s);
+  if (e != hipSuccess) return e;
+  if (p.chunks) {
+    n.col_block0 = p.blocks;
+    const dim3 cgrid(p.chunk_blocks * n.nslab);
+    hipLaunchKernelGGL((chunk_sums_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
+    const int waves = (n.a.n_graphs + 63) / 64, lgrid = (waves + 3) / 4 < n.a.n_cu ? (waves + 3) / 4 : n.a.n_cu;
+    hipLaunchKernelGGL((long_sums_kernel<kBack>), dim3(lgrid < 1 ? 1 : lgrid), dim3(256), 0, s, n);
+    hipLaunchKernelGGL((chunk_finish_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
+  }
+  if (kBack && n.a.dgamma)
+    hipLaunchKernelGGL(column_reduce_kernel, dim3((2 * n.a.C + 15) / 16), dim3(256), 0, s, n.cols, p.blocks + p.chunk_blocks, n.a.C,
+                       n.a.dgamma, n.a.dbeta, n.a.stop);
+  return hipGetLastError();
+}
+
+template <typename T, typename X, bool kBack>
+hipError_t dispatch(const GraphNormArgs& a, hipStream_t s) {
+  Norm n{};
+  n.a = a;
+  n.cg = a.C / a.G;
+  auto aligned = [&](const void* p, long long ld, size_t es, int v) {
+    return !p || (ld % v == 0 && reinterpret_cast<size_t>(p) % (es * v) == 0);
+  };
+  // the widest vectors, up to 16 bytes, that no group's end cuts and every row starts on
+  int v = 16 / (int)sizeof(T);
+  for (; v > 1; v >>= 1) {
+    bool ok = n.cg % v == 0 && aligned(a.Y, a.ldy, sizeof(T), v) && aligned(a.dY, a.lddy, sizeof(T), v) &&
+              aligned(a.dX, a.lddx, sizeof(T), v) && aligned(a.dRes, a.lddres, sizeof(T), v);
+    ok = ok && (a.kept.code ? aligned(a.kept.code, a.kept.ld_code, 1, v) : aligned(a.X, a.ldx, sizeof(T), v));
+    if (ok) break;
+  }
+  switch (v) {
+    case 8:
+      if constexpr (sizeof(T) == 2) return run<T, X, 8, kBack>(n, s);
+    case 4: return run<T, X, 4, kBack>(n, s);
+    case 2: return run<T, X, 2, kBack>(n, s);
+    default: return run<T, X, 1, kBack>(n, s);
+  }
+}
+
+}  // namespace
+
+size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
+  // what any vector width and type would need
+  const size_t chunks = (size_t)((rows + kChunkRows - 1) / kChunkRows) + (size_t)n_graphs + 1;
+  size_t b = rows > 1024 ? chunks * G * sizeof(double2) : 0;
+  if (backward) {
+    if (rows > 1024) b += (size_t)n_graphs * G * sizeof(float2);
+    const long long most = blocks_most(n_cu), nc = (rows + kChunkRows - 1) / kChunkRows;
+    b += (size_t)((n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most) + (rows > 1024 ? (nc < most ? nc : most) : 0)) * 2 * C * sizeof(float);
+  }
+  return b;
+}
+
+hipError_t launch_graph_norm(const GraphNormArgs& a, hipStream_t s) {
+  if (a.n_graphs <= 0) return hipSuccess;
+  return a.bf16 ? dispatch<u16, u16, false>(a, s) : dispatch<float, float, false>(a, s);
+}
+
+hipError_t launch_graph_norm_back(const GraphNormArgs& a, hipStream_t s) {
+  if (a.kept.code) return a.bf16 ? dispatch<u16, Kept8, true>(a, s) : dispatch<float, Kept8, true>(a, s);
+  return a.bf16 ? dispatch<u16, u16, true>(a, s) : dispatch<float, float, true>(a, s);
+}
+
+}  // namespace dc

@@ -1,0 +1,142 @@
+// Internal declarations of the operators on rows of a batch: dense layer (dense_layer.hip), norm over the rows of each
+// graph (graph_norm.hip), rows kept in 8 bits (kept_rows.hip), and what they share.
+#pragma once
+#include "common.h"
+
+namespace dc {
+
+// ---- activations, in fp32 ----
+__device__ __forceinline__ float activation(float z, int act) {
+  switch (act) {
+    case DC_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+    case DC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case DC_ACT_SILU: return z / (1.f + expf(-z));
+    default: return z;
+  }
+}
+__device__ __forceinline__ float activation_slope(float z, int act) {
+  switch (act) {
+    case DC_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+    case DC_ACT_GELU: return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * 0.70710678118654752f)));
+    case DC_ACT_SILU: {
+      const float s = 1.f / (1.f + expf(-z));
+      return s * fmaf(z, 1.f - s, 1.f);
+    }
+    default: return 1.f;
+  }
+}
+
+// ---- kept rows: 8-bit codes, one power of two per row and 32 columns ----
+constexpr int kKeptBlock = 32;
+constexpr int kKeptNan = 255;                      // exponent code of a block that holds a number that is not finite
+constexpr int kKeptLeast = -126, kKeptMost = 121;  // exponents: every code times its power of two is a normal, finite number
+// The power of two of an exponent code (127 + exponent); NaN for kKeptNan.
+__device__ __forceinline__ float kept_scale(unsigned code) {
+  return code == kKeptNan ? __uint_as_float(0x7FC00000u) : __uint_as_float(code << 23);
+}
+struct KeptView {
+  const signed char* code;       // [rows, ld_code]
+  const unsigned char* exponent; // [rows, ld_exponent]
+  long long ld_code, ld_exponent;
+};
+
+// ---- dense layer ----
+// Y = act(X W + b) + R on the rows of a batch; X is up to three matrices of d columns side by side (K = nseg * d).
+struct DenseArgs {
+  long long rows;                // or, with nrows, the most rows there can be
+  const int* nrows;              // device row count, or null
+  int d, nseg, N, bf16, act;
+  const void* X[3];
+  long long ldx;
+  const void* W;                 // [K, N]
+  long long ldw;
+  const float* bias;             // or null
+  const void* R;                 // or null
+  long long ldr;
+  void* Z;                       // or null
+  long long ldz;
+  void* Y;
+  long long ldy;
+  const int* stop;               // device word: not 0 = leave everything alone; or null
+  int n_cu;
+};
+hipError_t launch_dense(const DenseArgs& a, hipStream_t s);
+
+// dZ = dY act'(Z); dX = dZ W^T, dW = X^T dZ, db = sum of the rows of dZ.
+struct DenseBackArgs {
+  long long rows;
+  const int* nrows;
+  int d, nseg, N, bf16, act;
+  const void* dY;
+  long long lddy;
+  const void* Z;                 // act other than none
+  long long ldz;
+  const void* X[3];              // null where kept is taken
+  long long ldx;
+  KeptView kept;                 // code == null: X
+  const void* W;
+  long long ldw;
+  void* dX;                      // [rows, K] or null
+  long long lddx;
+  void* dW;                      // [K, N] or null
+  long long lddw;
+  float* db;                     // [N] or null
+  float* workspace;              // dense_back_floats() of them, if dW or db
+  const int* stop;
+  int n_cu;
+};
+size_t dense_back_floats(long long rows, int K, int N, int n_cu);
+hipError_t launch_dense_back(const DenseBackArgs& a, hipStream_t s);
+
+// ---- norm over the rows of each graph ----
+struct GraphNormArgs {
+  long long rows;                // rows of the arrays: a graph that reaches further is malformed
+  int n_graphs;                  // or, with n_graphs_dev, the most there can be
+  const int* n_graphs_dev;
+  const int* node_off;
+  int C, G, bf16, act;
+  float eps;
+  const void* X;                 // null where kept is taken (backward)
+  long long ldx;
+  KeptView kept;
+  const float* gamma;            // or null: 1
+  const float* beta;             // or null: 0
+  float* mean;                   // [n_graphs, G]
+  float* rstd;
+  void* Y;                       // forward
+  long long ldy;
+  const void* dY;                // backward
+  long long lddy;
+  const void* dRes;              // backward: added to dX, or null
+  long long lddres;
+  void* dX;
+  long long lddx;
+  float* dgamma;                 // [C] or null (both or none)
+  float* dbeta;
+  char* workspace;
+  int* status;                   // bad offsets set status[1] (and [0] if stop is taken)
+  const int* stop;
+  int n_cu;
+};
+size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu);
+hipError_t launch_graph_norm(const GraphNormArgs& a, hipStream_t s);
+hipError_t launch_graph_norm_back(const GraphNormArgs& a, hipStream_t s);
+
+// ---- kept rows ----
+struct KeepArgs {
+  long long rows;
+  const int* nrows;
+  int cols, bf16;                // type of x
+  const void* src;               // keep: rows; restore: unused
+  void* dst;                     // restore: rows
+  long long ld;
+  signed char* code;
+  unsigned char* exponent;
+  long long ld_code, ld_exponent;
+  const int* stop;
+  int n_cu;
+};
+hipError_t launch_keep_rows(const KeepArgs& a, hipStream_t s);
+hipError_t launch_restore_rows(const KeepArgs& a, hipStream_t s);
+
+}  // namespace dc
