@@ -413,8 +413,8 @@ dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* h
  * none uses its scratch, so calls on different streams may overlap as long as their arrays and workspaces are their
  * own.  They allocate nothing and do not synchronise, and may be captured into a graph.  Work is enqueued on
  * `stream`, a stream of the context's device, whatever device is current.  An array of outputs may be null where
- * the text says so; rows = 0 is allowed.  Limits: rows and graphs fit in int32, in and out are at most 65536,
- * channels per group at most 1024, channels at most 8192.                                                        */
+ * the text says so; rows = 0 is allowed.  Limits: rows and graphs fit in int32, rows are at most 2^22 elements
+ * apart, in and out are at most 65536, channels per group at most 1024, channels at most 8192.                  */
 typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 3 } dc_activation;
 /* GELU is z (1 + erf(z / sqrt 2)) / 2, SiLU z / (1 + e^-z). */
 
@@ -475,10 +475,10 @@ typedef struct {
   void* dW;             /* [in, out] or null                                          */
   int64_t lddw;
   float* db;            /* [out] or null                                              */
-  void* workspace;      /* dev, dc_dense_backward_bytes() of them, if dW or db        */
+  void* workspace;      /* dev, dc_dense_backward_bytes() of them                     */
   size_t workspace_bytes;
 } dc_dense_backward_args;
-size_t dc_dense_backward_bytes(const dc_ctx* ctx, int64_t rows, int32_t in, int32_t out);
+size_t dc_dense_backward_bytes(const dc_ctx* ctx, int32_t dtype, int32_t act, int64_t rows, int32_t in, int32_t out);
 dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, void* stream);
 
 /* Norm over the rows of each graph (a group norm whose positions are the rows of a graph), with an activation.  The

@@ -151,7 +151,7 @@ def lib():
         L.dc_keep_rows.argtypes = [vp, i32, i64, i32, vp, i64, C.POINTER(DcKeptRows), vp]
         L.dc_restore_rows.argtypes = [vp, i32, i64, i32, C.POINTER(DcKeptRows), vp, i64, vp]
         L.dc_dense.argtypes = [vp, C.POINTER(DcDenseArgs), vp]
-        L.dc_dense_backward_bytes.argtypes = [vp, i64, i32, i32]
+        L.dc_dense_backward_bytes.argtypes = [vp, i32, i32, i64, i32, i32]
         L.dc_dense_backward_bytes.restype = size
         L.dc_dense_backward.argtypes = [vp, C.POINTER(DcDenseBackwardArgs), vp]
         L.dc_graph_norm_bytes.argtypes = [vp, i64, i32, i32, i32, i32]
@@ -299,8 +299,8 @@ def dc_dense(ctx, args: DcDenseArgs, stream: int = 0) -> int:
     return lib().dc_dense(ctx, C.byref(args), stream)
 
 
-def dc_dense_backward_bytes(ctx, rows: int, n_in: int, n_out: int) -> int:
-    return int(lib().dc_dense_backward_bytes(ctx, rows, n_in, n_out))
+def dc_dense_backward_bytes(ctx, dtype: int, act: int, rows: int, n_in: int, n_out: int) -> int:
+    return int(lib().dc_dense_backward_bytes(ctx, dtype, act, rows, n_in, n_out))
 
 
 def dc_dense_backward(ctx, args: DcDenseBackwardArgs, stream: int = 0) -> int:
@@ -664,10 +664,9 @@ class Evaluator:
             a.dW, a.lddw = dw.data_ptr(), n_out
         if db is not None:
             a.db = db.data_ptr()
-        if dw is not None or db is not None:
-            a.workspace_bytes = dc_dense_backward_bytes(self.ctx, rows, n_in, n_out)
-            ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
-            a.workspace = ws.data_ptr()
+        a.workspace_bytes = dc_dense_backward_bytes(self.ctx, a.dtype, a.act, rows, n_in, n_out)
+        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
+        a.workspace = ws.data_ptr()
         self._ok(dc_dense_backward(self.ctx, a, self._stream()), "dc_dense_backward")
         return dx, dw, db
 

@@ -1402,7 +1402,7 @@ dc_status array_check(dc_ctx* ctx, const void* p, int64_t ld, int64_t rows, int3
   if (!p) return fail(ctx, DC_ERR_INVALID_ARG, std::string("null ") + name);
   if (!at(p, bytes)) return fail(ctx, DC_ERR_INVALID_ARG, std::string(name) + " is not aligned to its elements");
   if (ld < cols) return fail(ctx, DC_ERR_INVALID_ARG, std::string(name) + ": rows shorter than their columns");
-  if (ld > (1LL << 40)) return fail(ctx, DC_ERR_UNSUPPORTED, std::string(name) + ": rows too far apart");
+  if (ld > (1LL << 22)) return fail(ctx, DC_ERR_UNSUPPORTED, std::string(name) + ": rows too far apart");
   return DC_OK;
 }
 dc_status kept_check(dc_ctx* ctx, const dc_kept_rows* k, int64_t rows, int32_t cols) {
@@ -1565,9 +1565,11 @@ dc_status dc_dense(dc_ctx* ctx, const dc_dense_args* args, void* stream) {
   return enqueue_result(ctx, launch_dense(d, static_cast<hipStream_t>(stream)), "dense layer launch");
 }
 
-size_t dc_dense_backward_bytes(const dc_ctx* ctx, int64_t rows, int32_t in, int32_t out) {
-  if (!ctx || rows < 0 || rows > kRowsMost || in < 1 || out < 1 || in > 65536 || out > 65536) return 0;
-  return dense_back_floats(rows, in, out, ctx->n_cu) * sizeof(float);
+size_t dc_dense_backward_bytes(const dc_ctx* ctx, int32_t dtype, int32_t act, int64_t rows, int32_t in, int32_t out) {
+  if (!ctx || (dtype != DC_F32 && dtype != DC_BF16) || act < DC_ACT_NONE || act > DC_ACT_SILU || rows < 0 || rows > kRowsMost ||
+      in < 1 || out < 1 || in > 65536 || out > 65536)
+    return 0;
+  return dense_back_floats(rows, in, out, dtype == DC_BF16, act, ctx->n_cu) * sizeof(float);
 }
 
 dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, void* stream) {
@@ -1584,11 +1586,9 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   if (st == DC_OK && a.dX) st = array_check(ctx, a.W, a.ldw, a.in, a.out, es, "W");
   if (st != DC_OK) return st;
   if (!at(a.db, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "db is not aligned to its elements");
-  if (a.dW || a.db) {
-    if (!a.workspace || a.workspace_bytes < dc_dense_backward_bytes(ctx, a.rows, a.in, a.out))
-      return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_dense_backward_bytes");
-    if (!at(a.workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
-  }
+  if (!a.workspace || a.workspace_bytes < dc_dense_backward_bytes(ctx, a.dtype, a.act, a.rows, a.in, a.out))
+    return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_dense_backward_bytes");
+  if (!at(a.workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   DenseBackArgs d{};

@@ -4,14 +4,16 @@
 //   data      dX = dZ W^T, dZ = dY act'(Z) formed as the rows are loaded    contraction over the columns of dY
 //   weights   dW = X^T dZ, db = column sums of dZ                           contraction over the rows, split into slabs
 //
-// All three are tiles of 128 x 128 on the bf16 matrix cores (32 x 32 x 16), operands staged through LDS in the layout
-// that the instruction reads: units of eight consecutive contraction indices (16 bytes).
+// All three are tiles on the bf16 matrix cores (32 x 32 x 16), operands staged through LDS in the layout that the
+// instruction reads: units of eight consecutive contraction indices (16 bytes).
 // fp32: a number is the sum of three bf16 numbers; the six products of pieces with i + j <= 4 are formed (what is left
 // out is below 2^-25 of |x w|), sums of 64 indices go to a total of their own, and every other one is formed negated, so
 // that what the matrix cores drop below an accumulator's 24 bits (always downwards) cancels.  Kept rows are one exact
 // piece: three products instead of six.  Sums that come out not finite in pieces are formed again in fp32.
-// bf16: dZ is rounded to bf16 as an operand (by at most 2^-8 of its size, as dX and dW are rounded by
-// themselves); db is summed from dZ before that rounding, in 64 bits.
+// dZ: with ReLU formed as rows are loaded (a comparison).  The slopes of GELU and SiLU cost some twenty instructions a
+// value and every value is loaded by several tiles, so a pass of its own forms dZ once and leaves it in the workspace.
+// bf16: that dZ is bf16, as the operand has to be (off by at most 2^-8 of its size, as dX and dW are by their own
+// rounding); db is summed from the fp32 values in 64 bits.
 #include "operators.h"
 
 namespace dc {
@@ -28,15 +30,15 @@ struct F32 { static constexpr int kBytes = 4, kPieces = 3; };
 struct Bf16 { static constexpr int kBytes = 2, kPieces = 1; };
 struct Kept { static constexpr int kBytes = 1, kPieces = 1; };
 
-// An operand as it lies in memory: `rows` x `cols`, up to three matrices of d columns side by side; with z the values
-// are p * act'(z).
+// An operand as it lies in memory: `rows` x `cols`, up to three matrices of d columns side by side (one, where d is no
+// multiple of eight); with z (kDz) the values are p where z > 0, else 0.
 struct Source {
   const char* p[3];
   const char* z;
   const unsigned char* exponent;
   long long ld, ldz, ld_exponent;
   long long rows;
-  int cols, d, act;
+  int cols, d;
 };
 
 // kN consecutive columns of one row, as they come from memory
@@ -48,19 +50,24 @@ struct Raw {
   unsigned e;
 };
 
+// Rows may start anywhere an element may: global loads of several words need no more than that on this machine.
+typedef u32x4 u32x4_any __attribute__((aligned(1)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+typedef unsigned u32_any __attribute__((aligned(1)));
+typedef u16 u16_any __attribute__((aligned(1)));
 template <int kBytes>
 __device__ __forceinline__ void read_words(unsigned* w, const char* p) {
   if constexpr (kBytes == 1) w[0] = *reinterpret_cast<const unsigned char*>(p);
-  else if constexpr (kBytes == 2) w[0] = *reinterpret_cast<const u16*>(p);
-  else if constexpr (kBytes == 4) w[0] = *reinterpret_cast<const unsigned*>(p);
+  else if constexpr (kBytes == 2) w[0] = *reinterpret_cast<const u16_any*>(p);
+  else if constexpr (kBytes == 4) w[0] = *reinterpret_cast<const u32_any*>(p);
   else if constexpr (kBytes == 8) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+    const u32x2 v = *reinterpret_cast<const u32x2_any*>(p);
     w[0] = v.x;
     w[1] = v.y;
   } else {
 #pragma unroll
     for (int i = 0; i < kBytes / 16; ++i) {
-      const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
+      const u32x4 v = reinterpret_cast<const u32x4_any*>(p)[i];
       w[4 * i] = v.x;
       w[4 * i + 1] = v.y;
       w[4 * i + 2] = v.z;
@@ -75,52 +82,80 @@ __device__ __forceinline__ float value_of(const unsigned* w, int k, float scale)
   else if constexpr (E::kBytes == 2) return __uint_as_float(k & 1 ? w[k >> 1] & 0xFFFF0000u : w[k >> 1] << 16);
   else return (float)(signed char)(w[k >> 2] >> (8 * (k & 3))) * scale;
 }
+// The matrix of a part, chosen among values: a choice among places would move the arguments to scratch memory.
+__device__ __forceinline__ const char* part_of(const Source& s, int seg) {
+  const size_t p0 = (size_t)s.p[0], p1 = (size_t)s.p[1], p2 = (size_t)s.p[2];
+  return reinterpret_cast<const char*>(seg == 0 ? p0 : (seg == 1 ? p1 : p2));
+}
 template <class E, bool kDz>
 __device__ __forceinline__ float single(const Source& s, long long row, int col) {
   const int seg = col / s.d;
+  const char* p = part_of(s, seg);
   unsigned w[1], z[1];
-  read_words<E::kBytes>(w, s.p[seg] + (row * s.ld + col - seg * s.d) * E::kBytes);
+  read_words<E::kBytes>(w, p + (row * s.ld + col - seg * s.d) * E::kBytes);
   float scale = 1.f;
   if constexpr (E::kBytes == 1) scale = kept_scale(s.exponent[row * s.ld_exponent + col / kKeptBlock]);
   float x = value_of<E>(w, 0, scale);
   if constexpr (kDz) {
     read_words<E::kBytes>(z, s.z + (row * s.ldz + col) * E::kBytes);
-    x *= activation_slope(value_of<E>(z, 0, 1.f), s.act);
+    x = value_of<E>(z, 0, 1.f) > 0.f ? x : 0.f;
   }
   return x;
 }
-// kVec: rows start at, and have a multiple of, whole vectors, and the vector lies inside the matrix; else value by value,
-// zeros behind the last column.
+// kVec: the matrix ends, and its parts meet, between vectors, and the vector lies inside; else the last vector of a row is read
+// value by value, zeros behind the last column.
 template <class E, int kN, bool kDz, bool kVec>
 __device__ __forceinline__ void fetch(Raw<E, kN, kDz>& r, const Source& s, long long row, int col) {
-  if constexpr (kVec) {
-    const int seg = (col >= s.d ? 1 : 0) + (col >= 2 * s.d ? 1 : 0);
-    const char* p = seg == 0 ? s.p[0] : (seg == 1 ? s.p[1] : s.p[2]);
-    read_words<kN * E::kBytes>(r.w, p + (row * s.ld + col - seg * s.d) * E::kBytes);
-    if constexpr (kDz) read_words<kN * E::kBytes>(r.z, s.z + (row * s.ldz + col) * E::kBytes);
-    if constexpr (E::kBytes == 1) r.e = s.exponent[row * s.ld_exponent + col / kKeptBlock];
+  const int seg = (col >= s.d ? 1 : 0) + (col >= 2 * s.d ? 1 : 0), c = col - seg * s.d;
+  const char* p = part_of(s, seg) + (row * s.ld + c) * E::kBytes;
+  const char* z = kDz ? s.z + (row * s.ldz + col) * E::kBytes : nullptr;
+  if constexpr (E::kBytes == 1) r.e = s.exponent[row * s.ld_exponent + min(col, s.cols - 1) / kKeptBlock];
+  if (kVec || c + kN <= s.d) {
+    read_words<kN * E::kBytes>(r.w, p);
+    if constexpr (kDz) read_words<kN * E::kBytes>(r.z, z);
   } else {
 #pragma unroll
     for (int i = 0; i < Raw<E, kN, kDz>::kWords; ++i) {
       r.w[i] = 0;
       if constexpr (kDz) r.z[i] = 0;
     }
-    r.e = 0;
+    constexpr int kPer = 4 / E::kBytes;
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
-      const int c = col + k;
-      if (c >= s.cols) continue;
-      const int seg = (c >= s.d ? 1 : 0) + (c >= 2 * s.d ? 1 : 0);
-      const char* p = seg == 0 ? s.p[0] : (seg == 1 ? s.p[1] : s.p[2]);
+      if (c + k >= s.d) continue;
       unsigned x[1];
-      constexpr int kPer = 4 / E::kBytes;
-      read_words<E::kBytes>(x, p + (row * s.ld + c - seg * s.d) * E::kBytes);
+      read_words<E::kBytes>(x, p + k * E::kBytes);
       r.w[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
       if constexpr (kDz) {
-        read_words<E::kBytes>(x, s.z + (row * s.ldz + c) * E::kBytes);
+        read_words<E::kBytes>(x, z + k * E::kBytes);
         r.z[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
       }
-      if constexpr (E::kBytes == 1) r.e = s.exponent[row * s.ld_exponent + c / kKeptBlock];
+    }
+  }
+}
+// The same at an offset of less than 4 GB from a place that all lanes share; left: columns from there to the end of the row.
+template <class E, int kN, bool kDz, bool kVec>
+__device__ __forceinline__ void fetch_near(Raw<E, kN, kDz>& r, const char* p, const char* z, unsigned off, unsigned offz, int left) {
+  if (kVec || kN <= left) {
+    read_words<kN * E::kBytes>(r.w, p + off);
+    if constexpr (kDz) read_words<kN * E::kBytes>(r.z, z + offz);
+  } else {
+#pragma unroll
+    for (int i = 0; i < Raw<E, kN, kDz>::kWords; ++i) {
+      r.w[i] = 0;
+      if constexpr (kDz) r.z[i] = 0;
+    }
+    constexpr int kPer = 4 / E::kBytes;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      if (k >= left) continue;
+      unsigned x[1];
+      read_words<E::kBytes>(x, p + off + k * E::kBytes);
+      r.w[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
+      if constexpr (kDz) {
+        read_words<E::kBytes>(x, z + offz + k * E::kBytes);
+        r.z[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
+      }
     }
   }
 }
@@ -134,13 +169,13 @@ __device__ __forceinline__ void clear(Raw<E, kN, kDz>& r) {
   r.e = 0;
 }
 template <class E, int kN, bool kDz>
-__device__ __forceinline__ void values(float (&x)[kN], const Raw<E, kN, kDz>& r, int act) {
+__device__ __forceinline__ void values(float (&x)[kN], const Raw<E, kN, kDz>& r) {
   float scale = 1.f;
   if constexpr (E::kBytes == 1) scale = kept_scale(r.e);
 #pragma unroll
   for (int k = 0; k < kN; ++k) {
     x[k] = value_of<E>(r.w, k, scale);
-    if constexpr (kDz) x[k] *= activation_slope(value_of<E>(r.z, k, 1.f), act);
+    if constexpr (kDz) x[k] = value_of<E>(r.z, k, 1.f) > 0.f ? x[k] : 0.f;
   }
 }
 
@@ -180,90 +215,134 @@ __device__ __forceinline__ int unit_at(int r, int c) {
   return line * 8 + (u ^ ((line ^ (line >> 3)) & 7));
 }
 
-constexpr int kTile = 128, kThreads = 256;
+constexpr int kThreads = 256, kTileN = 128;
 
-// A tile of kTile rows (of the product's operand) by KS contraction indices, from memory through registers to LDS.
+// A tile of kR rows (of the product's operand) by KS contraction indices, from memory through registers to LDS.
 // kCols = false: the operand's rows are the rows of the matrix; true: its columns, and the contraction runs over the rows.
-template <class E, bool kCols, bool kDz, int KS, bool kVec>
+template <class E, bool kCols, bool kDz, int kR, int KS, bool kVec>
 struct Stager {
   static constexpr int kP = E::kPieces;
-  static constexpr int kUnits = kTile * KS / 8 / kThreads;      // per thread: 4 or 2
+  static constexpr int kUnits = kR * KS / 8 / kThreads;         // per thread
   static constexpr int kN = kCols ? kUnits : 8;                 // columns per vector
   static constexpr int kRaws = kCols ? 8 : kUnits;
+  static constexpr int kPlane = kR * KS / 8;                    // units per piece
   Raw<E, kN, kDz> raw[kRaws];
 
-  // r0: first row of the tile; k0 .. k_end: contraction indices
-  __device__ __forceinline__ void load(const Source& s, long long r0, long long k0, long long k_end) {
+  // rows: of the operand; r0: first row of the tile; k0 .. k_end: contraction indices.  Past the ends the last ones are read
+  // again, so that no request waits behind a branch: rows are not stored, indices are cleared by mask().
+  __device__ __forceinline__ void load(const Source& s, long long rows, long long r0, long long k0, long long k_end) {
     const int t = threadIdx.x;
     if constexpr (kCols) {
-      constexpr int kBlocks = kTile / kN;
+      constexpr int kBlocks = kR / kN;
       const int c = t / kBlocks;
       int col = (int)r0 + (t % kBlocks) * kN;
-      if constexpr (kVec) col = min(col, s.cols - kN);          // columns behind the last are not stored
+      if constexpr (kVec) col = min(col, s.cols - kN);
+      else col = min(col, s.cols - 1);
       const long long k = k0 + c * 8;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (k + i < k_end) fetch<E, kN, kDz, kVec>(raw[i], s, k + i, col);
-        else clear(raw[i]);
-      }
+      for (int i = 0; i < 8; ++i) fetch<E, kN, kDz, kVec>(raw[i], s, min(k + i, k_end - 1), col);
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
         const int u = t + kThreads * i, r = u / (KS / 8), c = u % (KS / 8);
-        long long row = r0 + r;
-        if (row >= s.rows) row = s.rows - 1;                    // rows behind the last are not stored
         const int k = (int)k0 + c * 8;
-        if (k < k_end) fetch<E, kN, kDz, kVec>(raw[i], s, row, k);
-        else clear(raw[i]);
+        fetch<E, kN, kDz, kVec>(raw[i], s, min(r0 + r, rows - 1), k < k_end ? k : 0);
       }
     }
   }
-  // sums: column sums of the values (kCols), or null
-  __device__ __forceinline__ void store(u32x4* lds, int act, float sign, double* sums) const {
+  // The same from a place that all lanes share: p (and z) at the tile's first row and index; ld, ldz in bytes; rows and
+  // indices from there to the ends.
+  __device__ __forceinline__ void load_near(const char* p, const char* z, unsigned ld, unsigned ldz, int rows, int indices) {
     const int t = threadIdx.x;
     if constexpr (kCols) {
-      constexpr int kBlocks = kTile / kN;
-      const int c = t / kBlocks, r = (t % kBlocks) * kN;
-      float x[8][kN];
+      constexpr int kBlocks = kR / kN;
+      const int c = t / kBlocks * 8, col = min(t % kBlocks * kN, rows - (kVec ? kN : 1));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) values<E, kN, kDz>(x[i], raw[i], act);
-      if (sums) {
+      for (int i = 0; i < 8; ++i)
+        fetch_near<E, kN, false, kVec>(raw[i], p, z, (unsigned)min(c + i, indices - 1) * ld + (unsigned)(col * E::kBytes), 0, rows - col);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const int u = t + kThreads * i;
+        const unsigned r = (unsigned)min(u / (KS / 8), rows - 1);
+        int k = u % (KS / 8) * 8;
+        k = k < indices ? k : 0;
+        fetch_near<E, kN, kDz, kVec>(raw[i], p, z, r * ld + (unsigned)(k * E::kBytes), r * ldz + (unsigned)(k * E::kBytes), indices - k);
+      }
+    }
+  }
+  __device__ __forceinline__ void mask(long long k0, long long k_end) {
+    if (k0 + KS <= k_end) return;
+    const int t = threadIdx.x;
+    if constexpr (kCols) {
+      const long long k = k0 + t / (kR / kN) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + i >= k_end) clear(raw[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+        if (k0 + (t + kThreads * i) % (KS / 8) * 8 >= k_end) clear(raw[i]);
+    }
+  }
+  __device__ __forceinline__ void store(u32x4* lds, float sign) const {
+    const int t = threadIdx.x;
+    if constexpr (kCols) {
+      constexpr int kBlocks = kR / kN;
+      const int c = t / kBlocks, r = (t % kBlocks) * kN;
+      if constexpr (E::kBytes == 2 && !kDz) {          // halves of the words of two rows
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
-          double v = 0.0;
+          u32x4 p;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v += (double)x[i][j];
-          sums[j] += v;
+          for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+          lds[unit_at<KS>(r + j, c)] = p;
         }
-      }
+      } else {
+        float x[8][kN];
 #pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        float y[8];
+        for (int i = 0; i < 8; ++i) values<E, kN, kDz>(x[i], raw[i]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = kP == 1 ? x[i][j] : x[i][j] * sign;
-        u32x4 p[kP];
-        pieces_of<kP>(p, y);
+        for (int j = 0; j < kN; ++j) {
+          float y[8];
 #pragma unroll
-        for (int q = 0; q < kP; ++q) lds[q * kTile * KS / 8 + unit_at<KS>(r + j, c)] = p[q];
+          for (int i = 0; i < 8; ++i) y[i] = kP == 1 ? x[i][j] : x[i][j] * sign;
+          u32x4 p[kP];
+          pieces_of<kP>(p, y);
+#pragma unroll
+          for (int q = 0; q < kP; ++q) lds[q * kPlane + unit_at<KS>(r + j, c)] = p[q];
+        }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
         const int u = t + kThreads * i, r = u / (KS / 8), c = u % (KS / 8);
         u32x4 p[kP];
-        if constexpr (E::kBytes == 2 && !kDz) {
-          p[0] = u32x4{raw[i].w[0], raw[i].w[1], raw[i].w[2], raw[i].w[3]};
-        } else {
-          float x[8];
-          values<E, kN, kDz>(x, raw[i], act);
-          if constexpr (kP > 1)
+        unit(p, raw[i], sign);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] *= sign;
-          pieces_of<kP>(p, x);
-        }
-#pragma unroll
-        for (int q = 0; q < kP; ++q) lds[q * kTile * KS / 8 + unit_at<KS>(r, c)] = p[q];
+        for (int q = 0; q < kP; ++q) lds[q * kPlane + unit_at<KS>(r, c)] = p[q];
       }
+    }
+  }
+  // Adds the columns' values of the tile (kCols).
+  __device__ __forceinline__ void add_columns(double (&sums)[kN]) const {
+    float x[8][kN];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) values<E, kN, kDz>(x[i], raw[i]);
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+      sums[j] += (double)(((x[0][j] + x[1][j]) + (x[2][j] + x[3][j])) + ((x[4][j] + x[5][j]) + (x[6][j] + x[7][j])));
+  }
+  static __device__ __forceinline__ void unit(u32x4 (&p)[kP], const Raw<E, 8, kDz>& raw, float sign) {
+    if constexpr (E::kBytes == 2 && !kDz) {
+      p[0] = u32x4{raw.w[0], raw.w[1], raw.w[2], raw.w[3]};
+    } else {
+      float x[8];
+      values<E, 8, kDz>(x, raw);
+      if constexpr (kP > 1)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] *= sign;
+      pieces_of<kP>(p, x);
     }
   }
 };
@@ -274,22 +353,26 @@ __device__ __forceinline__ f32x16 zero16() {
   for (int v = 0; v < 16; ++v) z[v] = 0.f;
   return z;
 }
+__device__ __forceinline__ f32x16 mfma(const u32x4& b, const u32x4& a, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
 
-// One staged step: acc[i][j] += A (rows 64 wm + 32 i ..) times B (rows 64 wn + 32 j ..).  The small products first.
-template <int kPA, int kPB, int KS>
-__device__ __forceinline__ void multiply(f32x16 (&acc)[2][2], const u32x4* A, const u32x4* B, int wm, int wn) {
-  constexpr int kMost = kPA > kPB ? kPA : kPB, kPlane = kTile * KS / 8;
+// One staged step: acc[i][j] += A (rows a0 + 32 i ..) times B (rows b0 + 32 j ..).  The small products first.
+template <int kPA, int kPB, int KS, int kRA, int kRB, int kI>
+__device__ __forceinline__ void multiply(f32x16 (&acc)[kI][2], const u32x4* A, const u32x4* B, int a0, int b0) {
+  constexpr int kMost = kPA > kPB ? kPA : kPB;
   const int lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
 #pragma unroll
   for (int k = 0; k < KS / 16; ++k) {
-    u32x4 a[kPA][2], b[kPB][2];
+    u32x4 a[kPA][kI], b[kPB][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int p = 0; p < kPA; ++p)
 #pragma unroll
-      for (int p = 0; p < kPA; ++p) a[p][i] = A[p * kPlane + unit_at<KS>(wm * 64 + i * 32 + l32, 2 * k + lh)];
+      for (int i = 0; i < kI; ++i) a[p][i] = A[p * (kRA * KS / 8) + unit_at<KS>(a0 + i * 32 + l32, 2 * k + lh)];
 #pragma unroll
-      for (int p = 0; p < kPB; ++p) b[p][i] = B[p * kPlane + unit_at<KS>(wn * 64 + i * 32 + l32, 2 * k + lh)];
-    }
+    for (int p = 0; p < kPB; ++p)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) b[p][j] = B[p * (kRB * KS / 8) + unit_at<KS>(b0 + j * 32 + l32, 2 * k + lh)];
 #pragma unroll
     for (int sum = kMost - 1; sum >= 0; --sum)
 #pragma unroll
@@ -297,13 +380,24 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[2][2], const u32x4* A, co
         const int q = sum - p;
         if (q < 0 || q >= kPB) continue;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kI; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[q][j]),
-                                                                __builtin_bit_cast(bf16x8, a[p][i]), acc[i][j], 0, 0, 0);
+          for (int j = 0; j < 2; ++j) acc[i][j] = mfma(b[q][j], a[p][i], acc[i][j]);
       }
+    __builtin_amdgcn_sched_barrier(0);                // one index's operands in registers at a time
   }
+}
+template <int kI>
+__device__ __forceinline__ void add_section(f32x16 (&total)[kI][2], f32x16 (&acc)[kI][2], float sign) {
+#pragma unroll
+  for (int i = 0; i < kI; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        total[i][j][v] = fmaf(acc[i][j][v], sign, total[i][j][v]);
+        acc[i][j][v] = 0.f;
+      }
 }
 
 // The part of a 1-D list of tiles that this workgroup takes: a contiguous eighth per XCD.
@@ -327,6 +421,7 @@ struct ProductArgs {
   long long ldz;
   char* Y;
   long long ldy;
+  int vec;               // rows of R, Z and Y start on 16 bytes
   const int* stop;
 };
 
@@ -341,77 +436,312 @@ __device__ __forceinline__ void store_value(char* p, long long i, float x) {
   if constexpr (E::kBytes == 4) reinterpret_cast<float*>(p)[i] = x;
   else reinterpret_cast<u16*>(p)[i] = to_bf16(x);
 }
+// 16 bytes of values
+template <class E>
+__device__ __forceinline__ void store_wide(char* p, long long i, const float (&x)[16 / E::kBytes]) {
+  u32x4 w;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (E::kBytes == 4) w[k] = __float_as_uint(x[k]);
+    else w[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
+  }
+  *reinterpret_cast<u32x4*>(p + i * E::kBytes) = w;
+}
 
-// rows x N outputs, contraction over K columns of a
+// What becomes of 16 / kBytes neighbouring sums z of a row.
+template <class E, bool kDz, bool kColsB>
+__device__ __forceinline__ void finish(const ProductArgs& g, long long row, int col, float (&z)[16 / E::kBytes]) {
+  constexpr int kW = 16 / E::kBytes;
+  if constexpr (E::kPieces > 1) {
+    unsigned bad = 0;
+#pragma unroll
+    for (int k = 0; k < kW; ++k) bad |= !__builtin_isfinite(z[k]) && col + k < g.N ? 1u << k : 0u;
+    for (; bad; bad &= bad - 1) {                      // formed again in fp32
+      const int c = __ffs(bad) - 1;
+      float s = 0.f;
+      for (int i = 0; i < g.K; ++i)
+        s = fmaf(single<E, kDz>(g.a, row, i), kColsB ? single<E, false>(g.b, i, col + c) : single<E, false>(g.b, col + c, i), s);
+#pragma unroll
+      for (int k = 0; k < kW; ++k) z[k] = k == c ? s : z[k];
+    }
+  }
+  if (g.vec && col + kW <= g.N) {
+    unsigned r[4];
+    if (g.R) read_words<16>(r, g.R + (row * g.ldr + col) * E::kBytes);
+    if (g.bias)
+#pragma unroll
+      for (int k = 0; k < kW; ++k) z[k] += g.bias[col + k];
+    if (g.Z) store_wide<E>(g.Z, row * g.ldz + col, z);
+    activate<kW>(z, g.act);
+    if (g.R)
+#pragma unroll
+      for (int k = 0; k < kW; ++k) z[k] += value_of<E>(r, k, 1.f);
+    store_wide<E>(g.Y, row * g.ldy + col, z);
+    return;
+  }
+  if (g.bias)
+#pragma unroll
+    for (int k = 0; k < kW; ++k) z[k] += col + k < g.N ? g.bias[col + k] : 0.f;
+  if (g.Z)
+#pragma unroll
+    for (int k = 0; k < kW; ++k)
+      if (col + k < g.N) store_value<E>(g.Z, row * g.ldz + col + k, z[k]);
+  activate<kW>(z, g.act);
+#pragma unroll
+  for (int k = 0; k < kW; ++k)
+    if (col + k < g.N) {
+      if (g.R) z[k] += load_value<E>(g.R, row * g.ldr + col + k);
+      store_value<E>(g.Y, row * g.ldy + col + k, z[k]);
+    }
+}
+
+// Few rows: a workgroup per 32 x 32 tile, operands straight from memory, the contraction dealt to its four waves in chunks of
+// 16; their sums meet in LDS.  A tile of the kernel below would keep one CU busy while the others have nothing to do.
+constexpr int kFewLd = 36;             // floats from row to row of a tile in LDS
 template <class E, bool kDz, bool kColsB, bool kVec>
-__global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
+__global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs g, int few) {
   if (g.stop && g.stop[0] != 0) return;
-  constexpr int kP = E::kPieces, KS = kP == 1 ? 64 : 32;
-  __shared__ u32x4 A[kP * kTile * KS / 8], B[kP * kTile * KS / 8];
-  if (g.nrows) g.a.rows = g.nrows[0];
-  const long long rows = g.a.rows;
+  constexpr int kP = E::kPieces, kW = 16 / E::kBytes;
+  __shared__ float lds[4 * 32 * kFewLd];
+  const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, l32 = lane & 31, lh = lane >> 5;
+  const int nct = (g.N + 31) >> 5, chunks = (g.K + 15) >> 4;
+  const long long ntiles = ((rows + 31) >> 5) * nct;
+  if (ntiles > few) return;                           // the tiles of product_kernel
+  const float sign = wave & 1 ? -1.f : 1.f;           // what the pieces' sums drop cancels between the waves
+  for (long long tile = blockIdx.x; tile < ntiles; tile += gridDim.x) {
+    const long long m0 = tile / nct * 32, row = min(m0 + l32, rows - 1);
+    const int n0 = (int)(tile % nct) * 32, col = min(n0 + l32, g.N - 1);
+    struct Chunk {
+      Raw<E, 8, kDz> a;
+      Raw<E, kColsB ? 1 : 8, false> b[kColsB ? 8 : 1];
+    };
+    // past the end the last chunk again, so that no request waits behind a branch
+    auto load = [&](Chunk& x, int c) {
+      const int k = min(c, chunks - 1) * 16 + 8 * lh, ka = k < g.K ? k : 0;
+      fetch<E, 8, kDz, kVec>(x.a, g.a, row, ka);
+      if constexpr (kColsB) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) fetch<E, 1, false, true>(x.b[i], g.b, min(k + i, g.K - 1), col);
+      } else {
+        fetch<E, 8, false, kVec>(x.b[0], g.b, col, ka);
+      }
+    };
+    f32x16 acc = zero16();
+    auto step = [&](const Chunk& x, int c) {
+      const int k = c * 16 + 8 * lh;
+      u32x4 a[kP], b[kP];
+      float y[8];
+      values<E, 8, kDz>(y, x.a);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = k + i < g.K ? y[i] : 0.f;
+      pieces_of<kP>(a, y);
+      if constexpr (kColsB) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = value_of<E>(x.b[i].w, 0, 1.f);
+      } else {
+        values<E, 8, false>(y, x.b[0]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = k + i < g.K ? (kP > 1 ? y[i] * sign : y[i]) : 0.f;
+      pieces_of<kP>(b, y);
+#pragma unroll
+      for (int sum = kP - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int p = 0; p <= sum; ++p) acc = mfma(b[sum - p], a[p], acc);
+    };
+    Chunk x0, x1, x2;
+    load(x0, wave);
+    load(x1, wave + 4);
+    load(x2, wave + 8);
+    for (int c = wave; c < chunks; c += 12) {
+      step(x0, c);
+      load(x0, c + 12);
+      if (c + 4 < chunks) step(x1, c + 4);
+      load(x1, c + 16);
+      if (c + 8 < chunks) step(x2, c + 8);
+      load(x2, c + 20);
+    }
+    __syncthreads();                                  // the last tile has been read
+    // register v of a lane: row l32, column 8 (v / 4) + 4 lh + v % 4
+    float* mine = lds + wave * 32 * kFewLd;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) mine[l32 * kFewLd + 8 * q + 4 * lh + v] = acc[4 * q + v];
+    __syncthreads();
+    const int r = t / (32 / kW), c0 = t % (32 / kW) * kW;
+    if (r < 32 && m0 + r < rows && n0 + c0 < g.N) {
+      float z[kW];
+#pragma unroll
+      for (int k = 0; k < kW; ++k) {
+        const float* p = lds + r * kFewLd + c0 + k;
+        const float u0 = p[0], u1 = p[32 * kFewLd], u2 = p[64 * kFewLd], u3 = p[96 * kFewLd];
+        z[k] = kP > 1 ? (u0 - u1) + (u2 - u3) : (u0 + u1) + (u2 + u3);
+      }
+      finish<E, kDz, kColsB>(g, m0 + r, n0 + c0, z);
+    }
+  }
+}
+
+// rows x N outputs, contraction over K columns of a.  Tiles of 64 kI rows x 128 columns, four waves of 32 kI x 64.
+template <class E, bool kDz, bool kColsB, bool kVec, int kI>
+__global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductArgs g, int few) {
+  if (g.stop && g.stop[0] != 0) return;
+  constexpr int kP = E::kPieces, KS = kP == 1 ? 64 : 32, kTileM = 64 * kI, kW = 16 / E::kBytes, kLd = 68;
+  constexpr int kUnitsA = kP * kTileM * KS / 8, kUnitsB = kP * kTileN * KS / 8;
+  constexpr int kEnd = 4 * 32 * kLd * 4 / 16, kLds = kUnitsA + kUnitsB > kEnd ? kUnitsA + kUnitsB : kEnd;
+  __shared__ u32x4 lds[kLds];
+  u32x4 *A = lds, *B = lds + kUnitsA;
+  const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
+  if (((rows + 31) >> 5) * ((g.N + 31) >> 5) <= few) return;      // few_rows_kernel
   const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
-  const int nct = (g.N + kTile - 1) / kTile, steps = (g.K + KS - 1) / KS;
-  const TileRange tr = tiles_of((rows + kTile - 1) / kTile * nct);
+  // the parts of a row one after another, each with steps of its own
+  const int nct = (g.N + kTileN - 1) / kTileN, d = g.a.d, per = (d + KS - 1) / KS, steps = g.K / d * per;
+  const unsigned lda = (unsigned)g.a.ld * E::kBytes, ldz = (unsigned)g.a.ldz * E::kBytes, ldb = (unsigned)g.b.ld * E::kBytes;
+  const TileRange tr = tiles_of((rows + kTileM - 1) / kTileM * nct);
   for (long long tile = tr.first; tile < tr.end; tile += tr.step) {
-    const long long m0 = tile / nct * kTile;
-    const int n0 = (int)(tile % nct) * kTile;
-    f32x16 acc[2][2], total[2][2];
+    const long long m0 = tile / nct * kTileM;
+    const int n0 = (int)(tile % nct) * kTileN;
+    f32x16 acc[kI][2], total[kP > 1 ? kI : 1][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kI; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = total[i][j] = zero16();
-    Stager<E, false, kDz, KS, kVec> sa;
-    Stager<E, kColsB, false, KS, kVec> sb;
-    sa.load(g.a, m0, 0, g.K);
-    sb.load(g.b, n0, 0, g.K);
+      for (int j = 0; j < 2; ++j) {
+        acc[i][j] = zero16();
+        if (kP > 1) total[i][j] = zero16();
+      }
+    Stager<E, false, kDz, kTileM, KS, kVec> sa;
+    Stager<E, kColsB, false, kTileN, KS, kVec> sb;
+    const int mleft = (int)min(rows - m0, (long long)kTileM), nleft = min(g.N - n0, kTileN);
+    auto load = [&](int step) {
+      const int seg = step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS, left = d - k0;
+      sa.load_near(part_of(g.a, seg) + m0 * lda + k0 * E::kBytes, kDz ? g.a.z + m0 * ldz + k0 * E::kBytes : nullptr, lda, ldz, mleft, left);
+      const long long kb = (long long)seg * d + k0;
+      sb.load_near(kColsB ? g.b.p[0] + kb * ldb + n0 * E::kBytes : g.b.p[0] + (long long)n0 * ldb + kb * E::kBytes, nullptr, ldb, 0, nleft, left);
+    };
+    load(0);
     for (int step = 0; step < steps; ++step) {
       const float sign = (step >> 1) & 1 ? -1.f : 1.f;
+      const int at = step % per * KS;
       __syncthreads();
-      sa.store(A, g.a.act, 1.f, nullptr);
-      sb.store(B, 0, sign, nullptr);
+      sa.mask(at, d);
+      sb.mask(at, d);
+      sa.store(A, 1.f);
+      sb.store(B, sign);
       __syncthreads();
-      if (step + 1 < steps) {
-        sa.load(g.a, m0, (step + 1) * KS, g.K);
-        sb.load(g.b, n0, (step + 1) * KS, g.K);
+      if (step + 1 < steps) load(step + 1);
+      multiply<kP, kP, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
+      if constexpr (kP > 1) {
+        if ((step & 1) || step + 1 == steps) add_section<kI>(total, acc, sign);
       }
-      multiply<kP, kP, KS>(acc, A, B, wm, wn);
-      if (kP > 1 && ((step & 1) || step + 1 == steps)) {
+    }
+    __syncthreads();
+    // register v of a lane: row l32, column 8 (v / 4) + 4 lh + v % 4 of a block; through LDS, 32 rows of a wave at a time, so
+    // that a wave reads and writes whole rows of its 64 columns
+    float* end = reinterpret_cast<float*>(lds) + wave * 32 * kLd;
+    for (int part = 0; part < kI; ++part) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < kI; ++i)
+        if (i == part) {
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              total[i][j][v] = fmaf(acc[i][j][v], sign, total[i][j][v]);
-              acc[i][j][v] = 0.f;
+            for (int q = 0; q < 4; ++q) {
+              float4 v;
+              if constexpr (kP > 1) v = make_float4(total[i][j][4 * q], total[i][j][4 * q + 1], total[i][j][4 * q + 2], total[i][j][4 * q + 3]);
+              else v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+              *reinterpret_cast<float4*>(end + l32 * kLd + j * 32 + 8 * q + 4 * lh) = v;
             }
-      }
-    }
-    // register v of a lane: row l32, column 8 (v / 4) + 4 lh + v % 4 of the block
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const long long row = m0 + wm * 64 + i * 32 + l32;
-      if (row >= rows) continue;
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int col = n0 + wn * 64 + j * 32 + 8 * (v / 4) + 4 * lh + v % 4;
-          if (col >= g.N) continue;
-          float z = kP > 1 ? total[i][j][v] : acc[i][j][v];
-          if (kP > 1 && !__builtin_isfinite(z)) {
-            z = 0.f;
-            for (int k = 0; k < g.K; ++k)
-              z = fmaf(single<E, kDz>(g.a, row, k), kColsB ? single<E, false>(g.b, k, col) : single<E, false>(g.b, col, k), z);
-          }
-          if (g.bias) z += g.bias[col];
-          if (g.Z) store_value<E>(g.Z, row * g.ldz + col, z);
-          float y = activation(z, g.act);
-          if (g.R) y += load_value<E>(g.R, row * g.ldr + col);
-          store_value<E>(g.Y, row * g.ldy + col, y);
         }
+      __builtin_amdgcn_wave_barrier();
+      const long long r0 = m0 + wm * 32 * kI + part * 32;
+      const int c0 = lane % (64 / kW) * kW, col = n0 + wn * 64 + c0;
+#pragma unroll 2
+      for (int r = lane / (64 / kW); r < 32; r += kW) {
+        if (r0 + r >= rows || col >= g.N) continue;
+        float z[kW];
+#pragma unroll
+        for (int k = 0; k < kW; k += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(end + r * kLd + c0 + k);
+          z[k] = v.x;
+          z[k + 1] = v.y;
+          z[k + 2] = v.z;
+          z[k + 3] = v.w;
+        }
+        finish<E, kDz, kColsB>(g, r0 + r, col, z);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
+  }
+}
+
+// ---- dZ of the smooth activations ----
+// dz = dy act'(z), and its column sums over the rows of a block: 32 vectors of columns x 8 rows of threads.
+struct SlopeArgs {
+  long long rows;
+  const int* nrows;
+  int N, act;
+  const char* dy;
+  long long lddy;
+  const char* z;
+  long long ldz;
+  char* dz;              // [rows, N]
+  float* part;           // [row blocks][N]
+  int row_blocks;
+  const int* stop;
+};
+template <class E, int kV>
+__global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g) {
+  if (g.stop && g.stop[0] != 0) return;
+  __shared__ double red[8][32 * kV];
+  const long long rows = g.nrows ? g.nrows[0] : g.rows;
+  const int t = threadIdx.x, cb = blockIdx.x / g.row_blocks, rb = blockIdx.x % g.row_blocks;
+  const int col = (cb * 32 + (t & 31)) * kV;
+  double sum[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) sum[k] = 0.0;
+  if (col < g.N)
+    for (long long r = (long long)rb * 8 + (t >> 5); r < rows; r += (long long)g.row_blocks * 16) {
+      unsigned y[2][(kV * E::kBytes + 3) / 4], z[2][(kV * E::kBytes + 3) / 4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {                    // two rows requested together; past the end the last one again
+        const long long row = min(r + (long long)u * g.row_blocks * 8, rows - 1);
+        read_words<kV * E::kBytes>(y[u], g.dy + (row * g.lddy + col) * E::kBytes);
+        read_words<kV * E::kBytes>(z[u], g.z + (row * g.ldz + col) * E::kBytes);
+      }
+      float d[2][kV];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const long long row = r + (long long)u * g.row_blocks * 8;
+#pragma unroll
+        for (int k = 0; k < kV; ++k) d[u][k] = value_of<E>(z[u], k, 1.f);
+        slopes<kV>(d[u], g.act);
+#pragma unroll
+        for (int k = 0; k < kV; ++k) d[u][k] = row < rows ? d[u][k] * value_of<E>(y[u], k, 1.f) : 0.f;
+        if (row < rows) {
+          if constexpr (kV * E::kBytes == 16) {
+            store_wide<E>(g.dz, row * g.N + col, d[u]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < kV; ++k) store_value<E>(g.dz, row * g.N + col + k, d[u][k]);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kV; ++k) sum[k] += (double)(d[0][k] + d[1][k]);
+    }
+  if (!g.part) return;
+#pragma unroll
+  for (int k = 0; k < kV; ++k) red[t >> 5][(t & 31) * kV + k] = sum[k];
+  __syncthreads();
+  for (int i = t; i < 32 * kV; i += 256) {
+    const int c = cb * 32 * kV + i;
+    if (c >= g.N) continue;
+    double s = 0.0;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) s += red[p][i];
+    g.part[(size_t)rb * g.N + c] = (float)s;
   }
 }
 
@@ -425,90 +755,104 @@ struct WeightArgs {
   int sums;              // column sums of dZ are wanted
   const int* stop;
 };
+struct Slab {
+  long long r0, r1;
+};
+__device__ __forceinline__ Slab slab_rows(const WeightArgs& g, long long rows, int slab, int KS) {
+  long long per = (rows + g.S - 1) / g.S;
+  per = (per + KS - 1) / KS * KS;
+  const long long r0 = min((long long)slab * per, rows);
+  return {r0, min(r0 + per, rows)};
+}
+template <class EA, class EB>
+struct WeightShape {
+  static constexpr int KS = EA::kPieces == 1 && EB::kPieces == 1 ? 64 : 32;
+  static constexpr int kI = 2, kTileM = 64 * kI;
+};
 
 template <class EA, class EB, bool kDz, bool kVec>
-__global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
+__global__ __launch_bounds__(kThreads, 2) void weight_kernel(const WeightArgs g) {
   if (g.stop && g.stop[0] != 0) return;
-  constexpr int kPA = EA::kPieces, kPB = EB::kPieces, KS = kPA == 1 && kPB == 1 ? 64 : 32, kHold = 256 / KS;
-  constexpr int kN = kTile * KS / 8 / kThreads;
-  __shared__ u32x4 A[kPA * kTile * KS / 8], B[kPB * kTile * KS / 8];
+  constexpr int kPA = EA::kPieces, kPB = EB::kPieces, KS = WeightShape<EA, EB>::KS, kI = WeightShape<EA, EB>::kI, kHold = 256 / KS;
+  constexpr int kTileM = WeightShape<EA, EB>::kTileM, kN = kTileN * KS / 8 / kThreads;
+  __shared__ u32x4 A[kPA * kTileM * KS / 8], B[kPB * kTileN * KS / 8];
   const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
   const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
-  const int tiles_n = (g.N + kTile - 1) / kTile, tiles_m = max(1, (g.M + kTile - 1) / kTile), ntile = tiles_m * tiles_n;
+  const int tiles_n = (g.N + kTileN - 1) / kTileN, tiles_m = max(1, (g.M + kTileM - 1) / kTileM), ntile = tiles_m * tiles_n;
   // the tiles of a slab read the same rows: they run on one XCD (the grid is ntile * S, S a multiple of eight)
   const int item = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
   const int tile = item % ntile, slab = item / ntile;
-  const int m0 = tile / tiles_n * kTile, n0 = tile % tiles_n * kTile;
-  long long per = (rows + g.S - 1) / g.S;
-  per = (per + KS - 1) / KS * KS;
-  const long long r0 = min((long long)slab * per, rows), r1 = min(r0 + per, rows);
-  const int steps = (int)((r1 - r0 + KS - 1) / KS);
-  f32x16 acc[2][2], total[2][2];
+  const int m0 = tile / tiles_n * kTileM, n0 = tile % tiles_n * kTileN;
+  const Slab sl = slab_rows(g, rows, slab, KS);
+  const int steps = (int)((sl.r1 - sl.r0 + KS - 1) / KS);
+  // fp32: sections of 256 rows into a total of their own, every other one negated, and so is the first of every other slab
+  f32x16 acc[kI][2], total[kPB > 1 ? kI : 1][2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < kI; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = total[i][j] = zero16();
+    for (int j = 0; j < 2; ++j) {
+      acc[i][j] = zero16();
+      if (kPB > 1) total[i][j] = zero16();
+    }
   const bool want_sums = g.sums && m0 == 0;
   double sums[kN];
 #pragma unroll
   for (int j = 0; j < kN; ++j) sums[j] = 0.0;
-  Stager<EA, true, false, KS, kVec> sa;
-  Stager<EB, true, kDz, KS, kVec> sb;
+  Stager<EA, true, false, kTileM, KS, kVec> sa;
+  Stager<EB, true, kDz, kTileN, KS, kVec> sb;
   if (steps > 0) {
-    if (g.M > 0) sa.load(g.a, m0, r0, r1);
-    sb.load(g.b, n0, r0, r1);
+    if (g.M > 0) sa.load(g.a, rows, m0, sl.r0, sl.r1);
+    sb.load(g.b, rows, n0, sl.r0, sl.r1);
   }
   for (int step = 0; step < steps; ++step) {
-    // sections of kHold steps; every other slab begins with the negated sign
     const float sign = ((step / kHold) ^ slab) & 1 ? -1.f : 1.f;
     __syncthreads();
-    if (g.M > 0) sa.store(A, 0, 1.f, nullptr);
-    sb.store(B, g.b.act, sign, want_sums ? sums : nullptr);
+    sa.mask(sl.r0 + (long long)step * KS, sl.r1);
+    sb.mask(sl.r0 + (long long)step * KS, sl.r1);
+    if (g.M > 0) sa.store(A, 1.f);
+    sb.store(B, sign);
+    if (want_sums) sb.add_columns(sums);
     __syncthreads();
     if (step + 1 < steps) {
-      if (g.M > 0) sa.load(g.a, m0, r0 + (long long)(step + 1) * KS, r1);
-      sb.load(g.b, n0, r0 + (long long)(step + 1) * KS, r1);
+      if (g.M > 0) sa.load(g.a, rows, m0, sl.r0 + (long long)(step + 1) * KS, sl.r1);
+      sb.load(g.b, rows, n0, sl.r0 + (long long)(step + 1) * KS, sl.r1);
     }
-    if (g.M > 0) multiply<kPA, kPB, KS>(acc, A, B, wm, wn);
-    if (step % kHold == kHold - 1 || step + 1 == steps) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            total[i][j][v] = fmaf(acc[i][j][v], kPB > 1 ? sign : 1.f, total[i][j][v]);
-            acc[i][j][v] = 0.f;
-          }
+    if (g.M > 0) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
+    if constexpr (kPB > 1) {
+      if (step % kHold == kHold - 1 || step + 1 == steps) add_section<kI>(total, acc, sign);
     }
   }
   float* P = g.part + (size_t)slab * ((size_t)g.M * g.N + g.N);
+  const bool quads = g.N % 4 == 0;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int m = m0 + wm * 64 + i * 32 + l32;
-    if (m >= g.M) continue;
+  for (int i = 0; i < kI; ++i) {
+    const int m = m0 + wm * 32 * kI + i * 32 + l32;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int n = n0 + wn * 64 + j * 32 + 8 * (v / 4) + 4 * lh + v % 4;
-        if (n >= g.N) continue;
-        float z = total[i][j][v];
-        if (kPB > 1 && !__builtin_isfinite(z)) {
-          z = 0.f;
-          for (long long r = r0; r < r1; ++r) z = fmaf(single<EA, false>(g.a, r, m), single<EB, kDz>(g.b, r, n), z);
+      for (int q = 0; q < 4; ++q) {
+        const int n = n0 + wn * 64 + j * 32 + 8 * q + 4 * lh;
+        const f32x16& s = kPB > 1 ? total[kPB > 1 ? i : 0][j] : acc[i][j];
+        float* p = P + (size_t)m * g.N + n;
+        if (m < g.M && n < g.N) {
+          if (quads) {
+            *reinterpret_cast<float4*>(p) = make_float4(s[4 * q], s[4 * q + 1], s[4 * q + 2], s[4 * q + 3]);
+          } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              if (n + v < g.N) p[v] = s[4 * q + v];
+          }
         }
-        P[(size_t)m * g.N + n] = z;
       }
   }
   if (want_sums) {                                   // the same for the whole workgroup
-    __shared__ double red[KS / 8][kTile];
-    constexpr int kBlocks = kTile / kN;
+    __shared__ double red[KS / 8][kTileN];
+    constexpr int kBlocks = kTileN / kN;
 #pragma unroll
     for (int j = 0; j < kN; ++j) red[threadIdx.x / kBlocks][threadIdx.x % kBlocks * kN + j] = sums[j];
     __syncthreads();
     const int n = n0 + (int)threadIdx.x;
-    if (threadIdx.x < kTile && n < g.N) {
+    if (threadIdx.x < kTileN && n < g.N) {
       double v = 0.0;
 #pragma unroll
       for (int c = 0; c < KS / 8; ++c) v += red[c][threadIdx.x];
@@ -517,56 +861,82 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
   }
 }
 
-// dW [M, N] and db [N] = sums of the slabs' parts in 64 bits, ascending slabs.
-template <class E>
-__global__ __launch_bounds__(256) void weight_reduce_kernel(const float* __restrict__ part, int S, long long MN, int N, char* dW,
-                                                            long long lddw, float* __restrict__ db, const int* stop) {
-  if (stop && stop[0] != 0) return;
-  const long long stride = MN + N;
-  const long long first = dW ? 0 : MN, end = db ? stride : MN;
-  for (long long i = first + (long long)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (long long)gridDim.x * blockDim.x) {
+// dW [M, N] and db [N] = sums of the slabs' parts in 64 bits, ascending slabs.  A part in pieces that is not finite is
+// formed again in fp32.
+template <class EA, class EB, bool kDz>
+__global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, char* dW, long long lddw, float* __restrict__ db) {
+  if (g.stop && g.stop[0] != 0) return;
+  const long long MN = (long long)g.M * g.N, stride = MN + g.N;
+  const long long end = db ? stride : MN;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (long long)gridDim.x * blockDim.x) {
     double s = 0.0;
-    const float* __restrict__ p = part + i;
-    for (int k = 0; k < S; k += 8, p += 8 * stride) {        // S is a multiple of eight; eight requested together
+    const float* __restrict__ p = g.part + i;
+    for (int k = 0; k < g.S; k += 8, p += 8 * stride) {        // S is a multiple of eight; eight requested together
       float x[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) x[u] = p[u * stride];
+      if constexpr (EB::kPieces > 1) {
+        float probe = 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) probe = fmaf(x[u], 0.f, probe);
+        if (!(probe == 0.f) && i < MN) {
+          const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
+          const int m = (int)(i / g.N), n = (int)(i % g.N);
+          for (int u = 0; u < 8; ++u) {
+            if (__builtin_isfinite(p[u * stride])) {
+              s += (double)p[u * stride];
+              continue;
+            }
+            const Slab sl = slab_rows(g, rows, k + u, WeightShape<EA, EB>::KS);
+            float v = 0.f;
+            for (long long r = sl.r0; r < sl.r1; ++r) v = fmaf(single<EA, false>(g.a, r, m), single<EB, kDz>(g.b, r, n), v);
+            s += (double)v;
+          }
+          continue;
+        }
+      }
 #pragma unroll
       for (int u = 0; u < 8; ++u) s += (double)x[u];
     }
-    if (i < MN) store_value<E>(dW, i / N * lddw + i % N, (float)s);
+    if (i < MN) store_value<EB>(dW, i / g.N * lddw + i % g.N, (float)s);
     else db[i - MN] = (float)s;
   }
 }
 
 // The slabs of a weight gradient: one round of workgroups at two per CU, and at least 256 rows each.
 int slabs_of(long long rows, int K, int N, int n_cu) {
-  const int ntile = ((K + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+  const int ntile = ((K + 127) / 128) * ((N + kTileN - 1) / kTileN);
   long long S = 2 * n_cu / (ntile < 1 ? 1 : ntile), by_rows = (rows + 255) / 256;
   if (S > by_rows) S = by_rows;
   S = (S + 7) / 8 * 8;
   return S < 8 ? 8 : (int)S;
 }
+bool smooth(int act) { return act == DC_ACT_GELU || act == DC_ACT_SILU; }
+int slope_blocks(long long rows, int n_cu) {           // row blocks of the pass that forms dZ
+  const long long want = (rows + 63) / 64, most = (long long)n_cu * 8;
+  return (int)(want < 1 ? 1 : (want < most ? want : most));
+}
 
-bool whole(const void* p, long long ld, int cols, int bytes, int n) {       // vectors of n values
-  return cols % n == 0 && ld % n == 0 && reinterpret_cast<size_t>(p) % ((size_t)n * bytes) == 0;
+// Up to `few` 32 x 32 tiles, each gets a workgroup: two rounds of two workgroups per CU.  Where only the device knows the
+// rows both kernels are launched, and one of them leaves at once.
+template <class E, bool kDz, bool kColsB, bool kVec>
+hipError_t product(const ProductArgs& g, long long rows, int n_cu, hipStream_t s) {
+  constexpr int kI = E::kPieces == 1 ? 4 : 2;
+  const int few = 4 * n_cu;
+  const long long most = 2LL * n_cu, small = (rows + 31) / 32 * ((g.N + 31) / 32), large = (rows + 64 * kI - 1) / (64 * kI) * ((g.N + kTileN - 1) / kTileN);
+  if (small <= few || g.nrows)
+    hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, kVec>), dim3((unsigned)(small < 2 * most ? small : 2 * most)), dim3(kThreads), 0, s, g, few);
+  if (small > few)
+    hipLaunchKernelGGL((product_kernel<E, kDz, kColsB, kVec, kI>), dim3((unsigned)((large < most ? large : most) + 7) / 8 * 8), dim3(kThreads), 0, s, g, few);
+  return hipGetLastError();
 }
-unsigned grid_of(long long tiles, int n_cu) {
-  const long long most = (long long)n_cu * 2;
-  long long g = tiles < most ? tiles : most;
-  return (unsigned)((g + 7) / 8 * 8);
-}
-long long tiles_count(long long rows, int N) { return (rows + kTile - 1) / kTile * ((N + kTile - 1) / kTile); }
 
 template <class E>
 hipError_t dense(const DenseArgs& a, hipStream_t s) {
   ProductArgs g{};
+  constexpr int kWide = 16 / E::kBytes;
   const int K = a.nseg * a.d;
-  bool vec = whole(a.W, a.ldw, a.N, E::kBytes, 4) && K % 8 == 0 && a.d % 8 == 0;
-  for (int i = 0; i < a.nseg; ++i) {
-    g.a.p[i] = static_cast<const char*>(a.X[i]);
-    vec = vec && whole(a.X[i], a.ldx, a.d, E::kBytes, 16 / E::kBytes);
-  }
+  for (int i = 0; i < a.nseg; ++i) g.a.p[i] = static_cast<const char*>(a.X[i]);
   g.a.ld = a.ldx;
   g.a.rows = a.rows;
   g.a.cols = K;
@@ -586,22 +956,27 @@ hipError_t dense(const DenseArgs& a, hipStream_t s) {
   g.ldz = a.ldz;
   g.Y = static_cast<char*>(a.Y);
   g.ldy = a.ldy;
+  auto starts = [](const void* p, long long ld) { return !p || (ld % kWide == 0 && reinterpret_cast<size_t>(p) % 16 == 0); };
+  g.vec = starts(a.R, a.ldr) && starts(a.Z, a.ldz) && starts(a.Y, a.ldy);
   g.stop = a.stop;
-  const dim3 grid(grid_of(tiles_count(a.rows, a.N), a.n_cu));
-  if (vec) hipLaunchKernelGGL((product_kernel<E, false, true, true>), grid, dim3(kThreads), 0, s, g);
-  else hipLaunchKernelGGL((product_kernel<E, false, true, false>), grid, dim3(kThreads), 0, s, g);
-  return hipGetLastError();
+  return a.d % 8 == 0 && a.N % 4 == 0 ? product<E, false, true, true>(g, a.rows, a.n_cu, s) : product<E, false, true, false>(g, a.rows, a.n_cu, s);
 }
 
 template <class E, class EX, bool kDz, bool kVec>
-void weight_launch(const WeightArgs& w, hipStream_t s) {
-  const int ntile = (w.M > 0 ? (w.M + kTile - 1) / kTile : 1) * ((w.N + kTile - 1) / kTile);
+hipError_t weight(const WeightArgs& w, const DenseBackArgs& a, float* db, hipStream_t s) {
+  constexpr int kTileM = WeightShape<EX, E>::kTileM;
+  const int ntile = (w.M > 0 ? (w.M + kTileM - 1) / kTileM : 1) * ((w.N + kTileN - 1) / kTileN);
   hipLaunchKernelGGL((weight_kernel<EX, E, kDz, kVec>), dim3(ntile * w.S), dim3(kThreads), 0, s, w);
+  const long long total = (long long)w.M * w.N + w.N, most = (long long)a.n_cu * 8, want = (total + 255) / 256;
+  hipLaunchKernelGGL((weight_reduce_kernel<EX, E, kDz>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, w,
+                     static_cast<char*>(a.dW), a.lddw, db);
+  return hipGetLastError();
 }
 
 template <class E, bool kDz>
 hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
   const int K = a.nseg * a.d;
+  constexpr int kWide = 16 / E::kBytes;
   Source dz{};
   dz.p[0] = static_cast<const char*>(a.dY);
   dz.z = static_cast<const char*>(a.Z);
@@ -609,9 +984,24 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
   dz.ldz = a.ldz;
   dz.rows = a.rows;
   dz.cols = dz.d = a.N;
-  dz.act = a.act;
-  constexpr int kWide = 16 / E::kBytes;
-  const bool dz_vec = whole(a.dY, a.lddy, a.N, E::kBytes, kWide) && (!kDz || whole(a.Z, a.ldz, a.N, E::kBytes, kWide));
+  float* workspace = a.workspace;
+  float* db = a.db;
+  if (smooth(a.act)) {
+    char* out = reinterpret_cast<char*>(workspace);
+    workspace += dense_dz_floats(a.rows, a.N, a.bf16);
+    SlopeArgs g{a.rows, a.nrows, a.N, a.act, dz.p[0], a.lddy, dz.z, a.ldz, out, a.db ? workspace : nullptr, slope_blocks(a.rows, a.n_cu), a.stop};
+    workspace += (size_t)g.row_blocks * a.N;
+    const bool wide = a.N % kWide == 0;
+    const int columns = 32 * (wide ? kWide : 1), cb = (a.N + columns - 1) / columns;
+    if (wide) hipLaunchKernelGGL((slope_kernel<E, kWide>), dim3(cb * g.row_blocks), dim3(256), 0, s, g);
+    else hipLaunchKernelGGL((slope_kernel<E, 1>), dim3(cb * g.row_blocks), dim3(256), 0, s, g);
+    if (a.db) launch_column_sums(g.part, g.row_blocks, a.N, a.db, 0, nullptr, a.stop, s);
+    db = nullptr;
+    dz.p[0] = out;
+    dz.z = nullptr;
+    dz.ld = a.N;
+  }
+  hipError_t e = hipSuccess;
   if (a.dX && a.rows > 0) {
     ProductArgs g{};
     g.a = dz;
@@ -625,53 +1015,37 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     g.act = DC_ACT_NONE;
     g.Y = static_cast<char*>(a.dX);
     g.ldy = a.lddx;
+    g.vec = a.lddx % kWide == 0 && reinterpret_cast<size_t>(a.dX) % 16 == 0;
     g.stop = a.stop;
-    const dim3 grid(grid_of(tiles_count(a.rows, K), a.n_cu));
-    if (dz_vec && a.N % 8 == 0 && whole(a.W, a.ldw, a.N, E::kBytes, kWide))
-      hipLaunchKernelGGL((product_kernel<E, kDz, false, true>), grid, dim3(kThreads), 0, s, g);
-    else
-      hipLaunchKernelGGL((product_kernel<E, kDz, false, false>), grid, dim3(kThreads), 0, s, g);
+    e = a.N % 8 == 0 ? product<E, kDz, false, true>(g, a.rows, a.n_cu, s) : product<E, kDz, false, false>(g, a.rows, a.n_cu, s);
   }
-  if (a.dW || a.db) {
+  if (e == hipSuccess && (a.dW || db)) {
     WeightArgs w{};
     w.a.rows = a.rows;
     w.M = a.dW ? K : 0;
     w.a.cols = K;
     w.a.d = a.d;
-    bool vec = dz_vec;
+    const bool vec = a.N % 4 == 0 && a.d % 4 == 0;
     if (a.kept.code) {
       w.a.p[0] = reinterpret_cast<const char*>(a.kept.code);
       w.a.exponent = a.kept.exponent;
       w.a.ld = a.kept.ld_code;
       w.a.ld_exponent = a.kept.ld_exponent;
-      vec = vec && whole(a.kept.code, a.kept.ld_code, K, 1, 4);
     } else {
-      for (int i = 0; i < a.nseg; ++i) {
-        w.a.p[i] = static_cast<const char*>(a.X[i]);
-        if (w.M) vec = vec && whole(a.X[i], a.ldx, a.d, E::kBytes, 4);
-      }
+      for (int i = 0; i < a.nseg; ++i) w.a.p[i] = static_cast<const char*>(a.X[i]);
       w.a.ld = a.ldx;
     }
     w.b = dz;
     w.nrows = a.nrows;
     w.N = a.N;
     w.S = slabs_of(a.rows, K, a.N, a.n_cu);
-    w.part = a.workspace;
-    w.sums = a.db != nullptr;
+    w.part = workspace;
+    w.sums = db != nullptr;
     w.stop = a.stop;
-    if (a.kept.code) {
-      if (vec) weight_launch<E, Kept, kDz, true>(w, s);
-      else weight_launch<E, Kept, kDz, false>(w, s);
-    } else {
-      if (vec) weight_launch<E, E, kDz, true>(w, s);
-      else weight_launch<E, E, kDz, false>(w, s);
-    }
-    const long long MN = (long long)w.M * a.N, total = MN + a.N;
-    const long long most = (long long)a.n_cu * 8, want = (total + 255) / 256;
-    hipLaunchKernelGGL((weight_reduce_kernel<E>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, w.part, w.S, MN,
-                       a.N, static_cast<char*>(a.dW), a.lddw, a.db, a.stop);
+    if (a.kept.code) e = vec ? weight<E, Kept, kDz, true>(w, a, db, s) : weight<E, Kept, kDz, false>(w, a, db, s);
+    else e = vec ? weight<E, E, kDz, true>(w, a, db, s) : weight<E, E, kDz, false>(w, a, db, s);
   }
-  return hipGetLastError();
+  return e;
 }
 
 }  // namespace
@@ -681,13 +1055,18 @@ hipError_t launch_dense(const DenseArgs& a, hipStream_t s) {
   return a.bf16 ? dense<Bf16>(a, s) : dense<F32>(a, s);
 }
 
-size_t dense_back_floats(long long rows, int K, int N, int n_cu) {
-  return (size_t)slabs_of(rows, K, N, n_cu) * ((size_t)K * N + N);
+size_t dense_dz_floats(long long rows, int N, int bf16) {
+  return ((size_t)rows * N * (bf16 ? 2 : 4) + 15) / 16 * 4;
+}
+size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu) {
+  size_t n = (size_t)slabs_of(rows, K, N, n_cu) * ((size_t)K * N + N);
+  if (smooth(act)) n += dense_dz_floats(rows, N, bf16) + (size_t)slope_blocks(rows, n_cu) * N;
+  return n;
 }
 
 hipError_t launch_dense_back(const DenseBackArgs& a, hipStream_t s) {
-  if (a.act == DC_ACT_NONE) return a.bf16 ? dense_back<Bf16, false>(a, s) : dense_back<F32, false>(a, s);
-  return a.bf16 ? dense_back<Bf16, true>(a, s) : dense_back<F32, true>(a, s);
+  if (a.act == DC_ACT_RELU) return a.bf16 ? dense_back<Bf16, true>(a, s) : dense_back<F32, true>(a, s);
+  return a.bf16 ? dense_back<Bf16, false>(a, s) : dense_back<F32, false>(a, s);
 }
 
 }  // namespace dc

@@ -110,42 +110,15 @@ __device__ __forceinline__ Affine<kV> affine_at(const GraphNormArgs& a, int c) {
   return f;
 }
 
-template <int kV>
-__device__ __forceinline__ void activate(float (&z)[kV], int act) {
-  switch (act) {
-    case DC_ACT_RELU:
-#pragma unroll
-      for (int k = 0; k < kV; ++k) z[k] = activation(z[k], DC_ACT_RELU);
-      break;
-    case DC_ACT_GELU:
-#pragma unroll
-      for (int k = 0; k < kV; ++k) z[k] = activation(z[k], DC_ACT_GELU);
-      break;
-    case DC_ACT_SILU:
-#pragma unroll
-      for (int k = 0; k < kV; ++k) z[k] = activation(z[k], DC_ACT_SILU);
-      break;
-    default: break;
-  }
-}
 // dy becomes dz.
 template <int kV>
 __device__ __forceinline__ void slope(float (&dy)[kV], const float (&xh)[kV], const Affine<kV>& f, int act) {
-  switch (act) {
-    case DC_ACT_RELU:
+  float z[kV];
 #pragma unroll
-      for (int k = 0; k < kV; ++k) dy[k] *= activation_slope(fmaf(f.gamma[k], xh[k], f.beta[k]), DC_ACT_RELU);
-      break;
-    case DC_ACT_GELU:
+  for (int k = 0; k < kV; ++k) z[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
+  slopes<kV>(z, act);
 #pragma unroll
-      for (int k = 0; k < kV; ++k) dy[k] *= activation_slope(fmaf(f.gamma[k], xh[k], f.beta[k]), DC_ACT_GELU);
-      break;
-    case DC_ACT_SILU:
-#pragma unroll
-      for (int k = 0; k < kV; ++k) dy[k] *= activation_slope(fmaf(f.gamma[k], xh[k], f.beta[k]), DC_ACT_SILU);
-      break;
-    default: break;
-  }
+  for (int k = 0; k < kV; ++k) dy[k] *= z[k];
 }
 
 // What a row's vector adds to the two sums.
@@ -535,23 +508,22 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
     }
 }
 
-// dgamma, dbeta = sums of the column blocks in 64 bits, ascending blocks: a wave per 64 columns' chain would be one round
-// trip per block, so a workgroup takes 16 columns with 16 threads each.
-__global__ __launch_bounds__(256) void column_reduce_kernel(const float* __restrict__ cols, int blocks, int C, float* __restrict__ dgamma,
-                                                            float* __restrict__ dbeta, const int* stop) {
+// One chain of additions per column would be a round trip per row: a workgroup takes 16 columns with 16 threads each.
+__global__ __launch_bounds__(256) void column_sums_kernel(const float* __restrict__ part, int blocks, int n1, float* __restrict__ out1,
+                                                          int n2, float* __restrict__ out2, const int* stop) {
   if (stop && stop[0] != 0) return;
   __shared__ double red[16][17];
-  const int j = threadIdx.x & 15, p = threadIdx.x >> 4, c = blockIdx.x * 16 + j;
+  const int j = threadIdx.x & 15, p = threadIdx.x >> 4, c = blockIdx.x * 16 + j, n = n1 + n2;
   double s = 0.0;
-  if (c < 2 * C)
-    for (int b = p; b < blocks; b += 16) s += (double)cols[(size_t)b * 2 * C + c];
+  if (c < n)
+    for (int b = p; b < blocks; b += 16) s += (double)part[(size_t)b * n + c];
   red[p][j] = s;
   __syncthreads();
-  if (p == 0 && c < 2 * C) {
+  if (p == 0 && c < n) {
     double v = 0.0;
     for (int i = 0; i < 16; ++i) v += red[i][j];
-    if (c < C) dgamma[c] = (float)v;
-    else dbeta[c - C] = (float)v;
+    if (c < n1) out1[c] = (float)v;
+    else out2[c - n1] = (float)v;
   }
 }
 
@@ -644,8 +616,7 @@ hipError_t run(Norm n, hipStream_t s) {
     hipLaunchKernelGGL((chunk_finish_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
   }
   if (kBack && n.a.dgamma)
-    hipLaunchKernelGGL(column_reduce_kernel, dim3((2 * n.a.C + 15) / 16), dim3(256), 0, s, n.cols, p.blocks + p.chunk_blocks, n.a.C,
-                       n.a.dgamma, n.a.dbeta, n.a.stop);
+    launch_column_sums(n.cols, p.blocks + p.chunk_blocks, n.a.C, n.a.dgamma, n.a.C, n.a.dbeta, n.a.stop, s);
   return hipGetLastError();
 }
 
@@ -675,6 +646,10 @@ hipError_t dispatch(const GraphNormArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+void launch_column_sums(const float* part, int blocks, int n1, float* out1, int n2, float* out2, const int* stop, hipStream_t s) {
+  hipLaunchKernelGGL(column_sums_kernel, dim3((n1 + n2 + 15) / 16), dim3(256), 0, s, part, blocks, n1, out1, n2, out2, stop);
+}
 
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
   // what any vector width and type would need

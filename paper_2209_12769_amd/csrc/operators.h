@@ -26,6 +26,47 @@ __device__ __forceinline__ float activation_slope(float z, int act) {
   }
 }
 
+// The same for kN values, the choice made once.
+template <int kN>
+__device__ __forceinline__ void activate(float (&z)[kN], int act) {
+  switch (act) {
+    case DC_ACT_RELU:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_RELU);
+      break;
+    case DC_ACT_GELU:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_GELU);
+      break;
+    case DC_ACT_SILU:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_SILU);
+      break;
+    default: break;
+  }
+}
+template <int kN>
+__device__ __forceinline__ void slopes(float (&z)[kN], int act) {
+  switch (act) {
+    case DC_ACT_RELU:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_RELU);
+      break;
+    case DC_ACT_GELU:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_GELU);
+      break;
+    case DC_ACT_SILU:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_SILU);
+      break;
+    default:
+#pragma unroll
+      for (int k = 0; k < kN; ++k) z[k] = 1.f;
+      break;
+  }
+}
+
 // ---- kept rows: 8-bit codes, one power of two per row and 32 columns ----
 constexpr int kKeptBlock = 32;
 constexpr int kKeptNan = 255;                      // exponent code of a block that holds a number that is not finite
@@ -81,11 +122,12 @@ struct DenseBackArgs {
   void* dW;                      // [K, N] or null
   long long lddw;
   float* db;                     // [N] or null
-  float* workspace;              // dense_back_floats() of them, if dW or db
+  float* workspace;              // dense_back_floats() of them
   const int* stop;
   int n_cu;
 };
-size_t dense_back_floats(long long rows, int K, int N, int n_cu);
+size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu);
+size_t dense_dz_floats(long long rows, int N, int bf16);    // of them, dZ of a smooth activation in the storage type
 hipError_t launch_dense_back(const DenseBackArgs& a, hipStream_t s);
 
 // ---- norm over the rows of each graph ----
@@ -121,6 +163,9 @@ struct GraphNormArgs {
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu);
 hipError_t launch_graph_norm(const GraphNormArgs& a, hipStream_t s);
 hipError_t launch_graph_norm_back(const GraphNormArgs& a, hipStream_t s);
+
+// out1 [n1] | out2 [n2] = sums over `blocks` rows of part [blocks, n1 + n2], in 64 bits and a fixed order.
+void launch_column_sums(const float* part, int blocks, int n1, float* out1, int n2, float* out2, const int* stop, hipStream_t s);
 
 // ---- kept rows ----
 struct KeepArgs {
