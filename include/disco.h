@@ -414,7 +414,7 @@ dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* h
  * own.  They allocate nothing and do not synchronise, and may be captured into a graph.  Work is enqueued on
  * `stream`, a stream of the context's device, whatever device is current.  An array of outputs may be null where
  * the text says so; rows = 0 is allowed.  Limits: rows and graphs fit in int32, rows are at most 2^22 elements
- * apart, in and out are at most 65536, channels per group at most 1024, channels at most 8192.                  */
+ * apart, in and out are at most 65536, channels per group at most 512, channels at most 8192.                   */
 typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 3 } dc_activation;
 /* GELU is z (1 + erf(z / sqrt 2)) / 2, SiLU z / (1 + e^-z). */
 

@@ -1460,8 +1460,8 @@ dc_status graph_norm_check(dc_ctx* ctx, const dc_graph_norm_args* a, bool backwa
   if (a->act < DC_ACT_NONE || a->act > DC_ACT_SILU) return fail(ctx, DC_ERR_INVALID_ARG, "unknown activation");
   if (a->n_graphs < 0 || a->channels < 1 || a->groups < 1 || a->channels % a->groups)
     return fail(ctx, DC_ERR_INVALID_ARG, "need n_graphs >= 0 and groups that divide the channels");
-  if (a->channels > 8192 || a->channels / a->groups > 1024)
-    return fail(ctx, DC_ERR_UNSUPPORTED, "at most 8192 channels and 1024 per group");
+  if (a->channels > 8192 || a->channels / a->groups > 512)
+    return fail(ctx, DC_ERR_UNSUPPORTED, "at most 8192 channels and 512 per group");
   if (!backward && !(a->eps > 0.f)) return fail(ctx, DC_ERR_INVALID_ARG, "need eps > 0");
   const int es = a->dtype == DC_BF16 ? 2 : 4;
   if (a->n_graphs > 0 && (!a->node_off || !a->mean || !a->rstd)) return fail(ctx, DC_ERR_INVALID_ARG, "null node_off, mean or rstd");

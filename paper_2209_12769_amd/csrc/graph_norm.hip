@@ -190,6 +190,13 @@ __device__ __forceinline__ void group_sums(double& s1, double& s2, double2* red,
   s2 = v.y;
 }
 
+// mean and 1 / sqrt(variance + eps) from the sums of x and x^2 over m values.
+__device__ __forceinline__ void statistics(double s1, double s2, double m, float eps, float& mu, float& rs) {
+  const double mean = m > 0 ? s1 / m : 0.0, var = m > 0 ? s2 / m - mean * mean : 0.0;
+  mu = (float)mean;
+  rs = (float)(1.0 / sqrt((var > 0.0 ? var : (var != var ? var : 0.0)) + (double)eps));
+}
+
 // The second pass of one vector.
 template <typename T, int kV, bool kBack>
 __device__ __forceinline__ void finish(const Norm& n, const float (&x)[kV], float (&dy)[kV], long long row, int c, float mu, float r,
@@ -267,8 +274,20 @@ __device__ __forceinline__ void column_sums(const Norm& n, double (&dg)[kV], dou
   }
 }
 
-// Steps u of a group of kStep row steps from i on: rows first + (i + u) * step below end.
+// A thread's rows first, first + step, .. (count of them) in groups of kStep: the requests of a group are made together, past the
+// end the last row again (a request in a branch would make every wait wait for everything).
 constexpr int kStep = 4;
+template <typename T, typename X, int kV, bool kBack, typename F>
+__device__ __forceinline__ void each_row(const Norm& n, long long first, int step, int from, int count, int c, F f) {
+  for (int i = from; i < count; i += kStep) {
+    Two<T, X, kV> h[kStep];
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) fetch<T, X, kV, kBack>(h[u], n, first + (long long)min(i + u, count - 1) * step, c);
+#pragma unroll
+    for (int u = 0; u < kStep; ++u)
+      if (i + u < count) f(h[u], i + u);
+  }
+}
 
 // One workgroup per (graph, slab), the slab fixed.  The first n.held row steps of every thread stay in LDS.
 template <typename T, typename X, int kV, int kThreads, bool kBack>
@@ -303,25 +322,15 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
     for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
     const long long r0 = r.lo + rl;
     const int count = in && r0 < r.hi ? (int)((r.hi - r0 + step - 1) / step) : 0;      // row steps of this thread
-    for (int i = 0; i < count; i += kStep) {
-      Item h[kStep];
-#pragma unroll
-      for (int u = 0; u < kStep; ++u)
-        if (i + u < count) fetch<T, X, kV, kBack>(h[u], n, r0 + (long long)(i + u) * step, c);
-#pragma unroll
-      for (int u = 0; u < kStep; ++u)
-        if (i + u < count) {
-          if (i + u < n.held) mine[(i + u) * kThreads] = h[u];
-          float x[kV], dy[kV];
-          open<T, X, kV, kBack>(x, dy, h[u]);
-          add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
-        }
-    }
+    each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Item& h, int i) {
+      if (i < n.held) mine[i * kThreads] = h;
+      float x[kV], dy[kV];
+      open<T, X, kV, kBack>(x, dy, h);
+      add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+    });
     group_sums(s1, s2, red, n.lanes, used, gv);
     if constexpr (!kBack) {
-      const double mean = m > 0 ? s1 / m : 0.0, var = m > 0 ? s2 / m - mean * mean : 0.0;
-      mu = (float)mean;
-      rs = (float)(1.0 / sqrt((var > 0.0 ? var : (var != var ? var : 0.0)) + (double)n.a.eps));
+      statistics(s1, s2, m, n.a.eps, mu, rs);
       if (in && rl == 0 && lane % gv == 0) {
         n.a.mean[(size_t)g * n.a.G + group] = mu;
         n.a.rstd[(size_t)g * n.a.G + group] = rs;
@@ -335,22 +344,14 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
         dbs[k] += (double)db[k];
       }
     }
-    for (int i = 0; i < count; i += kStep) {
-      Item h[kStep];
-#pragma unroll
-      for (int u = 0; u < kStep; ++u)
-        if (i + u < count) {
-          if (i + u < n.held) h[u] = mine[(i + u) * kThreads];
-          else fetch<T, X, kV, kBack>(h[u], n, r0 + (long long)(i + u) * step, c);
-        }
-#pragma unroll
-      for (int u = 0; u < kStep; ++u)
-        if (i + u < count) {
-          float x[kV], dy[kV];
-          open<T, X, kV, kBack>(x, dy, h[u]);
-          finish<T, kV, kBack>(n, x, dy, r0 + (long long)(i + u) * step, c, mu, rs, s1f, s2f, f);
-        }
-    }
+    auto second = [&](const Item& h, int i) {
+      float x[kV], dy[kV];
+      open<T, X, kV, kBack>(x, dy, h);
+      finish<T, kV, kBack>(n, x, dy, r0 + (long long)i * step, c, mu, rs, s1f, s2f, f);
+    };
+    const int here = min(count, n.held);
+    for (int i = 0; i < here; ++i) second(mine[i * kThreads], i);
+    each_row<T, X, kV, kBack>(n, r0, step, here, count, c, second);
   }
   if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
 }
@@ -389,7 +390,7 @@ __device__ __forceinline__ Segment segment_of(const Norm& n, int ng, long long c
   return s;
 }
 
-constexpr int kChunkThreads = 1024;
+constexpr int kChunkThreads = 512;
 
 template <typename T, typename X, int kV, bool kBack>
 __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n) {
@@ -419,14 +420,13 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
       float dg[kV], db[kV];
 #pragma unroll
       for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
-      if (in)
-        for (long long row = seg.lo + rl; row < seg.hi; row += step) {
-          Two<T, X, kV> w;
-          fetch<T, X, kV, kBack>(w, n, row, c);
-          float x[kV], dy[kV];
-          open<T, X, kV, kBack>(x, dy, w);
-          add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
-        }
+      const long long r0 = seg.lo + rl;
+      const int count = in && r0 < seg.hi ? (int)((seg.hi - r0 + step - 1) / step) : 0;
+      each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
+        float x[kV], dy[kV];
+        open<T, X, kV, kBack>(x, dy, h);
+        add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+      });
       group_sums(s1, s2, red, n.lanes, used, gv);
       if (in && rl == 0 && lane % gv == 0) n.part[(size_t)(chunk + seg.g) * n.a.G + group] = make_double2(s1, s2);
 #pragma unroll
@@ -471,10 +471,10 @@ __global__ __launch_bounds__(256) void long_sums_kernel(const Norm n) {
         if (kBack) {
           n.means[(size_t)g * n.a.G + q] = make_float2((float)(s1 / m), (float)(s2 / m));
         } else {
-          const double mean = s1 / m, var = s2 / m - mean * mean;
-          n.a.mean[(size_t)g * n.a.G + q] = (float)mean;
-          n.a.rstd[(size_t)g * n.a.G + q] =
-              (float)(1.0 / sqrt((var > 0.0 ? var : (var != var ? var : 0.0)) + (double)n.a.eps));
+          float mu, rs;
+          statistics(s1, s2, m, n.a.eps, mu, rs);
+          n.a.mean[(size_t)g * n.a.G + q] = mu;
+          n.a.rstd[(size_t)g * n.a.G + q] = rs;
         }
       }
     }
@@ -498,13 +498,13 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
       if (seg.lo >= seg.hi) continue;
       const float mu = n.a.mean[(size_t)seg.g * n.a.G + group], rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
       const float2 s = kBack ? n.means[(size_t)seg.g * n.a.G + group] : make_float2(0.f, 0.f);
-      for (long long row = seg.lo + rl; row < seg.hi; row += step) {
-        Two<T, X, kV> w;
-        fetch<T, X, kV, kBack>(w, n, row, c);
+      const long long r0 = seg.lo + rl;
+      const int count = r0 < seg.hi ? (int)((seg.hi - r0 + step - 1) / step) : 0;
+      each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
         float x[kV], dy[kV];
-        open<T, X, kV, kBack>(x, dy, w);
-        finish<T, kV, kBack>(n, x, dy, row, c, mu, rs, s.x, s.y, f);
-      }
+        open<T, X, kV, kBack>(x, dy, h);
+        finish<T, kV, kBack>(n, x, dy, r0 + (long long)i * step, c, mu, rs, s.x, s.y, f);
+      });
     }
 }
 
@@ -527,9 +527,16 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* __restric
   }
 }
 
-constexpr int kChunkRows = 256;
+constexpr int kMostThreads = 512;         // two waves per SIMD: the gradient needs more than 128 registers
+// Rows of a chunk: four chunks per CU, 64 to 512 rows.  Fewer than the shortest long graph.
+int chunk_rows(long long rows, int n_cu) {
+  const long long r = (rows / (4LL * n_cu) + 63) / 64 * 64;
+  return (int)(r < 64 ? 64 : (r > 512 ? 512 : r));
+}
+
 struct Plan {
   int threads, slab, nslab, lanes, held;
+  int chunk_slab, chunk_nslab, chunk_lanes;
   long long long_rows;
   bool chunks;             // there may be long graphs
   int blocks, chunk_blocks;    // column blocks: of the short graphs' kernel, of the chunk kernels
@@ -545,8 +552,8 @@ int slab_of(int C, int cg, int es) {
   return s >= C ? C : (int)s;
 }
 int blocks_most(int n_cu) { return n_cu * 8; }
-// LDS for rows of a workgroup of 64, 256 or 1024 threads: eight, three or one of them per CU
-int held_bytes(int threads) { return threads == 64 ? 18 * 1024 : (threads == 256 ? 48 * 1024 : 140 * 1024); }
+// LDS for rows of a workgroup of 64, 256 or 512 threads: eight, three or one of them per CU
+int held_bytes(int threads) { return threads == 64 ? 18 * 1024 : (threads == 256 ? 48 * 1024 : 148 * 1024); }
 
 Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item, int n_cu) {
   Plan p{};
@@ -555,22 +562,32 @@ Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item
   // whole rows and the fewest threads that hold it; else slabs
   p.slab = C;
   p.lanes = pow2_at_least((C + v - 1) / v);
-  for (p.threads = 64; p.threads < 1024; p.threads *= 4)
-    if (p.lanes <= p.threads && want <= (long long)held_bytes(p.threads) / (p.threads * item) * (p.threads / p.lanes)) break;
-  if (p.threads == 1024 && (p.lanes > 1024 || want > (long long)held_bytes(1024) / (1024 * item) * (1024 / p.lanes))) {
-    p.slab = slab_of(C, cg, es);
+  auto fits = [&](int threads, int lanes) {
+    return lanes <= threads && want <= (long long)held_bytes(threads) / (threads * item) * (threads / lanes);
+  };
+  p.threads = fits(64, p.lanes) ? 64 : (fits(256, p.lanes) ? 256 : kMostThreads);
+  const int narrow = slab_of(C, cg, es);
+  if (p.threads == kMostThreads && !fits(p.threads, p.lanes)) {
+    p.slab = narrow;
     p.lanes = pow2_at_least((p.slab + v - 1) / v);
   }
+  // chunks are not held: whole rows if the workgroup is wide enough
+  p.chunk_lanes = pow2_at_least((C + v - 1) / v);
+  p.chunk_slab = p.chunk_lanes <= kChunkThreads ? C : narrow;
+  p.chunk_lanes = pow2_at_least((p.chunk_slab + v - 1) / v);
+  p.chunk_nslab = (C + p.chunk_slab - 1) / p.chunk_slab;
   p.held = held_bytes(p.threads) / (p.threads * item);
   p.nslab = (C + p.slab - 1) / p.slab;
   // twice what a workgroup would have if all had the same
   const long long share = 2 * rows * p.nslab / n_cu;
   p.long_rows = share < 1024 ? 1024 : (share > 4096 ? 4096 : share);
   p.chunks = rows > p.long_rows;
-  const int most = blocks_most(n_cu) / p.nslab > 0 ? blocks_most(n_cu) / p.nslab : 1;
-  p.blocks = n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most;
-  const long long chunks = (rows + kChunkRows - 1) / kChunkRows;
-  p.chunk_blocks = p.chunks ? (int)(chunks < most ? chunks : most) : 0;
+  auto blocks = [&](long long items, int nslab) {
+    const long long most = blocks_most(n_cu) / nslab > 0 ? blocks_most(n_cu) / nslab : 1;
+    return (int)(items < 1 ? 1 : (items < most ? items : most));
+  };
+  p.blocks = blocks(n_graphs, p.nslab);
+  p.chunk_blocks = p.chunks ? blocks((rows + chunk_rows(rows, n_cu) - 1) / chunk_rows(rows, n_cu), p.chunk_nslab) : 0;
   return p;
 }
 
@@ -594,21 +611,24 @@ hipError_t run(Norm n, hipStream_t s) {
   n.lanes = p.lanes;
   n.held = p.held;
   n.long_rows = p.long_rows;
-  n.chunk_rows = kChunkRows;
+  n.chunk_rows = chunk_rows(n.a.rows, n.a.n_cu);
   char* w = n.a.workspace;
   if (p.chunks) {
     n.part = reinterpret_cast<double2*>(w);
-    w += ((size_t)((n.a.rows + kChunkRows - 1) / kChunkRows) + (size_t)n.a.n_graphs + 1) * n.a.G * sizeof(double2);
+    w += ((size_t)((n.a.rows + n.chunk_rows - 1) / n.chunk_rows) + (size_t)n.a.n_graphs + 1) * n.a.G * sizeof(double2);
     n.means = reinterpret_cast<float2*>(w);
     if (kBack) w += (size_t)n.a.n_graphs * n.a.G * sizeof(float2);
   }
   n.cols = reinterpret_cast<float*>(w);
   hipError_t e = p.threads == 64    ? run_short<T, X, kV, 64, kBack>(n, p.blocks, s)
                  : p.threads == 256 ? run_short<T, X, kV, 256, kBack>(n, p.blocks, s)
-                                    : run_short<T, X, kV, 1024, kBack>(n, p.blocks, s);
+                                    : run_short<T, X, kV, kMostThreads, kBack>(n, p.blocks, s);
   if (e != hipSuccess) return e;
   if (p.chunks) {
     n.col_block0 = p.blocks;
+    n.slab = p.chunk_slab;
+    n.nslab = p.chunk_nslab;
+    n.lanes = p.chunk_lanes;
     const dim3 cgrid(p.chunk_blocks * n.nslab);
     hipLaunchKernelGGL((chunk_sums_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
     const int waves = (n.a.n_graphs + 63) / 64, lgrid = (waves + 3) / 4 < n.a.n_cu ? (waves + 3) / 4 : n.a.n_cu;
@@ -653,12 +673,12 @@ void launch_column_sums(const float* part, int blocks, int n1, float* out1, int 
 
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
   // what any vector width and type would need
-  const size_t chunks = (size_t)((rows + kChunkRows - 1) / kChunkRows) + (size_t)n_graphs + 1;
-  size_t b = rows > 1024 ? chunks * G * sizeof(double2) : 0;
+  const long long cr = chunk_rows(rows, n_cu), nc = (rows + cr - 1) / cr, most = blocks_most(n_cu);
+  const bool chunks = rows > 1024;
+  size_t b = chunks ? ((size_t)nc + (size_t)n_graphs + 1) * G * sizeof(double2) : 0;
   if (backward) {
-    if (rows > 1024) b += (size_t)n_graphs * G * sizeof(float2);
-    const long long most = blocks_most(n_cu), nc = (rows + kChunkRows - 1) / kChunkRows;
-    b += (size_t)((n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most) + (rows > 1024 ? (nc < most ? nc : most) : 0)) * 2 * C * sizeof(float);
+    if (chunks) b += (size_t)n_graphs * G * sizeof(float2);
+    b += (size_t)((n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most) + (chunks ? (nc < most ? nc : most) : 0)) * 2 * C * sizeof(float);
   }
   return b;
 }

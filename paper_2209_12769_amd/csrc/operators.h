@@ -6,11 +6,16 @@
 namespace dc {
 
 // ---- activations, in fp32 ----
+// 1 / (1 + e^-z) from the machine's power of two and reciprocal, each off by one unit in the last place: relative to the result
+// about (3 + |z|) 2^-24, where the library's exponential and an exact division would take three times the instructions
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
+}
 __device__ __forceinline__ float activation(float z, int act) {
   switch (act) {
     case DC_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
     case DC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    case DC_ACT_SILU: return z / (1.f + expf(-z));
+    case DC_ACT_SILU: return z * sigmoid(z);
     default: return z;
   }
 }
@@ -19,7 +24,7 @@ __device__ __forceinline__ float activation_slope(float z, int act) {
     case DC_ACT_RELU: return z > 0.f ? 1.f : 0.f;
     case DC_ACT_GELU: return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * 0.70710678118654752f)));
     case DC_ACT_SILU: {
-      const float s = 1.f / (1.f + expf(-z));
+      const float s = sigmoid(z);
       return s * fmaf(z, 1.f - s, 1.f);
     }
     default: return 1.f;
