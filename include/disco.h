@@ -169,6 +169,21 @@ dc_status dc_set_weights(dc_ctx* ctx, const float* W_layers, const float* b_laye
 dc_status dc_set_attention_weights(dc_ctx* ctx, const float* W_layers, const float* att, const float* b_layers,
                                    const float* head, void* stream);
 
+/* Layers of deep estimators (contexts with DC_AGG_MEAN): above the first layer each layer adds to its input, and takes it
+ * through a norm over the rows of its graph (dc_graph_norm):
+ *     h_1 = [x | means of x] W^0 + b^0,  u = act(norm(h_l)),  h_{l+1} = h_l + [u | means of u] W^l + b^l,
+ * in place of ReLU layers; the sum over h_L and the regression network stay as they are.  Every later call on the context
+ * runs this form: in dc_gnn_forward and dc_eval_candidates a norm runs over the nodes of a candidate, in dc_module_times,
+ * dc_cost_candidates, dc_search and in training over the ops of a fused op.  With DC_BF16 h and u are bf16.  An estimate
+ * may differ in its last bits with the batch that it is part of.
+ *   groups  groups of neighbouring columns, a divisor of H; 0 returns to ReLU layers (the others are not read then)
+ *   act     dc_activation;  eps > 0;  gamma, beta: host fp32, concat over l = 1 .. L - 1 of [H]
+ * Allocates; ends training (dc_train_begin has to be called again).                                                  */
+dc_status dc_set_layer_norms(dc_ctx* ctx, int32_t groups, int32_t act, float eps, const float* gamma, const float* beta,
+                             void* stream);
+/* Copies gamma and beta as they are now to host arrays.  Synchronises `stream`. */
+dc_status dc_get_layer_norms(dc_ctx* ctx, float* gamma, float* beta, void* stream);
+
 /* Base graphs (set once, candidates refer to them by index).  All host pointers.
  *   g_node_off [n+1], g_edge_off [n+1]  node / edge offsets of the graphs
  *   rowptr     concatenated per-graph CSR row pointers: graph b has N_b+1 entries
@@ -366,11 +381,22 @@ typedef struct {
   int64_t max_rows;            /* rows per batch, at most the context's max_nodes                    */
 } dc_train_params;
 
-/* Number of fp32 parameters, in the order W_layers | b_layers | head of dc_set_weights. */
+/* Number of fp32 parameters, in the order W_layers | b_layers | head of dc_set_weights, then gamma | beta of
+ * dc_set_layer_norms if there are any. */
 int64_t dc_num_params(const dc_ctx* ctx);
 
-/* Allocates the training buffers (device; about (3 L + 6) * max_rows * max(F, H) * 4 bytes), clears both
- * moment vectors and the step count.  May be called again to restart or to change the sizes. */
+/* What a training pass keeps of every layer's rows for its reverse pass; host state, taken by the next dc_train_begin.
+ *   DC_KEEP_F32    the rows and both means (and what a norm leaves) in fp32: 12 (16) bytes per value and layer
+ *   DC_KEEP_8BIT   the rows in 8 bits (dc_keep_rows), 1 + 1/32 bytes; the reverse pass reads them back and forms means and
+ *                  norms again.  The loss and the estimates are those of DC_KEEP_F32; the gradient of layer l's matrix,
+ *                  and what comes through its norm, is formed from its input as kept.  ReLU's derivatives are the
+ *                  forward's (a kept value has the sign of the value).                                            */
+enum { DC_KEEP_F32 = 0, DC_KEEP_8BIT = 1 };
+dc_status dc_train_keep(dc_ctx* ctx, int32_t which);
+
+/* Allocates the training buffers (device; about (3 L + 6) * max_rows * max(F, H) * 4 bytes, with layer norms (4 L + 6),
+ * with DC_KEEP_8BIT (L / 4 + 8)), clears both moment vectors and the step count.  May be called again to restart or
+ * to change the sizes. */
 dc_status dc_train_begin(dc_ctx* ctx, const dc_train_params* params, void* stream);
 
 /* The training set of a list of labelings: contraction as in dc_contract_graphs, then every

@@ -32,6 +32,7 @@ DC_AGG_ATTENTION = 1
 DC_KERNELS_SEPARATE_LAYERS = 1
 DC_KERNELS_EVERY_FUSED_OP = 2
 DC_DRAW_DEPENDENCY, DC_DRAW_OP = 0, 1
+DC_KEEP_F32, DC_KEEP_8BIT = 0, 1
 DC_ACT_NONE, DC_ACT_RELU, DC_ACT_GELU, DC_ACT_SILU = 0, 1, 2, 3
 ACTIVATIONS = {"none": DC_ACT_NONE, "relu": DC_ACT_RELU, "gelu": DC_ACT_GELU, "silu": DC_ACT_SILU}
 STATUS_NAMES = {0: "DC_OK", 1: "DC_ERR_INVALID_ARG", 2: "DC_ERR_BAD_GRAPH", 3: "DC_ERR_BAD_PARTITION",
@@ -148,6 +149,9 @@ def lib():
         L.dc_train_step.argtypes = [vp, C.POINTER(DcBatch), vp, vp, vp]
         L.dc_get_weights.argtypes = [vp, vp, vp, vp, vp]
         i64, size = C.c_int64, C.c_size_t
+        L.dc_set_layer_norms.argtypes = [vp, i32, i32, C.c_float, vp, vp, vp]
+        L.dc_get_layer_norms.argtypes = [vp, vp, vp, vp]
+        L.dc_train_keep.argtypes = [vp, i32]
         L.dc_keep_rows.argtypes = [vp, i32, i64, i32, vp, i64, C.POINTER(DcKeptRows), vp]
         L.dc_restore_rows.argtypes = [vp, i32, i64, i32, C.POINTER(DcKeptRows), vp, i64, vp]
         L.dc_dense.argtypes = [vp, C.POINTER(DcDenseArgs), vp]
@@ -170,7 +174,7 @@ def lib():
                   "dc_profile_end", "dc_set_profile", "dc_module_times", "dc_cost_candidates", "dc_last_fused_ops",
                   "dc_last_fused_op_repeats", "dc_walked_modules", "dc_search",
                   "dc_train_begin", "dc_select_kernels", "dc_fused_op_batch", "dc_loss_gradients", "dc_train_step", "dc_get_weights",
-                  "dc_keep_rows", "dc_restore_rows", "dc_dense", "dc_dense_backward", "dc_graph_norm", "dc_graph_norm_backward"):
+                  "dc_set_layer_norms", "dc_get_layer_norms", "dc_train_keep", "dc_keep_rows", "dc_restore_rows", "dc_dense", "dc_dense_backward", "dc_graph_norm", "dc_graph_norm_backward"):
             getattr(L, n).restype = i32
         _lib = L
     return _lib
@@ -285,6 +289,20 @@ def dc_train_step(ctx, batch: DcBatch, target_ptr, loss_ptr, stream: int = 0) ->
 
 def dc_get_weights(ctx, W_layers: np.ndarray, b_layers: np.ndarray, head: np.ndarray, stream: int = 0) -> int:
     return lib().dc_get_weights(ctx, W_layers.ctypes.data, b_layers.ctypes.data, head.ctypes.data, stream)
+
+
+def dc_set_layer_norms(ctx, groups: int, act: int, eps: float, gamma: Optional[np.ndarray], beta: Optional[np.ndarray],
+                       stream: int = 0) -> int:
+    return lib().dc_set_layer_norms(ctx, groups, act, eps, None if gamma is None else gamma.ctypes.data,
+                                    None if beta is None else beta.ctypes.data, stream)
+
+
+def dc_get_layer_norms(ctx, gamma: np.ndarray, beta: np.ndarray, stream: int = 0) -> int:
+    return lib().dc_get_layer_norms(ctx, gamma.ctypes.data, beta.ctypes.data, stream)
+
+
+def dc_train_keep(ctx, which: int) -> int:
+    return lib().dc_train_keep(ctx, which)
 
 
 def dc_keep_rows(ctx, dtype: int, rows: int, cols: int, x_ptr, ldx: int, out: DcKeptRows, stream: int = 0) -> int:
@@ -527,12 +545,30 @@ class Evaluator:
         self._ok(dc_search(self.ctx, graph, p, labels, r, self._stream()), "dc_search")
         return labels, r
 
+    def set_layer_norms(self, groups: int, gamma=None, beta=None, act: str = "silu", eps: float = 1e-5):
+        """Residual layers with a norm in front (see dc_set_layer_norms); groups = 0: ReLU layers again."""
+        g = [None if v is None else np.ascontiguousarray(v, dtype=np.float32) for v in (gamma, beta)]
+        for v in g:
+            if v is not None and v.size != (self.cfg.L - 1) * self.cfg.H:
+                raise ValueError("gamma and beta: need [L - 1, H]")
+        self._ok(dc_set_layer_norms(self.ctx, groups, self._act(act), eps, g[0], g[1], self._stream()), "dc_set_layer_norms")
+
+    def get_layer_norms(self):
+        gamma = np.empty((self.cfg.L - 1, self.cfg.H), np.float32)
+        beta = np.empty_like(gamma)
+        self._ok(dc_get_layer_norms(self.ctx, gamma, beta, self._stream()), "dc_get_layer_norms")
+        return gamma, beta
+
     # ---- training of the estimator ----
     def num_params(self) -> int:
         return dc_num_params(self.ctx)
 
     def train_begin(self, lr: float, max_samples: int, max_rows: int, beta1: float = 0.9, beta2: float = 0.999,
-                    eps: float = 1e-8, floor: float = 1e-6):
+                    eps: float = 1e-8, floor: float = 1e-6, keep: str = "f32"):
+        """keep: what a pass keeps of every layer's rows, "f32" or "8bit" (see dc_train_keep)."""
+        if keep not in ("f32", "8bit"):
+            raise ValueError(f"keep: 'f32' or '8bit', not {keep!r}")
+        self._ok(dc_train_keep(self.ctx, DC_KEEP_8BIT if keep == "8bit" else DC_KEEP_F32), "dc_train_keep")
         p = DcTrainParams(lr, beta1, beta2, eps, floor, max_samples, max_rows)
         self._ok(dc_train_begin(self.ctx, p, self._stream()), "dc_train_begin")
 
@@ -611,7 +647,9 @@ class Evaluator:
         rows, cols = kept.rows, kept.cols
         if out is None:
             out = self.torch.empty((rows, cols), dtype=dtype or self.torch.float32, device=self.device)
-        ld = self._matrix(out, "out", cols, rows, dtype)
+        elif dtype is not None and out.dtype != dtype:
+            raise ValueError(f"out: need {dtype}, not {out.dtype}")
+        ld = self._matrix(out, "out", cols, rows)
         self._ok(dc_restore_rows(self.ctx, self._type(out), rows, cols, self._kept(kept, cols, rows).contents, out.data_ptr(),
                                  ld, self._stream()), "dc_restore_rows")
         return out

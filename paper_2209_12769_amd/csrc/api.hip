@@ -62,7 +62,7 @@ struct dc_ctx {
   float* head = nullptr;
   float* att = nullptr;     // attention vectors (DC_AGG_ATTENTION only)
   float* score[2] = {nullptr, nullptr};
-  bool have_weights = false;
+  bool have_weights = false, have_weights_copied = false;
   // base graphs
   BaseGraphs bg{};
   char* bg_mem = nullptr;
@@ -87,11 +87,17 @@ struct dc_ctx {
   std::vector<int> h_gno, h_geo;   // host copies of the base graphs' offsets
   int allow_fused = 1;
   int every_fused_op = 0;        // 1: the estimator also runs on fused ops that repeat an earlier one of the batch
+  // deep estimators (dc_set_layer_norms)
+  bool deep = false;
+  LayerNorms norms{};            // gamma | beta lie one behind the other
+  char* norm_mem = nullptr;
   // training (dc_train_begin)
+  int keep8 = 0;                 // what the next dc_train_begin lays out (dc_train_keep)
   bool training = false;
   dc_train_params tp{};
   long long train_t = 0;         // Adam steps taken
   char* train_mem = nullptr;
+  LayerNorms train_norms{};
   TrainPass tb{};                // the buffers of a pass
   unsigned short* train_WTs = nullptr;   // pieces of the transposed matrices (TrainPass::WTs)
   float* adam_m = nullptr;
@@ -107,7 +113,7 @@ const char* const kFamilyNames[kFamCount] = {"prep_scan", "contract", "finalize"
                                              "attention_project", "attention_scores", "attention_aggregate",
                                              "readout_head", "simulate", "fused_op_extract", "fused_op_head",
                                              "train_aggregate", "train_update", "train_head", "train_wgrad",
-                                             "train_dgrad", "train_gather_back", "train_adam"};
+                                             "train_dgrad", "train_gather_back", "train_adam", "graph_norm", "train_keep"};
 
 size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -284,6 +290,13 @@ int nseg_of(const dc_config& c) { return c.aggregator == DC_AGG_ATTENTION ? 1 : 
 
 dc_status do_forward(dc_ctx* ctx, int32_t n_cand, const BatchView& in, float* pred, hipStream_t s) {
   GnnArgs g = gnn_args(ctx, n_cand, in, pred);
+  LayerNorms norms = ctx->norms;
+  if (ctx->deep) {
+    norms.node_off = in.node_off;
+    norms.n_graphs = n_cand;
+    norms.rows = in.cap_nodes < norms.rows ? in.cap_nodes : norms.rows;
+    g.norms = &norms;
+  }
   g.fuse_readout = 1;                        // nothing but the readout looks at the last layer's rows here
   hipError_t e = launch_gnn_forward(g, ctx->prof.on ? &ctx->prof : nullptr, s);
   if (e != hipSuccess) return hip_fail(ctx, e, "forward launch");
@@ -388,6 +401,14 @@ dc_status do_module_times(dc_ctx* ctx, int32_t n_cand, const int32_t* cand_graph
   // the layer kernels only need the total row count: the batch is handed over as one graph
   GnnArgs g = gnn_args(ctx, 1, a.fb, nullptr);
   g.node_off = a.totals;
+  LayerNorms norms = ctx->norms;
+  if (ctx->deep) {                                // the norms run over each fused op
+    norms.node_off = a.fb.node_off;
+    norms.n_graphs = (int)a.cap_ops;
+    norms.n_graphs_dev = a.totals + 3;
+    norms.rows = a.cap_rows;
+    g.norms = &norms;
+  }
   const void* h_last = nullptr;
   e = launch_gnn_layers(g, prof, s, &h_last);
   if (e != hipSuccess) return hip_fail(ctx, e, "fused-op forward launch");
@@ -558,6 +579,7 @@ dc_status dc_destroy(dc_ctx* ctx) {
   if (ctx->slab) (void)hipFree(ctx->slab);
   if (ctx->sim_scratch) (void)hipFree(ctx->sim_scratch);
   if (ctx->train_mem) (void)hipFree(ctx->train_mem);
+  if (ctx->norm_mem) (void)hipFree(ctx->norm_mem);
   delete ctx;
   return DC_OK;
 }
@@ -600,6 +622,13 @@ static void refresh_pieces(dc_ctx* ctx, hipStream_t s) {
   launch_pack_split(jobs, n, s);
 }
 
+// The layer matrices of a deep bf16 estimator row by row.
+static void refresh_row_major(dc_ctx* ctx, hipStream_t s) {
+  if (ctx->cfg.dtype != DC_BF16 || !ctx->have_weights_copied) return;
+  launch_row_major(static_cast<const unsigned short*>(ctx->W), (long long)packed_weight_elems(ctx->cfg.F, ctx->cfg.H, ctx->cfg.L, 3), ctx->cfg.H,
+                   static_cast<unsigned short*>(const_cast<void*>(ctx->norms.W)), s);
+}
+
 static dc_status set_weights_common(dc_ctx* ctx, const float* W_layers, const float* att, const float* b_layers,
                                     const float* head, hipStream_t s) {
   const dc_config& c = ctx->cfg;
@@ -631,6 +660,7 @@ static dc_status set_weights_common(dc_ctx* ctx, const float* W_layers, const fl
   pack_weights_host(head, c.H, c.H, 1, 1, bf16, hw.data());
   pack_weights_host(head + HH + c.H, c.H, c.H, 1, 1, bf16, hw.data() + HH * es);
   hipError_t e = hipMemcpyAsync(ctx->W, packed.data(), nW * es, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) ctx->have_weights_copied = true;
   if (e == hipSuccess) e = hipMemcpyAsync(ctx->headW, hw.data(), hw.size(), hipMemcpyHostToDevice, s);
   if (e == hipSuccess) e = hipMemcpyAsync(ctx->b, b_layers, (size_t)c.L * c.H * sizeof(float), hipMemcpyHostToDevice, s);
   if (e == hipSuccess) e = hipMemcpyAsync(ctx->head, hd.data(), hd.size() * sizeof(float), hipMemcpyHostToDevice, s);
@@ -644,6 +674,7 @@ static dc_status set_weights_common(dc_ctx* ctx, const float* W_layers, const fl
     e = hipMemcpyAsync(ctx->Wx, wx.data(), wx.size() * sizeof(unsigned short), hipMemcpyHostToDevice, s);
   }
   if (e == hipSuccess) refresh_pieces(ctx, s);
+  if (e == hipSuccess && ctx->deep) refresh_row_major(ctx, s);
   if (e == hipSuccess) e = hipGetLastError();
   if (e == hipSuccess) e = hipStreamSynchronize(s);   // host staging buffers die at return
   if (e != hipSuccess) return hip_fail(ctx, e, "weight copy");
@@ -1121,6 +1152,7 @@ __global__ void zero_kernel(float* p, long long n) {
     p[i] = 0.f;
 }
 
+size_t n_norm_params(const dc_ctx* ctx) { return ctx->deep ? 2 * (size_t)(ctx->cfg.L - 1) * ctx->cfg.H : 0; }
 size_t n_layer_weights(const dc_config& c) { return packed_weight_elems(c.F, c.H, c.L, 3); }
 size_t n_head_params(const dc_config& c) { return 2 * (size_t)c.H * c.H + 3 * (size_t)c.H + 1; }
 
@@ -1163,7 +1195,7 @@ dc_status train_pass(dc_ctx* ctx, const dc_batch* in, const float* target, float
 
 int64_t dc_num_params(const dc_ctx* ctx) {
   if (!ctx || ctx->cfg.aggregator != DC_AGG_MEAN) return 0;
-  return (int64_t)(n_layer_weights(ctx->cfg) + (size_t)ctx->cfg.L * ctx->cfg.H + n_head_params(ctx->cfg));
+  return (int64_t)(n_layer_weights(ctx->cfg) + (size_t)ctx->cfg.L * ctx->cfg.H + n_head_params(ctx->cfg) + n_norm_params(ctx));
 }
 
 dc_status dc_train_begin(dc_ctx* ctx, const dc_train_params* params, void* stream) {
@@ -1192,12 +1224,22 @@ dc_status dc_train_begin(dc_ctx* ctx, const dc_train_params* params, void* strea
   const size_t P = (size_t)dc_num_params(ctx);
   const int S = train_slabs(ctx->n_cu, c.F, c.H);
   TrainPass t{};
+  char* norm_workspace = nullptr;
   float *m = nullptr, *v = nullptr;
   for (int pass = 0; pass < 2; ++pass) {
     Arena a;
     a.base = pass ? ctx->train_mem : nullptr;
-    t.hs = a.take<float>((size_t)c.L * R * H);
-    t.means = a.take<float>((size_t)c.L * 2 * R * dmax);
+    // every layer's rows in fp32, or in 8 bits and one place for each kind of rows
+    const size_t kept = ctx->keep8 ? 1 : (size_t)c.L, inner = c.L > 1 ? (size_t)c.L - 1 : 0;
+    t.hs = a.take<float>(ctx->keep8 ? 0 : (size_t)c.L * R * H);
+    t.means = a.take<float>(kept * 2 * R * dmax);
+    t.us = a.take<float>(ctx->keep8 ? R * H : (ctx->deep ? inner * R * H : 0));
+    t.code = a.take<signed char>(ctx->keep8 ? inner * R * H : 0);
+    t.exponent = a.take<unsigned char>(ctx->keep8 ? inner * R * (H / kKeptBlock) : 0);
+    const size_t stats = ctx->deep ? (ctx->keep8 ? 1 : inner) * B * ctx->norms.groups : 0;
+    t.nmean = a.take<float>(stats);
+    t.nrstd = a.take<float>(stats);
+    norm_workspace = a.take<char>(ctx->deep ? graph_norm_bytes(p.max_rows, (int)p.max_samples, c.H, ctx->norms.groups, true, ctx->n_cu) : 0);
     t.dA = a.take<float>(R * 3 * H);
     t.R = a.take<float>(B * H);
     t.Z1 = a.take<float>(B * H);
@@ -1231,6 +1273,11 @@ dc_status dc_train_begin(dc_ctx* ctx, const dc_train_params* params, void* strea
   t.dZ[1] = static_cast<float*>(ctx->act[1]);
   t.slabs = S;
   t.max_rows = p.max_rows;
+  t.max_samples = p.max_samples;
+  t.keep8 = ctx->keep8;
+  ctx->train_norms = ctx->norms;
+  ctx->train_norms.workspace = norm_workspace;
+  t.norms = ctx->deep ? &ctx->train_norms : nullptr;
   t.status = ctx->status;
   t.n_cu = ctx->n_cu;
   t.WTs = ctx->train_WTs;
@@ -1347,6 +1394,9 @@ dc_status dc_train_step(dc_ctx* ctx, const dc_batch* in, const float* target, fl
   if (e == hipSuccess)
     e = launch_adam(ctx->b, g + nW, ctx->adam_m + nW, ctx->adam_v + nW, nb, p.lr, p.beta1, p.beta2, p.eps, c1, c2,
                     ctx->status, s);
+  if (e == hipSuccess)
+    e = launch_adam(const_cast<float*>(ctx->norms.gamma), g + nW + nb + nh, ctx->adam_m + nW + nb + nh, ctx->adam_v + nW + nb + nh,
+                    (long long)n_norm_params(ctx), p.lr, p.beta1, p.beta2, p.eps, c1, c2, ctx->status, s);
   if (e == hipSuccess)
     e = launch_adam(ctx->head, g + nW + nb, ctx->adam_m + nW + nb, ctx->adam_v + nW + nb, nh, p.lr, p.beta1, p.beta2,
                     p.eps, c1, c2, ctx->status, s);
@@ -1514,6 +1564,89 @@ dc_status graph_norm_check(dc_ctx* ctx, const dc_graph_norm_args* a, bool backwa
   return DC_OK;
 }
 }  // namespace
+
+dc_status dc_set_layer_norms(dc_ctx* ctx, int32_t groups, int32_t act, float eps, const float* gamma, const float* beta, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  const dc_config& c = ctx->cfg;
+  if (c.aggregator != DC_AGG_MEAN) return fail(ctx, DC_ERR_UNSUPPORTED, "layer norms need a context with DC_AGG_MEAN");
+  if (groups < 0 || (groups > 0 && c.H % groups)) return fail(ctx, DC_ERR_INVALID_ARG, "groups must divide H (0: no norms)");
+  if (groups > 0 && (act < DC_ACT_NONE || act > DC_ACT_SILU || !(eps > 0.f) || (c.L > 1 && (!gamma || !beta))))
+    return fail(ctx, DC_ERR_INVALID_ARG, "need an activation, eps > 0, gamma and beta");
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Caps k = caps_of(c);
+  LayerNorms n{};
+  char* mem = nullptr;
+  if (groups > 0) {
+    const size_t H = (size_t)c.H, inner = (size_t)c.L - 1;
+    const long long graphs = k.C > k.NB / 2 + 1 ? k.C : k.NB / 2 + 1;      // candidates, or fused ops of two or more rows
+    for (int pass = 0; pass < 2; ++pass) {
+      Arena a;
+      a.base = mem;
+      float* gb = a.take<float>(2 * inner * H + 1);
+      n.gamma = gb;
+      n.beta = gb ? gb + inner * H : nullptr;
+      n.W = a.take<unsigned short>(c.dtype == DC_BF16 ? packed_weight_elems(c.F, c.H, c.L, 3) : 0);
+      n.mean = a.take<float>((size_t)graphs * groups);
+      n.rstd = a.take<float>((size_t)graphs * groups);
+      n.workspace = a.take<char>(graph_norm_bytes(k.NN > k.NB ? k.NN : k.NB, (int)graphs, c.H, groups, false, ctx->n_cu));
+      if (pass == 0 && hipMalloc(reinterpret_cast<void**>(&mem), a.off) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(ctx, DC_ERR_OOM, "layer norm allocation failed");
+      }
+    }
+    n.groups = groups;
+    n.act = act;
+    n.eps = eps;
+    n.rows = k.NN;
+    n.status = ctx->status;
+    hipError_t e = hipSuccess;
+    if (inner > 0) {
+      e = hipMemcpyAsync(const_cast<float*>(n.gamma), gamma, inner * H * sizeof(float), hipMemcpyHostToDevice, s);
+      if (e == hipSuccess) e = hipMemcpyAsync(const_cast<float*>(n.beta), beta, inner * H * sizeof(float), hipMemcpyHostToDevice, s);
+    }
+    if (e == hipSuccess) e = hipStreamSynchronize(s);
+    if (e != hipSuccess) {
+      (void)hipFree(mem);
+      return hip_fail(ctx, e, "dc_set_layer_norms copy");
+    }
+  }
+  (void)hipDeviceSynchronize();              // earlier calls may still use the old block
+  if (ctx->norm_mem) (void)hipFree(ctx->norm_mem);
+  ctx->norm_mem = mem;
+  ctx->norms = n;
+  ctx->deep = groups > 0;
+  ctx->training = false;                     // other parameters: dc_train_begin again
+  if (ctx->deep) {
+    refresh_row_major(ctx, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(ctx, e, "layer matrices");
+  }
+  return DC_OK;
+}
+
+dc_status dc_get_layer_norms(dc_ctx* ctx, float* gamma, float* beta, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  if (!ctx->deep) return fail(ctx, DC_ERR_INVALID_ARG, "dc_set_layer_norms has not been called");
+  if (!gamma || !beta) return fail(ctx, DC_ERR_INVALID_ARG, "null array");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const size_t bytes = n_norm_params(ctx) / 2 * sizeof(float);
+  hipError_t e = hipSuccess;
+  if (bytes > 0) {
+    e = hipMemcpyAsync(gamma, ctx->norms.gamma, bytes, hipMemcpyDeviceToHost, s);
+    if (e == hipSuccess) e = hipMemcpyAsync(beta, ctx->norms.beta, bytes, hipMemcpyDeviceToHost, s);
+  }
+  if (e == hipSuccess) e = hipStreamSynchronize(s);
+  return enqueue_result(ctx, e, "dc_get_layer_norms");
+}
+
+dc_status dc_train_keep(dc_ctx* ctx, int32_t which) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  if (which != DC_KEEP_F32 && which != DC_KEEP_8BIT) return fail(ctx, DC_ERR_INVALID_ARG, "DC_KEEP_F32 or DC_KEEP_8BIT");
+  ctx->keep8 = which == DC_KEEP_8BIT;
+  return DC_OK;
+}
 
 dc_status dc_keep_rows(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
                        const dc_kept_rows* out, void* stream) {

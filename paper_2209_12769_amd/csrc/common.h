@@ -68,7 +68,7 @@ struct BatchView {
 };
 
 // Optional per-kernel timing with HIP events on the launch stream.
-enum Family { kFamPrep = 0, kFamContract, kFamFinalize, kFamAggregate, kFamUpdate, kFamFused, kFamLayer256, kFamLayer64, kFamHeavy, kFamDesc, kFamAttProject, kFamAttScores, kFamAttAggregate, kFamReadout, kFamSimulate, kFamFusedOps, kFamFusedHead, kFamTrainAggregate, kFamTrainUpdate, kFamTrainHead, kFamTrainWgrad, kFamTrainDgrad, kFamTrainGatherBack, kFamTrainAdam, kFamCount };
+enum Family { kFamPrep = 0, kFamContract, kFamFinalize, kFamAggregate, kFamUpdate, kFamFused, kFamLayer256, kFamLayer64, kFamHeavy, kFamDesc, kFamAttProject, kFamAttScores, kFamAttAggregate, kFamReadout, kFamSimulate, kFamFusedOps, kFamFusedHead, kFamTrainAggregate, kFamTrainUpdate, kFamTrainHead, kFamTrainWgrad, kFamTrainDgrad, kFamTrainGatherBack, kFamTrainAdam, kFamGraphNorm, kFamTrainKeep, kFamCount };
 struct Profiler {
   bool on = false;
   static constexpr int kCap = 4096;
@@ -110,6 +110,22 @@ hipError_t contract_set_lds_limit(int bytes);
 // ints of the pre-pass's work counters: one counter per XCD, each on a cache line of its own
 constexpr int kHeavyCtrInts = 8 * 32;
 
+// The norms in front of the layers of a deep estimator (dc_set_layer_norms); null in GnnArgs: plain layers.
+struct LayerNorms {
+  int groups, act;
+  float eps;
+  const float* gamma;          // [L - 1][H]: layer l > 0 at (l - 1) H
+  const float* beta;
+  const void* W;               // bf16: the layer matrices row by row (fp32: GnnArgs::W is)
+  const int* node_off;         // graphs that the norms run over
+  int n_graphs;                // or, with n_graphs_dev, the most there can be
+  const int* n_graphs_dev;
+  long long rows;              // the most rows there can be
+  float* mean;                 // [n_graphs, groups]
+  float* rstd;
+  char* workspace;             // graph_norm_bytes()
+  int* status;
+};
 struct GnnArgs {
   int n_cand;
   const int* node_off;
@@ -146,6 +162,7 @@ struct GnnArgs {
   int heads = 0;
   const float* att = nullptr;   // per layer a_src[H] | a_dst[H]
   float* score[2] = {nullptr, nullptr};   // per node and head: a_src . z, a_dst . z  [max_nodes, heads]
+  const LayerNorms* norms = nullptr;
 };
 hipError_t launch_gnn_forward(const GnnArgs& a, Profiler* prof, hipStream_t s);
 // The message-passing layers alone; *h_last receives the final embeddings [node_off[n_cand], H].
@@ -350,7 +367,16 @@ struct TrainPass {
   int* cnt;                    // {0, n_samples}
   float* part;                 // [slabs][3 max(F,H) H + H] partial sums of the weight gradients
   int slabs;
-  long long max_rows;
+  long long max_rows, max_samples;
+  // deep estimators (dc_set_layer_norms): norms.node_off and n_graphs are set by the pass
+  const LayerNorms* norms;     // or null: plain layers
+  float* us;                   // [L - 1][max_rows, H] what the norms leave (keep8: one)
+  float* nmean;                // [L - 1][max_samples, groups] (keep8: one)
+  float* nrstd;
+  // keep8: the layers' outputs in 8 bits instead of hs, and one set of means; hs and per-layer means are not there
+  int keep8;
+  signed char* code;           // [L][max_rows, H]
+  unsigned char* exponent;     // [L][max_rows, H / 32]
   float* grad;                 // [n_params]
   float* loss;                 // [1]
   float* pred;                 // [n_samples] or null

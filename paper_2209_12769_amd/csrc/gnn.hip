@@ -14,7 +14,7 @@
 // synchronisation is needed between contraction and forward pass.
 #include <string.h>
 
-#include "common.h"
+#include "operators.h"
 
 namespace dc {
 namespace {
@@ -851,7 +851,7 @@ bool chunked_readout(const GnnArgs& a) {
   return a.heads == 0 && layer256_supported(a.L > 1 ? a.H : a.F, a.H, a.bf16);
 }
 bool readout_in_last_layer(const GnnArgs& a) {
-  return a.fuse_readout && a.allow_fused && chunked_readout(a) && a.ro_part && a.ro_first;
+  return a.fuse_readout && a.allow_fused && !a.norms && chunked_readout(a) && a.ro_part && a.ro_first;
 }
 
 // Layers with uniform coefficients: mean over predecessors, mean over successors, dense update.
@@ -913,6 +913,7 @@ hipError_t mean_layers(const GnnArgs& a, Profiler* prof, hipStream_t s, const vo
 }  // namespace
 
 hipError_t launch_gnn_layers(const GnnArgs& a, Profiler* prof, hipStream_t s, const void** h_last) {
+  if (a.norms) return launch_norm_layers(a, prof, s, h_last);
   return a.heads > 0 ? attention_layers(a, prof, s, h_last) : mean_layers(a, prof, s, h_last);
 }
 

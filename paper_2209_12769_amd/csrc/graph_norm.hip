@@ -672,8 +672,8 @@ void launch_column_sums(const float* part, int blocks, int n1, float* out1, int 
 }
 
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
-  // what any vector width and type would need
-  const long long cr = chunk_rows(rows, n_cu), nc = (rows + cr - 1) / cr, most = blocks_most(n_cu);
+  // what any vector width and type would need, and any smaller number of rows: chunks of fewer than 512 rows are at most four per CU
+  const long long most = blocks_most(n_cu), by_rows = rows / 512 + 1, nc = by_rows > 4LL * n_cu ? by_rows : 4LL * n_cu + 1;
   const bool chunks = rows > 1024;
   size_t b = chunks ? ((size_t)nc + (size_t)n_graphs + 1) * G * sizeof(double2) : 0;
   if (backward) {

@@ -172,6 +172,11 @@ hipError_t launch_graph_norm_back(const GraphNormArgs& a, hipStream_t s);
 // out1 [n1] | out2 [n2] = sums over `blocks` rows of part [blocks, n1 + n2], in 64 bits and a fixed order.
 void launch_column_sums(const float* part, int blocks, int n1, float* out1, int n2, float* out2, const int* stop, hipStream_t s);
 
+// norm_layers.hip: the layers of a deep estimator, and the arguments of its norm in front of layer l
+hipError_t launch_norm_layers(const GnnArgs& a, Profiler* prof, hipStream_t s, const void** h_last);
+GraphNormArgs norm_args(const LayerNorms& n, int l, int H, int bf16, int n_cu);
+void launch_row_major(const unsigned short* packed, long long n, int H, unsigned short* out, hipStream_t s);
+
 // ---- kept rows ----
 struct KeepArgs {
   long long rows;

@@ -10,7 +10,13 @@
 // index is the row of the batch (transposed-A product, split over slabs of rows, partial
 // results reduced in a fixed order, so a pass is bit-reproducible).  Everything else is
 // bandwidth-bound and done by plain grid-stride kernels.  Adam as published by Kingma & Ba.
-#include "common.h"
+//
+// Deep estimators (dc_set_layer_norms): u = act(norm(h_l)), h_{l+1} = h_l + [u | means of u] W_l + b_l above the first
+// layer, no ReLU; the reverse pass hands dh past each layer and adds what comes back through the norm.
+// keep8 (dc_train_keep): a pass keeps one byte and 1/32 per value of a layer's output where it else keeps 12 (16 with norms):
+// the output, its two means and what the norm leaves.  The reverse pass reads the rows back and forms means and
+// norm (with the statistics of the rows as they were kept) again.
+#include "operators.h"
 
 namespace dc {
 namespace {
@@ -149,7 +155,7 @@ __global__ __launch_bounds__(256) void top_kernel(const float* __restrict__ dR, 
     const long long v = i / cpr;
     const int ch = (int)(i - v * cpr);
     const float4 g = reinterpret_cast<const float4*>(dR)[(size_t)gid[v] * cpr + ch];
-    const float4 a = reinterpret_cast<const float4*>(hL)[i];
+    const float4 a = hL ? reinterpret_cast<const float4*>(hL)[i] : make_float4(1.f, 1.f, 1.f, 1.f);   // null: no ReLU
     reinterpret_cast<float4*>(dZ)[i] = make_float4(a.x > 0.f ? g.x : 0.f, a.y > 0.f ? g.y : 0.f,
                                                    a.z > 0.f ? g.z : 0.f, a.w > 0.f ? g.w : 0.f);
   }
@@ -186,7 +192,7 @@ __global__ __launch_bounds__(256) void gather_back_kernel(const float* __restric
       const float4 x = A4[(size_t)v * 3 * cpr + 2 * cpr + ch];
       acc.x += x.x * sc; acc.y += x.y * sc; acc.z += x.z * sc; acc.w += x.w * sc;
     }
-    const float4 a = reinterpret_cast<const float4*>(h)[i];
+    const float4 a = h ? reinterpret_cast<const float4*>(h)[i] : make_float4(1.f, 1.f, 1.f, 1.f);     // null: no ReLU below
     reinterpret_cast<float4*>(dZ)[i] = make_float4(a.x > 0.f ? acc.x : 0.f, a.y > 0.f ? acc.y : 0.f,
                                                    a.z > 0.f ? acc.z : 0.f, a.w > 0.f ? acc.w : 0.f);
   }
@@ -348,6 +354,44 @@ hipError_t launch_train_pass(const TrainPass& t, Profiler* prof, hipStream_t s) 
   float* gb2 = gW2 + HH;
   float* gw3 = gb2 + H;
   float* gb3 = gw3 + H;
+  float* ggamma = gb3 + 1;                     // [L - 1][H] each, with norms
+  float* gbeta = ggamma + (size_t)(L - 1) * H;
+  LayerNorms norms{};
+  if (t.norms) {
+    norms = *t.norms;
+    norms.node_off = t.node_off;
+    norms.n_graphs = B;
+    norms.rows = t.max_rows;
+  }
+  const bool deep = t.norms != nullptr;
+  // what a pass keeps: layer l's input (l > 0), its norm and its means, or one place each that every layer uses
+  const size_t RH = (size_t)t.max_rows * H;
+  auto means_of = [&](int l) { return t.means + (t.keep8 ? 0 : (size_t)(2 * l) * t.max_rows * (F > H ? F : H)); };
+  auto u_of = [&](int l) { return t.us + (t.keep8 ? 0 : (size_t)(l - 1) * RH); };
+  auto norm_of = [&](int l) {
+    GraphNormArgs a = norm_args(norms, l, H, 0, t.n_cu);
+    const size_t at = t.keep8 ? 0 : (size_t)(l - 1) * t.max_samples * norms.groups;
+    a.mean = t.nmean + at;
+    a.rstd = t.nrstd + at;
+    return a;
+  };
+  auto kept_of = [&](int l) {                  // output of layer l - 1
+    KeepArgs k{};
+    k.rows = t.max_rows;
+    k.nrows = t.node_off + B;
+    k.cols = H;
+    k.ld = k.ld_code = H;
+    k.ld_exponent = H / kKeptBlock;
+    k.code = t.code + (size_t)(l - 1) * RH;
+    k.exponent = t.exponent + (size_t)(l - 1) * (RH / kKeptBlock);
+    k.stop = t.status;
+    k.n_cu = t.n_cu;
+    return k;
+  };
+  hipError_t err = hipSuccess;
+  auto run = [&](hipError_t e) {
+    if (err == hipSuccess) err = e;
+  };
 
   hipLaunchKernelGGL(set_count_kernel, dim3(1), dim3(1), 0, s, t.cnt, B);
   hipLaunchKernelGGL(gid_kernel, dim3(grid_for(rows_cap, t.n_cu)), dim3(256), 0, s, t.node_off, B, t.gid, t.status);
@@ -360,15 +404,56 @@ hipError_t launch_train_pass(const TrainPass& t, Profiler* prof, hipStream_t s) 
   const float* Wl = t.W;
   const float* bl = t.b;
   for (int l = 0; l < L; ++l) {
-    float* hn = t.hs + (size_t)l * rows_cap * H;
-    float* mp = t.means + (size_t)(2 * l) * rows_cap * dmax;      // both means are kept for the reverse pass
+    // keep8: in the two buffers that the reverse pass uses later (deep: one, to which the layers add in place)
+    float* hn = t.keep8 ? t.dZ[deep ? 0 : l & 1] : t.hs + (size_t)l * rows_cap * H;
+    float* mp = means_of(l);
     float* ms = mp + (size_t)rows_cap * dmax;
+    const float* src = hcur;
+    if (deep && l > 0) {
+      GraphNormArgs a = norm_of(l);
+      a.X = hcur;
+      a.Y = u_of(l);
+      begin(kFamGraphNorm);
+      run(launch_graph_norm(a, s));
+      end();
+      src = u_of(l);
+    }
     begin(kFamTrainAggregate);
-    launch_mean_aggregate(g, hcur, d, mp, ms, s);
+    launch_mean_aggregate(g, src, d, mp, ms, s);
     end();
     begin(kFamTrainUpdate);
-    launch_dense_update(g, hcur, mp, ms, d, 3, Wl, bl, hn, s);
+    if (deep) {
+      DenseArgs p{};
+      p.rows = rows_cap;
+      p.nrows = nrows;
+      p.d = d;
+      p.nseg = 3;
+      p.N = H;
+      p.X[0] = src;
+      p.X[1] = mp;
+      p.X[2] = ms;
+      p.ldx = d;
+      p.W = Wl;
+      p.ldw = H;
+      p.bias = bl;
+      p.R = l > 0 ? hcur : nullptr;
+      p.ldr = H;
+      p.Y = hn;
+      p.ldy = H;
+      p.stop = t.status;
+      p.n_cu = t.n_cu;
+      run(launch_dense(p, s));
+    } else {
+      launch_dense_update(g, src, mp, ms, d, 3, Wl, bl, hn, s);
+    }
     end();
+    if (t.keep8 && t.grad && l < L - 1) {               // nothing asks for the last layer's rows again
+      KeepArgs k = kept_of(l + 1);
+      k.src = hn;
+      begin(kFamTrainKeep);
+      run(launch_keep_rows(k, s));
+      end();
+    }
     Wl += (size_t)3 * d * H;
     bl += H;
     hcur = hn;
@@ -384,7 +469,7 @@ hipError_t launch_train_pass(const TrainPass& t, Profiler* prof, hipStream_t s) 
   hipLaunchKernelGGL(loss_reduce_kernel, dim3(1), dim3(1024), 0, s, t.lterm, B, t.loss, t.status);
   if (!t.grad) {
     end();
-    return hipGetLastError();
+    return err == hipSuccess ? hipGetLastError() : err;
   }
 
   // ---- regression network, reverse ----
@@ -402,22 +487,44 @@ hipError_t launch_train_pass(const TrainPass& t, Profiler* prof, hipStream_t s) 
   data_gradient(gh, t.dZ1, H, W1, WTs, t.dR, s);
 
   // ---- graph layers, reverse ----
-  float* dZ = t.dZ[0];
-  float* dZn = t.dZ[1];
-  hipLaunchKernelGGL(top_kernel, dim3(grid_for(rows_cap * (H / 4), t.n_cu)), dim3(256), 0, s, t.dR, t.gid, hcur, nrows,
-                     H, dZ, t.status);
+  // keep8, plain layers: the last output lies in one of the two buffers and is asked for its ReLU
+  float* dZ = t.dZ[t.keep8 && !deep ? L & 1 : 0];
+  float* dZn = t.dZ[t.keep8 && !deep ? (L & 1) ^ 1 : 1];
+  hipLaunchKernelGGL(top_kernel, dim3(grid_for(rows_cap * (H / 4), t.n_cu)), dim3(256), 0, s, t.dR, t.gid,
+                     deep ? static_cast<const float*>(nullptr) : hcur, nrows, H, dZ, t.status);
   end();
   GnnArgs g3 = g;
   g3.H = 3 * H;                                // dA = dZ W^T is [rows, 3H] for the layers above the first
   for (int l = L - 1; l >= 0; --l) {
     const int dl = l == 0 ? F : H;
-    const float* hl = l == 0 ? t.X : t.hs + (size_t)(l - 1) * rows_cap * H;
+    const float* hl = l == 0 ? t.X : (t.keep8 ? t.us : t.hs + (size_t)(l - 1) * rows_cap * H);
+    const float* in = l > 0 && deep ? u_of(l) : hl;            // what the layer's product took
     size_t woff = 0;
     for (int k = 0; k < l; ++k) woff += (size_t)3 * (k == 0 ? F : H) * H;
-    const float* mp = t.means + (size_t)(2 * l) * rows_cap * dmax;
-    const float* ms = mp + (size_t)rows_cap * dmax;
+    float* mp = means_of(l);
+    float* ms = mp + (size_t)rows_cap * dmax;
+    if (t.keep8) {                                             // rows read back, norm and means formed again
+      if (l > 0) {
+        KeepArgs k = kept_of(l);
+        k.dst = deep ? dZn : t.us;
+        begin(kFamTrainKeep);
+        run(launch_restore_rows(k, s));
+        end();
+      }
+      if (l > 0 && deep) {
+        GraphNormArgs a = norm_of(l);
+        a.X = dZn;
+        a.Y = u_of(l);
+        begin(kFamGraphNorm);
+        run(launch_graph_norm(a, s));
+        end();
+      }
+      begin(kFamTrainAggregate);
+      launch_mean_aggregate(g, in, dl, mp, ms, s);
+      end();
+    }
     begin(kFamTrainWgrad);
-    weight_gradient(t, hl, mp, ms, dl, 3, dZ, H, nrows, gWl + woff, gbl + (size_t)l * H, s);
+    weight_gradient(t, in, mp, ms, dl, 3, dZ, H, nrows, gWl + woff, gbl + (size_t)l * H, s);
     end();
     if (l == 0) break;
     begin(kFamTrainDgrad);
@@ -425,13 +532,31 @@ hipError_t launch_train_pass(const TrainPass& t, Profiler* prof, hipStream_t s) 
     end();
     begin(kFamTrainGatherBack);
     hipLaunchKernelGGL(gather_back_kernel, dim3(grid_for(rows_cap * (H / 4), t.n_cu)), dim3(256), 0, s, t.dA, H,
-                       t.in_rowptr, t.in_col, t.out_rowptr, t.out_col, hl, nrows, dZn, t.status);
+                       t.in_rowptr, t.in_col, t.out_rowptr, t.out_col, deep ? static_cast<const float*>(nullptr) : hl, nrows, dZn,
+                       t.status);
     end();
+    if (deep) {                                                // through the norm, and past the layer
+      GraphNormArgs a = norm_of(l);
+      if (t.keep8) {
+        const KeepArgs k = kept_of(l);
+        a.kept = KeptView{k.code, k.exponent, k.ld_code, k.ld_exponent};
+      } else {
+        a.X = hl;
+      }
+      a.dY = dZn;
+      a.dRes = dZ;
+      a.dX = dZn;
+      a.dgamma = ggamma + (size_t)(l - 1) * H;
+      a.dbeta = gbeta + (size_t)(l - 1) * H;
+      begin(kFamGraphNorm);
+      run(launch_graph_norm_back(a, s));
+      end();
+    }
     float* tmp = dZ;
     dZ = dZn;
     dZn = tmp;
   }
-  return hipGetLastError();
+  return err == hipSuccess ? hipGetLastError() : err;
 }
 
 hipError_t launch_adam(float* theta, const float* grad, float* m, float* v, long long n, float lr, float beta1,

@@ -1,0 +1,269 @@
+"""Deep estimators (residual layers with a norm in front) and training with rows kept in 8 bits, through the framework's own
+calls: estimates, Cost(H'), gradients and Adam steps against the 64-bit oracle.
+
+Tolerances: those of the plain estimator's tests.  fp32 estimates within 1e-5 of their size, bf16 within 2e-2 (time-like head);
+a gradient tensor within 1e-5 of its largest entry.  With rows kept in 8 bits a value whose 127ths lie within fp32's
+rounding of a half may be kept one step apart from the oracle's: a tensor is within 2e-3 in norm (some values in 1000 off by
+a step of 2^-6 of their block's largest would be 1e-3)."""
+import numpy as np
+import pytest
+
+from oracle import deep
+from oracle import oracle as orc
+from oracle import train as ot
+from paper_2209_12769_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-3
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2209_12769_amd import binding
+    binding.lib()
+    return binding
+
+
+def norms(H, L, seed=7):
+    rng = np.random.default_rng(seed)
+    f = lambda v: v.astype(np.float32)
+    return f(1 + 0.2 * rng.standard_normal((L - 1, H))), f(0.2 * rng.standard_normal((L - 1, H)))
+
+
+def workload(F, H, L, dtype, n=60, C=7, seed=5):
+    g = wl.random_dag(seed, n, 0.1, F)
+    w = wl.custom("deep", wl.ModelSpec(F, H, L, dtype), [g], [wl.random_labels(seed, n, n // 2, C)], seed=seed, std=0.5 / np.sqrt(3 * H))
+    w.weights.head[-H - 1:-1] = np.abs(w.weights.head[-H - 1:-1])
+    w.weights.head[-1] += 3.0
+    return w
+
+
+def oracle_predictions(w, gamma, beta, groups, name):
+    b = orc.contract(w)
+    p = ot.Params.from_weights(w.weights, w.model.F, w.model.H, w.model.L)
+    return deep.forward(b, p, gamma, beta, groups, EPS, name)[0]
+
+
+@pytest.mark.parametrize("dtype,tol", [("f32", 1e-5), ("bf16", 2e-2)])
+@pytest.mark.parametrize("F,H,L,groups,name", [(16, 32, 2, 4, "relu"), (32, 128, 6, 8, "silu"), (64, 256, 4, 1, "gelu"), (48, 96, 3, 32, "none"), (16, 64, 1, 2, "silu")])
+def test_estimates(B, dtype, tol, F, H, L, groups, name):
+    w = workload(F, H, L, dtype)
+    gamma, beta = norms(H, L)
+    ev = B.evaluator_for(w)
+    cg, co, gid = ev.to_device(w.cand_graph), ev.to_device(w.cand_off), ev.to_device(w.group_id)
+    plain = ev.eval_candidates(cg, co, gid).cpu().numpy()
+    ev.set_layer_norms(groups, gamma, beta, name, EPS)
+    got = ev.eval_candidates(cg, co, gid).cpu().numpy()
+    assert ev.check() == B.DC_OK, B.dc_last_error(ev.ctx)
+    ref = oracle_predictions(w, gamma, beta, groups, name)
+    assert np.abs(got - ref).max() <= tol * np.abs(ref).max()
+    # weights set again afterwards, the two halves called on their own
+    ev.set_weights(w.weights)
+    nb, eb = int(w.cand_off[-1]), w.n_cand * w.graphs[0].e
+    batch = ev.contract_graphs(cg, co, gid, ev.alloc_batch(w.n_cand, nb, nb, eb))
+    again = ev.gnn_forward(batch).cpu().numpy()
+    assert np.abs(again - ref).max() <= tol * np.abs(ref).max()
+    a, b = ev.get_layer_norms()
+    assert np.array_equal(a, gamma) and np.array_equal(b, beta)
+    # and back to the plain layers: their bits
+    ev.set_layer_norms(0)
+    assert np.array_equal(ev.eval_candidates(cg, co, gid).cpu().numpy(), plain)
+    ev.close()
+
+
+@pytest.mark.parametrize("dtype,tol", [("f32", 2e-5), ("bf16", 2e-2)])
+def test_module_times(B, dtype, tol):
+    """Cost(H'): the norms run over the ops of each fused op; repeated fused ops take the first one's estimate."""
+    base = wl.make("cfg2", 1)
+    g, H, L, groups = base.graphs[0], 64, 4, 4
+    lab = wl.training_labels(g, 3, 2, kmax=24)
+    w = wl.custom("deep-cost", wl.ModelSpec(base.model.F, H, L, dtype), [g], [np.concatenate([lab, lab])], seed=3)
+    w.weights.head[-H - 1:-1] = np.abs(w.weights.head[-H - 1:-1])
+    w.weights.head[-1] += 3.0
+    gamma, beta = norms(H, L)
+    t, x = wl.profile_of(w)
+    ev = B.evaluator_for(w)
+    ev.set_profile(t, x)
+    ev.set_layer_norms(groups, gamma, beta, "silu", EPS)
+    cg, co, gid = ev.to_device(w.cand_graph), ev.to_device(w.cand_off), ev.to_device(w.group_id)
+    nb, eb = int(w.cand_off[-1]), w.n_cand * g.e
+    op_time, _ = ev.module_times(cg, co, gid, ev.alloc_batch(w.n_cand, nb, nb, eb))
+    assert ev.check() == B.DC_OK, B.dc_last_error(ev.ctx)
+    c = orc.contract(w)
+    fo, cnode, _ = orc.fused_ops(w, c, x)
+    p = ot.Params.from_weights(w.weights, w.model.F, H, L)
+    ref = np.maximum(deep.forward(fo, p, gamma, beta, groups, EPS, "silu")[0], 0)
+    got = op_time.cpu().numpy()[cnode]
+    assert np.abs(got - ref).max() <= tol * np.abs(ref).max()
+    assert ev.last_fused_op_repeats() > 0
+    cost = ev.cost_candidates(cg, co, gid, 0.02, 0.01).cpu().numpy()
+    # a module with a cycle costs infinity whatever its ops take: these labellings, drawn for training, may have one
+    assert np.array_equal(np.isfinite(cost), np.isfinite(orc.cost(w, t, x, 0.02, 0.01))) and np.array_equal(cost[:2], cost[2:])
+    ev.close()
+
+
+@pytest.mark.parametrize("dtype,tol", [("f32", 2e-5), ("bf16", 2e-2)])
+def test_cost(B, dtype, tol):
+    """Cost(H') of fusion candidates without cycles: the fused ops' estimates through the simulator."""
+    base = wl.make("cfg2", 5)
+    H, L, groups = 64, 3, 8
+    w = wl.custom("deep-cost", wl.ModelSpec(base.model.F, H, L, dtype), base.graphs, [base.group_id.reshape(5, -1)], seed=3)
+    positive_head(w)
+    gamma, beta = norms(H, L)
+    t, x = wl.profile_of(w)
+    ev = B.evaluator_for(w)
+    ev.set_profile(t, x)
+    ev.set_layer_norms(groups, gamma, beta, "silu", EPS)
+    cg, co, gid = ev.to_device(w.cand_graph), ev.to_device(w.cand_off), ev.to_device(w.group_id)
+    got = ev.cost_candidates(cg, co, gid, 0.02, 0.01).cpu().numpy()
+    assert ev.check() == B.DC_OK, B.dc_last_error(ev.ctx)
+    c = orc.contract(w)
+    fo, cnode, _ = orc.fused_ops(w, c, x)
+    p = ot.Params.from_weights(w.weights, w.model.F, H, L)
+    nb, eb = int(w.cand_off[-1]), w.n_cand * w.graphs[0].e
+    op_time, ar_size = ev.module_times(cg, co, gid, ev.alloc_batch(w.n_cand, nb, nb, eb))
+    times = op_time.cpu().numpy()[:c.ntot].copy()
+    times[cnode] = np.maximum(deep.forward(fo, p, gamma, beta, groups, EPS, "silu")[0], 0)
+    ref = orc.simulate(c, times, ar_size.cpu().numpy()[:c.ntot], 0.02, 0.01)
+    assert np.isfinite(ref).all() and np.abs(got - ref).max() <= tol * np.abs(ref).max()
+    ev.close()
+
+
+def training(B, F, H, L, C=3, seed=4):
+    g = wl.make("cfg2", 1).graphs[0]
+    w = wl.custom("deep-train", wl.ModelSpec(F, H, L, "f32"), [g], [wl.training_labels(g, seed, C, kmax=20)], seed=seed)
+    return w, g
+
+
+def run_gradient(B, w, g, keep, groups=0, gamma=None, beta=None, name="silu", steps=0):
+    import torch
+    t, x = wl.profile_of(w)
+    nb, eb = w.n_cand * g.n, w.n_cand * g.e
+    ev = B.Evaluator(w.model.F, w.model.H, w.model.L, "f32", nb // 2 + 1, nb, eb)
+    ev.set_base_graphs(w.g_node_off(), w.g_edge_off(), w.cat_rowptr(), w.cat_col(), w.cat_X())
+    ev.set_weights(w.weights)
+    ev.set_profile(t, x)
+    if groups:
+        ev.set_layer_norms(groups, gamma, beta, name, EPS)
+    batch = ev.fused_op_batch(ev.to_device(w.cand_graph), ev.to_device(w.cand_off), ev.to_device(w.group_id), ev.alloc_batch(nb // 2 + 1, nb, nb, eb))
+    fo, _, member = orc.fused_ops(w, orc.contract(w), x)
+    target = wl.synthetic_fused_times(fo.node_off, member, t, 5)
+    ev.train_begin(1e-3, fo.n_cand, fo.ntot, keep=keep)
+    td = torch.from_numpy(target).to(ev.device)
+    loss, pred, grad = ev.loss_gradients(batch, td)
+    assert ev.check() == B.DC_OK, B.dc_last_error(ev.ctx)
+    out = (float(loss.cpu()[0]), pred.cpu().numpy(), grad.cpu().numpy().astype(np.float64), fo, target)
+    losses = []
+    for _ in range(steps):
+        losses.append(ev.train_step(batch, td).clone())
+    if steps:
+        assert ev.check() == B.DC_OK
+        out += (np.concatenate([*ev.get_weights()]), ev.get_layer_norms() if groups else None, [float(v.cpu()[0]) for v in losses])
+    ev.close()
+    return out
+
+
+def tensors(flat, F, H, L, deep_form):
+    o, out = 0, []
+    for shp in ot.Params.shapes(F, H, L) + ([(L - 1, H)] * 2 if deep_form else []):
+        n = int(np.prod(shp))
+        out.append(flat[o:o + n])
+        o += n
+    assert o == flat.size
+    return out
+
+
+def positive_head(w):
+    H = w.model.H
+    w.weights.head[-H - 1:-1] = np.abs(w.weights.head[-H - 1:-1])
+    w.weights.head[-1] += 3.0
+
+
+@pytest.mark.parametrize("F,H,L,groups,name", [(32, 64, 2, 4, "silu"), (32, 128, 6, 8, "gelu"), (32, 96, 3, 1, "silu"), (32, 32, 1, 2, "silu")])
+def test_gradient(B, F, H, L, groups, name):
+    w, g = training(B, F, H, L)
+    positive_head(w)
+    gamma, beta = norms(H, L)
+    p = ot.Params.from_weights(w.weights, F, H, L)
+    for keep, bound in (("f32", None), ("8bit", 2e-3)):
+        loss, pred, grad, fo, target = run_gradient(B, w, g, keep, groups, gamma, beta, name)
+        rl, ry, rg, dga, dbe = deep.loss_and_gradients(fo, target, p, gamma, beta, groups, EPS, name, kept=keep == "8bit")
+        assert abs(loss - rl) <= 2e-5 * rl and np.abs(pred - ry).max() <= 1e-5 * np.abs(ry).max()
+        ref = np.concatenate([rg.flat(), dga.ravel(), dbe.ravel()])
+        for a, b in zip(tensors(grad, F, H, L, True), tensors(ref, F, H, L, True)):
+            if bound is None or L < 2:
+                assert np.abs(a - b).max(initial=0) <= 1e-5 * np.abs(b).max(initial=0)
+            else:
+                assert np.linalg.norm(a - b) <= bound * np.linalg.norm(b)
+
+
+@pytest.mark.parametrize("L", [1, 2, 3, 4])
+def test_plain_layers_in_8_bits(B, L):
+    """ReLU layers with rows kept in 8 bits: loss and estimates are those of the pass that keeps fp32, bit for bit, and so are the
+    gradients of the regression network; the layers' are close."""
+    F, H = 32, 128
+    w, g = training(B, F, H, L)
+    positive_head(w)
+    a = run_gradient(B, w, g, "f32")
+    b = run_gradient(B, w, g, "8bit")
+    assert a[0] == b[0] and np.array_equal(a[1], b[1])
+    ga, gb = tensors(a[2], F, H, L, False), tensors(b[2], F, H, L, False)
+    for k, (x, y) in enumerate(zip(ga, gb)):
+        if k == 0 or k >= L:                                # head, first layer (its input is the caller's), biases
+            assert np.array_equal(x, y), k
+        else:
+            # a value is off by half a step, at most 1/127 of its block's largest, at random; sums over rows average it
+            assert 0 < np.linalg.norm(x - y) <= np.linalg.norm(x) / 64, k
+
+
+def test_steps_train(B):
+    """Adam on all parameters, norms among them: three steps against the oracle's, in fp32; in 8 bits the loss follows."""
+    F, H, L, groups = 32, 64, 3, 4
+    w, g = training(B, F, H, L)
+    positive_head(w)
+    gamma, beta = norms(H, L)
+    out = run_gradient(B, w, g, "f32", groups, gamma, beta, "silu", steps=3)
+    fo, target = out[3], out[4]
+    theta = np.concatenate([ot.Params.from_weights(w.weights, F, H, L).flat(), gamma.ravel(), beta.ravel()]).astype(np.float64)
+    m, v, nP = np.zeros_like(theta), np.zeros_like(theta), theta.size - 2 * gamma.size
+    losses = []
+    for t in range(1, 4):
+        ga, be = theta[nP:nP + gamma.size].reshape(gamma.shape), theta[nP + gamma.size:].reshape(beta.shape)
+        loss, _, gr, dga, dbe = deep.loss_and_gradients(fo, target, ot.Params.from_flat(theta[:nP], F, H, L), ga, be, groups, EPS, "silu")
+        grad = np.concatenate([gr.flat(), dga.ravel(), dbe.ravel()])
+        theta, m, v = ot.adam_step(theta, grad, m, v, t, 1e-3, 0.9, 0.999, 1e-8)
+        losses.append(loss)
+    assert np.allclose(out[7], losses, rtol=1e-4)
+    got = np.concatenate([out[5].astype(np.float64), out[6][0].ravel(), out[6][1].ravel()])
+    # a step moves an entry by up to lr; entries with a tiny gradient may go either way
+    assert np.abs(got - theta).max() <= 3e-3 and np.mean(np.abs(got - theta) <= 6e-5) > 0.99
+    kept = run_gradient(B, w, g, "8bit", groups, gamma, beta, "silu", steps=3)
+    assert np.allclose(kept[7], losses, rtol=5e-2)
+
+
+def test_refusals(B):
+    import torch
+    w = workload(16, 32, 2, "f32")
+    ev = B.evaluator_for(w)
+    gamma, beta = norms(32, 2)
+    st = lambda *a: B.dc_set_layer_norms(ev.ctx, *a)
+    assert st(5, 0, 1e-5, gamma, beta) == B.DC_ERR_INVALID_ARG and st(-1, 0, 1e-5, gamma, beta) == B.DC_ERR_INVALID_ARG
+    assert st(4, 7, 1e-5, gamma, beta) == B.DC_ERR_INVALID_ARG and st(4, 0, 0.0, gamma, beta) == B.DC_ERR_INVALID_ARG
+    assert st(4, 0, 1e-5, None, beta) == B.DC_ERR_INVALID_ARG and B.dc_get_layer_norms(ev.ctx, gamma, beta) == B.DC_ERR_INVALID_ARG
+    assert B.dc_train_keep(ev.ctx, 2) == B.DC_ERR_INVALID_ARG
+    ev.train_begin(1e-3, 4, 64)
+    ev.set_layer_norms(4, gamma, beta)
+    assert ev.num_params() == sum(int(np.prod(s)) for s in ot.Params.shapes(16, 32, 2)) + 64
+    with pytest.raises(B.DiscoError):                       # other parameters: training has to begin again
+        ev.loss_gradients(ev.alloc_batch(1, 4, 4, 4), torch.ones(1, device=ev.device))
+    with pytest.raises(ValueError):
+        ev.train_begin(1e-3, 4, 64, keep="4bit")
+    with pytest.raises(ValueError):
+        ev.set_layer_norms(4, gamma[:, :5], beta)
+    ev.close()
+    att = B.Evaluator(16, 32, 2, "f32", 4, 64, 64, agg="attention", heads=2)
+    assert B.dc_set_layer_norms(att.ctx, 4, 0, 1e-5, gamma, beta) == B.DC_ERR_UNSUPPORTED
+    att.close()
