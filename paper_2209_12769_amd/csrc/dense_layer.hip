@@ -472,7 +472,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
 #pragma unroll
       for (int k = 0; k < kW; ++k) z[k] += g.bias[col + k];
     if (g.Z) store_wide<E>(g.Z, row * g.ldz + col, z);
-    activate<kW>(z, g.act);
+    activate<kW, E::kBytes == 2>(z, g.act);
     if (g.R)
 #pragma unroll
       for (int k = 0; k < kW; ++k) z[k] += value_of<E>(r, k, 1.f);
@@ -486,7 +486,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
 #pragma unroll
     for (int k = 0; k < kW; ++k)
       if (col + k < g.N) store_value<E>(g.Z, row * g.ldz + col + k, z[k]);
-  activate<kW>(z, g.act);
+  activate<kW, E::kBytes == 2>(z, g.act);
 #pragma unroll
   for (int k = 0; k < kW; ++k)
     if (col + k < g.N) {
@@ -716,7 +716,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g) {
         const long long row = r + (long long)u * g.row_blocks * 8;
 #pragma unroll
         for (int k = 0; k < kV; ++k) d[u][k] = value_of<E>(z[u], k, 1.f);
-        slopes<kV>(d[u], g.act);
+        slopes<kV, E::kBytes == 2>(d[u], g.act);
 #pragma unroll
         for (int k = 0; k < kV; ++k) d[u][k] = row < rows ? d[u][k] * value_of<E>(y[u], k, 1.f) : 0.f;
         if (row < rows) {

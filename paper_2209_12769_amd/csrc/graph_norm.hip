@@ -9,8 +9,9 @@
 // whole cache lines), holds its rows in LDS between the sums and the second pass and reads again only what
 // does not fit.  Sums are formed in 64 bits (v as mean x^2 - mu^2: exact enough for any offset that fp32 values can
 // have next to their spread), three instructions a value, which the loads hide.
-// Graphs longer than a.long_rows would keep one workgroup busy while the others are done: their rows are dealt in chunks
-// to three kernels (sums of a chunk; sums of a graph; second pass), the short graphs' kernel leaves them out.
+// Graphs of more than long_rows rows would keep one workgroup busy while the others are done: the kernel of the short graphs
+// only lists them, and their rows are dealt in chunks, counted from each graph's first row, to three kernels (sums of a chunk;
+// sums of a graph; second pass).  The list's order is that of the workgroups' arrival; no sum depends on it.
 #include "operators.h"
 
 namespace dc {
@@ -48,8 +49,11 @@ struct Norm {
   int held;                // row steps of a thread that stay in LDS
   long long long_rows;     // graphs with more rows are left to the chunk kernels
   int chunk_rows;
-  double2* part;           // [chunks + graphs][G] sums of a chunk's rows of a graph
-  float2* means;           // [graphs][G] s1, s2 of the long graphs (backward)
+  unsigned long long* found;   // long graphs << 32 | their chunks; null: there cannot be any
+  int2* longs;             // [most_longs] graph and its first chunk, ascending in the chunks
+  int most_longs, most_chunks; // offsets that ascend do not give more; what others give beyond is left out
+  double2* part;           // [chunks][G] sums of a chunk
+  float2* means;           // [long graphs][G] s1, s2 (backward)
   float* cols;             // [column blocks][2 C] parts of dgamma | dbeta
   int col_block0;          // first column block of this launch
 };
@@ -111,18 +115,18 @@ __device__ __forceinline__ Affine<kV> affine_at(const GraphNormArgs& a, int c) {
 }
 
 // dy becomes dz.
-template <int kV>
+template <int kV, bool kShort>
 __device__ __forceinline__ void slope(float (&dy)[kV], const float (&xh)[kV], const Affine<kV>& f, int act) {
   float z[kV];
 #pragma unroll
   for (int k = 0; k < kV; ++k) z[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
-  slopes<kV>(z, act);
+  slopes<kV, kShort>(z, act);
 #pragma unroll
   for (int k = 0; k < kV; ++k) dy[k] *= z[k];
 }
 
 // What a row's vector adds to the two sums.
-template <bool kBack, int kV>
+template <bool kBack, int kV, bool kShort>
 __device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x)[kV], float (&dy)[kV], float mu, float r,
                                          const Affine<kV>& f, int act, float (&dg)[kV], float (&db)[kV]) {
   if constexpr (!kBack) {
@@ -136,7 +140,7 @@ __device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x
     float xh[kV];
 #pragma unroll
     for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
-    slope<kV>(dy, xh, f, act);
+    slope<kV, kShort>(dy, xh, f, act);
 #pragma unroll
     for (int k = 0; k < kV; ++k) {
       const float u = f.gamma[k] * dy[k];
@@ -208,12 +212,12 @@ __device__ __forceinline__ void finish(const Norm& n, const float (&x)[kV], floa
   if constexpr (!kBack) {
 #pragma unroll
     for (int k = 0; k < kV; ++k) xh[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
-    activate<kV>(xh, n.a.act);
+    activate<kV, sizeof(T) == 2>(xh, n.a.act);
 #pragma unroll
     for (int k = 0; k < kV; ++k) narrow(xh[k], o.v[k]);
     *reinterpret_cast<Vec<T, kV>*>(static_cast<T*>(n.a.Y) + row * n.a.ldy + c) = o;
   } else {
-    slope<kV>(dy, xh, f, n.a.act);
+    slope<kV, sizeof(T) == 2>(dy, xh, f, n.a.act);
     Vec<T, kV> add{};
     if (n.a.dRes) add = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.dRes) + row * n.a.lddres + c);
 #pragma unroll
@@ -309,7 +313,15 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
   const int ng = graphs_of(n.a);
   for (int g = blockIdx.x / n.nslab; g < ng; g += gridDim.x / n.nslab) {
     const Rows r = rows_of(n.a, g);
-    if (!r.ok || r.hi - r.lo > n.long_rows) continue;
+    if (!r.ok) continue;
+    if (r.hi - r.lo > n.long_rows) {
+      if (slab == 0 && t == 0) {
+        const long long chunks = (r.hi - r.lo + n.chunk_rows - 1) / n.chunk_rows;
+        const unsigned long long at = atomicAdd(n.found, (1ull << 32) + (unsigned long long)chunks);
+        if ((at >> 32) < (unsigned)n.most_longs) n.longs[at >> 32] = make_int2(g, (int)(unsigned)at);
+      }
+      continue;
+    }
     const double m = (double)(r.hi - r.lo) * n.cg;
     float mu = 0.f, rs = 0.f, s1f = 0.f, s2f = 0.f;
     if (kBack) {
@@ -326,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       if (i < n.held) mine[i * kThreads] = h;
       float x[kV], dy[kV];
       open<T, X, kV, kBack>(x, dy, h);
-      add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+      add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
     });
     group_sums(s1, s2, red, n.lanes, used, gv);
     if constexpr (!kBack) {
@@ -357,36 +369,36 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
 }
 
 // ---- long graphs: rows in chunks ----
-// The last graph that starts at or before row v; offsets that do not ascend give some graph, whose rows are looked at.
-__device__ __forceinline__ int graph_at(const int* off, int ng, long long v) {
-  int lo = 0, hi = ng;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid] <= v) lo = mid;
-    else hi = mid;
-  }
-  return lo;
+__global__ __launch_bounds__(256) void no_longs_kernel(unsigned long long* found, int2* longs, int most) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i == 0) found[0] = 0;
+  for (int k = i; k < most; k += gridDim.x * blockDim.x) longs[k] = make_int2(0, 0);
 }
-// A long graph has more rows than a chunk, so that a chunk meets at most two: those of its first and of its last row.
+
 struct Segment {
-  int g;
-  long long lo, hi;        // rows of the chunk that belong to graph g; lo >= hi: none
-  double m;
+  int entry, g;            // place in the list, graph
+  long long lo, hi;        // rows of the chunk
 };
-__device__ __forceinline__ Segment segment_of(const Norm& n, int ng, long long chunk, int which) {
-  Segment s{0, 0, 0, 0.0};
-  const long long c0 = chunk * n.chunk_rows;
-  long long c1 = c0 + n.chunk_rows;
-  if (c1 > n.a.rows) c1 = n.a.rows;
-  if (ng <= 0 || c0 >= c1) return s;
-  const int first = graph_at(n.a.node_off, ng, c0), last = graph_at(n.a.node_off, ng, c1 - 1);
-  if (which == 1 && last == first) return s;
-  s.g = which == 0 ? first : last;
-  const Rows r = rows_of(n.a, s.g);
-  if (!r.ok || r.hi - r.lo <= n.long_rows) return s;
-  s.lo = r.lo > c0 ? r.lo : c0;
-  s.hi = r.hi < c1 ? r.hi : c1;
-  s.m = (double)(r.hi - r.lo) * n.cg;
+// The long graph of a chunk: the last entry whose first chunk is not behind it, found 64 entries at a time.
+__device__ __forceinline__ Segment segment_of(const Norm& n, int nlong, int chunk) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, count = nlong;                           // the entry is one of lo .. lo + count - 1
+  while (count > 1) {
+    const int stride = (count + 63) >> 6, i = lo + lane * stride;
+    const bool before = lane * stride < count && n.longs[i].y <= chunk;
+    const int k = __popcll(__ballot(before)) - 1;      // ascending: the lanes in front
+    count = min(stride, count - k * stride);
+    lo += k * stride;
+  }
+  Segment s;
+  s.entry = lo;
+  const int2 e = n.longs[lo];
+  s.g = e.x;
+  const long long first = n.a.node_off[e.x], end = n.a.node_off[e.x + 1];
+  s.lo = first + (long long)(chunk - e.y) * n.chunk_rows;
+  s.hi = s.lo + n.chunk_rows < end ? s.lo + n.chunk_rows : end;
+  // offsets that do not ascend can fill the list with more than it holds, and then a chunk's entry is not its graph
+  if (first < 0 || end > n.a.rows || s.lo < first || s.lo >= end) s.hi = s.lo;
   return s;
 }
 
@@ -405,11 +417,10 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
   double dgs[kV], dbs[kV];
 #pragma unroll
   for (int k = 0; k < kV; ++k) dgs[k] = dbs[k] = 0.0;
-  const int ng = graphs_of(n.a);
-  const long long nchunk = (n.a.rows + n.chunk_rows - 1) / n.chunk_rows;
-  for (long long chunk = blockIdx.x / n.nslab; chunk < nchunk; chunk += gridDim.x / n.nslab)
-    for (int which = 0; which < 2; ++which) {
-      const Segment seg = segment_of(n, ng, chunk, which);
+  const unsigned long long found = n.found[0];
+  const int nchunk = (int)min((unsigned)found, (unsigned)n.most_chunks), nlong = (int)min((unsigned)(found >> 32), (unsigned)n.most_longs);
+  for (int chunk = blockIdx.x / n.nslab; chunk < nchunk; chunk += gridDim.x / n.nslab) {
+      const Segment seg = segment_of(n, nlong, chunk);
       if (seg.lo >= seg.hi) continue;
       float mu = 0.f, rs = 0.f;
       if (kBack) {
@@ -425,10 +436,10 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
       each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
-        add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+        add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
       });
       group_sums(s1, s2, red, n.lanes, used, gv);
-      if (in && rl == 0 && lane % gv == 0) n.part[(size_t)(chunk + seg.g) * n.a.G + group] = make_double2(s1, s2);
+      if (in && rl == 0 && lane % gv == 0) n.part[(size_t)chunk * n.a.G + group] = make_double2(s1, s2);
 #pragma unroll
       for (int k = 0; k < kV; ++k) {
         dgs[k] += (double)dg[k];
@@ -438,44 +449,38 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
   if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
 }
 
-// The sums of a long graph: a wave looks at 64 graphs and takes the long ones of them, one after another, its lanes over the chunks.
+// The sums of a long graph from its chunks': a wave each, `wide` (a power of two, at least the groups or 64) lanes side by side
+// over the groups, the others over the chunks.
 template <bool kBack>
-__global__ __launch_bounds__(256) void long_sums_kernel(const Norm n) {
+__global__ __launch_bounds__(64) void long_sums_kernel(const Norm n, int wide) {
   if (n.a.stop && n.a.stop[0] != 0) return;
-  const int ng = graphs_of(n.a), lane = threadIdx.x & 63;
-  const int nw = gridDim.x * 4;
-  for (int g0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; g0 < ng; g0 += nw * 64) {
-    long long lo = 0, hi = 0;
-    if (g0 + lane < ng) {
-      lo = n.a.node_off[g0 + lane];
-      hi = n.a.node_off[g0 + lane + 1];
-    }
-    const bool mine = lo >= 0 && hi <= n.a.rows && hi - lo > n.long_rows;
-    for (unsigned long long todo = __ballot(mine); todo != 0; todo &= todo - 1) {
-      const int l = __ffsll(todo) - 1, g = g0 + l;
-      const long long a = __shfl(lo, l, 64), b = __shfl(hi, l, 64);
-      const long long k0 = a / n.chunk_rows, k1 = (b - 1) / n.chunk_rows;
-      const double m = (double)(b - a) * n.cg;
-      for (int q = 0; q < n.a.G; ++q) {
-        double s1 = 0.0, s2 = 0.0;
-        for (long long k = k0 + lane; k <= k1; k += 64) {
-          const double2 p = n.part[(size_t)(k + g) * n.a.G + q];
+  const int nlong = (int)min((unsigned)(n.found[0] >> 32), (unsigned)n.most_longs), lane = threadIdx.x, q0 = lane & (wide - 1), k0 = lane / wide;
+  for (int i = blockIdx.x; i < nlong; i += gridDim.x) {
+    const int2 e = n.longs[i];
+    const long long rows = (long long)n.a.node_off[e.x + 1] - n.a.node_off[e.x];
+    if (rows <= n.long_rows || e.y < 0) continue;
+    const int chunks = (int)min((rows + n.chunk_rows - 1) / n.chunk_rows, (long long)n.most_chunks - e.y);
+    const double m = (double)rows * n.cg;
+    for (int q = q0; q < n.a.G + q0; q += wide) {       // the same number of rounds for every lane
+      double s1 = 0.0, s2 = 0.0;
+      if (q < n.a.G)
+        for (int k = k0; k < chunks; k += 64 / wide) {
+          const double2 p = n.part[(size_t)(e.y + k) * n.a.G + q];
           s1 += p.x;
           s2 += p.y;
         }
-        for (int o = 32; o > 0; o >>= 1) {
-          s1 += __shfl_xor(s1, o, 64);
-          s2 += __shfl_xor(s2, o, 64);
-        }
-        if (lane != 0) continue;
-        if (kBack) {
-          n.means[(size_t)g * n.a.G + q] = make_float2((float)(s1 / m), (float)(s2 / m));
-        } else {
-          float mu, rs;
-          statistics(s1, s2, m, n.a.eps, mu, rs);
-          n.a.mean[(size_t)g * n.a.G + q] = mu;
-          n.a.rstd[(size_t)g * n.a.G + q] = rs;
-        }
+      for (int o = 32; o >= wide; o >>= 1) {
+        s1 += __shfl_xor(s1, o, 64);
+        s2 += __shfl_xor(s2, o, 64);
+      }
+      if (k0 != 0 || q >= n.a.G) continue;
+      if (kBack) {
+        n.means[(size_t)i * n.a.G + q] = make_float2((float)(s1 / m), (float)(s2 / m));
+      } else {
+        float mu, rs;
+        statistics(s1, s2, m, n.a.eps, mu, rs);
+        n.a.mean[(size_t)e.x * n.a.G + q] = mu;
+        n.a.rstd[(size_t)e.x * n.a.G + q] = rs;
       }
     }
   }
@@ -490,14 +495,13 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
   if (lane >= used) return;
   const int c = c0 + lane * kV, group = c / n.cg;
   const Affine<kV> f = affine_at<kV>(n.a, c);
-  const int ng = graphs_of(n.a);
-  const long long nchunk = (n.a.rows + n.chunk_rows - 1) / n.chunk_rows;
-  for (long long chunk = blockIdx.x / n.nslab; chunk < nchunk; chunk += gridDim.x / n.nslab)
-    for (int which = 0; which < 2; ++which) {
-      const Segment seg = segment_of(n, ng, chunk, which);
+  const unsigned long long found = n.found[0];
+  const int nchunk = (int)min((unsigned)found, (unsigned)n.most_chunks), nlong = (int)min((unsigned)(found >> 32), (unsigned)n.most_longs);
+  for (int chunk = blockIdx.x / n.nslab; chunk < nchunk; chunk += gridDim.x / n.nslab) {
+      const Segment seg = segment_of(n, nlong, chunk);
       if (seg.lo >= seg.hi) continue;
       const float mu = n.a.mean[(size_t)seg.g * n.a.G + group], rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
-      const float2 s = kBack ? n.means[(size_t)seg.g * n.a.G + group] : make_float2(0.f, 0.f);
+      const float2 s = kBack ? n.means[(size_t)seg.entry * n.a.G + group] : make_float2(0.f, 0.f);
       const long long r0 = seg.lo + rl;
       const int count = r0 < seg.hi ? (int)((seg.hi - r0 + step - 1) / step) : 0;
       each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
@@ -508,26 +512,35 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
     }
 }
 
-// One chain of additions per column would be a round trip per row: a workgroup takes 16 columns with 16 threads each.
-__global__ __launch_bounds__(256) void column_sums_kernel(const float* __restrict__ part, int blocks, int n1, float* __restrict__ out1,
-                                                          int n2, float* __restrict__ out2, const int* stop) {
+// One chain of additions per column would be a round trip per row: a workgroup takes 16 columns with 64 threads each, which
+// request eight rows together.
+__global__ __launch_bounds__(1024) void column_sums_kernel(const float* __restrict__ part, int blocks, int n1, float* __restrict__ out1,
+                                                           int n2, float* __restrict__ out2, const int* stop) {
   if (stop && stop[0] != 0) return;
-  __shared__ double red[16][17];
+  __shared__ double red[64][17];
   const int j = threadIdx.x & 15, p = threadIdx.x >> 4, c = blockIdx.x * 16 + j, n = n1 + n2;
   double s = 0.0;
   if (c < n)
-    for (int b = p; b < blocks; b += 16) s += (double)part[(size_t)b * n + c];
+    for (int b = p; b < blocks; b += 512) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = part[(size_t)min(b + 64 * u, blocks - 1) * n + c];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += b + 64 * u < blocks ? (double)x[u] : 0.0;
+    }
   red[p][j] = s;
   __syncthreads();
+  for (int o = 32; o > 0; o >>= 1) {
+    if (p < o) red[p][j] += red[p + o][j];
+    __syncthreads();
+  }
   if (p == 0 && c < n) {
-    double v = 0.0;
-    for (int i = 0; i < 16; ++i) v += red[i][j];
-    if (c < n1) out1[c] = (float)v;
-    else out2[c - n1] = (float)v;
+    if (c < n1) out1[c] = (float)red[0][j];
+    else out2[c - n1] = (float)red[0][j];
   }
 }
 
-constexpr int kMostThreads = 512;         // two waves per SIMD: the gradient needs more than 128 registers
+constexpr int most_threads(bool back) { return back ? 512 : 1024; }     // the gradient needs more than 128 registers
 // Rows of a chunk: four chunks per CU, 64 to 512 rows.  Fewer than the shortest long graph.
 int chunk_rows(long long rows, int n_cu) {
   const long long r = (rows / (4LL * n_cu) + 63) / 64 * 64;
@@ -552,11 +565,12 @@ int slab_of(int C, int cg, int es) {
   return s >= C ? C : (int)s;
 }
 int blocks_most(int n_cu) { return n_cu * 8; }
-// LDS for rows of a workgroup of 64, 256 or 512 threads: eight, three or one of them per CU
-int held_bytes(int threads) { return threads == 64 ? 18 * 1024 : (threads == 256 ? 48 * 1024 : 148 * 1024); }
+// LDS for rows of a workgroup of 64, 256 or more threads: eight, three or one of them per CU
+int held_bytes(int threads) { return threads == 64 ? 18 * 1024 : (threads == 256 ? 48 * 1024 : 140 * 1024); }
 
-Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item, int n_cu) {
+Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item, bool back, int n_cu) {
   Plan p{};
+  const int kMost = most_threads(back);
   const int cg = C / G;
   const long long want = rows / (n_graphs > 0 ? n_graphs : 1) * 3 / 2;       // a graph of one and a half times the mean
   // whole rows and the fewest threads that hold it; else slabs
@@ -565,9 +579,9 @@ Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item
   auto fits = [&](int threads, int lanes) {
     return lanes <= threads && want <= (long long)held_bytes(threads) / (threads * item) * (threads / lanes);
   };
-  p.threads = fits(64, p.lanes) ? 64 : (fits(256, p.lanes) ? 256 : kMostThreads);
+  p.threads = fits(64, p.lanes) ? 64 : (fits(256, p.lanes) ? 256 : kMost);
   const int narrow = slab_of(C, cg, es);
-  if (p.threads == kMostThreads && !fits(p.threads, p.lanes)) {
+  if (p.threads == kMost && !fits(p.threads, p.lanes)) {
     p.slab = narrow;
     p.lanes = pow2_at_least((p.slab + v - 1) / v);
   }
@@ -605,7 +619,7 @@ hipError_t run_short(const Norm& n, int blocks, hipStream_t s) {
 
 template <typename T, typename X, int kV, bool kBack>
 hipError_t run(Norm n, hipStream_t s) {
-  const Plan p = plan_of(n.a.rows, n.a.n_graphs, n.a.C, n.a.G, (int)sizeof(T), kV, (int)sizeof(Two<T, X, kV>), n.a.n_cu);
+  const Plan p = plan_of(n.a.rows, n.a.n_graphs, n.a.C, n.a.G, (int)sizeof(T), kV, (int)sizeof(Two<T, X, kV>), kBack, n.a.n_cu);
   n.slab = p.slab;
   n.nslab = p.nslab;
   n.lanes = p.lanes;
@@ -614,15 +628,22 @@ hipError_t run(Norm n, hipStream_t s) {
   n.chunk_rows = chunk_rows(n.a.rows, n.a.n_cu);
   char* w = n.a.workspace;
   if (p.chunks) {
+    const size_t longs = (size_t)(n.a.rows / p.long_rows) + 1;
+    n.found = reinterpret_cast<unsigned long long*>(w);
+    n.longs = reinterpret_cast<int2*>(w + 16);
+    w += 16 + (longs * sizeof(int2) + 15) / 16 * 16;
     n.part = reinterpret_cast<double2*>(w);
-    w += ((size_t)((n.a.rows + n.chunk_rows - 1) / n.chunk_rows) + (size_t)n.a.n_graphs + 1) * n.a.G * sizeof(double2);
+    n.most_longs = (int)longs;
+    n.most_chunks = (int)(n.a.rows / n.chunk_rows + (long long)longs);
+    w += (size_t)n.most_chunks * n.a.G * sizeof(double2);
     n.means = reinterpret_cast<float2*>(w);
-    if (kBack) w += (size_t)n.a.n_graphs * n.a.G * sizeof(float2);
+    if (kBack) w += longs * n.a.G * sizeof(float2);
+    hipLaunchKernelGGL(no_longs_kernel, dim3((unsigned)(longs < 16384 ? (longs + 255) / 256 : 64)), dim3(256), 0, s, n.found, n.longs, n.most_longs);
   }
   n.cols = reinterpret_cast<float*>(w);
   hipError_t e = p.threads == 64    ? run_short<T, X, kV, 64, kBack>(n, p.blocks, s)
                  : p.threads == 256 ? run_short<T, X, kV, 256, kBack>(n, p.blocks, s)
-                                    : run_short<T, X, kV, kMostThreads, kBack>(n, p.blocks, s);
+                                    : run_short<T, X, kV, most_threads(kBack), kBack>(n, p.blocks, s);
   if (e != hipSuccess) return e;
   if (p.chunks) {
     n.col_block0 = p.blocks;
@@ -631,8 +652,9 @@ hipError_t run(Norm n, hipStream_t s) {
     n.lanes = p.chunk_lanes;
     const dim3 cgrid(p.chunk_blocks * n.nslab);
     hipLaunchKernelGGL((chunk_sums_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
-    const int waves = (n.a.n_graphs + 63) / 64, lgrid = (waves + 3) / 4 < n.a.n_cu ? (waves + 3) / 4 : n.a.n_cu;
-    hipLaunchKernelGGL((long_sums_kernel<kBack>), dim3(lgrid < 1 ? 1 : lgrid), dim3(256), 0, s, n);
+    const long long longs = n.a.rows / p.long_rows + 1, most = 4LL * n.a.n_cu;
+    const int wide = n.a.G < 64 ? pow2_at_least(n.a.G) : 64;
+    hipLaunchKernelGGL((long_sums_kernel<kBack>), dim3((unsigned)(longs < most ? longs : most)), dim3(64), 0, s, n, wide);
     hipLaunchKernelGGL((chunk_finish_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
   }
   if (kBack && n.a.dgamma)
@@ -668,16 +690,17 @@ hipError_t dispatch(const GraphNormArgs& a, hipStream_t s) {
 }  // namespace
 
 void launch_column_sums(const float* part, int blocks, int n1, float* out1, int n2, float* out2, const int* stop, hipStream_t s) {
-  hipLaunchKernelGGL(column_sums_kernel, dim3((n1 + n2 + 15) / 16), dim3(256), 0, s, part, blocks, n1, out1, n2, out2, stop);
+  hipLaunchKernelGGL(column_sums_kernel, dim3((n1 + n2 + 15) / 16), dim3(1024), 0, s, part, blocks, n1, out1, n2, out2, stop);
 }
 
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
   // what any vector width and type would need, and any smaller number of rows: chunks of fewer than 512 rows are at most four per CU
   const long long most = blocks_most(n_cu), by_rows = rows / 512 + 1, nc = by_rows > 4LL * n_cu ? by_rows : 4LL * n_cu + 1;
   const bool chunks = rows > 1024;
-  size_t b = chunks ? ((size_t)nc + (size_t)n_graphs + 1) * G * sizeof(double2) : 0;
+  const size_t longs = chunks ? (size_t)(rows / 1024) + 1 : 0;
+  size_t b = chunks ? 16 + (longs * sizeof(int2) + 15) / 16 * 16 + ((size_t)nc + longs) * G * sizeof(double2) : 0;
   if (backward) {
-    if (chunks) b += (size_t)n_graphs * G * sizeof(float2);
+    b += longs * G * sizeof(float2);
     b += (size_t)((n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most) + (chunks ? (nc < most ? nc : most) : 0)) * 2 * C * sizeof(float);
   }
   return b;

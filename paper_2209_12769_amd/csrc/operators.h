@@ -11,18 +11,42 @@ namespace dc {
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
+// erfc(|x|) e^(x^2) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))), t = 1 / (1 + p |x|): Abramowitz and Stegun, Handbook of
+// Mathematical Functions, 7.1.26; erf is off by at most 1.5e-7, absolutely.
+struct NormalParts {
+  float cdf, density;    // of the standard normal distribution at z
+};
+__device__ __forceinline__ NormalParts normal_parts(float z) {
+  const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+  const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * x * x);
+  const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  const float half = 0.5f * poly * e;
+  return {z > 0.f ? 1.f - half : half, 0.39894228040143268f * e};
+}
+// kShort: for values that are stored in bf16.  GELU's error function is then the approximation above (2e-5 of bf16's rounding),
+// a third of the instructions of the library's, which bound the norms with GELU.
+template <bool kShort>
 __device__ __forceinline__ float activation(float z, int act) {
   switch (act) {
     case DC_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-    case DC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case DC_ACT_GELU:
+      if constexpr (kShort) return z * normal_parts(z).cdf;
+      else return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
     case DC_ACT_SILU: return z * sigmoid(z);
     default: return z;
   }
 }
+template <bool kShort>
 __device__ __forceinline__ float activation_slope(float z, int act) {
   switch (act) {
     case DC_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case DC_ACT_GELU: return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * 0.70710678118654752f)));
+    case DC_ACT_GELU:
+      if constexpr (kShort) {
+        const NormalParts n = normal_parts(z);
+        return fmaf(z, n.density, n.cdf);
+      } else {
+        return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * 0.70710678118654752f)));
+      }
     case DC_ACT_SILU: {
       const float s = sigmoid(z);
       return s * fmaf(z, 1.f - s, 1.f);
@@ -30,40 +54,39 @@ __device__ __forceinline__ float activation_slope(float z, int act) {
     default: return 1.f;
   }
 }
-
 // The same for kN values, the choice made once.
-template <int kN>
+template <int kN, bool kShort>
 __device__ __forceinline__ void activate(float (&z)[kN], int act) {
   switch (act) {
     case DC_ACT_RELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_RELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation<kShort>(z[k], DC_ACT_RELU);
       break;
     case DC_ACT_GELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_GELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation<kShort>(z[k], DC_ACT_GELU);
       break;
     case DC_ACT_SILU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_SILU);
+      for (int k = 0; k < kN; ++k) z[k] = activation<kShort>(z[k], DC_ACT_SILU);
       break;
     default: break;
   }
 }
-template <int kN>
+template <int kN, bool kShort>
 __device__ __forceinline__ void slopes(float (&z)[kN], int act) {
   switch (act) {
     case DC_ACT_RELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_RELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope<kShort>(z[k], DC_ACT_RELU);
       break;
     case DC_ACT_GELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_GELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope<kShort>(z[k], DC_ACT_GELU);
       break;
     case DC_ACT_SILU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_SILU);
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope<kShort>(z[k], DC_ACT_SILU);
       break;
     default:
 #pragma unroll

@@ -491,6 +491,18 @@ def test_graph_norm_reports_bad_offsets(B, ev):
         assert torch.equal((out != 7).any(1).cpu(), touched)
 
 
+def test_graph_norm_overlapping_long_graphs(B, ev):
+    """Offsets that jump back and forth name more long graphs than the rows can hold: reported, nothing outside is touched."""
+    C, G, rows = 16, 2, 5000
+    x = torch.full((rows + 64, C), 3.0, device="cuda")
+    off = torch.tensor([0, rows] * 40, dtype=torch.int32, device="cuda")
+    out = torch.full_like(x, 7.0)
+    ev.graph_norm(x[:rows], off, G, out=out[:rows])
+    ev.graph_norm_backward(x[:rows], x[:rows], off, G, None, None, torch.zeros(79, G, device="cuda"), torch.ones(79, G, device="cuda"))
+    assert ev.check() == B.DC_ERR_BAD_GRAPH
+    assert (out[rows:] == 7).all()
+
+
 # ---------------------------------------------------------------------------
 # differences, streams, graphs, chains
 # ---------------------------------------------------------------------------
