@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import Dict, Optional, Tuple
 
@@ -99,6 +100,15 @@ class DcGraphNormArgs(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+# The same structs for the wrapper's calls, packed from values (native sizes and alignment).
+_KEPT = struct.Struct("@PPqq")
+_DENSE = struct.Struct("@iiqiiPqPqPPqPqPq")
+_DENSE_BACK = struct.Struct("@iiqiiPqPqPqPPqPqPqPPN")
+_NORM = struct.Struct("@iiqiiifPPqPPPPPqPPqPqPqPPPN")
+assert [s.size for s in (_KEPT, _DENSE, _DENSE_BACK, _NORM)] == [
+    C.sizeof(s) for s in (DcKeptRows, DcDenseArgs, DcDenseBackwardArgs, DcGraphNormArgs)]
+
+
 class DiscoError(RuntimeError):
     def __init__(self, status: int, detail: str = ""):
         self.status = status
@@ -152,16 +162,17 @@ def lib():
         L.dc_set_layer_norms.argtypes = [vp, i32, i32, C.c_float, vp, vp, vp]
         L.dc_get_layer_norms.argtypes = [vp, vp, vp, vp]
         L.dc_train_keep.argtypes = [vp, i32]
-        L.dc_keep_rows.argtypes = [vp, i32, i64, i32, vp, i64, C.POINTER(DcKeptRows), vp]
-        L.dc_restore_rows.argtypes = [vp, i32, i64, i32, C.POINTER(DcKeptRows), vp, i64, vp]
-        L.dc_dense.argtypes = [vp, C.POINTER(DcDenseArgs), vp]
+        # argument structs as void pointers: a struct by reference, or the bytes of one
+        L.dc_keep_rows.argtypes = [vp, i32, i64, i32, vp, i64, vp, vp]
+        L.dc_restore_rows.argtypes = [vp, i32, i64, i32, vp, vp, i64, vp]
+        L.dc_dense.argtypes = [vp, vp, vp]
         L.dc_dense_backward_bytes.argtypes = [vp, i32, i32, i64, i32, i32]
         L.dc_dense_backward_bytes.restype = size
-        L.dc_dense_backward.argtypes = [vp, C.POINTER(DcDenseBackwardArgs), vp]
+        L.dc_dense_backward.argtypes = [vp, vp, vp]
         L.dc_graph_norm_bytes.argtypes = [vp, i64, i32, i32, i32, i32]
         L.dc_graph_norm_bytes.restype = size
-        L.dc_graph_norm.argtypes = [vp, C.POINTER(DcGraphNormArgs), vp]
-        L.dc_graph_norm_backward.argtypes = [vp, C.POINTER(DcGraphNormArgs), vp]
+        L.dc_graph_norm.argtypes = [vp, vp, vp]
+        L.dc_graph_norm_backward.argtypes = [vp, vp, vp]
         L.dc_check.argtypes = [vp, vp]
         L.dc_select_kernels.argtypes = [vp, i32]
         L.dc_last_totals.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64), vp]
@@ -595,172 +606,195 @@ class Evaluator:
         return loss
 
     # ---- operators on rows of a batch (device tensors; rows may be apart, columns are neighbours) ----
-    def _matrix(self, x, name: str, cols: Optional[int] = None, rows: Optional[int] = None, dtype=None):
-        """Checks a matrix and returns the elements from row to row."""
+    # A small call is bound by what happens here: the argument structs are packed in one go, every tensor is looked at once.
+    def _raw_stream(self) -> int:
+        return self.torch._C._cuda_getCurrentRawStream(self.device.index)
+
+    def _rows(self, x, name: str):
+        """(rows, cols, elements from row to row, type) of a matrix on the context's device."""
         if x.device != self.device or x.dim() != 2:
             raise ValueError(f"{name}: need a matrix on {self.device}")
+        dtype = self._types.get(x.dtype)
         if dtype is None:
-            if x.dtype not in (self.torch.float32, self.torch.bfloat16):
-                raise ValueError(f"{name}: need float32 or bfloat16, not {x.dtype}")
-        elif x.dtype != dtype:
-            raise ValueError(f"{name}: need {dtype}, not {x.dtype}")
-        if (cols is not None and x.shape[1] != cols) or (rows is not None and x.shape[0] != rows):
-            raise ValueError(f"{name}: shape {tuple(x.shape)} does not fit")
-        if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
+            raise ValueError(f"{name}: need float32 or bfloat16, not {x.dtype}")
+        rows, cols = x.shape
+        ld, step = x.stride()
+        if step != 1 and cols > 1 and rows:
             raise ValueError(f"{name}: the columns of a row must be neighbours")
-        return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+        return rows, cols, ld if rows > 1 else cols, dtype
 
-    def _vector(self, x, name: str, n: int, dtype=None):
+    def _like(self, x, name: str, rows: int, cols: int, dtype: int) -> int:
+        """Elements from row to row of a matrix that has to be rows x cols of that type."""
+        r, c, ld, t = self._rows(x, name)
+        if r != rows or c != cols or t != dtype:
+            raise ValueError(f"{name}: need {rows} x {cols} {'bfloat16' if dtype else 'float32'}, not {tuple(x.shape)} {x.dtype}")
+        return ld
+
+    def _vector(self, x, name: str, n: int, dtype=None) -> int:
         if x.device != self.device or x.dtype != (dtype or self.torch.float32) or tuple(x.shape) != (n,) or not x.is_contiguous():
             raise ValueError(f"{name}: need {n} contiguous {dtype or self.torch.float32} on {self.device}")
         return x.data_ptr()
 
-    def _kept(self, kept: KeptRows, cols: int, rows: int):
-        k = kept
-        if (k.code.device != self.device or k.exponent.device != self.device or k.code.dtype != self.torch.int8
-                or k.exponent.dtype != self.torch.uint8 or k.cols != cols or k.rows != rows or (rows and k.code.stride(1) != 1)
-                or (rows and k.exponent.shape[1] > 1 and k.exponent.stride(1) != 1)):
-            raise ValueError("kept rows do not fit")
-        return C.pointer(DcKeptRows(k.code.data_ptr(), k.exponent.data_ptr(), k.code.stride(0) if rows > 1 else k.code.shape[1],
-                                    k.exponent.stride(0) if rows > 1 else k.exponent.shape[1]))
+    def _kept(self, k: KeptRows, rows: int, cols: int) -> bytes:
+        """The packed dc_kept_rows."""
+        c, e = k.code, k.exponent
+        if (c.device != self.device or e.device != self.device or c.dtype != self.torch.int8 or e.dtype != self.torch.uint8
+                or k.cols != cols or c.shape[0] != rows):
+            raise ValueError(f"kept rows: need {rows} x {cols} on {self.device}")
+        lc, le = c.stride(0), e.stride(0)
+        if rows <= 1:
+            lc, le = c.shape[1], e.shape[1]
+        elif c.stride(1) != 1 or (e.shape[1] > 1 and e.stride(1) != 1):
+            raise ValueError("kept rows: the columns of a row must be neighbours")
+        return _KEPT.pack(c.data_ptr(), e.data_ptr(), lc, le)
 
     @staticmethod
     def _act(act: str) -> int:
-        if act not in ACTIVATIONS:
+        code = ACTIVATIONS.get(act)
+        if code is None:
             raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTIVATIONS)}")
-        return ACTIVATIONS[act]
+        return code
 
-    def _type(self, x) -> int:
-        return DC_BF16 if x.dtype == self.torch.bfloat16 else DC_F32
+    @property
+    def _types(self):
+        types = self.__dict__.get("_type_codes")
+        if types is None:
+            types = self.__dict__["_type_codes"] = {self.torch.float32: DC_F32, self.torch.bfloat16: DC_BF16}
+        return types
 
     def keep_rows(self, x) -> KeptRows:
         """x [rows, cols] in 8 bits, one power of two per row and 32 columns."""
-        ld, (rows, cols) = self._matrix(x, "x"), x.shape
+        rows, cols, ld, dtype = self._rows(x, "x")
         blocks = -(-cols // 32)
-        k = KeptRows(self.torch.empty((rows, 32 * blocks), dtype=self.torch.int8, device=self.device),
-                     self.torch.empty((rows, blocks), dtype=self.torch.uint8, device=self.device), cols)
-        self._ok(dc_keep_rows(self.ctx, self._type(x), rows, cols, x.data_ptr(), ld, self._kept(k, cols, rows).contents,
-                              self._stream()), "dc_keep_rows")
+        code = self.torch.empty((rows, 32 * blocks), dtype=self.torch.int8, device=self.device)
+        k = KeptRows(code, self.torch.empty((rows, blocks), dtype=self.torch.uint8, device=self.device), cols)
+        st = lib().dc_keep_rows(self.ctx, dtype, rows, cols, x.data_ptr(), ld, self._kept(k, rows, cols), self._raw_stream())
+        if st:
+            self._ok(st, "dc_keep_rows")
         return k
 
     def restore_rows(self, kept: KeptRows, dtype=None, out=None):
-        rows, cols = kept.rows, kept.cols
+        rows, cols = kept.code.shape[0], kept.cols
         if out is None:
             out = self.torch.empty((rows, cols), dtype=dtype or self.torch.float32, device=self.device)
         elif dtype is not None and out.dtype != dtype:
             raise ValueError(f"out: need {dtype}, not {out.dtype}")
-        ld = self._matrix(out, "out", cols, rows)
-        self._ok(dc_restore_rows(self.ctx, self._type(out), rows, cols, self._kept(kept, cols, rows).contents, out.data_ptr(),
-                                 ld, self._stream()), "dc_restore_rows")
+        r, c, ld, t = self._rows(out, "out")
+        if r != rows or c != cols:
+            raise ValueError(f"out: need {rows} x {cols}, not {tuple(out.shape)}")
+        st = lib().dc_restore_rows(self.ctx, t, rows, cols, self._kept(kept, rows, cols), out.data_ptr(), ld, self._raw_stream())
+        if st:
+            self._ok(st, "dc_restore_rows")
         return out
 
     def dense(self, x, w, bias=None, act: str = "none", residual=None, out=None, want_pre: bool = False):
         """act(x w + bias) + residual; with want_pre also x w + bias, which dense_backward takes as `pre`."""
-        a = DcDenseArgs()
-        a.ldx, (rows, n_in) = self._matrix(x, "x"), x.shape
-        a.ldw, n_out = self._matrix(w, "w", rows=n_in, dtype=x.dtype), int(w.shape[1])
+        rows, n_in, ldx, dtype = self._rows(x, "x")
+        wr, n_out, ldw, wt = self._rows(w, "w")
+        if wr != n_in or wt != dtype:
+            raise ValueError(f"w: need {n_in} rows of x's type")
         if out is None:
-            out = self.torch.empty((rows, n_out), dtype=x.dtype, device=self.device)
-        a.ldy = self._matrix(out, "out", n_out, rows, x.dtype)
-        a.dtype, a.act, a.rows, a.n_in, a.n_out = self._type(x), self._act(act), rows, n_in, n_out
-        a.X, a.W, a.Y = x.data_ptr(), w.data_ptr(), out.data_ptr()
-        if bias is not None:
-            a.bias = self._vector(bias, "bias", n_out)
-        if residual is not None:
-            a.ld_residual = self._matrix(residual, "residual", n_out, rows, x.dtype)
-            a.residual = residual.data_ptr()
-        pre = None
-        if want_pre:
-            pre = self.torch.empty((rows, n_out), dtype=x.dtype, device=self.device)
-            a.Z, a.ldz = pre.data_ptr(), n_out
-        self._ok(dc_dense(self.ctx, a, self._stream()), "dc_dense")
+            out, ldy = self.torch.empty((rows, n_out), dtype=x.dtype, device=self.device), n_out
+        else:
+            ldy = self._like(out, "out", rows, n_out, dtype)
+        pb = self._vector(bias, "bias", n_out) if bias is not None else 0
+        pr, ldr = (residual.data_ptr(), self._like(residual, "residual", rows, n_out, dtype)) if residual is not None else (0, 0)
+        pre = self.torch.empty((rows, n_out), dtype=x.dtype, device=self.device) if want_pre else None
+        a = _DENSE.pack(dtype, self._act(act), rows, n_in, n_out, x.data_ptr(), ldx, w.data_ptr(), ldw, pb, pr, ldr,
+                        pre.data_ptr() if want_pre else 0, n_out, out.data_ptr(), ldy)
+        st = lib().dc_dense(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_dense")
         return (out, pre) if want_pre else out
 
     def dense_backward(self, dy, x, w, act: str = "none", pre=None, want=("x", "w", "b")):
         """Gradients (dx, dw, db) of dense at x, w and bias for the gradient dy at its result; None for those not in
         `want`.  x: the rows, or KeptRows of them."""
         torch = self.torch
-        a = DcDenseBackwardArgs()
-        a.lddy, (rows, n_out) = self._matrix(dy, "dy"), dy.shape
-        a.ldw, n_in = self._matrix(w, "w", n_out, dtype=dy.dtype), int(w.shape[0])
-        a.dtype, a.act, a.rows, a.n_in, a.n_out = self._type(dy), self._act(act), rows, n_in, n_out
-        a.dY, a.W = dy.data_ptr(), w.data_ptr()
-        if a.act != DC_ACT_NONE:
-            if pre is None:
-                raise ValueError("pre: the gradient of the activation needs x w + bias")
-            a.ldz, a.Z = self._matrix(pre, "pre", n_out, rows, dy.dtype), pre.data_ptr()
-        if isinstance(x, KeptRows):
-            a.kept = self._kept(x, n_in, rows)
+        rows, n_out, lddy, dtype = self._rows(dy, "dy")
+        n_in, wc, ldw, wt = self._rows(w, "w")
+        if wc != n_out or wt != dtype:
+            raise ValueError(f"w: need {n_out} columns of dy's type")
+        code = self._act(act)
+        if code == DC_ACT_NONE:
+            pz, ldz = 0, 0
+        elif pre is None:
+            raise ValueError("pre: the gradient of the activation needs x w + bias")
         else:
-            a.ldx, a.X = self._matrix(x, "x", n_in, rows, dy.dtype), x.data_ptr()
+            pz, ldz = pre.data_ptr(), self._like(pre, "pre", rows, n_out, dtype)
+        px, ldx, kept = 0, 0, None
+        if isinstance(x, KeptRows):
+            kept = C.create_string_buffer(self._kept(x, rows, n_in), _KEPT.size)
+        else:
+            px, ldx = x.data_ptr(), self._like(x, "x", rows, n_in, dtype)
         dx = torch.empty((rows, n_in), dtype=dy.dtype, device=self.device) if "x" in want else None
         dw = torch.empty((n_in, n_out), dtype=dy.dtype, device=self.device) if "w" in want else None
         db = torch.empty(n_out, dtype=torch.float32, device=self.device) if "b" in want else None
-        if dx is not None:
-            a.dX, a.lddx = dx.data_ptr(), n_in
-        if dw is not None:
-            a.dW, a.lddw = dw.data_ptr(), n_out
-        if db is not None:
-            a.db = db.data_ptr()
-        a.workspace_bytes = dc_dense_backward_bytes(self.ctx, a.dtype, a.act, rows, n_in, n_out)
-        ws = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
-        a.workspace = ws.data_ptr()
-        self._ok(dc_dense_backward(self.ctx, a, self._stream()), "dc_dense_backward")
+        size = lib().dc_dense_backward_bytes(self.ctx, dtype, code, rows, n_in, n_out)
+        ws = torch.empty(size, dtype=torch.uint8, device=self.device)
+        a = _DENSE_BACK.pack(dtype, code, rows, n_in, n_out, dy.data_ptr(), lddy, pz, ldz, px, ldx,
+                             0 if kept is None else C.addressof(kept), w.data_ptr(), ldw, 0 if dx is None else dx.data_ptr(), n_in,
+                             0 if dw is None else dw.data_ptr(), n_out, 0 if db is None else db.data_ptr(), ws.data_ptr(), size)
+        st = lib().dc_dense_backward(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_dense_backward")
         return dx, dw, db
 
-    def _norm_args(self, rows: int, channels: int, like, node_off, groups: int, gamma, beta, act: str, backward: bool):
-        a = DcGraphNormArgs()
+    def _norm(self, node_off, channels: int, rows: int, groups: int, gamma, beta, backward: int):
+        """(graphs, offsets, gamma, beta, workspace, its size)"""
         if node_off.dim() != 1 or node_off.numel() < 1:
             raise ValueError("node_off: need at least one offset")
-        a.n_graphs = node_off.numel() - 1
-        a.node_off = self._vector(node_off, "node_off", a.n_graphs + 1, self.torch.int32)
-        a.dtype, a.act, a.rows, a.channels, a.groups = self._type(like), self._act(act), rows, channels, groups
-        if gamma is not None:
-            a.gamma = self._vector(gamma, "gamma", channels)
-        if beta is not None:
-            a.beta = self._vector(beta, "beta", channels)
-        a.workspace_bytes = dc_graph_norm_bytes(self.ctx, rows, a.n_graphs, channels, groups, backward)
-        ws = self.torch.empty(a.workspace_bytes, dtype=self.torch.uint8, device=self.device) if a.workspace_bytes else None
-        if ws is not None:
-            a.workspace = ws.data_ptr()
-        return a, ws
+        n = node_off.numel() - 1
+        off = self._vector(node_off, "node_off", n + 1, self.torch.int32)
+        pg = 0 if gamma is None else self._vector(gamma, "gamma", channels)
+        pb = 0 if beta is None else self._vector(beta, "beta", channels)
+        size = lib().dc_graph_norm_bytes(self.ctx, rows, n, channels, groups, backward)
+        return n, off, pg, pb, self.torch.empty(size, dtype=self.torch.uint8, device=self.device) if size else None, size
 
     def graph_norm(self, x, node_off, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: str = "none", out=None):
         """(y, mean, rstd): the norm over the rows of each graph and the channels of each group, with an activation.  Rows
         of no graph are left as they are in `out`."""
-        ldx, (rows, channels) = self._matrix(x, "x"), x.shape
+        rows, channels, ldx, dtype = self._rows(x, "x")
+        n, off, pg, pb, ws, size = self._norm(node_off, channels, rows, groups, gamma, beta, 0)
         if out is None:
-            out = self.torch.empty((rows, channels), dtype=x.dtype, device=self.device)
-        a, ws = self._norm_args(rows, channels, x, node_off, groups, gamma, beta, act, False)
-        a.X, a.ldx, a.Y, a.ldy, a.eps = x.data_ptr(), ldx, out.data_ptr(), self._matrix(out, "out", channels, rows, x.dtype), eps
-        mean = self.torch.empty((a.n_graphs, groups), dtype=self.torch.float32, device=self.device)
-        rstd = self.torch.empty_like(mean)
-        a.mean, a.rstd = mean.data_ptr(), rstd.data_ptr()
-        self._ok(dc_graph_norm(self.ctx, a, self._stream()), "dc_graph_norm")
+            out, ldy = self.torch.empty((rows, channels), dtype=x.dtype, device=self.device), channels
+        else:
+            ldy = self._like(out, "out", rows, channels, dtype)
+        mean, rstd = self.torch.empty((2, n, groups), dtype=self.torch.float32, device=self.device).unbind(0)
+        a = _NORM.pack(dtype, self._act(act), rows, n, channels, groups, eps, off, x.data_ptr(), ldx, pg, pb, mean.data_ptr(),
+                       rstd.data_ptr(), out.data_ptr(), ldy, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0 if ws is None else ws.data_ptr(), size)
+        st = lib().dc_graph_norm(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_graph_norm")
         return out, mean, rstd
 
     def graph_norm_backward(self, dy, x, node_off, groups: int, gamma, beta, mean, rstd, act: str = "none", residual=None,
                             out=None):
         """(dx, dgamma, dbeta) for the gradient dy at the result; `residual` is added to dx.  x: the rows, or KeptRows of
         them; mean, rstd: what graph_norm returned."""
-        lddy, (rows, channels) = self._matrix(dy, "dy"), dy.shape
-        a, ws = self._norm_args(rows, channels, dy, node_off, groups, gamma, beta, act, True)
+        rows, channels, lddy, dtype = self._rows(dy, "dy")
+        n, off, pg, pb, ws, size = self._norm(node_off, channels, rows, groups, gamma, beta, 1)
         for v, name in ((mean, "mean"), (rstd, "rstd")):
-            if v.device != self.device or v.dtype != self.torch.float32 or tuple(v.shape) != (a.n_graphs, groups) or not v.is_contiguous():
-                raise ValueError(f"{name}: need float32 [{a.n_graphs}, {groups}] on {self.device}")
+            if v.device != self.device or v.dtype != self.torch.float32 or tuple(v.shape) != (n, groups) or not v.is_contiguous():
+                raise ValueError(f"{name}: need contiguous float32 [{n}, {groups}] on {self.device}")
         if out is None:
-            out = self.torch.empty((rows, channels), dtype=dy.dtype, device=self.device)
-        if isinstance(x, KeptRows):
-            a.kept = self._kept(x, channels, rows)
+            out, lddx = self.torch.empty((rows, channels), dtype=dy.dtype, device=self.device), channels
         else:
-            a.ldx, a.X = self._matrix(x, "x", channels, rows, dy.dtype), x.data_ptr()
-        if residual is not None:
-            a.lddres, a.dres = self._matrix(residual, "residual", channels, rows, dy.dtype), residual.data_ptr()
-        grads = self.torch.empty((2, channels), dtype=self.torch.float32, device=self.device)
-        a.dY, a.lddy, a.dX, a.lddx = dy.data_ptr(), lddy, out.data_ptr(), self._matrix(out, "out", channels, rows, dy.dtype)
-        a.mean, a.rstd, a.dgamma, a.dbeta = mean.data_ptr(), rstd.data_ptr(), grads[0].data_ptr(), grads[1].data_ptr()
-        self._ok(dc_graph_norm_backward(self.ctx, a, self._stream()), "dc_graph_norm_backward")
-        return out, grads[0], grads[1]
+            lddx = self._like(out, "out", rows, channels, dtype)
+        px, ldx, kept = 0, 0, None
+        if isinstance(x, KeptRows):
+            kept = C.create_string_buffer(self._kept(x, rows, channels), _KEPT.size)
+        else:
+            px, ldx = x.data_ptr(), self._like(x, "x", rows, channels, dtype)
+        pr, ldr = (residual.data_ptr(), self._like(residual, "residual", rows, channels, dtype)) if residual is not None else (0, 0)
+        dgamma, dbeta = self.torch.empty((2, channels), dtype=self.torch.float32, device=self.device).unbind(0)
+        a = _NORM.pack(dtype, self._act(act), rows, n, channels, groups, 0.0, off, px, ldx, pg, pb, mean.data_ptr(), rstd.data_ptr(),
+                       0, 0, 0 if kept is None else C.addressof(kept), dy.data_ptr(), lddy, pr, ldr, out.data_ptr(), lddx,
+                       dgamma.data_ptr(), dbeta.data_ptr(), 0 if ws is None else ws.data_ptr(), size)
+        st = lib().dc_graph_norm_backward(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_graph_norm_backward")
+        return out, dgamma, dbeta
 
     def get_weights(self):
         """(W_layers, b_layers, head) as host fp32 arrays in the layout of dc_set_weights."""
