@@ -102,61 +102,32 @@ __device__ __forceinline__ float single(const Source& s, long long row, int col)
   }
   return x;
 }
-// kVec: the matrix ends, and its parts meet, between vectors, and the vector lies inside; else the last vector of a row is read
-// value by value, zeros behind the last column.
-template <class E, int kN, bool kDz, bool kVec>
-__device__ __forceinline__ void fetch(Raw<E, kN, kDz>& r, const Source& s, long long row, int col) {
-  const int seg = (col >= s.d ? 1 : 0) + (col >= 2 * s.d ? 1 : 0), c = col - seg * s.d;
-  const char* p = part_of(s, seg) + (row * s.ld + c) * E::kBytes;
-  const char* z = kDz ? s.z + (row * s.ldz + col) * E::kBytes : nullptr;
-  if constexpr (E::kBytes == 1) r.e = s.exponent[row * s.ld_exponent + min(col, s.cols - 1) / kKeptBlock];
-  if (kVec || c + kN <= s.d) {
-    read_words<kN * E::kBytes>(r.w, p);
-    if constexpr (kDz) read_words<kN * E::kBytes>(r.z, z);
-  } else {
-#pragma unroll
-    for (int i = 0; i < Raw<E, kN, kDz>::kWords; ++i) {
-      r.w[i] = 0;
-      if constexpr (kDz) r.z[i] = 0;
-    }
-    constexpr int kPer = 4 / E::kBytes;
-#pragma unroll
-    for (int k = 0; k < kN; ++k) {
-      if (c + k >= s.d) continue;
-      unsigned x[1];
-      read_words<E::kBytes>(x, p + k * E::kBytes);
-      r.w[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
-      if constexpr (kDz) {
-        read_words<E::kBytes>(x, z + k * E::kBytes);
-        r.z[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
-      }
-    }
-  }
+// kN neighbouring values at p + off (and z + offz).
+template <class E, int kN, bool kDz>
+__device__ __forceinline__ void fetch(Raw<E, kN, kDz>& r, const char* p, const char* z, unsigned off, unsigned offz) {
+  read_words<kN * E::kBytes>(r.w, p + off);
+  if constexpr (kDz) read_words<kN * E::kBytes>(r.z, z + offz);
 }
-// The same at an offset of less than 4 GB from a place that all lanes share; left: columns from there to the end of the row.
-template <class E, int kN, bool kDz, bool kVec>
-__device__ __forceinline__ void fetch_near(Raw<E, kN, kDz>& r, const char* p, const char* z, unsigned off, unsigned offz, int left) {
-  if (kVec || kN <= left) {
-    read_words<kN * E::kBytes>(r.w, p + off);
-    if constexpr (kDz) read_words<kN * E::kBytes>(r.z, z + offz);
-  } else {
+// The same value by value where only `left` (at least one) are there: the last one again behind them, no request in a branch.
+template <class E, int kN, bool kDz>
+__device__ __forceinline__ void fetch_some(Raw<E, kN, kDz>& r, const char* p, const char* z, unsigned off, unsigned offz, int left) {
+  constexpr int kPer = 4 / E::kBytes;
+  unsigned x[kN][1], y[kN][1];
 #pragma unroll
-    for (int i = 0; i < Raw<E, kN, kDz>::kWords; ++i) {
-      r.w[i] = 0;
-      if constexpr (kDz) r.z[i] = 0;
-    }
-    constexpr int kPer = 4 / E::kBytes;
+  for (int k = 0; k < kN; ++k) {
+    const unsigned at = (unsigned)min(k, left - 1) * E::kBytes;
+    read_words<E::kBytes>(x[k], p + off + at);
+    if constexpr (kDz) read_words<E::kBytes>(y[k], z + offz + at);
+  }
 #pragma unroll
-    for (int k = 0; k < kN; ++k) {
-      if (k >= left) continue;
-      unsigned x[1];
-      read_words<E::kBytes>(x, p + off + k * E::kBytes);
-      r.w[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
-      if constexpr (kDz) {
-        read_words<E::kBytes>(x, z + offz + k * E::kBytes);
-        r.z[k / kPer] |= x[0] << (8 * E::kBytes * (k % kPer) % 32);
-      }
-    }
+  for (int i = 0; i < Raw<E, kN, kDz>::kWords; ++i) {
+    r.w[i] = 0;
+    if constexpr (kDz) r.z[i] = 0;
+  }
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    r.w[k / kPer] |= x[k][0] << (8 * E::kBytes * (k % kPer) % 32);
+    if constexpr (kDz) r.z[k / kPer] |= y[k][0] << (8 * E::kBytes * (k % kPer) % 32);
   }
 }
 template <class E, int kN, bool kDz>
@@ -167,6 +138,18 @@ __device__ __forceinline__ void clear(Raw<E, kN, kDz>& r) {
     if constexpr (kDz) r.z[i] = 0;
   }
   r.e = 0;
+}
+// Clears the first `n` values.
+template <class E, int kN, bool kDz>
+__device__ __forceinline__ void clear_front(Raw<E, kN, kDz>& r, int n) {
+  constexpr int kPer = 4 / E::kBytes;
+#pragma unroll
+  for (int i = 0; i < Raw<E, kN, kDz>::kWords; ++i) {
+    const int c = n - i * kPer;                         // values of this word that go
+    const unsigned keep = c <= 0 ? ~0u : (c >= kPer ? 0u : ~0u << (8 * E::kBytes * c % 32));
+    r.w[i] &= keep;
+    if constexpr (kDz) r.z[i] &= keep;
+  }
 }
 template <class E, int kN, bool kDz>
 __device__ __forceinline__ void values(float (&x)[kN], const Raw<E, kN, kDz>& r) {
@@ -215,112 +198,105 @@ __device__ __forceinline__ int unit_at(int r, int c) {
   return line * 8 + (u ^ ((line ^ (line >> 3)) & 7));
 }
 
-constexpr int kThreads = 256, kTileN = 128;
+constexpr int kThreads = 256;             // of the kernels whose workgroups have four waves
 
-// A tile of kR rows (of the product's operand) by KS contraction indices, from memory through registers to LDS.
+// A tile of kR rows (of the product's operand) by KS contraction indices, from memory through registers of kT threads to LDS.
 // kCols = false: the operand's rows are the rows of the matrix; true: its columns, and the contraction runs over the rows.
-template <class E, bool kCols, bool kDz, int kR, int KS, bool kVec>
+template <class E, bool kCols, bool kDz, int kR, int KS, int kT>
 struct Stager {
   static constexpr int kP = E::kPieces;
-  static constexpr int kUnits = kR * KS / 8 / kThreads;         // per thread
+  static constexpr int kUnits = kR * KS / 8 / kT;               // per thread
   static constexpr int kN = kCols ? kUnits : 8;                 // columns per vector
   static constexpr int kRaws = kCols ? 8 : kUnits;
   static constexpr int kPlane = kR * KS / 8;                    // units per piece
   Raw<E, kN, kDz> raw[kRaws];
 
-  // rows: of the operand; r0: first row of the tile; k0 .. k_end: contraction indices.  Past the ends the last ones are read
-  // again, so that no request waits behind a branch: rows are not stored, indices are cleared by mask().
-  __device__ __forceinline__ void load(const Source& s, long long rows, long long r0, long long k0, long long k_end) {
+  // p (and z): the tile's first row, a place that all lanes share, and the first of `d` indices; the tile's begin at k0.
+  // ld, ldz in bytes; rows from the tile's first to the end.  Requests are whole vectors, none behind a branch:
+  //  - a unit that reaches behind index d is taken so much earlier that it ends there, in both operands alike, and mask()
+  //    clears the indices that the unit before has; d is at least eight;
+  //  - past the last row the last one is read again, and not stored; of columns the last whole vector (row() says which).
+  static __device__ __forceinline__ int first(int k, int d) { return min(k, d - 8); }
+  static __device__ __forceinline__ int row(int rows) {
+    if constexpr (kCols) return min((int)(threadIdx.x % (kR / kN)) * kN, rows - kN);
+    else return 0;
+  }
+  __device__ __forceinline__ void load(const char* p, const char* z, unsigned ld, unsigned ldz, int rows, int k0, int d) {
     const int t = threadIdx.x;
     if constexpr (kCols) {
-      constexpr int kBlocks = kR / kN;
-      const int c = t / kBlocks;
-      int col = (int)r0 + (t % kBlocks) * kN;
-      if constexpr (kVec) col = min(col, s.cols - kN);
-      else col = min(col, s.cols - 1);
-      const long long k = k0 + c * 8;
+      const unsigned at = (unsigned)(row(rows) * E::kBytes), k = (unsigned)(first(k0 + t / (kR / kN) * 8, d) - k0);
+      p += (long long)k0 * ld;                          // k may be negative: the sum is meant modulo 2^32 and comes out right
 #pragma unroll
-      for (int i = 0; i < 8; ++i) fetch<E, kN, kDz, kVec>(raw[i], s, min(k + i, k_end - 1), col);
+      for (int i = 0; i < 8; ++i) fetch<E, kN, false>(raw[i], p + (long long)(int)(k + i) * ld, z, at, 0);
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = t + kThreads * i, r = u / (KS / 8), c = u % (KS / 8);
-        const int k = (int)k0 + c * 8;
-        fetch<E, kN, kDz, kVec>(raw[i], s, min(r0 + r, rows - 1), k < k_end ? k : 0);
+        const int u = t + kT * i;
+        const unsigned r = (unsigned)min(u / (KS / 8), rows - 1), at = (unsigned)(first(k0 + u % (KS / 8) * 8, d) * E::kBytes);
+        fetch<E, kN, kDz>(raw[i], p, z, r * ld + at, r * ldz + at);
       }
     }
   }
-  // The same from a place that all lanes share: p (and z) at the tile's first row and index; ld, ldz in bytes; rows and
-  // indices from there to the ends.
-  __device__ __forceinline__ void load_near(const char* p, const char* z, unsigned ld, unsigned ldz, int rows, int indices) {
+  // Of the tile that was loaded; nothing to do where all its indices are there.
+  __device__ __forceinline__ void mask(int k0, int d) {
+    if (k0 + KS <= d) return;
     const int t = threadIdx.x;
     if constexpr (kCols) {
-      constexpr int kBlocks = kR / kN;
-      const int c = t / kBlocks * 8, col = min(t % kBlocks * kN, rows - (kVec ? kN : 1));
+      const int k = k0 + t / (kR / kN) * 8;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        fetch_near<E, kN, false, kVec>(raw[i], p, z, (unsigned)min(c + i, indices - 1) * ld + (unsigned)(col * E::kBytes), 0, rows - col);
+        if (i < k - first(k, d)) clear(raw[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = t + kThreads * i;
-        const unsigned r = (unsigned)min(u / (KS / 8), rows - 1);
-        int k = u % (KS / 8) * 8;
-        k = k < indices ? k : 0;
-        fetch_near<E, kN, kDz, kVec>(raw[i], p, z, r * ld + (unsigned)(k * E::kBytes), r * ldz + (unsigned)(k * E::kBytes), indices - k);
+        const int k = k0 + (t + kT * i) % (KS / 8) * 8;
+        clear_front(raw[i], k - first(k, d));
       }
     }
   }
-  __device__ __forceinline__ void mask(long long k0, long long k_end) {
-    if (k0 + KS <= k_end) return;
+  // r: of columns the place of the thread's first, row(); below zero where the tile has fewer columns than a vector: what
+  // lies in front of the tile is left out
+  __device__ __forceinline__ void store(u32x4* lds, float sign, int r) const {
     const int t = threadIdx.x;
     if constexpr (kCols) {
-      const long long k = k0 + t / (kR / kN) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i >= k_end) clear(raw[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kUnits; ++i)
-        if (k0 + (t + kThreads * i) % (KS / 8) * 8 >= k_end) clear(raw[i]);
-    }
-  }
-  __device__ __forceinline__ void store(u32x4* lds, float sign) const {
-    const int t = threadIdx.x;
-    if constexpr (kCols) {
-      constexpr int kBlocks = kR / kN;
-      const int c = t / kBlocks, r = (t % kBlocks) * kN;
-      if constexpr (E::kBytes == 2 && !kDz) {          // halves of the words of two rows
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          u32x4 p;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-          lds[unit_at<KS>(r + j, c)] = p;
-        }
-      } else {
-        float x[8][kN];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) values<E, kN, kDz>(x[i], raw[i]);
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          float y[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = kP == 1 ? x[i][j] : x[i][j] * sign;
-          u32x4 p[kP];
-          pieces_of<kP>(p, y);
-#pragma unroll
-          for (int q = 0; q < kP; ++q) lds[q * kPlane + unit_at<KS>(r + j, c)] = p[q];
-        }
-      }
+      if (r >= 0) store_columns<false>(lds, sign, r);
+      else store_columns<true>(lds, sign, r);
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = t + kThreads * i, r = u / (KS / 8), c = u % (KS / 8);
+        const int u = t + kT * i, r = u / (KS / 8), c = u % (KS / 8);
         u32x4 p[kP];
         unit(p, raw[i], sign);
 #pragma unroll
         for (int q = 0; q < kP; ++q) lds[q * kPlane + unit_at<KS>(r, c)] = p[q];
+      }
+    }
+  }
+  template <bool kInFront>
+  __device__ __forceinline__ void store_columns(u32x4* lds, float sign, int r) const {
+    const int c = threadIdx.x / (kR / kN);
+    if constexpr (E::kBytes == 2 && !kDz) {            // halves of the words of two rows
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        u32x4 p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+        if (!kInFront || r + j >= 0) lds[unit_at<KS>(r + j, c)] = p;
+      }
+    } else {
+      float x[8][kN];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) values<E, kN, kDz>(x[i], raw[i]);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = kP == 1 ? x[i][j] : x[i][j] * sign;
+        u32x4 p[kP];
+        pieces_of<kP>(p, y);
+#pragma unroll
+        for (int q = 0; q < kP; ++q)
+          if (!kInFront || r + j >= 0) lds[q * kPlane + unit_at<KS>(r + j, c)] = p[q];
       }
     }
   }
@@ -344,6 +320,67 @@ struct Stager {
         for (int k = 0; k < 8; ++k) x[k] *= sign;
       pieces_of<kP>(p, x);
     }
+  }
+};
+
+// The same for columns of up to three matrices side by side, whose rows are walked: every thread keeps the place of its own
+// columns, and steps from row to row.
+template <class E, bool kDz, int kR, int KS, int kT>
+struct ColumnStager : Stager<E, true, kDz, kR, KS, kT> {
+  typedef Stager<E, true, kDz, kR, KS, kT> Base;
+  using Base::kN;
+  using Base::raw;
+  const char *p, *z;
+  const unsigned char* e;
+  int place;             // of the thread's first column in the tile
+  int some;              // fewer columns than a vector has: so many; else 0
+
+  __device__ __forceinline__ void start(const Source& s, int col0, long long row0) {
+    // the last whole vector again where the columns end inside one
+    // (of kept rows, which are filled up to whole blocks, the last of its block)
+    const int cols = E::kBytes == 1 ? (s.cols + kKeptBlock - 1) / kKeptBlock * kKeptBlock : s.cols;
+    const int col = max(0, min(col0 + (int)(threadIdx.x % (kR / kN)) * kN, cols - kN));
+    place = col - col0;
+    some = cols < kN ? cols : 0;
+    // kept rows are one matrix, and columns of its last block may lie behind its last column
+    const int seg = E::kBytes == 1 ? 0 : (col >= s.d ? 1 : 0) + (col >= 2 * s.d ? 1 : 0), c = col - seg * s.d;
+    p = part_of(s, seg) + (row0 * s.ld + c) * E::kBytes;
+    z = kDz ? s.z + (row0 * s.ldz + col) * E::kBytes : nullptr;
+    e = E::kBytes == 1 ? s.exponent + row0 * s.ld_exponent + col / kKeptBlock : nullptr;
+  }
+  // rows: from the thread's place to the end of the slab; the place moves on by a step
+  __device__ __forceinline__ void load(const Source& s, long long rows) {
+    const int c = threadIdx.x / (kR / kN) * 8, most = (int)min(rows, (long long)KS) - 1;
+    const unsigned ld = (unsigned)s.ld * E::kBytes, ldz = (unsigned)s.ldz * E::kBytes, lde = (unsigned)s.ld_exponent;
+    if (some == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned r = (unsigned)min(c + i, most);
+        fetch<E, kN, kDz>(raw[i], p, z, r * ld, r * ldz);
+        if constexpr (E::kBytes == 1) raw[i].e = e[r * lde];
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const unsigned r = (unsigned)min(c + i, most);
+        Raw<E, kN, kDz> x;
+        fetch_some<E, kN, kDz>(x, p, z, r * ld, r * ldz, some);
+        if constexpr (E::kBytes == 1) x.e = e[r * lde];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k == i) raw[k] = x;
+      }
+    }
+    p += (size_t)KS * ld;
+    if constexpr (kDz) z += (size_t)KS * ldz;
+    if constexpr (E::kBytes == 1) e += (size_t)KS * lde;
+  }
+  __device__ __forceinline__ void mask(int rows) {
+    const int c = threadIdx.x / (kR / kN) * 8;
+    if (rows >= KS) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i >= rows) clear(raw[i]);
   }
 };
 
@@ -449,8 +486,9 @@ __device__ __forceinline__ void store_wide(char* p, long long i, const float (&x
 }
 
 // What becomes of 16 / kBytes neighbouring sums z of a row.
+// r: the residual's 16 bytes, where rows are read whole (g.vec, the columns inside).
 template <class E, bool kDz, bool kColsB>
-__device__ __forceinline__ void finish(const ProductArgs& g, long long row, int col, float (&z)[16 / E::kBytes]) {
+__device__ __forceinline__ void finish(const ProductArgs& g, long long row, int col, float (&z)[16 / E::kBytes], const unsigned (&r)[4]) {
   constexpr int kW = 16 / E::kBytes;
   if constexpr (E::kPieces > 1) {
     unsigned bad = 0;
@@ -466,8 +504,6 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
     }
   }
   if (g.vec && col + kW <= g.N) {
-    unsigned r[4];
-    if (g.R) read_words<16>(r, g.R + (row * g.ldr + col) * E::kBytes);
     if (g.bias)
 #pragma unroll
       for (int k = 0; k < kW; ++k) z[k] += g.bias[col + k];
@@ -498,8 +534,8 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
 // Few rows: a workgroup per 32 x 32 tile, operands straight from memory, the contraction dealt to its four waves in chunks of
 // 16; their sums meet in LDS.  A tile of the kernel below would keep one CU busy while the others have nothing to do.
 constexpr int kFewLd = 36;             // floats from row to row of a tile in LDS
-template <class E, bool kDz, bool kColsB, bool kVec>
-__global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs g, int few) {
+template <class E, bool kDz, bool kColsB, bool kVec>      // kVec: the contraction is a multiple of eight
+__global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs g, long long few) {
   if (g.stop && g.stop[0] != 0) return;
   constexpr int kP = E::kPieces, kW = 16 / E::kBytes;
   __shared__ float lds[4 * 32 * kFewLd];
@@ -517,14 +553,21 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
       Raw<E, kColsB ? 1 : 8, false> b[kColsB ? 8 : 1];
     };
     // past the end the last chunk again, so that no request waits behind a branch
+    const unsigned ldb = (unsigned)g.b.ld * E::kBytes;
+    const char* pb = g.b.p[0] + (kColsB ? (long long)col * E::kBytes : (long long)col * ldb);
     auto load = [&](Chunk& x, int c) {
       const int k = min(c, chunks - 1) * 16 + 8 * lh, ka = k < g.K ? k : 0;
-      fetch<E, 8, kDz, kVec>(x.a, g.a, row, ka);
+      const int seg = (ka >= 2 * g.a.d ? 2 : (ka >= g.a.d ? 1 : 0)), kd = ka - seg * g.a.d;      // parts are multiples of eight
+      const char* pa = part_of(g.a, seg) + (row * g.a.ld + kd) * E::kBytes;
+      const char* pz = kDz ? g.a.z + (row * g.a.ldz + kd) * E::kBytes : nullptr;
+      if constexpr (kVec) fetch<E, 8, kDz>(x.a, pa, pz, 0, 0);
+      else fetch_some<E, 8, kDz>(x.a, pa, pz, 0, 0, min(g.K - ka, 8));
       if constexpr (kColsB) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fetch<E, 1, false, true>(x.b[i], g.b, min(k + i, g.K - 1), col);
+        for (int i = 0; i < 8; ++i) fetch<E, 1, false>(x.b[i], pb + (long long)min(k + i, g.K - 1) * ldb, nullptr, 0, 0);
       } else {
-        fetch<E, 8, false, kVec>(x.b[0], g.b, col, ka);
+        if constexpr (kVec) fetch<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0);
+        else fetch_some<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0, min(g.K - ka, 8));
       }
     };
     f32x16 acc = zero16();
@@ -573,33 +616,56 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
     const int r = t / (32 / kW), c0 = t % (32 / kW) * kW;
     if (r < 32 && m0 + r < rows && n0 + c0 < g.N) {
       float z[kW];
+      unsigned res[4] = {0, 0, 0, 0};
+      if (g.R && g.vec && n0 + c0 + kW <= g.N) read_words<16>(res, g.R + ((m0 + r) * g.ldr + n0 + c0) * E::kBytes);
 #pragma unroll
       for (int k = 0; k < kW; ++k) {
         const float* p = lds + r * kFewLd + c0 + k;
         const float u0 = p[0], u1 = p[32 * kFewLd], u2 = p[64 * kFewLd], u3 = p[96 * kFewLd];
         z[k] = kP > 1 ? (u0 - u1) + (u2 - u3) : (u0 + u1) + (u2 + u3);
       }
-      finish<E, kDz, kColsB>(g, m0 + r, n0 + c0, z);
+      finish<E, kDz, kColsB>(g, m0 + r, n0 + c0, z, res);
     }
   }
 }
 
-// rows x N outputs, contraction over K columns of a.  Tiles of 64 kI rows x 128 columns, four waves of 32 kI x 64.
-template <class E, bool kDz, bool kColsB, bool kVec, int kI>
-__global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductArgs g, int few) {
+// rows x N outputs, contraction over K columns of a.  Tiles of 64 kI rows x 32 kWaves columns, waves of 32 kI x 64: two
+// side by side in rows, the others in columns.
+// What bounds it is how much is requested at a time: a step's loads (64 KB per CU) are on their way while the step before is
+// multiplied, some 2 us, so that every byte loaded twice shows.  Eight waves take 256 columns, and the rows of a layer of
+// that width are read once; LDS then holds two steps, and a step needs one barrier.  The next tile's first step is
+// requested before a tile's results are written, the residual's rows 32 at a time before the sums go through LDS.
+template <class E, int kWaves>
+struct ProductShape {
+  static constexpr int kI = E::kPieces == 1 ? 4 : 2, kTileM = 64 * kI, kTileN = 32 * kWaves, KS = E::kPieces == 1 ? 64 : 32;
+  static constexpr int kUnitsA = E::kPieces * kTileM * KS / 8, kUnitsB = E::kPieces * kTileN * KS / 8, kBuffers = kWaves / 4;
+  static constexpr int kLd = 68, kEnd = kWaves * 32 * kLd / 4;                    // of a wave's 32 x 64 sums, in units
+  static constexpr int kStep = kUnitsA + kUnitsB, kLds = kBuffers * kStep > kEnd ? kBuffers * kStep : kEnd;
+};
+template <class E, bool kDz, bool kColsB, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductArgs g, long long few) {
   if (g.stop && g.stop[0] != 0) return;
-  constexpr int kP = E::kPieces, KS = kP == 1 ? 64 : 32, kTileM = 64 * kI, kW = 16 / E::kBytes, kLd = 68;
-  constexpr int kUnitsA = kP * kTileM * KS / 8, kUnitsB = kP * kTileN * KS / 8;
-  constexpr int kEnd = 4 * 32 * kLd * 4 / 16, kLds = kUnitsA + kUnitsB > kEnd ? kUnitsA + kUnitsB : kEnd;
-  __shared__ u32x4 lds[kLds];
-  u32x4 *A = lds, *B = lds + kUnitsA;
+  typedef ProductShape<E, kWaves> Shape;
+  constexpr int kP = E::kPieces, KS = Shape::KS, kI = Shape::kI, kTileM = Shape::kTileM, kTileN = Shape::kTileN, kW = 16 / E::kBytes, kLd = Shape::kLd;
+  extern __shared__ u32x4 lds[];
   const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
   if (((rows + 31) >> 5) * ((g.N + 31) >> 5) <= few) return;      // few_rows_kernel
-  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
+  const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
   // the parts of a row one after another, each with steps of its own
   const int nct = (g.N + kTileN - 1) / kTileN, d = g.a.d, per = (d + KS - 1) / KS, steps = g.K / d * per;
   const unsigned lda = (unsigned)g.a.ld * E::kBytes, ldz = (unsigned)g.a.ldz * E::kBytes, ldb = (unsigned)g.b.ld * E::kBytes;
   const TileRange tr = tiles_of((rows + kTileM - 1) / kTileM * nct);
+  Stager<E, false, kDz, kTileM, KS, 64 * kWaves> sa;
+  Stager<E, kColsB, false, kTileN, KS, 64 * kWaves> sb;
+  auto load = [&](long long tile, int step) {
+    const long long m0 = tile / nct * kTileM;
+    const int n0 = (int)(tile % nct) * kTileN;
+    const int seg = step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS;
+    sa.load(part_of(g.a, seg) + m0 * lda, kDz ? g.a.z + m0 * ldz : nullptr, lda, ldz, (int)min(rows - m0, (long long)kTileM), k0, d);
+    const long long kb = (long long)seg * d;
+    sb.load(kColsB ? g.b.p[0] + kb * ldb + n0 * E::kBytes : g.b.p[0] + (long long)n0 * ldb + kb * E::kBytes, nullptr, ldb, 0,
+            min(g.N - n0, kTileN), k0, d);
+  };
   for (long long tile = tr.first; tile < tr.end; tile += tr.step) {
     const long long m0 = tile / nct * kTileM;
     const int n0 = (int)(tile % nct) * kTileN;
@@ -611,26 +677,19 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductArgs 
         acc[i][j] = zero16();
         if (kP > 1) total[i][j] = zero16();
       }
-    Stager<E, false, kDz, kTileM, KS, kVec> sa;
-    Stager<E, kColsB, false, kTileN, KS, kVec> sb;
-    const int mleft = (int)min(rows - m0, (long long)kTileM), nleft = min(g.N - n0, kTileN);
-    auto load = [&](int step) {
-      const int seg = step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS, left = d - k0;
-      sa.load_near(part_of(g.a, seg) + m0 * lda + k0 * E::kBytes, kDz ? g.a.z + m0 * ldz + k0 * E::kBytes : nullptr, lda, ldz, mleft, left);
-      const long long kb = (long long)seg * d + k0;
-      sb.load_near(kColsB ? g.b.p[0] + kb * ldb + n0 * E::kBytes : g.b.p[0] + (long long)n0 * ldb + kb * E::kBytes, nullptr, ldb, 0, nleft, left);
-    };
-    load(0);
+    load(tile, 0);
     for (int step = 0; step < steps; ++step) {
       const float sign = (step >> 1) & 1 ? -1.f : 1.f;
-      const int at = step % per * KS;
+      const int k0 = step % per * KS;
+      u32x4* A = lds + (Shape::kBuffers > 1 ? (step & 1) * Shape::kStep : 0);
+      u32x4* B = A + Shape::kUnitsA;
+      sa.mask(k0, d);
+      sb.mask(k0, d);
+      if (Shape::kBuffers == 1 || step == 0) __syncthreads();          // the last step's reads, or the last tile's sums, are done
+      sa.store(A, 1.f, 0);
+      sb.store(B, sign, sb.row(min(g.N - n0, kTileN)));
       __syncthreads();
-      sa.mask(at, d);
-      sb.mask(at, d);
-      sa.store(A, 1.f);
-      sb.store(B, sign);
-      __syncthreads();
-      if (step + 1 < steps) load(step + 1);
+      if (step + 1 < steps) load(tile, step + 1);
       multiply<kP, kP, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
       if constexpr (kP > 1) {
         if ((step & 1) || step + 1 == steps) add_section<kI>(total, acc, sign);
@@ -640,7 +699,16 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductArgs 
     // register v of a lane: row l32, column 8 (v / 4) + 4 lh + v % 4 of a block; through LDS, 32 rows of a wave at a time, so
     // that a wave reads and writes whole rows of its 64 columns
     float* end = reinterpret_cast<float*>(lds) + wave * 32 * kLd;
+    constexpr int kLanes = 64 / kW, kRounds = 32 / kW;
+    const int c0 = lane % kLanes * kW, col = n0 + wn * 64 + c0;
+    const bool wide = g.vec && col + kW <= g.N;
     for (int part = 0; part < kI; ++part) {
+      const long long r0 = m0 + wm * 32 * kI + part * 32 + lane / kLanes;
+      unsigned res[kRounds][4];
+      if (g.R && wide) {                               // requested together; past the end the last row again
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) read_words<16>(res[u], g.R + (min(r0 + u * kW, rows - 1) * g.ldr + col) * E::kBytes);
+      }
 #pragma unroll
       for (int i = 0; i < kI; ++i)
         if (i == part) {
@@ -655,21 +723,19 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const ProductArgs 
             }
         }
       __builtin_amdgcn_wave_barrier();
-      const long long r0 = m0 + wm * 32 * kI + part * 32;
-      const int c0 = lane % (64 / kW) * kW, col = n0 + wn * 64 + c0;
-#pragma unroll 2
-      for (int r = lane / (64 / kW); r < 32; r += kW) {
-        if (r0 + r >= rows || col >= g.N) continue;
+#pragma unroll
+      for (int u = 0; u < kRounds; ++u) {
+        if (r0 + u * kW >= rows || col >= g.N) continue;
         float z[kW];
 #pragma unroll
         for (int k = 0; k < kW; k += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(end + r * kLd + c0 + k);
+          const float4 v = *reinterpret_cast<const float4*>(end + (lane / kLanes + u * kW) * kLd + c0 + k);
           z[k] = v.x;
           z[k + 1] = v.y;
           z[k + 2] = v.z;
           z[k + 3] = v.w;
         }
-        finish<E, kDz, kColsB>(g, r0 + r, col, z);
+        finish<E, kDz, kColsB>(g, r0 + u * kW, col, z, res[u]);
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -764,20 +830,26 @@ __device__ __forceinline__ Slab slab_rows(const WeightArgs& g, long long rows, i
   const long long r0 = min((long long)slab * per, rows);
   return {r0, min(r0 + per, rows)};
 }
-template <class EA, class EB>
+// Tiles of dW: 64 kI x 32 kWaves, as above; every tile of a slab loads the slab's rows, so that wide ones load less.
+template <class EA, class EB, int kWaves>
 struct WeightShape {
-  static constexpr int KS = EA::kPieces == 1 && EB::kPieces == 1 ? 64 : 32;
-  static constexpr int kI = 2, kTileM = 64 * kI;
+  static constexpr int KS = EB::kPieces == 1 ? 64 : 32, kI = EB::kPieces == 1 ? kWaves / 2 : 2;
+  static constexpr int kTileM = 64 * kI, kTileN = 32 * kWaves, kT = 64 * kWaves, kBuffers = kWaves / 4;
+  static constexpr int kUnitsA = EA::kPieces * kTileM * KS / 8, kUnitsB = EB::kPieces * kTileN * KS / 8, kStep = kUnitsA + kUnitsB;
+  static constexpr int kLds = kBuffers * kStep;
 };
+template <class EB>
+constexpr int kSlabStep = EB::kPieces == 1 ? 64 : 32;
 
-template <class EA, class EB, bool kDz, bool kVec>
-__global__ __launch_bounds__(kThreads, 2) void weight_kernel(const WeightArgs g) {
+template <class EA, class EB, bool kDz, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs g) {
   if (g.stop && g.stop[0] != 0) return;
-  constexpr int kPA = EA::kPieces, kPB = EB::kPieces, KS = WeightShape<EA, EB>::KS, kI = WeightShape<EA, EB>::kI, kHold = 256 / KS;
-  constexpr int kTileM = WeightShape<EA, EB>::kTileM, kN = kTileN * KS / 8 / kThreads;
-  __shared__ u32x4 A[kPA * kTileM * KS / 8], B[kPB * kTileN * KS / 8];
+  typedef WeightShape<EA, EB, kWaves> Shape;
+  constexpr int kPA = EA::kPieces, kPB = EB::kPieces, KS = Shape::KS, kI = Shape::kI, kHold = 256 / KS, kT = Shape::kT;
+  constexpr int kTileM = Shape::kTileM, kTileN = Shape::kTileN;
+  extern __shared__ u32x4 lds[];
   const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
-  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
+  const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
   const int tiles_n = (g.N + kTileN - 1) / kTileN, tiles_m = max(1, (g.M + kTileM - 1) / kTileM), ntile = tiles_m * tiles_n;
   // the tiles of a slab read the same rows: they run on one XCD (the grid is ntile * S, S a multiple of eight)
   const int item = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
@@ -795,29 +867,36 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(const WeightArgs g)
       if (kPB > 1) total[i][j] = zero16();
     }
   const bool want_sums = g.sums && m0 == 0;
+  ColumnStager<EA, false, kTileM, KS, kT> sa;
+  ColumnStager<EB, kDz, kTileN, KS, kT> sb;
+  constexpr int kN = ColumnStager<EB, kDz, kTileN, KS, kT>::kN;
   double sums[kN];
 #pragma unroll
   for (int j = 0; j < kN; ++j) sums[j] = 0.0;
-  Stager<EA, true, false, kTileM, KS, kVec> sa;
-  Stager<EB, true, kDz, kTileN, KS, kVec> sb;
+  const bool product = g.M > 0;
+  if (product) sa.start(g.a, m0, sl.r0);
+  sb.start(g.b, n0, sl.r0);
   if (steps > 0) {
-    if (g.M > 0) sa.load(g.a, rows, m0, sl.r0, sl.r1);
-    sb.load(g.b, rows, n0, sl.r0, sl.r1);
+    if (product) sa.load(g.a, sl.r1 - sl.r0);
+    sb.load(g.b, sl.r1 - sl.r0);
   }
   for (int step = 0; step < steps; ++step) {
     const float sign = ((step / kHold) ^ slab) & 1 ? -1.f : 1.f;
-    __syncthreads();
-    sa.mask(sl.r0 + (long long)step * KS, sl.r1);
-    sb.mask(sl.r0 + (long long)step * KS, sl.r1);
-    if (g.M > 0) sa.store(A, 1.f);
-    sb.store(B, sign);
+    const long long left = sl.r1 - sl.r0 - (long long)step * KS;
+    u32x4* A = lds + (Shape::kBuffers > 1 ? (step & 1) * Shape::kStep : 0);
+    u32x4* B = A + Shape::kUnitsA;
+    sa.mask((int)min(left, (long long)KS));
+    sb.mask((int)min(left, (long long)KS));
+    if (Shape::kBuffers == 1) __syncthreads();
+    if (product) sa.store(A, 1.f, sa.place);
+    sb.store(B, sign, sb.place);
     if (want_sums) sb.add_columns(sums);
     __syncthreads();
     if (step + 1 < steps) {
-      if (g.M > 0) sa.load(g.a, rows, m0, sl.r0 + (long long)(step + 1) * KS, sl.r1);
-      sb.load(g.b, rows, n0, sl.r0 + (long long)(step + 1) * KS, sl.r1);
+      if (product) sa.load(g.a, left - KS);
+      sb.load(g.b, left - KS);
     }
-    if (g.M > 0) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
+    if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
     if constexpr (kPB > 1) {
       if (step % kHold == kHold - 1 || step + 1 == steps) add_section<kI>(total, acc, sign);
     }
@@ -846,16 +925,19 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(const WeightArgs g)
       }
   }
   if (want_sums) {                                   // the same for the whole workgroup
-    __shared__ double red[KS / 8][kTileN];
+    double* red = reinterpret_cast<double*>(lds);    // [KS / 8][kTileN]
     constexpr int kBlocks = kTileN / kN;
+    static_assert(KS / 8 * kTileN * 8 <= Shape::kLds * 16, "column sums in LDS");
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kN; ++j) red[threadIdx.x / kBlocks][threadIdx.x % kBlocks * kN + j] = sums[j];
+    for (int j = 0; j < kN; ++j)
+      if (sb.place + j >= 0) red[threadIdx.x / kBlocks * kTileN + sb.place + j] = sums[j];
     __syncthreads();
     const int n = n0 + (int)threadIdx.x;
     if (threadIdx.x < kTileN && n < g.N) {
       double v = 0.0;
 #pragma unroll
-      for (int c = 0; c < KS / 8; ++c) v += red[c][threadIdx.x];
+      for (int c = 0; c < KS / 8; ++c) v += red[c * kTileN + threadIdx.x];
       P[(size_t)g.M * g.N + n] = (float)v;
     }
   }
@@ -887,7 +969,7 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, 
               s += (double)p[u * stride];
               continue;
             }
-            const Slab sl = slab_rows(g, rows, k + u, WeightShape<EA, EB>::KS);
+            const Slab sl = slab_rows(g, rows, k + u, kSlabStep<EB>);
             float v = 0.f;
             for (long long r = sl.r0; r < sl.r1; ++r) v = fmaf(single<EA, false>(g.a, r, m), single<EB, kDz>(g.b, r, n), v);
             s += (double)v;
@@ -903,12 +985,16 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, 
   }
 }
 
-// The slabs of a weight gradient: one round of workgroups at two per CU, and at least 256 rows each.
-int slabs_of(long long rows, int K, int N, int n_cu) {
-  const int ntile = ((K + 127) / 128) * ((N + kTileN - 1) / kTileN);
-  long long S = 2 * n_cu / (ntile < 1 ? 1 : ntile), by_rows = (rows + 255) / 256;
-  if (S > by_rows) S = by_rows;
-  S = (S + 7) / 8 * 8;
+// Eight waves where they compute no more columns than four would: N is at least 129, and its last tile of 256 is more than half
+// full.
+bool eight_waves(int N) { return (N + 255) / 256 * 256 == (N + 127) / 128 * 128; }
+// The slabs of a weight gradient: one round of workgroups (two of four waves per CU, or one of eight), at least 256 rows each.
+int slabs_of(long long rows, int K, int N, int bf16, int n_cu) {
+  const bool eight = eight_waves(N);
+  const int m = eight && bf16 ? 256 : 128, n = eight ? 256 : 128;
+  const int ntile = ((K + m - 1) / m) * ((N + n - 1) / n);
+  long long S = (eight ? 1 : 2) * n_cu / (ntile < 1 ? 1 : ntile) / 8 * 8, by_rows = (rows + 255) / 256;
+  if (S > by_rows) S = (by_rows + 7) / 8 * 8;
   return S < 8 ? 8 : (int)S;
 }
 bool smooth(int act) { return act == DC_ACT_GELU || act == DC_ACT_SILU; }
@@ -917,17 +1003,33 @@ int slope_blocks(long long rows, int n_cu) {           // row blocks of the pass
   return (int)(want < 1 ? 1 : (want < most ? want : most));
 }
 
+template <class K>
+hipError_t allow_lds(K kernel, size_t bytes) {
+  return bytes > 64 * 1024 ? hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : hipSuccess;
+}
+template <class E, bool kDz, bool kColsB, int kWaves>
+hipError_t product_tiles(const ProductArgs& g, long long rows, int n_cu, long long few, hipStream_t s) {
+  typedef ProductShape<E, kWaves> Shape;
+  const long long most = (long long)n_cu * 8 / kWaves, tiles = (rows + Shape::kTileM - 1) / Shape::kTileM * ((g.N + Shape::kTileN - 1) / Shape::kTileN);
+  auto kernel = product_kernel<E, kDz, kColsB, kWaves>;
+  const hipError_t e = allow_lds(kernel, Shape::kLds * 16);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles < most ? tiles : most) + 7) / 8 * 8), dim3(64 * kWaves), Shape::kLds * 16, s, g, few);
+  return hipGetLastError();
+}
 // Up to `few` 32 x 32 tiles, each gets a workgroup: two rounds of two workgroups per CU.  Where only the device knows the
 // rows both kernels are launched, and one of them leaves at once.
-template <class E, bool kDz, bool kColsB, bool kVec>
+template <class E, bool kDz, bool kColsB>
 hipError_t product(const ProductArgs& g, long long rows, int n_cu, hipStream_t s) {
-  constexpr int kI = E::kPieces == 1 ? 4 : 2;
-  const int few = 4 * n_cu;
-  const long long most = 2LL * n_cu, small = (rows + 31) / 32 * ((g.N + 31) / 32), large = (rows + 64 * kI - 1) / (64 * kI) * ((g.N + kTileN - 1) / kTileN);
-  if (small <= few || g.nrows)
-    hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, kVec>), dim3((unsigned)(small < 2 * most ? small : 2 * most)), dim3(kThreads), 0, s, g, few);
-  if (small > few)
-    hipLaunchKernelGGL((product_kernel<E, kDz, kColsB, kVec, kI>), dim3((unsigned)((large < most ? large : most) + 7) / 8 * 8), dim3(kThreads), 0, s, g, few);
+  const bool narrow = g.a.d < 8 || g.N < 4;            // less than a vector of the tiles' loads
+  const long long small = (rows + 31) / 32 * ((g.N + 31) / 32);
+  const long long few = narrow ? (1LL << 62) : 4 * n_cu;
+  if (small <= few || g.nrows) {
+    const dim3 grid((unsigned)(small < 4 * n_cu ? small : 4 * n_cu));
+    if (g.a.d % 8 == 0) hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, true>), grid, dim3(kThreads), 0, s, g, few);
+    else hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, false>), grid, dim3(kThreads), 0, s, g, few);
+  }
+  if (small > few) return eight_waves(g.N) ? product_tiles<E, kDz, kColsB, 8>(g, rows, n_cu, few, s) : product_tiles<E, kDz, kColsB, 4>(g, rows, n_cu, few, s);
   return hipGetLastError();
 }
 
@@ -959,14 +1061,23 @@ hipError_t dense(const DenseArgs& a, hipStream_t s) {
   auto starts = [](const void* p, long long ld) { return !p || (ld % kWide == 0 && reinterpret_cast<size_t>(p) % 16 == 0); };
   g.vec = starts(a.R, a.ldr) && starts(a.Z, a.ldz) && starts(a.Y, a.ldy);
   g.stop = a.stop;
-  return a.d % 8 == 0 && a.N % 4 == 0 ? product<E, false, true, true>(g, a.rows, a.n_cu, s) : product<E, false, true, false>(g, a.rows, a.n_cu, s);
+  return product<E, false, true>(g, a.rows, a.n_cu, s);
 }
 
-template <class E, class EX, bool kDz, bool kVec>
+template <class E, class EX, bool kDz, int kWaves>
+hipError_t weight_tiles(const WeightArgs& w, hipStream_t s) {
+  typedef WeightShape<EX, E, kWaves> Shape;
+  const int ntile = (w.M > 0 ? (w.M + Shape::kTileM - 1) / Shape::kTileM : 1) * ((w.N + Shape::kTileN - 1) / Shape::kTileN);
+  auto kernel = weight_kernel<EX, E, kDz, kWaves>;
+  const hipError_t e = allow_lds(kernel, Shape::kLds * 16);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(ntile * w.S), dim3(64 * kWaves), Shape::kLds * 16, s, w);
+  return hipGetLastError();
+}
+template <class E, class EX, bool kDz>
 hipError_t weight(const WeightArgs& w, const DenseBackArgs& a, float* db, hipStream_t s) {
-  constexpr int kTileM = WeightShape<EX, E>::kTileM;
-  const int ntile = (w.M > 0 ? (w.M + kTileM - 1) / kTileM : 1) * ((w.N + kTileN - 1) / kTileN);
-  hipLaunchKernelGGL((weight_kernel<EX, E, kDz, kVec>), dim3(ntile * w.S), dim3(kThreads), 0, s, w);
+  const hipError_t e = eight_waves(w.N) ? weight_tiles<E, EX, kDz, 8>(w, s) : weight_tiles<E, EX, kDz, 4>(w, s);
+  if (e != hipSuccess) return e;
   const long long total = (long long)w.M * w.N + w.N, most = (long long)a.n_cu * 8, want = (total + 255) / 256;
   hipLaunchKernelGGL((weight_reduce_kernel<EX, E, kDz>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, w,
                      static_cast<char*>(a.dW), a.lddw, db);
@@ -1017,7 +1128,7 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     g.ldy = a.lddx;
     g.vec = a.lddx % kWide == 0 && reinterpret_cast<size_t>(a.dX) % 16 == 0;
     g.stop = a.stop;
-    e = a.N % 8 == 0 ? product<E, kDz, false, true>(g, a.rows, a.n_cu, s) : product<E, kDz, false, false>(g, a.rows, a.n_cu, s);
+    e = product<E, kDz, false>(g, a.rows, a.n_cu, s);
   }
   if (e == hipSuccess && (a.dW || db)) {
     WeightArgs w{};
@@ -1025,7 +1136,6 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     w.M = a.dW ? K : 0;
     w.a.cols = K;
     w.a.d = a.d;
-    const bool vec = a.N % 4 == 0 && a.d % 4 == 0;
     if (a.kept.code) {
       w.a.p[0] = reinterpret_cast<const char*>(a.kept.code);
       w.a.exponent = a.kept.exponent;
@@ -1038,12 +1148,11 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     w.b = dz;
     w.nrows = a.nrows;
     w.N = a.N;
-    w.S = slabs_of(a.rows, K, a.N, a.n_cu);
+    w.S = slabs_of(a.rows, K, a.N, a.bf16, a.n_cu);
     w.part = workspace;
     w.sums = db != nullptr;
     w.stop = a.stop;
-    if (a.kept.code) e = vec ? weight<E, Kept, kDz, true>(w, a, db, s) : weight<E, Kept, kDz, false>(w, a, db, s);
-    else e = vec ? weight<E, E, kDz, true>(w, a, db, s) : weight<E, E, kDz, false>(w, a, db, s);
+    e = a.kept.code ? weight<E, Kept, kDz>(w, a, db, s) : weight<E, E, kDz>(w, a, db, s);
   }
   return e;
 }
@@ -1059,7 +1168,7 @@ size_t dense_dz_floats(long long rows, int N, int bf16) {
   return ((size_t)rows * N * (bf16 ? 2 : 4) + 15) / 16 * 4;
 }
 size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu) {
-  size_t n = (size_t)slabs_of(rows, K, N, n_cu) * ((size_t)K * N + N);
+  size_t n = (size_t)slabs_of(rows, K, N, bf16, n_cu) * ((size_t)K * N + N);
   if (smooth(act)) n += dense_dz_floats(rows, N, bf16) + (size_t)slope_blocks(rows, n_cu) * N;
   return n;
 }
