@@ -152,14 +152,17 @@ __device__ __forceinline__ void clear_front(Raw<E, kN, kDz>& r, int n) {
   }
 }
 template <class E, int kN, bool kDz>
-__device__ __forceinline__ void values(float (&x)[kN], const Raw<E, kN, kDz>& r) {
+__device__ __forceinline__ float value(const Raw<E, kN, kDz>& r, int k) {
   float scale = 1.f;
   if constexpr (E::kBytes == 1) scale = kept_scale(r.e);
+  const float x = value_of<E>(r.w, k, scale);
+  if constexpr (kDz) return value_of<E>(r.z, k, 1.f) > 0.f ? x : 0.f;
+  else return x;
+}
+template <class E, int kN, bool kDz>
+__device__ __forceinline__ void values(float (&x)[kN], const Raw<E, kN, kDz>& r) {
 #pragma unroll
-  for (int k = 0; k < kN; ++k) {
-    x[k] = value_of<E>(r.w, k, scale);
-    if constexpr (kDz) x[k] = value_of<E>(r.z, k, 1.f) > 0.f ? x[k] : 0.f;
-  }
+  for (int k = 0; k < kN; ++k) x[k] = value(r, k);
 }
 
 // ---- pieces ----
@@ -198,49 +201,82 @@ __device__ __forceinline__ int unit_at(int r, int c) {
   return line * 8 + (u ^ ((line ^ (line >> 3)) & 7));
 }
 
+// Byte addresses in such a tile follow from one another by exclusive ors and constants, which keeps a step's addresses in a
+// handful of registers (kept apart, they did not fit, and a register read back from scratch memory waits for every load that
+// was requested before it):
+//  - n rows on (n a multiple of 32; KS = 32: of 16 within two such steps): rows_on<KS>(n) exclusive or, n * KS * 2 on;
+//  - chunk c on from chunk lh (0 or 1), in pairs: exclusive or c * 16.
+template <int KS>
+constexpr unsigned rows_on(int n) {
+  return (unsigned)((KS == 64 ? n >> 3 : n >> 4) & 7) << 4;
+}
+
 constexpr int kThreads = 256;             // of the kernels whose workgroups have four waves
 
 // A tile of kR rows (of the product's operand) by KS contraction indices, from memory through registers of kT threads to LDS.
 // kCols = false: the operand's rows are the rows of the matrix; true: its columns, and the contraction runs over the rows.
 template <class E, bool kCols, bool kDz, int kR, int KS, int kT>
 struct Stager {
-  static constexpr int kP = E::kPieces;
-  static constexpr int kUnits = kR * KS / 8 / kT;               // per thread
+  static constexpr int kP = E::kPieces, kC = KS / 8;
+  static constexpr int kUnits = kR * kC / kT;                   // per thread
   static constexpr int kN = kCols ? kUnits : 8;                 // columns per vector
   static constexpr int kRaws = kCols ? 8 : kUnits;
-  static constexpr int kPlane = kR * KS / 8;                    // units per piece
+  static constexpr int kPlane = kR * kC;                        // units per piece
+  static constexpr int kRowsOn = kT / kC;                       // rows between a thread's units (kCols = false)
   Raw<E, kN, kDz> raw[kRaws];
+  unsigned off, offz;    // of the thread's first vector from the tile's first row and index, in bytes
+  unsigned at;           // of its first unit in LDS, in bytes
 
-  // p (and z): the tile's first row, a place that all lanes share, and the first of `d` indices; the tile's begin at k0.
-  // ld, ldz in bytes; rows from the tile's first to the end.  Requests are whole vectors, none behind a branch:
+  // ld, ldz: bytes from row to row
+  __device__ __forceinline__ void start(unsigned ld, unsigned ldz) {
+    const unsigned t = threadIdx.x;
+    const unsigned row = kCols ? t / (kR / kN) * 8 : t / kC, col = kCols ? t % (kR / kN) * kN : t % kC * 8;
+    off = row * ld + col * E::kBytes;
+    offz = kDz ? row * ldz + col * E::kBytes : 0;
+    at = (unsigned)(kCols ? unit_at<KS>(col, row / 8) : unit_at<KS>(row, col / 8)) * 16;
+  }
+  // Requests are whole vectors, none behind a branch:
   //  - a unit that reaches behind index d is taken so much earlier that it ends there, in both operands alike, and mask()
   //    clears the indices that the unit before has; d is at least eight;
-  //  - past the last row the last one is read again, and not stored; of columns the last whole vector (row() says which).
+  //  - past the last row the last one is read again, and not stored; of columns the last whole vector (place() says which).
   static __device__ __forceinline__ int first(int k, int d) { return min(k, d - 8); }
-  static __device__ __forceinline__ int row(int rows) {
-    if constexpr (kCols) return min((int)(threadIdx.x % (kR / kN)) * kN, rows - kN);
-    else return 0;
+  // Place of the thread's first column in a tile of that many; below zero where they are fewer than a vector has.
+  static __device__ __forceinline__ int place(int t, int cols) { return min(t % (kR / kN) * kN, cols - kN); }
+  // The thread's number, not to be computed with ahead of time: what the last tiles need is formed where they need it.
+  static __device__ __forceinline__ int thread_now() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
   }
+  // p (and z): the tile's first row at index k0 (kCols: index k0 at the tile's first column), a place that all lanes share;
+  // rows from there to the end; the indices end at d.
   __device__ __forceinline__ void load(const char* p, const char* z, unsigned ld, unsigned ldz, int rows, int k0, int d) {
-    const int t = threadIdx.x;
-    if constexpr (kCols) {
-      const unsigned at = (unsigned)(row(rows) * E::kBytes), k = (unsigned)(first(k0 + t / (kR / kN) * 8, d) - k0);
-      p += (long long)k0 * ld;                          // k may be negative: the sum is meant modulo 2^32 and comes out right
+    if (rows >= kR && k0 + KS <= d) {                  // the same for all lanes
 #pragma unroll
-      for (int i = 0; i < 8; ++i) fetch<E, kN, false>(raw[i], p + (long long)(int)(k + i) * ld, z, at, 0);
+      for (int i = 0; i < kRaws; ++i) {
+        const size_t on = (size_t)(kCols ? i : i * kRowsOn);
+        fetch<E, kN, kDz>(raw[i], p + on * ld, kDz ? z + on * ldz : nullptr, off, offz);
+      }
+      return;
+    }
+    const int t = thread_now();
+    if constexpr (kCols) {
+      const int k = first(k0 + t / (kR / kN) * 8, d) - k0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) fetch<E, kN, kDz>(raw[i], p + (long long)(k + i) * ld + place(t, rows) * E::kBytes, nullptr, 0, 0);
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = t + kT * i;
-        const unsigned r = (unsigned)min(u / (KS / 8), rows - 1), at = (unsigned)(first(k0 + u % (KS / 8) * 8, d) * E::kBytes);
-        fetch<E, kN, kDz>(raw[i], p, z, r * ld + at, r * ldz + at);
+        const long long r = min(t / kC + i * kRowsOn, rows - 1);
+        const int c = (first(k0 + t % kC * 8, d) - k0) * E::kBytes;
+        fetch<E, kN, kDz>(raw[i], p + r * ld + c, kDz ? z + r * ldz + c : nullptr, 0, 0);
       }
     }
   }
   // Of the tile that was loaded; nothing to do where all its indices are there.
   __device__ __forceinline__ void mask(int k0, int d) {
     if (k0 + KS <= d) return;
-    const int t = threadIdx.x;
+    const int t = thread_now();
     if constexpr (kCols) {
       const int k = k0 + t / (kR / kN) * 8;
 #pragma unroll
@@ -249,55 +285,58 @@ struct Stager {
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int k = k0 + (t + kT * i) % (KS / 8) * 8;
+        const int k = k0 + (t + kT * i) % kC * 8;
         clear_front(raw[i], k - first(k, d));
       }
     }
   }
-  // r: of columns the place of the thread's first, row(); below zero where the tile has fewer columns than a vector: what
-  // lies in front of the tile is left out
-  __device__ __forceinline__ void store(u32x4* lds, float sign, int r) const {
-    const int t = threadIdx.x;
-    if constexpr (kCols) {
-      if (r >= 0) store_columns<false>(lds, sign, r);
-      else store_columns<true>(lds, sign, r);
-    } else {
+  __device__ __forceinline__ void put(u32x4* lds, unsigned byte, const u32x4 (&p)[kP]) const {
+#pragma unroll
+    for (int q = 0; q < kP; ++q) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(lds + q * kPlane) + byte) = p[q];
+  }
+  // cols (kCols): of the tile
+  __device__ __forceinline__ void store(u32x4* lds, float sign, int cols) const {
+    if constexpr (!kCols) {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = t + kT * i, r = u / (KS / 8), c = u % (KS / 8);
         u32x4 p[kP];
         unit(p, raw[i], sign);
-#pragma unroll
-        for (int q = 0; q < kP; ++q) lds[q * kPlane + unit_at<KS>(r, c)] = p[q];
+        put(lds, (at ^ rows_on<KS>(i * kRowsOn)) + (unsigned)(i * kRowsOn * KS * 2), p);
       }
-    }
-  }
-  template <bool kInFront>
-  __device__ __forceinline__ void store_columns(u32x4* lds, float sign, int r) const {
-    const int c = threadIdx.x / (kR / kN);
-    if constexpr (E::kBytes == 2 && !kDz) {            // halves of the words of two rows
+    } else if (cols >= kR) {
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
-        u32x4 p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-        if (!kInFront || r + j >= 0) lds[unit_at<KS>(r + j, c)] = p;
+        u32x4 p[kP];
+        column(p, j, sign);
+        // a row on within a vector: KS = 64 the next line and bit j of the spread, KS = 32 the other half of the line
+        put(lds, KS == 64 ? (at ^ (unsigned)(j << 4)) + (unsigned)(j * 128) : at ^ (unsigned)(j << 6), p);
       }
     } else {
-      float x[8][kN];
+      store_at(lds, sign, place(thread_now(), cols));
+    }
+  }
+  // The thread's first column at that place; what lies in front of the tile is left out.
+  __device__ __forceinline__ void store_at(u32x4* lds, float sign, int place) const {
+    const int c = thread_now() / (kR / kN);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) values<E, kN, kDz>(x[i], raw[i]);
+    for (int j = 0; j < kN; ++j) {
+      u32x4 p[kP];
+      column(p, j, sign);
+      if (place + j >= 0) put(lds, (unsigned)unit_at<KS>(place + j, c) * 16, p);
+    }
+  }
+  __device__ __forceinline__ void column(u32x4 (&p)[kP], int j, float sign) const {
+    if constexpr (E::kBytes == 2 && !kDz) {            // halves of the words of two rows
 #pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        float y[8];
+      for (int i = 0; i < 4; ++i) p[0][i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+    } else {
+      float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = kP == 1 ? x[i][j] : x[i][j] * sign;
-        u32x4 p[kP];
-        pieces_of<kP>(p, y);
-#pragma unroll
-        for (int q = 0; q < kP; ++q)
-          if (!kInFront || r + j >= 0) lds[q * kPlane + unit_at<KS>(r + j, c)] = p[q];
+      for (int i = 0; i < 8; ++i) {
+        const float x = value<E, kN, kDz>(raw[i], j);
+        y[i] = kP == 1 ? x : x * sign;
       }
+      pieces_of<kP>(p, y);
     }
   }
   // Adds the columns' values of the tile (kCols).
@@ -332,15 +371,18 @@ struct ColumnStager : Stager<E, true, kDz, kR, KS, kT> {
   using Base::raw;
   const char *p, *z;
   const unsigned char* e;
-  int place;             // of the thread's first column in the tile
+  int here;              // place of the thread's first column in the tile
   int some;              // fewer columns than a vector has: so many; else 0
+  bool whole;            // the tile's columns are all there
 
   __device__ __forceinline__ void start(const Source& s, int col0, long long row0) {
-    // the last whole vector again where the columns end inside one
-    // (of kept rows, which are filled up to whole blocks, the last of its block)
+    Base::start(0, 0);
+    // the last whole vector again where the columns end inside one (of kept rows, which are filled up to whole blocks, the
+    // last of its block)
     const int cols = E::kBytes == 1 ? (s.cols + kKeptBlock - 1) / kKeptBlock * kKeptBlock : s.cols;
     const int col = max(0, min(col0 + (int)(threadIdx.x % (kR / kN)) * kN, cols - kN));
-    place = col - col0;
+    here = col - col0;
+    whole = col0 + kR <= cols;
     some = cols < kN ? cols : 0;
     // kept rows are one matrix, and columns of its last block may lie behind its last column
     const int seg = E::kBytes == 1 ? 0 : (col >= s.d ? 1 : 0) + (col >= 2 * s.d ? 1 : 0), c = col - seg * s.d;
@@ -353,11 +395,23 @@ struct ColumnStager : Stager<E, true, kDz, kR, KS, kT> {
     const int c = threadIdx.x / (kR / kN) * 8, most = (int)min(rows, (long long)KS) - 1;
     const unsigned ld = (unsigned)s.ld * E::kBytes, ldz = (unsigned)s.ldz * E::kBytes, lde = (unsigned)s.ld_exponent;
     if (some == 0) {
+      // one offset a thread, of the last rows' steps one for each
+      unsigned r = c;
+      asm volatile("" : "+v"(r));
+      if (most == KS - 1) {
+        const unsigned o = r * ld, oz = r * ldz, oe = r * lde;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const unsigned r = (unsigned)min(c + i, most);
-        fetch<E, kN, kDz>(raw[i], p, z, r * ld, r * ldz);
-        if constexpr (E::kBytes == 1) raw[i].e = e[r * lde];
+        for (int i = 0; i < 8; ++i) {
+          fetch<E, kN, kDz>(raw[i], p + (size_t)i * ld, kDz ? z + (size_t)i * ldz : nullptr, o, oz);
+          if constexpr (E::kBytes == 1) raw[i].e = (e + (size_t)i * lde)[oe];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const unsigned q = (unsigned)min((int)r + i, most);
+          fetch<E, kN, kDz>(raw[i], p, z, q * ld, q * ldz);
+          if constexpr (E::kBytes == 1) raw[i].e = e[q * lde];
+        }
       }
     } else {
 #pragma unroll 1
@@ -376,11 +430,15 @@ struct ColumnStager : Stager<E, true, kDz, kR, KS, kT> {
     if constexpr (E::kBytes == 1) e += (size_t)KS * lde;
   }
   __device__ __forceinline__ void mask(int rows) {
-    const int c = threadIdx.x / (kR / kN) * 8;
     if (rows >= KS) return;
+    const int c = Base::thread_now() / (kR / kN) * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (c + i >= rows) clear(raw[i]);
+  }
+  __device__ __forceinline__ void store(u32x4* lds, float sign) const {
+    if (whole) Base::store(lds, sign, kR);
+    else Base::store_at(lds, sign, here);
   }
 };
 
@@ -394,22 +452,31 @@ __device__ __forceinline__ f32x16 mfma(const u32x4& b, const u32x4& a, const f32
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
 }
 
-// One staged step: acc[i][j] += A (rows a0 + 32 i ..) times B (rows b0 + 32 j ..).  The small products first.
+// Where a lane's operands of a wave's first 32 rows lie, in bytes: row `row0` (a multiple of 64) + lane % 32, chunk lane / 32.
+template <int KS>
+__device__ __forceinline__ unsigned operands_at(int row0) {
+  const int lane = threadIdx.x & 63;
+  return (unsigned)unit_at<KS>(row0 + (lane & 31), lane >> 5) * 16;
+}
+// One staged step: acc[i][j] += A (rows a0 + 32 i ..) times B (rows b0 + 32 j ..), from where operands_at() says for a0 and
+// b0.  The small products first.
 template <int kPA, int kPB, int KS, int kRA, int kRB, int kI>
-__device__ __forceinline__ void multiply(f32x16 (&acc)[kI][2], const u32x4* A, const u32x4* B, int a0, int b0) {
+__device__ __forceinline__ void multiply(f32x16 (&acc)[kI][2], const u32x4* A, const u32x4* B, unsigned a0, unsigned b0) {
   constexpr int kMost = kPA > kPB ? kPA : kPB;
-  const int lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
+  asm volatile("" : "+v"(a0), "+v"(b0));               // the addresses that follow are formed here, not kept from step to step
 #pragma unroll
   for (int k = 0; k < KS / 16; ++k) {
     u32x4 a[kPA][kI], b[kPB][2];
 #pragma unroll
     for (int p = 0; p < kPA; ++p)
 #pragma unroll
-      for (int i = 0; i < kI; ++i) a[p][i] = A[p * (kRA * KS / 8) + unit_at<KS>(a0 + i * 32 + l32, 2 * k + lh)];
+      for (int i = 0; i < kI; ++i)
+        a[p][i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(A + p * (kRA * KS / 8)) + (a0 ^ (unsigned)(k << 5) ^ rows_on<KS>(32 * i)) + i * KS * 64);
 #pragma unroll
     for (int p = 0; p < kPB; ++p)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) b[p][j] = B[p * (kRB * KS / 8) + unit_at<KS>(b0 + j * 32 + l32, 2 * k + lh)];
+      for (int j = 0; j < 2; ++j)
+        b[p][j] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(B + p * (kRB * KS / 8)) + (b0 ^ (unsigned)(k << 5) ^ rows_on<KS>(32 * j)) + j * KS * 64);
 #pragma unroll
     for (int sum = kMost - 1; sum >= 0; --sum)
 #pragma unroll
@@ -657,12 +724,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
   const TileRange tr = tiles_of((rows + kTileM - 1) / kTileM * nct);
   Stager<E, false, kDz, kTileM, KS, 64 * kWaves> sa;
   Stager<E, kColsB, false, kTileN, KS, 64 * kWaves> sb;
+  sa.start(lda, ldz);
+  sb.start(ldb, 0);
+  const unsigned a0 = operands_at<KS>(wm * 32 * kI), b0 = operands_at<KS>(wn * 64);
   auto load = [&](long long tile, int step) {
     const long long m0 = tile / nct * kTileM;
     const int n0 = (int)(tile % nct) * kTileN;
     const int seg = step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS;
-    sa.load(part_of(g.a, seg) + m0 * lda, kDz ? g.a.z + m0 * ldz : nullptr, lda, ldz, (int)min(rows - m0, (long long)kTileM), k0, d);
-    const long long kb = (long long)seg * d;
+    sa.load(part_of(g.a, seg) + m0 * lda + k0 * E::kBytes, kDz ? g.a.z + m0 * ldz + k0 * E::kBytes : nullptr, lda, ldz,
+            (int)min(rows - m0, (long long)kTileM), k0, d);
+    const long long kb = (long long)seg * d + k0;
     sb.load(kColsB ? g.b.p[0] + kb * ldb + n0 * E::kBytes : g.b.p[0] + (long long)n0 * ldb + kb * E::kBytes, nullptr, ldb, 0,
             min(g.N - n0, kTileN), k0, d);
   };
@@ -687,10 +758,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
       sb.mask(k0, d);
       if (Shape::kBuffers == 1 || step == 0) __syncthreads();          // the last step's reads, or the last tile's sums, are done
       sa.store(A, 1.f, 0);
-      sb.store(B, sign, sb.row(min(g.N - n0, kTileN)));
+      sb.store(B, sign, kColsB ? min(g.N - n0, kTileN) : 0);
       __syncthreads();
       if (step + 1 < steps) load(tile, step + 1);
-      multiply<kP, kP, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
+      multiply<kP, kP, KS, kTileM, kTileN, kI>(acc, A, B, a0, b0);
       if constexpr (kP > 1) {
         if ((step & 1) || step + 1 == steps) add_section<kI>(total, acc, sign);
       }
@@ -874,6 +945,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
 #pragma unroll
   for (int j = 0; j < kN; ++j) sums[j] = 0.0;
   const bool product = g.M > 0;
+  const unsigned a0 = operands_at<KS>(wm * 32 * kI), b0 = operands_at<KS>(wn * 64);
   if (product) sa.start(g.a, m0, sl.r0);
   sb.start(g.b, n0, sl.r0);
   if (steps > 0) {
@@ -888,15 +960,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
     sa.mask((int)min(left, (long long)KS));
     sb.mask((int)min(left, (long long)KS));
     if (Shape::kBuffers == 1) __syncthreads();
-    if (product) sa.store(A, 1.f, sa.place);
-    sb.store(B, sign, sb.place);
+    if (product) sa.store(A, 1.f);
+    sb.store(B, sign);
     if (want_sums) sb.add_columns(sums);
     __syncthreads();
     if (step + 1 < steps) {
       if (product) sa.load(g.a, left - KS);
       sb.load(g.b, left - KS);
     }
-    if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, A, B, wm * 32 * kI, wn * 64);
+    if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, A, B, a0, b0);
     if constexpr (kPB > 1) {
       if (step % kHold == kHold - 1 || step + 1 == steps) add_section<kI>(total, acc, sign);
     }
@@ -931,7 +1003,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kN; ++j)
-      if (sb.place + j >= 0) red[threadIdx.x / kBlocks * kTileN + sb.place + j] = sums[j];
+      if (sb.here + j >= 0) red[threadIdx.x / kBlocks * kTileN + sb.here + j] = sums[j];
     __syncthreads();
     const int n = n0 + (int)threadIdx.x;
     if (threadIdx.x < kTileN && n < g.N) {
@@ -988,9 +1060,11 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, 
 // Eight waves where they compute no more columns than four would: N is at least 129, and its last tile of 256 is more than half
 // full.
 bool eight_waves(int N) { return (N + 255) / 256 * 256 == (N + 127) / 128 * 128; }
+// For weight gradients; bf16 with a ReLU mask holds more of a step's rows than the registers of eight waves have room for.
+bool eight_weight_waves(int N, bool bf16, bool relu) { return eight_waves(N) && !(bf16 && relu); }
 // The slabs of a weight gradient: one round of workgroups (two of four waves per CU, or one of eight), at least 256 rows each.
-int slabs_of(long long rows, int K, int N, int bf16, int n_cu) {
-  const bool eight = eight_waves(N);
+int slabs_of(long long rows, int K, int N, int bf16, int act, int n_cu) {
+  const bool eight = eight_weight_waves(N, bf16, act == DC_ACT_RELU);
   const int m = eight && bf16 ? 256 : 128, n = eight ? 256 : 128;
   const int ntile = ((K + m - 1) / m) * ((N + n - 1) / n);
   long long S = (eight ? 1 : 2) * n_cu / (ntile < 1 ? 1 : ntile) / 8 * 8, by_rows = (rows + 255) / 256;
@@ -1076,7 +1150,9 @@ hipError_t weight_tiles(const WeightArgs& w, hipStream_t s) {
 }
 template <class E, class EX, bool kDz>
 hipError_t weight(const WeightArgs& w, const DenseBackArgs& a, float* db, hipStream_t s) {
-  const hipError_t e = eight_waves(w.N) ? weight_tiles<E, EX, kDz, 8>(w, s) : weight_tiles<E, EX, kDz, 4>(w, s);
+  hipError_t e;
+  if constexpr (kDz && E::kPieces == 1) e = weight_tiles<E, EX, kDz, 4>(w, s);
+  else e = eight_weight_waves(w.N, E::kPieces == 1, kDz) ? weight_tiles<E, EX, kDz, 8>(w, s) : weight_tiles<E, EX, kDz, 4>(w, s);
   if (e != hipSuccess) return e;
   const long long total = (long long)w.M * w.N + w.N, most = (long long)a.n_cu * 8, want = (total + 255) / 256;
   hipLaunchKernelGGL((weight_reduce_kernel<EX, E, kDz>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, w,
@@ -1148,7 +1224,7 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     w.b = dz;
     w.nrows = a.nrows;
     w.N = a.N;
-    w.S = slabs_of(a.rows, K, a.N, a.bf16, a.n_cu);
+    w.S = slabs_of(a.rows, K, a.N, a.bf16, a.act, a.n_cu);
     w.part = workspace;
     w.sums = db != nullptr;
     w.stop = a.stop;
@@ -1168,7 +1244,7 @@ size_t dense_dz_floats(long long rows, int N, int bf16) {
   return ((size_t)rows * N * (bf16 ? 2 : 4) + 15) / 16 * 4;
 }
 size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu) {
-  size_t n = (size_t)slabs_of(rows, K, N, bf16, n_cu) * ((size_t)K * N + N);
+  size_t n = (size_t)slabs_of(rows, K, N, bf16, act, n_cu) * ((size_t)K * N + N);
   if (smooth(act)) n += dense_dz_floats(rows, N, bf16) + (size_t)slope_blocks(rows, n_cu) * N;
   return n;
 }
