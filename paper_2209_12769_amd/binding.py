@@ -666,9 +666,12 @@ class Evaluator:
         """x [rows, cols] in 8 bits, one power of two per row and 32 columns."""
         rows, cols, ld, dtype = self._rows(x, "x")
         blocks = -(-cols // 32)
-        code = self.torch.empty((rows, 32 * blocks), dtype=self.torch.int8, device=self.device)
-        k = KeptRows(code, self.torch.empty((rows, blocks), dtype=self.torch.uint8, device=self.device), cols)
-        st = lib().dc_keep_rows(self.ctx, dtype, rows, cols, x.data_ptr(), ld, self._kept(k, rows, cols), self._raw_stream())
+        k = KeptRows.__new__(KeptRows)                   # of shapes that need no check
+        k.code = self.torch.empty((rows, 32 * blocks), dtype=self.torch.int8, device=self.device)
+        k.exponent = self.torch.empty((rows, blocks), dtype=self.torch.uint8, device=self.device)
+        k.cols = cols
+        st = lib().dc_keep_rows(self.ctx, dtype, rows, cols, x.data_ptr(), ld,
+                                _KEPT.pack(k.code.data_ptr(), k.exponent.data_ptr(), 32 * blocks, blocks), self._raw_stream())
         if st:
             self._ok(st, "dc_keep_rows")
         return k

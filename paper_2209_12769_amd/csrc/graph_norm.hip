@@ -565,23 +565,26 @@ int slab_of(int C, int cg, int es) {
   return s >= C ? C : (int)s;
 }
 int blocks_most(int n_cu) { return n_cu * 8; }
-// LDS for rows of a workgroup of 64, 256 or more threads: eight, three or one of them per CU
-int held_bytes(int threads) { return threads == 64 ? 18 * 1024 : (threads == 256 ? 48 * 1024 : 140 * 1024); }
+// LDS for rows of a workgroup of 64, 256 or more threads: twelve, three or one of them per CU
+int held_bytes(int threads) { return threads == 64 ? 12 * 1024 : (threads == 256 ? 48 * 1024 : 140 * 1024); }
 
 Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item, bool back, int n_cu) {
   Plan p{};
   const int kMost = most_threads(back);
   const int cg = C / G;
-  const long long want = rows / (n_graphs > 0 ? n_graphs : 1) * 3 / 2;       // a graph of one and a half times the mean
+  const long long mean = rows / (n_graphs > 0 ? n_graphs : 1), want = mean * 3 / 2;       // a graph of one and a half times the mean
   // whole rows and the fewest threads that hold it; else slabs
   p.slab = C;
   p.lanes = pow2_at_least((C + v - 1) / v);
   auto fits = [&](int threads, int lanes) {
     return lanes <= threads && want <= (long long)held_bytes(threads) / (threads * item) * (threads / lanes);
   };
-  p.threads = fits(64, p.lanes) ? 64 : (fits(256, p.lanes) ? 256 : kMost);
+  // a wave by itself needs no barriers, and what it does not hold it finds in L2: up to twice what it holds
+  const bool wave = p.lanes <= 64 && mean <= 2LL * (held_bytes(64) / (64 * item)) * (64 / p.lanes);
+  p.threads = wave ? 64 : (fits(256, p.lanes) ? 256 : kMost);
   const int narrow = slab_of(C, cg, es);
-  if (p.threads == kMost && !fits(p.threads, p.lanes)) {
+  // slabs also where whole rows would leave most CUs without work
+  if (p.threads == kMost && (!fits(p.threads, p.lanes) || n_graphs < n_cu / 2)) {
     p.slab = narrow;
     p.lanes = pow2_at_least((p.slab + v - 1) / v);
   }
