@@ -235,6 +235,9 @@ struct Two {
   Held<X, kV> x;
   Vec<T, kV> dy;
 };
+// LDS bytes of one row step of a thread: x, and dy for the gradient, in arrays of their own.
+template <typename T, typename X, int kV, bool kBack>
+constexpr int kItemBytes = (int)sizeof(Held<X, kV>) + (kBack ? (int)sizeof(Vec<T, kV>) : 0);
 template <typename T, typename X, int kV, bool kBack>
 __device__ __forceinline__ void fetch(Two<T, X, kV>& h, const Norm& n, long long row, int c) {
   hold<>(h.x, n, row, c);
@@ -301,7 +304,8 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
   extern __shared__ char lds[];
   double2* red = reinterpret_cast<double2*>(lds);
   const int slab = blockIdx.x % n.nslab, t = threadIdx.x;
-  Item* mine = reinterpret_cast<Item*>(lds + kThreads * sizeof(double2)) + t;
+  Held<X, kV>* held_x = reinterpret_cast<Held<X, kV>*>(lds + kThreads * sizeof(double2)) + t;
+  Vec<T, kV>* held_dy = reinterpret_cast<Vec<T, kV>*>(lds + kThreads * (sizeof(double2) + n.held * sizeof(Held<X, kV>))) + t;
   const int c0 = slab * n.slab, width = min(n.slab, n.a.C - c0);
   const int used = width / kV, lane = t & (n.lanes - 1), rl = t / n.lanes, step = kThreads / n.lanes, gv = n.cg / kV;
   const bool in = lane < used;
@@ -335,7 +339,10 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
     const long long r0 = r.lo + rl;
     const int count = in && r0 < r.hi ? (int)((r.hi - r0 + step - 1) / step) : 0;      // row steps of this thread
     each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Item& h, int i) {
-      if (i < n.held) mine[i * kThreads] = h;
+      if (i < n.held) {
+        held_x[i * kThreads] = h.x;
+        if constexpr (kBack) held_dy[i * kThreads] = h.dy;
+      }
       float x[kV], dy[kV];
       open<T, X, kV, kBack>(x, dy, h);
       add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
@@ -362,7 +369,13 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       finish<T, kV, kBack>(n, x, dy, r0 + (long long)i * step, c, mu, rs, s1f, s2f, f);
     };
     const int here = min(count, n.held);
-    for (int i = 0; i < here; ++i) second(mine[i * kThreads], i);
+#pragma unroll 2
+    for (int i = 0; i < here; ++i) {
+      Item h;
+      h.x = held_x[i * kThreads];
+      if constexpr (kBack) h.dy = held_dy[i * kThreads];
+      second(h, i);
+    }
     each_row<T, X, kV, kBack>(n, r0, step, here, count, c, second);
   }
   if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
@@ -564,7 +577,8 @@ int slab_of(int C, int cg, int es) {
   const long long s = (long long)((128 / es + cg - 1) / cg) * cg;
   return s >= C ? C : (int)s;
 }
-int blocks_most(int n_cu) { return n_cu * 8; }
+// Workgroups of a launch: two rounds of the single waves, more of the larger ones, so that long and short graphs even out.
+int blocks_most(int threads, int n_cu) { return n_cu * (threads == 64 ? 24 : 8); }
 // LDS for rows of a workgroup of 64, 256 or more threads: twelve, three or one of them per CU
 int held_bytes(int threads) { return threads == 64 ? 12 * 1024 : (threads == 256 ? 48 * 1024 : 140 * 1024); }
 
@@ -599,18 +613,19 @@ Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item
   const long long share = 2 * rows * p.nslab / n_cu;
   p.long_rows = share < 1024 ? 1024 : (share > 4096 ? 4096 : share);
   p.chunks = rows > p.long_rows;
-  auto blocks = [&](long long items, int nslab) {
-    const long long most = blocks_most(n_cu) / nslab > 0 ? blocks_most(n_cu) / nslab : 1;
+  auto blocks = [&](long long items, int threads, int nslab) {
+    const int m = blocks_most(threads, n_cu);
+    const long long most = m / nslab > 0 ? m / nslab : 1;
     return (int)(items < 1 ? 1 : (items < most ? items : most));
   };
-  p.blocks = blocks(n_graphs, p.nslab);
-  p.chunk_blocks = p.chunks ? blocks((rows + chunk_rows(rows, n_cu) - 1) / chunk_rows(rows, n_cu), p.chunk_nslab) : 0;
+  p.blocks = blocks(n_graphs, p.threads, p.nslab);
+  p.chunk_blocks = p.chunks ? blocks((rows + chunk_rows(rows, n_cu) - 1) / chunk_rows(rows, n_cu), kChunkThreads, p.chunk_nslab) : 0;
   return p;
 }
 
 template <typename T, typename X, int kV, int kThreads, bool kBack>
 hipError_t run_short(const Norm& n, int blocks, hipStream_t s) {
-  const size_t bytes = kThreads * sizeof(double2) + (size_t)n.held * kThreads * sizeof(Two<T, X, kV>);
+  const size_t bytes = kThreads * sizeof(double2) + (size_t)n.held * kThreads * kItemBytes<T, X, kV, kBack>;
   auto kernel = graph_norm_kernel<T, X, kV, kThreads, kBack>;
   if (bytes > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
@@ -622,7 +637,7 @@ hipError_t run_short(const Norm& n, int blocks, hipStream_t s) {
 
 template <typename T, typename X, int kV, bool kBack>
 hipError_t run(Norm n, hipStream_t s) {
-  const Plan p = plan_of(n.a.rows, n.a.n_graphs, n.a.C, n.a.G, (int)sizeof(T), kV, (int)sizeof(Two<T, X, kV>), kBack, n.a.n_cu);
+  const Plan p = plan_of(n.a.rows, n.a.n_graphs, n.a.C, n.a.G, (int)sizeof(T), kV, kItemBytes<T, X, kV, kBack>, kBack, n.a.n_cu);
   n.slab = p.slab;
   n.nslab = p.nslab;
   n.lanes = p.lanes;
@@ -698,7 +713,7 @@ void launch_column_sums(const float* part, int blocks, int n1, float* out1, int 
 
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
   // what any vector width and type would need, and any smaller number of rows: chunks of fewer than 512 rows are at most four per CU
-  const long long most = blocks_most(n_cu), by_rows = rows / 512 + 1, nc = by_rows > 4LL * n_cu ? by_rows : 4LL * n_cu + 1;
+  const long long most = blocks_most(64, n_cu), by_rows = rows / 512 + 1, nc = by_rows > 4LL * n_cu ? by_rows : 4LL * n_cu + 1;
   const bool chunks = rows > 1024;
   const size_t longs = chunks ? (size_t)(rows / 1024) + 1 : 0;
   size_t b = chunks ? 16 + (longs * sizeof(int2) + 15) / 16 * 16 + ((size_t)nc + longs) * G * sizeof(double2) : 0;
