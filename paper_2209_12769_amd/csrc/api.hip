@@ -1525,6 +1525,10 @@ dc_status graph_norm_check(dc_ctx* ctx, const dc_graph_norm_args* a, bool backwa
   if (st == DC_OK && backward) st = array_check(ctx, a->dX, a->lddx, a->rows, a->channels, es, "dX");
   if (st == DC_OK && backward && a->dres) st = array_check(ctx, a->dres, a->lddres, a->rows, a->channels, es, "dres");
   if (st != DC_OK) return st;
+  const int64_t apart = 1 << 17;                // the kernels' offsets inside a graph are 32 bits
+  if ((!(backward && a->kept) && a->ldx > apart) || (backward && a->kept && (a->kept->ld_code > apart || a->kept->ld_exponent > apart)) ||
+      (!backward && a->ldy > apart) || (backward && (a->lddy > apart || a->lddx > apart || (a->dres && a->lddres > apart))))
+    return fail(ctx, DC_ERR_UNSUPPORTED, "graph norm: rows at most 2^17 elements apart");
   if (backward && !a->dgamma != !a->dbeta) return fail(ctx, DC_ERR_INVALID_ARG, "dgamma and dbeta go together");
   const size_t need = graph_norm_bytes(a->rows, a->n_graphs, a->channels, a->groups, backward, ctx->n_cu);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_graph_norm_bytes");

@@ -12,6 +12,8 @@
 // Graphs of more than long_rows rows would keep one workgroup busy while the others are done: the kernel of the short graphs
 // only lists them, and their rows are dealt in chunks, counted from each graph's first row, to three kernels (sums of a chunk;
 // sums of a graph; second pass).  The list's order is that of the workgroups' arrival; no sum depends on it.
+#include <type_traits>
+
 #include "operators.h"
 
 namespace dc {
@@ -58,14 +60,38 @@ struct Norm {
   int col_block0;          // first column block of this launch
 };
 
+// Where the rows of a graph (or of a chunk) begin, at the thread's columns: places that all lanes share, plus the columns; a row
+// is a product of 24 bits away (rows of a graph: 4096 at most, 2^17 elements apart at most).
+struct Places {
+  const char *x, *dy, *res;
+  const unsigned char* e;
+  char* out;
+  unsigned ldx, lddy, ldres, lde, ldo;       // bytes from row to row
+};
+template <typename T, typename X, bool kBack>
+__device__ __forceinline__ Places places_of(const GraphNormArgs& a, long long row) {
+  Places p{};
+  constexpr bool kept = !std::is_same<T, X>::value;
+  p.ldx = kept ? (unsigned)a.kept.ld_code : (unsigned)(a.ldx * sizeof(T));
+  p.x = (kept ? reinterpret_cast<const char*>(a.kept.code) : static_cast<const char*>(a.X)) + row * p.ldx;
+  p.lde = (unsigned)a.kept.ld_exponent;
+  p.e = kept ? a.kept.exponent + row * p.lde : nullptr;
+  p.lddy = (unsigned)(a.lddy * sizeof(T));
+  p.dy = kBack ? static_cast<const char*>(a.dY) + row * p.lddy : nullptr;
+  p.ldres = (unsigned)(a.lddres * sizeof(T));
+  p.res = kBack && a.dRes ? static_cast<const char*>(a.dRes) + row * p.ldres : nullptr;
+  p.ldo = (unsigned)((kBack ? a.lddx : a.ldy) * sizeof(T));
+  p.out = static_cast<char*>(kBack ? a.dX : a.Y) + row * p.ldo;
+  return p;
+}
 template <typename T, int kV>
-__device__ __forceinline__ void hold(Held<T, kV>& h, const Norm& n, long long row, int c) {
-  h.v = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.X) + row * n.a.ldx + c);
+__device__ __forceinline__ void hold(Held<T, kV>& h, const Places& p, unsigned row, int c) {
+  h.v = *reinterpret_cast<const Vec<T, kV>*>(p.x + (__umul24(row, p.ldx) + (unsigned)(c * (int)sizeof(T))));
 }
 template <int kV>
-__device__ __forceinline__ void hold(Held<Kept8, kV>& h, const Norm& n, long long row, int c) {
-  h.v = *reinterpret_cast<const Vec<signed char, kV>*>(n.a.kept.code + row * n.a.kept.ld_code + c);
-  h.e = n.a.kept.exponent[row * n.a.kept.ld_exponent + c / kKeptBlock];
+__device__ __forceinline__ void hold(Held<Kept8, kV>& h, const Places& p, unsigned row, int c) {
+  h.v = *reinterpret_cast<const Vec<signed char, kV>*>(p.x + (__umul24(row, p.ldx) + (unsigned)c));
+  h.e = p.e[__umul24(row, p.lde) + (unsigned)(c / kKeptBlock)];
 }
 template <typename T, int kV>
 __device__ __forceinline__ void values(float (&x)[kV], const Held<T, kV>& h) {
@@ -141,14 +167,17 @@ __device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x
 #pragma unroll
     for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
     slope<kV, kShort>(dy, xh, f, act);
+    float v1 = 0.f, v2 = 0.f;                          // a vector's, before they go to the 64-bit sums
 #pragma unroll
     for (int k = 0; k < kV; ++k) {
       const float u = f.gamma[k] * dy[k];
-      s1 += (double)u;
-      s2 = fma((double)u, (double)xh[k], s2);
+      v1 += u;
+      v2 = fmaf(u, xh[k], v2);
       dg[k] = fmaf(dy[k], xh[k], dg[k]);
       db[k] += dy[k];
     }
+    s1 += (double)v1;
+    s2 += (double)v2;
   }
 }
 
@@ -203,8 +232,8 @@ __device__ __forceinline__ void statistics(double s1, double s2, double m, float
 
 // The second pass of one vector.
 template <typename T, int kV, bool kBack>
-__device__ __forceinline__ void finish(const Norm& n, const float (&x)[kV], float (&dy)[kV], long long row, int c, float mu, float r,
-                                       float s1, float s2, const Affine<kV>& f) {
+__device__ __forceinline__ void finish(int act, const Places& p, const float (&x)[kV], float (&dy)[kV], unsigned row, int c, float mu, float r, float s1,
+                                       float s2, const Affine<kV>& f) {
   Vec<T, kV> o;
   float xh[kV];
 #pragma unroll
@@ -212,22 +241,21 @@ __device__ __forceinline__ void finish(const Norm& n, const float (&x)[kV], floa
   if constexpr (!kBack) {
 #pragma unroll
     for (int k = 0; k < kV; ++k) xh[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
-    activate<kV, sizeof(T) == 2>(xh, n.a.act);
+    activate<kV, sizeof(T) == 2>(xh, act);
 #pragma unroll
     for (int k = 0; k < kV; ++k) narrow(xh[k], o.v[k]);
-    *reinterpret_cast<Vec<T, kV>*>(static_cast<T*>(n.a.Y) + row * n.a.ldy + c) = o;
   } else {
-    slope<kV, sizeof(T) == 2>(dy, xh, f, n.a.act);
+    slope<kV, sizeof(T) == 2>(dy, xh, f, act);
     Vec<T, kV> add{};
-    if (n.a.dRes) add = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.dRes) + row * n.a.lddres + c);
+    if (p.res) add = *reinterpret_cast<const Vec<T, kV>*>(p.res + (__umul24(row, p.ldres) + (unsigned)(c * (int)sizeof(T))));
 #pragma unroll
     for (int k = 0; k < kV; ++k) {
       float d = r * (f.gamma[k] * dy[k] - s1 - xh[k] * s2);
-      if (n.a.dRes) d += widen(add.v[k]);
+      if (p.res) d += widen(add.v[k]);
       narrow(d, o.v[k]);
     }
-    *reinterpret_cast<Vec<T, kV>*>(static_cast<T*>(n.a.dX) + row * n.a.lddx + c) = o;
   }
+  *reinterpret_cast<Vec<T, kV>*>(p.out + (__umul24(row, p.ldo) + (unsigned)(c * (int)sizeof(T)))) = o;
 }
 
 template <typename T, typename X, int kV>
@@ -239,9 +267,9 @@ struct Two {
 template <typename T, typename X, int kV, bool kBack>
 constexpr int kItemBytes = (int)sizeof(Held<X, kV>) + (kBack ? (int)sizeof(Vec<T, kV>) : 0);
 template <typename T, typename X, int kV, bool kBack>
-__device__ __forceinline__ void fetch(Two<T, X, kV>& h, const Norm& n, long long row, int c) {
-  hold<>(h.x, n, row, c);
-  if constexpr (kBack) h.dy = *reinterpret_cast<const Vec<T, kV>*>(static_cast<const T*>(n.a.dY) + row * n.a.lddy + c);
+__device__ __forceinline__ void fetch(Two<T, X, kV>& h, const Places& p, unsigned row, int c) {
+  hold<>(h.x, p, row, c);
+  if constexpr (kBack) h.dy = *reinterpret_cast<const Vec<T, kV>*>(p.dy + (__umul24(row, p.lddy) + (unsigned)(c * (int)sizeof(T))));
 }
 template <typename T, typename X, int kV, bool kBack>
 __device__ __forceinline__ void open(float (&x)[kV], float (&dy)[kV], const Two<T, X, kV>& h) {
@@ -285,11 +313,11 @@ __device__ __forceinline__ void column_sums(const Norm& n, double (&dg)[kV], dou
 // end the last row again (a request in a branch would make every wait wait for everything).
 constexpr int kStep = 4;
 template <typename T, typename X, int kV, bool kBack, typename F>
-__device__ __forceinline__ void each_row(const Norm& n, long long first, int step, int from, int count, int c, F f) {
+__device__ __forceinline__ void each_row(const Places& p, int first, int step, int from, int count, int c, F f) {
   for (int i = from; i < count; i += kStep) {
     Two<T, X, kV> h[kStep];
 #pragma unroll
-    for (int u = 0; u < kStep; ++u) fetch<T, X, kV, kBack>(h[u], n, first + (long long)min(i + u, count - 1) * step, c);
+    for (int u = 0; u < kStep; ++u) fetch<T, X, kV, kBack>(h[u], p, (unsigned)(first + (int)__umul24(min(i + u, count - 1), step)), c);
 #pragma unroll
     for (int u = 0; u < kStep; ++u)
       if (i + u < count) f(h[u], i + u);
@@ -336,9 +364,9 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
     float dg[kV], db[kV];
 #pragma unroll
     for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
-    const long long r0 = r.lo + rl;
-    const int count = in && r0 < r.hi ? (int)((r.hi - r0 + step - 1) / step) : 0;      // row steps of this thread
-    each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Item& h, int i) {
+    const Places at = places_of<T, X, kBack>(n.a, r.lo);
+    const int rows = (int)(r.hi - r.lo), count = in && rl < rows ? (rows - rl + step - 1) / step : 0;      // row steps of this thread
+    each_row<T, X, kV, kBack>(at, rl, step, 0, count, c, [&](const Item& h, int i) {
       if (i < n.held) {
         held_x[i * kThreads] = h.x;
         if constexpr (kBack) held_dy[i * kThreads] = h.dy;
@@ -366,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
     auto second = [&](const Item& h, int i) {
       float x[kV], dy[kV];
       open<T, X, kV, kBack>(x, dy, h);
-      finish<T, kV, kBack>(n, x, dy, r0 + (long long)i * step, c, mu, rs, s1f, s2f, f);
+      finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s1f, s2f, f);
     };
     const int here = min(count, n.held);
 #pragma unroll 2
@@ -376,7 +404,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       if constexpr (kBack) h.dy = held_dy[i * kThreads];
       second(h, i);
     }
-    each_row<T, X, kV, kBack>(n, r0, step, here, count, c, second);
+    each_row<T, X, kV, kBack>(at, rl, step, here, count, c, second);
   }
   if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
 }
@@ -444,9 +472,9 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
       float dg[kV], db[kV];
 #pragma unroll
       for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
-      const long long r0 = seg.lo + rl;
-      const int count = in && r0 < seg.hi ? (int)((seg.hi - r0 + step - 1) / step) : 0;
-      each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
+      const Places at = places_of<T, X, kBack>(n.a, seg.lo);
+      const int rows = (int)(seg.hi - seg.lo), count = in && rl < rows ? (rows - rl + step - 1) / step : 0;
+      each_row<T, X, kV, kBack>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
         add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
@@ -515,12 +543,12 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
       if (seg.lo >= seg.hi) continue;
       const float mu = n.a.mean[(size_t)seg.g * n.a.G + group], rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
       const float2 s = kBack ? n.means[(size_t)seg.entry * n.a.G + group] : make_float2(0.f, 0.f);
-      const long long r0 = seg.lo + rl;
-      const int count = r0 < seg.hi ? (int)((seg.hi - r0 + step - 1) / step) : 0;
-      each_row<T, X, kV, kBack>(n, r0, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
+      const Places at = places_of<T, X, kBack>(n.a, seg.lo);
+      const int rows = (int)(seg.hi - seg.lo), count = rl < rows ? (rows - rl + step - 1) / step : 0;
+      each_row<T, X, kV, kBack>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
-        finish<T, kV, kBack>(n, x, dy, r0 + (long long)i * step, c, mu, rs, s.x, s.y, f);
+        finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s.x, s.y, f);
       });
     }
 }
