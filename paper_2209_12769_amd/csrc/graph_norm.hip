@@ -311,8 +311,7 @@ __device__ __forceinline__ void column_sums(const Norm& n, double (&dg)[kV], dou
 
 // A thread's rows first, first + step, .. (count of them) in groups of kStep: the requests of a group are made together, past the
 // end the last row again (a request in a branch would make every wait wait for everything).
-constexpr int kStep = 4;
-template <typename T, typename X, int kV, bool kBack, typename F>
+template <typename T, typename X, int kV, bool kBack, int kStep, typename F>
 __device__ __forceinline__ void each_row(const Places& p, int first, int step, int from, int count, int c, F f) {
   for (int i = from; i < count; i += kStep) {
     Two<T, X, kV> h[kStep];
@@ -366,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
     for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
     const Places at = places_of<T, X, kBack>(n.a, r.lo);
     const int rows = (int)(r.hi - r.lo), count = in && rl < rows ? (rows - rl + step - 1) / step : 0;      // row steps of this thread
-    each_row<T, X, kV, kBack>(at, rl, step, 0, count, c, [&](const Item& h, int i) {
+    each_row<T, X, kV, kBack, kThreads == 64 ? 8 : 4>(at, rl, step, 0, count, c, [&](const Item& h, int i) {
       if (i < n.held) {
         held_x[i * kThreads] = h.x;
         if constexpr (kBack) held_dy[i * kThreads] = h.dy;
@@ -404,7 +403,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       if constexpr (kBack) h.dy = held_dy[i * kThreads];
       second(h, i);
     }
-    each_row<T, X, kV, kBack>(at, rl, step, here, count, c, second);
+    each_row<T, X, kV, kBack, 4>(at, rl, step, here, count, c, second);
   }
   if (kBack && n.a.dgamma) column_sums<kV>(n, dgs, dbs, n.lanes, used, c, n.col_block0 + blockIdx.x / n.nslab, red);
 }
@@ -474,7 +473,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
       for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
       const Places at = places_of<T, X, kBack>(n.a, seg.lo);
       const int rows = (int)(seg.hi - seg.lo), count = in && rl < rows ? (rows - rl + step - 1) / step : 0;
-      each_row<T, X, kV, kBack>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
+      each_row<T, X, kV, kBack, 4>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
         add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
@@ -545,7 +544,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
       const float2 s = kBack ? n.means[(size_t)seg.entry * n.a.G + group] : make_float2(0.f, 0.f);
       const Places at = places_of<T, X, kBack>(n.a, seg.lo);
       const int rows = (int)(seg.hi - seg.lo), count = rl < rows ? (rows - rl + step - 1) / step : 0;
-      each_row<T, X, kV, kBack>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
+      each_row<T, X, kV, kBack, 4>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
         finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s.x, s.y, f);
