@@ -525,7 +525,6 @@ struct ProductArgs {
   long long ldz;
   char* Y;
   long long ldy;
-  int vec;               // rows of R, Z and Y start on 16 bytes
   const int* stop;
 };
 
@@ -549,11 +548,11 @@ __device__ __forceinline__ void store_wide(char* p, long long i, const float (&x
     if constexpr (E::kBytes == 4) w[k] = __float_as_uint(x[k]);
     else w[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
   }
-  *reinterpret_cast<u32x4*>(p + i * E::kBytes) = w;
+  *reinterpret_cast<u32x4_any*>(p + i * E::kBytes) = w;
 }
 
 // What becomes of 16 / kBytes neighbouring sums z of a row.
-// r: the residual's 16 bytes, where rows are read whole (g.vec, the columns inside).
+// r: the residual's 16 bytes, where all of them are columns.
 template <class E, bool kDz, bool kColsB>
 __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int col, float (&z)[16 / E::kBytes], const unsigned (&r)[4]) {
   constexpr int kW = 16 / E::kBytes;
@@ -570,7 +569,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
       for (int k = 0; k < kW; ++k) z[k] = k == c ? s : z[k];
     }
   }
-  if (g.vec && col + kW <= g.N) {
+  if (col + kW <= g.N) {
     if (g.bias)
 #pragma unroll
       for (int k = 0; k < kW; ++k) z[k] += g.bias[col + k];
@@ -684,7 +683,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
     if (r < 32 && m0 + r < rows && n0 + c0 < g.N) {
       float z[kW];
       unsigned res[4] = {0, 0, 0, 0};
-      if (g.R && g.vec && n0 + c0 + kW <= g.N) read_words<16>(res, g.R + ((m0 + r) * g.ldr + n0 + c0) * E::kBytes);
+      if (g.R && n0 + c0 + kW <= g.N) read_words<16>(res, g.R + ((m0 + r) * g.ldr + n0 + c0) * E::kBytes);
 #pragma unroll
       for (int k = 0; k < kW; ++k) {
         const float* p = lds + r * kFewLd + c0 + k;
@@ -772,7 +771,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
     float* end = reinterpret_cast<float*>(lds) + wave * 32 * kLd;
     constexpr int kLanes = 64 / kW, kRounds = 32 / kW;
     const int c0 = lane % kLanes * kW, col = n0 + wn * 64 + c0;
-    const bool wide = g.vec && col + kW <= g.N;
+    const bool wide = col + kW <= g.N;
     for (int part = 0; part < kI; ++part) {
       const long long r0 = m0 + wm * 32 * kI + part * 32 + lane / kLanes;
       unsigned res[kRounds][4];
@@ -1110,7 +1109,6 @@ hipError_t product(const ProductArgs& g, long long rows, int n_cu, hipStream_t s
 template <class E>
 hipError_t dense(const DenseArgs& a, hipStream_t s) {
   ProductArgs g{};
-  constexpr int kWide = 16 / E::kBytes;
   const int K = a.nseg * a.d;
   for (int i = 0; i < a.nseg; ++i) g.a.p[i] = static_cast<const char*>(a.X[i]);
   g.a.ld = a.ldx;
@@ -1132,8 +1130,6 @@ hipError_t dense(const DenseArgs& a, hipStream_t s) {
   g.ldz = a.ldz;
   g.Y = static_cast<char*>(a.Y);
   g.ldy = a.ldy;
-  auto starts = [](const void* p, long long ld) { return !p || (ld % kWide == 0 && reinterpret_cast<size_t>(p) % 16 == 0); };
-  g.vec = starts(a.R, a.ldr) && starts(a.Z, a.ldz) && starts(a.Y, a.ldy);
   g.stop = a.stop;
   return product<E, false, true>(g, a.rows, a.n_cu, s);
 }
@@ -1202,7 +1198,6 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     g.act = DC_ACT_NONE;
     g.Y = static_cast<char*>(a.dX);
     g.ldy = a.lddx;
-    g.vec = a.lddx % kWide == 0 && reinterpret_cast<size_t>(a.dX) % 16 == 0;
     g.stop = a.stop;
     e = product<E, kDz, false>(g, a.rows, a.n_cu, s);
   }
