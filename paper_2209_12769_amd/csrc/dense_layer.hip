@@ -460,12 +460,12 @@ __device__ __forceinline__ unsigned operands_at(int row0) {
 }
 // One staged step: acc[i][j] += A (rows a0 + 32 i ..) times B (rows b0 + 32 j ..), from where operands_at() says for a0 and
 // b0.  The small products first.
-template <int kPA, int kPB, int KS, int kRA, int kRB, int kI>
+template <int kPA, int kPB, int KS, int kRA, int kRB, int kI, int kFrom = 0, int kTo = KS / 16>      // part of the step, in 16 indices
 __device__ __forceinline__ void multiply(f32x16 (&acc)[kI][2], const u32x4* A, const u32x4* B, unsigned a0, unsigned b0) {
   constexpr int kMost = kPA > kPB ? kPA : kPB;
   asm volatile("" : "+v"(a0), "+v"(b0));               // the addresses that follow are formed here, not kept from step to step
 #pragma unroll
-  for (int k = 0; k < KS / 16; ++k) {
+  for (int k = kFrom; k < kTo; ++k) {
     u32x4 a[kPA][kI], b[kPB][2];
 #pragma unroll
     for (int p = 0; p < kPA; ++p)
@@ -574,7 +574,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
 #pragma unroll
       for (int k = 0; k < kW; ++k) z[k] += g.bias[col + k];
     if (g.Z) store_wide<E>(g.Z, row * g.ldz + col, z);
-    activate<kW, E::kBytes == 2>(z, g.act);
+    activate<kW>(z, g.act);
     if (g.R)
 #pragma unroll
       for (int k = 0; k < kW; ++k) z[k] += value_of<E>(r, k, 1.f);
@@ -588,7 +588,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
 #pragma unroll
     for (int k = 0; k < kW; ++k)
       if (col + k < g.N) store_value<E>(g.Z, row * g.ldz + col + k, z[k]);
-  activate<kW, E::kBytes == 2>(z, g.act);
+  activate<kW>(z, g.act);
 #pragma unroll
   for (int k = 0; k < kW; ++k)
     if (col + k < g.N) {
@@ -747,25 +747,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
         acc[i][j] = zero16();
         if (kP > 1) total[i][j] = zero16();
       }
-    load(tile, 0);
-    for (int step = 0; step < steps; ++step) {
-      const float sign = (step >> 1) & 1 ? -1.f : 1.f;
+    auto sign_of = [](int step) { return (step >> 1) & 1 ? -1.f : 1.f; };
+    auto stash = [&](int step, u32x4* A) {
       const int k0 = step % per * KS;
-      u32x4* A = lds + (Shape::kBuffers > 1 ? (step & 1) * Shape::kStep : 0);
-      u32x4* B = A + Shape::kUnitsA;
       sa.mask(k0, d);
       sb.mask(k0, d);
-      if (Shape::kBuffers == 1 || step == 0) __syncthreads();          // the last step's reads, or the last tile's sums, are done
       sa.store(A, 1.f, 0);
-      sb.store(B, sign, kColsB ? min(g.N - n0, kTileN) : 0);
-      __syncthreads();
-      if (step + 1 < steps) load(tile, step + 1);
-      multiply<kP, kP, KS, kTileM, kTileN, kI>(acc, A, B, a0, b0);
+      sb.store(A + Shape::kUnitsA, sign_of(step), kColsB ? min(g.N - n0, kTileN) : 0);
+    };
+    auto section = [&](int step) {
       if constexpr (kP > 1) {
-        if ((step & 1) || step + 1 == steps) add_section<kI>(total, acc, sign);
+        if ((step & 1) || step + 1 == steps) add_section<kI>(total, acc, sign_of(step));
       }
+    };
+    load(tile, 0);
+    __syncthreads();                                   // the last tile's sums have been read
+    if constexpr (Shape::kBuffers > 1) {
+      // the next step's rows go to the other half of LDS between the two halves of a step's products, so that one wave's
+      // conversions run beside another's products; then the step after is requested
+      stash(0, lds);
+      if (steps > 1) load(tile, 1);
+      __syncthreads();
+      for (int step = 0; step < steps; ++step) {
+        const u32x4* A = lds + (step & 1) * Shape::kStep;
+        const u32x4* B = A + Shape::kUnitsA;
+        multiply<kP, kP, KS, kTileM, kTileN, kI, 0, KS / 32>(acc, A, B, a0, b0);
+        if (step + 1 < steps) stash(step + 1, lds + ((step + 1) & 1) * Shape::kStep);
+        if (step + 2 < steps) load(tile, step + 2);
+        multiply<kP, kP, KS, kTileM, kTileN, kI, KS / 32, KS / 16>(acc, A, B, a0, b0);
+        section(step);
+        __syncthreads();
+      }
+    } else {
+      for (int step = 0; step < steps; ++step) {
+        if (step > 0) __syncthreads();                 // the last step's operands have been read
+        stash(step, lds);
+        __syncthreads();
+        if (step + 1 < steps) load(tile, step + 1);
+        multiply<kP, kP, KS, kTileM, kTileN, kI>(acc, lds, lds + Shape::kUnitsA, a0, b0);
+        section(step);
+      }
+      __syncthreads();
     }
-    __syncthreads();
     // register v of a lane: row l32, column 8 (v / 4) + 4 lh + v % 4 of a block; through LDS, 32 rows of a wave at a time, so
     // that a wave reads and writes whole rows of its 64 columns
     float* end = reinterpret_cast<float*>(lds) + wave * 32 * kLd;
@@ -852,7 +875,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g) {
         const long long row = r + (long long)u * g.row_blocks * 8;
 #pragma unroll
         for (int k = 0; k < kV; ++k) d[u][k] = value_of<E>(z[u], k, 1.f);
-        slopes<kV, E::kBytes == 2>(d[u], g.act);
+        slopes<kV>(d[u], g.act);
 #pragma unroll
         for (int k = 0; k < kV; ++k) d[u][k] = row < rows ? d[u][k] * value_of<E>(y[u], k, 1.f) : 0.f;
         if (row < rows) {
@@ -947,29 +970,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
   const unsigned a0 = operands_at<KS>(wm * 32 * kI), b0 = operands_at<KS>(wn * 64);
   if (product) sa.start(g.a, m0, sl.r0);
   sb.start(g.b, n0, sl.r0);
-  if (steps > 0) {
-    if (product) sa.load(g.a, sl.r1 - sl.r0);
-    sb.load(g.b, sl.r1 - sl.r0);
-  }
-  for (int step = 0; step < steps; ++step) {
-    const float sign = ((step / kHold) ^ slab) & 1 ? -1.f : 1.f;
-    const long long left = sl.r1 - sl.r0 - (long long)step * KS;
-    u32x4* A = lds + (Shape::kBuffers > 1 ? (step & 1) * Shape::kStep : 0);
-    u32x4* B = A + Shape::kUnitsA;
-    sa.mask((int)min(left, (long long)KS));
-    sb.mask((int)min(left, (long long)KS));
-    if (Shape::kBuffers == 1) __syncthreads();
+  const long long all = sl.r1 - sl.r0;
+  auto load = [&](int step) {
+    if (product) sa.load(g.a, all - (long long)step * KS);
+    sb.load(g.b, all - (long long)step * KS);
+  };
+  auto sign_of = [&](int step) { return ((step / kHold) ^ slab) & 1 ? -1.f : 1.f; };
+  auto stash = [&](int step, u32x4* A) {
+    const int left = (int)min(all - (long long)step * KS, (long long)KS);
+    sa.mask(left);
+    sb.mask(left);
     if (product) sa.store(A, 1.f);
-    sb.store(B, sign);
+    sb.store(A + Shape::kUnitsA, sign_of(step));
     if (want_sums) sb.add_columns(sums);
-    __syncthreads();
-    if (step + 1 < steps) {
-      if (product) sa.load(g.a, left - KS);
-      sb.load(g.b, left - KS);
-    }
-    if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, A, B, a0, b0);
+  };
+  auto section = [&](int step) {
     if constexpr (kPB > 1) {
-      if (step % kHold == kHold - 1 || step + 1 == steps) add_section<kI>(total, acc, sign);
+      if (step % kHold == kHold - 1 || step + 1 == steps) add_section<kI>(total, acc, sign_of(step));
+    }
+  };
+  if (steps > 0) load(0);
+  if constexpr (Shape::kBuffers > 1) {                 // as in product_kernel
+    if (steps > 0) stash(0, lds);
+    if (steps > 1) load(1);
+    __syncthreads();
+    for (int step = 0; step < steps; ++step) {
+      const u32x4* A = lds + (step & 1) * Shape::kStep;
+      const u32x4* B = A + Shape::kUnitsA;
+      if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI, 0, KS / 32>(acc, A, B, a0, b0);
+      if (step + 1 < steps) stash(step + 1, lds + ((step + 1) & 1) * Shape::kStep);
+      if (step + 2 < steps) load(step + 2);
+      if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI, KS / 32, KS / 16>(acc, A, B, a0, b0);
+      section(step);
+      __syncthreads();
+    }
+  } else {
+    for (int step = 0; step < steps; ++step) {
+      if (step > 0) __syncthreads();
+      stash(step, lds);
+      __syncthreads();
+      if (step + 1 < steps) load(step + 1);
+      if (product) multiply<kPA, kPB, KS, kTileM, kTileN, kI>(acc, lds, lds + Shape::kUnitsA, a0, b0);
+      section(step);
     }
   }
   float* P = g.part + (size_t)slab * ((size_t)g.M * g.N + g.N);

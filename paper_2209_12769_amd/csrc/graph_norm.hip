@@ -141,18 +141,18 @@ __device__ __forceinline__ Affine<kV> affine_at(const GraphNormArgs& a, int c) {
 }
 
 // dy becomes dz.
-template <int kV, bool kShort>
+template <int kV>
 __device__ __forceinline__ void slope(float (&dy)[kV], const float (&xh)[kV], const Affine<kV>& f, int act) {
   float z[kV];
 #pragma unroll
   for (int k = 0; k < kV; ++k) z[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
-  slopes<kV, kShort>(z, act);
+  slopes<kV>(z, act);
 #pragma unroll
   for (int k = 0; k < kV; ++k) dy[k] *= z[k];
 }
 
 // What a row's vector adds to the two sums.
-template <bool kBack, int kV, bool kShort>
+template <bool kBack, int kV>
 __device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x)[kV], float (&dy)[kV], float mu, float r,
                                          const Affine<kV>& f, int act, float (&dg)[kV], float (&db)[kV]) {
   if constexpr (!kBack) {
@@ -166,7 +166,7 @@ __device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x
     float xh[kV];
 #pragma unroll
     for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
-    slope<kV, kShort>(dy, xh, f, act);
+    slope<kV>(dy, xh, f, act);
     float v1 = 0.f, v2 = 0.f;                          // a vector's, before they go to the 64-bit sums
 #pragma unroll
     for (int k = 0; k < kV; ++k) {
@@ -241,11 +241,11 @@ __device__ __forceinline__ void finish(int act, const Places& p, const float (&x
   if constexpr (!kBack) {
 #pragma unroll
     for (int k = 0; k < kV; ++k) xh[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
-    activate<kV, sizeof(T) == 2>(xh, act);
+    activate<kV>(xh, act);
 #pragma unroll
     for (int k = 0; k < kV; ++k) narrow(xh[k], o.v[k]);
   } else {
-    slope<kV, sizeof(T) == 2>(dy, xh, f, act);
+    slope<kV>(dy, xh, f, act);
     Vec<T, kV> add{};
     if (p.res) add = *reinterpret_cast<const Vec<T, kV>*>(p.res + (__umul24(row, p.ldres) + (unsigned)(c * (int)sizeof(T))));
 #pragma unroll
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       }
       float x[kV], dy[kV];
       open<T, X, kV, kBack>(x, dy, h);
-      add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+      add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
     });
     group_sums(s1, s2, red, n.lanes, used, gv);
     if constexpr (!kBack) {
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
       each_row<T, X, kV, kBack, 4>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
-        add_sums<kBack, kV, sizeof(T) == 2>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+        add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
       });
       group_sums(s1, s2, red, n.lanes, used, gv);
       if (in && rl == 0 && lane % gv == 0) n.part[(size_t)chunk * n.a.G + group] = make_double2(s1, s2);

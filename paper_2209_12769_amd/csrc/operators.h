@@ -11,42 +11,42 @@ namespace dc {
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
-// erfc(|x|) e^(x^2) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))), t = 1 / (1 + p |x|): Abramowitz and Stegun, Handbook of
-// Mathematical Functions, 7.1.26; erf is off by at most 1.5e-7, absolutely.
+// The standard normal distribution at -|z| is e^(-z^2 / 2) times a smooth function of |z|, here a polynomial of degree 8 in
+// t = 1 / (1 + p |z|) without a constant, fitted for the smallest largest relative error over 0 <= |z| <= 14 (1.3e-7).  GELU
+// by it is off by at most 4.9 roundings of |z|, and 0.5 z (1 + erf) in fp32 by up to 5.8, at about twice the
+// instructions: those of the library's error function bound the norms with GELU and took 45 us of 0.33 ms for a layer of
+// 27 M outputs.
 struct NormalParts {
   float cdf, density;    // of the standard normal distribution at z
 };
 __device__ __forceinline__ NormalParts normal_parts(float z) {
-  const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-  const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * x * x);
-  const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-  const float half = 0.5f * poly * e;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.2316419f, fabsf(z), 1.f));
+  const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * (z * z));
+  float poly = fmaf(t, -0.0704237595f, 0.247685075f);
+  poly = fmaf(t, poly, -0.201657608f);
+  poly = fmaf(t, poly, 0.225250751f);
+  poly = fmaf(t, poly, 0.0135532282f);
+  poly = fmaf(t, poly, 0.102649979f);
+  poly = fmaf(t, poly, 0.0904201567f);
+  poly = fmaf(t, poly, 0.0925222412f);
+  const float half = t * poly * e;
   return {z > 0.f ? 1.f - half : half, 0.39894228040143268f * e};
 }
-// kShort: for values that are stored in bf16.  GELU's error function is then the approximation above (2e-5 of bf16's rounding),
-// a third of the instructions of the library's, which bound the norms with GELU.
-template <bool kShort>
 __device__ __forceinline__ float activation(float z, int act) {
   switch (act) {
     case DC_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-    case DC_ACT_GELU:
-      if constexpr (kShort) return z * normal_parts(z).cdf;
-      else return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case DC_ACT_GELU: return z * normal_parts(z).cdf;
     case DC_ACT_SILU: return z * sigmoid(z);
     default: return z;
   }
 }
-template <bool kShort>
 __device__ __forceinline__ float activation_slope(float z, int act) {
   switch (act) {
     case DC_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case DC_ACT_GELU:
-      if constexpr (kShort) {
-        const NormalParts n = normal_parts(z);
-        return fmaf(z, n.density, n.cdf);
-      } else {
-        return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * 0.70710678118654752f)));
-      }
+    case DC_ACT_GELU: {
+      const NormalParts n = normal_parts(z);
+      return fmaf(z, n.density, n.cdf);
+    }
     case DC_ACT_SILU: {
       const float s = sigmoid(z);
       return s * fmaf(z, 1.f - s, 1.f);
@@ -55,38 +55,38 @@ __device__ __forceinline__ float activation_slope(float z, int act) {
   }
 }
 // The same for kN values, the choice made once.
-template <int kN, bool kShort>
+template <int kN>
 __device__ __forceinline__ void activate(float (&z)[kN], int act) {
   switch (act) {
     case DC_ACT_RELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation<kShort>(z[k], DC_ACT_RELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_RELU);
       break;
     case DC_ACT_GELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation<kShort>(z[k], DC_ACT_GELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_GELU);
       break;
     case DC_ACT_SILU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation<kShort>(z[k], DC_ACT_SILU);
+      for (int k = 0; k < kN; ++k) z[k] = activation(z[k], DC_ACT_SILU);
       break;
     default: break;
   }
 }
-template <int kN, bool kShort>
+template <int kN>
 __device__ __forceinline__ void slopes(float (&z)[kN], int act) {
   switch (act) {
     case DC_ACT_RELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation_slope<kShort>(z[k], DC_ACT_RELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_RELU);
       break;
     case DC_ACT_GELU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation_slope<kShort>(z[k], DC_ACT_GELU);
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_GELU);
       break;
     case DC_ACT_SILU:
 #pragma unroll
-      for (int k = 0; k < kN; ++k) z[k] = activation_slope<kShort>(z[k], DC_ACT_SILU);
+      for (int k = 0; k < kN; ++k) z[k] = activation_slope(z[k], DC_ACT_SILU);
       break;
     default:
 #pragma unroll
