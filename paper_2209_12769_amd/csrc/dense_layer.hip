@@ -793,7 +793,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
     // that a wave reads and writes whole rows of its 64 columns
     float* end = reinterpret_cast<float*>(lds) + wave * 32 * kLd;
     constexpr int kLanes = 64 / kW, kRounds = 32 / kW;
-    const int c0 = lane % kLanes * kW, col = n0 + wn * 64 + c0;
+    // a vector that the columns end in starts earlier, so that it is whole: some results are written twice, alike (value by
+    // value, a layer of 32 x 127 took 140 us where one of 32 x 128 took 73, each of 196311 rows)
+    const int at = lane % kLanes * kW, have = g.N - n0 - wn * 64;
+    const int c0 = have < kW ? at : min(at, have - kW), col = n0 + wn * 64 + c0;
     const bool wide = col + kW <= g.N;
     for (int part = 0; part < kI; ++part) {
       const long long r0 = m0 + wm * 32 * kI + part * 32 + lane / kLanes;
@@ -818,16 +821,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int u = 0; u < kRounds; ++u) {
-        if (r0 + u * kW >= rows || col >= g.N) continue;
+        if (r0 + u * kW >= rows || at >= have) continue;
         float z[kW];
 #pragma unroll
-        for (int k = 0; k < kW; k += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(end + (lane / kLanes + u * kW) * kLd + c0 + k);
-          z[k] = v.x;
-          z[k + 1] = v.y;
-          z[k + 2] = v.z;
-          z[k + 3] = v.w;
-        }
+        for (int k = 0; k < kW; ++k) z[k] = end[(lane / kLanes + u * kW) * kLd + c0 + k];
         finish<E, kDz, kColsB>(g, r0 + u * kW, col, z, res[u]);
       }
       __builtin_amdgcn_wave_barrier();
