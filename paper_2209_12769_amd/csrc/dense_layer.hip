@@ -551,10 +551,17 @@ __device__ __forceinline__ void store_wide(char* p, long long i, const float (&x
   *reinterpret_cast<u32x4_any*>(p + i * E::kBytes) = w;
 }
 
-// What becomes of 16 / kBytes neighbouring sums z of a row.
-// r: the residual's 16 bytes, where all of them are columns.
+// What becomes of 16 / kBytes neighbouring sums z of a row: a layer's results (kColsB), or a gradient, which is the sums.
+// r: the residual's 16 bytes, where all of them are columns.  The bias comes in registers: a load here would wait for the
+// stores of the rows before it.
+template <class E>
+__device__ __forceinline__ void bias_at(float (&bias)[16 / E::kBytes], const ProductArgs& g, int col) {
+#pragma unroll
+  for (int k = 0; k < 16 / E::kBytes; ++k) bias[k] = g.bias && col + k < g.N ? g.bias[col + k] : 0.f;
+}
 template <class E, bool kDz, bool kColsB>
-__device__ __forceinline__ void finish(const ProductArgs& g, long long row, int col, float (&z)[16 / E::kBytes], const unsigned (&r)[4]) {
+__device__ __forceinline__ void finish(const ProductArgs& g, long long row, int col, float (&z)[16 / E::kBytes],
+                                       const float (&bias)[16 / E::kBytes], const unsigned (&r)[4]) {
   constexpr int kW = 16 / E::kBytes;
   if constexpr (E::kPieces > 1) {
     unsigned bad = 0;
@@ -570,29 +577,31 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
     }
   }
   if (col + kW <= g.N) {
-    if (g.bias)
+    if constexpr (kColsB) {
 #pragma unroll
-      for (int k = 0; k < kW; ++k) z[k] += g.bias[col + k];
-    if (g.Z) store_wide<E>(g.Z, row * g.ldz + col, z);
-    activate<kW>(z, g.act);
-    if (g.R)
+      for (int k = 0; k < kW; ++k) z[k] += bias[k];
+      if (g.Z) store_wide<E>(g.Z, row * g.ldz + col, z);
+      activate<kW>(z, g.act);
+      if (g.R)
 #pragma unroll
-      for (int k = 0; k < kW; ++k) z[k] += value_of<E>(r, k, 1.f);
+        for (int k = 0; k < kW; ++k) z[k] += value_of<E>(r, k, 1.f);
+    }
     store_wide<E>(g.Y, row * g.ldy + col, z);
     return;
   }
-  if (g.bias)
+  if constexpr (kColsB) {
 #pragma unroll
-    for (int k = 0; k < kW; ++k) z[k] += col + k < g.N ? g.bias[col + k] : 0.f;
-  if (g.Z)
+    for (int k = 0; k < kW; ++k) z[k] += bias[k];
+    if (g.Z)
 #pragma unroll
-    for (int k = 0; k < kW; ++k)
-      if (col + k < g.N) store_value<E>(g.Z, row * g.ldz + col + k, z[k]);
-  activate<kW>(z, g.act);
+      for (int k = 0; k < kW; ++k)
+        if (col + k < g.N) store_value<E>(g.Z, row * g.ldz + col + k, z[k]);
+    activate<kW>(z, g.act);
+  }
 #pragma unroll
   for (int k = 0; k < kW; ++k)
     if (col + k < g.N) {
-      if (g.R) z[k] += load_value<E>(g.R, row * g.ldr + col + k);
+      if (kColsB && g.R) z[k] += load_value<E>(g.R, row * g.ldr + col + k);
       store_value<E>(g.Y, row * g.ldy + col + k, z[k]);
     }
 }
@@ -681,16 +690,17 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
     __syncthreads();
     const int r = t / (32 / kW), c0 = t % (32 / kW) * kW;
     if (r < 32 && m0 + r < rows && n0 + c0 < g.N) {
-      float z[kW];
+      float z[kW], bias[kW];
+      if constexpr (kColsB) bias_at<E>(bias, g, n0 + c0);
       unsigned res[4] = {0, 0, 0, 0};
-      if (g.R && n0 + c0 + kW <= g.N) read_words<16>(res, g.R + ((m0 + r) * g.ldr + n0 + c0) * E::kBytes);
+      if (kColsB && g.R && n0 + c0 + kW <= g.N) read_words<16>(res, g.R + ((m0 + r) * g.ldr + n0 + c0) * E::kBytes);
 #pragma unroll
       for (int k = 0; k < kW; ++k) {
         const float* p = lds + r * kFewLd + c0 + k;
         const float u0 = p[0], u1 = p[32 * kFewLd], u2 = p[64 * kFewLd], u3 = p[96 * kFewLd];
         z[k] = kP > 1 ? (u0 - u1) + (u2 - u3) : (u0 + u1) + (u2 + u3);
       }
-      finish<E, kDz, kColsB>(g, m0 + r, n0 + c0, z, res);
+      finish<E, kDz, kColsB>(g, m0 + r, n0 + c0, z, bias, res);
     }
   }
 }
@@ -729,7 +739,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
   auto load = [&](long long tile, int step) {
     const long long m0 = tile / nct * kTileM;
     const int n0 = (int)(tile % nct) * kTileN;
-    const int seg = step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS;
+    const int seg = !kColsB ? 0 : step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS;
     sa.load(part_of(g.a, seg) + m0 * lda + k0 * E::kBytes, kDz ? g.a.z + m0 * ldz + k0 * E::kBytes : nullptr, lda, ldz,
             (int)min(rows - m0, (long long)kTileM), k0, d);
     const long long kb = (long long)seg * d + k0;
@@ -798,10 +808,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
     const int at = lane % kLanes * kW, have = g.N - n0 - wn * 64;
     const int c0 = have < kW ? at : min(at, have - kW), col = n0 + wn * 64 + c0;
     const bool wide = col + kW <= g.N;
+    float bias[kW];
+    if constexpr (kColsB) bias_at<E>(bias, g, col);
     for (int part = 0; part < kI; ++part) {
       const long long r0 = m0 + wm * 32 * kI + part * 32 + lane / kLanes;
       unsigned res[kRounds][4];
-      if (g.R && wide) {                               // requested together; past the end the last row again
+      if (kColsB && g.R && wide) {                     // requested together; past the end the last row again
 #pragma unroll
         for (int u = 0; u < kRounds; ++u) read_words<16>(res[u], g.R + (min(r0 + u * kW, rows - 1) * g.ldr + col) * E::kBytes);
       }
@@ -825,7 +837,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
         float z[kW];
 #pragma unroll
         for (int k = 0; k < kW; ++k) z[k] = end[(lane / kLanes + u * kW) * kLd + c0 + k];
-        finish<E, kDz, kColsB>(g, r0 + u * kW, col, z, res[u]);
+        finish<E, kDz, kColsB>(g, r0 + u * kW, col, z, bias, res[u]);
       }
       __builtin_amdgcn_wave_barrier();
     }
