@@ -415,6 +415,30 @@ __global__ __launch_bounds__(256) void no_longs_kernel(unsigned long long* found
   for (int k = i; k < most; k += gridDim.x * blockDim.x) longs[k] = make_int2(0, 0);
 }
 
+// The list comes in the order in which the graphs were found.  Gradients of gamma and beta are sums over the chunks as they are
+// dealt out, so for them it is put in the graphs' order, a wave per entry, and a call gives the same bits each time.
+__global__ __launch_bounds__(256) void order_longs_kernel(const Norm n, int2* __restrict__ ordered) {
+  if (n.a.stop && n.a.stop[0] != 0) return;
+  const int nlong = (int)min((unsigned)(n.found[0] >> 32), (unsigned)n.most_longs), lane = threadIdx.x & 63;
+  for (int i = blockIdx.x * 4 + (threadIdx.x >> 6); i < nlong; i += gridDim.x * 4) {
+    const int2 e = n.longs[i];
+    int before = 0;
+    long long chunks = 0;                              // of the graphs in front
+    for (int k = lane; k < nlong; k += 64) {
+      const int g = n.longs[k].x;
+      if (g > e.x || (g == e.x && k >= i)) continue;
+      const long long rows = (long long)n.a.node_off[g + 1] - n.a.node_off[g];
+      ++before;
+      chunks += rows > 0 ? (rows + n.chunk_rows - 1) / n.chunk_rows : 0;
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+      before += __shfl_xor(before, o, 64);
+      chunks += __shfl_xor(chunks, o, 64);
+    }
+    if (lane == 0) ordered[before] = make_int2(e.x, (int)min(chunks, (long long)n.most_chunks));
+  }
+}
+
 struct Segment {
   int entry, g;            // place in the list, graph
   long long lo, hi;        // rows of the chunk
@@ -672,6 +696,7 @@ hipError_t run(Norm n, hipStream_t s) {
   n.long_rows = p.long_rows;
   n.chunk_rows = chunk_rows(n.a.rows, n.a.n_cu);
   char* w = n.a.workspace;
+  int2* ordered = nullptr;
   if (p.chunks) {
     const size_t longs = (size_t)(n.a.rows / p.long_rows) + 1;
     n.found = reinterpret_cast<unsigned long long*>(w);
@@ -682,7 +707,11 @@ hipError_t run(Norm n, hipStream_t s) {
     n.most_chunks = (int)(n.a.rows / n.chunk_rows + (long long)longs);
     w += (size_t)n.most_chunks * n.a.G * sizeof(double2);
     n.means = reinterpret_cast<float2*>(w);
-    if (kBack) w += longs * n.a.G * sizeof(float2);
+    if (kBack) {
+      w += longs * n.a.G * sizeof(float2);
+      ordered = reinterpret_cast<int2*>(w);
+      w += longs * sizeof(int2);
+    }
     hipLaunchKernelGGL(no_longs_kernel, dim3((unsigned)(longs < 16384 ? (longs + 255) / 256 : 64)), dim3(256), 0, s, n.found, n.longs, n.most_longs);
   }
   n.cols = reinterpret_cast<float*>(w);
@@ -696,6 +725,10 @@ hipError_t run(Norm n, hipStream_t s) {
     n.nslab = p.chunk_nslab;
     n.lanes = p.chunk_lanes;
     const dim3 cgrid(p.chunk_blocks * n.nslab);
+    if (kBack && n.a.dgamma) {
+      hipLaunchKernelGGL(order_longs_kernel, dim3((unsigned)(n.most_longs < 16 * n.a.n_cu ? (n.most_longs + 3) / 4 : 4 * n.a.n_cu)), dim3(256), 0, s, n, ordered);
+      n.longs = ordered;
+    }
     hipLaunchKernelGGL((chunk_sums_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
     const long long longs = n.a.rows / p.long_rows + 1, most = 4LL * n.a.n_cu;
     const int wide = n.a.G < 64 ? pow2_at_least(n.a.G) : 64;
@@ -745,7 +778,7 @@ size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backwar
   const size_t longs = chunks ? (size_t)(rows / 1024) + 1 : 0;
   size_t b = chunks ? 16 + (longs * sizeof(int2) + 15) / 16 * 16 + ((size_t)nc + longs) * G * sizeof(double2) : 0;
   if (backward) {
-    b += longs * G * sizeof(float2);
+    b += longs * (G * sizeof(float2) + sizeof(int2));
     b += (size_t)((n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most) + (chunks ? (nc < most ? nc : most) : 0)) * 2 * C * sizeof(float);
   }
   return b;

@@ -589,6 +589,20 @@ def test_results_do_not_depend_on_what_else_is_there(ev):
     assert all(torch.equal(u, v) for u, v in zip(p, q))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_graph_norm_gradients_of_many_long_graphs_repeat(ev, dtype):
+    """Graphs that are cut into chunks are found in any order; the sums over them are formed in theirs."""
+    s, C, G = [5000 + 137 * i for i in range(40)] + [3, 0, 9000], 32, 4
+    x, gamma, beta = norm_inputs(s, C, dtype)
+    dy, off = rand(9, sum(s), C).to(TYPES[dtype]).cuda(), offsets(s)
+    x, gamma, beta = x.cuda(), gamma.cuda(), beta.cuda()
+    _, mean, rstd = ev.graph_norm(x, off, G, gamma, beta, EPS, "silu")
+    first = ev.graph_norm_backward(dy, x, off, G, gamma, beta, mean, rstd, "silu")
+    for _ in range(20):
+        again = ev.graph_norm_backward(dy, x, off, G, gamma, beta, mean, rstd, "silu")
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
 # ---------------------------------------------------------------------------
 # refusals
 # ---------------------------------------------------------------------------
