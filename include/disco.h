@@ -473,7 +473,8 @@ typedef struct {
   const float* bias;    /* [out] or null                                              */
   const void* residual; /* R [rows, out] or null; may be the same array as Y          */
   int64_t ld_residual;
-  void* Z;              /* [rows, out] or null: what the gradient of the activation needs */
+  void* Z;              /* [rows, out] or null: what the gradient of the activation needs;
+                         * none of the other arrays                                   */
   int64_t ldz;
   void* Y;              /* [rows, out], not X                                         */
   int64_t ldy;
@@ -496,7 +497,7 @@ typedef struct {
   const dc_kept_rows* kept;  /* host struct, or null; X is not read then              */
   const void* W;
   int64_t ldw;
-  void* dX;             /* [rows, in] or null                                         */
+  void* dX;             /* [rows, in] or null; not dY, Z or X                         */
   int64_t lddx;
   void* dW;             /* [in, out] or null                                          */
   int64_t lddw;
@@ -511,8 +512,8 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
  * channels are in `groups` groups of channels / groups neighbours; per graph and group, over its rows and channels:
  *   mean, rstd = 1 / sqrt(variance + eps);  y = act(gamma (x - mean) rstd + beta)
  * A graph without rows has mean 0 and variance 0.  Rows of no graph (before node_off[0], behind node_off[n_graphs]) are
- * neither read nor written.  Rows are at most 2^17 elements apart here.  A graph whose offsets do not ascend within [0, rows] is left alone, and dc_check
- * reports DC_ERR_BAD_GRAPH.                                                                                         */
+ * neither read nor written.  Rows are at most 2^17 elements apart here.  A graph whose offsets do not ascend within
+ * [0, rows] is left alone, and dc_check reports DC_ERR_BAD_GRAPH.  The same call gives the same bits.               */
 typedef struct {
   int32_t dtype, act;
   int64_t rows;             /* rows of x and y                                            */

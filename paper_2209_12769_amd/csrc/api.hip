@@ -1678,6 +1678,8 @@ dc_status dc_dense(dc_ctx* ctx, const dc_dense_args* args, void* stream) {
   if (st == DC_OK && a.Z) st = array_check(ctx, a.Z, a.ldz, a.rows, a.out, es, "Z");
   if (st != DC_OK || a.rows == 0) return st;
   if (!at(a.bias, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "bias is not aligned to its elements");
+  if (a.Y == a.X || (a.Z && (a.Z == a.X || a.Z == a.Y || a.Z == a.residual)))
+    return fail(ctx, DC_ERR_INVALID_ARG, "Y cannot be X, and Z no array of the others");
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   DenseArgs d{};
@@ -1722,6 +1724,8 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   if (st == DC_OK && a.dX) st = array_check(ctx, a.dX, a.lddx, a.rows, a.in, es, "dX");
   if (st == DC_OK && a.dX) st = array_check(ctx, a.W, a.ldw, a.in, a.out, es, "W");
   if (st != DC_OK) return st;
+  if (a.rows > 0 && a.dX && (a.dX == a.dY || (a.act != DC_ACT_NONE && a.dX == a.Z) || (a.dW && !a.kept && a.dX == a.X)))
+    return fail(ctx, DC_ERR_INVALID_ARG, "dX cannot be dY, Z or X");
   if (!at(a.db, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "db is not aligned to its elements");
   if (!a.workspace || a.workspace_bytes < dc_dense_backward_bytes(ctx, a.dtype, a.act, a.rows, a.in, a.out))
     return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_dense_backward_bytes");

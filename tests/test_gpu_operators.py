@@ -606,6 +606,50 @@ def test_graph_norm_gradients_of_many_long_graphs_repeat(ev, dtype):
 # ---------------------------------------------------------------------------
 # refusals
 # ---------------------------------------------------------------------------
+def test_c_calls_refuse_arrays_in_each_others_place_and_rows_too_far_apart(B, ev):
+    """Each refused with nothing enqueued: what a kernel would still read, or offsets beyond what it counts in."""
+    x, w, y, z = (torch.zeros(8, 8, device="cuda") for _ in range(4))
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    ok = dict(dtype=B.DC_F32, act=1, rows=8, n_in=8, n_out=8, X=x.data_ptr(), ldx=8, W=w.data_ptr(), ldw=8, Z=z.data_ptr(), ldz=8,
+              Y=y.data_ptr(), ldy=8)
+    far = (1 << 22) + 1
+    for bad, want in [(dict(Y=x.data_ptr()), B.DC_ERR_INVALID_ARG), (dict(Z=x.data_ptr()), B.DC_ERR_INVALID_ARG),
+                      (dict(Z=y.data_ptr()), B.DC_ERR_INVALID_ARG), (dict(residual=z.data_ptr(), ld_residual=8), B.DC_ERR_INVALID_ARG),
+                      (dict(ldx=far), B.DC_ERR_UNSUPPORTED), (dict(ldw=far), B.DC_ERR_UNSUPPORTED), (dict(ldy=far), B.DC_ERR_UNSUPPORTED),
+                      (dict(ldz=far), B.DC_ERR_UNSUPPORTED)]:
+        assert B.dc_dense(ev.ctx, B.DcDenseArgs(**{**ok, **bad})) == want, bad
+    back = dict(dtype=B.DC_F32, act=1, rows=8, n_in=8, n_out=8, dY=y.data_ptr(), lddy=8, Z=z.data_ptr(), ldz=8, X=x.data_ptr(), ldx=8,
+                W=w.data_ptr(), ldw=8, dX=ws.data_ptr(), lddx=8, dW=ws.data_ptr() + 4096, lddw=8, workspace=ws.data_ptr() + 8192,
+                workspace_bytes=ws.numel() - 8192)
+    for bad, want in [(dict(dX=y.data_ptr()), B.DC_ERR_INVALID_ARG), (dict(dX=z.data_ptr()), B.DC_ERR_INVALID_ARG),
+                      (dict(dX=x.data_ptr()), B.DC_ERR_INVALID_ARG), (dict(lddx=far), B.DC_ERR_UNSUPPORTED)]:
+        assert B.dc_dense_backward(ev.ctx, B.DcDenseBackwardArgs(**{**back, **bad})) == want, bad
+    off = torch.tensor([0, 4, 8], dtype=torch.int32, device="cuda")
+    norm = dict(dtype=B.DC_F32, act=0, rows=8, n_graphs=2, channels=8, groups=2, eps=1e-5, node_off=off.data_ptr(), X=x.data_ptr(), ldx=8,
+                mean=w.data_ptr(), rstd=w.data_ptr() + 64, Y=y.data_ptr(), ldy=8)
+    far = (1 << 17) + 1
+    for bad in (dict(ldx=far), dict(ldy=far)):
+        assert B.dc_graph_norm(ev.ctx, B.DcGraphNormArgs(**{**norm, **bad})) == B.DC_ERR_UNSUPPORTED, bad
+    for bad in (dict(lddy=far), dict(lddx=far), dict(dres=z.data_ptr(), lddres=far)):
+        args = {**norm, **dict(dY=z.data_ptr(), lddy=8, dX=y.data_ptr(), lddx=8), **bad}
+        assert B.dc_graph_norm_backward(ev.ctx, B.DcGraphNormArgs(**args)) == B.DC_ERR_UNSUPPORTED, bad
+    torch.cuda.synchronize()
+    assert all((v == 0).all() for v in (x, w, y, z)) and ev.check() == B.DC_OK
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(700, 96, 139), (33, 40, 70), (3000, 64, 131), (1500, 32, 255)])
+def test_dense_adds_to_its_residual_in_place(ev, dtype, shape):
+    """Y may be the residual's array; vectors that the columns end in are formed twice and have to find the old values."""
+    M, K, N = shape
+    x, w, b, r = (rand(i, *s).to(TYPES[dtype]) for i, s in enumerate([(M, K), (K, N), (N,), (M, N)], 11))
+    b = b.float()
+    want = ev.dense(x.cuda(), w.cuda(), b.cuda(), "silu", r.cuda())
+    y = r.cuda()
+    ev.dense(x.cuda(), w.cuda(), b.cuda(), "silu", y, out=y)
+    assert torch.equal(y, want)
+
+
 def test_c_calls_refuse(B, ev):
     x = torch.zeros(4, 8, device="cuda")
     ok = dict(dtype=B.DC_F32, act=0, rows=4, n_in=8, n_out=8, X=x.data_ptr(), ldx=8, W=x.data_ptr(), ldw=8, Y=x.data_ptr(), ldy=8)
