@@ -157,6 +157,47 @@ def test_dense_keeps_rows_apart(ev, dtype, value):
         assert torch.equal(torch.isnan(got[7]).cpu(), torch.isnan(want)) and (math.isnan(value) or torch.equal(got[7].cpu(), want))
 
 
+# More than four 32 x 32 tiles per CU (256 of them): widths that end in every place of a tile, a wave's 64 columns and a vector,
+# contractions of one to many steps, the smallest widths that tiles take.
+TILED = [(33001, 32, 24), (9001, 201, 139), (4501, 70, 255), (7003, 129, 131), (3001, 1031, 390), (2203, 8, 513), (40001, 8, 4),
+         (17003, 40, 65), (9007, 33, 129), (8200, 72, 256), (4100, 9, 260), (33000, 8, 5), (5000, 256, 257)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", TILED)
+def test_dense_of_many_rows(ev, dtype, shape):
+    test_dense(ev, dtype, shape, ["silu", "none", "relu", "gelu"][(shape[0] + shape[2]) % 4])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ld,first", [(3, 1), (8, 8)])
+@pytest.mark.parametrize("shape", [(9000, 72, 131), (4600, 33, 250)])
+def test_dense_of_many_rows_anywhere(ev, dtype, ld, first, shape):
+    test_dense_rows_anywhere(ev, dtype, ld, first, shape)
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan, -3.4e38])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [64, 139])
+def test_dense_of_many_rows_keeps_them_apart(ev, dtype, value, N):
+    t, rows, K = TYPES[dtype], 20001, 96
+    x, w = rand(1, rows, K).to(t), (rand(2, K, N) / math.sqrt(K)).to(t)
+    w[5] = w[5].abs() * 0.25 + 0.01
+    clean = ev.dense(x.cuda(), w.cuda())
+    bad = [7, 12345, rows - 1]
+    x[bad, 5] = value
+    got = ev.dense(x.cuda(), w.cuda())
+    others = torch.ones(rows, dtype=torch.bool)
+    others[bad] = False
+    assert torch.equal(got[others.cuda()], clean[others.cuda()])
+    for i in bad:
+        want = (x[i].double() @ w.double()).to(t)
+        if abs(value) == 3.4e38:
+            assert torch.allclose(got[i].cpu().double(), want.double(), rtol=1e-2 if dtype == "bf16" else 1e-6)
+        else:
+            assert torch.equal(torch.isnan(got[i]).cpu(), torch.isnan(want)) and (math.isnan(value) or torch.equal(got[i].cpu(), want))
+
+
 def backward_reference(dy, x, w, z, name, t):
     """Gradients and their tolerances, all in 64 bits; x as the values that are multiplied."""
     d = dy.double()
@@ -198,6 +239,14 @@ def test_dense_backward(B, ev, dtype, shape, name, kept):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(33001, 24, 32), (9001, 201, 139), (4501, 255, 70), (7003, 131, 129), (3001, 390, 1031), (2203, 513, 8),
+                                   (40001, 4, 8), (17003, 65, 40), (9007, 129, 33), (8200, 256, 256), (4100, 260, 9)])
+@pytest.mark.parametrize("name,kept", [("relu", False), ("relu", True), ("gelu", True)])
+def test_dense_backward_of_many_rows(B, ev, dtype, shape, name, kept):
+    test_dense_backward(B, ev, dtype, shape, name, kept)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("ld,first", [(0, 1), (3, 0), (8, 8)])
 def test_dense_backward_rows_anywhere(ev, dtype, ld, first):
     t, rows, K, N = TYPES[dtype], 170, 72, 40
@@ -219,6 +268,19 @@ def test_dense_backward_keeps_sums_apart(ev, dtype):
     dx, dw, db = ev.dense_backward(dy.cuda(), x.cuda(), w.cuda())
     assert torch.isinf(dx[11]).all() and torch.isinf(dw[:, 3]).all() and torch.isinf(db[3])
     row, col = torch.arange(rows, device="cuda") != 11, torch.arange(N, device="cuda") != 3
+    assert torch.equal(dx[row], clean[0][row]) and torch.equal(dw[:, col], clean[1][:, col]) and torch.equal(db[col], clean[2][col])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dense_backward_of_many_rows_keeps_sums_apart(ev, dtype):
+    t, rows, K, N = TYPES[dtype], 20001, 70, 48
+    x, w, dy = rand(1, rows, K).abs().to(t) + 0.1, (rand(2, K, N).abs() + 0.1).to(t), rand(3, rows, N).to(t)
+    z = torch.ones(rows, N, dtype=t)
+    clean = ev.dense_backward(dy.cuda(), x.cuda(), w.cuda(), "relu", z.cuda())
+    dy[11111, 3] = math.inf
+    dx, dw, db = ev.dense_backward(dy.cuda(), x.cuda(), w.cuda(), "relu", z.cuda())
+    assert torch.isinf(dx[11111]).all() and torch.isinf(dw[:, 3]).all() and torch.isinf(db[3])
+    row, col = torch.arange(rows, device="cuda") != 11111, torch.arange(N, device="cuda") != 3
     assert torch.equal(dx[row], clean[0][row]) and torch.equal(dw[:, col], clean[1][:, col]) and torch.equal(db[col], clean[2][col])
 
 
@@ -638,7 +700,7 @@ def test_c_calls_refuse_arrays_in_each_others_place_and_rows_too_far_apart(B, ev
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("shape", [(700, 96, 139), (33, 40, 70), (3000, 64, 131), (1500, 32, 255)])
+@pytest.mark.parametrize("shape", [(700, 96, 139), (33, 40, 70), (8000, 64, 131), (4500, 32, 255)])
 def test_dense_adds_to_its_residual_in_place(ev, dtype, shape):
     """Y may be the residual's array; vectors that the columns end in are formed twice and have to find the old values."""
     M, K, N = shape
