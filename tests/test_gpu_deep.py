@@ -132,6 +132,40 @@ def test_cost(B, dtype, tol):
     ev.close()
 
 
+@pytest.mark.parametrize("dtype,tol", [("f32", 1e-5), ("bf16", 2e-2)])
+def test_estimates_of_many_candidates(B, dtype, tol):
+    """Enough rows for the dense layer's tiles, beside a handful of them that the same context takes next."""
+    F, H, L, groups, name = 32, 128, 3, 8, "gelu"
+    w, few = workload(F, H, L, dtype, C=500), workload(F, H, L, dtype, C=3)
+    gamma, beta = norms(H, L)
+    ev = B.evaluator_for(w)
+    ev.set_layer_norms(groups, gamma, beta, name, EPS)
+    for v in (w, few, w):
+        got = ev.eval_candidates(ev.to_device(v.cand_graph), ev.to_device(v.cand_off), ev.to_device(v.group_id)).cpu().numpy()
+        assert ev.check() == B.DC_OK, B.dc_last_error(ev.ctx)
+        ref = oracle_predictions(v, gamma, beta, groups, name)
+        assert np.abs(got - ref).max() <= tol * np.abs(ref).max()
+    ev.close()
+
+
+@pytest.mark.parametrize("keep,bound", [("f32", 1e-5), ("8bit", 2e-3)])
+def test_gradient_of_many_samples(B, keep, bound):
+    F, H, L, groups, name = 32, 128, 3, 4, "silu"
+    w, g = training(B, F, H, L, C=150)
+    positive_head(w)
+    gamma, beta = norms(H, L)
+    loss, pred, grad, fo, target = run_gradient(B, w, g, keep, groups, gamma, beta, name)
+    assert fo.ntot > 8200                                  # more than 1024 tiles of 32 x 32
+    p = ot.Params.from_weights(w.weights, F, H, L)
+    rl, ry, rg, dga, dbe = deep.loss_and_gradients(fo, target, p, gamma, beta, groups, EPS, name, kept=keep == "8bit")
+    assert abs(loss - rl) <= 2e-5 * rl and np.abs(pred - ry).max() <= 1e-5 * np.abs(ry).max()
+    for a, b in zip(tensors(grad, F, H, L, True), tensors(np.concatenate([rg.flat(), dga.ravel(), dbe.ravel()]), F, H, L, True)):
+        if keep == "f32":
+            assert np.abs(a - b).max(initial=0) <= bound * np.abs(b).max(initial=0)
+        else:
+            assert np.linalg.norm(a - b) <= bound * np.linalg.norm(b)
+
+
 def training(B, F, H, L, C=3, seed=4):
     g = wl.make("cfg2", 1).graphs[0]
     w = wl.custom("deep-train", wl.ModelSpec(F, H, L, "f32"), [g], [wl.training_labels(g, seed, C, kmax=20)], seed=seed)
