@@ -556,8 +556,8 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
   const int slab = blockIdx.x % n.nslab, t = threadIdx.x;
   const int c0 = slab * n.slab, width = min(n.slab, n.a.C - c0);
   const int used = width / kV, lane = t & (n.lanes - 1), rl = t / n.lanes, step = kChunkThreads / n.lanes;
-  if (lane >= used) return;
-  const int c = c0 + lane * kV, group = c / n.cg;
+  const bool in = lane < used;                         // all lanes of a wave stay: they look for its segments together
+  const int c = c0 + (in ? lane * kV : 0), group = c / n.cg;
   const Affine<kV> f = affine_at<kV>(n.a, c);
   const unsigned long long found = n.found[0];
   const int nchunk = (int)min((unsigned)found, (unsigned)n.most_chunks), nlong = (int)min((unsigned)(found >> 32), (unsigned)n.most_longs);
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
       const float mu = n.a.mean[(size_t)seg.g * n.a.G + group], rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
       const float2 s = kBack ? n.means[(size_t)seg.entry * n.a.G + group] : make_float2(0.f, 0.f);
       const Places at = places_of<T, X, kBack>(n.a, seg.lo);
-      const int rows = (int)(seg.hi - seg.lo), count = rl < rows ? (rows - rl + step - 1) / step : 0;
+      const int rows = (int)(seg.hi - seg.lo), count = in && rl < rows ? (rows - rl + step - 1) / step : 0;
       each_row<T, X, kV, kBack, 4>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);

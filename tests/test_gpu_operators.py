@@ -652,6 +652,22 @@ def test_results_do_not_depend_on_what_else_is_there(ev):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,G", [(208, 16), (36, 9), (24, 1), (512, 8)])
+def test_graph_norm_of_many_long_graphs(ev, dtype, C, G):
+    """More long graphs than the last wave of a row of channels has channels."""
+    s = [4100 + 61 * i for i in range(70)] if C < 40 else [4200 + 353 * i for i in range(22)]
+    x, gamma, beta = norm_inputs(s, C, dtype)
+    off = offsets(s)
+    got = ev.graph_norm(x.cuda(), off, G, gamma.cuda(), beta.cuda(), EPS, "silu")
+    check_norm(ev, x, s, G, gamma, beta, "silu", dtype, got)
+    dy = rand(9, sum(s), C).to(TYPES[dtype])
+    ref = norm_back_reference(x, dy, None, s, G, gamma, beta, got[1].cpu(), got[2].cpu(), "silu", TYPES[dtype])
+    back = ev.graph_norm_backward(dy.cuda(), x.cuda(), off, G, gamma.cuda(), beta.cuda(), got[1], got[2], "silu")
+    for g, (want, tol), what in zip(back, ref, ("dx", "dgamma", "dbeta")):
+        close(g, want, tol, what)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_graph_norm_gradients_of_many_long_graphs_repeat(ev, dtype):
     """Graphs that are cut into chunks are found in any order; the sums over them are formed in theirs."""
     s, C, G = [5000 + 137 * i for i in range(40)] + [3, 0, 9000], 32, 4
