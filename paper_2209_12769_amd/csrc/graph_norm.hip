@@ -772,8 +772,9 @@ void launch_column_sums(const float* part, int blocks, int n1, float* out1, int 
 }
 
 size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backward, int n_cu) {
-  // what any vector width and type would need, and any smaller number of rows: chunks of fewer than 512 rows are at most four per CU
-  const long long most = blocks_most(64, n_cu), by_rows = rows / 512 + 1, nc = by_rows > 4LL * n_cu ? by_rows : 4LL * n_cu + 1;
+  // what any vector width and type would need, and any smaller number of rows: chunks of 512 rows, or four per CU and, as their
+  // rows are rounded (from 64 on) before the last CU has its four, up to a 64th more
+  const long long most = blocks_most(64, n_cu), by_rows = rows / 512 + 1, per_cu = 4LL * n_cu + n_cu / 16 + 2, nc = by_rows > per_cu ? by_rows : per_cu;
   const bool chunks = rows > 1024;
   const size_t longs = chunks ? (size_t)(rows / 1024) + 1 : 0;
   size_t b = chunks ? 16 + (longs * sizeof(int2) + 15) / 16 * 16 + ((size_t)nc + longs) * G * sizeof(double2) : 0;

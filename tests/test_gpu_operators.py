@@ -684,6 +684,47 @@ def test_graph_norm_gradients_of_many_long_graphs_repeat(ev, dtype):
 # ---------------------------------------------------------------------------
 # refusals
 # ---------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,graphs,C,G", [(66559, 1, 32, 4), (66559, 3, 490, 1), (65617, 29, 175, 1), (65638, 388, 366, 1), (300, 7, 64, 8)])
+def test_graph_norm_stays_in_its_workspace(B, ev, rows, graphs, C, G):
+    """A workspace of just the bytes asked for, between others that stay as they are; rows where a CU's four chunks come
+    out a little shorter than a fourth of its share."""
+    x, dy = rand(1, rows, C).float().cuda(), rand(2, rows, C).float().cuda()
+    out, dx, stats, vectors = torch.empty_like(x), torch.empty_like(x), torch.empty(2, graphs, G, device="cuda"), torch.empty(2, C, device="cuda")
+    cut = np.linspace(0, rows, graphs + 1).astype(np.int64)
+    off = torch.tensor(cut, dtype=torch.int32, device="cuda")
+    args = dict(dtype=B.DC_F32, act=3, rows=rows, n_graphs=graphs, channels=C, groups=G, eps=1e-5, node_off=off.data_ptr(),
+                X=x.data_ptr(), ldx=C, mean=stats[0].data_ptr(), rstd=stats[1].data_ptr(), Y=out.data_ptr(), ldy=C, dY=dy.data_ptr(), lddy=C,
+                dX=dx.data_ptr(), lddx=C, dgamma=vectors[0].data_ptr(), dbeta=vectors[1].data_ptr())
+    for back, call in ((False, B.dc_graph_norm), (True, B.dc_graph_norm_backward)):
+        size = B.dc_graph_norm_bytes(ev.ctx, rows, graphs, C, G, back)
+        buf = torch.full((size + (4 << 20),), 77, dtype=torch.uint8, device="cuda")
+        ws = buf[2 << 20:(2 << 20) + size]
+        torch.cuda.synchronize()
+        assert call(ev.ctx, B.DcGraphNormArgs(**args, workspace=ws.data_ptr(), workspace_bytes=size)) == B.DC_OK
+        torch.cuda.synchronize()
+        assert ev.check() == B.DC_OK
+        assert (buf[:2 << 20] == 77).all() and (buf[(2 << 20) + size:] == 77).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("rows,K,N", [(1, 1, 1), (5000, 96, 139), (9001, 257, 256), (257, 700, 33)])
+def test_dense_backward_stays_in_its_workspace(B, ev, dtype, act, rows, K, N):
+    t, code = TYPES[dtype], B.DC_F32 if dtype == "f32" else B.DC_BF16
+    x, w, dy, z = (rand(i, *s).to(t).cuda() for i, s in enumerate([(rows, K), (K, N), (rows, N), (rows, N)], 1))
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device="cuda")
+    size = B.dc_dense_backward_bytes(ev.ctx, code, act, rows, K, N)
+    buf = torch.full((size + (4 << 20),), 77, dtype=torch.uint8, device="cuda")
+    ws = buf[2 << 20:(2 << 20) + size]
+    torch.cuda.synchronize()
+    assert B.dc_dense_backward(ev.ctx, B.DcDenseBackwardArgs(
+        dtype=code, act=act, rows=rows, n_in=K, n_out=N, dY=dy.data_ptr(), lddy=N, Z=z.data_ptr(), ldz=N, X=x.data_ptr(), ldx=K,
+        W=w.data_ptr(), ldw=N, dX=dx.data_ptr(), lddx=K, dW=dw.data_ptr(), lddw=N, db=db.data_ptr(), workspace=ws.data_ptr(),
+        workspace_bytes=size)) == B.DC_OK
+    torch.cuda.synchronize()
+    assert (buf[:2 << 20] == 77).all() and (buf[(2 << 20) + size:] == 77).all()
+
+
 def test_c_calls_refuse_arrays_in_each_others_place_and_rows_too_far_apart(B, ev):
     """Each refused with nothing enqueued: what a kernel would still read, or offsets beyond what it counts in."""
     x, w, y, z = (torch.zeros(8, 8, device="cuda") for _ in range(4))
