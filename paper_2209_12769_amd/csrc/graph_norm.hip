@@ -644,9 +644,26 @@ Plan plan_of(long long rows, int n_graphs, int C, int G, int es, int v, int item
   auto fits = [&](int threads, int lanes) {
     return lanes <= threads && want <= (long long)held_bytes(threads) / (threads * item) * (threads / lanes);
   };
-  // a wave by itself needs no barriers, and what it does not hold it finds in L2: up to twice what it holds
-  const bool wave = p.lanes <= 64 && mean <= 2LL * (held_bytes(64) / (64 * item)) * (64 / p.lanes);
-  p.threads = wave ? 64 : (fits(256, p.lanes) ? 256 : kMost);
+  // A wave by itself needs no barriers, and what it does not hold it finds in L2: up to twice what it holds, in slabs of whole
+  // groups where the rows are wider than its vectors (47207 graphs of 3 rows, 52 groups of 9 channels, bf16: 417 us, and 528
+  // by workgroups).  Else 256 threads that hold whole rows; else narrower slabs (20000 graphs of 30 rows of 512 channels,
+  // gradients in fp32: 883 us, and 2270 by workgroups of 512), for many graphs up to four times what a wave holds (6000 of
+  // 120 rows of 256: 608 us, and 938).
+  auto wave = [&](int most_lanes, long long times) {
+    const int each = most_lanes * v / cg;              // groups
+    if (each < 1) return false;
+    const int slabs = (G + each - 1) / each, slab = (G + slabs - 1) / slabs * cg, lanes = pow2_at_least((slab + v - 1) / v);
+    if ((slab * es < 64 && slabs > 1) || mean > times * (held_bytes(64) / (64 * item)) * (64 / lanes)) return false;
+    p.slab = slab;
+    p.lanes = lanes;
+    return true;
+  };
+  auto narrower = [&](long long times) { return wave(32, times) || wave(16, times) || wave(8, times); };
+  if (wave(64, 2)) p.threads = 64;
+  else if (fits(256, p.lanes)) p.threads = 256;
+  else if (narrower(2)) p.threads = 64;
+  else if (n_graphs >= 4 * n_cu && !fits(kMost, p.lanes) && (narrower(4) || wave(64, 4))) p.threads = 64;
+  else p.threads = kMost;
   const int narrow = slab_of(C, cg, es);
   // slabs also where whole rows would leave most CUs without work
   if (p.threads == kMost && (!fits(p.threads, p.lanes) || n_graphs < n_cu / 2)) {

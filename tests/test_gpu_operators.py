@@ -668,6 +668,21 @@ def test_graph_norm_of_many_long_graphs(ev, dtype, C, G):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes,C,G", [([30, 31, 0, 40] * 25, 512, 8), ([30, 31, 0, 40] * 25, 468, 52), ([110, 131, 1] * 700, 75, 5), ([100] * 1030, 104, 8)])
+def test_graph_norm_in_slabs_of_waves(ev, dtype, sizes, C, G):
+    """Rows wider than a wave's vectors, and graphs of more rows than a wave holds of them."""
+    x, gamma, beta = norm_inputs(sizes, C, dtype)
+    off = offsets(sizes)
+    got = ev.graph_norm(x.cuda(), off, G, gamma.cuda(), beta.cuda(), EPS, "gelu")
+    check_norm(ev, x, sizes, G, gamma, beta, "gelu", dtype, got)
+    dy, dres = rand(9, sum(sizes), C).to(TYPES[dtype]), rand(10, sum(sizes), C).to(TYPES[dtype])
+    ref = norm_back_reference(x, dy, dres, sizes, G, gamma, beta, got[1].cpu(), got[2].cpu(), "gelu", TYPES[dtype])
+    back = ev.graph_norm_backward(dy.cuda(), x.cuda(), off, G, gamma.cuda(), beta.cuda(), got[1], got[2], "gelu", dres.cuda())
+    for g, (want, tol), what in zip(back, ref, ("dx", "dgamma", "dbeta")):
+        close(g, want, tol, what)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_graph_norm_gradients_of_many_long_graphs_repeat(ev, dtype):
     """Graphs that are cut into chunks are found in any order; the sums over them are formed in theirs."""
     s, C, G = [5000 + 137 * i for i in range(40)] + [3, 0, 9000], 32, 4
