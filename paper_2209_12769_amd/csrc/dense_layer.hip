@@ -608,8 +608,10 @@ __device__ __forceinline__ void finish(const ProductArgs& g, long long row, int 
 
 // Few rows: a workgroup per 32 x 32 tile, operands straight from memory, the contraction dealt to its four waves in chunks of
 // 16; their sums meet in LDS.  A tile of the kernel below would keep one CU busy while the others have nothing to do.
+// Bound by latency: the launch, two or three rounds of requests, the exchange (1 x 256 -> 256 in bf16 and 437 x 384 -> 128 in
+// fp32 take 5 to 8 us).
 constexpr int kFewLd = 36;             // floats from row to row of a tile in LDS
-template <class E, bool kDz, bool kColsB, bool kVec>      // kVec: the contraction is a multiple of eight
+template <class E, bool kDz, bool kColsB, bool kVec>      // kVec: the contraction is at least eight
 __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs g, long long few) {
   if (g.stop && g.stop[0] != 0) return;
   constexpr int kP = E::kPieces, kW = 16 / E::kBytes;
@@ -627,11 +629,12 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
       Raw<E, 8, kDz> a;
       Raw<E, kColsB ? 1 : 8, false> b[kColsB ? 8 : 1];
     };
-    // past the end the last chunk again, so that no request waits behind a branch
+    // past the end the last chunk again, so that no request waits behind a branch; eight indices that reach behind the last
+    // one are taken earlier, and those that the eight before have are cleared
     const unsigned ldb = (unsigned)g.b.ld * E::kBytes;
     const char* pb = g.b.p[0] + (kColsB ? (long long)col * E::kBytes : (long long)col * ldb);
     auto load = [&](Chunk& x, int c) {
-      const int k = min(c, chunks - 1) * 16 + 8 * lh, ka = k < g.K ? k : 0;
+      const int k = min(c, chunks - 1) * 16 + 8 * lh, ka = kVec ? min(k, g.K - 8) : 0;
       const int seg = (ka >= 2 * g.a.d ? 2 : (ka >= g.a.d ? 1 : 0)), kd = ka - seg * g.a.d;      // parts are multiples of eight
       const char* pa = part_of(g.a, seg) + (row * g.a.ld + kd) * E::kBytes;
       const char* pz = kDz ? g.a.z + (row * g.a.ldz + kd) * E::kBytes : nullptr;
@@ -639,7 +642,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
       else fetch_some<E, 8, kDz>(x.a, pa, pz, 0, 0, min(g.K - ka, 8));
       if constexpr (kColsB) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fetch<E, 1, false>(x.b[i], pb + (long long)min(k + i, g.K - 1) * ldb, nullptr, 0, 0);
+        for (int i = 0; i < 8; ++i) fetch<E, 1, false>(x.b[i], pb + (long long)(kVec ? ka + i : min(k + i, g.K - 1)) * ldb, nullptr, 0, 0);
       } else {
         if constexpr (kVec) fetch<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0);
         else fetch_some<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0, min(g.K - ka, 8));
@@ -647,12 +650,12 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
     };
     f32x16 acc = zero16();
     auto step = [&](const Chunk& x, int c) {
-      const int k = c * 16 + 8 * lh;
+      const int k = c * 16 + 8 * lh, from = kVec ? k - min(k, g.K - 8) : 0, to = kVec ? 8 : g.K - k;      // the indices that count
       u32x4 a[kP], b[kP];
       float y[8];
       values<E, 8, kDz>(y, x.a);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = k + i < g.K ? y[i] : 0.f;
+      for (int i = 0; i < 8; ++i) y[i] = i >= from && i < to ? y[i] : 0.f;
       pieces_of<kP>(a, y);
       if constexpr (kColsB) {
 #pragma unroll
@@ -661,7 +664,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
         values<E, 8, false>(y, x.b[0]);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = k + i < g.K ? (kP > 1 ? y[i] * sign : y[i]) : 0.f;
+      for (int i = 0; i < 8; ++i) y[i] = i >= from && i < to ? (kP > 1 ? y[i] * sign : y[i]) : 0.f;
       pieces_of<kP>(b, y);
 #pragma unroll
       for (int sum = kP - 1; sum >= 0; --sum)
@@ -709,8 +712,11 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
 // side by side in rows, the others in columns.
 // What bounds it is how much is requested at a time: a step's loads (64 KB per CU) are on their way while the step before is
 // multiplied, some 2 us, so that every byte loaded twice shows.  Eight waves take 256 columns, and the rows of a layer of
-// that width are read once; LDS then holds two steps, and a step needs one barrier.  The next tile's first step is
-// requested before a tile's results are written, the residual's rows 32 at a time before the sums go through LDS.
+// that width are read once; LDS then holds two steps, and a step needs one barrier.  The residual's rows are requested 32 at a
+// time before the sums go through LDS.
+// Measured: bf16 2000003 x 768 -> 256 with residual 1.25 ms (4.1 TB/s, 630 TFLOP/s; library product alone 0.97 ms); fp32
+// 196311 x 201 -> 139 with GELU, residual and Z 0.212 ms (matrix cores 25 % busy; the rest is conversions, the
+// epilogue's instructions and waiting); dX of 524309 x 256 -> 768 in bf16 0.42 ms.
 template <class E, int kWaves>
 struct ProductShape {
   static constexpr int kI = E::kPieces == 1 ? 4 : 2, kTileM = 64 * kI, kTileN = 32 * kWaves, KS = E::kPieces == 1 ? 64 : 32;
@@ -845,7 +851,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
 }
 
 // ---- dZ of the smooth activations ----
-// dz = dy act'(z), and its column sums over the rows of a block: 32 vectors of columns x 8 rows of threads.
+// dz = dy act'(z), and its column sums over the rows of a block: 32 vectors of columns x 8 rows of threads.  Bound by memory:
+// 524309 x 256 in bf16 0.15 ms, 5.3 TB/s.
 struct SlopeArgs {
   long long rows;
   const int* nrows;
@@ -932,7 +939,8 @@ __device__ __forceinline__ Slab slab_rows(const WeightArgs& g, long long rows, i
   const long long r0 = min((long long)slab * per, rows);
   return {r0, min(r0 + per, rows)};
 }
-// Tiles of dW: 64 kI x 32 kWaves, as above; every tile of a slab loads the slab's rows, so that wide ones load less.
+// Tiles of dW: 64 kI x 32 kWaves, as above; every tile of a slab loads the slab's rows, so that wide ones load less.  Measured:
+// 524309 rows, 768 x 256 in bf16 0.33 ms (620 TFLOP/s); 474011 rows, 384 x 128, kept rows times fp32 ones 0.35 ms.
 template <class EA, class EB, int kWaves>
 struct WeightShape {
   static constexpr int KS = EB::kPieces == 1 ? 64 : 32, kI = EB::kPieces == 1 ? kWaves / 2 : 2;
@@ -1108,7 +1116,8 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, 
 }
 
 // Eight waves where they compute no more columns than four would: N is at least 129, and its last tile of 256 is more than half
-// full.
+// full (200000 rows, fp32, 256 -> 384: 316 us by four waves, 391 by eight; 256 -> 512: 404 and 387; weight gradients 416 and
+// 375 for 512, 240 and 220 for 256).
 bool eight_waves(int N) { return (N + 255) / 256 * 256 == (N + 127) / 128 * 128; }
 // For weight gradients; bf16 with a ReLU mask holds more of a step's rows than the registers of eight waves have room for.
 bool eight_weight_waves(int N, bool bf16, bool relu) { return eight_waves(N) && !(bf16 && relu); }
@@ -1141,8 +1150,9 @@ hipError_t product_tiles(const ProductArgs& g, long long rows, int n_cu, long lo
   hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles < most ? tiles : most) + 7) / 8 * 8), dim3(64 * kWaves), Shape::kLds * 16, s, g, few);
   return hipGetLastError();
 }
-// Up to `few` 32 x 32 tiles, each gets a workgroup: two rounds of two workgroups per CU.  Where only the device knows the
-// rows both kernels are launched, and one of them leaves at once.
+// Up to `few` 32 x 32 tiles, each gets a workgroup: two rounds of two workgroups per CU (2048 x 256 -> 256 in fp32 9.9 us, by
+// the larger tiles 28.3; 4096 rows 17.7 and 28.8; 8192 rows 31.5 and 29.8).  Where only the device knows the rows both
+// kernels are launched, and one of them leaves at once.
 template <class E, bool kDz, bool kColsB>
 hipError_t product(const ProductArgs& g, long long rows, int n_cu, hipStream_t s) {
   const bool narrow = g.a.d < 8 || g.N < 4;            // less than a vector of the tiles' loads
@@ -1150,11 +1160,15 @@ hipError_t product(const ProductArgs& g, long long rows, int n_cu, hipStream_t s
   const long long few = narrow ? (1LL << 62) : 4 * n_cu;
   if (small <= few || g.nrows) {
     const dim3 grid((unsigned)(small < 4 * n_cu ? small : 4 * n_cu));
-    if (g.a.d % 8 == 0) hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, true>), grid, dim3(kThreads), 0, s, g, few);
+    if (g.a.d >= 8) hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, true>), grid, dim3(kThreads), 0, s, g, few);
     else hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, false>), grid, dim3(kThreads), 0, s, g, few);
   }
-  if (small > few) return eight_waves(g.N) ? product_tiles<E, kDz, kColsB, 8>(g, rows, n_cu, few, s) : product_tiles<E, kDz, kColsB, 4>(g, rows, n_cu, few, s);
-  return hipGetLastError();
+  if (small <= few) return hipGetLastError();
+  // eight waves where every CU gets a few of their tiles (2000003 x 768 -> 256 in bf16 1.24 ms, by four waves 1.33; 16384 x 256
+  // -> 256 18.1 us, by four 14.6)
+  typedef ProductShape<E, 8> Wide;
+  const bool wide = eight_waves(g.N) && (rows + Wide::kTileM - 1) / Wide::kTileM * ((g.N + Wide::kTileN - 1) / Wide::kTileN) >= 4 * n_cu;
+  return wide ? product_tiles<E, kDz, kColsB, 8>(g, rows, n_cu, few, s) : product_tiles<E, kDz, kColsB, 4>(g, rows, n_cu, few, s);
 }
 
 template <class E>
