@@ -709,7 +709,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
 }
 
 // rows x N outputs, contraction over K columns of a.  Tiles of 64 kI rows x 32 kWaves columns, waves of 32 kI x 64: two
-// side by side in rows, the others in columns.
+// side by side in rows, the others in columns.  kShort: of half the rows.
 // What bounds it is how much is requested at a time: a step's loads (64 KB per CU) are on their way while the step before is
 // multiplied, some 2 us, so that every byte loaded twice shows.  Eight waves take 256 columns, and the rows of a layer of
 // that width are read once; LDS then holds two steps, and a step needs one barrier.  The residual's rows are requested 32 at a
@@ -717,17 +717,17 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
 // Measured: bf16 2000003 x 768 -> 256 with residual 1.25 ms (4.1 TB/s, 630 TFLOP/s; library product alone 0.97 ms); fp32
 // 196311 x 201 -> 139 with GELU, residual and Z 0.212 ms (matrix cores 25 % busy; the rest is conversions, the
 // epilogue's instructions and waiting); dX of 524309 x 256 -> 768 in bf16 0.42 ms.
-template <class E, int kWaves>
+template <class E, int kWaves, bool kShort>
 struct ProductShape {
-  static constexpr int kI = E::kPieces == 1 ? 4 : 2, kTileM = 64 * kI, kTileN = 32 * kWaves, KS = E::kPieces == 1 ? 64 : 32;
+  static constexpr int kI = (E::kPieces == 1 ? 4 : 2) / (kShort ? 2 : 1), kTileM = 64 * kI, kTileN = 32 * kWaves, KS = E::kPieces == 1 ? 64 : 32;
   static constexpr int kUnitsA = E::kPieces * kTileM * KS / 8, kUnitsB = E::kPieces * kTileN * KS / 8, kBuffers = kWaves / 4;
   static constexpr int kLd = 68, kEnd = kWaves * 32 * kLd / 4;                    // of a wave's 32 x 64 sums, in units
   static constexpr int kStep = kUnitsA + kUnitsB, kLds = kBuffers * kStep > kEnd ? kBuffers * kStep : kEnd;
 };
-template <class E, bool kDz, bool kColsB, int kWaves>
+template <class E, bool kDz, bool kColsB, int kWaves, bool kShort>
 __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductArgs g, long long few) {
   if (g.stop && g.stop[0] != 0) return;
-  typedef ProductShape<E, kWaves> Shape;
+  typedef ProductShape<E, kWaves, kShort> Shape;
   constexpr int kP = E::kPieces, KS = Shape::KS, kI = Shape::kI, kTileM = Shape::kTileM, kTileN = Shape::kTileN, kW = 16 / E::kBytes, kLd = Shape::kLd;
   extern __shared__ u32x4 lds[];
   const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
@@ -1140,11 +1140,11 @@ template <class K>
 hipError_t allow_lds(K kernel, size_t bytes) {
   return bytes > 64 * 1024 ? hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : hipSuccess;
 }
-template <class E, bool kDz, bool kColsB, int kWaves>
+template <class E, bool kDz, bool kColsB, int kWaves, bool kShort>
 hipError_t product_tiles(const ProductArgs& g, long long rows, int n_cu, long long few, hipStream_t s) {
-  typedef ProductShape<E, kWaves> Shape;
-  const long long most = (long long)n_cu * 8 / kWaves, tiles = (rows + Shape::kTileM - 1) / Shape::kTileM * ((g.N + Shape::kTileN - 1) / Shape::kTileN);
-  auto kernel = product_kernel<E, kDz, kColsB, kWaves>;
+  typedef ProductShape<E, kWaves, kShort> Shape;
+  const long long most = (long long)n_cu * 8 / kWaves * (kShort ? 2 : 1), tiles = (rows + Shape::kTileM - 1) / Shape::kTileM * ((g.N + Shape::kTileN - 1) / Shape::kTileN);
+  auto kernel = product_kernel<E, kDz, kColsB, kWaves, kShort>;
   const hipError_t e = allow_lds(kernel, Shape::kLds * 16);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles < most ? tiles : most) + 7) / 8 * 8), dim3(64 * kWaves), Shape::kLds * 16, s, g, few);
@@ -1164,11 +1164,15 @@ hipError_t product(const ProductArgs& g, long long rows, int n_cu, hipStream_t s
     else hipLaunchKernelGGL((few_rows_kernel<E, kDz, kColsB, false>), grid, dim3(kThreads), 0, s, g, few);
   }
   if (small <= few) return hipGetLastError();
-  // eight waves where every CU gets a few of their tiles (2000003 x 768 -> 256 in bf16 1.24 ms, by four waves 1.33; 16384 x 256
-  // -> 256 18.1 us, by four 14.6)
-  typedef ProductShape<E, 8> Wide;
-  const bool wide = eight_waves(g.N) && (rows + Wide::kTileM - 1) / Wide::kTileM * ((g.N + Wide::kTileN - 1) / Wide::kTileN) >= 4 * n_cu;
-  return wide ? product_tiles<E, kDz, kColsB, 8>(g, rows, n_cu, few, s) : product_tiles<E, kDz, kColsB, 4>(g, rows, n_cu, few, s);
+  // Eight waves where every CU gets a few of their tiles (2000003 x 768 -> 256 in bf16 1.24 ms, by four waves 1.33; 16384 x 256
+  // -> 256 18.1 us, by four 14.6); of four waves, tiles of half the rows where those would not fill the CUs (16384 x 256 -> 256
+  // in bf16 14.7 and 10.6 us; 9000 x 512 -> 256 in fp32 43 and 35; beyond, 60000 x 256 -> 128 in fp32 35 and 43).
+  auto tiles = [&](int m, int n) { return (rows + m - 1) / m * ((g.N + n - 1) / n); };
+  typedef ProductShape<E, 8, false> Wide;
+  typedef ProductShape<E, 4, false> Tall;
+  if (eight_waves(g.N) && tiles(Wide::kTileM, Wide::kTileN) >= 4 * n_cu) return product_tiles<E, kDz, kColsB, 8, false>(g, rows, n_cu, few, s);
+  return tiles(Tall::kTileM, Tall::kTileN) > (E::kPieces > 1 ? n_cu : 2 * n_cu) ? product_tiles<E, kDz, kColsB, 4, false>(g, rows, n_cu, few, s)
+                                                                             : product_tiles<E, kDz, kColsB, 4, true>(g, rows, n_cu, few, s);
 }
 
 template <class E>

@@ -169,6 +169,15 @@ def test_dense_of_many_rows(ev, dtype, shape):
     test_dense(ev, dtype, shape, ["silu", "none", "relu", "gelu"][(shape[0] + shape[2]) % 4])
 
 
+# Four of the largest tiles per CU, and between one and two of the next.
+@pytest.mark.parametrize("dtype,shape", [("f32", (131200, 17, 139)), ("f32", (131100, 40, 130)), ("bf16", (262500, 9, 139)), ("bf16", (262300, 70, 130)),
+                                         ("f32", (33100, 40, 70)), ("f32", (17000, 33, 129)), ("bf16", (132000, 40, 70)), ("bf16", (70000, 70, 129))])
+def test_dense_of_the_most_rows(B, ev, dtype, shape):
+    rows, K, N = shape
+    test_dense(ev, dtype, shape, "silu" if K % 2 else "relu")
+    test_dense_backward(B, ev, dtype, (rows, N, K), "relu", K % 2 == 0)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("ld,first", [(3, 1), (8, 8)])
 @pytest.mark.parametrize("shape", [(9000, 72, 131), (4600, 33, 250)])
