@@ -705,6 +705,46 @@ def test_graph_norm_gradients_of_many_long_graphs_repeat(ev, dtype):
         assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
+def test_offsets_beyond_32_bits(ev):
+    """Arrays of more than 4 GiB: the last rows against 64 bits, everything that is summed over all rows too."""
+    rows, C, G, per = 8_600_000, 128, 4, 1000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(rows, C, generator=g, device="cuda")
+    w = torch.randn(C, C, generator=g, device="cuda") / math.sqrt(C)
+    last = slice(rows - per, rows)
+    tail, wc = x[last].cpu(), w.cpu()
+    y = ev.dense(x, w, act="silu")
+    _, _, want, tol = dense_reference(tail, wc, None, None, "silu", torch.float32)
+    close(y[last], want, tol, "dense")
+    # gradients: y serves as dy
+    dx, dw, db = ev.dense_backward(y, x, w)
+    dy = y[last].cpu()
+    (rx, tx), _, _ = backward_reference(dy, tail, wc, None, "none", torch.float32)
+    close(dx[last], rx, tx, "dx")
+    del dx
+    rw, aw, rb, ab = (torch.zeros(s, dtype=torch.float64, device="cuda") for s in ((C, C), (C, C), (C,), (C,)))
+    for lo in range(0, rows, 1_000_000):
+        a, d = x[lo:lo + 1_000_000].double(), y[lo:lo + 1_000_000].double()
+        rw += a.t().contiguous() @ d
+        aw += a.abs().t().contiguous() @ d.abs()
+        rb += d.sum(0)
+        ab += d.abs().sum(0)
+    sections = 3 * 96 + rows // (64 * 128) + 4              # of a slab, of which there are at least 128 here
+    close(dw, rw.cpu(), (sections * U * aw + 2 * U * rw.abs()).cpu(), "dw")
+    close(db, rb.cpu(), (4 * U * ab).cpu(), "db")
+    # norms of graphs of 1000 rows, then rows in 8 bits
+    off = torch.arange(0, rows + 1, per, dtype=torch.int32, device="cuda")
+    out, mean, rstd = ev.graph_norm(x, off, G, eps=EPS, act="silu", out=y)
+    one = torch.ones(C), torch.zeros(C)
+    check_norm(ev, tail, [per], G, *one, "silu", "f32", (out[last], mean[-1:], rstd[-1:]))
+    ref = norm_back_reference(tail, tail, None, [per], G, *one, mean[-1:].cpu(), rstd[-1:].cpu(), "silu", torch.float32)
+    back = ev.graph_norm_backward(x, x, off, G, None, None, mean, rstd, "silu", out=y)
+    close((back[0] if isinstance(back, tuple) else back)[last], *ref[0][:2], "dx of the norm")
+    kept = ev.keep_rows(x)
+    ev.restore_rows(kept, out=y)
+    assert torch.equal(y[last], ev.restore_rows(ev.keep_rows(x[last])))
+
+
 # ---------------------------------------------------------------------------
 # refusals
 # ---------------------------------------------------------------------------
