@@ -511,7 +511,7 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
 /* Norm over the rows of each graph (a group norm whose positions are the rows of a graph), with an activation.  The
  * channels are in `groups` groups of channels / groups neighbours; per graph and group, over its rows and channels:
  *   mean, rstd = 1 / sqrt(variance + eps);  y = act(gamma (x - mean) rstd + beta)
- * A graph without rows has mean 0 and variance 0.  Rows of no graph (before node_off[0], behind node_off[n_graphs]) are
+ * Both are returned rounded to fp32; y takes the mean as it was before.  A graph without rows has mean 0 and variance 0.  Rows of no graph (before node_off[0], behind node_off[n_graphs]) are
  * neither read nor written.  Rows are at most 2^17 elements apart here.  A graph whose offsets do not ascend within
  * [0, rows] is left alone, and dc_check reports DC_ERR_BAD_GRAPH.  The same call gives the same bits.               */
 typedef struct {

@@ -7,9 +7,13 @@
 //
 // Bound by memory, x read once and y written once: a workgroup takes a graph (or a slab of its channels, whole groups and
 // whole cache lines), holds its rows in LDS between the sums and the second pass and reads again only what
-// does not fit.  Sums are formed in 64 bits (v as mean x^2 - mu^2: exact enough for any offset that fp32 values can
-// have next to their spread), three instructions a value, which the loads hide.
-// Measured: forward over 4096 graphs of 1390 rows, 256 channels in bf16, SiLU, 1.385 ms (4.2 TB/s; a copy 4.87); gradient over
+// does not fit.  The forward's sums are formed in 64 bits, of x - x0 and its square, x0 the first value of the graph's group:
+//   mu = x0 + mean (x - x0),  v = mean (x - x0)^2 - (mean (x - x0))^2
+// Of x itself the two terms of v would be up to 2^46 times v (values may lie 2^23 times their spread from zero), and their
+// rounding some percent of it.  Four instructions a value, which the loads hide.  mu is taken in two parts, the fp32 number that
+// is returned and what it lacks, else a value next to mu would be off by mu's rounding; the second pass has two instructions a
+// value in front of the activation: (gamma r) (x - mu) + (beta - (gamma r) lacks).
+// Measured: forward over 4096 graphs of 1390 rows, 256 channels in bf16, SiLU, 1.395 ms (4.2 TB/s; a copy 4.87); gradient over
 // 52901 graphs of 9 rows, 256 channels in fp32, x as kept rows, 0.351 ms (3.1 TB/s).
 // Graphs of more than long_rows rows would keep one workgroup busy while the others are done: the kernel of the short graphs
 // only lists them, and their rows are dealt in chunks, counted from each graph's first row, to three kernels (sums of a chunk;
@@ -58,7 +62,7 @@ struct Norm {
   int2* longs;             // [most_longs] graph and its first chunk, ascending in the chunks
   int most_longs, most_chunks; // offsets that ascend do not give more; what others give beyond is left out
   double2* part;           // [chunks][G] sums of a chunk
-  float2* means;           // [long graphs][G] s1, s2 (backward)
+  float2* means;           // [long graphs][G] s1, s2; forward: what the mean lacks
   float* cols;             // [column blocks][2 C] parts of dgamma | dbeta
   int col_block0;          // first column block of this launch
 };
@@ -154,14 +158,20 @@ __device__ __forceinline__ void slope(float (&dy)[kV], const float (&xh)[kV], co
   for (int k = 0; k < kV; ++k) dy[k] *= z[k];
 }
 
+// What the sums of a group are counted from: its first value in row `row`, or zero if that is not finite.
+template <typename T>
+__device__ __forceinline__ double origin(const GraphNormArgs& a, long long row, int channel) {
+  const float x = widen(static_cast<const T*>(a.X)[row * a.ldx + channel]);
+  return __builtin_isfinite(x) ? (double)x : 0.0;
+}
 // What a row's vector adds to the two sums.
 template <bool kBack, int kV>
-__device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x)[kV], float (&dy)[kV], float mu, float r,
+__device__ __forceinline__ void add_sums(double& s1, double& s2, const float (&x)[kV], float (&dy)[kV], double x0, float mu, float r,
                                          const Affine<kV>& f, int act, float (&dg)[kV], float (&db)[kV]) {
   if constexpr (!kBack) {
 #pragma unroll
     for (int k = 0; k < kV; ++k) {
-      const double d = (double)x[k];
+      const double d = (double)x[k] - x0;
       s1 += d;
       s2 = fma(d, d, s2);
     }
@@ -226,28 +236,40 @@ __device__ __forceinline__ void group_sums(double& s1, double& s2, double2* red,
   s2 = v.y;
 }
 
-// mean and 1 / sqrt(variance + eps) from the sums of x and x^2 over m values.
-__device__ __forceinline__ void statistics(double s1, double s2, double m, float eps, float& mu, float& rs) {
-  const double mean = m > 0 ? s1 / m : 0.0, var = m > 0 ? s2 / m - mean * mean : 0.0;
+// mean (and what its fp32 value lacks) and 1 / sqrt(variance + eps) from the sums of x - x0 and (x - x0)^2 over m values.
+__device__ __forceinline__ void statistics(double s1, double s2, double m, double x0, float eps, float& mu, float& lacks, float& rs) {
+  const double from = m > 0 ? s1 / m : 0.0, var = m > 0 ? s2 / m - from * from : 0.0, mean = x0 + from;
   mu = (float)mean;
+  lacks = (float)(mean - (double)mu);
   rs = (float)(1.0 / sqrt((var > 0.0 ? var : (var != var ? var : 0.0)) + (double)eps));
 }
 
-// The second pass of one vector.
+// What x - mu (mu as fp32) takes in the forward's second pass.
+template <int kV>
+__device__ __forceinline__ Affine<kV> of_graph(const Affine<kV>& f, float r, float lacks) {
+  Affine<kV> h;
+#pragma unroll
+  for (int k = 0; k < kV; ++k) {
+    h.gamma[k] = f.gamma[k] * r;
+    h.beta[k] = fmaf(-lacks, h.gamma[k], f.beta[k]);
+  }
+  return h;
+}
+// The second pass of one vector.  Forward: f is of_graph's, r, s1 and s2 are not taken.
 template <typename T, int kV, bool kBack>
 __device__ __forceinline__ void finish(int act, const Places& p, const float (&x)[kV], float (&dy)[kV], unsigned row, int c, float mu, float r, float s1,
                                        float s2, const Affine<kV>& f) {
   Vec<T, kV> o;
   float xh[kV];
-#pragma unroll
-  for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
   if constexpr (!kBack) {
 #pragma unroll
-    for (int k = 0; k < kV; ++k) xh[k] = fmaf(f.gamma[k], xh[k], f.beta[k]);
+    for (int k = 0; k < kV; ++k) xh[k] = fmaf(f.gamma[k], x[k] - mu, f.beta[k]);
     activate<kV>(xh, act);
 #pragma unroll
     for (int k = 0; k < kV; ++k) narrow(xh[k], o.v[k]);
   } else {
+#pragma unroll
+    for (int k = 0; k < kV; ++k) xh[k] = (x[k] - mu) * r;
     slope<kV>(dy, xh, f, act);
     Vec<T, kV> add{};
     if (p.res) add = *reinterpret_cast<const Vec<T, kV>*>(p.res + (__umul24(row, p.ldres) + (unsigned)(c * (int)sizeof(T))));
@@ -362,7 +384,8 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       mu = n.a.mean[(size_t)g * n.a.G + group];
       rs = n.a.rstd[(size_t)g * n.a.G + group];
     }
-    double s1 = 0.0, s2 = 0.0;
+    double s1 = 0.0, s2 = 0.0, x0 = 0.0;
+    if (!kBack && r.hi > r.lo) x0 = origin<T>(n.a, r.lo, group * n.cg);
     float dg[kV], db[kV];
 #pragma unroll
     for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
@@ -375,11 +398,11 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       }
       float x[kV], dy[kV];
       open<T, X, kV, kBack>(x, dy, h);
-      add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+      add_sums<kBack, kV>(s1, s2, x, dy, x0, mu, rs, f, n.a.act, dg, db);
     });
     group_sums(s1, s2, red, n.lanes, used, gv);
     if constexpr (!kBack) {
-      statistics(s1, s2, m, n.a.eps, mu, rs);
+      statistics(s1, s2, m, x0, n.a.eps, mu, s1f, rs);
       if (in && rl == 0 && lane % gv == 0) {
         n.a.mean[(size_t)g * n.a.G + group] = mu;
         n.a.rstd[(size_t)g * n.a.G + group] = rs;
@@ -393,10 +416,11 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
         dbs[k] += (double)db[k];
       }
     }
+    const Affine<kV> fg = kBack ? f : of_graph(f, rs, s1f);
     auto second = [&](const Item& h, int i) {
       float x[kV], dy[kV];
       open<T, X, kV, kBack>(x, dy, h);
-      finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s1f, s2f, f);
+      finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s1f, s2f, fg);
     };
     const int here = min(count, n.held);
 #pragma unroll 2
@@ -444,6 +468,7 @@ __global__ __launch_bounds__(256) void order_longs_kernel(const Norm n, int2* __
 
 struct Segment {
   int entry, g;            // place in the list, graph
+  long long first;         // its first row
   long long lo, hi;        // rows of the chunk
 };
 // The long graph of a chunk: the last entry whose first chunk is not behind it, found 64 entries at a time.
@@ -462,6 +487,7 @@ __device__ __forceinline__ Segment segment_of(const Norm& n, int nlong, int chun
   const int2 e = n.longs[lo];
   s.g = e.x;
   const long long first = n.a.node_off[e.x], end = n.a.node_off[e.x + 1];
+  s.first = first;
   s.lo = first + (long long)(chunk - e.y) * n.chunk_rows;
   s.hi = s.lo + n.chunk_rows < end ? s.lo + n.chunk_rows : end;
   // offsets that do not ascend can fill the list with more than it holds, and then a chunk's entry is not its graph
@@ -494,7 +520,8 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
         mu = n.a.mean[(size_t)seg.g * n.a.G + group];
         rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
       }
-      double s1 = 0.0, s2 = 0.0;
+      double s1 = 0.0, s2 = 0.0, x0 = 0.0;
+      if (!kBack) x0 = origin<T>(n.a, seg.first, group * n.cg);
       float dg[kV], db[kV];
 #pragma unroll
       for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
@@ -503,7 +530,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
       each_row<T, X, kV, kBack, 4>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
-        add_sums<kBack, kV>(s1, s2, x, dy, mu, rs, f, n.a.act, dg, db);
+        add_sums<kBack, kV>(s1, s2, x, dy, x0, mu, rs, f, n.a.act, dg, db);
       });
       group_sums(s1, s2, red, n.lanes, used, gv);
       if (in && rl == 0 && lane % gv == 0) n.part[(size_t)chunk * n.a.G + group] = make_double2(s1, s2);
@@ -518,14 +545,14 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
 
 // The sums of a long graph from its chunks': a wave each, `wide` (a power of two, at least the groups or 64) lanes side by side
 // over the groups, the others over the chunks.
-template <bool kBack>
+template <typename T, bool kBack>
 __global__ __launch_bounds__(64) void long_sums_kernel(const Norm n, int wide) {
   if (n.a.stop && n.a.stop[0] != 0) return;
   const int nlong = (int)min((unsigned)(n.found[0] >> 32), (unsigned)n.most_longs), lane = threadIdx.x, q0 = lane & (wide - 1), k0 = lane / wide;
   for (int i = blockIdx.x; i < nlong; i += gridDim.x) {
     const int2 e = n.longs[i];
-    const long long rows = (long long)n.a.node_off[e.x + 1] - n.a.node_off[e.x];
-    if (rows <= n.long_rows || e.y < 0) continue;
+    const long long first = n.a.node_off[e.x], rows = (long long)n.a.node_off[e.x + 1] - first;
+    if (rows <= n.long_rows || first < 0 || first + rows > n.a.rows || e.y < 0) continue;
     const int chunks = (int)min((rows + n.chunk_rows - 1) / n.chunk_rows, (long long)n.most_chunks - e.y);
     const double m = (double)rows * n.cg;
     for (int q = q0; q < n.a.G + q0; q += wide) {       // the same number of rounds for every lane
@@ -544,8 +571,9 @@ __global__ __launch_bounds__(64) void long_sums_kernel(const Norm n, int wide) {
       if (kBack) {
         n.means[(size_t)i * n.a.G + q] = make_float2((float)(s1 / m), (float)(s2 / m));
       } else {
-        float mu, rs;
-        statistics(s1, s2, m, n.a.eps, mu, rs);
+        float mu, lacks, rs;
+        statistics(s1, s2, m, origin<T>(n.a, first, q * n.cg), n.a.eps, mu, lacks, rs);
+        n.means[(size_t)i * n.a.G + q] = make_float2(lacks, 0.f);
         n.a.mean[(size_t)e.x * n.a.G + q] = mu;
         n.a.rstd[(size_t)e.x * n.a.G + q] = rs;
       }
@@ -568,13 +596,14 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_finish_kernel(const Norm 
       const Segment seg = segment_of(n, nlong, chunk);
       if (seg.lo >= seg.hi) continue;
       const float mu = n.a.mean[(size_t)seg.g * n.a.G + group], rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
-      const float2 s = kBack ? n.means[(size_t)seg.entry * n.a.G + group] : make_float2(0.f, 0.f);
+      const float2 s = n.means[(size_t)seg.entry * n.a.G + group];
+      const Affine<kV> fg = kBack ? f : of_graph(f, rs, s.x);
       const Places at = places_of<T, X, kBack>(n.a, seg.lo);
       const int rows = (int)(seg.hi - seg.lo), count = in && rl < rows ? (rows - rl + step - 1) / step : 0;
       each_row<T, X, kV, kBack, 4>(at, rl, step, 0, count, c, [&](const Two<T, X, kV>& h, int i) {
         float x[kV], dy[kV];
         open<T, X, kV, kBack>(x, dy, h);
-        finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s.x, s.y, f);
+        finish<T, kV, kBack>(n.a.act, at, x, dy, (unsigned)(rl + i * step), c, mu, rs, s.x, s.y, fg);
       });
     }
 }
@@ -729,8 +758,8 @@ hipError_t run(Norm n, hipStream_t s) {
     n.most_chunks = (int)(n.a.rows / n.chunk_rows + (long long)longs);
     w += (size_t)n.most_chunks * n.a.G * sizeof(double2);
     n.means = reinterpret_cast<float2*>(w);
+    w += longs * n.a.G * sizeof(float2);
     if (kBack) {
-      w += longs * n.a.G * sizeof(float2);
       ordered = reinterpret_cast<int2*>(w);
       w += longs * sizeof(int2);
     }
@@ -754,7 +783,7 @@ hipError_t run(Norm n, hipStream_t s) {
     hipLaunchKernelGGL((chunk_sums_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
     const long long longs = n.a.rows / p.long_rows + 1, most = 4LL * n.a.n_cu;
     const int wide = n.a.G < 64 ? pow2_at_least(n.a.G) : 64;
-    hipLaunchKernelGGL((long_sums_kernel<kBack>), dim3((unsigned)(longs < most ? longs : most)), dim3(64), 0, s, n, wide);
+    hipLaunchKernelGGL((long_sums_kernel<T, kBack>), dim3((unsigned)(longs < most ? longs : most)), dim3(64), 0, s, n, wide);
     hipLaunchKernelGGL((chunk_finish_kernel<T, X, kV, kBack>), cgrid, dim3(kChunkThreads), 0, s, n);
   }
   if (kBack && n.a.dgamma)
@@ -799,9 +828,9 @@ size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backwar
   const long long most = blocks_most(64, n_cu), by_rows = rows / 512 + 1, per_cu = 4LL * n_cu + n_cu / 16 + 2, nc = by_rows > per_cu ? by_rows : per_cu;
   const bool chunks = rows > 1024;
   const size_t longs = chunks ? (size_t)(rows / 1024) + 1 : 0;
-  size_t b = chunks ? 16 + (longs * sizeof(int2) + 15) / 16 * 16 + ((size_t)nc + longs) * G * sizeof(double2) : 0;
+  size_t b = chunks ? 16 + (longs * sizeof(int2) + 15) / 16 * 16 + ((size_t)nc + longs) * G * sizeof(double2) + longs * G * sizeof(float2) : 0;
   if (backward) {
-    b += longs * (G * sizeof(float2) + sizeof(int2));
+    b += longs * sizeof(int2);
     b += (size_t)((n_graphs < most ? (n_graphs > 0 ? n_graphs : 1) : most) + (chunks ? (nc < most ? nc : most) : 0)) * 2 * C * sizeof(float);
   }
   return b;

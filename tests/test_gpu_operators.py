@@ -463,6 +463,60 @@ def test_graph_norm_large_offset(ev, dtype):
     assert not got[0][700:703, :8].any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset,spread", [(1e5, 1.0), (1e6, 0.1), (1e7, 1.0), (-1e8, 8.0)])
+@pytest.mark.parametrize("sizes", [[9] * 300 + [0, 1, 40], [300, 700, 2, 1000], [5000, 3, 9000]], ids=["waves", "held", "chunks"])
+def test_graph_norm_far_from_zero(ev, dtype, offset, spread, sizes):
+    """Values that lie up to 2^23 times their spread from zero, and a group that is constant: the statistics and the result
+    are off by roundings of their own size, whatever the offset."""
+    C, G, t = 32, 4, TYPES[dtype]
+    x = (offset * (1 + 1e-8 * rand(6, C)) + spread * rand(5, sum(sizes), C)).to(t)
+    x[:, 8:16] = 123456.7
+    gamma, beta = (1 + 0.2 * rand(7, C)).float(), (0.2 * rand(8, C)).float()
+    xd, off = x.cuda(), offsets(sizes)
+    y, mean, rstd = ev.graph_norm(xd, off, G, gamma.cuda(), beta.cuda(), EPS, "silu")
+    mu, var = norm_statistics(x, sizes, G)
+    rs = 1 / torch.sqrt(var + EPS)
+    # 64-bit sums over m values, counted from the first one, x0: m roundings of 2^-53 of their size at most
+    first = torch.tensor(np.minimum(np.concatenate([[0], np.cumsum(sizes)])[:-1], sum(sizes) - 1))
+    far = var + (x[first][:, ::C // G].double() - mu) ** 2
+    sums = 4 * max(sizes) * (C // G) * 2.0 ** -53 * far
+    filled = torch.tensor([n > 0 for n in sizes])[:, None]
+    mu, far, sums = (torch.where(filled, v, torch.zeros_like(v)) for v in (mu, far, sums))
+    close(mean, mu, 1.01 * U * mu.abs() + torch.sqrt(sums * 2.0 ** -53), "mean")
+    close(rstd, rs, 2 * U * rs + rs * sums / (var + EPS), "rstd")
+    m, r = per_row(mu, sizes, C), per_row(rs, sizes, C)
+    d = x.double() - m
+    z = gamma.double() * d * r + beta.double()
+    # x - mu: two roundings of its size, and mu's second part, rounded once
+    ez = gamma.double().abs() * r * (8 * U * d.abs() + 4 * U * U * m.abs()) + 2 * U * (z.abs() + beta.double().abs())
+    ez = ez + (gamma.double() * d * r).abs() * per_row(sums / (var + EPS), sizes, C)
+    want = act(z, "silu")
+    close(y, want, 1.13 * ez + 8 * U * z.abs() + (R(t) + U) * want.abs(), "y")
+    assert (rstd[:, 1] == rstd[0, 1]).all() and (mean[filled[:, 0].cuda(), 1] == x[0, 8].float().item()).all()
+    again = ev.graph_norm(xd, off, G, gamma.cuda(), beta.cuda(), EPS, "silu", out=xd)
+    assert all(torch.equal(a, b) for a, b in zip(again, (y, mean, rstd)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_graph_norm_of_what_is_not_finite(ev, dtype, bad):
+    """A value that is not finite, a graph's first one among them, reaches its graph and group and nothing else."""
+    s, C, G = [9, 40, 5000, 7], 32, 4
+    x = rand(3, sum(s), C).to(TYPES[dtype])
+    hit = [(0, 0, 0), (9, 1, 8), (30, 1, 16), (49, 2, 0), (4000, 2, 24)]           # row, graph, column
+    for row, _, col in hit:
+        x[row, col] = bad
+    y, mean, rstd = ev.graph_norm(x.cuda(), offsets(s), G, None, None, EPS)
+    lost = torch.zeros(len(s), G, dtype=torch.bool)
+    for _, g, col in hit:
+        lost[g, col // (C // G)] = True
+    want = torch.tensor(bad).expand(int(lost.sum()))
+    assert torch.equal(mean.cpu()[lost].nan_to_num(nan=7.0), want.nan_to_num(nan=7.0)) and torch.isnan(rstd.cpu()[lost]).all()
+    assert torch.isfinite(mean.cpu()[~lost]).all() and torch.isfinite(rstd.cpu()[~lost]).all()
+    assert torch.equal(torch.isnan(y).cpu(), per_row(lost, s, C))
+
+
 def norm_back_reference(x, dy, dres, sizes, G, gamma, beta, mean, rstd, name, t):
     C = x.shape[1]
     g, b = gamma.double(), beta.double()
