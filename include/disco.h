@@ -178,7 +178,8 @@ dc_status dc_set_attention_weights(dc_ctx* ctx, const float* W_layers, const flo
  * may differ in its last bits with the batch that it is part of.
  *   groups  groups of neighbouring columns, a divisor of H; 0 returns to ReLU layers (the others are not read then)
  *   act     dc_activation;  eps > 0;  gamma, beta: host fp32, concat over l = 1 .. L - 1 of [H]
- * Allocates; ends training (dc_train_begin has to be called again).                                                  */
+ * Allocates and synchronises the device: the next call may be made on any stream.  Ends training (dc_train_begin has to be
+ * called again).                                                                                                      */
 dc_status dc_set_layer_norms(dc_ctx* ctx, int32_t groups, int32_t act, float eps, const float* gamma, const float* beta,
                              void* stream);
 /* Copies gamma and beta as they are now to host arrays.  Synchronises `stream`. */

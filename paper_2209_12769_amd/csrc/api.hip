@@ -622,11 +622,11 @@ static void refresh_pieces(dc_ctx* ctx, hipStream_t s) {
   launch_pack_split(jobs, n, s);
 }
 
-// The layer matrices of a deep bf16 estimator row by row.
-static void refresh_row_major(dc_ctx* ctx, hipStream_t s) {
+// The layer matrices of a deep bf16 estimator row by row, to LayerNorms::W.
+static void refresh_row_major(dc_ctx* ctx, const void* W, hipStream_t s) {
   if (ctx->cfg.dtype != DC_BF16 || !ctx->have_weights_copied) return;
   launch_row_major(static_cast<const unsigned short*>(ctx->W), (long long)packed_weight_elems(ctx->cfg.F, ctx->cfg.H, ctx->cfg.L, 3), ctx->cfg.H,
-                   static_cast<unsigned short*>(const_cast<void*>(ctx->norms.W)), s);
+                   static_cast<unsigned short*>(const_cast<void*>(W)), s);
 }
 
 static dc_status set_weights_common(dc_ctx* ctx, const float* W_layers, const float* att, const float* b_layers,
@@ -674,7 +674,7 @@ static dc_status set_weights_common(dc_ctx* ctx, const float* W_layers, const fl
     e = hipMemcpyAsync(ctx->Wx, wx.data(), wx.size() * sizeof(unsigned short), hipMemcpyHostToDevice, s);
   }
   if (e == hipSuccess) refresh_pieces(ctx, s);
-  if (e == hipSuccess && ctx->deep) refresh_row_major(ctx, s);
+  if (e == hipSuccess && ctx->deep) refresh_row_major(ctx, ctx->norms.W, s);
   if (e == hipSuccess) e = hipGetLastError();
   if (e == hipSuccess) e = hipStreamSynchronize(s);   // host staging buffers die at return
   if (e != hipSuccess) return hip_fail(ctx, e, "weight copy");
@@ -1610,7 +1610,9 @@ dc_status dc_set_layer_norms(dc_ctx* ctx, int32_t groups, int32_t act, float eps
       e = hipMemcpyAsync(const_cast<float*>(n.gamma), gamma, inner * H * sizeof(float), hipMemcpyHostToDevice, s);
       if (e == hipSuccess) e = hipMemcpyAsync(const_cast<float*>(n.beta), beta, inner * H * sizeof(float), hipMemcpyHostToDevice, s);
     }
-    if (e == hipSuccess) e = hipStreamSynchronize(s);
+    if (e == hipSuccess) refresh_row_major(ctx, n.W, s);
+    if (e == hipSuccess) e = hipGetLastError();
+    if (e == hipSuccess) e = hipStreamSynchronize(s);   // host arrays, and the next call may come on another stream
     if (e != hipSuccess) {
       (void)hipFree(mem);
       return hip_fail(ctx, e, "dc_set_layer_norms copy");
@@ -1622,11 +1624,6 @@ dc_status dc_set_layer_norms(dc_ctx* ctx, int32_t groups, int32_t act, float eps
   ctx->norms = n;
   ctx->deep = groups > 0;
   ctx->training = false;                     // other parameters: dc_train_begin again
-  if (ctx->deep) {
-    refresh_row_major(ctx, s);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return hip_fail(ctx, e, "layer matrices");
-  }
   return DC_OK;
 }
 

@@ -74,6 +74,26 @@ def test_estimates(B, dtype, tol, F, H, L, groups, name):
     ev.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norms_are_there_for_every_stream(B, dtype):
+    """Nothing that dc_set_layer_norms starts is still under way when it returns, and a call on another stream finds it all."""
+    import torch
+    w = workload(64, 256, 6, dtype)
+    gamma, beta = norms(256, 6)
+    ev = B.evaluator_for(w)
+    cg, co, gid = ev.to_device(w.cand_graph), ev.to_device(w.cand_off), ev.to_device(w.group_id)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        st = B.dc_set_layer_norms(ev.ctx, 8, B.DC_ACT_SILU, EPS, gamma, beta, side.cuda_stream)
+        done = side.query()
+        assert st == B.DC_OK and done
+    got = ev.eval_candidates(cg, co, gid).cpu().numpy()            # on the current stream
+    ref = oracle_predictions(w, gamma, beta, 8, "silu")
+    assert np.abs(got - ref).max() <= (1e-5 if dtype == "f32" else 2e-2) * np.abs(ref).max()
+    ev.close()
+
+
 @pytest.mark.parametrize("dtype,tol", [("f32", 2e-5), ("bf16", 2e-2)])
 def test_module_times(B, dtype, tol):
     """Cost(H'): the norms run over the ops of each fused op; repeated fused ops take the first one's estimate."""
