@@ -408,11 +408,17 @@ class KeptRows:
     """Rows kept in 8 bits (see dc_kept_rows): int8 codes and uint8 exponents, device tensors."""
 
     def __init__(self, code, exponent, cols: int):
-        rows, blocks = int(code.shape[0]), -(-cols // 32)
-        if code.dim() != 2 or exponent.dim() != 2 or code.shape[1] < 32 * blocks or tuple(exponent.shape) != (rows, blocks):
+        blocks = -(-cols // 32)
+        if code.dim() != 2 or exponent.dim() != 2 or code.shape[1] < 32 * blocks or tuple(exponent.shape) != (code.shape[0], blocks):
             raise ValueError(f"kept rows of {cols} columns need codes [rows, {32 * blocks}] and exponents [rows, {blocks}]")
         self.code, self.exponent, self.cols = code, exponent, cols
-        self.c = DcKeptRows(code.data_ptr(), exponent.data_ptr(), code.stride(0), exponent.stride(0))
+
+    @property
+    def c(self) -> DcKeptRows:
+        code, exponent = self.code, self.exponent
+        apart = self.rows > 1                              # of a single row any distance may be written down
+        return DcKeptRows(code.data_ptr(), exponent.data_ptr(), code.stride(0) if apart else code.shape[1],
+                          exponent.stride(0) if apart else exponent.shape[1])
 
     @property
     def rows(self) -> int:

@@ -371,6 +371,21 @@ def test_keep_rows_anywhere(B, ev, dtype, ld, first):
     assert np.array_equal(ev.restore_rows(k2, t, out=out).double().cpu().numpy(), kept_values(code, exponent, cols))
 
 
+@pytest.mark.parametrize("rows", [1, 37])
+def test_kept_rows_in_c_calls(B, ev, rows):
+    """The struct of kept rows, of those that keep_rows made and of those put together from tensors."""
+    cols = 72
+    x = rand(3, rows, cols).float().cuda()
+    k = ev.keep_rows(x)
+    wide = torch.zeros(rows, 128, dtype=torch.int8, device="cuda")
+    wide[:, :96] = k.code
+    want = ev.restore_rows(k)
+    for kept in (k, B.KeptRows(k.code, k.exponent, cols), B.KeptRows(wide[:, :96], k.exponent, cols)):
+        out = torch.empty_like(x)
+        assert B.dc_restore_rows(ev.ctx, B.DC_F32, rows, cols, kept.c, out.data_ptr(), cols, torch.cuda.current_stream().cuda_stream) == B.DC_OK
+        assert torch.equal(out, want)
+
+
 # ---------------------------------------------------------------------------
 # graph norm
 # ---------------------------------------------------------------------------

@@ -100,6 +100,13 @@ def test_binding_refuses():
             print("not refused:", k)
 
 
+def test_kept_rows_as_a_struct():
+    import torch
+    code, exponent = torch.zeros(5, 96, dtype=torch.int8), torch.zeros(5, 2, dtype=torch.uint8)
+    for k, want in ((B.KeptRows(code[:, :64], exponent, 33), (96, 2)), (B.KeptRows(code[:1].as_strided((1, 64), (7, 1)), exponent[:1], 64), (64, 2))):
+        assert (k.c.code, k.c.exponent, k.c.ld_code, k.c.ld_exponent) == (code.data_ptr(), exponent.data_ptr(), *want)
+
+
 def test_null_contexts_are_errors():
     lib = B.lib()
     for name, args in (("dc_dense", (None, None, None)), ("dc_dense_backward", (None, None, None)), ("dc_graph_norm", (None, None, None)),
