@@ -440,8 +440,11 @@ dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* h
  * none uses its scratch, so calls on different streams may overlap as long as their arrays and workspaces are their
  * own.  They allocate nothing and do not synchronise, and may be captured into a graph.  Work is enqueued on
  * `stream`, a stream of the context's device, whatever device is current.  An array of outputs may be null where
- * the text says so; rows = 0 is allowed.  Limits: rows and graphs fit in int32, rows are at most 2^22 elements
- * apart, in and out are at most 65536, channels per group at most 512, channels at most 8192.                   */
+ * the text says so; rows = 0 is allowed.  A result may lie in another array of the call only where the text says so, and
+ * then in the same place with rows equally far apart; else a call whose results overlap each other, the workspace or what
+ * it still reads is refused.  Rows may lie between another array's rows if both are equally far apart.
+ * Limits: rows and graphs fit in int32, rows are at most 2^22 elements apart, in and out are at most 65536, channels per
+ * group at most 512, channels at most 8192.                                                                       */
 typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 3 } dc_activation;
 /* GELU is z (1 + erf(z / sqrt 2)) / 2, SiLU z / (1 + e^-z). */
 
@@ -472,12 +475,11 @@ typedef struct {
   const void* W;
   int64_t ldw;
   const float* bias;    /* [out] or null                                              */
-  const void* residual; /* R [rows, out] or null; may be the same array as Y          */
+  const void* residual; /* R [rows, out] or null; Y may be the same array             */
   int64_t ld_residual;
-  void* Z;              /* [rows, out] or null: what the gradient of the activation needs;
-                         * none of the other arrays                                   */
+  void* Z;              /* [rows, out] or null: what the gradient of the activation needs */
   int64_t ldz;
-  void* Y;              /* [rows, out], not X                                         */
+  void* Y;              /* [rows, out]                                                */
   int64_t ldy;
 } dc_dense_args;
 dc_status dc_dense(dc_ctx* ctx, const dc_dense_args* args, void* stream);
@@ -498,7 +500,7 @@ typedef struct {
   const dc_kept_rows* kept;  /* host struct, or null; X is not read then              */
   const void* W;
   int64_t ldw;
-  void* dX;             /* [rows, in] or null; not dY, Z or X                         */
+  void* dX;             /* [rows, in] or null                                         */
   int64_t lddx;
   void* dW;             /* [in, out] or null                                          */
   int64_t lddw;
@@ -512,9 +514,10 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
 /* Norm over the rows of each graph (a group norm whose positions are the rows of a graph), with an activation.  The
  * channels are in `groups` groups of channels / groups neighbours; per graph and group, over its rows and channels:
  *   mean, rstd = 1 / sqrt(variance + eps);  y = act(gamma (x - mean) rstd + beta)
- * Both are returned rounded to fp32; y takes the mean as it was before.  A graph without rows has mean 0 and variance 0.  Rows of no graph (before node_off[0], behind node_off[n_graphs]) are
- * neither read nor written.  Rows are at most 2^17 elements apart here.  A graph whose offsets do not ascend within
- * [0, rows] is left alone, and dc_check reports DC_ERR_BAD_GRAPH.  The same call gives the same bits.               */
+ * Both are returned rounded to fp32; y takes the mean as it was before.  A graph without rows has mean 0 and variance 0.
+ * Rows of no graph (before node_off[0], behind node_off[n_graphs]) are neither read nor written.  Rows are at most 2^17
+ * elements apart here.  A graph whose offsets do not ascend within [0, rows] is left alone, and dc_check reports
+ * DC_ERR_BAD_GRAPH.  The same call gives the same bits.                                                             */
 typedef struct {
   int32_t dtype, act;
   int64_t rows;             /* rows of x and y                                            */
@@ -536,7 +539,7 @@ typedef struct {
   int64_t lddy;
   const void* dres;         /* [rows, channels] or null: the gradient that goes past the norm */
   int64_t lddres;
-  void* dX;                 /* may be dY or dres                                          */
+  void* dX;                 /* may be dY, dres or X                                       */
   int64_t lddx;
   float* dgamma;            /* [channels], null together with dbeta                       */
   float* dbeta;

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <new>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -1461,6 +1462,37 @@ dc_status kept_check(dc_ctx* ctx, const dc_kept_rows* k, int64_t rows, int32_t c
   if (st != DC_OK) return st;
   return array_check(ctx, k->exponent, k->ld_exponent, rows, nb, 1, "exponent");
 }
+// Where an array of a call lies: rows of `width` bytes, `ld` bytes from one to the next.
+struct Place {
+  const char* name;
+  const char* p;           // null: not there
+  int64_t rows, width, ld;
+};
+Place rows_place(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) {
+  return Place{name, static_cast<const char*>(p), rows, cols * bytes, ld * bytes};
+}
+Place vector_place(const char* name, const void* p, int64_t bytes) { return Place{name, static_cast<const char*>(p), 1, bytes, bytes}; }
+bool same(const Place& a, const Place& b) { return a.p == b.p && (a.rows <= 1 || a.ld == b.ld); }
+// Whether two arrays have a byte in common.  Rows that lie between the other's rows are told apart where both are equally far
+// apart; else arrays whose first and last bytes enclose each other's count as overlapping.
+bool overlap(const Place& a, const Place& b) {
+  if (!a.p || !b.p || a.rows < 1 || b.rows < 1 || a.width < 1 || b.width < 1) return false;
+  const int64_t to = (int64_t)(reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p));
+  if (to >= (a.rows - 1) * a.ld + a.width || -to >= (b.rows - 1) * b.ld + b.width) return false;
+  if ((a.rows > 1 && b.rows > 1 && a.ld != b.ld) || (a.rows == 1 && b.rows == 1)) return true;
+  // row i of a and row j of b, k = i - j:  to - width of a < k ld < to + width of b
+  const int64_t ld = a.rows > 1 ? a.ld : b.ld;
+  auto floor_of = [&](int64_t x) { return x >= 0 ? x / ld : -((-x + ld - 1) / ld); };
+  const int64_t lo = floor_of(to - a.width) + 1, hi = -floor_of(-(to + b.width)) - 1;
+  return (lo > 1 - b.rows ? lo : 1 - b.rows) <= (hi < a.rows - 1 ? hi : a.rows - 1);
+}
+// A result that lies in what the call still reads, or in another result.  `in_place`: the same array is allowed.
+dc_status lies_apart(dc_ctx* ctx, const Place& result, std::initializer_list<Place> others, bool in_place = false) {
+  for (const Place& o : others)
+    if (overlap(result, o) && !(in_place && same(result, o)))
+      return fail(ctx, DC_ERR_INVALID_ARG, std::string(result.name) + " overlaps " + o.name);
+  return DC_OK;
+}
 KeptView kept_view(const dc_kept_rows* k) {
   KeptView v{};
   if (k) v = KeptView{reinterpret_cast<const signed char*>(k->code), k->exponent, (long long)k->ld_code, (long long)k->ld_exponent};
@@ -1477,6 +1509,13 @@ dc_status keep_or_restore(dc_ctx* ctx, int32_t dtype, int64_t rows, int32_t cols
   st = array_check(ctx, src ? src : dst, ldx, rows, cols, dtype == DC_BF16 ? 2 : 4, "x");
   if (st == DC_OK) st = kept_check(ctx, kept, rows, cols);
   if (st != DC_OK || rows == 0) return st;
+  const int nb = (cols + kKeptBlock - 1) / kKeptBlock;
+  const Place x = rows_place("x", src ? src : dst, rows, cols, ldx, dtype == DC_BF16 ? 2 : 4),
+              code = rows_place("code", kept->code, rows, nb * kKeptBlock, kept->ld_code, 1),
+              exponent = rows_place("exponent", kept->exponent, rows, nb, kept->ld_exponent, 1);
+  st = lies_apart(ctx, x, {code, exponent});
+  if (st == DC_OK && src) st = lies_apart(ctx, code, {exponent});
+  if (st != DC_OK) return st;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   KeepArgs a{};
@@ -1533,6 +1572,32 @@ dc_status graph_norm_check(dc_ctx* ctx, const dc_graph_norm_args* a, bool backwa
   const size_t need = graph_norm_bytes(a->rows, a->n_graphs, a->channels, a->groups, backward, ctx->n_cu);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_graph_norm_bytes");
   if (need > 0 && !at(a->workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+  const bool kept = backward && a->kept;
+  const int nb = (a->channels + kKeptBlock - 1) / kKeptBlock;
+  const int64_t stats = 4 * (int64_t)a->n_graphs * a->groups, vec = 4 * (int64_t)a->channels;
+  const Place X = rows_place("X", a->X, kept ? 0 : a->rows, a->channels, a->ldx, es),
+              code = rows_place("code", kept ? a->kept->code : nullptr, a->rows, nb * kKeptBlock, kept ? a->kept->ld_code : 0, 1),
+              exponent = rows_place("exponent", kept ? a->kept->exponent : nullptr, a->rows, nb, kept ? a->kept->ld_exponent : 0, 1),
+              off = vector_place("node_off", a->node_off, 4 * ((int64_t)a->n_graphs + 1)), gamma = vector_place("gamma", a->gamma, vec),
+              beta = vector_place("beta", a->beta, vec), mean = vector_place("mean", a->mean, stats), rstd = vector_place("rstd", a->rstd, stats),
+              workspace = vector_place("the workspace", a->workspace, (int64_t)need);
+  if (!backward) {
+    const Place Y = rows_place("Y", a->Y, a->rows, a->channels, a->ldy, es);
+    st = lies_apart(ctx, Y, {X}, true);
+    if (st == DC_OK) st = lies_apart(ctx, Y, {off, gamma, beta, mean, rstd});
+    if (st == DC_OK) st = lies_apart(ctx, mean, {X, off, gamma, beta, rstd});
+    if (st == DC_OK) st = lies_apart(ctx, rstd, {X, off, gamma, beta});
+    if (st == DC_OK) st = lies_apart(ctx, workspace, {X, Y, off, gamma, beta, mean, rstd});
+  } else {
+    const Place dY = rows_place("dY", a->dY, a->rows, a->channels, a->lddy, es), dX = rows_place("dX", a->dX, a->rows, a->channels, a->lddx, es),
+                dres = rows_place("dres", a->dres, a->rows, a->channels, a->lddres, es), dgamma = vector_place("dgamma", a->dgamma, vec),
+                dbeta = vector_place("dbeta", a->dbeta, vec);
+    st = lies_apart(ctx, dX, {X, dY, dres}, true);                 // dgamma and dbeta come last: what is only read has been by then
+    if (st == DC_OK) st = lies_apart(ctx, dX, {code, exponent, off, gamma, beta, mean, rstd, dgamma, dbeta});
+    if (st == DC_OK) st = lies_apart(ctx, dgamma, {dbeta});
+    if (st == DC_OK) st = lies_apart(ctx, workspace, {X, code, exponent, dY, dres, dX, off, gamma, beta, mean, rstd, dgamma, dbeta});
+  }
+  if (st != DC_OK) return st;
   *g = GraphNormArgs{};
   g->rows = a->rows;
   g->n_graphs = a->n_graphs;
@@ -1675,8 +1740,14 @@ dc_status dc_dense(dc_ctx* ctx, const dc_dense_args* args, void* stream) {
   if (st == DC_OK && a.Z) st = array_check(ctx, a.Z, a.ldz, a.rows, a.out, es, "Z");
   if (st != DC_OK || a.rows == 0) return st;
   if (!at(a.bias, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "bias is not aligned to its elements");
-  if (a.Y == a.X || (a.Z && (a.Z == a.X || a.Z == a.Y || a.Z == a.residual)))
-    return fail(ctx, DC_ERR_INVALID_ARG, "Y cannot be X, and Z no array of the others");
+  const Place X = rows_place("X", a.X, a.rows, a.in, a.ldx, es), W = rows_place("W", a.W, a.in, a.out, a.ldw, es),
+              Y = rows_place("Y", a.Y, a.rows, a.out, a.ldy, es), Z = rows_place("Z", a.Z, a.rows, a.out, a.ldz, es),
+              R = rows_place("the residual", a.residual, a.rows, a.out, a.ld_residual, es),
+              bias = vector_place("bias", a.bias, 4 * (int64_t)a.out);
+  st = lies_apart(ctx, Y, {X, W, bias});
+  if (st == DC_OK) st = lies_apart(ctx, Y, {R}, true);
+  if (st == DC_OK) st = lies_apart(ctx, Z, {X, W, bias, R, Y});
+  if (st != DC_OK) return st;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   DenseArgs d{};
@@ -1721,12 +1792,25 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   if (st == DC_OK && a.dX) st = array_check(ctx, a.dX, a.lddx, a.rows, a.in, es, "dX");
   if (st == DC_OK && a.dX) st = array_check(ctx, a.W, a.ldw, a.in, a.out, es, "W");
   if (st != DC_OK) return st;
-  if (a.rows > 0 && a.dX && (a.dX == a.dY || (a.act != DC_ACT_NONE && a.dX == a.Z) || (a.dW && !a.kept && a.dX == a.X)))
-    return fail(ctx, DC_ERR_INVALID_ARG, "dX cannot be dY, Z or X");
   if (!at(a.db, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "db is not aligned to its elements");
-  if (!a.workspace || a.workspace_bytes < dc_dense_backward_bytes(ctx, a.dtype, a.act, a.rows, a.in, a.out))
-    return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_dense_backward_bytes");
+  const size_t need = dc_dense_backward_bytes(ctx, a.dtype, a.act, a.rows, a.in, a.out);
+  // arrays that the call does not read have no place
+  const int64_t read_rows = a.dW ? a.rows : 0, kept_rows = a.kept ? read_rows : 0, nb = (a.in + kKeptBlock - 1) / kKeptBlock;
+  const Place dY = rows_place("dY", a.dY, a.rows, a.out, a.lddy, es), Z = rows_place("Z", a.Z, a.act == DC_ACT_NONE ? 0 : a.rows, a.out, a.ldz, es),
+              X = rows_place("X", a.X, a.kept ? 0 : read_rows, a.in, a.ldx, es),
+              code = rows_place("code", a.kept ? a.kept->code : nullptr, kept_rows, nb * kKeptBlock, a.kept ? a.kept->ld_code : 0, 1),
+              exponent = rows_place("exponent", a.kept ? a.kept->exponent : nullptr, kept_rows, nb, a.kept ? a.kept->ld_exponent : 0, 1),
+              W = rows_place("W", a.W, a.dX ? a.in : 0, a.out, a.ldw, es), dX = rows_place("dX", a.dX, a.rows, a.in, a.lddx, es),
+              dW = rows_place("dW", a.dW, a.in, a.out, a.lddw, es), db = vector_place("db", a.db, 4 * (int64_t)a.out),
+              workspace = vector_place("the workspace", a.workspace, (int64_t)need);
+  st = lies_apart(ctx, dX, {dY, Z, X, code, exponent, W});
+  if (st != DC_OK) return st;
+  if (!a.workspace || a.workspace_bytes < need) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_dense_backward_bytes");
   if (!at(a.workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+  st = lies_apart(ctx, dW, {dX, dY, Z, X, code, exponent});        // W has been read by then
+  if (st == DC_OK) st = lies_apart(ctx, db, {dX, dW, dY, Z, X, code, exponent, W});
+  if (st == DC_OK) st = lies_apart(ctx, workspace, {dX, dW, db, dY, Z, X, code, exponent, W});
+  if (st != DC_OK) return st;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   DenseBackArgs d{};

@@ -889,6 +889,77 @@ def test_c_calls_refuse_arrays_in_each_others_place_and_rows_too_far_apart(B, ev
     assert all((v == 0).all() for v in (x, w, y, z)) and ev.check() == B.DC_OK
 
 
+def test_c_calls_refuse_results_that_overlap(B, ev):
+    """A result in what the call still reads, in another result or in the workspace: refused with nothing enqueued, also where
+    the arrays only touch, or begin alike with rows at other distances."""
+    n, buf = 16, torch.zeros(40 * 64, device="cuda")
+    at = lambda i: buf.data_ptr() + 4 * i
+    X, W, Y, Z, R, V, S = (at(i * 256) for i in range(7))                 # arrays of 16 x 16, one behind the other
+    ok = dict(dtype=B.DC_F32, act=1, rows=n, n_in=n, n_out=n, X=X, ldx=n, W=W, ldw=n, Y=Y, ldy=n, Z=Z, ldz=n, residual=R, ld_residual=n, bias=V)
+    for bad in (dict(Y=R, ldy=n + 4), dict(Y=R + 4 * n), dict(Y=X + 4), dict(Y=X - 4 * n), dict(Y=W), dict(Y=V - 4), dict(Z=W), dict(Z=V),
+                dict(Z=R), dict(Z=R - 4, ldz=n), dict(Z=Y + 4 * n), dict(Z=X, ldz=n + 1)):
+        assert B.dc_dense(ev.ctx, B.DcDenseArgs(**{**ok, **bad})) == B.DC_ERR_INVALID_ARG, bad
+    need = B.dc_dense_backward_bytes(ev.ctx, B.DC_F32, 1, n, n, n)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    kept = B.DcKeptRows(S, S + 1024, 32, 1)
+    back = dict(dtype=B.DC_F32, act=1, rows=n, n_in=n, n_out=n, dY=Y, lddy=n, Z=Z, ldz=n, X=X, ldx=n, W=W, ldw=n, dX=R, lddx=n, dW=V, lddw=n,
+                db=at(9 * 256), workspace=ws.data_ptr(), workspace_bytes=need)
+    for bad in (dict(dX=Y + 4), dict(dX=Z - 4), dict(dX=X + 4 * n), dict(dX=W), dict(dW=Y), dict(dW=Z), dict(dW=X), dict(dW=R + 4), dict(db=Y),
+                dict(db=Z), dict(db=X), dict(db=W), dict(db=R + 64), dict(db=V), dict(workspace=X), dict(dX=ws.data_ptr() + need - 16),
+                dict(dW=ws.data_ptr()), dict(db=ws.data_ptr() + 64), dict(kept=kept, dX=S + 64), dict(kept=kept, dW=S + 1024 - 16)):
+        args = {**back, **{k: v for k, v in bad.items() if k != "kept"}}
+        if "kept" in bad:
+            args["kept"] = B.C.pointer(bad["kept"])
+        assert B.dc_dense_backward(ev.ctx, B.DcDenseBackwardArgs(**args)) == B.DC_ERR_INVALID_ARG, bad
+    off = torch.tensor([0, 9, n], dtype=torch.int32, device="cuda")
+    norm = dict(dtype=B.DC_F32, act=0, rows=n, n_graphs=2, channels=n, groups=2, eps=1e-5, node_off=off.data_ptr(), X=X, ldx=n, gamma=V, beta=V + 64,
+                mean=V + 128, rstd=V + 144, Y=Y, ldy=n)
+    for bad in (dict(Y=X, ldy=n + 4), dict(Y=X + 4 * n), dict(Y=V - 4), dict(Y=V + 64), dict(Y=off.data_ptr()), dict(mean=X), dict(rstd=V + 132), dict(mean=Y),
+                dict(mean=V), dict(rstd=V + 64), dict(rstd=off.data_ptr() + 4)):
+        assert B.dc_graph_norm(ev.ctx, B.DcGraphNormArgs(**{**norm, **bad})) == B.DC_ERR_INVALID_ARG, bad
+    need = B.dc_graph_norm_bytes(ev.ctx, n, 2, n, 2, True)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    norm = {**norm, **dict(Y=0, dY=Y, lddy=n, dres=Z, lddres=n, dX=R, lddx=n, dgamma=V + 256, dbeta=V + 320, workspace=ws.data_ptr(), workspace_bytes=need)}
+    for bad in (dict(dX=Y, lddx=n + 4), dict(dX=Z, lddx=n + 4), dict(dX=X, lddx=n + 4), dict(dX=Y + 4), dict(dX=Z - 4 * n), dict(dX=V), dict(dX=V + 136),
+                dict(dX=off.data_ptr()), dict(dgamma=V + 316), dict(dX=V + 256), dict(workspace=X), dict(dX=ws.data_ptr()), dict(dgamma=ws.data_ptr()),
+                dict(kept=kept, dX=S + 64), dict(kept=kept, dX=S + 1024 - 64)):
+        args = {**norm, **{k: v for k, v in bad.items() if k != "kept"}}
+        if "kept" in bad:
+            args["kept"] = B.C.pointer(bad["kept"])
+        assert B.dc_graph_norm_backward(ev.ctx, B.DcGraphNormArgs(**args)) == B.DC_ERR_INVALID_ARG, bad
+    for x, k in ((S + 64, kept), (S + 1024 - 4, kept), (X, B.DcKeptRows(S, S + 32, 32, 1))):
+        assert B.dc_keep_rows(ev.ctx, B.DC_F32, n, n, x, n, k) == B.DC_ERR_INVALID_ARG
+    assert B.dc_restore_rows(ev.ctx, B.DC_F32, n, n, kept, S + 64, n) == B.DC_ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert not buf.any() and not ws.any() and ev.check() == B.DC_OK
+    y = torch.zeros(32, 24, device="cuda")
+    with pytest.raises(B.DiscoError):                      # the residual's rows at another distance than those of the result
+        ev.dense(torch.ones(16, 8, device="cuda"), torch.ones(8, 16, device="cuda"), residual=y[:16, :16], out=y.view(16, 48)[:, :16])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 300, 5000])
+def test_results_beside_what_is_read(ev, dtype, rows):
+    """Columns of one matrix as the arrays of a call, each beside the others, and what may be done in place."""
+    t, C, G = TYPES[dtype], 32, 4
+    big = rand(1, rows, 4 * C).to(t).cuda()
+    x, dy, y, z = (big[:, i * C:(i + 1) * C] for i in range(4))
+    w, off = (rand(2, C, C) / 6).to(t).cuda(), offsets([rows // 3, rows - rows // 3])
+    copies = [v.clone() for v in (x, dy)]
+    want = ev.dense(copies[0], w, act="silu")
+    ev.dense(x, w, act="silu", out=y)
+    assert torch.equal(y, want)
+    want, mean, rstd = ev.graph_norm(copies[0], off, G, act="gelu")
+    ev.graph_norm(x, off, G, act="gelu", out=z)
+    assert torch.equal(z, want) and torch.equal(x, copies[0]) and torch.equal(dy, copies[1])
+    want = ev.graph_norm_backward(copies[1], copies[0], off, G, None, None, mean, rstd, "gelu", residual=copies[0])
+    for place in (x, dy):                                  # in place of the rows, of the gradient
+        keep = place.clone()
+        got = ev.graph_norm_backward(dy, x, off, G, None, None, mean, rstd, "gelu", residual=x, out=place)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        place.copy_(keep)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(700, 96, 139), (33, 40, 70), (8000, 64, 131), (4500, 32, 255)])
 def test_dense_adds_to_its_residual_in_place(ev, dtype, shape):
