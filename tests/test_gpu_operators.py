@@ -592,6 +592,25 @@ def test_graph_norm_backward(ev, dtype, sizes, C, G):
         close(g, want, tol, what)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,G", [(256, 8), (128, 4)])
+def test_graph_norm_vector_gradients_of_a_long_graph_among_short_ones(ev, dtype, C, G):
+    """A thousand rows that one wave takes beside thousands of graphs of nine: terms of one sign that a running sum in fp32 rounds
+    to the same side each time; dgamma and dbeta are off by at most the 70 roundings of runs of 64 rows."""
+    sizes, t = [9] * 1500 + [1000] + [9] * 1500, TYPES[dtype]
+    first = 9 * 1500
+    x = torch.zeros(sum(sizes), C)
+    x[first:first + 1000] = 1 + 2.0 ** -15 - 2.0 ** -22          # a constant xh, below
+    dy = torch.zeros(sum(sizes), C)
+    dy[first:first + 1000] = 1 + 2.0 ** -15 - 2.0 ** -22
+    x, dy = x.to(t), dy.to(t)
+    mean, rstd = torch.zeros(len(sizes), G, device="cuda"), torch.ones(len(sizes), G, device="cuda")
+    ref = norm_back_reference(x, dy, None, sizes, G, torch.ones(C), torch.zeros(C), mean.cpu(), rstd.cpu(), "none", t)
+    got = ev.graph_norm_backward(dy.cuda(), x.cuda(), offsets(sizes), G, None, None, mean, rstd)
+    for g, (want, tol), what in zip(got, ref, ("dx", "dgamma", "dbeta")):
+        close(g, want, tol, what)
+
+
 @pytest.mark.parametrize("sizes", ["short", "middle", "long"])
 def test_graph_norm_backward_relu_in_place(ev, sizes):
     """ReLU, on inputs whose normalised values are not next to its corner; dx in place of dy, rows of no graph as they were."""
