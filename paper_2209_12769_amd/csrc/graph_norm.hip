@@ -160,8 +160,15 @@ __device__ __forceinline__ void slope(float (&dy)[kV], const float (&xh)[kV], co
 
 // What the sums of a group are counted from: its first value in row `row`, or zero if that is not finite.
 template <typename T>
-__device__ __forceinline__ double origin(const GraphNormArgs& a, long long row, int channel) {
-  const float x = widen(static_cast<const T*>(a.X)[row * a.ldx + channel]);
+__device__ __forceinline__ T first_value(const GraphNormArgs& a, long long row, int channel) {
+  return static_cast<const T*>(a.X)[row * a.ldx + channel];
+}
+// Not to be widened, and waited for, where it was requested.
+template <typename T>
+__device__ __forceinline__ double origin(T first) {
+  unsigned bits = __builtin_bit_cast(std::conditional_t<sizeof(T) == 4, unsigned, u16>, first);
+  asm volatile("" : "+v"(bits));
+  const float x = __uint_as_float(sizeof(T) == 4 ? bits : bits << 16);
   return __builtin_isfinite(x) ? (double)x : 0.0;
 }
 // What a row's vector adds to the two sums.
@@ -362,13 +369,15 @@ __device__ __forceinline__ void each_row(const Places& p, int first, int step, i
 // Gradients of vectors: a thread's terms of so many rows are summed in fp32, these sums in 64 bits (1000 equal terms in fp32 alone were up
 // to 250 roundings off; the runs cost at most 1.6 %, of 60000 graphs of 3 rows of 128).
 constexpr int kRun = 64;
-// each_row of all rows, `flush` behind each run.
-template <typename T, typename X, int kV, bool kBack, int kStep, typename F, typename E>
-__device__ __forceinline__ void each_run(const Places& p, int first, int step, int count, int c, F f, E flush) {
+// each_row of all rows.  Forward: `begin` (which waits for a request made before) once the first group has been requested;
+// gradient: `flush` behind each run.
+template <typename T, typename X, int kV, bool kBack, int kStep, typename F, typename B, typename E>
+__device__ __forceinline__ void each_run(const Places& p, int first, int step, int count, int c, F f, B begin, E flush) {
   for (int i = 0; i < count; i += kStep) {
     Two<T, X, kV> h[kStep];
 #pragma unroll
     for (int u = 0; u < kStep; ++u) fetch<T, X, kV, kBack>(h[u], p, (unsigned)(first + (int)__umul24(min(i + u, count - 1), step)), c);
+    if (!kBack && i == 0) begin();
 #pragma unroll
     for (int u = 0; u < kStep; ++u)
       if (i + u < count) f(h[u], i + u);
@@ -414,7 +423,8 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       rs = n.a.rstd[(size_t)g * n.a.G + group];
     }
     double s1 = 0.0, s2 = 0.0, x0 = 0.0;
-    if (!kBack && r.hi > r.lo) x0 = origin<T>(n.a, r.lo, group * n.cg);
+    T first{};
+    if (!kBack && r.hi > r.lo) first = first_value<T>(n.a, r.lo, group * n.cg);
     float dg[kV], db[kV];
 #pragma unroll
     for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
@@ -429,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void graph_norm_kernel(const Norm n) {
       open<T, X, kV, kBack>(x, dy, h);
       add_sums<kBack, kV>(s1, s2, x, dy, x0, mu, rs, f, n.a.act, dg, db);
     };
-    each_run<T, X, kV, kBack, kThreads == 64 ? 8 : 4>(at, rl, step, count, c, add, [&] { flush<kV>(dgs, dbs, dg, db); });
+    each_run<T, X, kV, kBack, kThreads == 64 ? 8 : 4>(at, rl, step, count, c, add, [&] { x0 = origin(first); }, [&] { flush<kV>(dgs, dbs, dg, db); });
     group_sums(s1, s2, red, n.lanes, used, gv);
     if constexpr (!kBack) {
       statistics(s1, s2, m, x0, n.a.eps, mu, s1f, rs);
@@ -546,7 +556,8 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
         rs = n.a.rstd[(size_t)seg.g * n.a.G + group];
       }
       double s1 = 0.0, s2 = 0.0, x0 = 0.0;
-      if (!kBack) x0 = origin<T>(n.a, seg.first, group * n.cg);
+      T first{};
+      if (!kBack) first = first_value<T>(n.a, seg.first, group * n.cg);
       float dg[kV], db[kV];
 #pragma unroll
       for (int k = 0; k < kV; ++k) dg[k] = db[k] = 0.f;
@@ -557,7 +568,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_sums_kernel(const Norm n)
         open<T, X, kV, kBack>(x, dy, h);
         add_sums<kBack, kV>(s1, s2, x, dy, x0, mu, rs, f, n.a.act, dg, db);
       };
-      each_run<T, X, kV, kBack, 4>(at, rl, step, count, c, add, [&] { flush<kV>(dgs, dbs, dg, db); });
+      each_run<T, X, kV, kBack, 4>(at, rl, step, count, c, add, [&] { x0 = origin(first); }, [&] { flush<kV>(dgs, dbs, dg, db); });
       group_sums(s1, s2, red, n.lanes, used, gv);
       if (in && rl == 0 && lane % gv == 0) n.part[(size_t)chunk * n.a.G + group] = make_double2(s1, s2);
     }
@@ -593,7 +604,7 @@ __global__ __launch_bounds__(64) void long_sums_kernel(const Norm n, int wide) {
         n.means[(size_t)i * n.a.G + q] = make_float2((float)(s1 / m), (float)(s2 / m));
       } else {
         float mu, lacks, rs;
-        statistics(s1, s2, m, origin<T>(n.a, first, q * n.cg), n.a.eps, mu, lacks, rs);
+        statistics(s1, s2, m, origin(first_value<T>(n.a, first, q * n.cg)), n.a.eps, mu, lacks, rs);
         n.means[(size_t)i * n.a.G + q] = make_float2(lacks, 0.f);
         n.a.mean[(size_t)e.x * n.a.G + q] = mu;
         n.a.rstd[(size_t)e.x * n.a.G + q] = rs;
