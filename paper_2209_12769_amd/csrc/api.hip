@@ -1815,8 +1815,7 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   DenseBackArgs d{};
   d.rows = a.rows;
-  d.d = a.in;
-  d.nseg = 1;
+  d.K = a.in;
   d.N = a.out;
   d.bf16 = a.dtype == DC_BF16;
   d.act = a.act;
@@ -1824,7 +1823,7 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   d.lddy = a.lddy;
   d.Z = a.act == DC_ACT_NONE ? nullptr : a.Z;
   d.ldz = a.ldz;
-  d.X[0] = a.X;
+  d.X = a.X;
   d.ldx = a.ldx;
   d.kept = kept_view(a.dW ? a.kept : nullptr);
   d.W = a.W;

@@ -375,8 +375,8 @@ struct TrainPass {
   float* nrstd;
   // keep8: the layers' outputs in 8 bits instead of hs, and one set of means; hs and per-layer means are not there
   int keep8;
-  signed char* code;           // [L][max_rows, H]
-  unsigned char* exponent;     // [L][max_rows, H / 32]
+  signed char* code;           // [L - 1][max_rows, H]
+  unsigned char* exponent;     // [L - 1][max_rows, H / 32]
   float* grad;                 // [n_params]
   float* loss;                 // [1]
   float* pred;                 // [n_samples] or null

@@ -362,8 +362,8 @@ struct Stager {
   }
 };
 
-// The same for columns of up to three matrices side by side, whose rows are walked: every thread keeps the place of its own
-// columns, and steps from row to row.
+// The same for the columns of a matrix whose rows are walked: every thread keeps the place of its own columns, and steps from
+// row to row.
 template <class E, bool kDz, int kR, int KS, int kT>
 struct ColumnStager : Stager<E, true, kDz, kR, KS, kT> {
   typedef Stager<E, true, kDz, kR, KS, kT> Base;
@@ -384,9 +384,7 @@ struct ColumnStager : Stager<E, true, kDz, kR, KS, kT> {
     here = col - col0;
     whole = col0 + kR <= cols;
     some = cols < kN ? cols : 0;
-    // kept rows are one matrix, and columns of its last block may lie behind its last column
-    const int seg = E::kBytes == 1 ? 0 : (col >= s.d ? 1 : 0) + (col >= 2 * s.d ? 1 : 0), c = col - seg * s.d;
-    p = part_of(s, seg) + (row0 * s.ld + c) * E::kBytes;
+    p = s.p[0] + (row0 * s.ld + col) * E::kBytes;
     z = kDz ? s.z + (row0 * s.ldz + col) * E::kBytes : nullptr;
     e = E::kBytes == 1 ? s.exponent + row0 * s.ld_exponent + col / kKeptBlock : nullptr;
   }
@@ -452,7 +450,7 @@ __device__ __forceinline__ f32x16 mfma(const u32x4& b, const u32x4& a, const f32
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
 }
 
-// Where a lane's operands of a wave's first 32 rows lie, in bytes: row `row0` (a multiple of 64) + lane % 32, chunk lane / 32.
+// Where a lane's operands of a wave's first 32 rows lie, in bytes: row `row0` (a multiple of 32 kI) + lane % 32, chunk lane / 32.
 template <int KS>
 __device__ __forceinline__ unsigned operands_at(int row0) {
   const int lane = threadIdx.x & 63;
@@ -855,7 +853,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
 // 524309 x 256 in bf16 0.15 ms, 5.3 TB/s.
 struct SlopeArgs {
   long long rows;
-  const int* nrows;
   int N, act;
   const char* dy;
   long long lddy;
@@ -864,13 +861,11 @@ struct SlopeArgs {
   char* dz;              // [rows, N]
   float* part;           // [row blocks][N]
   int row_blocks;
-  const int* stop;
 };
 template <class E, int kV>
 __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g) {
-  if (g.stop && g.stop[0] != 0) return;
   __shared__ double red[8][32 * kV];
-  const long long rows = g.nrows ? g.nrows[0] : g.rows;
+  const long long rows = g.rows;
   const int t = threadIdx.x, cb = blockIdx.x / g.row_blocks, rb = blockIdx.x % g.row_blocks;
   const int col = (cb * 32 + (t & 31)) * kV;
   double sum[kV];
@@ -924,11 +919,9 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g) {
 struct WeightArgs {
   Source a;              // X  [rows, M]
   Source b;              // dZ [rows, N]
-  const int* nrows;
   int M, N, S;
   float* part;           // [S][M * N + N]
   int sums;              // column sums of dZ are wanted
-  const int* stop;
 };
 struct Slab {
   long long r0, r1;
@@ -953,12 +946,11 @@ constexpr int kSlabStep = EB::kPieces == 1 ? 64 : 32;
 
 template <class EA, class EB, bool kDz, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs g) {
-  if (g.stop && g.stop[0] != 0) return;
   typedef WeightShape<EA, EB, kWaves> Shape;
   constexpr int kPA = EA::kPieces, kPB = EB::kPieces, KS = Shape::KS, kI = Shape::kI, kHold = 256 / KS, kT = Shape::kT;
   constexpr int kTileM = Shape::kTileM, kTileN = Shape::kTileN;
   extern __shared__ u32x4 lds[];
-  const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
+  const long long rows = g.a.rows;
   const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1, lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
   const int tiles_n = (g.N + kTileN - 1) / kTileN, tiles_m = max(1, (g.M + kTileM - 1) / kTileM), ntile = tiles_m * tiles_n;
   // the tiles of a slab read the same rows: they run on one XCD (the grid is ntile * S, S a multiple of eight)
@@ -1077,7 +1069,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
 // formed again in fp32.
 template <class EA, class EB, bool kDz>
 __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, char* dW, long long lddw, float* __restrict__ db) {
-  if (g.stop && g.stop[0] != 0) return;
   const long long MN = (long long)g.M * g.N, stride = MN + g.N;
   const long long end = db ? stride : MN;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (long long)gridDim.x * blockDim.x) {
@@ -1092,7 +1083,7 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, 
 #pragma unroll
         for (int u = 0; u < 8; ++u) probe = fmaf(x[u], 0.f, probe);
         if (!(probe == 0.f) && i < MN) {
-          const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
+          const long long rows = g.a.rows;
           const int m = (int)(i / g.N), n = (int)(i % g.N);
           for (int u = 0; u < 8; ++u) {
             if (__builtin_isfinite(p[u * stride])) {
@@ -1227,7 +1218,7 @@ hipError_t weight(const WeightArgs& w, const DenseBackArgs& a, float* db, hipStr
 
 template <class E, bool kDz>
 hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
-  const int K = a.nseg * a.d;
+  const int K = a.K;
   constexpr int kWide = 16 / E::kBytes;
   Source dz{};
   dz.p[0] = static_cast<const char*>(a.dY);
@@ -1241,13 +1232,13 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
   if (smooth(a.act)) {
     char* out = reinterpret_cast<char*>(workspace);
     workspace += dense_dz_floats(a.rows, a.N, a.bf16);
-    SlopeArgs g{a.rows, a.nrows, a.N, a.act, dz.p[0], a.lddy, dz.z, a.ldz, out, a.db ? workspace : nullptr, slope_blocks(a.rows, a.n_cu), a.stop};
+    SlopeArgs g{a.rows, a.N, a.act, dz.p[0], a.lddy, dz.z, a.ldz, out, a.db ? workspace : nullptr, slope_blocks(a.rows, a.n_cu)};
     workspace += (size_t)g.row_blocks * a.N;
     const bool wide = a.N % kWide == 0;
     const int columns = 32 * (wide ? kWide : 1), cb = (a.N + columns - 1) / columns;
     if (wide) hipLaunchKernelGGL((slope_kernel<E, kWide>), dim3(cb * g.row_blocks), dim3(256), 0, s, g);
     else hipLaunchKernelGGL((slope_kernel<E, 1>), dim3(cb * g.row_blocks), dim3(256), 0, s, g);
-    if (a.db) launch_column_sums(g.part, g.row_blocks, a.N, a.db, 0, nullptr, a.stop, s);
+    if (a.db) launch_column_sums(g.part, g.row_blocks, a.N, a.db, 0, nullptr, nullptr, s);
     db = nullptr;
     dz.p[0] = out;
     dz.z = nullptr;
@@ -1261,37 +1252,32 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     g.b.ld = a.ldw;
     g.b.rows = K;
     g.b.cols = g.b.d = a.N;
-    g.nrows = a.nrows;
     g.K = a.N;
     g.N = K;
     g.act = DC_ACT_NONE;
     g.Y = static_cast<char*>(a.dX);
     g.ldy = a.lddx;
-    g.stop = a.stop;
     e = product<E, kDz, false>(g, a.rows, a.n_cu, s);
   }
   if (e == hipSuccess && (a.dW || db)) {
     WeightArgs w{};
     w.a.rows = a.rows;
     w.M = a.dW ? K : 0;
-    w.a.cols = K;
-    w.a.d = a.d;
+    w.a.cols = w.a.d = K;
     if (a.kept.code) {
       w.a.p[0] = reinterpret_cast<const char*>(a.kept.code);
       w.a.exponent = a.kept.exponent;
       w.a.ld = a.kept.ld_code;
       w.a.ld_exponent = a.kept.ld_exponent;
     } else {
-      for (int i = 0; i < a.nseg; ++i) w.a.p[i] = static_cast<const char*>(a.X[i]);
+      w.a.p[0] = static_cast<const char*>(a.X);
       w.a.ld = a.ldx;
     }
     w.b = dz;
-    w.nrows = a.nrows;
     w.N = a.N;
     w.S = slabs_of(a.rows, K, a.N, a.bf16, a.act, a.n_cu);
     w.part = workspace;
     w.sums = db != nullptr;
-    w.stop = a.stop;
     e = a.kept.code ? weight<E, Kept, kDz>(w, a, db, s) : weight<E, E, kDz>(w, a, db, s);
   }
   return e;

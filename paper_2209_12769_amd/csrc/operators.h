@@ -134,13 +134,12 @@ hipError_t launch_dense(const DenseArgs& a, hipStream_t s);
 // dZ = dY act'(Z); dX = dZ W^T, dW = X^T dZ, db = sum of the rows of dZ.
 struct DenseBackArgs {
   long long rows;
-  const int* nrows;
-  int d, nseg, N, bf16, act;
+  int K, N, bf16, act;
   const void* dY;
   long long lddy;
   const void* Z;                 // act other than none
   long long ldz;
-  const void* X[3];              // null where kept is taken
+  const void* X;                 // null where kept is taken
   long long ldx;
   KeptView kept;                 // code == null: X
   const void* W;
@@ -151,7 +150,6 @@ struct DenseBackArgs {
   long long lddw;
   float* db;                     // [N] or null
   float* workspace;              // dense_back_floats() of them
-  const int* stop;
   int n_cu;
 };
 size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu);
