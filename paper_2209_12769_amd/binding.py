@@ -34,6 +34,7 @@ DC_KERNELS_SEPARATE_LAYERS = 1
 DC_KERNELS_EVERY_FUSED_OP = 2
 DC_DRAW_DEPENDENCY, DC_DRAW_OP = 0, 1
 DC_KEEP_F32, DC_KEEP_8BIT = 0, 1
+DC_DZ_WHOLE, DC_DZ_ROUNDED = 0, 1
 DC_ACT_NONE, DC_ACT_RELU, DC_ACT_GELU, DC_ACT_SILU = 0, 1, 2, 3
 ACTIVATIONS = {"none": DC_ACT_NONE, "relu": DC_ACT_RELU, "gelu": DC_ACT_GELU, "silu": DC_ACT_SILU}
 STATUS_NAMES = {0: "DC_OK", 1: "DC_ERR_INVALID_ARG", 2: "DC_ERR_BAD_GRAPH", 3: "DC_ERR_BAD_PARTITION",
@@ -87,7 +88,7 @@ class DcDenseBackwardArgs(C.Structure):
                 ("dY", C.c_void_p), ("lddy", C.c_int64), ("Z", C.c_void_p), ("ldz", C.c_int64), ("X", C.c_void_p),
                 ("ldx", C.c_int64), ("kept", C.POINTER(DcKeptRows)), ("W", C.c_void_p), ("ldw", C.c_int64),
                 ("dX", C.c_void_p), ("lddx", C.c_int64), ("dW", C.c_void_p), ("lddw", C.c_int64), ("db", C.c_void_p),
-                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("dz", C.c_int32)]
 
 
 class DcGraphNormArgs(C.Structure):
@@ -103,7 +104,7 @@ class DcGraphNormArgs(C.Structure):
 # The same structs for the wrapper's calls, packed from values (native sizes and alignment).
 _KEPT = struct.Struct("@PPqq")
 _DENSE = struct.Struct("@iiqiiPqPqPPqPqPq")
-_DENSE_BACK = struct.Struct("@iiqiiPqPqPqPPqPqPqPPN")
+_DENSE_BACK = struct.Struct("@iiqiiPqPqPqPPqPqPqPPNi0q")
 _NORM = struct.Struct("@iiqiiifPPqPPPPPqPPqPqPqPPPN")
 assert [s.size for s in (_KEPT, _DENSE, _DENSE_BACK, _NORM)] == [
     C.sizeof(s) for s in (DcKeptRows, DcDenseArgs, DcDenseBackwardArgs, DcGraphNormArgs)]
@@ -716,9 +717,10 @@ class Evaluator:
             self._ok(st, "dc_dense")
         return (out, pre) if want_pre else out
 
-    def dense_backward(self, dy, x, w, act: str = "none", pre=None, want=("x", "w", "b")):
+    def dense_backward(self, dy, x, w, act: str = "none", pre=None, want=("x", "w", "b"), round_dz: bool = False):
         """Gradients (dx, dw, db) of dense at x, w and bias for the gradient dy at its result; None for those not in
-        `want`.  x: the rows, or KeptRows of them."""
+        `want`.  x: the rows, or KeptRows of them.  round_dz: in bfloat16 with "gelu" and "silu", the gradient at x w + bias
+        rounded to bfloat16 for the products: faster, and less exact (DC_DZ_ROUNDED)."""
         torch = self.torch
         rows, n_out, lddy, dtype = self._rows(dy, "dy")
         n_in, wc, ldw, wt = self._rows(w, "w")
@@ -743,7 +745,8 @@ class Evaluator:
         ws = torch.empty(size, dtype=torch.uint8, device=self.device)
         a = _DENSE_BACK.pack(dtype, code, rows, n_in, n_out, dy.data_ptr(), lddy, pz, ldz, px, ldx,
                              0 if kept is None else C.addressof(kept), w.data_ptr(), ldw, 0 if dx is None else dx.data_ptr(), n_in,
-                             0 if dw is None else dw.data_ptr(), n_out, 0 if db is None else db.data_ptr(), ws.data_ptr(), size)
+                             0 if dw is None else dw.data_ptr(), n_out, 0 if db is None else db.data_ptr(), ws.data_ptr(), size,
+                             DC_DZ_ROUNDED if round_dz else DC_DZ_WHOLE)
         st = lib().dc_dense_backward(self.ctx, a, self._raw_stream())
         if st:
             self._ok(st, "dc_dense_backward")

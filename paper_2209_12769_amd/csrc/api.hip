@@ -1785,6 +1785,7 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   const dc_dense_backward_args& a = *args;
   dc_status st = dense_shape_check(ctx, a.dtype, a.act, a.rows, a.in, a.out);
   const int es = a.dtype == DC_BF16 ? 2 : 4;
+  if (st == DC_OK && a.dz != DC_DZ_WHOLE && a.dz != DC_DZ_ROUNDED) st = fail(ctx, DC_ERR_INVALID_ARG, "DC_DZ_WHOLE or DC_DZ_ROUNDED");
   if (st == DC_OK) st = array_check(ctx, a.dY, a.lddy, a.rows, a.out, es, "dY");
   if (st == DC_OK && a.act != DC_ACT_NONE) st = array_check(ctx, a.Z, a.ldz, a.rows, a.out, es, "Z");
   if (st == DC_OK && a.dW) st = a.kept ? kept_check(ctx, a.kept, a.rows, a.in) : array_check(ctx, a.X, a.ldx, a.rows, a.in, es, "X");
@@ -1819,6 +1820,7 @@ dc_status dc_dense_backward(dc_ctx* ctx, const dc_dense_backward_args* args, voi
   d.N = a.out;
   d.bf16 = a.dtype == DC_BF16;
   d.act = a.act;
+  d.round_dz = a.dz == DC_DZ_ROUNDED;
   d.dY = a.dY;
   d.lddy = a.lddy;
   d.Z = a.act == DC_ACT_NONE ? nullptr : a.Z;

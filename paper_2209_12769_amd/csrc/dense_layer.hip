@@ -12,8 +12,10 @@
 // piece: three products instead of six.  Sums that come out not finite in pieces are formed again in fp32.
 // dZ: with ReLU formed as rows are loaded (a comparison).  The slopes of GELU and SiLU cost some twenty instructions a
 // value and every value is loaded by several tiles, so a pass of its own forms dZ once and leaves it in the workspace.
-// bf16: that dZ is bf16, as the operand has to be (off by at most 2^-8 of its size, as dX and dW are by their own
-// rounding); db is summed from the fp32 values in 64 bits.
+// bf16: the operand has to be bf16, and dZ is left as the sum of two of its numbers, 16 bits, in two arrays: dX = [dZ0 | dZ1] [W | W]^T,
+// dW by two products of one load of X.  Rounded to one (off by 2^-8 at most, the caller's choice) dX and dW are further from 64 bits
+// than their own rounding has them, 0.0024 in norm for 0.0017, in two thirds of the time (524309 x 768 -> 256: 820 us for 1190).
+// db is summed from the fp32 values in 64 bits.
 #include "operators.h"
 
 namespace dc {
@@ -29,9 +31,10 @@ typedef unsigned short u16;
 struct F32 { static constexpr int kBytes = 4, kPieces = 3; };
 struct Bf16 { static constexpr int kBytes = 2, kPieces = 1; };
 struct Kept { static constexpr int kBytes = 1, kPieces = 1; };
+struct Bf16Pair { static constexpr int kBytes = 2, kPieces = 2; };      // a number is the sum of one of p and one of z
 
-// An operand as it lies in memory: `rows` x `cols`, up to three matrices of d columns side by side (one, where d is no
-// multiple of eight); with z (kDz) the values are p where z > 0, else 0.
+// An operand as it lies in memory: `rows` x `cols`, up to three matrices of d columns side by side; with z (kDz) the values are p
+// where z > 0, else 0 (Bf16Pair: p + z).
 struct Source {
   const char* p[3];
   const char* z;
@@ -326,9 +329,12 @@ struct Stager {
     }
   }
   __device__ __forceinline__ void column(u32x4 (&p)[kP], int j, float sign) const {
-    if constexpr (E::kBytes == 2 && !kDz) {            // halves of the words of two rows
+    if constexpr (E::kBytes == 2 && (!kDz || kP == 2)) {            // halves of the words of two rows
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[0][i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kP == 2) p[1][i] = __builtin_amdgcn_perm(raw[2 * i + 1].z[j / 2], raw[2 * i].z[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+        p[0][i] = __builtin_amdgcn_perm(raw[2 * i + 1].w[j / 2], raw[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+      }
     } else {
       float y[8];
 #pragma unroll
@@ -616,7 +622,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
   __shared__ float lds[4 * 32 * kFewLd];
   const long long rows = g.nrows ? g.nrows[0] : g.a.rows;
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63, l32 = lane & 31, lh = lane >> 5;
-  const int nct = (g.N + 31) >> 5, chunks = (g.K + 15) >> 4;
+  const int nct = (g.N + 31) >> 5, d = g.a.d, per = (d + 15) >> 4, chunks = g.K / d * per;      // the parts of a row one after another
   const long long ntiles = ((rows + 31) >> 5) * nct;
   if (ntiles > few) return;                           // the tiles of product_kernel
   const float sign = wave & 1 ? -1.f : 1.f;           // what the pieces' sums drop cancels between the waves
@@ -632,23 +638,24 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
     const unsigned ldb = (unsigned)g.b.ld * E::kBytes;
     const char* pb = g.b.p[0] + (kColsB ? (long long)col * E::kBytes : (long long)col * ldb);
     auto load = [&](Chunk& x, int c) {
-      const int k = min(c, chunks - 1) * 16 + 8 * lh, ka = kVec ? min(k, g.K - 8) : 0;
-      const int seg = (ka >= 2 * g.a.d ? 2 : (ka >= g.a.d ? 1 : 0)), kd = ka - seg * g.a.d;      // parts are multiples of eight
-      const char* pa = part_of(g.a, seg) + (row * g.a.ld + kd) * E::kBytes;
-      const char* pz = kDz ? g.a.z + (row * g.a.ldz + kd) * E::kBytes : nullptr;
+      c = min(c, chunks - 1);
+      const int seg = c >= 2 * per ? 2 : (c >= per ? 1 : 0), k = (c - seg * per) * 16 + 8 * lh, ka = kVec ? min(k, d - 8) : 0;
+      const char* pa = part_of(g.a, seg) + (row * g.a.ld + ka) * E::kBytes;
+      const char* pz = kDz ? g.a.z + (row * g.a.ldz + ka) * E::kBytes : nullptr;
       if constexpr (kVec) fetch<E, 8, kDz>(x.a, pa, pz, 0, 0);
-      else fetch_some<E, 8, kDz>(x.a, pa, pz, 0, 0, min(g.K - ka, 8));
+      else fetch_some<E, 8, kDz>(x.a, pa, pz, 0, 0, min(d - ka, 8));
       if constexpr (kColsB) {
+        const int kb = seg * d;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fetch<E, 1, false>(x.b[i], pb + (long long)(kVec ? ka + i : min(k + i, g.K - 1)) * ldb, nullptr, 0, 0);
+        for (int i = 0; i < 8; ++i) fetch<E, 1, false>(x.b[i], pb + (long long)(kb + (kVec ? ka + i : min(k + i, d - 1))) * ldb, nullptr, 0, 0);
       } else {
         if constexpr (kVec) fetch<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0);
-        else fetch_some<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0, min(g.K - ka, 8));
+        else fetch_some<E, 8, false>(x.b[0], pb, nullptr, (unsigned)(ka * E::kBytes), 0, min(d - ka, 8));
       }
     };
     f32x16 acc = zero16();
     auto step = [&](const Chunk& x, int c) {
-      const int k = c * 16 + 8 * lh, from = kVec ? k - min(k, g.K - 8) : 0, to = kVec ? 8 : g.K - k;      // the indices that count
+      const int k = c % per * 16 + 8 * lh, from = kVec ? k - min(k, d - 8) : 0, to = kVec ? 8 : d - k;      // the indices that count
       u32x4 a[kP], b[kP];
       float y[8];
       values<E, 8, kDz>(y, x.a);
@@ -714,7 +721,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
 // time before the sums go through LDS.
 // Measured: bf16 2000003 x 768 -> 256 with residual 1.25 ms (4.1 TB/s, 630 TFLOP/s; library product alone 0.97 ms); fp32
 // 196311 x 201 -> 139 with GELU, residual and Z 0.212 ms (matrix cores 25 % busy; the rest is conversions, the
-// epilogue's instructions and waiting); dX of 524309 x 256 -> 768 in bf16 0.42 ms.
+// epilogue's instructions and waiting); dX of 524309 x 256 -> 768 in bf16 0.42 ms, of two arrays of dZ 0.65 ms (630 TFLOP/s).
 template <class E, int kWaves, bool kShort>
 struct ProductShape {
   static constexpr int kI = (E::kPieces == 1 ? 4 : 2) / (kShort ? 2 : 1), kTileM = 64 * kI, kTileN = 32 * kWaves, KS = E::kPieces == 1 ? 64 : 32;
@@ -743,10 +750,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
   auto load = [&](long long tile, int step) {
     const long long m0 = tile / nct * kTileM;
     const int n0 = (int)(tile % nct) * kTileN;
-    const int seg = !kColsB ? 0 : step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS;
+    const int seg = step >= 2 * per ? 2 : (step >= per ? 1 : 0), k0 = (step - seg * per) * KS;
     sa.load(part_of(g.a, seg) + m0 * lda + k0 * E::kBytes, kDz ? g.a.z + m0 * ldz + k0 * E::kBytes : nullptr, lda, ldz,
             (int)min(rows - m0, (long long)kTileM), k0, d);
-    const long long kb = (long long)seg * d + k0;
+    const long long kb = kColsB ? (long long)seg * d + k0 : k0;      // the parts of a gradient meet the same columns of W
     sb.load(kColsB ? g.b.p[0] + kb * ldb + n0 * E::kBytes : g.b.p[0] + (long long)n0 * ldb + kb * E::kBytes, nullptr, ldb, 0,
             min(g.N - n0, kTileN), k0, d);
   };
@@ -850,7 +857,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const ProductAr
 
 // ---- dZ of the smooth activations ----
 // dz = dy act'(z), and its column sums over the rows of a block: 32 vectors of columns x 8 rows of threads.  Bound by memory:
-// 524309 x 256 in bf16 0.15 ms, 5.3 TB/s.
+// 524309 x 256 in bf16 0.15 ms, 5.3 TB/s, with the second number 0.20 ms.
 struct SlopeArgs {
   long long rows;
   int N, act;
@@ -858,7 +865,8 @@ struct SlopeArgs {
   long long lddy;
   const char* z;
   long long ldz;
-  char* dz;              // [rows, N]
+  char* dz;              // [rows, N]; with pair (bf16) behind it what each value's rounding left, as bf16
+  int pair;
   float* part;           // [row blocks][N]
   int row_blocks;
 };
@@ -890,11 +898,22 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g) {
 #pragma unroll
         for (int k = 0; k < kV; ++k) d[u][k] = row < rows ? d[u][k] * value_of<E>(y[u], k, 1.f) : 0.f;
         if (row < rows) {
+          const long long i = row * g.N + col;
+          float left[kV];
+#pragma unroll
+          for (int k = 0; k < kV; ++k) {                 // what is not finite in its first number has no second
+            const float first = __uint_as_float((unsigned)to_bf16(d[u][k]) << 16);
+            left[k] = __builtin_isfinite(first) ? d[u][k] - first : 0.f;
+          }
           if constexpr (kV * E::kBytes == 16) {
-            store_wide<E>(g.dz, row * g.N + col, d[u]);
+            store_wide<E>(g.dz, i, d[u]);
+            if (E::kBytes == 2 && g.pair) store_wide<E>(g.dz, rows * g.N + i, left);
           } else {
 #pragma unroll
-            for (int k = 0; k < kV; ++k) store_value<E>(g.dz, row * g.N + col + k, d[u][k]);
+            for (int k = 0; k < kV; ++k) {
+              store_value<E>(g.dz, i + k, d[u][k]);
+              if (E::kBytes == 2 && g.pair) store_value<E>(g.dz, rows * g.N + i + k, left[k]);
+            }
           }
         }
       }
@@ -933,10 +952,11 @@ __device__ __forceinline__ Slab slab_rows(const WeightArgs& g, long long rows, i
   return {r0, min(r0 + per, rows)};
 }
 // Tiles of dW: 64 kI x 32 kWaves, as above; every tile of a slab loads the slab's rows, so that wide ones load less.  Measured:
-// 524309 rows, 768 x 256 in bf16 0.33 ms (620 TFLOP/s); 474011 rows, 384 x 128, kept rows times fp32 ones 0.35 ms.
+// 524309 rows, 768 x 256 in bf16 0.33 ms (620 TFLOP/s), with dZ in two numbers 0.50 ms (820 TFLOP/s); 474011 rows, 384 x 128, kept rows times fp32 ones 0.35 ms.
 template <class EA, class EB, int kWaves>
 struct WeightShape {
-  static constexpr int KS = EB::kPieces == 1 ? 64 : 32, kI = EB::kPieces == 1 ? kWaves / 2 : 2;
+  static constexpr int KS = EB::kPieces == 1 ? 64 : 32, kI = EB::kBytes == 2 ? kWaves / 2 : 2;
+  static constexpr bool kSections = EB::kBytes == 4;
   static constexpr int kTileM = 64 * kI, kTileN = 32 * kWaves, kT = 64 * kWaves, kBuffers = kWaves / 4;
   static constexpr int kUnitsA = EA::kPieces * kTileM * KS / 8, kUnitsB = EB::kPieces * kTileN * KS / 8, kStep = kUnitsA + kUnitsB;
   static constexpr int kLds = kBuffers * kStep;
@@ -960,13 +980,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
   const Slab sl = slab_rows(g, rows, slab, KS);
   const int steps = (int)((sl.r1 - sl.r0 + KS - 1) / KS);
   // fp32: sections of 256 rows into a total of their own, every other one negated, and so is the first of every other slab
-  f32x16 acc[kI][2], total[kPB > 1 ? kI : 1][2];
+  f32x16 acc[kI][2], total[Shape::kSections ? kI : 1][2];
 #pragma unroll
   for (int i = 0; i < kI; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       acc[i][j] = zero16();
-      if (kPB > 1) total[i][j] = zero16();
+      if (Shape::kSections) total[i][j] = zero16();
     }
   const bool want_sums = g.sums && m0 == 0;
   ColumnStager<EA, false, kTileM, KS, kT> sa;
@@ -984,17 +1004,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
     if (product) sa.load(g.a, all - (long long)step * KS);
     sb.load(g.b, all - (long long)step * KS);
   };
-  auto sign_of = [&](int step) { return ((step / kHold) ^ slab) & 1 ? -1.f : 1.f; };
+  auto sign_of = [&](int step) { return Shape::kSections && ((step / kHold) ^ slab) & 1 ? -1.f : 1.f; };
   auto stash = [&](int step, u32x4* A) {
     const int left = (int)min(all - (long long)step * KS, (long long)KS);
     sa.mask(left);
     sb.mask(left);
     if (product) sa.store(A, 1.f);
     sb.store(A + Shape::kUnitsA, sign_of(step));
-    if (want_sums) sb.add_columns(sums);
+    if constexpr (!(kPB == 2)) if (want_sums) sb.add_columns(sums);
   };
   auto section = [&](int step) {
-    if constexpr (kPB > 1) {
+    if constexpr (Shape::kSections) {
       if (step % kHold == kHold - 1 || step + 1 == steps) add_section<kI>(total, acc, sign_of(step));
     }
   };
@@ -1033,7 +1053,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_kernel(const WeightArgs
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int n = n0 + wn * 64 + j * 32 + 8 * q + 4 * lh;
-        const f32x16& s = kPB > 1 ? total[kPB > 1 ? i : 0][j] : acc[i][j];
+        const f32x16& s = Shape::kSections ? total[Shape::kSections ? i : 0][j] : acc[i][j];
         float* p = P + (size_t)m * g.N + n;
         if (m < g.M && n < g.N) {
           if (quads) {
@@ -1078,7 +1098,7 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const WeightArgs g, 
       float x[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) x[u] = p[u * stride];
-      if constexpr (EB::kPieces > 1) {
+      if constexpr (EB::kBytes == 4) {
         float probe = 0.f;
 #pragma unroll
         for (int u = 0; u < 8; ++u) probe = fmaf(x[u], 0.f, probe);
@@ -1208,7 +1228,7 @@ template <class E, class EX, bool kDz>
 hipError_t weight(const WeightArgs& w, const DenseBackArgs& a, float* db, hipStream_t s) {
   hipError_t e;
   if constexpr (kDz && E::kPieces == 1) e = weight_tiles<E, EX, kDz, 4>(w, s);
-  else e = eight_weight_waves(w.N, E::kPieces == 1, kDz) ? weight_tiles<E, EX, kDz, 8>(w, s) : weight_tiles<E, EX, kDz, 4>(w, s);
+  else e = eight_weight_waves(w.N, E::kBytes == 2, kDz && E::kPieces != 2) ? weight_tiles<E, EX, kDz, 8>(w, s) : weight_tiles<E, EX, kDz, 4>(w, s);
   if (e != hipSuccess) return e;
   const long long total = (long long)w.M * w.N + w.N, most = (long long)a.n_cu * 8, want = (total + 255) / 256;
   hipLaunchKernelGGL((weight_reduce_kernel<EX, E, kDz>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, w,
@@ -1231,8 +1251,8 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
   float* db = a.db;
   if (smooth(a.act)) {
     char* out = reinterpret_cast<char*>(workspace);
-    workspace += dense_dz_floats(a.rows, a.N, a.bf16);
-    SlopeArgs g{a.rows, a.N, a.act, dz.p[0], a.lddy, dz.z, a.ldz, out, a.db ? workspace : nullptr, slope_blocks(a.rows, a.n_cu)};
+    workspace += dense_dz_floats(a.rows, a.N);
+    SlopeArgs g{a.rows, a.N, a.act, dz.p[0], a.lddy, dz.z, a.ldz, out, a.bf16 && !a.round_dz, a.db ? workspace : nullptr, slope_blocks(a.rows, a.n_cu)};
     workspace += (size_t)g.row_blocks * a.N;
     const bool wide = a.N % kWide == 0;
     const int columns = 32 * (wide ? kWide : 1), cb = (a.N + columns - 1) / columns;
@@ -1243,6 +1263,7 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     dz.p[0] = out;
     dz.z = nullptr;
     dz.ld = a.N;
+    if (g.pair) dz.p[1] = out + a.rows * a.N * 2;
   }
   hipError_t e = hipSuccess;
   if (a.dX && a.rows > 0) {
@@ -1252,7 +1273,7 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     g.b.ld = a.ldw;
     g.b.rows = K;
     g.b.cols = g.b.d = a.N;
-    g.K = a.N;
+    g.K = dz.p[1] ? 2 * a.N : a.N;
     g.N = K;
     g.act = DC_ACT_NONE;
     g.Y = static_cast<char*>(a.dX);
@@ -1278,6 +1299,13 @@ hipError_t dense_back(const DenseBackArgs& a, hipStream_t s) {
     w.S = slabs_of(a.rows, K, a.N, a.bf16, a.act, a.n_cu);
     w.part = workspace;
     w.sums = db != nullptr;
+    if constexpr (E::kBytes == 2 && !kDz) {
+      if (dz.p[1]) {
+        w.b.z = dz.p[1];
+        w.b.ldz = a.N;
+        return a.kept.code ? weight<Bf16Pair, Kept, true>(w, a, db, s) : weight<Bf16Pair, E, true>(w, a, db, s);
+      }
+    }
     e = a.kept.code ? weight<E, Kept, kDz>(w, a, db, s) : weight<E, E, kDz>(w, a, db, s);
   }
   return e;
@@ -1290,12 +1318,12 @@ hipError_t launch_dense(const DenseArgs& a, hipStream_t s) {
   return a.bf16 ? dense<Bf16>(a, s) : dense<F32>(a, s);
 }
 
-size_t dense_dz_floats(long long rows, int N, int bf16) {
-  return ((size_t)rows * N * (bf16 ? 2 : 4) + 15) / 16 * 4;
+size_t dense_dz_floats(long long rows, int N) {
+  return ((size_t)rows * N * 4 + 15) / 16 * 4;
 }
 size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu) {
   size_t n = (size_t)slabs_of(rows, K, N, bf16, act, n_cu) * ((size_t)K * N + N);
-  if (smooth(act)) n += dense_dz_floats(rows, N, bf16) + (size_t)slope_blocks(rows, n_cu) * N;
+  if (smooth(act)) n += dense_dz_floats(rows, N) + (size_t)slope_blocks(rows, n_cu) * N;
   return n;
 }
 

@@ -135,6 +135,7 @@ hipError_t launch_dense(const DenseArgs& a, hipStream_t s);
 struct DenseBackArgs {
   long long rows;
   int K, N, bf16, act;
+  int round_dz;                  // bf16, GELU and SiLU: dZ as one bf16 number, else as the sum of two
   const void* dY;
   long long lddy;
   const void* Z;                 // act other than none
@@ -153,7 +154,7 @@ struct DenseBackArgs {
   int n_cu;
 };
 size_t dense_back_floats(long long rows, int K, int N, int bf16, int act, int n_cu);
-size_t dense_dz_floats(long long rows, int N, int bf16);    // of them, dZ of a smooth activation in the storage type
+size_t dense_dz_floats(long long rows, int N);              // of them, dZ of a smooth activation: fp32, or two bf16 numbers
 hipError_t launch_dense_back(const DenseBackArgs& a, hipStream_t s);
 
 // ---- norm over the rows of each graph ----

@@ -247,6 +247,70 @@ def test_dense_backward(B, ev, dtype, shape, name, kept):
         assert [a is not None for a in alone] == [k == i for k in range(3)] and torch.equal(alone[i], got[i])
 
 
+@pytest.mark.parametrize("shape", [(1, 256, 256), (3, 5, 7), (17, 384, 128), (127, 129, 131), (515, 40, 24), (64, 1031, 8), (9001, 201, 139), (2203, 513, 8),
+                                   (40001, 4, 8), (17003, 65, 40), (8200, 256, 256), (33001, 24, 32), (12000, 300, 520)])
+@pytest.mark.parametrize("name,kept", [("gelu", False), ("silu", True)])
+def test_dense_backward_holds_dz_in_16_bits(B, ev, shape, name, kept):
+    """bf16 and a smooth activation: dx and dw are off by their own rounding and what fp32 would be off by, unless the caller
+    has dz rounded."""
+    t, (rows, K, N) = torch.bfloat16, shape
+    x, w, dy, z = rand(1, rows, K).to(t), (rand(2, K, N) / math.sqrt(K)).to(t), rand(3, rows, N).to(t), rand(4, rows, N).to(t)
+    xd = x.cuda()
+    if kept:
+        xd = ev.keep_rows(xd)
+        x = ev.restore_rows(xd, torch.float32).cpu()
+    d = dy.double()
+    dz = d * slope(z.double(), name)
+    # evaluating the slope as in fp32; the second number's own rounding, 2^-8 of 2^-8
+    edz = d.abs() * 16 * U * (1 + z.double().abs()) + 2.0 ** -16 * dz.abs()
+    aw, ax = w.double().abs(), x.double().abs()
+    dx, dw = dz @ w.double().t(), x.double().t() @ dz
+    # two instructions per 16 indices
+    tx = edz @ aw.t() + (3 * 2 * (N // 16 + 1) + 2) * U * (dz.abs() @ aw.t()) + (R(t) + U) * dx.abs()
+    sections = 2 * 3 * (rows // 128 + 96) + 4              # a slab's instructions (of eight slabs at least), then the slabs
+    tw = ax.t() @ edz + sections * U * (ax.t() @ dz.abs()) + (R(t) + U) * dw.abs()
+    got = ev.dense_backward(dy.cuda(), xd, w.cuda(), name, z.cuda())
+    close(got[0], dx, tx, "dx")
+    close(got[1], dw, tw, "dw")
+    less = ev.dense_backward(dy.cuda(), xd, w.cuda(), name, z.cuda(), round_dz=True)
+    for a, (want, tol), what in zip(less, backward_reference(dy, x, w, z, name, t), ("dx", "dw", "db")):
+        close(a, want, tol, what)
+    assert torch.equal(less[2], got[2])
+    # the other calls do not go by it
+    for other, u in ((name, torch.float32), ("relu", t), ("none", t)):
+        args = [dy.to(u).cuda(), xd if kept else xd.to(u), w.to(u).cuda(), other, None if other == "none" else z.to(u).cuda()]
+        assert all(torch.equal(a, b) for a, b in zip(ev.dense_backward(*args), ev.dense_backward(*args, round_dz=True)))
+
+
+@pytest.mark.parametrize("rows", [40, 9000])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan, "largest"])
+def test_dense_backward_of_what_is_not_finite_in_two_numbers(ev, rows, bad):
+    """A gradient that is not finite, or rounds to what is not, reaches its row of dx and its column of dw as with one number."""
+    t, K, N = torch.bfloat16, 64, 32
+    x, w, dy = rand(1, rows, K).to(t).cuda(), (1 + rand(2, K, N).abs()).to(t).cuda(), rand(3, rows, N).to(t).cuda()
+    z = torch.full((rows, N), 30.0, dtype=t, device="cuda")             # a slope of one
+    dy[7, 5] = torch.finfo(t).max if bad == "largest" else bad
+    if bad == "largest":
+        z[7, 5] = 1.2890625                                              # a slope of 1.0023: 3.397e38, which bf16 does not have
+    whole, rounded = (ev.dense_backward(dy, x, w, "silu", z, round_dz=r) for r in (False, True))
+    for a, b in zip(whole, rounded):
+        assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.isinf(a), torch.isinf(b))
+        assert torch.equal(a[torch.isinf(a)], b[torch.isinf(b)])
+    fine = torch.ones(rows, dtype=torch.bool)
+    fine[7] = False
+    assert torch.isfinite(whole[0][fine]).all() and not torch.isfinite(whole[0][7]).any()
+
+
+def test_dense_backward_refuses_an_unknown_dz(B, ev):
+    x = torch.zeros(4, 8, device="cuda")
+    w, dw, ws = torch.zeros(8, 8, device="cuda"), torch.zeros(8, 8, device="cuda"), torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    args = dict(dtype=B.DC_BF16, act=3, rows=4, n_in=8, n_out=8, dY=x.data_ptr(), lddy=8, Z=x.data_ptr(), ldz=8, X=x.data_ptr(), ldx=8,
+                W=w.data_ptr(), ldw=8, dW=dw.data_ptr(), lddw=8, workspace=ws.data_ptr(), workspace_bytes=ws.numel())
+    for dz in (-1, 2):
+        assert B.dc_dense_backward(ev.ctx, B.DcDenseBackwardArgs(**args, dz=dz)) == B.DC_ERR_INVALID_ARG
+        assert "DC_DZ" in B.dc_last_error(ev.ctx)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(33001, 24, 32), (9001, 201, 139), (4501, 255, 70), (7003, 131, 129), (3001, 390, 1031), (2203, 513, 8),
                                    (40001, 4, 8), (17003, 65, 40), (9007, 129, 33), (8200, 256, 256), (4100, 260, 9)])
