@@ -436,7 +436,8 @@ dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* h
  *
  * The parts that layers of deep estimators are made of, on device arrays of the caller: rows of `ld` elements each, in
  * the storage type of the call (fp32 or bf16, whatever the context's own type is); statistics, biases and the gradients
- * of vectors are fp32.  Sums are formed in fp32 or more.  The calls take the context for its device and its error text;
+ * of vectors are fp32.  Sums are formed in fp32 or more; of DC_F32 operands of products what lies below about 2^-134 is
+ * left out (numbers from 2^-110 on are whole).  The calls take the context for its device and its error text;
  * none uses its scratch, so calls on different streams may overlap as long as their arrays and workspaces are their
  * own.  They allocate nothing and do not synchronise, and may be captured into a graph.  Work is enqueued on
  * `stream`, a stream of the context's device, whatever device is current.  An array of outputs may be null where
@@ -449,9 +450,9 @@ typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 
 /* GELU is z (1 + erf(z / sqrt 2)) / 2, SiLU z / (1 + e^-z). */
 
 /* Rows kept in 8 bits for a backward pass.  Per row and 32 columns (the last block may be short): m = max |x|, e = the
- * smallest integer of [-126, 121] with m <= 127 * 2^e, code = x * 2^-e rounded to nearest even within +-127, and +-1
- * where x is not zero but would round to it; exponent = e + 127.  The value kept is code * 2^e: off by at most half a step
- * 2^e, a whole one where |x| is below half of it; its sign is x's.  A block that holds a number that is not finite
+ * smallest integer of [-126, 121] with m <= 127 * 2^e (121 if there is none), code = x * 2^-e rounded to nearest even within
+ * +-127, and +-1 where x is not zero but would round to it; exponent = e + 127.  The value kept is code * 2^e: off by at
+ * most half a step 2^e, a whole one where |x| is below half of it or above 127 * 2^121; its sign is x's.  A block that holds a number that is not finite
  * has exponent 255 and only NaN.  code [rows, 32 * ceil(cols / 32)] (behind the last column: zeros), exponent
  * [rows, ceil(cols / 32)].                                                                                          */
 typedef struct {

@@ -12,7 +12,9 @@
 // Of x itself the two terms of v would be up to 2^46 times v (values may lie 2^23 times their spread from zero), and their
 // rounding some percent of it.  Four instructions a value, which the loads hide.  mu is taken in two parts, the fp32 number that
 // is returned and what it lacks, else a value next to mu would be off by mu's rounding; the second pass has two instructions a
-// value in front of the activation: (gamma r) (x - mu) + (beta - (gamma r) lacks).
+// value in front of the activation: (gamma r) (x - mu) + (beta - (gamma r) lacks).  The gradient's sums are formed of a vector's
+// values in fp32 and of the vectors in 64 bits; those of gamma and beta of 64 rows of a thread in fp32, of a workgroup's rows in
+// 64 bits, rounded to fp32, and of the workgroups in 64 bits again.
 // Measured: forward over 4096 graphs of 1390 rows, 256 channels in bf16, SiLU, 1.395 ms (4.2 TB/s; a copy 4.87); gradient over
 // 52901 graphs of 9 rows, 256 channels in fp32, x as kept rows, 0.351 ms (3.1 TB/s).
 // Graphs of more than long_rows rows would keep one workgroup busy while the others are done: the kernel of the short graphs

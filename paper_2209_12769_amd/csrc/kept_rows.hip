@@ -2,7 +2,7 @@
 //
 // Per row and 32 columns: m = max |x|, e = the smallest integer of [-126, 121] with m <= 127 * 2^e, codes
 // q = x * 2^-e rounded to nearest even within +-127, and +-1 where x is not zero but would round to it (so that the
-// sign, and with it ReLU's derivative, survives).  Off by at most half a step 2^e (a whole one for |x| below half of it).
+// sign, and with it ReLU's derivative, survives).  Off by at most half a step 2^e (a whole one for |x| below half of it or above 127 * 2^121).
 // The scale is a power of two so that q * 2^e has at most seven significant bits: it is a bf16 number, and a
 // product with kept rows needs one exact operand on the bf16 matrix cores where fp32 rows need three pieces.  A finer
 // scale (m / 127) would gain half a bit on average and lose that.

@@ -12,7 +12,8 @@ __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
 // The standard normal distribution at -|z| is e^(-z^2 / 2) times a smooth function of |z|, here a polynomial of degree 8 in
-// t = 1 / (1 + p |z|) without a constant, fitted for the smallest largest relative error over 0 <= |z| <= 14 (1.3e-7).  GELU
+// t = 1 / (1 + p |z|) without a constant: the form of Abramowitz and Stegun 26.2.17 and its p, with three more
+// coefficients, fitted for the smallest largest relative error over 0 <= |z| <= 14 (1.3e-7).  GELU
 // by it is off by at most 4.9 roundings of |z|, and 0.5 z (1 + erf) in fp32 by up to 5.8, at about twice the
 // instructions: those of the library's error function bound the norms with GELU and took 45 us of 0.33 ms for a layer of
 // 27 M outputs.
