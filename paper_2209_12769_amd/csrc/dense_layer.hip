@@ -721,7 +721,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_rows_kernel(const ProductArgs
 // time before the sums go through LDS.
 // Measured: bf16 2000003 x 768 -> 256 with residual 1.25 ms (4.1 TB/s, 630 TFLOP/s; library product alone 0.97 ms); fp32
 // 196311 x 201 -> 139 with GELU, residual and Z 0.212 ms (matrix cores 25 % busy; the rest is conversions, the
-// epilogue's instructions and waiting); dX of 524309 x 256 -> 768 in bf16 0.42 ms, of two arrays of dZ 0.65 ms (630 TFLOP/s).
+// epilogue's instructions and waiting); dX of 524309 x 256 -> 768 in bf16 0.36 ms, of two arrays of dZ 0.56 ms (740 TFLOP/s).
 template <class E, int kWaves, bool kShort>
 struct ProductShape {
   static constexpr int kI = (E::kPieces == 1 ? 4 : 2) / (kShort ? 2 : 1), kTileM = 64 * kI, kTileN = 32 * kWaves, KS = E::kPieces == 1 ? 64 : 32;
@@ -952,7 +952,7 @@ __device__ __forceinline__ Slab slab_rows(const WeightArgs& g, long long rows, i
   return {r0, min(r0 + per, rows)};
 }
 // Tiles of dW: 64 kI x 32 kWaves, as above; every tile of a slab loads the slab's rows, so that wide ones load less.  Measured:
-// 524309 rows, 768 x 256 in bf16 0.33 ms (620 TFLOP/s), with dZ in two numbers 0.50 ms (820 TFLOP/s); 474011 rows, 384 x 128, kept rows times fp32 ones 0.35 ms.
+// 524309 rows, 768 x 256 in bf16 0.29 ms (710 TFLOP/s), with dZ in two numbers 0.41 ms (1000 TFLOP/s); 474011 rows, 384 x 128, kept rows times fp32 ones 0.32 ms.
 template <class EA, class EB, int kWaves>
 struct WeightShape {
   static constexpr int KS = EB::kPieces == 1 ? 64 : 32, kI = EB::kBytes == 2 ? kWaves / 2 : 2;
