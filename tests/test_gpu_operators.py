@@ -247,6 +247,14 @@ def test_dense_backward(B, ev, dtype, shape, name, kept):
         assert [a is not None for a in alone] == [k == i for k in range(3)] and torch.equal(alone[i], got[i])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 65536, 40), (5, 24, 65536), (600, 20001, 9), (300, 9, 20001)])
+@pytest.mark.parametrize("name,kept", [("relu", True), ("gelu", False)])
+def test_dense_of_the_widest_layers(B, ev, dtype, shape, name, kept):
+    test_dense(ev, dtype, shape, name)
+    test_dense_backward(B, ev, dtype, shape, name, kept)
+
+
 @pytest.mark.parametrize("shape", [(1, 256, 256), (3, 5, 7), (17, 384, 128), (127, 129, 131), (515, 40, 24), (64, 1031, 8), (9001, 201, 139), (2203, 513, 8),
                                    (40001, 4, 8), (17003, 65, 40), (8200, 256, 256), (33001, 24, 32), (12000, 300, 520)])
 @pytest.mark.parametrize("name,kept", [("gelu", False), ("silu", True)])
@@ -798,6 +806,33 @@ def test_operators_on_another_stream_and_in_a_graph(ev):
             assert all(torch.equal(a, b) for a, b in zip(out, want)), k
 
 
+def test_bf16_gradients_in_a_graph(ev):
+    """dz in two numbers and in one, and a norm far from zero, captured together and replayed with eager work in between."""
+    s, C, G, N, t = [900, 2, 0, 1700, 40] * 2, 64, 4, 96, torch.bfloat16
+    x, gamma, beta = norm_inputs(s, C, "bf16")
+    off, w, gy = offsets(s), (rand(7, C, N) / 8).to(t).cuda(), rand(9, sum(s), N).to(t).cuda()
+    xs, gd, bd = x.cuda(), gamma.cuda(), beta.cuda()
+
+    def step():
+        u, mean, rstd = ev.graph_norm(xs, off, G, gd, bd, EPS, "silu")
+        _, pre = ev.dense(u, w, None, "gelu", want_pre=True)
+        out = (mean, rstd)
+        for rounded in (False, True):
+            du, dw, db = ev.dense_backward(gy, u, w, "gelu", pre, round_dz=rounded)
+            out += (dw, db) + ev.graph_norm_backward(du, xs, off, G, gd, bd, mean, rstd, "silu")
+        return out
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for k in range(4):
+        xs.copy_(x.cuda() * (1 + k) + 50 * k)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, step())), k
+        torch.cuda.synchronize()
+
+
 def test_results_do_not_depend_on_what_else_is_there(ev):
     """The same call twice, and the rows of a graph next to other graphs: the same bits."""
     s, C, G = [40, 700, 3, 5000], 64, 8
@@ -839,6 +874,24 @@ def test_graph_norm_in_slabs_of_waves(ev, dtype, sizes, C, G):
     dy, dres = rand(9, sum(sizes), C).to(TYPES[dtype]), rand(10, sum(sizes), C).to(TYPES[dtype])
     ref = norm_back_reference(x, dy, dres, sizes, G, gamma, beta, got[1].cpu(), got[2].cpu(), "gelu", TYPES[dtype])
     back = ev.graph_norm_backward(dy.cuda(), x.cuda(), off, G, gamma.cuda(), beta.cuda(), got[1], got[2], "gelu", dres.cuda())
+    for g, (want, tol), what in zip(back, ref, ("dx", "dgamma", "dbeta")):
+        close(g, want, tol, what)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("C,G", [(8192, 16), (8184, 24), (1023, 3), (2048, 2048)])
+def test_graph_norm_of_wide_rows(ev, dtype, C, G, odd):
+    """Channels up to the most there may be, groups of one channel to 512; rows that no vector of channels fits (odd)."""
+    sizes, t = [3, 0, 1300, 40], TYPES[dtype]
+    x, gamma, beta = norm_inputs(sizes, C, dtype)
+    off, ld = offsets(sizes), C + (5 if odd else 0)
+    place = lambda v: off_grid(v, ld, 1 if odd else 0)
+    got = ev.graph_norm(place(x), off, G, gamma.cuda(), beta.cuda(), EPS, "silu", out=place(x))
+    check_norm(ev, x, sizes, G, gamma, beta, "silu", dtype, got)
+    dy = rand(9, sum(sizes), C).to(t)
+    ref = norm_back_reference(x, dy, None, sizes, G, gamma, beta, got[1].cpu(), got[2].cpu(), "silu", t)
+    back = ev.graph_norm_backward(place(dy), place(x), off, G, gamma.cuda(), beta.cuda(), got[1], got[2], "silu", out=place(dy))
     for g, (want, tol), what in zip(back, ref, ("dx", "dgamma", "dbeta")):
         close(g, want, tol, what)
 
