@@ -538,7 +538,8 @@ typedef struct {
   void* Y;                  /* [rows, channels]; may be X                                 */
   int64_t ldy;
   /* backward only: u = gamma dY act'(.), xh = (x - mean) rstd,
-   * dX = rstd (u - mean u - xh mean(u xh)) + dres, dgamma = sum dY act'(.) xh, dbeta = sum dY act'(.)  */
+   * dX = rstd (u - mean u - xh mean(u xh)) + dres, dgamma = sum dY act'(.) xh, dbeta = sum dY act'(.)
+   * by mean and rstd as they are given: their rounding to fp32 moves xh by up to 2^-24 |mean| rstd        */
   const dc_kept_rows* kept; /* x as kept rows, or null                                    */
   const void* dY;
   int64_t lddy;
