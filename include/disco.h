@@ -32,6 +32,9 @@
  *   dc_dense, dc_graph_norm, dc_keep_rows   the parts of deep estimators one by one, with
  *                       their gradients: a dense layer with bias, activation and residual,
  *                       a norm over the rows of each graph, rows kept in 8 bits.
+ *   dc_embed_rows, dc_row_norm, dc_adamw   what a training loop of one's own needs around
+ *                       them: rows looked up by kind and a norm over the channels of each
+ *                       row, with their gradients, and an AdamW step over many tensors.
  *
  * Conventions
  *  - Every call returns a dc_status; nothing throws or aborts.
@@ -556,6 +559,117 @@ size_t dc_graph_norm_bytes(const dc_ctx* ctx, int64_t rows, int32_t n_graphs, in
                            int32_t backward);
 dc_status dc_graph_norm(dc_ctx* ctx, const dc_graph_norm_args* args, void* stream);
 dc_status dc_graph_norm_backward(dc_ctx* ctx, const dc_graph_norm_args* args, void* stream);
+
+/* Norm over the channels of each row, with an activation.  Per row:
+ *   mean, rstd = 1 / sqrt(variance + eps);  y = act(gamma (x - mean) rstd + beta)
+ * Both are returned rounded to fp32; y takes the mean as it was before.  The row's sum and the squares of x - mean have to be
+ * fp32 numbers (values below about 10^18 in size); a row that has others, or a number that is not finite, has NaN or infinities
+ * itself, and no other row.  Channels are at most 16384.  The same call gives the same bits.                           */
+typedef struct {
+  int32_t dtype, act;
+  int64_t rows;
+  int32_t channels;
+  float eps;                /* > 0; not read by the backward                              */
+  const void* X;            /* [rows, channels]; backward: null with kept                 */
+  int64_t ldx;
+  const float* gamma;       /* [channels], or null for 1                                  */
+  const float* beta;        /* [channels], or null for 0                                  */
+  float* mean;              /* [rows]: written by the forward (null together with rstd if no backward follows), read by */
+  float* rstd;              /* the backward                                               */
+  void* Y;                  /* [rows, channels]; may be X                                 */
+  int64_t ldy;
+  /* backward only: u = gamma dY act'(.), xh = (x - mean) rstd,
+   * dX = rstd (u - mean u - xh mean(u xh)) + dres, dgamma = sum dY act'(.) xh, dbeta = sum dY act'(.)
+   * by mean and rstd as they are given                                                   */
+  const dc_kept_rows* kept; /* x as kept rows, or null                                    */
+  const void* dY;
+  int64_t lddy;
+  const void* dres;         /* [rows, channels] or null: the gradient that goes past the norm */
+  int64_t lddres;
+  void* dX;                 /* may be dY, dres or X                                       */
+  int64_t lddx;
+  float* dgamma;            /* [channels], null together with dbeta                       */
+  float* dbeta;
+  void* workspace;          /* dev, dc_row_norm_bytes() of them; not taken without dgamma */
+  size_t workspace_bytes;
+} dc_row_norm_args;
+size_t dc_row_norm_bytes(const dc_ctx* ctx, int64_t rows, int32_t channels);   /* of the backward */
+dc_status dc_row_norm(dc_ctx* ctx, const dc_row_norm_args* args, void* stream);
+dc_status dc_row_norm_backward(dc_ctx* ctx, const dc_row_norm_args* args, void* stream);
+
+/* Rows by kind: y_i = scale * table[id_i], a row of zeros where id_i is -1 (a row that stands for nothing); rounded once.  The
+ * gradient of the table: dtable_k = scale * sum of dY_i over the rows with id_i = k, zeros where there is none, all of it written;
+ * formed in the order of the rows, so the same call gives the same bits.  An id outside [-1, kinds) counts as -1, and dc_check
+ * reports DC_ERR_INVALID_ARG.                                                                                        */
+typedef struct {
+  int32_t dtype;
+  int64_t rows;
+  int32_t kinds, channels;  /* at least 1 each, channels at most 65536                    */
+  float scale;
+  const int32_t* id;        /* dev [rows]                                                 */
+  const void* table;        /* [kinds, channels]; not read by the backward                */
+  int64_t ld_table;
+  void* Y;                  /* [rows, channels]                                           */
+  int64_t ldy;
+  /* backward only */
+  const void* dY;           /* [rows, channels]                                           */
+  int64_t lddy;
+  void* dtable;             /* [kinds, channels]                                          */
+  int64_t ld_dtable;
+  void* workspace;          /* dev, dc_embed_rows_bytes() of them                         */
+  size_t workspace_bytes;
+} dc_embed_rows_args;
+size_t dc_embed_rows_bytes(const dc_ctx* ctx, int64_t rows, int32_t kinds, int32_t channels);   /* of the backward */
+dc_status dc_embed_rows(dc_ctx* ctx, const dc_embed_rows_args* args, void* stream);
+dc_status dc_embed_rows_backward(dc_ctx* ctx, const dc_embed_rows_args* args, void* stream);
+
+/* One AdamW step over many tensors.  With t the number of this step, from 1, and g the gradient times *grad_scale, in fp32:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   w = w - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay w)
+ * A parameter p is fp32 (w itself) or bf16: then w is the value of p and of 16 more bits in `low`, p is w rounded to bf16 (halves
+ * away from zero), and nothing of w is lost.  A caller who writes a bf16 parameter anew clears its places of `low`, or has a w
+ * up to half a rounding beside it.
+ * The state of all tensors lies in arrays of `total` places, a multiple of 128; tensor k has the places at_k .. at_k + n_k - 1, at_k
+ * a multiple of 128, ascending.  All of them zero is the state before the first step; places between tensors stay zero.
+ *   DC_MOMENTS_F32    m, v: fp32
+ *   DC_MOMENTS_8BIT   m, v: 8-bit codes with an exponent byte E for each 128 places, x = E - 127.  A code is s eeee fff (m) or
+ *                     eeeee fff (v), of the value (8 + fff) 2^(eeee - 1) 2^(x - 17), or 2^(x - 33) for v, without the 8 and with
+ *                     eeee as 1 where it is 0; x is the smallest with 1.875 2^x at least the block's largest value (m: -126 at
+ *                     least, v: -116; 127 at most).  E = 255: the block holds a number that is not finite, all of it reads back as
+ *                     NaN.  Rounded up or down by chance, 16 bits r for m and for v: the code is floor(value in steps +
+ *                     (2 r + 1) / 2^17), v at least 1 if it is not zero; mix the output function of splitmix64, place q / 2 of the
+ *                     state takes from mix(mix(seed ^ mix(t)) + (q / 2) 0xD1342543DE82EF95) the low 32 bits (q even) or the high
+ *                     ones, of them the low half for m and the high half for v.  m, v and g^2 (1 - beta2) are formed by
+ *                     operations of fp32 rounded one by one, w from m and v before they are rounded to codes.
+ * Tensors and states may not overlap, gradients may be each other.  `tensors` is read before the call returns.  All
+ * tensors are one launch per 96 of them.                                                                             */
+enum { DC_MOMENTS_F32 = 0, DC_MOMENTS_8BIT = 1 };
+typedef struct {
+  void* p;                  /* dev [n], neighbours                                        */
+  const void* g;            /* dev [n], or null: the tensor and its state stay as they are */
+  int64_t n;
+  int64_t at;
+  int32_t p_dtype, g_dtype; /* dc_dtype                                                   */
+  double weight_decay;      /* >= 0                                                       */
+} dc_adamw_tensor;
+typedef struct {
+  int32_t moments, n_tensors;
+  const dc_adamw_tensor* tensors;   /* host [n_tensors]                                   */
+  int64_t total;            /* at most 2^38                                               */
+  void* m;                  /* dev [total], aligned to 16 bytes, as v and low             */
+  void* v;
+  uint8_t* m_exponent;      /* dev [total / 128], 8-bit moments only                      */
+  uint8_t* v_exponent;
+  uint16_t* low;            /* dev [total], null if no parameter is bf16                  */
+  int32_t* steps;           /* dev [2]: steps done, counted up by the call; 0 between calls */
+  const float* grad_scale;  /* dev [1], or null for 1                                     */
+  double lr, beta1, beta2, eps;     /* lr >= 0, betas in [0, 1), eps > 0 in fp32          */
+  uint64_t seed;
+} dc_adamw_args;
+dc_status dc_adamw(dc_ctx* ctx, const dc_adamw_args* args, void* stream);
+/* w, m and v of all tensors as fp32 values at their places, zeros behind each tensor's last up to the next multiple of 128: dev
+ * [total], aligned to 16 bytes, or null.  Reads p and the state only; gradients, lr, betas, eps, steps and seed do not count. */
+dc_status dc_adamw_values(dc_ctx* ctx, const dc_adamw_args* args, float* w, float* m, float* v, void* stream);
 
 /* dc_contract_graphs into context-owned buffers followed by dc_gnn_forward. */
 dc_status dc_eval_candidates(dc_ctx* ctx, int32_t n_cand, const int32_t* cand_graph, const int32_t* cand_off,

@@ -35,6 +35,7 @@ DC_KERNELS_EVERY_FUSED_OP = 2
 DC_DRAW_DEPENDENCY, DC_DRAW_OP = 0, 1
 DC_KEEP_F32, DC_KEEP_8BIT = 0, 1
 DC_DZ_WHOLE, DC_DZ_ROUNDED = 0, 1
+DC_MOMENTS_F32, DC_MOMENTS_8BIT = 0, 1
 DC_ACT_NONE, DC_ACT_RELU, DC_ACT_GELU, DC_ACT_SILU = 0, 1, 2, 3
 ACTIVATIONS = {"none": DC_ACT_NONE, "relu": DC_ACT_RELU, "gelu": DC_ACT_GELU, "silu": DC_ACT_SILU}
 STATUS_NAMES = {0: "DC_OK", 1: "DC_ERR_INVALID_ARG", 2: "DC_ERR_BAD_GRAPH", 3: "DC_ERR_BAD_PARTITION",
@@ -101,13 +102,47 @@ class DcGraphNormArgs(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+class DcRowNormArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("channels", C.c_int32), ("eps", C.c_float),
+                ("X", C.c_void_p), ("ldx", C.c_int64), ("gamma", C.c_void_p), ("beta", C.c_void_p), ("mean", C.c_void_p),
+                ("rstd", C.c_void_p), ("Y", C.c_void_p), ("ldy", C.c_int64), ("kept", C.POINTER(DcKeptRows)),
+                ("dY", C.c_void_p), ("lddy", C.c_int64), ("dres", C.c_void_p), ("lddres", C.c_int64), ("dX", C.c_void_p),
+                ("lddx", C.c_int64), ("dgamma", C.c_void_p), ("dbeta", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class DcEmbedRowsArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int64), ("kinds", C.c_int32), ("channels", C.c_int32), ("scale", C.c_float),
+                ("id", C.c_void_p), ("table", C.c_void_p), ("ld_table", C.c_int64), ("Y", C.c_void_p), ("ldy", C.c_int64),
+                ("dY", C.c_void_p), ("lddy", C.c_int64), ("dtable", C.c_void_p), ("ld_dtable", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class DcAdamwTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("n", C.c_int64), ("at", C.c_int64), ("p_dtype", C.c_int32),
+                ("g_dtype", C.c_int32), ("weight_decay", C.c_double)]
+
+
+class DcAdamwArgs(C.Structure):
+    _fields_ = [("moments", C.c_int32), ("n_tensors", C.c_int32), ("tensors", C.c_void_p), ("total", C.c_int64),
+                ("m", C.c_void_p), ("v", C.c_void_p), ("m_exponent", C.c_void_p), ("v_exponent", C.c_void_p),
+                ("low", C.c_void_p), ("steps", C.c_void_p), ("grad_scale", C.c_void_p), ("lr", C.c_double),
+                ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("seed", C.c_uint64)]
+
+
 # The same structs for the wrapper's calls, packed from values (native sizes and alignment).
 _KEPT = struct.Struct("@PPqq")
 _DENSE = struct.Struct("@iiqiiPqPqPPqPqPq")
 _DENSE_BACK = struct.Struct("@iiqiiPqPqPqPPqPqPqPPNi0q")
 _NORM = struct.Struct("@iiqiiifPPqPPPPPqPPqPqPqPPPN")
-assert [s.size for s in (_KEPT, _DENSE, _DENSE_BACK, _NORM)] == [
-    C.sizeof(s) for s in (DcKeptRows, DcDenseArgs, DcDenseBackwardArgs, DcGraphNormArgs)]
+_ROW_NORM = struct.Struct("@iiqifPqPPPPPqPPqPqPqPPPN")
+_EMBED = struct.Struct("@iqiifPPqPqPqPqPN")
+_ADAMW = struct.Struct("@iiPqPPPPPPPddddQ")
+_ADAMW_TENSOR = np.dtype([("p", np.uint64), ("g", np.uint64), ("n", np.int64), ("at", np.int64), ("p_dtype", np.int32),
+                          ("g_dtype", np.int32), ("weight_decay", np.float64)])
+assert [s.size for s in (_KEPT, _DENSE, _DENSE_BACK, _NORM, _ROW_NORM, _EMBED, _ADAMW)] == [
+    C.sizeof(s) for s in (DcKeptRows, DcDenseArgs, DcDenseBackwardArgs, DcGraphNormArgs, DcRowNormArgs, DcEmbedRowsArgs, DcAdamwArgs)]
+assert _ADAMW_TENSOR.itemsize == C.sizeof(DcAdamwTensor)
 
 
 class DiscoError(RuntimeError):
@@ -174,6 +209,16 @@ def lib():
         L.dc_graph_norm_bytes.restype = size
         L.dc_graph_norm.argtypes = [vp, vp, vp]
         L.dc_graph_norm_backward.argtypes = [vp, vp, vp]
+        L.dc_row_norm_bytes.argtypes = [vp, i64, i32]
+        L.dc_row_norm_bytes.restype = size
+        L.dc_row_norm.argtypes = [vp, vp, vp]
+        L.dc_row_norm_backward.argtypes = [vp, vp, vp]
+        L.dc_embed_rows_bytes.argtypes = [vp, i64, i32, i32]
+        L.dc_embed_rows_bytes.restype = size
+        L.dc_embed_rows.argtypes = [vp, vp, vp]
+        L.dc_embed_rows_backward.argtypes = [vp, vp, vp]
+        L.dc_adamw.argtypes = [vp, vp, vp]
+        L.dc_adamw_values.argtypes = [vp, vp, vp, vp, vp, vp]
         L.dc_check.argtypes = [vp, vp]
         L.dc_select_kernels.argtypes = [vp, i32]
         L.dc_last_totals.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64), vp]
@@ -186,7 +231,8 @@ def lib():
                   "dc_profile_end", "dc_set_profile", "dc_module_times", "dc_cost_candidates", "dc_last_fused_ops",
                   "dc_last_fused_op_repeats", "dc_walked_modules", "dc_search",
                   "dc_train_begin", "dc_select_kernels", "dc_fused_op_batch", "dc_loss_gradients", "dc_train_step", "dc_get_weights",
-                  "dc_set_layer_norms", "dc_get_layer_norms", "dc_train_keep", "dc_keep_rows", "dc_restore_rows", "dc_dense", "dc_dense_backward", "dc_graph_norm", "dc_graph_norm_backward"):
+                  "dc_set_layer_norms", "dc_get_layer_norms", "dc_train_keep", "dc_keep_rows", "dc_restore_rows", "dc_dense", "dc_dense_backward", "dc_graph_norm", "dc_graph_norm_backward",
+                  "dc_row_norm", "dc_row_norm_backward", "dc_embed_rows", "dc_embed_rows_backward", "dc_adamw", "dc_adamw_values"):
             getattr(L, n).restype = i32
         _lib = L
     return _lib
@@ -349,6 +395,38 @@ def dc_graph_norm_backward(ctx, args: DcGraphNormArgs, stream: int = 0) -> int:
     return lib().dc_graph_norm_backward(ctx, C.byref(args), stream)
 
 
+def dc_row_norm_bytes(ctx, rows: int, channels: int) -> int:
+    return int(lib().dc_row_norm_bytes(ctx, rows, channels))
+
+
+def dc_row_norm(ctx, args: DcRowNormArgs, stream: int = 0) -> int:
+    return lib().dc_row_norm(ctx, C.byref(args), stream)
+
+
+def dc_row_norm_backward(ctx, args: DcRowNormArgs, stream: int = 0) -> int:
+    return lib().dc_row_norm_backward(ctx, C.byref(args), stream)
+
+
+def dc_embed_rows_bytes(ctx, rows: int, kinds: int, channels: int) -> int:
+    return int(lib().dc_embed_rows_bytes(ctx, rows, kinds, channels))
+
+
+def dc_embed_rows(ctx, args: DcEmbedRowsArgs, stream: int = 0) -> int:
+    return lib().dc_embed_rows(ctx, C.byref(args), stream)
+
+
+def dc_embed_rows_backward(ctx, args: DcEmbedRowsArgs, stream: int = 0) -> int:
+    return lib().dc_embed_rows_backward(ctx, C.byref(args), stream)
+
+
+def dc_adamw(ctx, args: DcAdamwArgs, stream: int = 0) -> int:
+    return lib().dc_adamw(ctx, C.byref(args), stream)
+
+
+def dc_adamw_values(ctx, args: DcAdamwArgs, w_ptr, m_ptr, v_ptr, stream: int = 0) -> int:
+    return lib().dc_adamw_values(ctx, C.byref(args), w_ptr, m_ptr, v_ptr, stream)
+
+
 def dc_check(ctx, stream: int = 0) -> int:
     return lib().dc_check(ctx, stream)
 
@@ -424,6 +502,89 @@ class KeptRows:
     @property
     def rows(self) -> int:
         return int(self.code.shape[0])
+
+
+class AdamW:
+    """AdamW over many tensors in one call (see dc_adamw), made by Evaluator.adamw.
+
+    The state, device tensors of `total` places: m, v (float32, or uint8 codes with m_exponent and v_exponent for each 128
+    places), low (int16: the low halves of bfloat16 parameters), steps (int32: steps done, 0).  Tensor k has the places
+    at[k] .. at[k] + its elements.  Saved and restored as they are, they go on where they were.  lr, betas, eps and seed may be
+    changed between steps."""
+
+    def __init__(self, ev: "Evaluator", params, lr: float, betas, eps: float, weight_decay, states: str, seed: int):
+        torch = ev.torch
+        if states not in ("f32", "8bit"):
+            raise ValueError(f"states: 'f32' or '8bit', not {states!r}")
+        self.ev, self.params, self.states = ev, list(params), states
+        self.lr, self.betas, self.eps, self.seed = lr, tuple(betas), eps, seed
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * len(self.params)
+        if len(decay) != len(self.params):
+            raise ValueError("weight_decay: need a number, or one for every tensor")
+        self._table = np.zeros(len(self.params), _ADAMW_TENSOR)
+        self.at, total, half = [], 0, False
+        for k, p in enumerate(self.params):
+            if p.device != ev.device or p.dtype not in ev._types or not p.is_contiguous():
+                raise ValueError(f"tensor {k}: need contiguous float32 or bfloat16 on {ev.device}")
+            n = p.numel()
+            self._table[k] = (0, 0, n, total, ev._types[p.dtype], 0, decay[k])
+            self.at.append(total)
+            total += -(-n // 128) * 128
+            half = half or (p.dtype == torch.bfloat16 and n > 0)
+        self.total = total
+        self._shapes = [p.shape for p in self.params]
+        eight = states == "8bit"
+        with torch.no_grad():
+            self.m, self.v = (torch.zeros(total, dtype=torch.uint8 if eight else torch.float32, device=ev.device) for _ in range(2))
+            self.m_exponent, self.v_exponent = (torch.zeros(total // 128, dtype=torch.uint8, device=ev.device) if eight else None for _ in range(2))
+            self.low = torch.zeros(total, dtype=torch.int16, device=ev.device) if half else None
+            self.steps = torch.zeros(2, dtype=torch.int32, device=ev.device)
+
+    def _args(self, grad_scale: int) -> bytes:
+        table = self._table
+        table["p"] = [p.data_ptr() for p in self.params]
+        eight = self.m_exponent is not None
+        return _ADAMW.pack(DC_MOMENTS_8BIT if eight else DC_MOMENTS_F32, len(table), table.ctypes.data, self.total, self.m.data_ptr(),
+                           self.v.data_ptr(), self.m_exponent.data_ptr() if eight else 0, self.v_exponent.data_ptr() if eight else 0,
+                           0 if self.low is None else self.low.data_ptr(), self.steps.data_ptr(), grad_scale, self.lr, self.betas[0],
+                           self.betas[1], self.eps, self.seed)
+
+    def step(self, grads, grad_scale=None):
+        """One step with a gradient for every tensor (float32 or bfloat16, contiguous, its shape), None for tensors that stay as
+        they are.  grad_scale: a float32 device tensor of one number that the gradients are multiplied by."""
+        ev, types = self.ev, self.ev._types
+        index = ev.device.index
+        if len(grads) != len(self.params):
+            raise ValueError(f"need {len(self.params)} gradients, not {len(grads)}")
+        ptrs, codes = [], []
+        for k, g in enumerate(grads):
+            if g is None:
+                ptrs.append(0)
+                codes.append(0)
+                continue
+            code = types.get(g.dtype)
+            if code is None or g.shape != self._shapes[k] or g.get_device() != index or not g.is_contiguous():
+                raise ValueError(f"gradient {k}: need contiguous float32 or bfloat16 {tuple(self._shapes[k])} on {ev.device}")
+            ptrs.append(g.data_ptr())
+            codes.append(code)
+        self._table["g"] = ptrs
+        self._table["g_dtype"] = codes
+        args = self._args(0 if grad_scale is None else ev._vector(grad_scale.reshape(-1), "grad_scale", 1))
+        st = lib().dc_adamw(ev.ctx, args, ev._raw_stream())
+        if st:
+            ev._ok(st, "dc_adamw")
+
+    def values(self, which: str = "wmv"):
+        """The float32 values of the parameters (w) and moments (m, v) that `which` names, in its order, each a tensor of `total`
+        places."""
+        ev = self.ev
+        if not which or set(which) - set("wmv") or len(set(which)) != len(which):
+            raise ValueError(f"which: letters of 'wmv', each once, not {which!r}")
+        out = {c: ev.torch.empty(self.total, dtype=ev.torch.float32, device=ev.device) for c in which}
+        st = lib().dc_adamw_values(ev.ctx, self._args(0), *(out[c].data_ptr() if c in out else 0 for c in "wmv"), ev._raw_stream())
+        if st:
+            ev._ok(st, "dc_adamw_values")
+        return tuple(out[c] for c in which)
 
 
 class Evaluator:
@@ -807,6 +968,92 @@ class Evaluator:
         if st:
             self._ok(st, "dc_graph_norm_backward")
         return out, dgamma, dbeta
+
+    def row_norm(self, x, gamma=None, beta=None, eps: float = 1e-5, act: str = "none", out=None):
+        """(y, mean, rstd): the norm over the channels of each row, with an activation."""
+        rows, channels, ldx, dtype = self._rows(x, "x")
+        pg = 0 if gamma is None else self._vector(gamma, "gamma", channels)
+        pb = 0 if beta is None else self._vector(beta, "beta", channels)
+        if out is None:
+            out, ldy = self.torch.empty((rows, channels), dtype=x.dtype, device=self.device), channels
+        else:
+            ldy = self._like(out, "out", rows, channels, dtype)
+        mean, rstd = self.torch.empty((2, rows), dtype=self.torch.float32, device=self.device).unbind(0)
+        a = _ROW_NORM.pack(dtype, self._act(act), rows, channels, eps, x.data_ptr(), ldx, pg, pb, mean.data_ptr(), rstd.data_ptr(),
+                           out.data_ptr(), ldy, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+        st = lib().dc_row_norm(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_row_norm")
+        return out, mean, rstd
+
+    def row_norm_backward(self, dy, x, gamma, beta, mean, rstd, act: str = "none", residual=None, out=None):
+        """(dx, dgamma, dbeta) for the gradient dy at the result; `residual` is added to dx.  x: the rows, or KeptRows of
+        them; mean, rstd: what row_norm returned."""
+        rows, channels, lddy, dtype = self._rows(dy, "dy")
+        pg = 0 if gamma is None else self._vector(gamma, "gamma", channels)
+        pb = 0 if beta is None else self._vector(beta, "beta", channels)
+        pm, ps = self._vector(mean, "mean", rows), self._vector(rstd, "rstd", rows)
+        if out is None:
+            out, lddx = self.torch.empty((rows, channels), dtype=dy.dtype, device=self.device), channels
+        else:
+            lddx = self._like(out, "out", rows, channels, dtype)
+        px, ldx, kept = 0, 0, None
+        if isinstance(x, KeptRows):
+            kept = C.create_string_buffer(self._kept(x, rows, channels), _KEPT.size)
+        else:
+            px, ldx = x.data_ptr(), self._like(x, "x", rows, channels, dtype)
+        pr, ldr = (residual.data_ptr(), self._like(residual, "residual", rows, channels, dtype)) if residual is not None else (0, 0)
+        dgamma, dbeta = self.torch.empty((2, channels), dtype=self.torch.float32, device=self.device).unbind(0)
+        size = lib().dc_row_norm_bytes(self.ctx, rows, channels)
+        ws = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+        a = _ROW_NORM.pack(dtype, self._act(act), rows, channels, 0.0, px, ldx, pg, pb, pm, ps, 0, 0,
+                           0 if kept is None else C.addressof(kept), dy.data_ptr(), lddy, pr, ldr, out.data_ptr(), lddx,
+                           dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), size)
+        st = lib().dc_row_norm_backward(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_row_norm_backward")
+        return out, dgamma, dbeta
+
+    def _ids(self, ids, rows=None) -> int:
+        if ids.dim() != 1 or (rows is not None and ids.shape[0] != rows):
+            raise ValueError("ids: need one number for each row")
+        return self._vector(ids, "ids", ids.shape[0], self.torch.int32)
+
+    def embed_rows(self, ids, table, scale: float = 1.0, out=None):
+        """scale * table[ids], rows of zeros where an id is -1.  check() reports ids that are neither."""
+        kinds, channels, ldt, dtype = self._rows(table, "table")
+        pid, rows = self._ids(ids), ids.shape[0]
+        if out is None:
+            out, ldy = self.torch.empty((rows, channels), dtype=table.dtype, device=self.device), channels
+        else:
+            ldy = self._like(out, "out", rows, channels, dtype)
+        a = _EMBED.pack(dtype, rows, kinds, channels, scale, pid, table.data_ptr(), ldt, out.data_ptr(), ldy, 0, 0, 0, 0, 0, 0)
+        st = lib().dc_embed_rows(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_embed_rows")
+        return out
+
+    def embed_rows_backward(self, dy, ids, kinds: int, scale: float = 1.0, out=None):
+        """The gradient of embed_rows' table of `kinds` rows for the gradient dy at the result."""
+        rows, channels, lddy, dtype = self._rows(dy, "dy")
+        pid = self._ids(ids, rows)
+        if out is None:
+            out, ldt = self.torch.empty((kinds, channels), dtype=dy.dtype, device=self.device), channels
+        else:
+            ldt = self._like(out, "out", kinds, channels, dtype)
+        size = lib().dc_embed_rows_bytes(self.ctx, rows, kinds, channels)
+        ws = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+        a = _EMBED.pack(dtype, rows, kinds, channels, scale, pid, 0, 0, 0, 0, dy.data_ptr(), lddy, out.data_ptr(), ldt, ws.data_ptr(), size)
+        st = lib().dc_embed_rows_backward(self.ctx, a, self._raw_stream())
+        if st:
+            self._ok(st, "dc_embed_rows_backward")
+        return out
+
+    def adamw(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, states: str = "f32",
+              seed: int = 0) -> AdamW:
+        """An AdamW optimiser of the tensors `params` (float32 or bfloat16, updated in place), all of them in one call a step.
+        weight_decay: a number, or one for every tensor; states: moments in "f32" or "8bit", rounded by draws from `seed`."""
+        return AdamW(self, params, lr, betas, eps, weight_decay, states, seed)
 
     def get_weights(self):
         """(W_layers, b_layers, head) as host fp32 arrays in the layout of dc_set_weights."""

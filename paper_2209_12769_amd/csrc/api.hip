@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <new>
 #include <initializer_list>
 #include <string>
@@ -1864,6 +1865,328 @@ dc_status dc_graph_norm_backward(dc_ctx* ctx, const dc_graph_norm_args* args, vo
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
   return enqueue_result(ctx, launch_graph_norm_back(g, static_cast<hipStream_t>(stream)), "graph norm gradient launch");
+}
+
+namespace {
+dc_status row_norm_check(dc_ctx* ctx, const dc_row_norm_args* a, bool backward, RowNormArgs* g) {
+  if (!a) return fail(ctx, DC_ERR_INVALID_ARG, "null arguments");
+  dc_status st = shape_check(ctx, a->dtype, a->rows);
+  if (st != DC_OK) return st;
+  if (a->act < DC_ACT_NONE || a->act > DC_ACT_SILU) return fail(ctx, DC_ERR_INVALID_ARG, "unknown activation");
+  if (a->channels < 1) return fail(ctx, DC_ERR_INVALID_ARG, "need at least one channel");
+  if (a->channels > kRowNormMost) return fail(ctx, DC_ERR_UNSUPPORTED, "at most 16384 channels");
+  if (!backward && !(a->eps > 0.f)) return fail(ctx, DC_ERR_INVALID_ARG, "need eps > 0");
+  const int es = a->dtype == DC_BF16 ? 2 : 4;
+  if (backward ? (a->rows > 0 && (!a->mean || !a->rstd)) : !a->mean != !a->rstd) return fail(ctx, DC_ERR_INVALID_ARG, "null mean or rstd");
+  if (!at(a->mean, 4) || !at(a->rstd, 4) || !at(a->gamma, 4) || !at(a->beta, 4) || !at(a->dgamma, 4) || !at(a->dbeta, 4))
+    return fail(ctx, DC_ERR_INVALID_ARG, "statistics or vectors are not aligned to their elements");
+  const bool kept = backward && a->kept;
+  if (kept) st = kept_check(ctx, a->kept, a->rows, a->channels);
+  else st = array_check(ctx, a->X, a->ldx, a->rows, a->channels, es, "X");
+  if (st == DC_OK && !backward) st = array_check(ctx, a->Y, a->ldy, a->rows, a->channels, es, "Y");
+  if (st == DC_OK && backward) st = array_check(ctx, a->dY, a->lddy, a->rows, a->channels, es, "dY");
+  if (st == DC_OK && backward) st = array_check(ctx, a->dX, a->lddx, a->rows, a->channels, es, "dX");
+  if (st == DC_OK && backward && a->dres) st = array_check(ctx, a->dres, a->lddres, a->rows, a->channels, es, "dres");
+  if (st != DC_OK) return st;
+  if (backward && !a->dgamma != !a->dbeta) return fail(ctx, DC_ERR_INVALID_ARG, "dgamma and dbeta go together");
+  const size_t need = backward && a->dgamma ? dc_row_norm_bytes(ctx, a->rows, a->channels) : 0;
+  if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_row_norm_bytes");
+  if (need > 0 && !at(a->workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+  const int nb = (a->channels + kKeptBlock - 1) / kKeptBlock;
+  const int64_t vec = 4 * (int64_t)a->channels;
+  const Place X = rows_place("X", a->X, kept ? 0 : a->rows, a->channels, a->ldx, es),
+              code = rows_place("code", kept ? a->kept->code : nullptr, a->rows, nb * kKeptBlock, kept ? a->kept->ld_code : 0, 1),
+              exponent = rows_place("exponent", kept ? a->kept->exponent : nullptr, a->rows, nb, kept ? a->kept->ld_exponent : 0, 1),
+              gamma = vector_place("gamma", a->gamma, vec), beta = vector_place("beta", a->beta, vec),
+              mean = vector_place("mean", a->mean, 4 * a->rows), rstd = vector_place("rstd", a->rstd, 4 * a->rows);
+  if (!backward) {
+    const Place Y = rows_place("Y", a->Y, a->rows, a->channels, a->ldy, es);
+    st = lies_apart(ctx, Y, {X}, true);
+    if (st == DC_OK) st = lies_apart(ctx, Y, {gamma, beta, mean, rstd});
+    if (st == DC_OK) st = lies_apart(ctx, mean, {X, gamma, beta, rstd});
+    if (st == DC_OK) st = lies_apart(ctx, rstd, {X, gamma, beta});
+  } else {
+    const Place dY = rows_place("dY", a->dY, a->rows, a->channels, a->lddy, es), dX = rows_place("dX", a->dX, a->rows, a->channels, a->lddx, es),
+                dres = rows_place("dres", a->dres, a->rows, a->channels, a->lddres, es), dgamma = vector_place("dgamma", a->dgamma, vec),
+                dbeta = vector_place("dbeta", a->dbeta, vec), workspace = vector_place("the workspace", need > 0 ? a->workspace : nullptr, (int64_t)need);
+    st = lies_apart(ctx, dX, {X, dY, dres}, true);                 // dgamma and dbeta come last: what is only read has been by then
+    if (st == DC_OK) st = lies_apart(ctx, dX, {code, exponent, gamma, beta, mean, rstd, dgamma, dbeta});
+    if (st == DC_OK) st = lies_apart(ctx, dgamma, {dbeta});
+    if (st == DC_OK) st = lies_apart(ctx, workspace, {X, code, exponent, dY, dres, dX, gamma, beta, mean, rstd, dgamma, dbeta});
+  }
+  if (st != DC_OK) return st;
+  *g = RowNormArgs{};
+  g->rows = a->rows;
+  g->C = a->channels;
+  g->bf16 = a->dtype == DC_BF16;
+  g->act = a->act;
+  g->eps = a->eps;
+  g->X = a->X;
+  g->ldx = a->ldx;
+  g->gamma = a->gamma;
+  g->beta = a->beta;
+  g->mean = a->mean;
+  g->rstd = a->rstd;
+  g->n_cu = ctx->n_cu;
+  if (!backward) {
+    g->Y = a->Y;
+    g->ldy = a->ldy;
+    return DC_OK;
+  }
+  g->kept = kept_view(a->kept);
+  g->dY = a->dY;
+  g->lddy = a->lddy;
+  g->dRes = a->dres;
+  g->lddres = a->lddres;
+  g->dX = a->dX;
+  g->lddx = a->lddx;
+  g->dgamma = a->dgamma;
+  g->dbeta = a->dbeta;
+  g->workspace = static_cast<float*>(a->workspace);
+  return DC_OK;
+}
+
+dc_status embed_rows_check(dc_ctx* ctx, const dc_embed_rows_args* a, bool backward, EmbedArgs* g) {
+  if (!a) return fail(ctx, DC_ERR_INVALID_ARG, "null arguments");
+  dc_status st = shape_check(ctx, a->dtype, a->rows);
+  if (st != DC_OK) return st;
+  if (a->kinds < 1 || a->channels < 1) return fail(ctx, DC_ERR_INVALID_ARG, "need at least one kind and one channel");
+  if (a->channels > 65536) return fail(ctx, DC_ERR_UNSUPPORTED, "at most 65536 channels");
+  const int es = a->dtype == DC_BF16 ? 2 : 4;
+  if (a->rows > 0 && !a->id) return fail(ctx, DC_ERR_INVALID_ARG, "null id");
+  if (!at(a->id, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "id is not aligned to its elements");
+  if (!backward) {
+    st = array_check(ctx, a->table, a->ld_table, a->kinds, a->channels, es, "table");
+    if (st == DC_OK) st = array_check(ctx, a->Y, a->ldy, a->rows, a->channels, es, "Y");
+  } else {
+    st = array_check(ctx, a->dY, a->lddy, a->rows, a->channels, es, "dY");
+    if (st == DC_OK) st = array_check(ctx, a->dtable, a->ld_dtable, a->kinds, a->channels, es, "dtable");
+  }
+  if (st != DC_OK) return st;
+  const Place id = vector_place("id", a->id, 4 * a->rows);
+  if (!backward) {
+    st = lies_apart(ctx, rows_place("Y", a->Y, a->rows, a->channels, a->ldy, es), {rows_place("table", a->table, a->kinds, a->channels, a->ld_table, es), id});
+  } else {
+    const size_t need = dc_embed_rows_bytes(ctx, a->rows, a->kinds, a->channels);
+    if (!a->workspace || a->workspace_bytes < need) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_embed_rows_bytes");
+    if (!at(a->workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+    const Place dY = rows_place("dY", a->dY, a->rows, a->channels, a->lddy, es), dtable = rows_place("dtable", a->dtable, a->kinds, a->channels, a->ld_dtable, es);
+    st = lies_apart(ctx, dtable, {dY, id});
+    if (st == DC_OK) st = lies_apart(ctx, vector_place("the workspace", a->workspace, (int64_t)need), {dY, dtable, id});
+  }
+  if (st != DC_OK) return st;
+  *g = EmbedArgs{};
+  g->rows = a->rows;
+  g->kinds = a->kinds;
+  g->C = a->channels;
+  g->bf16 = a->dtype == DC_BF16;
+  g->scale = a->scale;
+  g->id = a->id;
+  g->table = a->table;
+  g->ldt = a->ld_table;
+  g->Y = a->Y;
+  g->ldy = a->ldy;
+  g->dY = a->dY;
+  g->lddy = a->lddy;
+  g->dtable = a->dtable;
+  g->lddt = a->ld_dtable;
+  g->workspace = static_cast<char*>(a->workspace);
+  g->status = ctx->status;
+  g->n_cu = ctx->n_cu;
+  return DC_OK;
+}
+
+// Arrays of a call with many of them: none that is written may share a byte with another.
+struct Span {
+  intptr_t from, to;
+  bool written;
+  const char* name;
+};
+dc_status spans_apart(dc_ctx* ctx, std::vector<Span>& spans) {
+  auto before = [](const Span& x, const Span& y) { return x.from < y.from; };
+  if (!std::is_sorted(spans.begin(), spans.end(), before)) std::sort(spans.begin(), spans.end(), before);
+  const Span *far = nullptr, *far_written = nullptr;              // that reach furthest so far
+  for (const Span& s : spans) {
+    const Span* hit = s.written ? far : far_written;
+    if (hit && s.from < hit->to) return fail(ctx, DC_ERR_INVALID_ARG, std::string(s.name) + " overlaps " + hit->name);
+    if (!far || s.to > far->to) far = &s;
+    if (s.written && (!far_written || s.to > far_written->to)) far_written = &s;
+  }
+  return DC_OK;
+}
+
+// The tensors and the state of dc_adamw (step) or of dc_adamw_values, which writes out[0 .. 2].
+dc_status adamw_call(dc_ctx* ctx, const dc_adamw_args* a, bool step, float* const out[3], hipStream_t s) {
+  if (!a) return fail(ctx, DC_ERR_INVALID_ARG, "null arguments");
+  if (a->moments != DC_MOMENTS_F32 && a->moments != DC_MOMENTS_8BIT) return fail(ctx, DC_ERR_INVALID_ARG, "DC_MOMENTS_F32 or DC_MOMENTS_8BIT");
+  const bool eight = a->moments == DC_MOMENTS_8BIT;
+  if (a->n_tensors < 0 || (a->n_tensors > 0 && !a->tensors)) return fail(ctx, DC_ERR_INVALID_ARG, "null tensors, or a negative number of them");
+  if (a->total < 0 || a->total % kMomentBlock) return fail(ctx, DC_ERR_INVALID_ARG, "total must be a multiple of 128");
+  if (a->total > (1LL << 38)) return fail(ctx, DC_ERR_UNSUPPORTED, "total must be at most 2^38");
+  if (a->total > 0 && (!a->m || !a->v || (eight && (!a->m_exponent || !a->v_exponent)))) return fail(ctx, DC_ERR_INVALID_ARG, "null moments");
+  if (!at(a->m, 16) || !at(a->v, 16) || !at(a->low, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "m, v and low must be aligned to 16 bytes");
+  std::vector<Span> spans;
+  auto span = [&](const char* name, const void* p, int64_t bytes, bool written) {
+    if (p && bytes > 0) spans.push_back(Span{reinterpret_cast<intptr_t>(p), reinterpret_cast<intptr_t>(p) + (intptr_t)bytes, written, name});
+  };
+  if (step) {
+    if (!a->steps || !at(a->steps, 4) || !at(a->grad_scale, 4)) return fail(ctx, DC_ERR_INVALID_ARG, "steps (two numbers on the device) or grad_scale missing or not aligned");
+    if (!(a->lr >= 0.0 && a->lr <= 3.4e38) || !(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0) || !((float)a->eps > 0.f))
+      return fail(ctx, DC_ERR_INVALID_ARG, "need lr >= 0, betas in [0, 1) and eps > 0");
+    span("steps", a->steps, 8, true);
+    span("grad_scale", a->grad_scale, 4, false);
+  }
+  AdamwArgs k{};
+  k.m = a->m;
+  k.v = a->v;
+  k.m_exponent = a->m_exponent;
+  k.v_exponent = a->v_exponent;
+  k.low = a->low;
+  k.n_cu = ctx->n_cu;
+  if (step) {
+    k.steps = a->steps;
+    k.grad_scale = a->grad_scale;
+    k.beta1 = a->beta1;
+    k.beta2 = a->beta2;
+    k.lr = (float)a->lr;
+    k.b1 = (float)a->beta1;
+    k.b2 = (float)a->beta2;
+    k.o1 = (float)(1.0 - a->beta1);
+    k.o2 = (float)(1.0 - a->beta2);
+    k.eps = (float)a->eps;
+    k.seed = a->seed;
+  } else {
+    k.out_w = out[0];
+    k.out_m = out[1];
+    k.out_v = out[2];
+    static const char* const names[3] = {"w", "the values of m", "the values of v"};
+    for (int i = 0; i < 3; ++i) {
+      if (!at(out[i], 16)) return fail(ctx, DC_ERR_INVALID_ARG, "results must be aligned to 16 bytes");
+      span(names[i], out[i], 4 * a->total, true);
+    }
+  }
+  int64_t end = 0;
+  bool any16 = false;
+  for (int32_t i = 0; i < a->n_tensors; ++i) {
+    const dc_adamw_tensor& t = a->tensors[i];
+    if (t.n < 0 || t.at < end || t.at % kMomentBlock || t.n > a->total - t.at)
+      return fail(ctx, DC_ERR_INVALID_ARG, "tensor " + std::to_string(i) + ": its places are not a part of the state's, from a multiple of 128 behind the last one's");
+    end = t.at + (t.n + kMomentBlock - 1) / kMomentBlock * kMomentBlock;
+    if ((t.p_dtype != DC_F32 && t.p_dtype != DC_BF16) || (step && t.g_dtype != DC_F32 && t.g_dtype != DC_BF16))
+      return fail(ctx, DC_ERR_INVALID_ARG, "dtype must be DC_F32 or DC_BF16");
+    if (step && !((float)t.weight_decay >= 0.f && t.weight_decay <= 3.4e38)) return fail(ctx, DC_ERR_INVALID_ARG, "need weight_decay >= 0");
+    if (t.n == 0) continue;
+    const int ep = t.p_dtype == DC_BF16 ? 2 : 4, eg = t.g_dtype == DC_BF16 ? 2 : 4;
+    if (!t.p || !at(t.p, ep) || (step && t.g && !at(t.g, eg)))
+      return fail(ctx, DC_ERR_INVALID_ARG, "tensor " + std::to_string(i) + " is null or not aligned to its elements");
+    any16 = any16 || ep == 2;
+    span("a parameter", t.p, t.n * ep, step);
+    if (step) span("a gradient", t.g, t.n * eg, false);
+  }
+  if (any16 && !a->low) return fail(ctx, DC_ERR_INVALID_ARG, "bf16 parameters need `low`");
+  span("m", a->m, a->total * (eight ? 1 : 4), step);
+  span("v", a->v, a->total * (eight ? 1 : 4), step);
+  if (eight) {
+    span("m_exponent", a->m_exponent, a->total / kMomentBlock, step);
+    span("v_exponent", a->v_exponent, a->total / kMomentBlock, step);
+  }
+  span("low", a->low, 2 * a->total, step);
+  const dc_status st = spans_apart(ctx, spans);
+  if (st != DC_OK) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  auto launch = [&]() {
+    const hipError_t e = step ? launch_adamw(k, eight, s) : launch_adamw_values(k, eight, s);
+    k.tensors = k.chunks = 0;
+    return e;
+  };
+  for (int32_t i = 0; i < a->n_tensors; ++i) {
+    const dc_adamw_tensor& t = a->tensors[i];
+    if (t.n == 0 || (step && !t.g)) continue;
+    if (k.tensors == kAdamwTensors) {
+      const hipError_t e = launch();
+      if (e != hipSuccess) return hip_fail(ctx, e, "AdamW launch");
+    }
+    const int j = k.tensors++;
+    k.first[j] = k.chunks;
+    k.chunks += (int)adamw_chunks(t.n);          // 2^27 of all tensors at most
+    k.p16[j] = t.p_dtype == DC_BF16;
+    k.g16[j] = t.g_dtype == DC_BF16;
+    k.t[j] = AdamwTensor{t.p, t.g, (long long)t.n, (unsigned)(t.at / kMomentBlock), (float)t.weight_decay};
+  }
+  k.count_up = step;
+  if (step || k.chunks > 0) return enqueue_result(ctx, launch(), "AdamW launch");
+  return DC_OK;
+}
+}  // namespace
+
+size_t dc_row_norm_bytes(const dc_ctx* ctx, int64_t rows, int32_t channels) {
+  if (!ctx || rows < 0 || rows > kRowsMost || channels < 1 || channels > kRowNormMost) return 0;
+  return row_norm_floats(rows, channels, ctx->n_cu) * sizeof(float);
+}
+
+dc_status dc_row_norm(dc_ctx* ctx, const dc_row_norm_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  RowNormArgs g;
+  const dc_status st = row_norm_check(ctx, args, false, &g);
+  if (st != DC_OK || g.rows == 0) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  return enqueue_result(ctx, launch_row_norm(g, static_cast<hipStream_t>(stream)), "row norm launch");
+}
+
+dc_status dc_row_norm_backward(dc_ctx* ctx, const dc_row_norm_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  RowNormArgs g;
+  const dc_status st = row_norm_check(ctx, args, true, &g);
+  if (st != DC_OK) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  return enqueue_result(ctx, launch_row_norm_back(g, static_cast<hipStream_t>(stream)), "row norm gradient launch");
+}
+
+size_t dc_embed_rows_bytes(const dc_ctx* ctx, int64_t rows, int32_t kinds, int32_t channels) {
+  if (!ctx || rows < 0 || rows > kRowsMost || kinds < 1 || channels < 1 || channels > 65536) return 0;
+  return embed_rows_bytes(rows, kinds, channels, ctx->n_cu);
+}
+
+dc_status dc_embed_rows(dc_ctx* ctx, const dc_embed_rows_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  EmbedArgs g;
+  const dc_status st = embed_rows_check(ctx, args, false, &g);
+  if (st != DC_OK || g.rows == 0) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  return enqueue_result(ctx, launch_embed_rows(g, static_cast<hipStream_t>(stream)), "rows by kind launch");
+}
+
+dc_status dc_embed_rows_backward(dc_ctx* ctx, const dc_embed_rows_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  EmbedArgs g;
+  const dc_status st = embed_rows_check(ctx, args, true, &g);
+  if (st != DC_OK) return st;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, DC_ERR_HIP, "the context's device cannot be selected");
+  return enqueue_result(ctx, launch_embed_rows_back(g, static_cast<hipStream_t>(stream)), "table gradient launch");
+}
+
+dc_status dc_adamw(dc_ctx* ctx, const dc_adamw_args* args, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  try {
+    return adamw_call(ctx, args, true, nullptr, static_cast<hipStream_t>(stream));
+  } catch (const std::exception&) {              // of the list of arrays: host memory
+    return DC_ERR_OOM;
+  }
+}
+
+dc_status dc_adamw_values(dc_ctx* ctx, const dc_adamw_args* args, float* w, float* m, float* v, void* stream) {
+  if (!ctx) return DC_ERR_INVALID_ARG;
+  float* const out[3] = {w, m, v};
+  try {
+    return adamw_call(ctx, args, false, out, static_cast<hipStream_t>(stream));
+  } catch (const std::exception&) {
+    return DC_ERR_OOM;
+  }
 }
 
 dc_status dc_get_weights(dc_ctx* ctx, float* W_layers, float* b_layers, float* head, void* stream) {

@@ -1,0 +1,571 @@
+// Rows by kind: y_i = s T[id_i] (a row of zeros where id_i is -1), and the table's gradient dT_k = s sum of dy_i over id_i = k
+// (gfx950).
+//
+// Forward: bound by the rows it writes; the table's used rows stay in the caches.
+// Gradient: the row numbers are sorted by kind (stable radix sort, up to nine bits a pass), so that a kind's rows become
+// neighbours, and the sorted list is cut into chunks of equal length.  A chunk sums its rows kind by kind in the list's order.  A
+// kind that lies inside one chunk is written at once; what it has of kinds that reach beyond it, the first and the last of
+// its list at most, are entries of a second, shorter list, which is treated alike until it is short enough for one workgroup a
+// kind.  No atomics: the same call gives the same bits.  Sums: 64 rows in fp32, these in fp32 again (up to 256 rows a chunk), the
+// chunks' in 64 bits.  Kinds without rows are found by a search in the sorted list and cleared by further workgroups of the same
+// launch.
+#include "row_vectors.h"
+
+namespace dc {
+namespace {
+
+typedef unsigned long long u64;
+
+// ---- forward ----
+__device__ __forceinline__ int kind_of(const EmbedArgs& a, long long row) {
+  const int k = a.id[row];
+  if (k >= 0 && k < a.kinds) return k;
+  if (k != -1) atomicCAS(&a.status[1], 0, (int)DC_ERR_INVALID_ARG);
+  return -1;
+}
+
+constexpr int kAtOnce = 4;     // rows of a seat
+
+// Items: kAtOnce neighbouring rows and a slab of `lanes` vectors.
+template <typename T>
+__global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a, int lanes, int nslab) {
+  constexpr int kV = kVector<T>;
+  const int t = threadIdx.x & (lanes - 1), seats = 256 / lanes;
+  const long long groups = (a.rows + kAtOnce - 1) / kAtOnce, items = groups * nslab;
+  for (long long i = (long long)blockIdx.x * seats + threadIdx.x / lanes; i < items; i += (long long)gridDim.x * seats) {
+    const long long group = nslab == 1 ? i : i / nslab;
+    const int slab = (int)(i - group * nslab), c = (slab * lanes + t) * kV;
+    int kind[kAtOnce];
+    u32x4 v[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) kind[u] = kind_of(a, min(group * kAtOnce + u, a.rows - 1));
+    if (c >= a.C) continue;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+      v[u] = load_vector<T, false>(static_cast<const T*>(a.table) + (long long)max(kind[u], 0) * a.ldt, c, a.C);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const long long row = group * kAtOnce + u;
+      if (row >= a.rows) break;
+      float x[kV];
+      unpack(x, v[u], T());
+#pragma unroll
+      for (int k = 0; k < kV; ++k) x[k] = kind[u] < 0 ? 0.f : x[k] * a.scale;
+      store_vector<T, false>(static_cast<T*>(a.Y) + row * a.ldy, c, a.C, pack(x, T()));
+    }
+  }
+}
+
+// ---- sort ----
+constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64, kPer = 16, kTile = kSortThreads * kPer;
+constexpr int kBits = 9, kBins = 1 << kBits;
+
+struct Pair {
+  int kind, row;
+};
+// Rows that stand for nothing, or for no kind of the table, come last, as kind `kinds`.
+__device__ __forceinline__ Pair pair_at(const EmbedArgs& a, const Pair* in, int i) {
+  if (in) return in[i];
+  const int k = kind_of(a, i);
+  return Pair{k < 0 ? a.kinds : k, i};
+}
+// The lanes of the wave, among `active`, whose digit is the same.
+__device__ __forceinline__ u64 same_digit(int digit, int bits, u64 active) {
+  u64 m = active;
+  for (int b = 0; b < bits; ++b) {
+    const u64 set = __ballot(digit >> b & 1);
+    m &= (digit >> b & 1) ? set : ~set;
+  }
+  return m;
+}
+
+// Between a wave's own accesses of LDS, which the hardware does in their order: nothing moves across.
+__device__ __forceinline__ void in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// How many pairs of each tile have each digit: count[digit][tile].
+__global__ __launch_bounds__(kSortThreads) void count_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, int* count) {
+  __shared__ int bin[kBins];
+  const int bins = 1 << bits, n = (int)a.rows, tile = blockIdx.x;
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) bin[i] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int k = 0; k < kPer; ++k) {
+    const long long i = (long long)tile * kTile + k * kSortThreads + threadIdx.x;
+    const bool in_range = i < n;
+    const int digit = in_range ? pair_at(a, in, (int)i).kind >> shift & (bins - 1) : 0;
+    const u64 peers = same_digit(digit, bits, __ballot(in_range));
+    // one addition for the lanes of a digit
+    if (in_range && (peers & ((1ULL << (threadIdx.x & 63)) - 1)) == 0) atomicAdd(&bin[digit], __popcll(peers));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) count[(size_t)i * tiles + tile] = bin[i];
+}
+
+// Exclusive sums over the workgroup's 256 threads; returns the sum of all in `all`.
+__device__ __forceinline__ int scan256(int x, int* part, int& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int v = x;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int w = __shfl_up(v, o, 64);
+    if (lane >= o) v += w;
+  }
+  __syncthreads();
+  if (lane == 63) part[wave] = v;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += part[w];
+    all += part[w];
+  }
+  return before + v - x;
+}
+
+// A digit's counts become the number of its pairs in the tiles in front; total[digit].
+__global__ __launch_bounds__(256) void scan_kernel(int* count, int tiles, int* total) {
+  __shared__ int part[4];
+  int* c = count + (size_t)blockIdx.x * tiles;
+  int before = 0;
+  for (int i0 = 0; i0 < tiles; i0 += 256) {
+    const int i = i0 + threadIdx.x, x = i < tiles ? c[i] : 0;
+    int all;
+    const int at = scan256(x, part, all);
+    if (i < tiles) c[i] = before + at;
+    before += all;
+  }
+  if (threadIdx.x == 0) total[blockIdx.x] = before;
+}
+
+// Every pair to its place: its digit's first place, the tiles in front, the pairs of the tile in front.
+__global__ __launch_bounds__(kSortThreads) void scatter_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, const int* count,
+                                                               const int* total, Pair* out) {
+  __shared__ int first[kBins];
+  __shared__ int next[kSortWaves][kBins];
+  __shared__ int part[4];
+  const int bins = 1 << bits, n = (int)a.rows, tile = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int d0 = 0; d0 < bins; d0 += 256) {
+    const int d = d0 + threadIdx.x, x = d < bins ? total[d] : 0;
+    int all;
+    const int at = scan256(x, part, all);
+    if (d < bins) first[d] = before + at + count[(size_t)d * tiles + tile];
+    before += all;
+  }
+  for (int i = threadIdx.x; i < kSortWaves * bins; i += kSortThreads) next[i / bins][i % bins] = 0;
+  __syncthreads();
+  // a wave's pairs are neighbours: 64 at a time
+  Pair p[kPer];
+  u64 peers[kPer];
+  const long long base = (long long)tile * kTile + wave * 64 * kPer + lane;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const long long i = base + k * 64;
+    p[k] = i < n ? pair_at(a, in, (int)i) : Pair{0, -1};
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int digit = p[k].kind >> shift & (bins - 1);
+    const bool in_range = base + k * 64 < n;
+    peers[k] = same_digit(digit, bits, __ballot(in_range));
+    if (in_range && (peers[k] & ((1ULL << lane) - 1)) == 0) next[wave][digit] += __popcll(peers[k]);
+    in_order();
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < bins; d += kSortThreads) {
+    int at = first[d];
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = next[w][d];
+      next[w][d] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int digit = p[k].kind >> shift & (bins - 1);
+    const bool in_range = base + k * 64 < n;
+    const int rank = __popcll(peers[k] & ((1ULL << lane) - 1)), at = next[wave][digit];
+    in_order();
+    if (in_range) out[at + rank] = p[k];
+    if (in_range && rank == 0) next[wave][digit] = at + __popcll(peers[k]);
+    in_order();
+  }
+}
+
+// ---- sums ----
+struct Sums {
+  EmbedArgs a;
+  const Pair* sorted;          // [rows]
+  int n;                       // entries of the list: rows, or entries of the level below
+  int chunk;                   // entries of a chunk
+  int nchunk;
+  int lanes, nslab;            // vectors of a slab, slabs of a row
+  const float* in;             // levels above the first: [n][C]
+  const int* in_kind;          // [n]: the kind, or ~kind of an entry without a sum
+  float* out;                  // [2 nchunk][C]
+  int* out_kind;
+  int fill_blocks;             // first level: workgroups that clear the kinds without rows
+};
+
+template <typename T>
+__device__ __forceinline__ void write_kind(const EmbedArgs& a, int kind, int c, const float (&x)[kVector<T>]) {
+  float y[kVector<T>];
+#pragma unroll
+  for (int k = 0; k < kVector<T>; ++k) y[k] = x[k] * a.scale;
+  store_vector<T, false>(static_cast<T*>(a.dtable) + (long long)kind * a.lddt, c, a.C, pack(y, T()));
+}
+// An entry of the next list: kVector<T> columns from c.
+template <int kV>
+__device__ __forceinline__ void write_entry(float* row, int c, int C, const float (&x)[kV]) {
+#pragma unroll
+  for (int k = 0; k < kV; k += 4) {
+    const float y[4] = {x[k], x[k + 1], x[k + 2], x[k + 3]};
+    if (c + k < C) store_vector<float, false>(row, c + k, C, pack(y, 0.f));
+  }
+}
+template <int kV>
+__device__ __forceinline__ void read_entry(float (&x)[kV], const float* row, int c, int C) {
+#pragma unroll
+  for (int k = 0; k < kV; k += 4) {
+    float y[4];
+    unpack(y, c + k < C ? load_vector<float, false>(row, c + k, C) : u32x4{0, 0, 0, 0}, 0.f);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[k + u] = y[u];
+  }
+}
+
+constexpr int kRun = 64;       // rows summed in fp32 before they join the others'
+
+// What a chunk has of one kind is done with: the last one, if `last`.
+template <typename T>
+__device__ __forceinline__ void close_kind(const Sums& s, int chunk, int kind, int c, const float (&x)[kVector<T>], bool any, bool first, bool last,
+                                           bool from_before, bool goes_on) {
+  const bool up = (first && from_before) || (last && goes_on);
+  const int entry = 2 * chunk + (first ? 0 : 1);
+  if (!up) {
+    if (any) write_kind<T>(s.a, kind, c, x);
+  } else if (any) {
+    write_entry(s.out + (size_t)entry * s.a.C, c, s.a.C, x);
+  }
+  if (c < kVector<T>) {        // the row's first vector says what the entries are
+    if (first) s.out_kind[2 * chunk] = up && any ? kind : ~kind;
+    if (last && first) s.out_kind[2 * chunk + 1] = ~kind;
+    if (last && !first) s.out_kind[2 * chunk + 1] = up && any ? kind : ~kind;
+  }
+}
+
+// Clears the kinds that have no row: 64 kinds a wave.
+template <typename T>
+__device__ void clear_unused(const Sums& s, int block) {
+  const EmbedArgs& a = s.a;
+  const int lane = threadIdx.x & 63;
+  const long long waves = (long long)s.fill_blocks * 4;
+  for (long long k0 = ((long long)block * 4 + (threadIdx.x >> 6)) * 64; k0 < a.kinds; k0 += waves * 64) {
+    const int kind = (int)min(k0 + lane, (long long)a.kinds - 1);
+    int lo = 0, hi = s.n;      // the first pair of that kind or a larger one
+    while (lo < hi) {
+      const int mid = lo + (hi - lo) / 2;
+      if (s.sorted[mid].kind < kind) lo = mid + 1;
+      else hi = mid;
+    }
+    const bool none = k0 + lane < a.kinds && (lo >= s.n || s.sorted[lo].kind != kind);
+    for (u64 left = __ballot(none); left; left &= left - 1) {
+      T* row = static_cast<T*>(a.dtable) + (k0 + __builtin_ctzll(left)) * a.lddt;
+      for (int c = lane * kVector<T>; c < a.C; c += 64 * kVector<T>) store_vector<T, false>(row, c, a.C, u32x4{0, 0, 0, 0});
+    }
+  }
+}
+
+// First level: chunks of the sorted rows.
+template <typename T>
+__global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
+  constexpr int kV = kVector<T>, kAhead = 8;
+  const EmbedArgs& a = s.a;
+  if ((int)blockIdx.x < s.fill_blocks) return clear_unused<T>(s, blockIdx.x);
+  const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
+  const long long item = (long long)(blockIdx.x - s.fill_blocks) * seats + threadIdx.x / s.lanes;
+  if (item >= (long long)s.nchunk * s.nslab) return;
+  const int chunk = (int)(item / s.nslab), c = ((int)(item - (long long)chunk * s.nslab) * s.lanes + t) * kV;
+  if (c >= a.C) return;
+  const long long p0l = (long long)chunk * s.chunk;
+  const int p0 = (int)p0l, p1 = (int)min(p0l + s.chunk, (long long)s.n), len = p1 - p0;
+  const T* dY = static_cast<const T*>(a.dY);
+  int kind = s.sorted[p0].kind;
+  const bool from_before = p0 > 0 && s.sorted[p0 - 1].kind == kind;
+  const int past = p1 < s.n ? s.sorted[p1].kind : -1;
+  float sum[kV], run[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) sum[k] = run[k] = 0.f;
+  int count = 0;
+  bool first = true;
+  for (int q = 0; q < len; q += kAhead) {
+    Pair e[kAhead];
+    u32x4 v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) e[u] = s.sorted[p0 + min(q + u, len - 1)];
+    if (e[0].kind >= a.kinds) break;                     // only rows that stand for nothing are left
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c, a.C);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (q + u >= len || e[u].kind >= a.kinds) break;
+      if (e[u].kind != kind) {
+#pragma unroll
+        for (int k = 0; k < kV; ++k) sum[k] += run[k];
+        close_kind<T>(s, chunk, kind, c, sum, true, first, false, from_before, false);
+#pragma unroll
+        for (int k = 0; k < kV; ++k) sum[k] = run[k] = 0.f;
+        count = 0;
+        first = false;
+        kind = e[u].kind;
+      }
+      float x[kV];
+      unpack(x, v[u], T());
+#pragma unroll
+      for (int k = 0; k < kV; ++k) run[k] += x[k];
+      if (++count == kRun) {
+        count = 0;
+#pragma unroll
+        for (int k = 0; k < kV; ++k) {
+          sum[k] += run[k];
+          run[k] = 0.f;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kV; ++k) sum[k] += run[k];
+  close_kind<T>(s, chunk, kind, c, sum, kind < a.kinds, first, true, from_before, past == kind);
+}
+
+__device__ __forceinline__ int kind_of_entry(int k) { return k < 0 ? ~k : k; }
+
+// Levels between: chunks of a list of entries, sums in 64 bits.
+template <typename T>
+__global__ __launch_bounds__(256) void sum_entries_kernel(const Sums s) {
+  constexpr int kV = kVector<T>;
+  const EmbedArgs& a = s.a;
+  const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
+  const long long item = (long long)blockIdx.x * seats + threadIdx.x / s.lanes;
+  if (item >= (long long)s.nchunk * s.nslab) return;
+  const int chunk = (int)(item / s.nslab), c = ((int)(item - (long long)chunk * s.nslab) * s.lanes + t) * kV;
+  if (c >= a.C) return;
+  const int p0 = chunk * s.chunk, p1 = min(p0 + s.chunk, s.n);
+  int kind = kind_of_entry(s.in_kind[p0]);
+  const bool from_before = p0 > 0 && kind_of_entry(s.in_kind[p0 - 1]) == kind;
+  const int past = p1 < s.n ? kind_of_entry(s.in_kind[p1]) : -1;
+  double sum[kV];
+  float x[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) sum[k] = 0.0;
+  bool first = true, any = false;
+  for (int p = p0; p < p1; ++p) {
+    const int e = s.in_kind[p], of = kind_of_entry(e);
+    if (of != kind) {
+#pragma unroll
+      for (int k = 0; k < kV; ++k) {
+        x[k] = (float)sum[k];
+        sum[k] = 0.0;
+      }
+      close_kind<T>(s, chunk, kind, c, x, any, first, false, from_before, false);
+      first = any = false;
+      kind = of;
+    }
+    if (e < 0) continue;
+    any = true;
+    read_entry(x, s.in + (size_t)p * a.C, c, a.C);
+#pragma unroll
+    for (int k = 0; k < kV; ++k) sum[k] += (double)x[k];
+  }
+#pragma unroll
+  for (int k = 0; k < kV; ++k) x[k] = (float)sum[k];
+  close_kind<T>(s, chunk, kind, c, x, any, first, true, from_before, past == kind);
+}
+
+// The last list: a workgroup for each entry that begins a kind, and 64 vectors of its columns; its waves take the entries in turn.
+constexpr int kLastWaves = 4;
+template <typename T>
+__global__ __launch_bounds__(64 * kLastWaves) void last_sums_kernel(const Sums s) {
+  constexpr int kV = kVector<T>;
+  const EmbedArgs& a = s.a;
+  const int p0 = blockIdx.x, kind = kind_of_entry(s.in_kind[p0]);
+  if (kind >= a.kinds || (p0 > 0 && kind_of_entry(s.in_kind[p0 - 1]) == kind)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * kV;
+  __shared__ double part[kLastWaves][64][kV + 1];
+  __shared__ int found[kLastWaves];
+  double sum[kV];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) sum[k] = 0.0;
+  int any = 0;
+  for (int p = p0 + wave; p < s.n; p += kLastWaves) {
+    const int e = s.in_kind[p];
+    if (kind_of_entry(e) != kind) break;
+    if (e < 0) continue;
+    any = 1;
+    if (c >= a.C) continue;
+    float x[kV];
+    read_entry(x, s.in + (size_t)p * a.C, c, a.C);
+#pragma unroll
+    for (int k = 0; k < kV; ++k) sum[k] += (double)x[k];
+  }
+#pragma unroll
+  for (int k = 0; k < kV; ++k) part[wave][lane][k] = sum[k];
+  if (lane == 0) found[wave] = any;
+  __syncthreads();
+  if (wave != 0 || c >= a.C) return;
+  float x[kV];
+  for (int w = 1; w < kLastWaves; ++w) any |= found[w];
+#pragma unroll
+  for (int k = 0; k < kV; ++k) {
+    double v = part[0][lane][k];
+    for (int w = 1; w < kLastWaves; ++w) v += part[w][lane][k];
+    x[k] = (float)v;
+  }
+  if (any) write_kind<T>(a, kind, c, x);
+}
+
+constexpr int kLastMost = 2048;        // entries that the last launch takes
+constexpr int kEntryChunk = 64;
+
+int lanes_of(int vectors) {
+  int l = 1;
+  while (l < vectors && l < 64) l *= 2;
+  return l;
+}
+
+struct Plan {
+  int passes, bits, tiles;
+  int lanes, nslab;            // of rows of 16-byte vectors
+  int chunk, nchunk;
+  long long entries[8];        // of each level's list
+  int levels;                  // lists of entries
+};
+Plan plan(long long rows, int kinds, int C, int bytes, int n_cu) {
+  Plan p{};
+  int bits = 1;
+  while (bits < 31 && (kinds >> bits) != 0) ++bits;            // values 0 .. kinds
+  p.passes = (bits + kBits - 1) / kBits;
+  p.bits = (bits + p.passes - 1) / p.passes;
+  p.tiles = (int)((rows + kTile - 1) / kTile);
+  const int vectors = (C * bytes + 15) / 16;
+  p.lanes = lanes_of(vectors);
+  p.nslab = (vectors + p.lanes - 1) / p.lanes;
+  // 32 waves a CU, 16 to 256 rows a chunk
+  const long long seats = (long long)n_cu * 32 * (64 / p.lanes);
+  long long chunk = (rows * p.nslab + seats - 1) / seats;
+  p.chunk = (int)(chunk < 16 ? 16 : (chunk > 256 ? 256 : (chunk + 7) / 8 * 8));
+  p.nchunk = (int)((rows + p.chunk - 1) / p.chunk);
+  long long e = 2LL * p.nchunk;
+  while (e > 0) {
+    p.entries[p.levels++] = e;
+    if (e <= kLastMost) break;
+    e = 2 * ((e + kEntryChunk - 1) / kEntryChunk);
+  }
+  return p;
+}
+size_t round_up(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Where the arrays of a call lie in its workspace; its size.
+struct Room {
+  size_t pair[2], count, total, kind[8], sum[8], bytes;
+};
+Room room(const Plan& p, long long rows, int C) {
+  Room r{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round_up(bytes);
+    return here;
+  };
+  r.pair[0] = take(rows * sizeof(Pair));
+  r.pair[1] = p.passes > 1 ? take(rows * sizeof(Pair)) : 0;
+  r.count = take(((size_t)p.tiles << p.bits) * sizeof(int));
+  r.total = take(((size_t)1 << p.bits) * sizeof(int));
+  for (int l = 0; l < p.levels; ++l) {
+    r.kind[l] = take(p.entries[l] * sizeof(int));
+    r.sum[l] = take((size_t)p.entries[l] * C * sizeof(float));
+  }
+  r.bytes = at;
+  return r;
+}
+
+template <typename T>
+void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sorted, hipStream_t s) {
+  Sums m{};
+  m.a = a;
+  m.sorted = sorted;
+  m.n = (int)a.rows;
+  m.chunk = p.chunk;
+  m.nchunk = p.nchunk;
+  m.lanes = p.lanes;
+  m.nslab = p.nslab;
+  const long long fill = ((long long)a.kinds + 255) / 256, fill_most = 8LL * a.n_cu;
+  m.fill_blocks = (int)(fill < fill_most ? fill : fill_most);
+  const int seats = 256 / p.lanes;
+  auto blocks = [&](long long chunks) { return (unsigned)((chunks * p.nslab + seats - 1) / seats); };
+  if (p.levels > 0) {
+    m.out = reinterpret_cast<float*>(a.workspace + r.sum[0]);
+    m.out_kind = reinterpret_cast<int*>(a.workspace + r.kind[0]);
+  }
+  hipLaunchKernelGGL((sum_rows_kernel<T>), dim3(m.fill_blocks + blocks(p.nchunk)), dim3(256), 0, s, m);
+  for (int l = 0; l < p.levels; ++l) {
+    m.n = (int)p.entries[l];
+    m.in = m.out;
+    m.in_kind = m.out_kind;
+    if (l + 1 < p.levels) {
+      m.chunk = kEntryChunk;
+      m.nchunk = (int)(p.entries[l + 1] / 2);
+      m.out = reinterpret_cast<float*>(a.workspace + r.sum[l + 1]);
+      m.out_kind = reinterpret_cast<int*>(a.workspace + r.kind[l + 1]);
+      hipLaunchKernelGGL((sum_entries_kernel<T>), dim3(blocks(m.nchunk)), dim3(256), 0, s, m);
+    } else {
+      const int vectors = (a.C + kVector<T> - 1) / kVector<T>;
+      hipLaunchKernelGGL((last_sums_kernel<T>), dim3((unsigned)m.n, (vectors + 63) / 64), dim3(64 * kLastWaves), 0, s, m);
+    }
+  }
+}
+
+}  // namespace
+
+size_t embed_rows_bytes(long long rows, int kinds, int C, int n_cu) {
+  const Plan p2 = plan(rows, kinds, C, 2, n_cu), p4 = plan(rows, kinds, C, 4, n_cu);
+  const size_t b2 = room(p2, rows, C).bytes, b4 = room(p4, rows, C).bytes;
+  return b2 > b4 ? b2 : b4;
+}
+
+hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  const int vectors = (a.C * (a.bf16 ? 2 : 4) + 15) / 16, lanes = lanes_of(vectors), nslab = (vectors + lanes - 1) / lanes;
+  const long long items = (a.rows + kAtOnce - 1) / kAtOnce * nslab, seats = 256 / lanes, need = (items + seats - 1) / seats, most = 16LL * a.n_cu;
+  const dim3 grid((unsigned)(need < most ? need : most));
+  if (a.bf16) hipLaunchKernelGGL((embed_kernel<u16>), grid, dim3(256), 0, s, a, lanes, nslab);
+  else hipLaunchKernelGGL((embed_kernel<float>), grid, dim3(256), 0, s, a, lanes, nslab);
+  return hipGetLastError();
+}
+
+hipError_t launch_embed_rows_back(const EmbedArgs& a, hipStream_t s) {
+  const Plan p = plan(a.rows, a.kinds, a.C, a.bf16 ? 2 : 4, a.n_cu);
+  const Room r = room(p, a.rows, a.C);
+  Pair* pair[2] = {reinterpret_cast<Pair*>(a.workspace + r.pair[0]), reinterpret_cast<Pair*>(a.workspace + r.pair[1])};
+  const Pair* in = nullptr;
+  if (a.rows > 0) {
+    int* count = reinterpret_cast<int*>(a.workspace + r.count);
+    int* total = reinterpret_cast<int*>(a.workspace + r.total);
+    for (int k = 0; k < p.passes; ++k) {
+      const int shift = k * p.bits;
+      Pair* out = pair[k & 1];
+      hipLaunchKernelGGL(count_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, count);
+      hipLaunchKernelGGL(scan_kernel, dim3(1 << p.bits), dim3(256), 0, s, count, p.tiles, total);
+      hipLaunchKernelGGL(scatter_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, (const int*)count, (const int*)total, out);
+      in = out;
+    }
+  }
+  if (a.bf16) gradient<u16>(a, p, r, in, s);
+  else gradient<float>(a, p, r, in, s);
+  return hipGetLastError();
+}
+
+}  // namespace dc

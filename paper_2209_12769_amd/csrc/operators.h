@@ -192,6 +192,89 @@ size_t graph_norm_bytes(long long rows, int n_graphs, int C, int G, bool backwar
 hipError_t launch_graph_norm(const GraphNormArgs& a, hipStream_t s);
 hipError_t launch_graph_norm_back(const GraphNormArgs& a, hipStream_t s);
 
+// ---- norm over the channels of each row ----
+struct RowNormArgs {
+  long long rows;
+  int C, bf16, act;
+  float eps;
+  const void* X;                 // null where kept is taken (backward)
+  long long ldx;
+  KeptView kept;
+  const float* gamma;            // or null: 1
+  const float* beta;             // or null: 0
+  float* mean;                   // [rows]; forward: both or null
+  float* rstd;
+  void* Y;                       // forward
+  long long ldy;
+  const void* dY;                // backward
+  long long lddy;
+  const void* dRes;              // backward: added to dX, or null
+  long long lddres;
+  void* dX;
+  long long lddx;
+  float* dgamma;                 // [C] or null (both or none)
+  float* dbeta;
+  float* workspace;
+  int n_cu;
+};
+constexpr int kRowNormMost = 16384;                         // channels
+size_t row_norm_floats(long long rows, int C, int n_cu);    // backward, with dgamma
+hipError_t launch_row_norm(const RowNormArgs& a, hipStream_t s);
+hipError_t launch_row_norm_back(const RowNormArgs& a, hipStream_t s);
+
+// ---- rows by kind ----
+struct EmbedArgs {
+  long long rows;
+  int kinds, C, bf16;
+  float scale;
+  const int* id;                 // [rows]
+  const void* table;             // forward: [kinds, C]
+  long long ldt;
+  void* Y;
+  long long ldy;
+  const void* dY;                // backward
+  long long lddy;
+  void* dtable;                  // [kinds, C]
+  long long lddt;
+  char* workspace;
+  int* status;                   // ids out of range set status[1]
+  int n_cu;
+};
+size_t embed_rows_bytes(long long rows, int kinds, int C, int n_cu);
+hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t s);
+hipError_t launch_embed_rows_back(const EmbedArgs& a, hipStream_t s);
+
+// ---- AdamW over many tensors ----
+constexpr int kMomentBlock = 128;      // places of the state arrays that share an exponent; a tensor begins at a multiple of it
+struct AdamwTensor {
+  void* p;
+  const void* g;
+  long long n;
+  unsigned block;              // its first place / kMomentBlock
+  float decay;
+};
+constexpr int kAdamwTensors = 96;      // of one launch: its arguments stay below 4 KiB
+struct AdamwArgs {
+  void *m, *v;                 // fp32 or codes
+  unsigned char *m_exponent, *v_exponent;
+  unsigned short* low;
+  int* steps;                  // steps done; workgroups that are done with this one
+  const float* grad_scale;     // or null
+  double beta1, beta2;
+  float lr, b1, b2, o1, o2, eps;       // o: 1 - beta
+  unsigned long long seed;
+  float *out_w, *out_m, *out_v;        // values: each or null
+  int n_cu;
+  int count_up;                // the last launch of a call
+  int tensors, chunks;
+  int first[kAdamwTensors];    // first chunk of each tensor
+  unsigned char p16[kAdamwTensors], g16[kAdamwTensors];
+  AdamwTensor t[kAdamwTensors];
+};
+long long adamw_chunks(long long n);
+hipError_t launch_adamw(const AdamwArgs& a, bool eight, hipStream_t s);
+hipError_t launch_adamw_values(const AdamwArgs& a, bool eight, hipStream_t s);
+
 // out1 [n1] | out2 [n2] = sums over `blocks` rows of part [blocks, n1 + n2], in 64 bits and a fixed order.
 void launch_column_sums(const float* part, int blocks, int n1, float* out1, int n2, float* out2, const int* stop, hipStream_t s);
 

@@ -1,0 +1,104 @@
+"""Argument checks of the operators for training loops that need no GPU: the binding's own, and the library's where there is no
+context."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2209_12769_amd import binding as B
+
+
+@pytest.fixture()
+def ev():
+    """An Evaluator without a context, its tensors on the CPU: calls get as far as the library, which refuses them."""
+    e = B.Evaluator.__new__(B.Evaluator)
+    e.torch, e.device, e.ctx = torch, torch.device("cpu"), None
+    e._raw_stream = lambda: 0
+    return e
+
+
+def refused(message, call, *args, **kw):
+    with pytest.raises(ValueError, match=message):
+        call(*args, **kw)
+
+
+def without_context(call, *args, **kw):
+    with pytest.raises(B.DiscoError) as e:
+        call(*args, **kw)
+    assert e.value.status == B.DC_ERR_INVALID_ARG
+
+
+def test_row_norm(ev):
+    x, v = torch.zeros(3, 8), torch.zeros(8)
+    without_context(ev.row_norm, x, v, v)
+    refused("need a matrix", ev.row_norm, torch.zeros(8))
+    refused("float32 or bfloat16", ev.row_norm, x.double())
+    refused("neighbours", ev.row_norm, torch.zeros(8, 3).t())
+    refused("gamma", ev.row_norm, x, torch.zeros(7))
+    refused("beta", ev.row_norm, x, v, v.bfloat16())
+    refused("unknown activation", ev.row_norm, x, v, v, 1e-5, "tanh")
+    refused("out", ev.row_norm, x, v, v, out=torch.zeros(3, 9))
+    refused("out", ev.row_norm, x, out=x.bfloat16())
+    s = torch.zeros(3)
+    without_context(ev.row_norm_backward, x, x, v, v, s, s)
+    refused("mean", ev.row_norm_backward, x, x, v, v, torch.zeros(4), s)
+    refused("rstd", ev.row_norm_backward, x, x, v, v, s, torch.zeros(3, 1))
+    refused("x: need", ev.row_norm_backward, x, torch.zeros(2, 8), v, v, s, s)
+    refused("residual", ev.row_norm_backward, x, x, v, v, s, s, residual=x.bfloat16())
+    kept = B.KeptRows(torch.zeros(3, 32, dtype=torch.int8), torch.zeros(3, 1, dtype=torch.uint8), 9)
+    refused("kept rows", ev.row_norm_backward, x, kept, v, v, s, s)
+
+
+def test_embed_rows(ev):
+    table, ids, dy = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int32), torch.zeros(3, 8)
+    without_context(ev.embed_rows, ids, table)
+    refused("ids", ev.embed_rows, ids.long(), table)
+    refused("ids", ev.embed_rows, ids[None], table)
+    refused("ids", ev.embed_rows, torch.zeros(6, dtype=torch.int32)[::2], table)
+    refused("table", ev.embed_rows, ids, table.half())
+    refused("out", ev.embed_rows, ids, table, out=torch.zeros(4, 8))
+    without_context(ev.embed_rows_backward, dy, ids, 5)
+    refused("one number for each row", ev.embed_rows_backward, dy, ids[:2], 5)
+    refused("out", ev.embed_rows_backward, dy, ids, 5, out=torch.zeros(4, 8))
+
+
+def test_adamw(ev):
+    p, q = torch.zeros(3, 5), torch.zeros(300, dtype=torch.bfloat16)
+    o = ev.adamw([p, q], weight_decay=[0.1, 0.0], states="8bit")
+    assert o.at == [0, 128] and o.total == 512 and o.m.dtype == torch.uint8 and o.low.numel() == 512 and o.m_exponent.numel() == 4
+    assert ev.adamw([p]).low is None and ev.adamw([p]).m.dtype == torch.float32 and ev.adamw([]).total == 0
+    refused("states", ev.adamw, [p], states="4bit")
+    refused("weight_decay", ev.adamw, [p, q], weight_decay=[0.1])
+    refused("tensor 1", ev.adamw, [p, torch.zeros(4, 3).t()])
+    refused("tensor 0", ev.adamw, [p.double()])
+    refused("2 gradients", o.step, [p])
+    refused("which", o.values, "x")
+    refused("which", o.values, "ww")
+    refused("which", o.values, "")
+    without_context(o.values, "w")
+
+
+@pytest.mark.parametrize("name,args", [("dc_row_norm", 1), ("dc_row_norm_backward", 1), ("dc_embed_rows", 1), ("dc_embed_rows_backward", 1), ("dc_adamw", 1), ("dc_adamw_values", 4)])
+def test_calls_without_a_context(name, args):
+    assert getattr(B.lib(), name)(None, *[None] * args, None) == B.DC_ERR_INVALID_ARG
+
+
+def test_workspaces_without_a_context():
+    assert B.dc_row_norm_bytes(None, 5, 8) == 0 and B.dc_embed_rows_bytes(None, 5, 5, 8) == 0
+
+
+def test_structs_have_the_header_s_layout(tmp_path):
+    """Offsets of every field as the C compiler has them."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    structs = {"dc_row_norm_args": B.DcRowNormArgs, "dc_embed_rows_args": B.DcEmbedRowsArgs, "dc_adamw_args": B.DcAdamwArgs, "dc_adamw_tensor": B.DcAdamwTensor}
+    lines = ['printf("%%zu", sizeof(%s));' % s + "".join('printf(" %%zu", offsetof(%s, %s));' % (s, f[0]) for f in c._fields_) + 'printf("\\n");' for s, c in structs.items()]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include "disco.h"\nint main(void) { %s return 0; }\n' % "\n".join(lines))
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "layout"), str(src)], check=True)
+    got = subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout.splitlines()
+    for line, c in zip(got, structs.values()):
+        assert list(map(int, line.split())) == [ctypes.sizeof(c)] + [getattr(c, f[0]).offset for f in c._fields_]
+    assert np.dtype(B._ADAMW_TENSOR).itemsize == ctypes.sizeof(B.DcAdamwTensor)
