@@ -524,15 +524,16 @@ class AdamW:
         self._table = np.zeros(len(self.params), _ADAMW_TENSOR)
         self.at, total, half = [], 0, False
         for k, p in enumerate(self.params):
-            if p.device != ev.device or p.dtype not in ev._types or not p.is_contiguous():
-                raise ValueError(f"tensor {k}: need contiguous float32 or bfloat16 on {ev.device}")
+            self._check(k, p)
             n = p.numel()
-            self._table[k] = (0, 0, n, total, ev._types[p.dtype], 0, decay[k])
+            self._table[k] = (p.data_ptr(), 0, n, total, ev._types[p.dtype], 0, decay[k])
             self.at.append(total)
             total += -(-n // 128) * 128
             half = half or (p.dtype == torch.bfloat16 and n > 0)
         self.total = total
-        self._shapes = [p.shape for p in self.params]
+        self._shapes, self._dtypes = [p.shape for p in self.params], [p.dtype for p in self.params]
+        # what the table holds of the tensors' places and the gradients' types, as lists
+        self._ptrs, self._codes = [p.data_ptr() for p in self.params], [0] * len(self.params)
         eight = states == "8bit"
         with torch.no_grad():
             self.m, self.v = (torch.zeros(total, dtype=torch.uint8 if eight else torch.float32, device=ev.device) for _ in range(2))
@@ -540,11 +541,20 @@ class AdamW:
             self.low = torch.zeros(total, dtype=torch.int16, device=ev.device) if half else None
             self.steps = torch.zeros(2, dtype=torch.int32, device=ev.device)
 
+    def _check(self, k: int, p):
+        if p.device != self.ev.device or p.dtype not in self.ev._types or not p.is_contiguous():
+            raise ValueError(f"tensor {k}: need contiguous float32 or bfloat16 on {self.ev.device}")
+
     def _args(self, grad_scale: int) -> bytes:
-        table = self._table
-        table["p"] = [p.data_ptr() for p in self.params]
+        ptrs = [p.data_ptr() for p in self.params]
+        if ptrs != self._ptrs:                             # tensors whose owner gave them other memory
+            for k, p in enumerate(self.params):
+                self._check(k, p)
+                if p.shape != self._shapes[k] or p.dtype != self._dtypes[k]:
+                    raise ValueError(f"tensor {k}: was {tuple(self._shapes[k])} {self._dtypes[k]}, not {tuple(p.shape)} {p.dtype}")
+            self._table["p"] = self._ptrs = ptrs
         eight = self.m_exponent is not None
-        return _ADAMW.pack(DC_MOMENTS_8BIT if eight else DC_MOMENTS_F32, len(table), table.ctypes.data, self.total, self.m.data_ptr(),
+        return _ADAMW.pack(DC_MOMENTS_8BIT if eight else DC_MOMENTS_F32, len(ptrs), self._table.ctypes.data, self.total, self.m.data_ptr(),
                            self.v.data_ptr(), self.m_exponent.data_ptr() if eight else 0, self.v_exponent.data_ptr() if eight else 0,
                            0 if self.low is None else self.low.data_ptr(), self.steps.data_ptr(), grad_scale, self.lr, self.betas[0],
                            self.betas[1], self.eps, self.seed)
@@ -552,25 +562,24 @@ class AdamW:
     def step(self, grads, grad_scale=None):
         """One step with a gradient for every tensor (float32 or bfloat16, contiguous, its shape), None for tensors that stay as
         they are.  grad_scale: a float32 device tensor of one number that the gradients are multiplied by."""
-        ev, types = self.ev, self.ev._types
-        index = ev.device.index
+        ev, types, index = self.ev, self.ev._types, self.ev.device.index
         if len(grads) != len(self.params):
             raise ValueError(f"need {len(self.params)} gradients, not {len(grads)}")
         ptrs, codes = [], []
-        for k, g in enumerate(grads):
+        for g, shape in zip(grads, self._shapes):
             if g is None:
                 ptrs.append(0)
                 codes.append(0)
                 continue
             code = types.get(g.dtype)
-            if code is None or g.shape != self._shapes[k] or g.get_device() != index or not g.is_contiguous():
-                raise ValueError(f"gradient {k}: need contiguous float32 or bfloat16 {tuple(self._shapes[k])} on {ev.device}")
+            if code is None or g.shape != shape or g.get_device() != index or not g.is_contiguous():
+                raise ValueError(f"gradient {len(ptrs)}: need contiguous float32 or bfloat16 {tuple(shape)} on {ev.device}")
             ptrs.append(g.data_ptr())
             codes.append(code)
         self._table["g"] = ptrs
-        self._table["g_dtype"] = codes
-        args = self._args(0 if grad_scale is None else ev._vector(grad_scale.reshape(-1), "grad_scale", 1))
-        st = lib().dc_adamw(ev.ctx, args, ev._raw_stream())
+        if codes != self._codes:
+            self._table["g_dtype"] = self._codes = codes
+        st = lib().dc_adamw(ev.ctx, self._args(0 if grad_scale is None else ev._vector(grad_scale.reshape(-1), "grad_scale", 1)), ev._raw_stream())
         if st:
             ev._ok(st, "dc_adamw")
 

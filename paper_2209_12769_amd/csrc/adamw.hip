@@ -3,9 +3,11 @@
 //   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
 //   w = w - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + decay w)
 //
-// Bound by memory.  The tensors are cut into chunks of 2048 elements, eight a thread, dealt to the resident workgroups; a chunk's
-// tensor is found in a table that travels with the launch.  The step count t lies in device memory and the last workgroup counts
-// it up, so that a captured step goes on counting.
+// (the corrections as factors: k2 sqrt(v) and c1 m / (k2 sqrt(v) + eps), of which nothing is too small for fp32 before m and v are).
+// Bound by memory.  The tensors are cut into chunks of 4096 elements, eight a thread, a workgroup each, so that memory is gone
+// through in the order in which workgroups are handed out; a chunk's tensor is found in a table that travels with the launch.  The
+// step count t lies in device memory, so that a captured step goes on counting: the last workgroup counts it up, or, of more than
+// can be counted one by one, a launch of its own.
 // A bf16 parameter has the low 16 bits of its fp32 value w beside it (2 bytes where a copy of w would take 4): w is rounded to bf16
 // with halves away from zero, so a low half of 0x8000 or more says that the bf16 number is one step above w's upper half, and the
 // two are w itself.
@@ -24,7 +26,9 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kPer = 8, kThreads = 256, kChunk = kPer * kThreads;
+constexpr int kPer = 8, kThreads = 512, kChunk = kPer * kThreads;
+constexpr u64 kDraw = 0xD1342543DE82EF95ULL;    // from one draw to the next
+constexpr unsigned kCounted = 2048;            // workgroups that are counted one by one
 constexpr int kExponentNan = 255;              // of a block of moments that holds a number that is not finite
 
 __host__ __device__ __forceinline__ u64 mix(u64 z) {
@@ -33,63 +37,76 @@ __host__ __device__ __forceinline__ u64 mix(u64 z) {
   return z ^ (z >> 31);
 }
 
-struct Place {
-  const AdamwTensor* t;
+// A part of a tensor, the same for a workgroup.
+struct Chunk {
+  char* p;                     // its first element
+  const char* g;
+  int n;                       // elements
   bool p16, g16;
-  long long i;                 // the thread's first element in the tensor
-  int left;                    // how many of its eight are there: 1 to 8
+  float decay;
   long long at;                // its first place in the state arrays
-  bool block;                  // its 128 places hold an element
 };
-__device__ __forceinline__ Place place_of(const AdamwArgs& a, int chunk) {
-  int lo = 0, hi = a.tensors;  // the last tensor whose first chunk is not behind this one
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.first[mid] <= chunk) lo = mid;
-    else hi = mid;
-  }
-  Place p;
-  p.t = &a.t[lo];
-  p.p16 = a.p16[lo] != 0;
-  p.g16 = a.g16[lo] != 0;
-  p.i = (long long)(chunk - a.first[lo]) * kChunk + threadIdx.x * kPer;
-  const long long left = p.t->n - p.i;
-  p.left = left > kPer ? kPer : (left < 0 ? 0 : (int)left);
-  p.at = (long long)p.t->block * kMomentBlock + p.i;
-  p.block = (p.i & ~(long long)(kMomentBlock - 1)) < p.t->n;
-  return p;
+__device__ __forceinline__ Chunk chunk_of(const AdamwArgs& a, int chunk) {
+  // the last tensor whose first chunk is not behind this one: all are looked at at once (a search would wait for the table in
+  // every step)
+  const int lane = threadIdx.x & 63;
+  static_assert(kAdamwTensors <= 128, "two a lane");
+  const bool in1 = lane < a.tensors, in2 = 64 + lane < a.tensors;
+  const int f1 = a.t[in1 ? lane : 0].first, f2 = a.t[in2 ? 64 + lane : 0].first;
+  const AdamwTensor t = a.t[__builtin_amdgcn_readfirstlane(__popcll(__ballot(in1 && f1 <= chunk)) + __popcll(__ballot(in2 && f2 <= chunk)) - 1)];
+  const long long i = (long long)(chunk - t.first) * kChunk, left = t.n - i;
+  Chunk c;
+  c.p16 = t.types & 1;
+  c.g16 = t.types & 2;
+  c.p = static_cast<char*>(t.p) + i * (c.p16 ? 2 : 4);
+  c.g = static_cast<const char*>(t.g) + i * (c.g16 ? 2 : 4);
+  c.n = left < kChunk ? (int)left : kChunk;
+  c.decay = t.decay;
+  c.at = (long long)t.block * kMomentBlock + i;
+  return c;
 }
 
-// Eight elements from i, zeros behind the last.
-__device__ __forceinline__ void load8(float (&x)[kPer], const void* from, long long i, int left, bool bf16) {
+// Eight elements as they come from memory: fp32, or bf16 in the first four words.  kAll: all are there; else `left` of them, and
+// zeros behind.
+struct Raw {
+  u32x4 v[2];
+};
+template <bool kAll>
+__device__ __forceinline__ Raw request(const char* from, unsigned i, int left, bool bf16) {
+  Raw r;
+  if (kAll || left >= kPer) {
+    if (bf16) {
+      r.v[0] = *reinterpret_cast<const u32x4_any*>(from + 2 * i);
+    } else {
+      r.v[0] = *reinterpret_cast<const u32x4_any*>(from + 4 * i);
+      r.v[1] = *reinterpret_cast<const u32x4_any*>(from + 4 * i + 16);
+    }
+    return r;
+  }
+  r.v[0] = r.v[1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)
+    if (k < left) {
+      if (bf16) r.v[0][k / 2] |= (unsigned)reinterpret_cast<const u16*>(from)[i + k] << (16 * (k & 1));
+      else r.v[k / 4][k & 3] = reinterpret_cast<const unsigned*>(from)[i + k];
+    }
+  return r;
+}
+__device__ __forceinline__ void open(float (&x)[kPer], const Raw& r, bool bf16) {
   if (bf16) {
-    const u16* p = static_cast<const u16*>(from) + i;
-    u32x4 v = {0, 0, 0, 0};
-    if (left == kPer) {
-      v = *reinterpret_cast<const u32x4_any*>(p);
-    } else {
 #pragma unroll
-      for (int k = 0; k < kPer; ++k)
-        if (k < left) v[k / 2] |= (unsigned)p[k] << (16 * (k & 1));
+    for (int k = 0; k < 4; ++k) {
+      x[2 * k] = __uint_as_float(r.v[0][k] << 16);
+      x[2 * k + 1] = __uint_as_float(r.v[0][k] & 0xFFFF0000u);
     }
-    unpack(x, v, u16());
   } else {
-    const float* p = static_cast<const float*>(from) + i;
-    if (left == kPer) {
-      const u32x4 lo = *reinterpret_cast<const u32x4_any*>(p), hi = *reinterpret_cast<const u32x4_any*>(p + 4);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[k] = __uint_as_float(lo[k]);
-        x[4 + k] = __uint_as_float(hi[k]);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) x[k] = k < left ? p[k] : 0.f;
-    }
+    for (int k = 0; k < kPer; ++k) x[k] = __uint_as_float(r.v[k / 4][k & 3]);
   }
 }
+template <bool kAll>
 __device__ __forceinline__ void store8(const float (&x)[kPer], float* p, int left) {
-  if (left == kPer) {
+  if (kAll || left >= kPer) {
     *reinterpret_cast<u32x4_any*>(p) = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
     *reinterpret_cast<u32x4_any*>(p + 4) = u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
   } else {
@@ -105,55 +122,43 @@ __device__ __forceinline__ float whole(unsigned p, unsigned low) {
   const unsigned borrow = low >= 0x8000u && (p & 0x7FFFu) != 0 ? 1u : 0u;
   return __uint_as_float(((p - borrow) << 16) | low);
 }
-__device__ __forceinline__ void load_whole(float (&w)[kPer], const Place& p, const u16* low) {
-  const u32x4 l = *reinterpret_cast<const u32x4*>(low + p.at);
-  const u16* from = static_cast<const u16*>(p.t->p) + p.i;
-  u32x4 v = {0, 0, 0, 0};
-  if (p.left == kPer) {
-    v = *reinterpret_cast<const u32x4_any*>(from);
-  } else {
-#pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (k < p.left) v[k / 2] |= (unsigned)from[k] << (16 * (k & 1));
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    w[2 * k] = whole(v[k] & 0xFFFFu, l[k] & 0xFFFFu);
-    w[2 * k + 1] = whole(v[k] >> 16, l[k] >> 16);
-  }
-}
-__device__ __forceinline__ void store_whole(const float (&w)[kPer], const Place& p, u16* low) {
+template <bool kAll>
+__device__ __forceinline__ void store_whole(const float (&w)[kPer], u16* to, u16* low, int left) {
   unsigned hi[kPer], lo[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const unsigned b = __float_as_uint(w[k]);
-    const bool nan = (b & 0x7FFFFFFFu) > 0x7F800000u;
-    hi[k] = nan ? (b >> 16) | 0x40u : (b + 0x8000u) >> 16;
-    lo[k] = nan || k >= p.left ? 0u : b & 0xFFFFu;
+    const bool nan = w[k] != w[k];
+    hi[k] = nan ? 0x7FC0u : (b + 0x8000u) >> 16;
+    lo[k] = nan || (!kAll && k >= left) ? 0u : b;
   }
-  u16* to = static_cast<u16*>(p.t->p) + p.i;
-  if (p.left == kPer) {
-    *reinterpret_cast<u32x4_any*>(to) = u32x4{hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
+  const u32x4 h = {hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
+  if (kAll || left >= kPer) {
+    *reinterpret_cast<u32x4_any*>(to) = h;
   } else {
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
-      if (k < p.left) to[k] = (u16)hi[k];
+      if (k < left) to[k] = (u16)hi[k];
   }
-  *reinterpret_cast<u32x4*>(low + p.at) = u32x4{lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16};
+  u32x4 l;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) l[k] = __builtin_amdgcn_perm(lo[2 * k + 1], lo[2 * k], 0x05040100u);   // their lower halves
+  *reinterpret_cast<u32x4*>(low) = l;
 }
 
 // ---- moments in 8 bits ----
 // What a code's fp32 bits are times 2^(exponent - kUnit).
 template <bool kM>
 constexpr int kUnit = kM ? 15 : 31;
+// Four codes.
 template <bool kM>
-__device__ __forceinline__ void decode(float (&x)[kPer], u32x2 code, int exponent) {
+__device__ __forceinline__ void decode(float (&x)[4], unsigned code, int exponent) {
+  const float nan = exponent == kExponentNan ? __uint_as_float(0x7FC00000u) : 0.f;     // of the whole block, or nothing
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const unsigned c = code[k / 4] >> (8 * (k & 3)) & 0xFFu;
-    const float f = __uint_as_float((kM ? c & 0x7Fu : c) << 20);
-    const float y = exponent == kExponentNan ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(f, exponent - kUnit<kM>);
-    x[k] = kM && (c & 0x80u) ? -y : y;
+  for (int k = 0; k < 4; ++k) {
+    const unsigned top = code << (24 - 8 * k);           // the code in the upper byte
+    const unsigned bits = kM ? (top >> 4 & 0x07F00000u) | (top & 0x80000000u) : top >> 4 & 0x0FF00000u;
+    x[k] = __builtin_amdgcn_ldexpf(__uint_as_float(bits), exponent - kUnit<kM>) + nan;
   }
 }
 __device__ __forceinline__ unsigned max_dpp16(unsigned x) {
@@ -162,10 +167,9 @@ __device__ __forceinline__ unsigned max_dpp16(unsigned x) {
   x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));
   return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true));
 }
-// chance: 16 bits a place.  Returns the exponent of the 16 lanes' block.
+// r: a draw for two places, 16 bits for m and for v of the first and of the second.  Returns the exponent of the 16 lanes' block.
 template <bool kM>
-__device__ __forceinline__ int encode(u32x2& code, const float (&x)[kPer], const unsigned (&chance)[kPer]) {
-  constexpr int kMost = kM ? 127 : 255;
+__device__ __forceinline__ int encode(u32x2& code, const float (&x)[kPer], const u64 (&r)[kPer / 2]) {
   unsigned top = 0;            // the bits of |x| order as |x| does, what is not finite above all
 #pragma unroll
   for (int k = 0; k < kPer; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
@@ -177,10 +181,15 @@ __device__ __forceinline__ int encode(u32x2& code, const float (&x)[kPer], const
   if (top >= 0x7F800000u) return kExponentNan;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const unsigned bits = __float_as_uint(__builtin_amdgcn_ldexpf(fabsf(x[k]), kUnit<kM> - e));
-    unsigned c = min((bits + (chance[k] << 4 | 8u)) >> 20, (unsigned)kMost);
-    if (!kM) c = max(c, x[k] > 0.f ? 1u : 0u);
-    if (kM) c |= __float_as_uint(x[k]) >> 31 << 7;
+    const unsigned half = (unsigned)(r[k / 2] >> (32 * (k & 1)));
+    // 2^-17 of a step above the 16 bits, which leave 20 to be cut off
+    const unsigned chance = kM ? (half & 0xFFFFu) << 4 | 8u : half >> 12 & 0xFFFF0u | 8u;
+    unsigned c = (__float_as_uint(__builtin_amdgcn_ldexpf(fabsf(x[k]), kUnit<kM> - e)) + chance) >> 20;
+    if constexpr (kM) {
+      c = min(c, 127u) | (__float_as_uint(x[k]) >> 24 & 0x80u);
+    } else {
+      c = min(max(c, min(__float_as_uint(x[k]), 1u)), 255u);     // v is not negative: 1 at least if it is not zero
+    }
     code[k / 4] |= c << (8 * (k & 3));
   }
   return e;
@@ -193,73 +202,144 @@ __device__ __forceinline__ double power(double b, unsigned n) {
   return r;
 }
 
-template <bool kEight>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwArgs a) {
+// What all elements of a step share; worked out by one wave of a workgroup.
+struct Step {
+  float c1, k2;                // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  float scale;                 // of the gradients
+  // Whether the machine's root and reciprocal serve, one unit in the last place each at a tenth of the instructions of exact ones.
+  // They take what is no normal number as zero: a root of 1.1e-19 at most, times k2 a 16th of the rounding of eps or less.
+  bool fast;
+  u64 key;
+};
+
+// A chunk's step.  kAll: of kChunk elements.  `first`: the workgroup's first one, its requests go out before `step` is there.
+template <bool kEight, bool kAll>
+__device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const Step& step, bool first) {
   // the 8-bit codes are those of operations in fp32 rounded one by one
 #pragma clang fp contract(off)
-  const int before = a.steps[0], t = before < 2147483647 ? before + 1 : before;
-  const float c1 = (float)(1.0 / (1.0 - power(a.beta1, (unsigned)t))), c2 = (float)(1.0 / (1.0 - power(a.beta2, (unsigned)t)));
-  const float scale = a.grad_scale ? a.grad_scale[0] : 1.f;
-  const u64 key = kEight ? mix(a.seed ^ mix((u64)t)) : 0;
-  for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-    const Place p = place_of(a, chunk);
-    if (kEight ? !p.block : p.left == 0) continue;
-    float g[kPer], w[kPer], m[kPer], v[kPer];
-    load8(g, p.t->g, p.i, p.left, p.g16);
-    if (p.p16) load_whole(w, p, a.low);
-    else load8(w, p.t->p, p.i, p.left, false);
+  const unsigned i = threadIdx.x * kPer;
+  const int left = kAll ? kPer : min(max(c.n - (int)i, 0), kPer);
+  const bool there = kAll || (kEight ? (int)(i & ~(unsigned)(kMomentBlock - 1)) < c.n : left > 0);
+  unsigned char* const m8 = static_cast<unsigned char*>(a.m) + c.at;
+  unsigned char* const v8 = static_cast<unsigned char*>(a.v) + c.at;
+  float* const m32 = static_cast<float*>(a.m) + c.at;
+  float* const v32 = static_cast<float*>(a.v) + c.at;
+  unsigned char* const me = a.m_exponent + c.at / kMomentBlock;
+  unsigned char* const ve = a.v_exponent + c.at / kMomentBlock;
+  Raw rg, rw, rm, rv;
+  u32x4 rl = {0, 0, 0, 0};
+  u32x2 mc, vc;
+  int em, ev;
+  if (there) {
+    rg = request<kAll>(c.g, i, left, c.g16);
+    rw = request<kAll>(c.p, i, left, c.p16);
+    if (c.p16) rl = *reinterpret_cast<const u32x4*>(a.low + c.at + i);
     if constexpr (kEight) {
-      const u32x2 mc = *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.m) + p.at);
-      const u32x2 vc = *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.v) + p.at);
-      decode<true>(m, mc, a.m_exponent[p.at / kMomentBlock]);
-      decode<false>(v, vc, a.v_exponent[p.at / kMomentBlock]);
+      mc = *reinterpret_cast<const u32x2*>(m8 + i);
+      vc = *reinterpret_cast<const u32x2*>(v8 + i);
+      em = me[i / kMomentBlock];
+      ev = ve[i / kMomentBlock];
     } else {
-      load8(m, a.m, p.at, kPer, false);
-      load8(v, a.v, p.at, kPer, false);
-    }
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const float gk = g[k] * scale;
-      m[k] = m[k] * a.b1 + gk * a.o1;
-      v[k] = v[k] * a.b2 + (gk * gk) * a.o2;
-      const float step = (m[k] * c1) / (sqrtf(v[k] * c2) + a.eps);
-      w[k] = fmaf(-a.lr, fmaf(p.t->decay, w[k], step), w[k]);
-    }
-    if constexpr (kEight) {
-      unsigned cm[kPer], cv[kPer];
-#pragma unroll
-      for (int k = 0; k < kPer; k += 2) {
-        const u64 r = mix(key + (u64)(p.at / 2 + k / 2) * 0xD1342543DE82EF95ULL);
-        cm[k] = (unsigned)r & 0xFFFFu;
-        cv[k] = (unsigned)r >> 16;
-        cm[k + 1] = (unsigned)(r >> 32) & 0xFFFFu;
-        cv[k + 1] = (unsigned)(r >> 48);
-      }
-#pragma unroll
-      for (int k = 0; k < kPer; ++k)           // places behind the tensor's last element hold zeros
-        if (k >= p.left) m[k] = v[k] = 0.f;
-      u32x2 mc, vc;
-      const int em = encode<true>(mc, m, cm), ev = encode<false>(vc, v, cv);
-      *reinterpret_cast<u32x2*>(static_cast<unsigned char*>(a.m) + p.at) = mc;
-      *reinterpret_cast<u32x2*>(static_cast<unsigned char*>(a.v) + p.at) = vc;
-      if ((threadIdx.x & 15) == 0) {
-        a.m_exponent[p.at / kMomentBlock] = (unsigned char)em;
-        a.v_exponent[p.at / kMomentBlock] = (unsigned char)ev;
-      }
-    } else {
-      store8(m, static_cast<float*>(a.m) + p.at, p.left);
-      store8(v, static_cast<float*>(a.v) + p.at, p.left);
-    }
-    if (p.p16) {
-      if (p.left > 0) store_whole(w, p, a.low);
-    } else {
-      store8(w, static_cast<float*>(p.t->p) + p.i, p.left);
+      rm = request<true>(reinterpret_cast<const char*>(m32), i, kPer, false);
+      rv = request<true>(reinterpret_cast<const char*>(v32), i, kPer, false);
     }
   }
-  if (!a.count_up) return;
-  __syncthreads();                             // every wave has read the count
+  if (first) __syncthreads();
+  if (!there) return;
+  float g[kPer], w[kPer], m[kPer], v[kPer];
+  open(g, rg, c.g16);
+  if (c.p16) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      w[2 * k] = whole(rw.v[0][k] & 0xFFFFu, rl[k] & 0xFFFFu);
+      w[2 * k + 1] = whole(rw.v[0][k] >> 16, rl[k] >> 16);
+    }
+  } else {
+    open(w, rw, false);
+  }
+  if constexpr (kEight) {
+#pragma unroll
+    for (int k = 0; k < kPer; k += 4) {
+      float y[4], z[4];
+      decode<true>(y, mc[k / 4], em);
+      decode<false>(z, vc[k / 4], ev);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        m[k + u] = y[u];
+        v[k + u] = z[u];
+      }
+    }
+  } else {
+    open(m, rm, false);
+    open(v, rv, false);
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const float gk = g[k] * step.scale;
+    m[k] = m[k] * a.b1 + gk * a.o1;
+    v[k] = v[k] * a.b2 + (gk * gk) * a.o2;
+  }
+  float by[kPer];              // m / (sqrt(v) k2 + eps)
+  if (step.fast) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) by[k] = m[k] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[k]), step.k2, a.eps));
+  } else {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) by[k] = m[k] / fmaf(sqrtf(v[k]), step.k2, a.eps);
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) w[k] = fmaf(-a.lr, fmaf(c.decay, w[k], by[k] * step.c1), w[k]);
+  if constexpr (kEight) {
+    if (!kAll) {               // places behind the tensor's last element hold zeros
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (k >= left) m[k] = v[k] = 0.f;
+    }
+    u64 r[kPer / 2], place = step.key + (u64)((c.at + i) / 2) * kDraw;
+#pragma unroll
+    for (int k = 0; k < kPer / 2; ++k, place += kDraw) r[k] = mix(place);
+    em = encode<true>(mc, m, r);
+    ev = encode<false>(vc, v, r);
+    *reinterpret_cast<u32x2*>(m8 + i) = mc;
+    *reinterpret_cast<u32x2*>(v8 + i) = vc;
+    if ((threadIdx.x & 15) == 0) {
+      me[i / kMomentBlock] = (unsigned char)em;
+      ve[i / kMomentBlock] = (unsigned char)ev;
+    }
+  } else {
+    store8<kAll>(m, m32 + i, left);
+    store8<kAll>(v, v32 + i, left);
+  }
+  if (c.p16) {
+    if (left > 0) store_whole<kAll>(w, reinterpret_cast<u16*>(c.p) + i, a.low + c.at + i, left);
+  } else {
+    store8<kAll>(w, reinterpret_cast<float*>(c.p) + i, left);
+  }
+}
+
+template <bool kEight>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwArgs a) {
+  __shared__ Step step;
+  const int before = a.steps[0], t = before < 2147483647 ? before + 1 : before;
+  if (threadIdx.x < 64) {
+    Step s;
+    s.c1 = (float)(1.0 / (1.0 - power(a.beta1, (unsigned)t)));
+    s.k2 = (float)sqrt(1.0 / (1.0 - power(a.beta2, (unsigned)t)));
+    s.fast = a.eps >= 3e-11f * s.k2;
+    s.scale = a.grad_scale ? a.grad_scale[0] : 1.f;
+    s.key = mix(a.seed ^ mix((u64)t));
+    if (threadIdx.x == 0) step = s;
+  }
+  for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    const Chunk c = chunk_of(a, chunk);
+    if (c.n == kChunk) update<kEight, true>(a, c, step, chunk == (int)blockIdx.x);
+    else update<kEight, false>(a, c, step, chunk == (int)blockIdx.x);
+  }
+  if (!a.count_up || gridDim.x > kCounted) return;
+  // Every wave has read the count by now, and nothing else is handed from one workgroup to another: no fence, which would write
+  // an XCD's whole L2 back for each of them (1.14 M parameters 29 us instead of 8).
+  __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
     if (atomicAdd(&a.steps[1], 1) == (int)gridDim.x - 1) {
       a.steps[1] = 0;
       a.steps[0] = t;
@@ -267,39 +347,69 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwArgs a) {
   }
 }
 
+__global__ void count_up_kernel(int* steps) {
+  if (steps[0] < 2147483647) steps[0] += 1;
+}
+
+// Four values a thread, so that a wave's stores are neighbours: a workgroup takes half a chunk.
 template <bool kEight>
 __global__ __launch_bounds__(kThreads) void values_kernel(const AdamwArgs a) {
-  for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-    const Place p = place_of(a, chunk);
-    if (!p.block) continue;
-    float x[kPer];
-    if (a.out_w) {
-      if (p.p16) load_whole(x, p, a.low);
-      else load8(x, p.t->p, p.i, p.left, false);
+  for (long long half = blockIdx.x; half < 2LL * a.chunks; half += gridDim.x) {
+    const Chunk c = chunk_of(a, (int)(half / 2));
+    const unsigned i = (unsigned)(half & 1) * (kChunk / 2) + threadIdx.x * 4;
+    if ((int)(i & ~(unsigned)(kMomentBlock - 1)) >= c.n) continue;
+    const int left = min(max(c.n - (int)i, 0), 4);
+    auto put = [&](float* to, const float (&x)[4]) {
+      u32x4 v;
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) x[k] = k < p.left ? x[k] : 0.f;
-      store8(x, a.out_w + p.at, kPer);
+      for (int k = 0; k < 4; ++k) v[k] = k < left ? __float_as_uint(x[k]) : 0u;
+      *reinterpret_cast<u32x4*>(to + c.at + i) = v;
+    };
+    float w[4], m[4], v[4];
+    if (a.out_w) {
+      if (c.p16) {
+        const u32x2 l = *reinterpret_cast<const u32x2*>(a.low + c.at + i);
+        const u16* from = reinterpret_cast<const u16*>(c.p) + i;
+        u32x2 h = {0, 0};
+        if (left == 4) {
+          h = *reinterpret_cast<const u32x2_any*>(from);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < left) h[k / 2] |= (unsigned)from[k] << (16 * (k & 1));
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          w[2 * k] = whole(h[k] & 0xFFFFu, l[k] & 0xFFFFu);
+          w[2 * k + 1] = whole(h[k] >> 16, l[k] >> 16);
+        }
+      } else {
+        const float* from = reinterpret_cast<const float*>(c.p) + i;
+        if (left == 4) {
+          unpack(w, *reinterpret_cast<const u32x4_any*>(from), 0.f);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = k < left ? from[k] : 0.f;
+        }
+      }
     }
     if (a.out_m) {
-      if constexpr (kEight) decode<true>(x, *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.m) + p.at), a.m_exponent[p.at / kMomentBlock]);
-      else load8(x, a.m, p.at, kPer, false);
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) x[k] = k < p.left ? x[k] : 0.f;
-      store8(x, a.out_m + p.at, kPer);
+      if constexpr (kEight) decode<true>(m, *reinterpret_cast<const unsigned*>(static_cast<const unsigned char*>(a.m) + c.at + i), a.m_exponent[(c.at + i) / kMomentBlock]);
+      else unpack(m, *reinterpret_cast<const u32x4*>(static_cast<const float*>(a.m) + c.at + i), 0.f);
     }
     if (a.out_v) {
-      if constexpr (kEight) decode<false>(x, *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.v) + p.at), a.v_exponent[p.at / kMomentBlock]);
-      else load8(x, a.v, p.at, kPer, false);
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) x[k] = k < p.left ? x[k] : 0.f;
-      store8(x, a.out_v + p.at, kPer);
+      if constexpr (kEight) decode<false>(v, *reinterpret_cast<const unsigned*>(static_cast<const unsigned char*>(a.v) + c.at + i), a.v_exponent[(c.at + i) / kMomentBlock]);
+      else unpack(v, *reinterpret_cast<const u32x4*>(static_cast<const float*>(a.v) + c.at + i), 0.f);
     }
+    if (a.out_w) put(a.out_w, w);
+    if (a.out_m) put(a.out_m, m);
+    if (a.out_v) put(a.out_v, v);
   }
 }
 
-unsigned blocks_of(const AdamwArgs& a) {
-  const long long most = 8LL * a.n_cu;
-  return (unsigned)(a.chunks < 1 ? 1 : (a.chunks < most ? a.chunks : most));
+unsigned blocks_of(long long work) {
+  const int most = 1 << 23;                    // a launch has less than 2^32 threads
+  return (unsigned)(work < 1 ? 1 : (work < most ? work : most));
 }
 
 }  // namespace
@@ -308,14 +418,15 @@ long long adamw_chunks(long long n) { return (n + kChunk - 1) / kChunk; }
 
 hipError_t launch_adamw(const AdamwArgs& a, bool eight, hipStream_t s) {
   static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
-  if (eight) hipLaunchKernelGGL((adamw_kernel<true>), dim3(blocks_of(a)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((adamw_kernel<false>), dim3(blocks_of(a)), dim3(kThreads), 0, s, a);
+  if (eight) hipLaunchKernelGGL((adamw_kernel<true>), dim3(blocks_of(a.chunks)), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((adamw_kernel<false>), dim3(blocks_of(a.chunks)), dim3(kThreads), 0, s, a);
+  if (a.count_up && blocks_of(a.chunks) > kCounted) hipLaunchKernelGGL(count_up_kernel, dim3(1), dim3(1), 0, s, a.steps);
   return hipGetLastError();
 }
 hipError_t launch_adamw_values(const AdamwArgs& a, bool eight, hipStream_t s) {
   if (a.chunks < 1) return hipSuccess;
-  if (eight) hipLaunchKernelGGL((values_kernel<true>), dim3(blocks_of(a)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((values_kernel<false>), dim3(blocks_of(a)), dim3(kThreads), 0, s, a);
+  if (eight) hipLaunchKernelGGL((values_kernel<true>), dim3(blocks_of(2LL * a.chunks)), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((values_kernel<false>), dim3(blocks_of(2LL * a.chunks)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -2042,7 +2042,6 @@ dc_status adamw_call(dc_ctx* ctx, const dc_adamw_args* a, bool step, float* cons
   k.m_exponent = a->m_exponent;
   k.v_exponent = a->v_exponent;
   k.low = a->low;
-  k.n_cu = ctx->n_cu;
   if (step) {
     k.steps = a->steps;
     k.grad_scale = a->grad_scale;
@@ -2107,12 +2106,9 @@ dc_status adamw_call(dc_ctx* ctx, const dc_adamw_args* a, bool step, float* cons
       const hipError_t e = launch();
       if (e != hipSuccess) return hip_fail(ctx, e, "AdamW launch");
     }
-    const int j = k.tensors++;
-    k.first[j] = k.chunks;
-    k.chunks += (int)adamw_chunks(t.n);          // 2^27 of all tensors at most
-    k.p16[j] = t.p_dtype == DC_BF16;
-    k.g16[j] = t.g_dtype == DC_BF16;
-    k.t[j] = AdamwTensor{t.p, t.g, (long long)t.n, (unsigned)(t.at / kMomentBlock), (float)t.weight_decay};
+    k.t[k.tensors++] = AdamwTensor{t.p, t.g, (long long)t.n, (unsigned)(t.at / kMomentBlock), (float)t.weight_decay, k.chunks,
+                                   (t.p_dtype == DC_BF16 ? 1 : 0) | (t.g_dtype == DC_BF16 ? 2 : 0)};
+    k.chunks += (int)adamw_chunks(t.n);          // 2^26 of all tensors at most
   }
   k.count_up = step;
   if (step || k.chunks > 0) return enqueue_result(ctx, launch(), "AdamW launch");

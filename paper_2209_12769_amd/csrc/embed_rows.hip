@@ -24,40 +24,55 @@ __device__ __forceinline__ int kind_of(const EmbedArgs& a, long long row) {
   return -1;
 }
 
-constexpr int kAtOnce = 4;     // rows of a seat
-
-// Items: kAtOnce neighbouring rows and a slab of `lanes` vectors.
+#ifndef ATONCE
+#define ATONCE 8
+#endif
+constexpr int kAtOnce = ATONCE;     // rows of a thread, its columns are the same in all of them
+// A workgroup takes `across` neighbouring rows of `used` vectors at a time, kAtOnce times; slabs of rows too wide for one are
+// blockIdx.y.
 template <typename T>
-__global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a, int lanes, int nslab) {
+__global__ __launch_bounds__(1024) void embed_kernel(const EmbedArgs a, int used, int across) {
   constexpr int kV = kVector<T>;
-  const int t = threadIdx.x & (lanes - 1), seats = 256 / lanes;
-  const long long groups = (a.rows + kAtOnce - 1) / kAtOnce, items = groups * nslab;
-  for (long long i = (long long)blockIdx.x * seats + threadIdx.x / lanes; i < items; i += (long long)gridDim.x * seats) {
-    const long long group = nslab == 1 ? i : i / nslab;
-    const int slab = (int)(i - group * nslab), c = (slab * lanes + t) * kV;
+  int seat = (int)((float)threadIdx.x / (float)used);          // the quotient put right where it is one off
+  if ((seat + 1) * used <= (int)threadIdx.x) ++seat;
+  if (seat * used > (int)threadIdx.x) --seat;
+  const int t = (int)threadIdx.x - seat * used, column = ((int)blockIdx.y * used + t) * kV;
+  if (seat >= across || column >= a.C) return;
+  const unsigned c = max(min(column, a.C - kV), 0);            // the last vector ends with the row
+  const unsigned y_on = (unsigned)seat * (unsigned)a.ldy + c;  // rows are at most 2^22 elements apart, seats 1024
+  const T* table = static_cast<const T*>(a.table);
+  for (long long row0 = (long long)blockIdx.x * across * kAtOnce; row0 < a.rows; row0 += (long long)gridDim.x * across * kAtOnce) {
+    const int left = (int)min(a.rows - row0, (long long)across * kAtOnce);
+    const int* id = a.id + row0;
+    T* Y = static_cast<T*>(a.Y) + row0 * a.ldy;
     int kind[kAtOnce];
     u32x4 v[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) kind[u] = kind_of(a, min(group * kAtOnce + u, a.rows - 1));
-    if (c >= a.C) continue;
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-      v[u] = load_vector<T, false>(static_cast<const T*>(a.table) + (long long)max(kind[u], 0) * a.ldt, c, a.C);
+    for (int u = 0; u < kAtOnce; ++u) kind[u] = id[min(u * across + seat, left - 1)];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      const long long row = group * kAtOnce + u;
-      if (row >= a.rows) break;
+      if (kind[u] < 0 || kind[u] >= a.kinds) {
+        if (kind[u] != -1) atomicCAS(&a.status[1], 0, (int)DC_ERR_INVALID_ARG);
+        kind[u] = -1;
+      }
+      v[u] = load_vector<T, false>(table + (long long)max(kind[u], 0) * a.ldt, (int)c, a.C);
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (u * across + seat >= left) break;
       float x[kV];
       unpack(x, v[u], T());
 #pragma unroll
       for (int k = 0; k < kV; ++k) x[k] = kind[u] < 0 ? 0.f : x[k] * a.scale;
-      store_vector<T, false>(static_cast<T*>(a.Y) + row * a.ldy, c, a.C, pack(x, T()));
+      T* to = Y + (long long)(u * across) * a.ldy;
+      if (a.C >= kV) *reinterpret_cast<u32x4_any*>(to + y_on) = pack(x, T());
+      else store_vector<T, false>(to + y_on, 0, a.C, pack(x, T()));
     }
   }
 }
 
 // ---- sort ----
-constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64, kPer = 16, kTile = kSortThreads * kPer;
+constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64;
 constexpr int kBits = 9, kBins = 1 << kBits;
 
 struct Pair {
@@ -86,6 +101,7 @@ __device__ __forceinline__ void in_order() {
 }
 
 // How many pairs of each tile have each digit: count[digit][tile].
+template <int kPer>
 __global__ __launch_bounds__(kSortThreads) void count_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, int* count) {
   __shared__ int bin[kBins];
   const int bins = 1 << bits, n = (int)a.rows, tile = blockIdx.x;
@@ -93,7 +109,7 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(const EmbedArgs a, 
   __syncthreads();
 #pragma unroll 4
   for (int k = 0; k < kPer; ++k) {
-    const long long i = (long long)tile * kTile + k * kSortThreads + threadIdx.x;
+    const long long i = (long long)tile * (kSortThreads * kPer) + k * kSortThreads + threadIdx.x;
     const bool in_range = i < n;
     const int digit = in_range ? pair_at(a, in, (int)i).kind >> shift & (bins - 1) : 0;
     const u64 peers = same_digit(digit, bits, __ballot(in_range));
@@ -140,6 +156,7 @@ __global__ __launch_bounds__(256) void scan_kernel(int* count, int tiles, int* t
 }
 
 // Every pair to its place: its digit's first place, the tiles in front, the pairs of the tile in front.
+template <int kPer>
 __global__ __launch_bounds__(kSortThreads) void scatter_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, const int* count,
                                                                const int* total, Pair* out) {
   __shared__ int first[kBins];
@@ -159,7 +176,7 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(const EmbedArgs a
   // a wave's pairs are neighbours: 64 at a time
   Pair p[kPer];
   u64 peers[kPer];
-  const long long base = (long long)tile * kTile + wave * 64 * kPer + lane;
+  const long long base = (long long)tile * (kSortThreads * kPer) + wave * 64 * kPer + lane;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const long long i = base + k * 64;
@@ -202,7 +219,8 @@ struct Sums {
   int n;                       // entries of the list: rows, or entries of the level below
   int chunk;                   // entries of a chunk
   int nchunk;
-  int lanes, nslab;            // vectors of a slab, slabs of a row
+  int lanes, nslab;            // places for a slab's vectors, slabs of a row
+  int used;                    // vectors of a slab
   const float* in;             // levels above the first: [n][C]
   const int* in_kind;          // [n]: the kind, or ~kind of an entry without a sum
   float* out;                  // [2 nchunk][C]
@@ -217,7 +235,8 @@ __device__ __forceinline__ void write_kind(const EmbedArgs& a, int kind, int c, 
   for (int k = 0; k < kVector<T>; ++k) y[k] = x[k] * a.scale;
   store_vector<T, false>(static_cast<T*>(a.dtable) + (long long)kind * a.lddt, c, a.C, pack(y, T()));
 }
-// An entry of the next list: kVector<T> columns from c.
+// Four columns of an entry from c.
+__device__ __forceinline__ void read_entry(float (&x)[4], const float* row, int c, int C) { unpack(x, load_vector<float, false>(row, c, C), 0.f); }
 template <int kV>
 __device__ __forceinline__ void write_entry(float* row, int c, int C, const float (&x)[kV]) {
 #pragma unroll
@@ -226,35 +245,53 @@ __device__ __forceinline__ void write_entry(float* row, int c, int C, const floa
     if (c + k < C) store_vector<float, false>(row, c + k, C, pack(y, 0.f));
   }
 }
-template <int kV>
-__device__ __forceinline__ void read_entry(float (&x)[kV], const float* row, int c, int C) {
+// Four columns of a kind.
+__device__ __forceinline__ void write_kind4(const EmbedArgs& a, int kind, int c, const float (&x)[4]) {
+  float y[4];
 #pragma unroll
-  for (int k = 0; k < kV; k += 4) {
-    float y[4];
-    unpack(y, c + k < C ? load_vector<float, false>(row, c + k, C) : u32x4{0, 0, 0, 0}, 0.f);
+  for (int k = 0; k < 4; ++k) y[k] = x[k] * a.scale;
+  if (!a.bf16) {
+    store_vector<float, false>(static_cast<float*>(a.dtable) + (long long)kind * a.lddt, c, a.C, pack(y, 0.f));
+    return;
+  }
+  u16* row = static_cast<u16*>(a.dtable) + (long long)kind * a.lddt;
+  const unsigned lo = pack_bf16x2(y[0], y[1]), hi = pack_bf16x2(y[2], y[3]);
+  if (c + 4 <= a.C) {
+    *reinterpret_cast<u32x2_any*>(row + c) = u32x2{lo, hi};
+  } else {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[k + u] = y[u];
+    for (int k = 0; k < 4; ++k)
+      if (c + k < a.C) row[c + k] = (u16)((k < 2 ? lo : hi) >> (16 * (k & 1)));
   }
 }
 
 constexpr int kRun = 64;       // rows summed in fp32 before they join the others'
 
-// What a chunk has of one kind is done with: the last one, if `last`.
-template <typename T>
-__device__ __forceinline__ void close_kind(const Sums& s, int chunk, int kind, int c, const float (&x)[kVector<T>], bool any, bool first, bool last,
-                                           bool from_before, bool goes_on) {
-  const bool up = (first && from_before) || (last && goes_on);
-  const int entry = 2 * chunk + (first ? 0 : 1);
-  if (!up) {
-    if (any) write_kind<T>(s.a, kind, c, x);
-  } else if (any) {
-    write_entry(s.out + (size_t)entry * s.a.C, c, s.a.C, x);
+// What a chunk has of one kind is done with: kind and columns written at once, or an entry of the next list.
+struct Close {
+  int chunk;
+  bool from_before, goes_on;   // the chunk's first kind began in front of it, its last one goes on behind
+};
+template <int kV, typename F>
+__device__ __forceinline__ void close_kind(const Sums& s, const Close& k, int kind, int c, const float (&x)[kV], bool any, bool first, bool last, F write) {
+  const bool up = (first && k.from_before) || (last && k.goes_on);
+  const size_t entry = 2 * (size_t)k.chunk + (first ? 0 : 1);
+  if (any) {
+    if (up) write_entry<kV>(s.out + entry * s.a.C, c, s.a.C, x);
+    else write(kind, x);
   }
-  if (c < kVector<T>) {        // the row's first vector says what the entries are
-    if (first) s.out_kind[2 * chunk] = up && any ? kind : ~kind;
-    if (last && first) s.out_kind[2 * chunk + 1] = ~kind;
-    if (last && !first) s.out_kind[2 * chunk + 1] = up && any ? kind : ~kind;
+  if (c == 0) {                // the thread of the row's first columns says what the entries are
+    if (first) s.out_kind[2 * (size_t)k.chunk] = up && any ? kind : ~kind;
+    if (last && first) s.out_kind[2 * (size_t)k.chunk + 1] = ~kind;
+    if (last && !first) s.out_kind[2 * (size_t)k.chunk + 1] = up && any ? kind : ~kind;
   }
+}
+// The columns of a seat's thread; below zero if it has none.  The last vector ends with the row, so that two threads may have
+// the same columns and write the same.
+template <int kV>
+__device__ __forceinline__ int columns_of(const Sums& s, int slab, int t) {
+  const int c = (slab * s.used + t) * kV;
+  return t < s.used && c < s.a.C ? max(min(c, s.a.C - kV), 0) : -1;
 }
 
 // Clears the kinds that have no row: 64 kinds a wave.
@@ -288,14 +325,17 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
   const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
   const long long item = (long long)(blockIdx.x - s.fill_blocks) * seats + threadIdx.x / s.lanes;
   if (item >= (long long)s.nchunk * s.nslab) return;
-  const int chunk = (int)(item / s.nslab), c = ((int)(item - (long long)chunk * s.nslab) * s.lanes + t) * kV;
-  if (c >= a.C) return;
-  const long long p0l = (long long)chunk * s.chunk;
+  Close close;
+  close.chunk = (int)(item / s.nslab);
+  const int c = columns_of<kV>(s, (int)(item - (long long)close.chunk * s.nslab), t);
+  if (c < 0) return;
+  const long long p0l = (long long)close.chunk * s.chunk;
   const int p0 = (int)p0l, p1 = (int)min(p0l + s.chunk, (long long)s.n), len = p1 - p0;
   const T* dY = static_cast<const T*>(a.dY);
   int kind = s.sorted[p0].kind;
-  const bool from_before = p0 > 0 && s.sorted[p0 - 1].kind == kind;
+  close.from_before = p0 > 0 && s.sorted[p0 - 1].kind == kind;
   const int past = p1 < s.n ? s.sorted[p1].kind : -1;
+  auto write = [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c, x); };
   float sum[kV], run[kV];
 #pragma unroll
   for (int k = 0; k < kV; ++k) sum[k] = run[k] = 0.f;
@@ -315,7 +355,7 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
       if (e[u].kind != kind) {
 #pragma unroll
         for (int k = 0; k < kV; ++k) sum[k] += run[k];
-        close_kind<T>(s, chunk, kind, c, sum, true, first, false, from_before, false);
+        close_kind(s, close, kind, c, sum, true, first, false, write);
 #pragma unroll
         for (int k = 0; k < kV; ++k) sum[k] = run[k] = 0.f;
         count = 0;
@@ -338,97 +378,110 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
   }
 #pragma unroll
   for (int k = 0; k < kV; ++k) sum[k] += run[k];
-  close_kind<T>(s, chunk, kind, c, sum, kind < a.kinds, first, true, from_before, past == kind);
+  close.goes_on = past == kind;
+  close_kind(s, close, kind, c, sum, kind < a.kinds, first, true, write);
 }
 
 __device__ __forceinline__ int kind_of_entry(int k) { return k < 0 ? ~k : k; }
 
-// Levels between: chunks of a list of entries, sums in 64 bits.
-template <typename T>
+// Levels between: chunks of a list of entries, four columns a thread, sums in 64 bits.
 __global__ __launch_bounds__(256) void sum_entries_kernel(const Sums s) {
-  constexpr int kV = kVector<T>;
+  constexpr int kAhead = 8;
   const EmbedArgs& a = s.a;
   const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
   const long long item = (long long)blockIdx.x * seats + threadIdx.x / s.lanes;
   if (item >= (long long)s.nchunk * s.nslab) return;
-  const int chunk = (int)(item / s.nslab), c = ((int)(item - (long long)chunk * s.nslab) * s.lanes + t) * kV;
-  if (c >= a.C) return;
-  const int p0 = chunk * s.chunk, p1 = min(p0 + s.chunk, s.n);
+  Close close;
+  close.chunk = (int)(item / s.nslab);
+  const int c = columns_of<4>(s, (int)(item - (long long)close.chunk * s.nslab), t);
+  if (c < 0) return;
+  const int p0 = close.chunk * s.chunk, p1 = min(p0 + s.chunk, s.n);
   int kind = kind_of_entry(s.in_kind[p0]);
-  const bool from_before = p0 > 0 && kind_of_entry(s.in_kind[p0 - 1]) == kind;
+  close.from_before = p0 > 0 && kind_of_entry(s.in_kind[p0 - 1]) == kind;
   const int past = p1 < s.n ? kind_of_entry(s.in_kind[p1]) : -1;
-  double sum[kV];
-  float x[kV];
-#pragma unroll
-  for (int k = 0; k < kV; ++k) sum[k] = 0.0;
+  auto write = [&](int of, const float (&x)[4]) { write_kind4(a, of, c, x); };
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  float x[4];
   bool first = true, any = false;
-  for (int p = p0; p < p1; ++p) {
-    const int e = s.in_kind[p], of = kind_of_entry(e);
-    if (of != kind) {
+  for (int p = p0; p < p1; p += kAhead) {
+    int e[kAhead];
+    float v[kAhead][4];
 #pragma unroll
-      for (int k = 0; k < kV; ++k) {
-        x[k] = (float)sum[k];
-        sum[k] = 0.0;
+    for (int u = 0; u < kAhead; ++u) e[u] = s.in_kind[min(p + u, p1 - 1)];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (e[u] >= 0) read_entry(v[u], s.in + (size_t)min(p + u, p1 - 1) * a.C, c, a.C);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (p + u >= p1) break;
+      const int of = kind_of_entry(e[u]);
+      if (of != kind) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = (float)sum[k];
+          sum[k] = 0.0;
+        }
+        close_kind(s, close, kind, c, x, any, first, false, write);
+        first = any = false;
+        kind = of;
       }
-      close_kind<T>(s, chunk, kind, c, x, any, first, false, from_before, false);
-      first = any = false;
-      kind = of;
-    }
-    if (e < 0) continue;
-    any = true;
-    read_entry(x, s.in + (size_t)p * a.C, c, a.C);
+      if (e[u] < 0) continue;
+      any = true;
 #pragma unroll
-    for (int k = 0; k < kV; ++k) sum[k] += (double)x[k];
+      for (int k = 0; k < 4; ++k) sum[k] += (double)v[u][k];
+    }
   }
 #pragma unroll
-  for (int k = 0; k < kV; ++k) x[k] = (float)sum[k];
-  close_kind<T>(s, chunk, kind, c, x, any, first, true, from_before, past == kind);
+  for (int k = 0; k < 4; ++k) x[k] = (float)sum[k];
+  close.goes_on = past == kind;
+  close_kind(s, close, kind, c, x, any, first, true, write);
 }
 
-// The last list: a workgroup for each entry that begins a kind, and 64 vectors of its columns; its waves take the entries in turn.
-constexpr int kLastWaves = 4;
-template <typename T>
+// The last list: a workgroup for each entry that begins a kind, and 256 of its columns; its waves take the entries in turn.
+constexpr int kLastWaves = 16;
 __global__ __launch_bounds__(64 * kLastWaves) void last_sums_kernel(const Sums s) {
-  constexpr int kV = kVector<T>;
+  constexpr int kAhead = 4;
   const EmbedArgs& a = s.a;
   const int p0 = blockIdx.x, kind = kind_of_entry(s.in_kind[p0]);
   if (kind >= a.kinds || (p0 > 0 && kind_of_entry(s.in_kind[p0 - 1]) == kind)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * kV;
-  __shared__ double part[kLastWaves][64][kV + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = (blockIdx.y * 64 + lane) * 4, c = max(min(at, a.C - 4), 0);
+  __shared__ double part[kLastWaves][64][4];
   __shared__ int found[kLastWaves];
-  double sum[kV];
-#pragma unroll
-  for (int k = 0; k < kV; ++k) sum[k] = 0.0;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
   int any = 0;
-  for (int p = p0 + wave; p < s.n; p += kLastWaves) {
-    const int e = s.in_kind[p];
-    if (kind_of_entry(e) != kind) break;
-    if (e < 0) continue;
-    any = 1;
-    if (c >= a.C) continue;
-    float x[kV];
-    read_entry(x, s.in + (size_t)p * a.C, c, a.C);
+  for (int p = p0 + wave; p < s.n; p += kLastWaves * kAhead) {
+    int e[kAhead];
+    float v[kAhead][4];
 #pragma unroll
-    for (int k = 0; k < kV; ++k) sum[k] += (double)x[k];
+    for (int u = 0; u < kAhead; ++u) e[u] = s.in_kind[min(p + u * kLastWaves, s.n - 1)];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (e[u] == kind) read_entry(v[u], s.in + (size_t)min(p + u * kLastWaves, s.n - 1) * a.C, c, a.C);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (p + u * kLastWaves >= s.n || e[u] != kind) continue;
+      any = 1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum[k] += (double)v[u][k];
+    }
+    if (kind_of_entry(e[kAhead - 1]) != kind) break;
   }
 #pragma unroll
-  for (int k = 0; k < kV; ++k) part[wave][lane][k] = sum[k];
+  for (int k = 0; k < 4; ++k) part[wave][lane][k] = sum[k];
   if (lane == 0) found[wave] = any;
   __syncthreads();
-  if (wave != 0 || c >= a.C) return;
-  float x[kV];
-  for (int w = 1; w < kLastWaves; ++w) any |= found[w];
+  if (wave != 0 || at >= a.C) return;
+  for (int w = 1; w < kLastWaves; ++w) {
+    any |= found[w];
 #pragma unroll
-  for (int k = 0; k < kV; ++k) {
-    double v = part[0][lane][k];
-    for (int w = 1; w < kLastWaves; ++w) v += part[w][lane][k];
-    x[k] = (float)v;
+    for (int k = 0; k < 4; ++k) sum[k] += part[w][lane][k];
   }
-  if (any) write_kind<T>(a, kind, c, x);
+  const float x[4] = {(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]};
+  if (any) write_kind4(a, kind, c, x);
 }
 
 constexpr int kLastMost = 2048;        // entries that the last launch takes
-constexpr int kEntryChunk = 64;
+constexpr int kEntryChunk = 16;
 
 int lanes_of(int vectors) {
   int l = 1;
@@ -437,7 +490,8 @@ int lanes_of(int vectors) {
 }
 
 struct Plan {
-  int passes, bits, tiles;
+  int passes, bits;
+  int per, tiles;              // pairs of a thread; workgroups of the sort
   int lanes, nslab;            // of rows of 16-byte vectors
   int chunk, nchunk;
   long long entries[8];        // of each level's list
@@ -449,7 +503,8 @@ Plan plan(long long rows, int kinds, int C, int bytes, int n_cu) {
   while (bits < 31 && (kinds >> bits) != 0) ++bits;            // values 0 .. kinds
   p.passes = (bits + kBits - 1) / kBits;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.tiles = (int)((rows + kTile - 1) / kTile);
+  p.per = rows <= 65536 ? 1 : (rows <= 1048576 ? 4 : 16);
+  p.tiles = (int)((rows + kSortThreads * p.per - 1) / (kSortThreads * p.per));
   const int vectors = (C * bytes + 15) / 16;
   p.lanes = lanes_of(vectors);
   p.nslab = (vectors + p.lanes - 1) / p.lanes;
@@ -502,6 +557,7 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
   m.nchunk = p.nchunk;
   m.lanes = p.lanes;
   m.nslab = p.nslab;
+  m.used = ((a.C + kVector<T> - 1) / kVector<T> + p.nslab - 1) / p.nslab;
   const long long fill = ((long long)a.kinds + 255) / 256, fill_most = 8LL * a.n_cu;
   m.fill_blocks = (int)(fill < fill_most ? fill : fill_most);
   const int seats = 256 / p.lanes;
@@ -511,6 +567,11 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
     m.out_kind = reinterpret_cast<int*>(a.workspace + r.kind[0]);
   }
   hipLaunchKernelGGL((sum_rows_kernel<T>), dim3(m.fill_blocks + blocks(p.nchunk)), dim3(256), 0, s, m);
+  // entries: four columns a thread
+  const int fours = (a.C + 3) / 4;
+  m.lanes = lanes_of(fours);
+  m.nslab = (fours + m.lanes - 1) / m.lanes;
+  m.used = (fours + m.nslab - 1) / m.nslab;
   for (int l = 0; l < p.levels; ++l) {
     m.n = (int)p.entries[l];
     m.in = m.out;
@@ -520,12 +581,29 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
       m.nchunk = (int)(p.entries[l + 1] / 2);
       m.out = reinterpret_cast<float*>(a.workspace + r.sum[l + 1]);
       m.out_kind = reinterpret_cast<int*>(a.workspace + r.kind[l + 1]);
-      hipLaunchKernelGGL((sum_entries_kernel<T>), dim3(blocks(m.nchunk)), dim3(256), 0, s, m);
+      const long long seats = 256 / m.lanes, items = (long long)m.nchunk * m.nslab;
+      hipLaunchKernelGGL(sum_entries_kernel, dim3((unsigned)((items + seats - 1) / seats)), dim3(256), 0, s, m);
     } else {
-      const int vectors = (a.C + kVector<T> - 1) / kVector<T>;
-      hipLaunchKernelGGL((last_sums_kernel<T>), dim3((unsigned)m.n, (vectors + 63) / 64), dim3(64 * kLastWaves), 0, s, m);
+      hipLaunchKernelGGL(last_sums_kernel, dim3((unsigned)m.n, (fours + 63) / 64), dim3(64 * kLastWaves), 0, s, m);
     }
   }
+}
+
+template <int kPer>
+const Pair* sort(const EmbedArgs& a, const Plan& p, const Room& r, hipStream_t s) {
+  Pair* pair[2] = {reinterpret_cast<Pair*>(a.workspace + r.pair[0]), reinterpret_cast<Pair*>(a.workspace + r.pair[1])};
+  int* count = reinterpret_cast<int*>(a.workspace + r.count);
+  int* total = reinterpret_cast<int*>(a.workspace + r.total);
+  const Pair* in = nullptr;
+  for (int k = 0; k < p.passes; ++k) {
+    const int shift = k * p.bits;
+    Pair* out = pair[k & 1];
+    hipLaunchKernelGGL((count_kernel<kPer>), dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, count);
+    hipLaunchKernelGGL(scan_kernel, dim3(1 << p.bits), dim3(256), 0, s, count, p.tiles, total);
+    hipLaunchKernelGGL((scatter_kernel<kPer>), dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, (const int*)count, (const int*)total, out);
+    in = out;
+  }
+  return in;
 }
 
 }  // namespace
@@ -538,33 +616,32 @@ size_t embed_rows_bytes(long long rows, int kinds, int C, int n_cu) {
 
 hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  const int vectors = (a.C * (a.bf16 ? 2 : 4) + 15) / 16, lanes = lanes_of(vectors), nslab = (vectors + lanes - 1) / lanes;
-  const long long items = (a.rows + kAtOnce - 1) / kAtOnce * nslab, seats = 256 / lanes, need = (items + seats - 1) / seats, most = 16LL * a.n_cu;
-  const dim3 grid((unsigned)(need < most ? need : most));
-  if (a.bf16) hipLaunchKernelGGL((embed_kernel<u16>), grid, dim3(256), 0, s, a, lanes, nslab);
-  else hipLaunchKernelGGL((embed_kernel<float>), grid, dim3(256), 0, s, a, lanes, nslab);
+  const int vectors = (a.C * (a.bf16 ? 2 : 4) + 15) / 16, slabs = (vectors + 1023) / 1024, used = (vectors + slabs - 1) / slabs;
+  // rows of a workgroup: the fewest that leave less than an eighth of its waves' places empty, at least 256 places
+  int across = 1;
+  for (int best = 0, n = 1; n * used <= 1024; ++n) {
+    const int fill = n * used * 1000 / ((n * used + 63) / 64 * 64);
+    if (n * used < 192 && (n + 1) * used <= 1024) continue;
+    if (fill > best) {
+      best = fill;
+      across = n;
+    }
+    if (fill >= 875) break;
+  }
+  const int threads = (across * used + 63) / 64 * 64;
+  const long long need = (a.rows + across * kAtOnce - 1) / (across * kAtOnce), most = (1LL << 31) / threads;     // a launch has less than 2^32 threads
+  const dim3 grid((unsigned)(need < most ? need : most), (unsigned)slabs), block((unsigned)threads);
+  if (a.bf16) hipLaunchKernelGGL((embed_kernel<u16>), grid, block, 0, s, a, used, across);
+  else hipLaunchKernelGGL((embed_kernel<float>), grid, block, 0, s, a, used, across);
   return hipGetLastError();
 }
 
 hipError_t launch_embed_rows_back(const EmbedArgs& a, hipStream_t s) {
   const Plan p = plan(a.rows, a.kinds, a.C, a.bf16 ? 2 : 4, a.n_cu);
   const Room r = room(p, a.rows, a.C);
-  Pair* pair[2] = {reinterpret_cast<Pair*>(a.workspace + r.pair[0]), reinterpret_cast<Pair*>(a.workspace + r.pair[1])};
-  const Pair* in = nullptr;
-  if (a.rows > 0) {
-    int* count = reinterpret_cast<int*>(a.workspace + r.count);
-    int* total = reinterpret_cast<int*>(a.workspace + r.total);
-    for (int k = 0; k < p.passes; ++k) {
-      const int shift = k * p.bits;
-      Pair* out = pair[k & 1];
-      hipLaunchKernelGGL(count_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, count);
-      hipLaunchKernelGGL(scan_kernel, dim3(1 << p.bits), dim3(256), 0, s, count, p.tiles, total);
-      hipLaunchKernelGGL(scatter_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, (const int*)count, (const int*)total, out);
-      in = out;
-    }
-  }
-  if (a.bf16) gradient<u16>(a, p, r, in, s);
-  else gradient<float>(a, p, r, in, s);
+  const Pair* sorted = a.rows == 0 ? nullptr : p.per == 1 ? sort<1>(a, p, r, s) : p.per == 4 ? sort<4>(a, p, r, s) : sort<16>(a, p, r, s);
+  if (a.bf16) gradient<u16>(a, p, r, sorted, s);
+  else gradient<float>(a, p, r, sorted, s);
   return hipGetLastError();
 }
 

@@ -252,6 +252,8 @@ struct AdamwTensor {
   long long n;
   unsigned block;              // its first place / kMomentBlock
   float decay;
+  int first;                   // its first chunk in the launch
+  int types;                   // 1: p is bf16, 2: g is
 };
 constexpr int kAdamwTensors = 96;      // of one launch: its arguments stay below 4 KiB
 struct AdamwArgs {
@@ -264,11 +266,8 @@ struct AdamwArgs {
   float lr, b1, b2, o1, o2, eps;       // o: 1 - beta
   unsigned long long seed;
   float *out_w, *out_m, *out_v;        // values: each or null
-  int n_cu;
   int count_up;                // the last launch of a call
   int tensors, chunks;
-  int first[kAdamwTensors];    // first chunk of each tensor
-  unsigned char p16[kAdamwTensors], g16[kAdamwTensors];
   AdamwTensor t[kAdamwTensors];
 };
 long long adamw_chunks(long long n);

@@ -24,7 +24,34 @@ constexpr int kNarrow = 512;   // channels that a wave's lanes hold
 constexpr int kRun = 64;       // rows whose terms are summed in fp32 before they join the others'
 constexpr int kMostWaves = 16;
 
-// NV vectors of a row, vector j of a thread at columns (j * lanes + t) * kVector.
+// How a thread's vectors lie in a row, vector j of kVector values at columns (j * lanes + t) * kVector:
+//   kWhole  the row is all of them;
+//   kBack   the row ends before the last: the vector that would reach beyond it ends with the row instead, and its first
+//           `skip` values are its neighbour's, which it may write, being the same, but not count;
+//   kShort  the row is shorter than one vector.
+enum Fit { kWhole, kBack, kShort };
+template <typename T, int NV>
+struct Columns {
+  int at[NV], skip[NV];        // skip: kVector<T> of a vector with no value of its own
+};
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ Columns<T, NV> columns_of(int t, int lanes, int C) {
+  constexpr int kV = kVector<T>;
+  Columns<T, NV> q;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * lanes + t) * kV;
+    q.at[j] = kFit == kWhole ? c : max(min(c, C - kV), 0);
+    q.skip[j] = kFit == kWhole ? 0 : min(c - q.at[j], kV);
+  }
+  return q;
+}
+// Whether value k of vector j is the thread's own.
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ bool own(const Columns<T, NV>& q, int j, int k, int C) {
+  return kFit == kWhole || (k >= q.skip[j] && (kFit == kBack || k < C));
+}
+
 template <typename T, typename X, int NV>
 struct Fetched {
   u32x4 v[NV];
@@ -32,38 +59,36 @@ struct Fetched {
 template <int NV>
 struct Fetched<u16, Kept8, NV> {
   u32x2 v[NV];
-  unsigned e[NV];
+  unsigned e[NV], e2[NV];      // exponents of its first and of its last value
 };
 template <int NV>
 struct Fetched<float, Kept8, NV> {
   unsigned v[NV];
-  unsigned e[NV];
+  unsigned e[NV], e2[NV];
 };
-template <typename T, int NV, bool kFull>
-__device__ __forceinline__ void fetch(Fetched<T, T, NV>& f, const void* rows, long long ld, long long row, int t, int lanes, int C) {
-  const T* p = static_cast<const T*>(rows) + row * ld;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) f.v[j] = load_vector<T, kFull>(p, (j * lanes + t) * kVector<T>, C);
-}
-// A row of codes goes up to a multiple of 32: a vector that begins inside the row ends inside it.
-template <typename T, int NV, bool kFull>
-__device__ __forceinline__ void fetch(Fetched<T, Kept8, NV>& f, const KeptView& k, long long row, int t, int lanes, int C) {
-  const signed char* p = k.code + row * k.ld_code;
-  const unsigned char* e = k.exponent + row * k.ld_exponent;
+// `row` elements from p on: p is the same for the wave, so that only 32 bits are the lane's own.
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ void fetch(Fetched<T, T, NV>& f, const T* p, unsigned row, const Columns<T, NV>& q, int C) {
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int c = (j * lanes + t) * kVector<T>;
-    f.v[j] = decltype(f.v[j] + f.v[j]){};
-    f.e[j] = 0;
-    if (kFull || c < C) {
-      if constexpr (sizeof(T) == 2) f.v[j] = *reinterpret_cast<const u32x2_any*>(p + c);
-      else f.v[j] = *reinterpret_cast<const u32_any*>(p + c);
-      f.e[j] = e[c / kKeptBlock];
-    }
+    if constexpr (kFit == kShort) f.v[j] = load_vector<T, false>(p + row, q.at[j], C);
+    else f.v[j] = *reinterpret_cast<const u32x4_any*>(p + (row + (unsigned)q.at[j]));
   }
 }
-template <typename T, int NV>
-__device__ __forceinline__ void values(float (&x)[NV * kVector<T>], const Fetched<T, T, NV>& f) {
+// A row of codes goes up to a multiple of 32, so a short one has a whole vector too.
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ void fetch(Fetched<T, Kept8, NV>& f, const signed char* p, unsigned row, const unsigned char* e, unsigned row_e, const Columns<T, NV>& q) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const unsigned at = q.at[j];
+    if constexpr (sizeof(T) == 2) f.v[j] = *reinterpret_cast<const u32x2_any*>(p + (row + at));
+    else f.v[j] = *reinterpret_cast<const u32_any*>(p + (row + at));
+    f.e[j] = e[row_e + at / kKeptBlock];
+    f.e2[j] = kFit == kBack ? e[row_e + (at + kVector<T> - 1) / kKeptBlock] : 0;
+  }
+}
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ void values(float (&x)[NV * kVector<T>], const Fetched<T, T, NV>& f, const Columns<T, NV>&) {
   constexpr int kV = kVector<T>;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -73,64 +98,73 @@ __device__ __forceinline__ void values(float (&x)[NV * kVector<T>], const Fetche
     for (int k = 0; k < kV; ++k) x[j * kV + k] = w[k];
   }
 }
-template <typename T, int NV>
-__device__ __forceinline__ void values(float (&x)[NV * kVector<T>], const Fetched<T, Kept8, NV>& f) {
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ void values(float (&x)[NV * kVector<T>], const Fetched<T, Kept8, NV>& f, const Columns<T, NV>& q) {
   constexpr int kV = kVector<T>;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const float s = kept_scale(f.e[j]);
+    const float s = kept_scale(f.e[j]), s2 = kFit == kBack ? kept_scale(f.e2[j]) : 0.f;
+    const int turn = kFit == kBack ? kKeptBlock - q.at[j] % kKeptBlock : kV;     // its first value of the second block
 #pragma unroll
     for (int k = 0; k < kV; ++k) {
       unsigned w;
       if constexpr (kV == 8) w = f.v[j][k / 4];
       else w = f.v[j];
-      x[j * kV + k] = (float)(signed char)(w >> (8 * (k & 3))) * s;
+      x[j * kV + k] = (float)(signed char)(w >> (8 * (k & 3))) * (kFit == kBack && k >= turn ? s2 : s);
     }
   }
 }
 
-template <typename T, int NV>
-__device__ __forceinline__ void vectors_at(float (&g)[NV * kVector<T>], const float* v, float none, int t, int lanes, int C) {
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ void vectors_at(float (&g)[NV * kVector<T>], const float* v, float none, const Columns<T, NV>& q, int C) {
   constexpr int kV = kVector<T>;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int k = 0; k < kV; ++k) {
-      const int c = (j * lanes + t) * kV + k;
-      g[j * kV + k] = v ? (c < C ? v[c] : 0.f) : none;
+    for (int k = 0; k < kV; k += 4) {
+      float w[4] = {none, none, none, none};
+      if (v) unpack(w, load_vector<float, kFit != kShort>(v, q.at[j] + k, C), 0.f);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) g[j * kV + k + u] = w[u];
     }
 }
-template <typename T, int NV, bool kFull>
-__device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], void* rows, long long ld, long long row, int t, int lanes, int C) {
+template <typename T, int NV, Fit kFit>
+__device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], T* p, unsigned row, const Columns<T, NV>& q, int C) {
   constexpr int kV = kVector<T>;
-  T* p = static_cast<T*>(rows) + row * ld;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     float w[kV];
 #pragma unroll
     for (int k = 0; k < kV; ++k) w[k] = y[j * kV + k];
-    store_vector<T, kFull>(p, (j * lanes + t) * kV, C, pack(w, T()));
+    if (kFit == kWhole || q.skip[j] < kV) {
+      if constexpr (kFit == kShort) store_vector<T, false>(p + row, q.at[j], C, pack(w, T()));
+      else *reinterpret_cast<u32x4_any*>(p + (row + (unsigned)q.at[j])) = pack(w, T());
+    }
   }
 }
 
-// Sums over a row's threads, in all of them.  kWide: the workgroup; `red` has room for two numbers a wave, and another row's
-// sums may use it only after one more barrier.
-template <bool kWide>
+// Threads of a row: kLanes of a wave (0: a number that is not known when the kernel is built), or the workgroup.
+constexpr int kGroup = 128;
+// Sums over a row's threads, in all of them.  kGroup: `red` has room for a number of each wave, and another row's sums may use it
+// only after one more barrier.
+template <int kLanes>
 __device__ __forceinline__ float row_sum(float x, int lanes, float* red) {
-  x = lane_sum(x, kWide ? 64 : lanes);
-  if constexpr (kWide) {
+  if constexpr (kLanes == kGroup) {
+    x = lane_sum<64>(x);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
     __syncthreads();
     x = 0.f;
     for (int w = 0; w < (int)blockDim.x >> 6; ++w) x += red[w];
+    return x;
+  } else {
+    return lane_sum<kLanes>(x, lanes);
   }
-  return x;
 }
-template <bool kWide>
+template <int kLanes>
 __device__ __forceinline__ void row_sums(float& x, float& y, int lanes, float* red) {
-  x = lane_sum(x, kWide ? 64 : lanes);
-  y = lane_sum(y, kWide ? 64 : lanes);
-  if constexpr (kWide) {
+  if constexpr (kLanes == kGroup) {
+    x = lane_sum<64>(x);
+    y = lane_sum<64>(y);
     if ((threadIdx.x & 63) == 0) {
       red[threadIdx.x >> 6] = x;
       red[kMostWaves + (threadIdx.x >> 6)] = y;
@@ -141,6 +175,9 @@ __device__ __forceinline__ void row_sums(float& x, float& y, int lanes, float* r
       x += red[w];
       y += red[kMostWaves + w];
     }
+  } else {
+    x = lane_sum<kLanes>(x, lanes);
+    y = lane_sum<kLanes>(y, lanes);
   }
 }
 
@@ -155,100 +192,132 @@ __device__ __forceinline__ float inverse_root(float x) {
   return x < 1.17549435e-38f ? 1.f / sqrtf(x) : __builtin_amdgcn_rsqf(x);
 }
 
-// Threads of a row: lanes of a wave, or the workgroup.
-template <bool kWide>
+// The thread's place: `lanes` threads a row, `seats` rows of a workgroup at a time.
+template <int kLanes>
 struct Seat {
-  int lanes, t;
-  long long row, step;
-  __device__ __forceinline__ explicit Seat(int l)
-      : lanes(kWide ? (int)blockDim.x : l), t(kWide ? (int)threadIdx.x : (int)threadIdx.x & (l - 1)) {
-    const int seats = kWide ? 1 : (int)blockDim.x / l;
-    row = (long long)blockIdx.x * seats + (kWide ? 0 : (int)threadIdx.x / l);
-    step = (long long)gridDim.x * seats;
+  int lanes, seats, seat, t;
+  __device__ __forceinline__ explicit Seat(int l) {
+    lanes = kLanes == kGroup ? (int)blockDim.x : (kLanes ? kLanes : l);
+    seats = kLanes == kGroup ? 1 : 256 / lanes;
+    seat = kLanes == kGroup ? 0 : (int)threadIdx.x / lanes;
+    t = kLanes == kGroup ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
   }
 };
+// Elements between the workgroup's first row and the seat's: below 2^32 / sizeof(float), rows are at most 2^22 elements apart.
+__device__ __forceinline__ unsigned rows_on(int seat, long long ld) { return (unsigned)seat * (unsigned)ld; }
 
-template <typename T, int NV, bool kWide, bool kFull>
-__global__ __launch_bounds__(kWide ? 1024 : 256) void row_norm_kernel(const RowNormArgs a, int row_lanes) {
-  constexpr int kV = kVector<T>, kN = NV * kV;
-  __shared__ float red[kWide ? 3 * kMostWaves : 1];
-  Seat<kWide> s(row_lanes);
-  float gamma[kN], beta[kN];
-  vectors_at<T, NV>(gamma, a.gamma, 1.f, s.t, s.lanes, a.C);
-  vectors_at<T, NV>(beta, a.beta, 0.f, s.t, s.lanes, a.C);
-  if (s.row >= a.rows) return;
+#ifndef ROWS
+#define ROWS 2
+#endif
+template <typename T, int NV, int kLanes, Fit kFit>
+__global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel(const RowNormArgs a, int row_lanes) {
+  constexpr int kV = kVector<T>, kN = NV * kV, kRows = kLanes == kGroup ? 1 : ROWS;
+  __shared__ float red[kLanes == kGroup ? 3 * kMostWaves : 1];
+  const Seat<kLanes> s(row_lanes);
+  const Columns<T, NV> q = columns_of<T, NV, kFit>(s.t, s.lanes, a.C);
   const float share = 1.f / (float)a.C;
-  Fetched<T, T, NV> f;
-  fetch<T, NV, kFull>(f, a.X, a.ldx, s.row, s.t, s.lanes, a.C);
-  for (;;) {
-    const long long next = s.row + s.step;
-    Fetched<T, T, NV> ahead;
-    fetch<T, NV, kFull>(ahead, a.X, a.ldx, next < a.rows ? next : s.row, s.t, s.lanes, a.C);
-    float x[kN];
-    values<T, NV>(x, f);
-    float sum = 0.f;
+  const unsigned x_on = rows_on(s.seat, a.ldx), y_on = rows_on(s.seat, a.ldy);
+  for (long long row0 = (long long)blockIdx.x * s.seats * kRows; row0 < a.rows; row0 += (long long)gridDim.x * s.seats * kRows) {
+    const int left = (int)min(a.rows - row0, (long long)s.seats * kRows);     // rows of the workgroup
+    const T* X = static_cast<const T*>(a.X) + row0 * a.ldx;
+    T* Y = static_cast<T*>(a.Y) + row0 * a.ldy;
+    // the requests of all its rows first; behind the last row the first one again
+    Fetched<T, T, NV> f[kRows];
 #pragma unroll
-    for (int k = 0; k < kN; ++k) sum += x[k];
-    const float m = rounded_product(row_sum<kWide>(sum, s.lanes, red), share);
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int k = 0; k < kV; ++k) {
-        float& d = x[j * kV + k];
-        d -= m;
-        if (!kFull && (j * s.lanes + s.t) * kV + k >= a.C) d = 0.f;
-        s1 += d;
-        s2 = fmaf(d, d, s2);
-      }
-    row_sums<kWide>(s1, s2, s.lanes, red + kMostWaves);
-    const float lacks = s1 * share, var = fmaf(-lacks, lacks, s2 * share);
-    const float r = inverse_root((var < 0.f ? 0.f : var) + a.eps);
-    const float shift = -lacks * r;
-#pragma unroll
-    for (int k = 0; k < kN; ++k) x[k] = fmaf(fmaf(x[k], r, shift), gamma[k], beta[k]);
-    activate<kN>(x, a.act);
-    put<T, NV, kFull>(x, a.Y, a.ldy, s.row, s.t, s.lanes, a.C);
-    if (a.mean && s.t == 0) {
-      a.mean[s.row] = m + lacks;
-      a.rstd[s.row] = r;
+    for (int u = 0; u < kRows; ++u) {
+      const bool there = u * s.seats + s.seat < left;
+      fetch<T, NV, kFit>(f[u], u * s.seats < left ? X + u * s.seats * a.ldx : X, there ? x_on : 0u, q, a.C);
     }
-    if (next >= a.rows) return;
-    s.row = next;
-    f = ahead;
+    float gamma[kN], beta[kN];
+    vectors_at<T, NV, kFit>(gamma, a.gamma, 1.f, q, a.C);
+    vectors_at<T, NV, kFit>(beta, a.beta, 0.f, q, a.C);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      if (u * s.seats + s.seat >= left) break;
+      float x[kN];
+      values<T, NV, kFit>(x, f[u], q);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < kV; ++k) sum += own<T, NV, kFit>(q, j, k, a.C) ? x[j * kV + k] : 0.f;
+      const float m = rounded_product(row_sum<kLanes>(sum, s.lanes, red), share);
+      float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < kV; ++k) {
+          x[j * kV + k] -= m;
+          const float d = own<T, NV, kFit>(q, j, k, a.C) ? x[j * kV + k] : 0.f;
+          s1 += d;
+          s2 = fmaf(d, d, s2);
+        }
+      row_sums<kLanes>(s1, s2, s.lanes, red + kMostWaves);
+      const float lacks = s1 * share, var = fmaf(-lacks, lacks, s2 * share);
+      const float r = inverse_root((var < 0.f ? 0.f : var) + a.eps);
+      const float shift = -lacks * r;
+#pragma unroll
+      for (int k = 0; k < kN; ++k) x[k] = fmaf(fmaf(x[k], r, shift), gamma[k], beta[k]);
+      activate<kN>(x, a.act);
+      put<T, NV, kFit>(x, Y + u * s.seats * a.ldy, y_on, q, a.C);
+      if (a.mean && s.t == 0) {
+        a.mean[row0 + u * s.seats + s.seat] = m + lacks;
+        a.rstd[row0 + u * s.seats + s.seat] = r;
+      }
+    }
   }
 }
 
-template <typename T, typename X, int NV, bool kWide, bool kFull>
-__global__ __launch_bounds__(kWide ? 1024 : 256) void row_norm_back_kernel(const RowNormArgs a, int row_lanes) {
+template <typename T, typename X, int NV, int kLanes, Fit kFit>
+__global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_kernel(const RowNormArgs a, int row_lanes) {
   constexpr int kV = kVector<T>, kN = NV * kV;
-  constexpr bool kKept = !std::is_same<T, X>::value;
+  constexpr bool kKept = !std::is_same<T, X>::value, kWide = kLanes == kGroup;
   __shared__ float red[kWide ? 4 * kMostWaves : 2 * 256 * kN];
-  Seat<kWide> s(row_lanes);
+  const Seat<kLanes> s(row_lanes);
+  const Columns<T, NV> q = columns_of<T, NV, kFit>(s.t, s.lanes, a.C);
   float gamma[kN], beta[kN], dg[kN], db[kN], dgs[kN], dbs[kN];
   if (kN == 8) {
-    vectors_at<T, NV>(gamma, a.gamma, 1.f, s.t, s.lanes, a.C);
-    vectors_at<T, NV>(beta, a.beta, 0.f, s.t, s.lanes, a.C);
+    vectors_at<T, NV, kFit>(gamma, a.gamma, 1.f, q, a.C);
+    vectors_at<T, NV, kFit>(beta, a.beta, 0.f, q, a.C);
   }
+  float* out = a.workspace + (size_t)blockIdx.x * 2 * a.C;
+  // the runs' sums: in registers, or, of sixteen values a thread, where the workgroup's go
+  auto join = [&](bool begin) {
 #pragma unroll
-  for (int k = 0; k < kN; ++k) dg[k] = db[k] = dgs[k] = dbs[k] = 0.f;
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int v = 0; v < kV; ++v) {
+        const int k = j * kV + v, c = q.at[j] + v;
+        if (kN == 8) {
+          dgs[k] = begin ? 0.f : dgs[k] + dg[k];
+          dbs[k] = begin ? 0.f : dbs[k] + db[k];
+        } else if (a.dgamma && own<T, NV, kFit>(q, j, v, a.C)) {
+          out[c] = begin ? 0.f : out[c] + dg[k];
+          out[a.C + c] = begin ? 0.f : out[a.C + c] + db[k];
+        }
+        dg[k] = db[k] = 0.f;
+      }
+  };
+  join(true);
   const float share = 1.f / (float)a.C;
   int run = 0, parity = 0;
-  for (; s.row < a.rows; s.row += s.step) {
+  const unsigned x_on = kKept ? rows_on(s.seat, a.kept.ld_code) : rows_on(s.seat, a.ldx), e_on = rows_on(s.seat, a.kept.ld_exponent),
+                 dy_on = rows_on(s.seat, a.lddy), res_on = rows_on(s.seat, a.lddres), dx_on = rows_on(s.seat, a.lddx);
+  for (long long row0 = (long long)blockIdx.x * s.seats; row0 + s.seat < a.rows; row0 += (long long)gridDim.x * s.seats) {
     Fetched<T, X, NV> f;
     Fetched<T, T, NV> fd, fr;
-    if constexpr (kKept) fetch<T, NV, kFull>(f, a.kept, s.row, s.t, s.lanes, a.C);
-    else fetch<T, NV, kFull>(f, a.X, a.ldx, s.row, s.t, s.lanes, a.C);
-    fetch<T, NV, kFull>(fd, a.dY, a.lddy, s.row, s.t, s.lanes, a.C);
-    if (a.dRes) fetch<T, NV, kFull>(fr, a.dRes, a.lddres, s.row, s.t, s.lanes, a.C);
-    const float m = a.mean[s.row], r = a.rstd[s.row];
+    if constexpr (kKept) fetch<T, NV, kFit>(f, a.kept.code + row0 * a.kept.ld_code, x_on, a.kept.exponent + row0 * a.kept.ld_exponent, e_on, q);
+    else fetch<T, NV, kFit>(f, static_cast<const T*>(a.X) + row0 * a.ldx, x_on, q, a.C);
+    fetch<T, NV, kFit>(fd, static_cast<const T*>(a.dY) + row0 * a.lddy, dy_on, q, a.C);
+    if (a.dRes) fetch<T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
+    const float m = a.mean[row0 + s.seat], r = a.rstd[row0 + s.seat];
     if (kN > 8) {                                        // registers for eight values a thread only
-      vectors_at<T, NV>(gamma, a.gamma, 1.f, s.t, s.lanes, a.C);
-      vectors_at<T, NV>(beta, a.beta, 0.f, s.t, s.lanes, a.C);
+      vectors_at<T, NV, kFit>(gamma, a.gamma, 1.f, q, a.C);
+      vectors_at<T, NV, kFit>(beta, a.beta, 0.f, q, a.C);
     }
     float xh[kN], dz[kN], z[kN];
-    values<T, NV>(xh, f);
-    values<T, NV>(dz, fd);
+    values<T, NV, kFit>(xh, f, q);
+    values<T, NV, kFit>(dz, fd, q);
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
       xh[k] = (xh[k] - m) * r;
@@ -261,14 +330,23 @@ __global__ __launch_bounds__(kWide ? 1024 : 256) void row_norm_back_kernel(const
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int k = 0; k < kN; ++k) {
-      dg[k] = fmaf(dz[k], xh[k], dg[k]);
-      db[k] += dz[k];
-      dz[k] *= gamma[k];
-      s1 += dz[k];
-      s2 = fmaf(dz[k], xh[k], s2);
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int v = 0; v < kV; ++v) {
+        const int k = j * kV + v;
+        dg[k] = fmaf(dz[k], xh[k], dg[k]);
+        db[k] += dz[k];
+        dz[k] *= gamma[k];
+        const float u = own<T, NV, kFit>(q, j, v, a.C) ? dz[k] : 0.f;
+        s1 += u;
+        s2 = fmaf(u, xh[k], s2);
+      }
+    // dX may be dres, and a vector that ends with the row is its neighbour's too, which may be another wave's: read before that writes
+    if (kWide && kFit == kBack && a.dRes) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) asm volatile("" ::"v"(fr.v[j]));
     }
-    row_sums<kWide>(s1, s2, s.lanes, red + 2 * kMostWaves * parity);
+    row_sums<kLanes>(s1, s2, s.lanes, red + 2 * kMostWaves * parity);
     parity ^= 1;
     s1 *= share;
     s2 *= share;
@@ -276,35 +354,26 @@ __global__ __launch_bounds__(kWide ? 1024 : 256) void row_norm_back_kernel(const
     for (int k = 0; k < kN; ++k) dz[k] = r * (dz[k] - s1 - xh[k] * s2);
     if (a.dRes) {
       float add[kN];
-      values<T, NV>(add, fr);
+      values<T, NV, kFit>(add, fr, q);
 #pragma unroll
       for (int k = 0; k < kN; ++k) dz[k] += add[k];
     }
-    put<T, NV, kFull>(dz, a.dX, a.lddx, s.row, s.t, s.lanes, a.C);
+    put<T, NV, kFit>(dz, static_cast<T*>(a.dX) + row0 * a.lddx, dx_on, q, a.C);
     if (++run == kRun) {
       run = 0;
-#pragma unroll
-      for (int k = 0; k < kN; ++k) {
-        dgs[k] += dg[k];
-        dbs[k] += db[k];
-        dg[k] = db[k] = 0.f;
-      }
+      join(false);
     }
   }
   if (!a.dgamma) return;
-  float* out = a.workspace + (size_t)blockIdx.x * 2 * a.C;
-#pragma unroll
-  for (int k = 0; k < kN; ++k) {
-    dgs[k] += dg[k];
-    dbs[k] += db[k];
-  }
+  join(false);
+  if constexpr (kN > 8) return;
   if constexpr (kWide) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int k = 0; k < kV; ++k) {
-        const int c = (j * s.lanes + s.t) * kV + k;
-        if (c < a.C) {
+        const int c = q.at[j] + k;
+        if (own<T, NV, kFit>(q, j, k, a.C)) {
           out[c] = dgs[j * kV + k];
           out[a.C + c] = dbs[j * kV + k];
         }
@@ -316,9 +385,10 @@ __global__ __launch_bounds__(kWide ? 1024 : 256) void row_norm_back_kernel(const
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int k = 0; k < kV; ++k) {
-        const int c = (j * s.lanes + s.t) * kV + k;
-        red[seat * width + c] = dgs[j * kV + k];
-        red[256 * kN + seat * width + c] = dbs[j * kV + k];
+        if (own<T, NV, kFit>(q, j, k, a.C)) {
+          red[seat * width + q.at[j] + k] = dgs[j * kV + k];
+          red[256 * kN + seat * width + q.at[j] + k] = dbs[j * kV + k];
+        }
       }
     __syncthreads();
     for (int c = threadIdx.x; c < a.C; c += 256) {
@@ -334,7 +404,7 @@ __global__ __launch_bounds__(kWide ? 1024 : 256) void row_norm_back_kernel(const
 }
 
 struct Plan {
-  bool wide, full;
+  bool wide;
   int nv16;                    // sixteen values a thread instead of eight
   int threads, lanes;          // of a workgroup; of a row
   long long blocks;
@@ -351,44 +421,62 @@ Plan plan(long long rows, int C, int n_cu, bool back) {
     p.lanes = 1;
     while (p.lanes < need) p.lanes *= 2;
   }
-  p.full = C == p.lanes * per;
-  const long long seats = p.wide ? 1 : 256 / p.lanes, need_blocks = (rows + seats - 1) / seats;
-  // what a CU holds at a time
-  const int threads_of_cu = back ? 1024 : 2048, each = threads_of_cu / p.threads;
-  const long long most = (long long)n_cu * (each < 1 ? 1 : each);
+  const long long seats = (p.wide ? 1 : 256 / p.lanes) * (back || p.wide ? 1 : ROWS), need_blocks = (rows + seats - 1) / seats;
+  // Forward: a row a seat, so that the rows come in the order in which the workgroups are handed out (a launch has less than
+  // 2^32 threads).  Backward: what a CU holds at a time, each workgroup sums gradients of gamma and beta.
+  const long long most = back ? (long long)n_cu * (1024 / p.threads < 1 ? 1 : 1024 / p.threads) : (1LL << 31) / p.threads;
   p.blocks = need_blocks < most ? need_blocks : most;
   return p;
 }
 
+// f gets kLanes and kFit as types: the lanes of 65 to 512 channels are known when the kernel is built.
+template <int kI>
+using Number = std::integral_constant<int, kI>;
+template <typename T, typename F>
+void each_fit(const Plan& p, int C, int held, F f) {
+  const bool whole = C == p.lanes * held;
+  auto fit = [&](auto lanes) {
+    if (whole) f(lanes, std::integral_constant<Fit, kWhole>());
+    else f(lanes, std::integral_constant<Fit, kBack>());
+  };
+  if (p.wide) fit(Number<kGroup>());
+  else if (p.lanes == 64) fit(Number<64>());
+  else if (p.lanes == 32) fit(Number<32>());
+  else if (p.lanes == 16) fit(Number<16>());
+  else if (C >= kVector<T>) fit(Number<0>());
+  else f(Number<0>(), std::integral_constant<Fit, kShort>());
+}
 template <typename T>
 void forward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
   constexpr int NV = 8 / kVector<T>;
   const dim3 g((unsigned)p.blocks), b((unsigned)p.threads);
-  if (p.nv16) {
-    if (p.full) hipLaunchKernelGGL((row_norm_kernel<T, 2 * NV, true, true>), g, b, 0, s, a, p.lanes);
-    else hipLaunchKernelGGL((row_norm_kernel<T, 2 * NV, true, false>), g, b, 0, s, a, p.lanes);
-  } else if (p.wide) {
-    if (p.full) hipLaunchKernelGGL((row_norm_kernel<T, NV, true, true>), g, b, 0, s, a, p.lanes);
-    else hipLaunchKernelGGL((row_norm_kernel<T, NV, true, false>), g, b, 0, s, a, p.lanes);
-  } else {
-    if (p.full) hipLaunchKernelGGL((row_norm_kernel<T, NV, false, true>), g, b, 0, s, a, p.lanes);
-    else hipLaunchKernelGGL((row_norm_kernel<T, NV, false, false>), g, b, 0, s, a, p.lanes);
-  }
+  each_fit<T>(p, a.C, p.nv16 ? 16 : 8, [&](auto lanes, auto fit) {
+    constexpr int kLanes = decltype(lanes)::value;
+    constexpr Fit kFit = decltype(fit)::value;
+    if constexpr (kLanes == kGroup) {
+      if (p.nv16) {
+        hipLaunchKernelGGL((row_norm_kernel<T, 2 * NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((row_norm_kernel<T, NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
+  });
 }
 template <typename T, typename X>
 void backward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
   constexpr int NV = 8 / kVector<T>;
   const dim3 g((unsigned)p.blocks), b((unsigned)p.threads);
-  if (p.nv16) {
-    if (p.full) hipLaunchKernelGGL((row_norm_back_kernel<T, X, 2 * NV, true, true>), g, b, 0, s, a, p.lanes);
-    else hipLaunchKernelGGL((row_norm_back_kernel<T, X, 2 * NV, true, false>), g, b, 0, s, a, p.lanes);
-  } else if (p.wide) {
-    if (p.full) hipLaunchKernelGGL((row_norm_back_kernel<T, X, NV, true, true>), g, b, 0, s, a, p.lanes);
-    else hipLaunchKernelGGL((row_norm_back_kernel<T, X, NV, true, false>), g, b, 0, s, a, p.lanes);
-  } else {
-    if (p.full) hipLaunchKernelGGL((row_norm_back_kernel<T, X, NV, false, true>), g, b, 0, s, a, p.lanes);
-    else hipLaunchKernelGGL((row_norm_back_kernel<T, X, NV, false, false>), g, b, 0, s, a, p.lanes);
-  }
+  each_fit<T>(p, a.C, p.nv16 ? 16 : 8, [&](auto lanes, auto fit) {
+    constexpr int kLanes = decltype(lanes)::value;
+    constexpr Fit kFit = decltype(fit)::value;
+    if constexpr (kLanes == kGroup) {
+      if (p.nv16) {
+        hipLaunchKernelGGL((row_norm_back_kernel<T, X, 2 * NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((row_norm_back_kernel<T, X, NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
+  });
 }
 
 }  // namespace

@@ -73,17 +73,19 @@ template <int kControl>
 __device__ __forceinline__ float dpp(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kControl, 0xF, 0xF, true));
 }
-// The sum over `lanes` neighbours (a power of two up to 64, the same for the wave), in all of them.
-__device__ __forceinline__ float lane_sum(float x, int lanes) {
-  if (lanes > 1) x += dpp<0xB1>(x);            // quad_perm 1 0 3 2
-  if (lanes > 2) x += dpp<0x4E>(x);            // quad_perm 2 3 0 1
-  if (lanes > 4) x += dpp<0x141>(x);           // row_half_mirror
-  if (lanes > 8) x += dpp<0x140>(x);           // row_mirror
-  if (lanes > 16) {
+// The sum over `lanes` neighbours (a power of two up to 64, the same for the wave), in all of them.  kLanes: their number where it
+// is known when the kernel is built, else 0.
+template <int kLanes = 0>
+__device__ __forceinline__ float lane_sum(float x, int lanes = kLanes) {
+  if (kLanes ? kLanes > 1 : lanes > 1) x += dpp<0xB1>(x);            // quad_perm 1 0 3 2
+  if (kLanes ? kLanes > 2 : lanes > 2) x += dpp<0x4E>(x);            // quad_perm 2 3 0 1
+  if (kLanes ? kLanes > 4 : lanes > 4) x += dpp<0x141>(x);           // row_half_mirror
+  if (kLanes ? kLanes > 8 : lanes > 8) x += dpp<0x140>(x);           // row_mirror
+  if (kLanes ? kLanes > 16 : lanes > 16) {
     const u32x2 h = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     x = __uint_as_float(h[0]) + __uint_as_float(h[1]);
   }
-  if (lanes > 32) {
+  if (kLanes ? kLanes > 32 : lanes > 32) {
     const u32x2 h = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     x = __uint_as_float(h[0]) + __uint_as_float(h[1]);
   }

@@ -594,8 +594,9 @@ def test_adamw_leaves_tensors_without_a_gradient(ev, states):
 
 
 @pytest.mark.parametrize("states", ["f32", "8bit"])
+@pytest.mark.parametrize("eps", [1e-8, 1.1e-10, 0.9e-10, 1e-30])
 @pytest.mark.parametrize("values", ["zeros", "wide", "edges", "bad"])
-def test_adamw_of_unusual_gradients(ev, states, values):
+def test_adamw_of_unusual_gradients(ev, states, values, eps):
     n = 128 * 6
     r = np.random.default_rng(3)
     with np.errstate(over="ignore"):
@@ -604,7 +605,7 @@ def test_adamw_of_unusual_gradients(ev, states, values):
              "edges": np.concatenate([np.full(128, 1e-22), np.full(128, 1.8e19), [1e19] + [1e-15] * 127, np.geomspace(1e-20, 1, 128), [-1.875] + [1.0] * 127, [1.8750001] + [2.0 ** -k for k in range(127)]]),
              "bad": np.concatenate([[np.nan] + [1.0] * 127, [np.inf] + [1.0] * 127, [-np.inf] + [2.0] * 127, np.full(128, 3e38), np.full(128, 1e20), np.ones(128)])}[values].astype(f32)
     params = tensors_of([n], "f32")
-    args = dict(lr=1e-3, betas=(0.9, 0.999), eps=1e-8)
+    args = dict(lr=1e-3, betas=(0.9, 0.999), eps=eps)
     o, plain = ev.adamw(params, **args, weight_decay=0.0, states=states), Plain(params, [0.0], states, 0, **args)
     for k in range(3):
         grads = [torch.from_numpy(g * f32(0.5) ** k).cuda()]
