@@ -4,7 +4,7 @@
 //   w = w - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + decay w)
 //
 // (the corrections as factors: k2 sqrt(v) and c1 m / (k2 sqrt(v) + eps), of which nothing is too small for fp32 before m and v are).
-// Bound by memory.  The tensors are cut into chunks of 4096 elements, eight a thread, a workgroup each, so that memory is gone
+// Bound by memory.  The tensors are cut into chunks of 2048 elements, eight a thread, a workgroup each, so that memory is gone
 // through in the order in which workgroups are handed out; a chunk's tensor is found in a table that travels with the launch.  The
 // step count t lies in device memory, so that a captured step goes on counting: the last workgroup counts it up, or, of more than
 // can be counted one by one, a launch of its own.
@@ -26,7 +26,7 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kPer = 8, kThreads = 512, kChunk = kPer * kThreads;
+constexpr int kPer = 8, kThreads = 256, kChunk = kPer * kThreads;
 constexpr u64 kDraw = 0xD1342543DE82EF95ULL;    // from one draw to the next
 constexpr unsigned kCounted = 2048;            // workgroups that are counted one by one
 constexpr int kExponentNan = 255;              // of a block of moments that holds a number that is not finite
@@ -116,33 +116,46 @@ __device__ __forceinline__ void store8(const float (&x)[kPer], float* p, int lef
   }
 }
 
-// w from the bf16 number and the low half.  Zero has nothing below it to borrow from (its low half is less than 0x8000 unless the
-// caller wrote the parameter anew).
-__device__ __forceinline__ float whole(unsigned p, unsigned low) {
-  const unsigned borrow = low >= 0x8000u && (p & 0x7FFFu) != 0 ? 1u : 0u;
-  return __uint_as_float(((p - borrow) << 16) | low);
+// w of a word of two halves, the bf16 number above, the low half below: where that is 0x8000 or more the number is one step too
+// far.  Zero has nothing below it to give (its low half is less than 0x8000 unless the caller wrote the parameter anew).
+__device__ __forceinline__ float whole(unsigned word) {
+  return __uint_as_float(word - min(word << 1 & 0x10000u, word & 0x7FFF0000u));
+}
+__device__ __forceinline__ void wholes(float& w0, float& w1, unsigned p, unsigned low) {     // of two places
+  w0 = whole(__builtin_amdgcn_perm(p, low, 0x05040100u));
+  w1 = whole(__builtin_amdgcn_perm(p, low, 0x07060302u));
 }
 template <bool kAll>
 __device__ __forceinline__ void store_whole(const float (&w)[kPer], u16* to, u16* low, int left) {
-  unsigned hi[kPer], lo[kPer];
+  unsigned hi[kPer], lo[kPer];       // a number's upper half of one, lower half of the other
+  float sum = 0.f;                   // not a number if one of them is none
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const unsigned b = __float_as_uint(w[k]);
-    const bool nan = w[k] != w[k];
-    hi[k] = nan ? 0x7FC0u : (b + 0x8000u) >> 16;
-    lo[k] = nan || (!kAll && k >= left) ? 0u : b;
+    sum += w[k];
+    hi[k] = __float_as_uint(w[k]) + 0x8000u;
+    lo[k] = !kAll && k >= left ? 0u : __float_as_uint(w[k]);
   }
-  const u32x4 h = {hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
+  if (__ballot(sum != sum) != 0) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      if (w[k] != w[k]) {
+        hi[k] = 0x7FC00000u;
+        lo[k] = 0u;
+      }
+  }
+  u32x4 h;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) h[k] = __builtin_amdgcn_perm(hi[2 * k + 1], hi[2 * k], 0x07060302u);
   if (kAll || left >= kPer) {
     *reinterpret_cast<u32x4_any*>(to) = h;
   } else {
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
-      if (k < left) to[k] = (u16)hi[k];
+      if (k < left) to[k] = (u16)(hi[k] >> 16);
   }
   u32x4 l;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) l[k] = __builtin_amdgcn_perm(lo[2 * k + 1], lo[2 * k], 0x05040100u);   // their lower halves
+  for (int k = 0; k < 4; ++k) l[k] = __builtin_amdgcn_perm(lo[2 * k + 1], lo[2 * k], 0x05040100u);
   *reinterpret_cast<u32x4*>(low) = l;
 }
 
@@ -153,13 +166,15 @@ constexpr int kUnit = kM ? 15 : 31;
 // Four codes.
 template <bool kM>
 __device__ __forceinline__ void decode(float (&x)[4], unsigned code, int exponent) {
-  const float nan = exponent == kExponentNan ? __uint_as_float(0x7FC00000u) : 0.f;     // of the whole block, or nothing
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const unsigned top = code << (24 - 8 * k);           // the code in the upper byte
-    const unsigned bits = kM ? (top >> 4 & 0x07F00000u) | (top & 0x80000000u) : top >> 4 & 0x0FF00000u;
-    x[k] = __builtin_amdgcn_ldexpf(__uint_as_float(bits), exponent - kUnit<kM>) + nan;
+    const unsigned c = code >> (8 * k) & 0xFFu;
+    // m: the sign stays at the top while the rest goes to the place of an exponent and three bits
+    const unsigned bits = kM ? (unsigned)((int)(c << 24) >> 4) & 0x87F00000u : c << 20;
+    x[k] = __builtin_amdgcn_ldexpf(__uint_as_float(bits), exponent - kUnit<kM>);
   }
+  // a branch for the wave: it is all but never taken
+  if (__ballot(exponent == kExponentNan) != 0 && exponent == kExponentNan) x[0] = x[1] = x[2] = x[3] = __uint_as_float(0x7FC00000u);
 }
 __device__ __forceinline__ unsigned max_dpp16(unsigned x) {
   x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));
@@ -167,29 +182,40 @@ __device__ __forceinline__ unsigned max_dpp16(unsigned x) {
   x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));
   return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true));
 }
+// 1 if x, which is not negative, is not zero; as one instruction (the compiler makes a comparison and a choice of it).
+__device__ __forceinline__ unsigned not_zero(float x) {
+  unsigned r;
+  asm("v_min_u32 %0, 1, %1" : "=v"(r) : "v"(x));
+  return r;
+}
 // r: a draw for two places, 16 bits for m and for v of the first and of the second.  Returns the exponent of the 16 lanes' block.
 template <bool kM>
 __device__ __forceinline__ int encode(u32x2& code, const float (&x)[kPer], const u64 (&r)[kPer / 2]) {
-  unsigned top = 0;            // the bits of |x| order as |x| does, what is not finite above all
+  unsigned top = 0;            // the bits of |x| order as |x| does, what is not finite above all; v has no sign
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+  for (int k = 0; k < kPer; ++k) top = max(top, kM ? __float_as_uint(x[k]) & 0x7FFFFFFFu : __float_as_uint(x[k]));
   top = max_dpp16(top);
-  // the smallest exponent whose largest value, 1.875 2^x, reaches the top
+  // the smallest exponent whose largest value, 1.875 2^x, reaches the top; beyond the largest of all, that
   int e = (int)(top >> 23) + ((top & 0x7FFFFFu) > 0x700000u ? 1 : 0);
   e = min(max(e, kM ? 1 : 11), 254);
   code = u32x2{0, 0};
   if (top >= 0x7F800000u) return kExponentNan;
+  constexpr float kLargest = 0x1.Ep127f;
+  float y[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) y[k] = fabsf(x[k]);
+  if (top > __float_as_uint(kLargest)) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] = fminf(y[k], kLargest);
+  }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const unsigned half = (unsigned)(r[k / 2] >> (32 * (k & 1)));
     // 2^-17 of a step above the 16 bits, which leave 20 to be cut off
-    const unsigned chance = kM ? (half & 0xFFFFu) << 4 | 8u : half >> 12 & 0xFFFF0u | 8u;
-    unsigned c = (__float_as_uint(__builtin_amdgcn_ldexpf(fabsf(x[k]), kUnit<kM> - e)) + chance) >> 20;
-    if constexpr (kM) {
-      c = min(c, 127u) | (__float_as_uint(x[k]) >> 24 & 0x80u);
-    } else {
-      c = min(max(c, min(__float_as_uint(x[k]), 1u)), 255u);     // v is not negative: 1 at least if it is not zero
-    }
+    const unsigned chance = kM ? (half & 0xFFFFu) << 4 : (half >> 16) << 4;
+    unsigned c = (__float_as_uint(__builtin_amdgcn_ldexpf(y[k], kUnit<kM> - e)) + chance + 8u) >> 20;
+    if constexpr (kM) c |= __float_as_uint(x[k]) >> 24 & 0x80u;
+    else c = max(c, not_zero(x[k]));
     code[k / 4] |= c << (8 * (k & 3));
   }
   return e;
@@ -246,14 +272,20 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const
   }
   if (first) __syncthreads();
   if (!there) return;
+  u64 r[kPer / 2];
+  if constexpr (kEight) {      // the draws, while the requests are under way: kept in front of what waits for them
+    u64 place = step.key + (u64)((c.at + i) / 2) * kDraw;
+#pragma unroll
+    for (int k = 0; k < kPer / 2; ++k, place += kDraw) {
+      r[k] = mix(place);
+      asm volatile("" : "+v"(r[k]));
+    }
+  }
   float g[kPer], w[kPer], m[kPer], v[kPer];
   open(g, rg, c.g16);
   if (c.p16) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      w[2 * k] = whole(rw.v[0][k] & 0xFFFFu, rl[k] & 0xFFFFu);
-      w[2 * k + 1] = whole(rw.v[0][k] >> 16, rl[k] >> 16);
-    }
+    for (int k = 0; k < 4; ++k) wholes(w[2 * k], w[2 * k + 1], rw.v[0][k], rl[k]);
   } else {
     open(w, rw, false);
   }
@@ -273,11 +305,14 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const
     open(m, rm, false);
     open(v, rv, false);
   }
+  if (a.grad_scale) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) g[k] *= step.scale;
+  }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const float gk = g[k] * step.scale;
-    m[k] = m[k] * a.b1 + gk * a.o1;
-    v[k] = v[k] * a.b2 + (gk * gk) * a.o2;
+    m[k] = m[k] * a.b1 + g[k] * a.o1;
+    v[k] = v[k] * a.b2 + (g[k] * g[k]) * a.o2;
   }
   float by[kPer];              // m / (sqrt(v) k2 + eps)
   if (step.fast) {
@@ -295,9 +330,6 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const
       for (int k = 0; k < kPer; ++k)
         if (k >= left) m[k] = v[k] = 0.f;
     }
-    u64 r[kPer / 2], place = step.key + (u64)((c.at + i) / 2) * kDraw;
-#pragma unroll
-    for (int k = 0; k < kPer / 2; ++k, place += kDraw) r[k] = mix(place);
     em = encode<true>(mc, m, r);
     ev = encode<false>(vc, v, r);
     *reinterpret_cast<u32x2*>(m8 + i) = mc;
@@ -318,7 +350,7 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const
 }
 
 template <bool kEight>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwArgs a) {
+__global__ __launch_bounds__(kThreads, kEight ? 5 : 8) void adamw_kernel(const AdamwArgs a) {
   __shared__ Step step;
   const int before = a.steps[0], t = before < 2147483647 ? before + 1 : before;
   if (threadIdx.x < 64) {
@@ -379,10 +411,7 @@ __global__ __launch_bounds__(kThreads) void values_kernel(const AdamwArgs a) {
             if (k < left) h[k / 2] |= (unsigned)from[k] << (16 * (k & 1));
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          w[2 * k] = whole(h[k] & 0xFFFFu, l[k] & 0xFFFFu);
-          w[2 * k + 1] = whole(h[k] >> 16, l[k] >> 16);
-        }
+        for (int k = 0; k < 2; ++k) wholes(w[2 * k], w[2 * k + 1], h[k], l[k]);
       } else {
         const float* from = reinterpret_cast<const float*>(c.p) + i;
         if (left == 4) {

@@ -1968,11 +1968,11 @@ dc_status embed_rows_check(dc_ctx* ctx, const dc_embed_rows_args* a, bool backwa
     st = lies_apart(ctx, rows_place("Y", a->Y, a->rows, a->channels, a->ldy, es), {rows_place("table", a->table, a->kinds, a->channels, a->ld_table, es), id});
   } else {
     const size_t need = dc_embed_rows_bytes(ctx, a->rows, a->kinds, a->channels);
-    if (!a->workspace || a->workspace_bytes < need) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_embed_rows_bytes");
-    if (!at(a->workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+    if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return fail(ctx, DC_ERR_CAPACITY, "workspace smaller than dc_embed_rows_bytes");
+    if (need > 0 && !at(a->workspace, 16)) return fail(ctx, DC_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
     const Place dY = rows_place("dY", a->dY, a->rows, a->channels, a->lddy, es), dtable = rows_place("dtable", a->dtable, a->kinds, a->channels, a->ld_dtable, es);
     st = lies_apart(ctx, dtable, {dY, id});
-    if (st == DC_OK) st = lies_apart(ctx, vector_place("the workspace", a->workspace, (int64_t)need), {dY, dtable, id});
+    if (st == DC_OK) st = lies_apart(ctx, vector_place("the workspace", need > 0 ? a->workspace : nullptr, (int64_t)need), {dY, dtable, id});
   }
   if (st != DC_OK) return st;
   *g = EmbedArgs{};
@@ -1992,7 +1992,6 @@ dc_status embed_rows_check(dc_ctx* ctx, const dc_embed_rows_args* a, bool backwa
   g->lddt = a->ld_dtable;
   g->workspace = static_cast<char*>(a->workspace);
   g->status = ctx->status;
-  g->n_cu = ctx->n_cu;
   return DC_OK;
 }
 
@@ -2143,7 +2142,7 @@ dc_status dc_row_norm_backward(dc_ctx* ctx, const dc_row_norm_args* args, void* 
 
 size_t dc_embed_rows_bytes(const dc_ctx* ctx, int64_t rows, int32_t kinds, int32_t channels) {
   if (!ctx || rows < 0 || rows > kRowsMost || kinds < 1 || channels < 1 || channels > 65536) return 0;
-  return embed_rows_bytes(rows, kinds, channels, ctx->n_cu);
+  return embed_rows_bytes(rows, kinds, channels);
 }
 
 dc_status dc_embed_rows(dc_ctx* ctx, const dc_embed_rows_args* args, void* stream) {

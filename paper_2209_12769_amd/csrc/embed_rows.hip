@@ -2,13 +2,13 @@
 // (gfx950).
 //
 // Forward: bound by the rows it writes; the table's used rows stay in the caches.
-// Gradient: the row numbers are sorted by kind (stable radix sort, up to nine bits a pass), so that a kind's rows become
-// neighbours, and the sorted list is cut into chunks of equal length.  A chunk sums its rows kind by kind in the list's order.  A
-// kind that lies inside one chunk is written at once; what it has of kinds that reach beyond it, the first and the last of
-// its list at most, are entries of a second, shorter list, which is treated alike until it is short enough for one workgroup a
-// kind.  No atomics: the same call gives the same bits.  Sums: 64 rows in fp32, these in fp32 again (up to 256 rows a chunk), the
-// chunks' in 64 bits.  Kinds without rows are found by a search in the sorted list and cleared by further workgroups of the same
-// launch.
+// Gradient: the row numbers are sorted by kind (stable radix sort, up to nine bits a pass; a short list by one workgroup), so that
+// a kind's rows become neighbours, and the sorted list is cut into chunks of equal length.  A chunk sums its rows kind by kind in
+// the list's order.  A kind that lies inside one chunk is written at once; what a chunk has of kinds that reach beyond it, the
+// first and the last of its list at most, are entries of a second, shorter list, which is treated alike until it is short
+// enough for one workgroup a kind.  No atomics: the same call gives the same bits.  Sums: up to 64 rows in fp32, the chunks' in
+// 64 bits, rounded to fp32 from list to list.  Kinds without rows are found by a search in the sorted list and cleared by further
+// workgroups of the first sums' launch.
 #include "row_vectors.h"
 
 namespace dc {
@@ -24,10 +24,7 @@ __device__ __forceinline__ int kind_of(const EmbedArgs& a, long long row) {
   return -1;
 }
 
-#ifndef ATONCE
-#define ATONCE 8
-#endif
-constexpr int kAtOnce = ATONCE;     // rows of a thread, its columns are the same in all of them
+constexpr int kAtOnce = 8;     // rows of a thread, its columns are the same in all of them
 // A workgroup takes `across` neighbouring rows of `used` vectors at a time, kAtOnce times; slabs of rows too wide for one are
 // blockIdx.y.
 template <typename T>
@@ -120,7 +117,7 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(const EmbedArgs a, 
   for (int i = threadIdx.x; i < bins; i += kSortThreads) count[(size_t)i * tiles + tile] = bin[i];
 }
 
-// Exclusive sums over the workgroup's 256 threads; returns the sum of all in `all`.
+// Exclusive sums over the workgroup's first 256 threads, the sum of all in `all`; every thread calls it.
 __device__ __forceinline__ int scan256(int x, int* part, int& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int v = x;
@@ -129,7 +126,7 @@ __device__ __forceinline__ int scan256(int x, int* part, int& all) {
     if (lane >= o) v += w;
   }
   __syncthreads();
-  if (lane == 63) part[wave] = v;
+  if (lane == 63 && wave < 4) part[wave] = v;
   __syncthreads();
   int before = 0;
   all = 0;
@@ -212,6 +209,61 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(const EmbedArgs a
   }
 }
 
+// The whole sort of a list of up to kSmall pairs by one workgroup, in LDS: the same passes, of up to kSmallBits bits.
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kSmallPer = 4, kSmall = kSmallThreads * kSmallPer, kSmallBits = 8, kSmallBins = 1 << kSmallBits;
+__global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(const EmbedArgs a, int bits, Pair* out) {
+  __shared__ Pair list[kSmall];
+  __shared__ int next[kSmallWaves][kSmallBins];
+  __shared__ int part[4];
+  const int n = (int)a.rows, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, base = wave * 64 * kSmallPer + lane;
+  Pair p[kSmallPer];
+#pragma unroll
+  for (int k = 0; k < kSmallPer; ++k) p[k] = base + k * 64 < n ? pair_at(a, nullptr, base + k * 64) : Pair{0, -1};
+  for (int shift = 0; shift < bits; shift += kSmallBits) {
+    for (int i = threadIdx.x; i < kSmallWaves * kSmallBins; i += kSmallThreads) next[i / kSmallBins][i % kSmallBins] = 0;
+    __syncthreads();
+    u64 peers[kSmallPer];
+#pragma unroll
+    for (int k = 0; k < kSmallPer; ++k) {
+      const int digit = p[k].kind >> shift & (kSmallBins - 1);
+      const bool in_range = base + k * 64 < n;
+      peers[k] = same_digit(digit, kSmallBits, __ballot(in_range));
+      if (in_range && (peers[k] & ((1ULL << lane) - 1)) == 0) next[wave][digit] += __popcll(peers[k]);
+      in_order();
+    }
+    __syncthreads();
+    // the digits in front, then the waves in front: a thread a digit (the others take part in the barriers)
+    int sum = 0, all;
+    if (threadIdx.x < kSmallBins)
+      for (int w = 0; w < kSmallWaves; ++w) sum += next[w][threadIdx.x];
+    int at = scan256(sum, part, all);
+    if (threadIdx.x < kSmallBins)
+      for (int w = 0; w < kSmallWaves; ++w) {
+        const int c = next[w][threadIdx.x];
+        next[w][threadIdx.x] = at;
+        at += c;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSmallPer; ++k) {
+      const int digit = p[k].kind >> shift & (kSmallBins - 1);
+      const bool in_range = base + k * 64 < n;
+      const int rank = __popcll(peers[k] & ((1ULL << lane) - 1)), place = next[wave][digit];
+      in_order();
+      if (in_range) list[place + rank] = p[k];
+      if (in_range && rank == 0) next[wave][digit] = place + __popcll(peers[k]);
+      in_order();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSmallPer; ++k)
+      if (base + k * 64 < n) p[k] = list[base + k * 64];
+  }
+#pragma unroll
+  for (int k = 0; k < kSmallPer; ++k)
+    if (base + k * 64 < n) out[base + k * 64] = p[k];
+}
+
 // ---- sums ----
 struct Sums {
   EmbedArgs a;
@@ -220,7 +272,7 @@ struct Sums {
   int chunk;                   // entries of a chunk
   int nchunk;
   int lanes, nslab;            // places for a slab's vectors, slabs of a row
-  int used;                    // vectors of a slab
+  int used;                    // places that are taken
   const float* in;             // levels above the first: [n][C]
   const int* in_kind;          // [n]: the kind, or ~kind of an entry without a sum
   float* out;                  // [2 nchunk][C]
@@ -265,8 +317,6 @@ __device__ __forceinline__ void write_kind4(const EmbedArgs& a, int kind, int c,
   }
 }
 
-constexpr int kRun = 64;       // rows summed in fp32 before they join the others'
-
 // What a chunk has of one kind is done with: kind and columns written at once, or an entry of the next list.
 struct Close {
   int chunk;
@@ -280,27 +330,27 @@ __device__ __forceinline__ void close_kind(const Sums& s, const Close& k, int ki
     if (up) write_entry<kV>(s.out + entry * s.a.C, c, s.a.C, x);
     else write(kind, x);
   }
-  if (c == 0) {                // the thread of the row's first columns says what the entries are
+  if (c == 0 && s.out_kind) {  // the thread of the row's first columns says what the entries are, if there is another list
     if (first) s.out_kind[2 * (size_t)k.chunk] = up && any ? kind : ~kind;
     if (last && first) s.out_kind[2 * (size_t)k.chunk + 1] = ~kind;
     if (last && !first) s.out_kind[2 * (size_t)k.chunk + 1] = up && any ? kind : ~kind;
   }
 }
-// The columns of a seat's thread; below zero if it has none.  The last vector ends with the row, so that two threads may have
-// the same columns and write the same.
+// A thread's first column of kV from place `at` of a row; below zero if it has none.  The last vector ends with the row, so that
+// two threads may have the same columns and write the same.
 template <int kV>
-__device__ __forceinline__ int columns_of(const Sums& s, int slab, int t) {
-  const int c = (slab * s.used + t) * kV;
-  return t < s.used && c < s.a.C ? max(min(c, s.a.C - kV), 0) : -1;
+__device__ __forceinline__ int column_of(int at, int C) {
+  const int c = at * kV;
+  return c < C ? max(min(c, C - kV), 0) : -1;
 }
 
-// Clears the kinds that have no row: 64 kinds a wave.
+// Clears the kinds that have no row: 64 kinds a workgroup, its waves take them in turn.
+constexpr int kClear = 64;
 template <typename T>
 __device__ void clear_unused(const Sums& s, int block) {
   const EmbedArgs& a = s.a;
-  const int lane = threadIdx.x & 63;
-  const long long waves = (long long)s.fill_blocks * 4;
-  for (long long k0 = ((long long)block * 4 + (threadIdx.x >> 6)) * 64; k0 < a.kinds; k0 += waves * 64) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (long long k0 = (long long)block * kClear; k0 < a.kinds; k0 += (long long)s.fill_blocks * kClear) {
     const int kind = (int)min(k0 + lane, (long long)a.kinds - 1);
     int lo = 0, hi = s.n;      // the first pair of that kind or a larger one
     while (lo < hi) {
@@ -309,17 +359,19 @@ __device__ void clear_unused(const Sums& s, int block) {
       else hi = mid;
     }
     const bool none = k0 + lane < a.kinds && (lo >= s.n || s.sorted[lo].kind != kind);
-    for (u64 left = __ballot(none); left; left &= left - 1) {
+    int turn = 0;
+    for (u64 left = __ballot(none); left; left &= left - 1, ++turn) {
+      if ((turn & 3) != wave) continue;
       T* row = static_cast<T*>(a.dtable) + (k0 + __builtin_ctzll(left)) * a.lddt;
-      for (int c = lane * kVector<T>; c < a.C; c += 64 * kVector<T>) store_vector<T, false>(row, c, a.C, u32x4{0, 0, 0, 0});
+      for (int at = lane; at * kVector<T> < a.C; at += 64) store_vector<T, false>(row, column_of<kVector<T>>(at, a.C), a.C, u32x4{0, 0, 0, 0});
     }
   }
 }
 
-// First level: chunks of the sorted rows.
-template <typename T>
+// First level: chunks of the sorted rows, of up to 64 of them: one sum in fp32 a kind.  A thread has NV vectors of a row, `lanes` apart.
+template <typename T, int NV>
 __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
-  constexpr int kV = kVector<T>, kAhead = 8;
+  constexpr int kV = kVector<T>, kAhead = NV > 2 ? 4 : 8;
   const EmbedArgs& a = s.a;
   if ((int)blockIdx.x < s.fill_blocks) return clear_unused<T>(s, blockIdx.x);
   const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
@@ -327,59 +379,63 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
   if (item >= (long long)s.nchunk * s.nslab) return;
   Close close;
   close.chunk = (int)(item / s.nslab);
-  const int c = columns_of<kV>(s, (int)(item - (long long)close.chunk * s.nslab), t);
-  if (c < 0) return;
+  const int slab = (int)(item - (long long)close.chunk * s.nslab);
+  int c[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) c[j] = column_of<kV>(slab * NV * s.lanes + j * s.lanes + t, a.C);
+  if (c[0] < 0) return;
   const long long p0l = (long long)close.chunk * s.chunk;
   const int p0 = (int)p0l, p1 = (int)min(p0l + s.chunk, (long long)s.n), len = p1 - p0;
   const T* dY = static_cast<const T*>(a.dY);
   int kind = s.sorted[p0].kind;
   close.from_before = p0 > 0 && s.sorted[p0 - 1].kind == kind;
   const int past = p1 < s.n ? s.sorted[p1].kind : -1;
-  auto write = [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c, x); };
-  float sum[kV], run[kV];
+  float sum[NV][kV];
+  auto clear = [&]() {
 #pragma unroll
-  for (int k = 0; k < kV; ++k) sum[k] = run[k] = 0.f;
-  int count = 0;
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < kV; ++k) sum[j][k] = 0.f;
+  };
+  auto end_kind = [&](bool any, bool first, bool last) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (c[j] >= 0)
+        close_kind(s, close, kind, c[j], sum[j], any, first, last, [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c[j], x); });
+  };
+  clear();
   bool first = true;
   for (int q = 0; q < len; q += kAhead) {
     Pair e[kAhead];
-    u32x4 v[kAhead];
+    u32x4 v[kAhead][NV];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) e[u] = s.sorted[p0 + min(q + u, len - 1)];
     if (e[0].kind >= a.kinds) break;                     // only rows that stand for nothing are left
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c, a.C);
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (NV == 1 || c[j] >= 0) v[u][j] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c[j], a.C);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (q + u >= len || e[u].kind >= a.kinds) break;
       if (e[u].kind != kind) {
-#pragma unroll
-        for (int k = 0; k < kV; ++k) sum[k] += run[k];
-        close_kind(s, close, kind, c, sum, true, first, false, write);
-#pragma unroll
-        for (int k = 0; k < kV; ++k) sum[k] = run[k] = 0.f;
-        count = 0;
+        end_kind(true, first, false);
+        clear();
         first = false;
         kind = e[u].kind;
       }
-      float x[kV];
-      unpack(x, v[u], T());
 #pragma unroll
-      for (int k = 0; k < kV; ++k) run[k] += x[k];
-      if (++count == kRun) {
-        count = 0;
+      for (int j = 0; j < NV; ++j) {
+        float x[kV];
+        unpack(x, v[u][j], T());
 #pragma unroll
-        for (int k = 0; k < kV; ++k) {
-          sum[k] += run[k];
-          run[k] = 0.f;
-        }
+        for (int k = 0; k < kV; ++k) sum[j][k] += x[k];
       }
     }
   }
-#pragma unroll
-  for (int k = 0; k < kV; ++k) sum[k] += run[k];
   close.goes_on = past == kind;
-  close_kind(s, close, kind, c, sum, kind < a.kinds, first, true, write);
+  end_kind(kind < a.kinds, first, true);
 }
 
 __device__ __forceinline__ int kind_of_entry(int k) { return k < 0 ? ~k : k; }
@@ -393,7 +449,7 @@ __global__ __launch_bounds__(256) void sum_entries_kernel(const Sums s) {
   if (item >= (long long)s.nchunk * s.nslab) return;
   Close close;
   close.chunk = (int)(item / s.nslab);
-  const int c = columns_of<4>(s, (int)(item - (long long)close.chunk * s.nslab), t);
+  const int c = t < s.used ? column_of<4>((int)(item - (long long)close.chunk * s.nslab) * s.used + t, a.C) : -1;
   if (c < 0) return;
   const int p0 = close.chunk * s.chunk, p1 = min(p0 + s.chunk, s.n);
   int kind = kind_of_entry(s.in_kind[p0]);
@@ -481,7 +537,7 @@ __global__ __launch_bounds__(64 * kLastWaves) void last_sums_kernel(const Sums s
 }
 
 constexpr int kLastMost = 2048;        // entries that the last launch takes
-constexpr int kEntryChunk = 16;
+constexpr int kEntryChunk = 32;
 
 int lanes_of(int vectors) {
   int l = 1;
@@ -490,30 +546,31 @@ int lanes_of(int vectors) {
 }
 
 struct Plan {
-  int passes, bits;
-  int per, tiles;              // pairs of a thread; workgroups of the sort
-  int lanes, nslab;            // of rows of 16-byte vectors
+  int all_bits, passes, bits;
+  int per, tiles;              // pairs of a thread; workgroups of the sort; 0: it is one
+  int nv, lanes, nslab;        // vectors of a thread, threads of a row's slab, slabs
   int chunk, nchunk;
   long long entries[8];        // of each level's list
   int levels;                  // lists of entries
 };
-Plan plan(long long rows, int kinds, int C, int bytes, int n_cu) {
+Plan plan(long long rows, int kinds, int C, int bytes) {
   Plan p{};
-  int bits = 1;
-  while (bits < 31 && (kinds >> bits) != 0) ++bits;            // values 0 .. kinds
-  p.passes = (bits + kBits - 1) / kBits;
-  p.bits = (bits + p.passes - 1) / p.passes;
+  p.all_bits = 1;
+  while (p.all_bits < 31 && (kinds >> p.all_bits) != 0) ++p.all_bits;          // values 0 .. kinds
+  p.passes = rows <= kSmall ? 1 : (p.all_bits + kBits - 1) / kBits;
+  p.bits = (p.all_bits + p.passes - 1) / p.passes;
+  // Small tiles until there are some hundred of them (65521 rows by tiles of 4096: 16 us a kernel, by tiles of 256: 5).
   p.per = rows <= 65536 ? 1 : (rows <= 1048576 ? 4 : 16);
-  p.tiles = (int)((rows + kSortThreads * p.per - 1) / (kSortThreads * p.per));
+  p.tiles = rows <= kSmall ? 0 : (int)((rows + kSortThreads * p.per - 1) / (kSortThreads * p.per));
   const int vectors = (C * bytes + 15) / 16;
-  p.lanes = lanes_of(vectors);
-  p.nslab = (vectors + p.lanes - 1) / p.lanes;
-  // 32 waves a CU, 16 to 256 rows a chunk
-  const long long seats = (long long)n_cu * 32 * (64 / p.lanes);
-  long long chunk = (rows * p.nslab + seats - 1) / seats;
-  p.chunk = (int)(chunk < 16 ? 16 : (chunk > 256 ? 256 : (chunk + 7) / 8 * 8));
+  p.nv = vectors <= 64 ? 1 : (vectors <= 128 ? 2 : 4);
+  p.lanes = lanes_of((vectors + p.nv - 1) / p.nv);
+  p.nslab = (vectors + p.nv * p.lanes - 1) / (p.nv * p.lanes);
+  // a thousand waves, but 16 to 64 rows a chunk
+  const long long waves = 1024, chunk = (rows * p.nslab * p.lanes / 64 + waves - 1) / waves;
+  p.chunk = (int)(chunk < 16 ? 16 : (chunk > 64 ? 64 : (chunk + 7) / 8 * 8));
   p.nchunk = (int)((rows + p.chunk - 1) / p.chunk);
-  long long e = 2LL * p.nchunk;
+  long long e = p.nchunk > 1 ? 2LL * p.nchunk : 0;           // of one chunk nothing is left to sum
   while (e > 0) {
     p.entries[p.levels++] = e;
     if (e <= kLastMost) break;
@@ -538,7 +595,7 @@ Room room(const Plan& p, long long rows, int C) {
   r.pair[0] = take(rows * sizeof(Pair));
   r.pair[1] = p.passes > 1 ? take(rows * sizeof(Pair)) : 0;
   r.count = take(((size_t)p.tiles << p.bits) * sizeof(int));
-  r.total = take(((size_t)1 << p.bits) * sizeof(int));
+  r.total = take(p.tiles > 0 ? ((size_t)1 << p.bits) * sizeof(int) : 0);
   for (int l = 0; l < p.levels; ++l) {
     r.kind[l] = take(p.entries[l] * sizeof(int));
     r.sum[l] = take((size_t)p.entries[l] * C * sizeof(float));
@@ -557,16 +614,17 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
   m.nchunk = p.nchunk;
   m.lanes = p.lanes;
   m.nslab = p.nslab;
-  m.used = ((a.C + kVector<T> - 1) / kVector<T> + p.nslab - 1) / p.nslab;
-  const long long fill = ((long long)a.kinds + 255) / 256, fill_most = 8LL * a.n_cu;
+  const long long fill = ((long long)a.kinds + kClear - 1) / kClear, fill_most = 1 << 20;
   m.fill_blocks = (int)(fill < fill_most ? fill : fill_most);
-  const int seats = 256 / p.lanes;
-  auto blocks = [&](long long chunks) { return (unsigned)((chunks * p.nslab + seats - 1) / seats); };
   if (p.levels > 0) {
     m.out = reinterpret_cast<float*>(a.workspace + r.sum[0]);
     m.out_kind = reinterpret_cast<int*>(a.workspace + r.kind[0]);
   }
-  hipLaunchKernelGGL((sum_rows_kernel<T>), dim3(m.fill_blocks + blocks(p.nchunk)), dim3(256), 0, s, m);
+  const long long seats = 256 / p.lanes, items = (long long)p.nchunk * p.nslab;
+  const dim3 grid((unsigned)(m.fill_blocks + (items + seats - 1) / seats));
+  if (p.nv == 1) hipLaunchKernelGGL((sum_rows_kernel<T, 1>), grid, dim3(256), 0, s, m);
+  else if (p.nv == 2) hipLaunchKernelGGL((sum_rows_kernel<T, 2>), grid, dim3(256), 0, s, m);
+  else hipLaunchKernelGGL((sum_rows_kernel<T, 4>), grid, dim3(256), 0, s, m);
   // entries: four columns a thread
   const int fours = (a.C + 3) / 4;
   m.lanes = lanes_of(fours);
@@ -594,6 +652,10 @@ const Pair* sort(const EmbedArgs& a, const Plan& p, const Room& r, hipStream_t s
   Pair* pair[2] = {reinterpret_cast<Pair*>(a.workspace + r.pair[0]), reinterpret_cast<Pair*>(a.workspace + r.pair[1])};
   int* count = reinterpret_cast<int*>(a.workspace + r.count);
   int* total = reinterpret_cast<int*>(a.workspace + r.total);
+  if (p.tiles == 0) {
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSmallThreads), 0, s, a, p.all_bits, pair[0]);
+    return pair[0];
+  }
   const Pair* in = nullptr;
   for (int k = 0; k < p.passes; ++k) {
     const int shift = k * p.bits;
@@ -608,8 +670,8 @@ const Pair* sort(const EmbedArgs& a, const Plan& p, const Room& r, hipStream_t s
 
 }  // namespace
 
-size_t embed_rows_bytes(long long rows, int kinds, int C, int n_cu) {
-  const Plan p2 = plan(rows, kinds, C, 2, n_cu), p4 = plan(rows, kinds, C, 4, n_cu);
+size_t embed_rows_bytes(long long rows, int kinds, int C) {
+  const Plan p2 = plan(rows, kinds, C, 2), p4 = plan(rows, kinds, C, 4);
   const size_t b2 = room(p2, rows, C).bytes, b4 = room(p4, rows, C).bytes;
   return b2 > b4 ? b2 : b4;
 }
@@ -637,7 +699,7 @@ hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_embed_rows_back(const EmbedArgs& a, hipStream_t s) {
-  const Plan p = plan(a.rows, a.kinds, a.C, a.bf16 ? 2 : 4, a.n_cu);
+  const Plan p = plan(a.rows, a.kinds, a.C, a.bf16 ? 2 : 4);
   const Room r = room(p, a.rows, a.C);
   const Pair* sorted = a.rows == 0 ? nullptr : p.per == 1 ? sort<1>(a, p, r, s) : p.per == 4 ? sort<4>(a, p, r, s) : sort<16>(a, p, r, s);
   if (a.bf16) gradient<u16>(a, p, r, sorted, s);

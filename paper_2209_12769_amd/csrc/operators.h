@@ -238,9 +238,8 @@ struct EmbedArgs {
   long long lddt;
   char* workspace;
   int* status;                   // ids out of range set status[1]
-  int n_cu;
 };
-size_t embed_rows_bytes(long long rows, int kinds, int C, int n_cu);
+size_t embed_rows_bytes(long long rows, int kinds, int C);
 hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t s);
 hipError_t launch_embed_rows_back(const EmbedArgs& a, hipStream_t s);
 
