@@ -344,6 +344,36 @@ __device__ __forceinline__ int column_of(int at, int C) {
   return c < C ? max(min(c, C - kV), 0) : -1;
 }
 
+// The first pair of the sorted list with that kind or a larger one: the wave looks at 64 places at a time (three steps for 200000
+// pairs, where halving waits for memory 17 times).
+__device__ __forceinline__ int first_of(const Pair* sorted, int n, long long kind) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, count = n;       // it is one of lo .. lo + count
+  while (count > 0) {
+    const int stride = (count + 63) >> 6, at = lane * stride;
+    const bool below = at < count && sorted[lo + at].kind < kind;
+    const int steps = __popcll(__ballot(below));       // a pair that is below has all in front of it below
+    if (steps == 0) return lo;
+    lo += (steps - 1) * stride + 1;
+    count = min(stride - 1, count - (steps - 1) * stride - 1);
+  }
+  return lo;
+}
+// Zeros by one wave, on 16-byte boundaries but for the row's first and last vector.
+template <typename T>
+__device__ __forceinline__ void clear_row(T* row, int C) {
+  const int lane = threadIdx.x & 63;
+  const u32x4 zero = {0, 0, 0, 0};
+  if (C < kVector<T>) {
+    if (lane < C) row[lane] = 0;
+    return;
+  }
+  const int skip = (int)(-(reinterpret_cast<size_t>(row) / sizeof(T)) & (kVector<T> - 1)), whole = (C - skip) / kVector<T>;
+  u32x4* to = reinterpret_cast<u32x4*>(row + skip);
+  for (int at = lane; at < whole; at += 64) to[at] = zero;
+  if (lane == 0 && skip != 0) *reinterpret_cast<u32x4_any*>(row) = zero;
+  if (lane == 1 && skip + whole * kVector<T> < C) *reinterpret_cast<u32x4_any*>(row + (C - kVector<T>)) = zero;
+}
 // Clears the kinds that have no row: 64 kinds a workgroup, its waves take them in turn.
 constexpr int kClear = 64;
 template <typename T>
@@ -351,91 +381,72 @@ __device__ void clear_unused(const Sums& s, int block) {
   const EmbedArgs& a = s.a;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (long long k0 = (long long)block * kClear; k0 < a.kinds; k0 += (long long)s.fill_blocks * kClear) {
-    const int kind = (int)min(k0 + lane, (long long)a.kinds - 1);
-    int lo = 0, hi = s.n;      // the first pair of that kind or a larger one
+    const long long kind = k0 + lane;
+    int lo = first_of(s.sorted, s.n, k0), hi = first_of(s.sorted, s.n, k0 + kClear);
+    const int end = hi;
     while (lo < hi) {
       const int mid = lo + (hi - lo) / 2;
       if (s.sorted[mid].kind < kind) lo = mid + 1;
       else hi = mid;
     }
-    const bool none = k0 + lane < a.kinds && (lo >= s.n || s.sorted[lo].kind != kind);
+    const bool none = kind < a.kinds && (lo >= end || s.sorted[lo].kind != kind);
     int turn = 0;
-    for (u64 left = __ballot(none); left; left &= left - 1, ++turn) {
-      if ((turn & 3) != wave) continue;
-      T* row = static_cast<T*>(a.dtable) + (k0 + __builtin_ctzll(left)) * a.lddt;
-      for (int at = lane; at * kVector<T> < a.C; at += 64) store_vector<T, false>(row, column_of<kVector<T>>(at, a.C), a.C, u32x4{0, 0, 0, 0});
-    }
+    for (u64 left = __ballot(none); left; left &= left - 1, ++turn)
+      if (turn % 4 == wave) clear_row<T>(static_cast<T*>(a.dtable) + (k0 + __builtin_ctzll(left)) * a.lddt, a.C);
   }
 }
 
-// First level: chunks of the sorted rows, of up to 64 of them: one sum in fp32 a kind.  A thread has NV vectors of a row, `lanes` apart.
-template <typename T, int NV>
+// First level: chunks of the sorted rows, of up to 64 of them: one sum in fp32 a kind.
+template <typename T>
 __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
-  constexpr int kV = kVector<T>, kAhead = NV > 2 ? 4 : 8;
+  constexpr int kV = kVector<T>, kAhead = 8;
   const EmbedArgs& a = s.a;
   if ((int)blockIdx.x < s.fill_blocks) return clear_unused<T>(s, blockIdx.x);
+  const int block = blockIdx.x - s.fill_blocks;
   const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
-  const long long item = (long long)(blockIdx.x - s.fill_blocks) * seats + threadIdx.x / s.lanes;
+  const long long item = (long long)block * seats + threadIdx.x / s.lanes;
   if (item >= (long long)s.nchunk * s.nslab) return;
   Close close;
   close.chunk = (int)(item / s.nslab);
-  const int slab = (int)(item - (long long)close.chunk * s.nslab);
-  int c[NV];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) c[j] = column_of<kV>(slab * NV * s.lanes + j * s.lanes + t, a.C);
-  if (c[0] < 0) return;
+  const int c = t < s.used ? column_of<kV>((int)(item - (long long)close.chunk * s.nslab) * s.used + t, a.C) : -1;
+  if (c < 0) return;
   const long long p0l = (long long)close.chunk * s.chunk;
   const int p0 = (int)p0l, p1 = (int)min(p0l + s.chunk, (long long)s.n), len = p1 - p0;
   const T* dY = static_cast<const T*>(a.dY);
   int kind = s.sorted[p0].kind;
   close.from_before = p0 > 0 && s.sorted[p0 - 1].kind == kind;
   const int past = p1 < s.n ? s.sorted[p1].kind : -1;
-  float sum[NV][kV];
-  auto clear = [&]() {
+  auto write = [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c, x); };
+  float sum[kV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int k = 0; k < kV; ++k) sum[j][k] = 0.f;
-  };
-  auto end_kind = [&](bool any, bool first, bool last) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (c[j] >= 0)
-        close_kind(s, close, kind, c[j], sum[j], any, first, last, [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c[j], x); });
-  };
-  clear();
+  for (int k = 0; k < kV; ++k) sum[k] = 0.f;
   bool first = true;
   for (int q = 0; q < len; q += kAhead) {
     Pair e[kAhead];
-    u32x4 v[kAhead][NV];
+    u32x4 v[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) e[u] = s.sorted[p0 + min(q + u, len - 1)];
     if (e[0].kind >= a.kinds) break;                     // only rows that stand for nothing are left
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (NV == 1 || c[j] >= 0) v[u][j] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c[j], a.C);
+    for (int u = 0; u < kAhead; ++u) v[u] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c, a.C);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (q + u >= len || e[u].kind >= a.kinds) break;
       if (e[u].kind != kind) {
-        end_kind(true, first, false);
-        clear();
+        close_kind(s, close, kind, c, sum, true, first, false, write);
+#pragma unroll
+        for (int k = 0; k < kV; ++k) sum[k] = 0.f;
         first = false;
         kind = e[u].kind;
       }
+      float x[kV];
+      unpack(x, v[u], T());
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        float x[kV];
-        unpack(x, v[u][j], T());
-#pragma unroll
-        for (int k = 0; k < kV; ++k) sum[j][k] += x[k];
-      }
+      for (int k = 0; k < kV; ++k) sum[k] += x[k];
     }
   }
   close.goes_on = past == kind;
-  end_kind(kind < a.kinds, first, true);
+  close_kind(s, close, kind, c, sum, kind < a.kinds, first, true, write);
 }
 
 __device__ __forceinline__ int kind_of_entry(int k) { return k < 0 ? ~k : k; }
@@ -494,7 +505,7 @@ __global__ __launch_bounds__(256) void sum_entries_kernel(const Sums s) {
 }
 
 // The last list: a workgroup for each entry that begins a kind, and 256 of its columns; its waves take the entries in turn.
-constexpr int kLastWaves = 16;
+constexpr int kLastWaves = 8;
 __global__ __launch_bounds__(64 * kLastWaves) void last_sums_kernel(const Sums s) {
   constexpr int kAhead = 4;
   const EmbedArgs& a = s.a;
@@ -548,7 +559,7 @@ int lanes_of(int vectors) {
 struct Plan {
   int all_bits, passes, bits;
   int per, tiles;              // pairs of a thread; workgroups of the sort; 0: it is one
-  int nv, lanes, nslab;        // vectors of a thread, threads of a row's slab, slabs
+  int lanes, nslab;            // threads of a row's slab, slabs
   int chunk, nchunk;
   long long entries[8];        // of each level's list
   int levels;                  // lists of entries
@@ -563,11 +574,10 @@ Plan plan(long long rows, int kinds, int C, int bytes) {
   p.per = rows <= 65536 ? 1 : (rows <= 1048576 ? 4 : 16);
   p.tiles = rows <= kSmall ? 0 : (int)((rows + kSortThreads * p.per - 1) / (kSortThreads * p.per));
   const int vectors = (C * bytes + 15) / 16;
-  p.nv = vectors <= 64 ? 1 : (vectors <= 128 ? 2 : 4);
-  p.lanes = lanes_of((vectors + p.nv - 1) / p.nv);
-  p.nslab = (vectors + p.nv * p.lanes - 1) / (p.nv * p.lanes);
-  // a thousand waves, but 16 to 64 rows a chunk
-  const long long waves = 1024, chunk = (rows * p.nslab * p.lanes / 64 + waves - 1) / waves;
+  p.lanes = lanes_of(vectors);
+  p.nslab = (vectors + p.lanes - 1) / p.lanes;
+  // eight thousand waves, but 16 to 64 rows a chunk
+  const long long seats = 8192LL * (64 / p.lanes), chunk = (rows * p.nslab + seats - 1) / seats;
   p.chunk = (int)(chunk < 16 ? 16 : (chunk > 64 ? 64 : (chunk + 7) / 8 * 8));
   p.nchunk = (int)((rows + p.chunk - 1) / p.chunk);
   long long e = p.nchunk > 1 ? 2LL * p.nchunk : 0;           // of one chunk nothing is left to sum
@@ -614,6 +624,7 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
   m.nchunk = p.nchunk;
   m.lanes = p.lanes;
   m.nslab = p.nslab;
+  m.used = ((a.C + kVector<T> - 1) / kVector<T> + p.nslab - 1) / p.nslab;
   const long long fill = ((long long)a.kinds + kClear - 1) / kClear, fill_most = 1 << 20;
   m.fill_blocks = (int)(fill < fill_most ? fill : fill_most);
   if (p.levels > 0) {
@@ -622,9 +633,7 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
   }
   const long long seats = 256 / p.lanes, items = (long long)p.nchunk * p.nslab;
   const dim3 grid((unsigned)(m.fill_blocks + (items + seats - 1) / seats));
-  if (p.nv == 1) hipLaunchKernelGGL((sum_rows_kernel<T, 1>), grid, dim3(256), 0, s, m);
-  else if (p.nv == 2) hipLaunchKernelGGL((sum_rows_kernel<T, 2>), grid, dim3(256), 0, s, m);
-  else hipLaunchKernelGGL((sum_rows_kernel<T, 4>), grid, dim3(256), 0, s, m);
+  hipLaunchKernelGGL((sum_rows_kernel<T>), grid, dim3(256), 0, s, m);
   // entries: four columns a thread
   const int fours = (a.C + 3) / 4;
   m.lanes = lanes_of(fours);

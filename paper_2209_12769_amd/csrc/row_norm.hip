@@ -115,20 +115,30 @@ __device__ __forceinline__ void values(float (&x)[NV * kVector<T>], const Fetche
   }
 }
 
+// gamma or beta at a vector's columns.
+template <typename T, Fit kFit>
+__device__ __forceinline__ void vector_at(float (&g)[kVector<T>], const float* v, float none, int at, int C) {
+#pragma unroll
+  for (int k = 0; k < kVector<T>; k += 4) {
+    float w[4] = {none, none, none, none};
+    if (v) unpack(w, load_vector<float, kFit != kShort>(v, at + k, C), 0.f);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) g[k + u] = w[u];
+  }
+}
 template <typename T, int NV, Fit kFit>
 __device__ __forceinline__ void vectors_at(float (&g)[NV * kVector<T>], const float* v, float none, const Columns<T, NV>& q, int C) {
   constexpr int kV = kVector<T>;
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+  for (int j = 0; j < NV; ++j) {
+    float w[kV];
+    vector_at<T, kFit>(w, v, none, q.at[j], C);
 #pragma unroll
-    for (int k = 0; k < kV; k += 4) {
-      float w[4] = {none, none, none, none};
-      if (v) unpack(w, load_vector<float, kFit != kShort>(v, q.at[j] + k, C), 0.f);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) g[j * kV + k + u] = w[u];
-    }
+    for (int k = 0; k < kV; ++k) g[j * kV + k] = w[k];
+  }
 }
-template <typename T, int NV, Fit kFit>
+// kOwn: a vector that ends with the row writes only what is its own, so that its neighbour's may be read until then.
+template <typename T, int NV, Fit kFit, bool kOwn = false>
 __device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], T* p, unsigned row, const Columns<T, NV>& q, int C) {
   constexpr int kV = kVector<T>;
 #pragma unroll
@@ -137,8 +147,13 @@ __device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], T* p, uns
 #pragma unroll
     for (int k = 0; k < kV; ++k) w[k] = y[j * kV + k];
     if (kFit == kWhole || q.skip[j] < kV) {
-      if constexpr (kFit == kShort) store_vector<T, false>(p + row, q.at[j], C, pack(w, T()));
-      else *reinterpret_cast<u32x4_any*>(p + (row + (unsigned)q.at[j])) = pack(w, T());
+      if constexpr (kFit == kShort) {
+        store_vector<T, false>(p + row, q.at[j], C, pack(w, T()));
+      } else if (kOwn && kFit == kBack && q.skip[j] > 0) {
+#pragma unroll
+        for (int k = 0; k < kV; ++k)
+          if (k >= q.skip[j]) narrow(w[k], p[row + (unsigned)(q.at[j] + k)]);
+      } else *reinterpret_cast<u32x4_any*>(p + (row + (unsigned)q.at[j])) = pack(w, T());
     }
   }
 }
@@ -206,12 +221,12 @@ struct Seat {
 // Elements between the workgroup's first row and the seat's: below 2^32 / sizeof(float), rows are at most 2^22 elements apart.
 __device__ __forceinline__ unsigned rows_on(int seat, long long ld) { return (unsigned)seat * (unsigned)ld; }
 
-#ifndef ROWS
-#define ROWS 2
-#endif
+// Rows of a seat in the forward pass, whose requests go out together (5.7 M rows of 256 in bf16 with SiLU: one 1090 us, two 995,
+// four 1018).
+constexpr int kSeatRows = 2;
 template <typename T, int NV, int kLanes, Fit kFit>
 __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel(const RowNormArgs a, int row_lanes) {
-  constexpr int kV = kVector<T>, kN = NV * kV, kRows = kLanes == kGroup ? 1 : ROWS;
+  constexpr int kV = kVector<T>, kN = NV * kV, kRows = kLanes == kGroup ? 1 : kSeatRows;
   __shared__ float red[kLanes == kGroup ? 3 * kMostWaves : 1];
   const Seat<kLanes> s(row_lanes);
   const Columns<T, NV> q = columns_of<T, NV, kFit>(s.t, s.lanes, a.C);
@@ -253,7 +268,10 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel
           s2 = fmaf(d, d, s2);
         }
       row_sums<kLanes>(s1, s2, s.lanes, red + kMostWaves);
-      const float lacks = s1 * share, var = fmaf(-lacks, lacks, s2 * share);
+      // What is less than the rounding of the d's own (2^-24 of their size) says nothing about m: the d of one size are rounded alike,
+      // which would move a mean that is far smaller than they are.
+      const float square = s2 * share, found = s1 * share, lacks = found * found <= 0x1p-48f * square ? 0.f : found;
+      const float var = fmaf(-lacks, lacks, square);
       const float r = inverse_root((var < 0.f ? 0.f : var) + a.eps);
       const float shift = -lacks * r;
 #pragma unroll
@@ -272,30 +290,40 @@ template <typename T, typename X, int NV, int kLanes, Fit kFit>
 __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_kernel(const RowNormArgs a, int row_lanes) {
   constexpr int kV = kVector<T>, kN = NV * kV;
   constexpr bool kKept = !std::is_same<T, X>::value, kWide = kLanes == kGroup;
+  // of sixteen values a thread the sums over rows stay in LDS, a thread's fours of both 1024 fours apart
+  constexpr bool kLds = kN > 8;
   __shared__ float red[kWide ? 4 * kMostWaves : 2 * 256 * kN];
+  __shared__ float4 sums[kLds ? 1024 * kN / 2 : 1];
   const Seat<kLanes> s(row_lanes);
   const Columns<T, NV> q = columns_of<T, NV, kFit>(s.t, s.lanes, a.C);
-  float gamma[kN], beta[kN], dg[kN], db[kN], dgs[kN], dbs[kN];
-  if (kN == 8) {
+  float gamma[kN], beta[kN], dg[kN], db[kN], dgs[kN], dbs[kN];     // of eight values a thread
+  if (!kLds) {
     vectors_at<T, NV, kFit>(gamma, a.gamma, 1.f, q, a.C);
     vectors_at<T, NV, kFit>(beta, a.beta, 0.f, q, a.C);
   }
   float* out = a.workspace + (size_t)blockIdx.x * 2 * a.C;
-  // the runs' sums: in registers, or, of sixteen values a thread, where the workgroup's go
+  // the runs' sums: in registers, or where the workgroup's go
   auto join = [&](bool begin) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int v = 0; v < kV; ++v) {
         const int k = j * kV + v, c = q.at[j] + v;
-        if (kN == 8) {
+        if constexpr (!kLds) {
           dgs[k] = begin ? 0.f : dgs[k] + dg[k];
           dbs[k] = begin ? 0.f : dbs[k] + db[k];
-        } else if (a.dgamma && own<T, NV, kFit>(q, j, v, a.C)) {
-          out[c] = begin ? 0.f : out[c] + dg[k];
-          out[a.C + c] = begin ? 0.f : out[a.C + c] + db[k];
+          dg[k] = db[k] = 0.f;
+        } else {
+          float4& g4 = sums[(k / 4 * 2) * 1024 + threadIdx.x];
+          float4& b4 = sums[(k / 4 * 2 + 1) * 1024 + threadIdx.x];
+          float& g = reinterpret_cast<float*>(&g4)[k & 3];
+          float& b = reinterpret_cast<float*>(&b4)[k & 3];
+          if (a.dgamma && own<T, NV, kFit>(q, j, v, a.C)) {
+            out[c] = begin ? 0.f : out[c] + g;
+            out[a.C + c] = begin ? 0.f : out[a.C + c] + b;
+          }
+          g = b = 0.f;
         }
-        dg[k] = db[k] = 0.f;
       }
   };
   join(true);
@@ -309,40 +337,62 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
     if constexpr (kKept) fetch<T, NV, kFit>(f, a.kept.code + row0 * a.kept.ld_code, x_on, a.kept.exponent + row0 * a.kept.ld_exponent, e_on, q);
     else fetch<T, NV, kFit>(f, static_cast<const T*>(a.X) + row0 * a.ldx, x_on, q, a.C);
     fetch<T, NV, kFit>(fd, static_cast<const T*>(a.dY) + row0 * a.lddy, dy_on, q, a.C);
-    if (a.dRes) fetch<T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
+    if (!kLds && a.dRes) fetch<T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
     const float m = a.mean[row0 + s.seat], r = a.rstd[row0 + s.seat];
-    if (kN > 8) {                                        // registers for eight values a thread only
-      vectors_at<T, NV, kFit>(gamma, a.gamma, 1.f, q, a.C);
-      vectors_at<T, NV, kFit>(beta, a.beta, 0.f, q, a.C);
-    }
-    float xh[kN], dz[kN], z[kN];
+    float xh[kN], dz[kN];
     values<T, NV, kFit>(xh, f, q);
     values<T, NV, kFit>(dz, fd, q);
-#pragma unroll
-    for (int k = 0; k < kN; ++k) {
-      xh[k] = (xh[k] - m) * r;
-      z[k] = fmaf(gamma[k], xh[k], beta[k]);
-    }
-    if (a.act != DC_ACT_NONE) {
-      slopes<kN>(z, a.act);
-#pragma unroll
-      for (int k = 0; k < kN; ++k) dz[k] *= z[k];
-    }
     float s1 = 0.f, s2 = 0.f;
+    // vector by vector: of sixteen values a thread there are no registers for all, nor for gamma, beta and dres all the time
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      float gj[kV], bj[kV], z[kV];
+      if (kLds) {
+        vector_at<T, kFit>(gj, a.gamma, 1.f, q.at[j], a.C);
+        vector_at<T, kFit>(bj, a.beta, 0.f, q.at[j], a.C);
+      }
 #pragma unroll
       for (int v = 0; v < kV; ++v) {
         const int k = j * kV + v;
-        dg[k] = fmaf(dz[k], xh[k], dg[k]);
-        db[k] += dz[k];
-        dz[k] *= gamma[k];
+        if (!kLds) {
+          gj[v] = gamma[k];
+          bj[v] = beta[k];
+        }
+        xh[k] = (xh[k] - m) * r;
+        z[v] = fmaf(gj[v], xh[k], bj[v]);
+      }
+      if (a.act != DC_ACT_NONE) {
+        slopes<kV>(z, a.act);
+#pragma unroll
+        for (int v = 0; v < kV; ++v) dz[j * kV + v] *= z[v];
+      }
+#pragma unroll
+      for (int v = 0; v < kV; ++v) {
+        const int k = j * kV + v;
+        if constexpr (!kLds) {
+          dg[k] = fmaf(dz[k], xh[k], dg[k]);
+          db[k] += dz[k];
+        } else if (k % 4 == 0) {
+          float4 g = sums[(k / 4 * 2) * 1024 + threadIdx.x], b = sums[(k / 4 * 2 + 1) * 1024 + threadIdx.x];
+          g.x = fmaf(dz[k], xh[k], g.x);
+          g.y = fmaf(dz[k + 1], xh[k + 1], g.y);
+          g.z = fmaf(dz[k + 2], xh[k + 2], g.z);
+          g.w = fmaf(dz[k + 3], xh[k + 3], g.w);
+          b.x += dz[k];
+          b.y += dz[k + 1];
+          b.z += dz[k + 2];
+          b.w += dz[k + 3];
+          sums[(k / 4 * 2) * 1024 + threadIdx.x] = g;
+          sums[(k / 4 * 2 + 1) * 1024 + threadIdx.x] = b;
+        }
+        dz[k] *= gj[v];
         const float u = own<T, NV, kFit>(q, j, v, a.C) ? dz[k] : 0.f;
         s1 += u;
         s2 = fmaf(u, xh[k], s2);
       }
+    }
     // dX may be dres, and a vector that ends with the row is its neighbour's too, which may be another wave's: read before that writes
-    if (kWide && kFit == kBack && a.dRes) {
+    if (!kLds && kWide && kFit == kBack && a.dRes) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) asm volatile("" ::"v"(fr.v[j]));
     }
@@ -350,6 +400,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
     parity ^= 1;
     s1 *= share;
     s2 *= share;
+    if (kLds && a.dRes) fetch<T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
 #pragma unroll
     for (int k = 0; k < kN; ++k) dz[k] = r * (dz[k] - s1 - xh[k] * s2);
     if (a.dRes) {
@@ -358,7 +409,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
 #pragma unroll
       for (int k = 0; k < kN; ++k) dz[k] += add[k];
     }
-    put<T, NV, kFit>(dz, static_cast<T*>(a.dX) + row0 * a.lddx, dx_on, q, a.C);
+    put<T, NV, kFit, kLds>(dz, static_cast<T*>(a.dX) + row0 * a.lddx, dx_on, q, a.C);
     if (++run == kRun) {
       run = 0;
       join(false);
@@ -366,7 +417,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
   }
   if (!a.dgamma) return;
   join(false);
-  if constexpr (kN > 8) return;
+  if constexpr (kLds) return;
   if constexpr (kWide) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -405,27 +456,40 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
 
 struct Plan {
   bool wide;
-  int nv16;                    // sixteen values a thread instead of eight
+  int per;                     // values a thread
   int threads, lanes;          // of a workgroup; of a row
   long long blocks;
 };
-Plan plan(long long rows, int C, int n_cu, bool back) {
+// `per` values a thread: in one row's lanes up to 64 threads, else in a workgroup.
+Plan plan(long long rows, int C, int per) {
   Plan p{};
-  p.wide = C > kNarrow;
-  p.nv16 = C > 8192;
-  const int per = p.nv16 ? 16 : 8, need = (C + per - 1) / per;
-  if (p.wide) {
-    p.threads = p.lanes = (need + 63) / 64 * 64;
-  } else {
-    p.threads = 256;
-    p.lanes = 1;
-    while (p.lanes < need) p.lanes *= 2;
-  }
-  const long long seats = (p.wide ? 1 : 256 / p.lanes) * (back || p.wide ? 1 : ROWS), need_blocks = (rows + seats - 1) / seats;
-  // Forward: a row a seat, so that the rows come in the order in which the workgroups are handed out (a launch has less than
-  // 2^32 threads).  Backward: what a CU holds at a time, each workgroup sums gradients of gamma and beta.
-  const long long most = back ? (long long)n_cu * (1024 / p.threads < 1 ? 1 : 1024 / p.threads) : (1LL << 31) / p.threads;
-  p.blocks = need_blocks < most ? need_blocks : most;
+  p.per = per;
+  const int need = (C + per - 1) / per;
+  p.wide = need > 64;
+  p.lanes = 1;
+  while (!p.wide && p.lanes < need) p.lanes *= 2;
+  if (p.wide) p.lanes = (need + 63) / 64 * 64;
+  p.threads = p.wide ? p.lanes : 256;
+  const long long seats = p.wide ? 1 : 256 / p.lanes;
+  p.blocks = (rows + seats - 1) / seats;
+  return p;
+}
+// A row a seat at a time, in the order in which the workgroups are handed out (a launch has less than 2^32 threads).  Wide rows in
+// bf16 take sixteen values a thread, two requests, as rows in fp32 do with eight (50000 x 4096 in bf16 211 -> MEASURE us).
+Plan forward_plan(long long rows, int C, bool bf16) {
+  Plan p = plan(rows, C, C > 8192 || (bf16 && C > kNarrow) ? 16 : 8);
+  if (!p.wide) p.blocks = (p.blocks + kSeatRows - 1) / kSeatRows;
+  const long long most = (1LL << 31) / p.threads;
+  if (p.blocks > most) p.blocks = most;
+  return p;
+}
+// What a CU works on at a time, as each workgroup sums gradients of gamma and beta: 512 threads, or 1024 that read less than 40 bytes
+// of a row each (1000000 x 64 in fp32 142 us by 512, 160 by 1024; 2000000 x 64 in bf16 193 and 150).
+Plan back_plan(long long rows, int C, int n_cu, bool few) {
+  Plan p = plan(rows, C, C > 8192 ? 16 : 8);
+  const int each = (few ? 512 : 1024) / p.threads;
+  const long long most = (long long)n_cu * (each < 1 ? 1 : each);
+  if (p.blocks > most) p.blocks = most;
   return p;
 }
 
@@ -433,8 +497,8 @@ Plan plan(long long rows, int C, int n_cu, bool back) {
 template <int kI>
 using Number = std::integral_constant<int, kI>;
 template <typename T, typename F>
-void each_fit(const Plan& p, int C, int held, F f) {
-  const bool whole = C == p.lanes * held;
+void each_fit(const Plan& p, int C, F f) {
+  const bool whole = C == p.lanes * p.per;
   auto fit = [&](auto lanes) {
     if (whole) f(lanes, std::integral_constant<Fit, kWhole>());
     else f(lanes, std::integral_constant<Fit, kBack>());
@@ -447,14 +511,16 @@ void each_fit(const Plan& p, int C, int held, F f) {
   else f(Number<0>(), std::integral_constant<Fit, kShort>());
 }
 template <typename T>
-void forward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
+void forward(const RowNormArgs& a, hipStream_t s) {
   constexpr int NV = 8 / kVector<T>;
+  const Plan p = forward_plan(a.rows, a.C, a.bf16);
   const dim3 g((unsigned)p.blocks), b((unsigned)p.threads);
-  each_fit<T>(p, a.C, p.nv16 ? 16 : 8, [&](auto lanes, auto fit) {
+  each_fit<T>(p, a.C, [&](auto lanes, auto fit) {
     constexpr int kLanes = decltype(lanes)::value;
     constexpr Fit kFit = decltype(fit)::value;
-    if constexpr (kLanes == kGroup) {
-      if (p.nv16) {
+    // sixteen values: a workgroup's rows, and a whole wave's in bf16
+    if constexpr (kLanes == kGroup || (kLanes == 64 && sizeof(T) == 2)) {
+      if (p.per == 16) {
         hipLaunchKernelGGL((row_norm_kernel<T, 2 * NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
         return;
       }
@@ -466,11 +532,11 @@ template <typename T, typename X>
 void backward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
   constexpr int NV = 8 / kVector<T>;
   const dim3 g((unsigned)p.blocks), b((unsigned)p.threads);
-  each_fit<T>(p, a.C, p.nv16 ? 16 : 8, [&](auto lanes, auto fit) {
+  each_fit<T>(p, a.C, [&](auto lanes, auto fit) {
     constexpr int kLanes = decltype(lanes)::value;
     constexpr Fit kFit = decltype(fit)::value;
     if constexpr (kLanes == kGroup) {
-      if (p.nv16) {
+      if (p.per == 16) {
         hipLaunchKernelGGL((row_norm_back_kernel<T, X, 2 * NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
         return;
       }
@@ -481,18 +547,18 @@ void backward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
 
 }  // namespace
 
-size_t row_norm_floats(long long rows, int C, int n_cu) { return (size_t)plan(rows, C, n_cu, true).blocks * 2 * C; }
+size_t row_norm_floats(long long rows, int C, int n_cu) { return (size_t)back_plan(rows, C, n_cu, false).blocks * 2 * C; }
 
 hipError_t launch_row_norm(const RowNormArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  const Plan p = plan(a.rows, a.C, a.n_cu, false);
-  if (a.bf16) forward<u16>(a, p, s);
-  else forward<float>(a, p, s);
+  if (a.bf16) forward<u16>(a, s);
+  else forward<float>(a, s);
   return hipGetLastError();
 }
 
 hipError_t launch_row_norm_back(const RowNormArgs& a, hipStream_t s) {
-  const Plan p = plan(a.rows, a.C, a.n_cu, true);
+  const int bytes = a.bf16 ? 16 : 32;              // of eight values
+  const Plan p = back_plan(a.rows, a.C, a.n_cu, (a.kept.code ? 8 : bytes) + bytes + (a.dRes ? bytes : 0) >= 40);
   if (a.rows > 0) {
     if (a.kept.code) {
       if (a.bf16) backward<u16, Kept8>(a, p, s);

@@ -89,7 +89,8 @@ def norm_reference(x, gamma, beta, name, t):
     # the sum over C is off by D roundings; what it lacks is found from the differences, off by D + 4 of their size
     m_off = (D + 2) * U * d.abs().mean(1, keepdim=True)
     size = c.abs().mean(1, keepdim=True) + m_off
-    e_mean = (D + 4) * U * size
+    # less than a rounding of the differences' root mean square is not added
+    e_mean = (D + 4) * U * size + U * torch.sqrt(var + m_off ** 2)
     # d = x - m squared and summed, less the square of what m lacks; both in units of the larger sum
     e_var = (D + 8) * U * (var + 2 * m_off ** 2)
     e_rstd = rstd * (0.5 * e_var / (var + EPS) + 4 * U)
