@@ -637,7 +637,8 @@ dc_status dc_embed_rows_backward(dc_ctx* ctx, const dc_embed_rows_args* args, vo
  *                     eeee as 1 where it is 0; x is the smallest with 1.875 2^x at least the block's largest value (m: -126 at
  *                     least, v: -116; 127 at most).  E = 255: the block holds a number that is not finite, all of it reads back as
  *                     NaN.  Rounded up or down by chance, 16 bits r for m and for v: the code is floor(value in steps +
- *                     (2 r + 1) / 2^17), v at least 1 if it is not zero; mix the output function of splitmix64, place q / 2 of the
+ *                     (2 r + 1) / 2^17) (a value below 8 of the least steps first to the nearest 2^-20 of one, as fp32 has it
+ *                     there; beyond 1.875 2^127: that), v at least 1 if it is not zero; mix the output function of splitmix64, place q / 2 of the
  *                     state takes from mix(mix(seed ^ mix(t)) + (q / 2) 0xD1342543DE82EF95) the low 32 bits (q even) or the high
  *                     ones, of them the low half for m and the high half for v.  m, v and g^2 (1 - beta2) are formed by
  *                     operations of fp32 rounded one by one, w from m and v before they are rounded to codes.

@@ -435,6 +435,7 @@ class Plain:
         for p, a, n, d in zip(params, self.at, self.sizes, decay):
             self.w[a:a + n], self.decay[a:a + n], self.mask[a:a + n] = p.double().cpu().numpy().reshape(-1), d, True
         self.mc = self.vc = self.me = self.ve = None
+        self.first = 0                                     # the state's place that these begin at
 
     def flat(self, grads):
         g = np.zeros(self.w.size, f32)
@@ -471,7 +472,7 @@ class Plain:
             return z ^ (z >> np.uint64(31))
         with np.errstate(over="ignore"):
             key = mix(np.array([self.seed], np.uint64) ^ mix(np.array([self.t], np.uint64)))
-            r = mix(key + np.arange(self.w.size // 2, dtype=np.uint64) * np.uint64(0xD1342543DE82EF95))
+            r = mix(key + (self.first // 2 + np.arange(self.w.size // 2, dtype=np.uint64)) * np.uint64(0xD1342543DE82EF95))
         return r.view(np.uint16).reshape(-1, 2)[:, 0], r.view(np.uint16).reshape(-1, 2)[:, 1]
 
     def codes(self, a, is_m):
@@ -790,6 +791,75 @@ def test_calls_on_two_streams_at_once(ev):
                 got.append(work())
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+
+
+def test_offsets_beyond_32_bits(ev):
+    """Arrays of more than 4 GiB: the last rows against 64 bits, everything that is summed over all rows too."""
+    rows, C, per, kinds = 8_600_000, 128, 500, 1000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(rows, C, generator=g, device="cuda")
+    one = torch.ones(C), torch.zeros(C)
+    last = slice(rows - per, rows)
+    tail = x[last].cpu()
+    y, mean, rstd = ev.row_norm(x, eps=EPS, act="silu")
+    check_norm(tail, *one, "silu", torch.float32, (y[last], mean[last], rstd[last]))
+    dx, dgamma, dbeta = ev.row_norm_backward(x, x, None, None, mean, rstd, "silu", out=y)
+    ref = norm_back_reference(tail, tail, None, *one, mean[last].cpu(), rstd[last].cpu(), "silu", torch.float32)
+    close(dx[last], *ref[0], "dx")
+    sums = torch.zeros(4, C, dtype=torch.float64, device="cuda")
+    for lo in range(0, rows, 1_000_000):
+        v = x[lo:lo + 1_000_000].double()
+        xh = (v - mean[lo:lo + 1_000_000, None]) * rstd[lo:lo + 1_000_000, None]
+        dz = v * slope(xh, "silu")
+        sums += torch.stack([(dz * xh).sum(0), dz.sum(0), (dz * xh).abs().sum(0), dz.abs().sum(0)])
+    # 64 rows of a thread, its runs (128 rows of a workgroup's 16 or more at a time on 256 CUs), 64 bits twice; the terms' own 30
+    n = 64 + rows / (256 * 16 * 64) + 6 + 30
+    close(dgamma, sums[0].cpu(), (n * U * sums[2]).cpu(), "dgamma")
+    close(dbeta, sums[1].cpu(), (n * U * sums[3]).cpu(), "dbeta")
+    # rows by kind, and a table of as many kinds
+    ids = torch.randint(0, kinds, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    ev.embed_rows(ids, x[:kinds], 2.0, out=y)
+    assert torch.equal(y[last], x[ids[last].long()] * 2)
+    far = torch.tensor([rows - 1, 3, rows - 77], dtype=torch.int32, device="cuda")
+    assert torch.equal(ev.embed_rows(far, x), x[far.long()])
+    dt = ev.embed_rows_backward(x, ids, kinds)
+    want, size = (torch.zeros(kinds, C, dtype=torch.float64, device="cuda") for _ in range(2))
+    for lo in range(0, rows, 1_000_000):
+        v = x[lo:lo + 1_000_000].double()
+        want.index_add_(0, ids[lo:lo + 1_000_000].long(), v)
+        size.index_add_(0, ids[lo:lo + 1_000_000].long(), v.abs())
+    # 64 rows of a chunk in fp32, five lists rounded to fp32
+    close(dt, want.cpu(), (70 * U * size + 2 * U * want.abs()).cpu(), "dtable")
+    y.fill_(7)
+    ev.embed_rows_backward(x[:3], far, rows, out=y)
+    assert torch.equal(y[far.long()], x[:3]) and not y[last][:per - 77].any() and int((y != 0).any(1).sum()) == 3
+
+
+@pytest.mark.parametrize("states,n", [("f32", 2 ** 30 + 131 * 128 + 5), ("8bit", 2 ** 31 + 131 * 128 + 5)])
+def test_adamw_beyond_32_bits(ev, states, n):
+    """One tensor of more than 4 GiB (and more than 2^31 places): its last elements."""
+    t = torch.float32 if states == "f32" else torch.bfloat16
+    p, g = torch.zeros(n, dtype=t, device="cuda"), torch.zeros(n, dtype=t, device="cuda")
+    first = (n - 3000) // 128 * 128
+    p[first:].copy_(0.1 * rand(1, n - first))
+    g[first:].copy_(rand(2, n - first))
+    args = dict(lr=1e-2, betas=(0.9, 0.99), eps=1e-8)
+    o, plain = ev.adamw([p], **args, weight_decay=0.1, states=states, seed=4), Plain([p[first:]], [0.1], states, 4, **args)
+    plain.first = first
+    o.step([g])
+    plain.step([g[first:]])
+    if states == "f32":
+        off = np.abs(p[first:].double().cpu().numpy() - plain.want[:n - first])
+        assert (off <= plain.tol[:n - first]).all()
+        assert np.array_equal(o.m[first:].cpu().numpy(), plain.m) and np.array_equal(o.v[first:].cpu().numpy(), plain.v)
+        assert not p[:first].any() and not o.m[:first].any()
+    else:
+        assert np.array_equal(o.m[first:].cpu().numpy(), plain.mc) and np.array_equal(o.v[first:].cpu().numpy(), plain.vc)
+        assert np.array_equal(o.m_exponent[first // 128:].cpu().numpy(), plain.me) and np.array_equal(o.v_exponent[first // 128:].cpu().numpy(), plain.ve)
+        off = np.abs(p[first:].double().cpu().numpy() - plain.want[:n - first])
+        assert (off <= plain.tol[:n - first] + 2.0 ** -8 * np.abs(plain.want[:n - first])).all()
+        assert not p[:first].any() and not o.m[:first].any() and not o.low[:first].any()
+    assert o.steps.tolist() == [1, 0]
 
 
 # ---------------------------------------------------------------------------
