@@ -597,10 +597,10 @@ size_t dc_row_norm_bytes(const dc_ctx* ctx, int64_t rows, int32_t channels);   /
 dc_status dc_row_norm(dc_ctx* ctx, const dc_row_norm_args* args, void* stream);
 dc_status dc_row_norm_backward(dc_ctx* ctx, const dc_row_norm_args* args, void* stream);
 
-/* Rows by kind: y_i = scale * table[id_i], a row of zeros where id_i is -1 (a row that stands for nothing); rounded once.  The
- * gradient of the table: dtable_k = scale * sum of dY_i over the rows with id_i = k, zeros where there is none, all of it written;
- * formed in the order of the rows, so the same call gives the same bits.  An id outside [-1, kinds) counts as -1, and dc_check
- * reports DC_ERR_INVALID_ARG.                                                                                        */
+/* Rows by kind: y_i = scale * table[id_i] in fp32, rounded to the rows' type, a row of zeros where id_i is -1 (it stands for
+ * nothing).  The gradient of the table: dtable_k = scale * sum of dY_i over the rows with id_i = k, zeros where there is none, all
+ * of it written; formed in the order of the rows, so the same call gives the same bits.  An id outside [-1, kinds) counts as -1,
+ * and dc_check reports DC_ERR_INVALID_ARG.                                                                           */
 typedef struct {
   int32_t dtype;
   int64_t rows;

@@ -509,8 +509,15 @@ class AdamW:
 
     The state, device tensors of `total` places: m, v (float32, or uint8 codes with m_exponent and v_exponent for each 128
     places), low (int16: the low halves of bfloat16 parameters), steps (int32: steps done, 0).  Tensor k has the places
-    at[k] .. at[k] + its elements.  Saved and restored as they are, they go on where they were.  lr, betas, eps and seed may be
-    changed between steps."""
+    at[k] .. at[k] + its elements.  Saved, and copied back into them (copy_), they go on where they were.  lr, betas, eps and seed
+    may be changed between steps.  A parameter may be given other memory (data) of its shape and type."""
+
+    _STATE = frozenset(("m", "v", "m_exponent", "v_exponent", "low", "steps", "params", "at", "total", "states"))
+
+    def __setattr__(self, name, value):
+        if name in self._STATE and name in self.__dict__:              # the calls go by where they lie
+            raise AttributeError(f"{name} is kept where it is: copy_ into it")
+        object.__setattr__(self, name, value)
 
     def __init__(self, ev: "Evaluator", params, lr: float, betas, eps: float, weight_decay, states: str, seed: int):
         torch = ev.torch
@@ -532,14 +539,18 @@ class AdamW:
             half = half or (p.dtype == torch.bfloat16 and n > 0)
         self.total = total
         self._shapes, self._dtypes = [p.shape for p in self.params], [p.dtype for p in self.params]
-        # what the table holds of the tensors' places and the gradients' types, as lists
+        # what the table holds of the tensors' places and the gradients' types, as lists; `_held` keeps that memory theirs, so that a
+        # place that is still the same needs no further look
         self._ptrs, self._codes = [p.data_ptr() for p in self.params], [0] * len(self.params)
+        self._held = [p.detach() for p in self.params]
         eight = states == "8bit"
         with torch.no_grad():
             self.m, self.v = (torch.zeros(total, dtype=torch.uint8 if eight else torch.float32, device=ev.device) for _ in range(2))
             self.m_exponent, self.v_exponent = (torch.zeros(total // 128, dtype=torch.uint8, device=ev.device) if eight else None for _ in range(2))
             self.low = torch.zeros(total, dtype=torch.int16, device=ev.device) if half else None
             self.steps = torch.zeros(2, dtype=torch.int32, device=ev.device)
+        self._where = (total, self.m.data_ptr(), self.v.data_ptr(), self.m_exponent.data_ptr() if eight else 0,
+                       self.v_exponent.data_ptr() if eight else 0, self.low.data_ptr() if half else 0, self.steps.data_ptr())
 
     def _check(self, k: int, p):
         if p.device != self.ev.device or p.dtype not in self.ev._types or not p.is_contiguous():
@@ -553,11 +564,9 @@ class AdamW:
                 if p.shape != self._shapes[k] or p.dtype != self._dtypes[k]:
                     raise ValueError(f"tensor {k}: was {tuple(self._shapes[k])} {self._dtypes[k]}, not {tuple(p.shape)} {p.dtype}")
             self._table["p"] = self._ptrs = ptrs
-        eight = self.m_exponent is not None
-        return _ADAMW.pack(DC_MOMENTS_8BIT if eight else DC_MOMENTS_F32, len(ptrs), self._table.ctypes.data, self.total, self.m.data_ptr(),
-                           self.v.data_ptr(), self.m_exponent.data_ptr() if eight else 0, self.v_exponent.data_ptr() if eight else 0,
-                           0 if self.low is None else self.low.data_ptr(), self.steps.data_ptr(), grad_scale, self.lr, self.betas[0],
-                           self.betas[1], self.eps, self.seed)
+            self._held = [p.detach() for p in self.params]
+        return _ADAMW.pack(DC_MOMENTS_F32 if self.m_exponent is None else DC_MOMENTS_8BIT, len(ptrs), self._table.ctypes.data, *self._where,
+                           grad_scale, self.lr, self.betas[0], self.betas[1], self.eps, self.seed)
 
     def step(self, grads, grad_scale=None):
         """One step with a gradient for every tensor (float32 or bfloat16, contiguous, its shape), None for tensors that stay as
@@ -1045,6 +1054,8 @@ class Evaluator:
     def embed_rows_backward(self, dy, ids, kinds: int, scale: float = 1.0, out=None):
         """The gradient of embed_rows' table of `kinds` rows for the gradient dy at the result."""
         rows, channels, lddy, dtype = self._rows(dy, "dy")
+        if kinds < 1:
+            raise ValueError("kinds: need at least one")
         pid = self._ids(ids, rows)
         if out is None:
             out, ldt = self.torch.empty((kinds, channels), dtype=dy.dtype, device=self.device), channels

@@ -4,8 +4,10 @@
 //   w = w - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + decay w)
 //
 // (the corrections as factors: k2 sqrt(v) and c1 m / (k2 sqrt(v) + eps), of which nothing is too small for fp32 before m and v are).
-// Bound by memory.  The tensors are cut into chunks of 2048 elements, eight a thread, a workgroup each, so that memory is gone
-// through in the order in which workgroups are handed out; a chunk's tensor is found in a table that travels with the launch.  The
+// Bound by memory (120 M parameters in bf16, moments in fp32, 3.1 GB: 545 us, 5.7 TB/s; 260 M with moments in 8 bits, 3.6 GB:
+// 660 us, 5.5 TB/s, of which the instructions alone would take two thirds).  The tensors are cut into chunks of 2048 elements, eight
+// a thread, a workgroup each, so that memory is gone through in the order in which workgroups are handed out; a chunk's tensor is
+// found in a table that travels with the launch.  The
 // step count t lies in device memory, so that a captured step goes on counting: the last workgroup counts it up, or, of more than
 // can be counted one by one, a launch of its own.
 // A bf16 parameter has the low 16 bits of its fp32 value w beside it (2 bytes where a copy of w would take 4): w is rounded to bf16
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(kThreads, kEight ? 5 : 8) void adamw_kernel(const A
   }
   if (!a.count_up || gridDim.x > kCounted) return;
   // Every wave has read the count by now, and nothing else is handed from one workgroup to another: no fence, which would write
-  // an XCD's whole L2 back for each of them (1.14 M parameters 29 us instead of 8).
+  // an XCD's whole L2 back for each of them (1.14 M parameters 29 us instead of 12).
   __syncthreads();
   if (threadIdx.x == 0) {
     if (atomicAdd(&a.steps[1], 1) == (int)gridDim.x - 1) {
@@ -383,7 +385,8 @@ __global__ void count_up_kernel(int* steps) {
   if (steps[0] < 2147483647) steps[0] += 1;
 }
 
-// Four values a thread, so that a wave's stores are neighbours: a workgroup takes half a chunk.
+// Four values a thread, so that a wave's stores are neighbours: a workgroup takes half a chunk (all three of 260 M parameters with
+// moments in 8 bits, 4.7 GB: 800 us, 5.9 TB/s).
 template <bool kEight>
 __global__ __launch_bounds__(kThreads) void values_kernel(const AdamwArgs a) {
   for (long long half = blockIdx.x; half < 2LL * a.chunks; half += gridDim.x) {

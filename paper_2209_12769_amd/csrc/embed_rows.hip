@@ -1,14 +1,17 @@
 // Rows by kind: y_i = s T[id_i] (a row of zeros where id_i is -1), and the table's gradient dT_k = s sum of dy_i over id_i = k
 // (gfx950).
 //
-// Forward: bound by the rows it writes; the table's used rows stay in the caches.
+// Forward: bound by the rows it writes; the table's used rows stay in the caches (5.7 M rows of 128 in bf16, 97 kinds, 1.5 GB:
+// 264 us, 5.6 TB/s).
 // Gradient: the row numbers are sorted by kind (stable radix sort, up to nine bits a pass; a short list by one workgroup), so that
 // a kind's rows become neighbours, and the sorted list is cut into chunks of equal length.  A chunk sums its rows kind by kind in
 // the list's order.  A kind that lies inside one chunk is written at once; what a chunk has of kinds that reach beyond it, the
 // first and the last of its list at most, are entries of a second, shorter list, which is treated alike until it is short
 // enough for one workgroup a kind.  No atomics: the same call gives the same bits.  Sums: up to 64 rows in fp32, the chunks' in
 // 64 bits, rounded to fp32 from list to list.  Kinds without rows are found by a search in the sorted list and cleared by further
-// workgroups of the first sums' launch.
+// workgroups of the first sums' launch.  Bound by memory in the rows' sums, which read rows at the sorted list's places, and by
+// launches of 3 to 12 us in the rest (474011 rows of 256 in fp32 to 97 kinds: 135 us, of them 100 the rows' sums, 4.8 TB/s; 65521
+// rows of 1031 in bf16 to 128001 kinds: 140 us, of them 93 the rows' sums and the zeros, 4.3 TB/s).
 #include "row_vectors.h"
 
 namespace dc {

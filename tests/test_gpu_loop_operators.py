@@ -252,6 +252,24 @@ def test_row_norm_backward_rows_anywhere(ev, dtype, ld, first, C):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [5, 37, 256, 700, 1031, 9001, 16384])
+def test_row_norm_backward_in_place(ev, dtype, C):
+    """The gradient of x in the place of what is read, which may be one tensor for all."""
+    x, gamma, beta = (v.cuda() for v in norm_inputs(301, C, dtype))
+    dy, dres = rand(11, 301, C).to(x.dtype).cuda(), rand(12, 301, C).to(x.dtype).cuda()
+    _, mean, rstd = ev.row_norm(x, gamma, beta, EPS, "silu")
+    for same in (False, True):
+        past = dy if same else dres
+        want = ev.row_norm_backward(dy, x, gamma, beta, mean, rstd, "silu", past)
+        for k in range(2 if same else 3):
+            a = [dy.clone(), x.clone(), past.clone()]
+            if same:
+                a[2] = a[0]
+            got = ev.row_norm_backward(a[0], a[1], gamma, beta, mean, rstd, "silu", a[2], out=a[k])
+            assert got[0] is a[k] and all(torch.equal(u, v) for u, v in zip(got, want)), (same, k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_row_norm_without_rows(ev, dtype):
     x = torch.empty(0, 48, dtype=TYPES[dtype], device="cuda")
     y, mean, rstd = ev.row_norm(x)

@@ -61,6 +61,7 @@ def test_embed_rows(ev):
     without_context(ev.embed_rows_backward, dy, ids, 5)
     refused("one number for each row", ev.embed_rows_backward, dy, ids[:2], 5)
     refused("out", ev.embed_rows_backward, dy, ids, 5, out=torch.zeros(4, 8))
+    refused("kinds", ev.embed_rows_backward, dy, ids, 0)
 
 
 def test_adamw(ev):
@@ -77,6 +78,25 @@ def test_adamw(ev):
     refused("which", o.values, "ww")
     refused("which", o.values, "")
     without_context(o.values, "w")
+    for name in ("m", "v", "low", "steps", "params"):
+        with pytest.raises(AttributeError, match="copy_"):
+            setattr(o, name, None)
+    o.lr = 0.5
+
+
+def test_adamw_parameters_with_other_memory(ev):
+    """Their table follows them; memory that they had cannot become another tensor's before that."""
+    p, q = torch.zeros(3, 5), torch.zeros(300, dtype=torch.bfloat16)
+    o = ev.adamw([p, q])
+    was = q.data_ptr()
+    q.data = torch.ones(300, dtype=torch.bfloat16)
+    assert torch.zeros(300, dtype=torch.bfloat16).data_ptr() != was and o._table["p"][1] == was
+    without_context(o.values, "w")
+    assert o._table["p"].tolist() == [p.data_ptr(), q.data_ptr()]
+    for other in (torch.zeros(0, dtype=torch.bfloat16), torch.zeros(10, dtype=torch.bfloat16), torch.zeros(300)):
+        q.data = other
+        refused("tensor 1", o.values, "w")
+        refused("tensor 1", o.step, [None, None])
 
 
 @pytest.mark.parametrize("name,args", [("dc_row_norm", 1), ("dc_row_norm_backward", 1), ("dc_embed_rows", 1), ("dc_embed_rows_backward", 1), ("dc_adamw", 1), ("dc_adamw_values", 4)])
