@@ -8,6 +8,8 @@ the shared library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import itertools
+import operator
 import os
 import struct
 from dataclasses import dataclass
@@ -541,7 +543,7 @@ class AdamW:
         self._shapes, self._dtypes = [p.shape for p in self.params], [p.dtype for p in self.params]
         # what the table holds of the tensors' places and the gradients' types, as lists; `_held` keeps that memory theirs, so that a
         # place that is still the same needs no further look
-        self._ptrs, self._codes = [p.data_ptr() for p in self.params], [0] * len(self.params)
+        self._ptrs, self._g_dtypes = [p.data_ptr() for p in self.params], None
         self._held = [p.detach() for p in self.params]
         eight = states == "8bit"
         with torch.no_grad():
@@ -557,7 +559,7 @@ class AdamW:
             raise ValueError(f"tensor {k}: need contiguous float32 or bfloat16 on {self.ev.device}")
 
     def _args(self, grad_scale: int) -> bytes:
-        ptrs = [p.data_ptr() for p in self.params]
+        ptrs = list(map(self.ev.torch.Tensor.data_ptr, self.params))
         if ptrs != self._ptrs:                             # tensors whose owner gave them other memory
             for k, p in enumerate(self.params):
                 self._check(k, p)
@@ -571,23 +573,26 @@ class AdamW:
     def step(self, grads, grad_scale=None):
         """One step with a gradient for every tensor (float32 or bfloat16, contiguous, its shape), None for tensors that stay as
         they are.  grad_scale: a float32 device tensor of one number that the gradients are multiplied by."""
-        ev, types, index = self.ev, self.ev._types, self.ev.device.index
+        ev, T = self.ev, self.ev.torch.Tensor
         if len(grads) != len(self.params):
             raise ValueError(f"need {len(self.params)} gradients, not {len(grads)}")
-        ptrs, codes = [], []
-        for g, shape in zip(grads, self._shapes):
-            if g is None:
-                ptrs.append(0)
-                codes.append(0)
-                continue
-            code = types.get(g.dtype)
-            if code is None or g.shape != shape or g.get_device() != index or not g.is_contiguous():
-                raise ValueError(f"gradient {len(ptrs)}: need contiguous float32 or bfloat16 {tuple(shape)} on {ev.device}")
-            ptrs.append(g.data_ptr())
-            codes.append(code)
-        self._table["g"] = ptrs
-        if codes != self._codes:
-            self._table["g_dtype"] = self._codes = codes
+        which, have, shapes = slice(None), grads, self._shapes
+        if any(map(operator.is_, grads, itertools.repeat(None))):
+            which = [k for k, g in enumerate(grads) if g is not None]
+            have, shapes = [grads[k] for k in which], [shapes[k] for k in which]
+            self._table["g"] = 0
+        # A small step is bound by what happens here: one look at all of them after the other takes a quarter less than all at one.
+        dtypes = list(map(T.dtype.__get__, have))
+        if (not ev._types.keys() >= set(dtypes) or list(map(T.shape.__get__, have)) != shapes
+                or list(map(T.get_device, have)).count(ev.device.index) != len(have)
+                or not all(map(T.is_contiguous, have))):
+            for k, (g, shape) in enumerate(zip(grads, self._shapes)):
+                if g is not None and (g.dtype not in ev._types or g.shape != shape or g.device != ev.device or not g.is_contiguous()):
+                    raise ValueError(f"gradient {k}: need contiguous float32 or bfloat16 {tuple(shape)} on {ev.device}")
+        self._table["g"][which] = list(map(T.data_ptr, have))
+        if dtypes != self._g_dtypes or have is not grads:
+            self._table["g_dtype"][which] = [ev._types[t] for t in dtypes]
+            self._g_dtypes = dtypes if have is grads else None
         st = lib().dc_adamw(ev.ctx, self._args(0 if grad_scale is None else ev._vector(grad_scale.reshape(-1), "grad_scale", 1)), ev._raw_stream())
         if st:
             ev._ok(st, "dc_adamw")

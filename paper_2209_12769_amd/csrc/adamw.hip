@@ -5,11 +5,11 @@
 //
 // (the corrections as factors: k2 sqrt(v) and c1 m / (k2 sqrt(v) + eps), of which nothing is too small for fp32 before m and v are).
 // Bound by memory (120 M parameters in bf16, moments in fp32, 3.1 GB: 545 us, 5.7 TB/s; 260 M with moments in 8 bits, 3.6 GB:
-// 660 us, 5.5 TB/s, of which the instructions alone would take two thirds).  The tensors are cut into chunks of 2048 elements, eight
-// a thread, a workgroup each, so that memory is gone through in the order in which workgroups are handed out; a chunk's tensor is
-// found in a table that travels with the launch.  The
-// step count t lies in device memory, so that a captured step goes on counting: the last workgroup counts it up, or, of more than
-// can be counted one by one, a launch of its own.
+// 660 us, 5.5 TB/s, of which vector instructions are issued for 510).  The tensors are cut into chunks of 2048 elements, eight a
+// thread, a workgroup each, so that memory is gone through in the order in which workgroups are handed out; a chunk's tensor is
+// found in a table that travels with the launch.  The step count t lies in device memory, so that a captured step goes on counting: in
+// a small call the last workgroup counts it up, otherwise a launch of its own (2.5 us of the host's time, which a small call is bound
+// by; one by one would be 9 us of 500 workgroups).
 // A bf16 parameter has the low 16 bits of its fp32 value w beside it (2 bytes where a copy of w would take 4): w is rounded to bf16
 // with halves away from zero, so a low half of 0x8000 or more says that the bf16 number is one step above w's upper half, and the
 // two are w itself.
@@ -30,7 +30,8 @@ typedef unsigned long long u64;
 
 constexpr int kPer = 8, kThreads = 256, kChunk = kPer * kThreads;
 constexpr u64 kDraw = 0xD1342543DE82EF95ULL;    // from one draw to the next
-constexpr unsigned kCounted = 2048;            // workgroups that are counted one by one
+constexpr int kCounted = 2048;                 // chunks of a small call
+constexpr int kSmall = 4;                      // and of its workgroups
 constexpr int kExponentNan = 255;              // of a block of moments that holds a number that is not finite
 
 __host__ __device__ __forceinline__ u64 mix(u64 z) {
@@ -240,12 +241,13 @@ struct Step {
   u64 key;
 };
 
-// A chunk's step.  kAll: of kChunk elements.  `first`: the workgroup's first one, its requests go out before `step` is there.
-template <bool kEight, bool kAll>
-__device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const Step& step, bool first) {
+// A chunk's step.  kAll: of kChunk elements.  `first`: the workgroup's first one, its requests go out before `step` is there; then
+// counted() is called.
+template <bool kEight, bool kAll, typename F>
+__device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const Step& step, bool first, F counted) {
   // the 8-bit codes are those of operations in fp32 rounded one by one
 #pragma clang fp contract(off)
-  const unsigned i = threadIdx.x * kPer;
+  const unsigned i = threadIdx.x % kThreads * kPer;
   const int left = kAll ? kPer : min(max(c.n - (int)i, 0), kPer);
   const bool there = kAll || (kEight ? (int)(i & ~(unsigned)(kMomentBlock - 1)) < c.n : left > 0);
   unsigned char* const m8 = static_cast<unsigned char*>(a.m) + c.at;
@@ -272,7 +274,10 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const
       rv = request<true>(reinterpret_cast<const char*>(v32), i, kPer, false);
     }
   }
-  if (first) __syncthreads();
+  if (first) {
+    __syncthreads();
+    counted();
+  }
   if (!there) return;
   u64 r[kPer / 2];
   if constexpr (kEight) {      // the draws, while the requests are under way: kept in front of what waits for them
@@ -351,8 +356,9 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Chunk& c, const
   }
 }
 
-template <bool kEight>
-__global__ __launch_bounds__(kThreads, kEight ? 5 : 8) void adamw_kernel(const AdamwArgs a) {
+// kMany: chunks of a workgroup side by side.  One, or four in small calls, which count the step up themselves.
+template <bool kEight, int kMany>
+__global__ __launch_bounds__(kThreads * kMany, kMany > 1 ? 4 : (kEight ? 5 : 8)) void adamw_kernel(const AdamwArgs a) {
   __shared__ Step step;
   const int before = a.steps[0], t = before < 2147483647 ? before + 1 : before;
   if (threadIdx.x < 64) {
@@ -364,20 +370,23 @@ __global__ __launch_bounds__(kThreads, kEight ? 5 : 8) void adamw_kernel(const A
     s.key = mix(a.seed ^ mix((u64)t));
     if (threadIdx.x == 0) step = s;
   }
-  for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-    const Chunk c = chunk_of(a, chunk);
-    if (c.n == kChunk) update<kEight, true>(a, c, step, chunk == (int)blockIdx.x);
-    else update<kEight, false>(a, c, step, chunk == (int)blockIdx.x);
-  }
-  if (!a.count_up || gridDim.x > kCounted) return;
-  // Every wave has read the count by now, and nothing else is handed from one workgroup to another: no fence, which would write
-  // an XCD's whole L2 back for each of them (1.14 M parameters 29 us instead of 12).
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    if (atomicAdd(&a.steps[1], 1) == (int)gridDim.x - 1) {
-      a.steps[1] = 0;
-      a.steps[0] = t;
+  if constexpr (kMany == 1) {
+    for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+      const Chunk c = chunk_of(a, chunk);
+      if (c.n == kChunk) update<kEight, true>(a, c, step, chunk == (int)blockIdx.x, []() {});
+      else update<kEight, false>(a, c, step, chunk == (int)blockIdx.x, []() {});
     }
+  } else {
+    // The last workgroup counts the step up.  Thread 0 counts its own once it has read the count of steps, and no other thread uses what
+    // it read; nothing else is handed from one workgroup to another: no fence, which would write an XCD's whole L2 back for each of
+    // them.  Additions to one place take 9 to 18 ns each, one after the other: hence four chunks each, and they are requested behind the
+    // elements and waited for at the end (1.14 M parameters: 13.0 us by a chunk each and counted at the end, 9.1 so, 29 with a fence).
+    unsigned before_it = 0;
+    const int part = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    update<kEight, false>(a, chunk_of(a, (int)blockIdx.x * kMany + part), step, true, [&]() {
+      if (a.count_up && threadIdx.x == 0) before_it = atomicInc(reinterpret_cast<unsigned*>(&a.steps[1]), gridDim.x - 1);
+    });
+    if (a.count_up && threadIdx.x == 0 && before_it == gridDim.x - 1) a.steps[0] = t;       // its addition made the other 0 again
   }
 }
 
@@ -450,9 +459,17 @@ long long adamw_chunks(long long n) { return (n + kChunk - 1) / kChunk; }
 
 hipError_t launch_adamw(const AdamwArgs& a, bool eight, hipStream_t s) {
   static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
-  if (eight) hipLaunchKernelGGL((adamw_kernel<true>), dim3(blocks_of(a.chunks)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((adamw_kernel<false>), dim3(blocks_of(a.chunks)), dim3(kThreads), 0, s, a);
-  if (a.count_up && blocks_of(a.chunks) > kCounted) hipLaunchKernelGGL(count_up_kernel, dim3(1), dim3(1), 0, s, a.steps);
+  if (a.chunks > 0 && a.chunks <= kCounted) {
+    const dim3 grid(blocks_of((a.chunks + kSmall - 1) / kSmall));
+    if (eight) hipLaunchKernelGGL((adamw_kernel<true, kSmall>), grid, dim3(kThreads * kSmall), 0, s, a);
+    else hipLaunchKernelGGL((adamw_kernel<false, kSmall>), grid, dim3(kThreads * kSmall), 0, s, a);
+    return hipGetLastError();
+  }
+  if (a.chunks > 0) {
+    if (eight) hipLaunchKernelGGL((adamw_kernel<true, 1>), dim3(blocks_of(a.chunks)), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((adamw_kernel<false, 1>), dim3(blocks_of(a.chunks)), dim3(kThreads), 0, s, a);
+  }
+  if (a.count_up) hipLaunchKernelGGL(count_up_kernel, dim3(1), dim3(1), 0, s, a.steps);
   return hipGetLastError();
 }
 hipError_t launch_adamw_values(const AdamwArgs& a, bool eight, hipStream_t s) {

@@ -2065,6 +2065,7 @@ dc_status adamw_call(dc_ctx* ctx, const dc_adamw_args* a, bool step, float* cons
   }
   int64_t end = 0;
   bool any16 = false;
+  spans.reserve(2 * (size_t)a->n_tensors + 10);
   for (int32_t i = 0; i < a->n_tensors; ++i) {
     const dc_adamw_tensor& t = a->tensors[i];
     if (t.n < 0 || t.at < end || t.at % kMomentBlock || t.n > a->total - t.at)

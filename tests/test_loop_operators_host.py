@@ -122,3 +122,19 @@ def test_structs_have_the_header_s_layout(tmp_path):
     for line, c in zip(got, structs.values()):
         assert list(map(int, line.split())) == [ctypes.sizeof(c)] + [getattr(c, f[0]).offset for f in c._fields_]
     assert np.dtype(B._ADAMW_TENSOR).itemsize == ctypes.sizeof(B.DcAdamwTensor)
+
+
+def test_adamw_looks_at_every_gradient(ev):
+    """What the table holds of gradients, some of them missing, of types that change from step to step."""
+    ps = [torch.zeros(3, 5), torch.zeros(7), torch.zeros(0), torch.zeros(300, dtype=torch.bfloat16)]
+    o = ev.adamw(ps)
+    good = [torch.zeros_like(p) for p in ps]
+    half = [g.bfloat16() for g in good]
+    for grads in (good, [None, good[1], None, good[3]], half, good, [half[0], None, half[2], None], [None] * 4, tuple(half), good):
+        without_context(o.step, grads)
+        assert o._table["g"].tolist() == [0 if g is None else g.data_ptr() for g in grads]
+        assert all(g is None or code == (g.dtype == torch.bfloat16) for g, code in zip(grads, o._table["g_dtype"].tolist()))
+    for k, bad in [(0, torch.zeros(5, 3)), (0, torch.zeros(5, 3).t()), (1, torch.zeros(7).double()), (1, torch.zeros(1).expand(7)), (3, torch.zeros(299)),
+                   (2, torch.zeros(1))]:
+        for rest in (good, [None] * 4):
+            refused(f"gradient {k}", o.step, [bad if i == k else g for i, g in enumerate(rest)])
