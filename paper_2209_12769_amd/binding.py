@@ -998,10 +998,10 @@ class Evaluator:
         pg = 0 if gamma is None else self._vector(gamma, "gamma", channels)
         pb = 0 if beta is None else self._vector(beta, "beta", channels)
         if out is None:
-            out, ldy = self.torch.empty((rows, channels), dtype=x.dtype, device=self.device), channels
+            out, ldy = x.new_empty(rows, channels), channels
         else:
             ldy = self._like(out, "out", rows, channels, dtype)
-        mean, rstd = self.torch.empty((2, rows), dtype=self.torch.float32, device=self.device).unbind(0)
+        mean, rstd = x.new_empty(rows, dtype=self.torch.float32), x.new_empty(rows, dtype=self.torch.float32)
         a = _ROW_NORM.pack(dtype, self._act(act), rows, channels, eps, x.data_ptr(), ldx, pg, pb, mean.data_ptr(), rstd.data_ptr(),
                            out.data_ptr(), ldy, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
         st = lib().dc_row_norm(self.ctx, a, self._raw_stream())
@@ -1047,7 +1047,7 @@ class Evaluator:
         kinds, channels, ldt, dtype = self._rows(table, "table")
         pid, rows = self._ids(ids), ids.shape[0]
         if out is None:
-            out, ldy = self.torch.empty((rows, channels), dtype=table.dtype, device=self.device), channels
+            out, ldy = table.new_empty(rows, channels), channels
         else:
             ldy = self._like(out, "out", rows, channels, dtype)
         a = _EMBED.pack(dtype, rows, kinds, channels, scale, pid, table.data_ptr(), ldt, out.data_ptr(), ldy, 0, 0, 0, 0, 0, 0)
