@@ -7,11 +7,11 @@
 // a kind's rows become neighbours, and the sorted list is cut into chunks of equal length.  A chunk sums its rows kind by kind in
 // the list's order.  A kind that lies inside one chunk is written at once; what a chunk has of kinds that reach beyond it, the
 // first and the last of its list at most, are entries of a second, shorter list, which is treated alike until it is short
-// enough for one workgroup a kind.  No atomics: the same call gives the same bits.  Sums: up to 64 rows in fp32, the chunks' in
-// 64 bits, rounded to fp32 from list to list.  Kinds without rows are found by a search in the sorted list and cleared by further
-// workgroups of the first sums' launch.  Bound by memory in the rows' sums, which read rows at the sorted list's places, and by
-// launches of 3 to 12 us in the rest (474011 rows of 256 in fp32 to 97 kinds: 135 us, of them 100 the rows' sums, 4.8 TB/s; 65521
-// rows of 1031 in bf16 to 128001 kinds: 140 us, of them 93 the rows' sums and the zeros, 4.3 TB/s).
+// enough for one workgroup a kind.  No atomics: the same call gives the same bits.  Sums: up to 64 rows in fp32, up to four such runs
+// in fp32, the chunks' in 64 bits, rounded to fp32 from list to list.  The table is cleared by the sort's launches, kinds that have
+// rows are written after that.  Bound by memory in the rows' sums, which read rows at the sorted list's places, and by launches in
+// the rest (474011 rows of 256 in fp32 to 97 kinds: 120 us, of them 89 the rows' sums, 5.4 TB/s; 65521 rows of 1031 in bf16 to
+// 128001 kinds: 126 us, of them 52 the sort and the zeros, 56 the rows' sums).
 #include "row_vectors.h"
 
 namespace dc {
@@ -72,6 +72,7 @@ __global__ __launch_bounds__(1024) void embed_kernel(const EmbedArgs a, int used
 }
 
 // ---- sort ----
+constexpr int kRun = 64;       // rows that are summed in fp32 before they join the others of their chunk
 constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64;
 constexpr int kBits = 9, kBins = 1 << kBits;
 
@@ -100,10 +101,62 @@ __device__ __forceinline__ void in_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// ---- zeros ----
+// The launches of the sort wait for memory most of the time.  They clear the table besides, a part of it each, by further workgroups
+// (65521 rows of 1031 in bf16 to 128001 kinds, half of them without a row: the call 136 us, and 144 where the sums' launch looks for
+// those and clears no others; 3000 rows of 1024 to 250000 kinds 99 and 120; 65536 rows of 1024, one of each kind, 99 and 90).
+struct Zeros {
+  u16* table;                  // in halves of a word: rows of `width`, the last of `last`, `stride` from one to the next
+  long long stride, rows;
+  int width, last;
+};
+struct Part {
+  Zeros z;
+  long long from, to;          // rows
+  int blocks;
+};
+constexpr int kClear = 8192;   // halves of a word that a wave clears
+// A row by one wave, on 16-byte boundaries but for its first and last vector.
+__device__ __forceinline__ void clear_row(u16* row, int n) {
+  const int lane = threadIdx.x & 63;
+  const u32x4 zero = {0, 0, 0, 0};
+  if (n < 8) {
+    if (lane < n) row[lane] = 0;
+    return;
+  }
+  const int skip = (int)(-(reinterpret_cast<size_t>(row) / 2) & 7), whole = (n - skip) / 8;
+  u32x4* to = reinterpret_cast<u32x4*>(row + skip);
+  for (int at = lane; at < whole; at += 64) to[at] = zero;
+  if (lane == 0 && skip != 0) *reinterpret_cast<u32x4_any*>(row) = zero;
+  if (lane == 1 && skip + whole * 8 < n) *reinterpret_cast<u32x4_any*>(row + (n - 8)) = zero;
+}
+__device__ __forceinline__ void clear(const Part& p, int block) {
+  const int waves = (int)blockDim.x >> 6;
+  for (long long k = p.from + (long long)block * waves + ((int)threadIdx.x >> 6); k < p.to; k += (long long)p.blocks * waves)
+    clear_row(p.z.table + k * p.z.stride, k == p.z.rows - 1 ? p.z.last : p.z.width);
+}
+// The table as one long row, cut, or its rows one by one.
+Zeros zeros_of(const EmbedArgs& a) {
+  const int halves = a.bf16 ? 1 : 2, width = a.C * halves;
+  const long long stride = a.lddt * halves, all = (long long)a.kinds * width;
+  u16* table = static_cast<u16*>(a.dtable);
+  if (stride != width && a.kinds > 1) return Zeros{table, stride, a.kinds, width, width};
+  const long long rows = (all + kClear - 1) / kClear;
+  return Zeros{table, kClear, rows, kClear, (int)(all - (rows - 1) * kClear)};
+}
+// Part k of n; workgroups of `waves`.
+Part part_of(const Zeros& z, int k, int n, int waves) {
+  Part p{z, z.rows * k / n, z.rows * (k + 1) / n, 0};
+  const long long each = (long long)waves * (z.width < kClear ? kClear / z.width : 1), need = (p.to - p.from + each - 1) / each;
+  p.blocks = (int)(need < 1 << 20 ? need : 1 << 20);
+  return p;
+}
+
 // How many pairs of each tile have each digit: count[digit][tile].
 template <int kPer>
-__global__ __launch_bounds__(kSortThreads) void count_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, int* count) {
+__global__ __launch_bounds__(kSortThreads) void count_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, int* count, Part zeros) {
   __shared__ int bin[kBins];
+  if ((int)blockIdx.x >= tiles) return clear(zeros, blockIdx.x - tiles);
   const int bins = 1 << bits, n = (int)a.rows, tile = blockIdx.x;
   for (int i = threadIdx.x; i < bins; i += kSortThreads) bin[i] = 0;
   __syncthreads();
@@ -141,8 +194,9 @@ __device__ __forceinline__ int scan256(int x, int* part, int& all) {
 }
 
 // A digit's counts become the number of its pairs in the tiles in front; total[digit].
-__global__ __launch_bounds__(256) void scan_kernel(int* count, int tiles, int* total) {
+__global__ __launch_bounds__(256) void scan_kernel(int* count, int bins, int tiles, int* total, Part zeros) {
   __shared__ int part[4];
+  if ((int)blockIdx.x >= bins) return clear(zeros, blockIdx.x - bins);
   int* c = count + (size_t)blockIdx.x * tiles;
   int before = 0;
   for (int i0 = 0; i0 < tiles; i0 += 256) {
@@ -158,10 +212,11 @@ __global__ __launch_bounds__(256) void scan_kernel(int* count, int tiles, int* t
 // Every pair to its place: its digit's first place, the tiles in front, the pairs of the tile in front.
 template <int kPer>
 __global__ __launch_bounds__(kSortThreads) void scatter_kernel(const EmbedArgs a, const Pair* in, int shift, int bits, int tiles, const int* count,
-                                                               const int* total, Pair* out) {
+                                                               const int* total, Pair* out, Part zeros) {
   __shared__ int first[kBins];
   __shared__ int next[kSortWaves][kBins];
   __shared__ int part[4];
+  if ((int)blockIdx.x >= tiles) return clear(zeros, blockIdx.x - tiles);
   const int bins = 1 << bits, n = (int)a.rows, tile = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int before = 0;
   for (int d0 = 0; d0 < bins; d0 += 256) {
@@ -214,10 +269,11 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(const EmbedArgs a
 
 // The whole sort of a list of up to kSmall pairs by one workgroup, in LDS: the same passes, of up to kSmallBits bits.
 constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kSmallPer = 4, kSmall = kSmallThreads * kSmallPer, kSmallBits = 8, kSmallBins = 1 << kSmallBits;
-__global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(const EmbedArgs a, int bits, Pair* out) {
+__global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(const EmbedArgs a, int bits, Pair* out, Part zeros) {
   __shared__ Pair list[kSmall];
   __shared__ int next[kSmallWaves][kSmallBins];
   __shared__ int part[4];
+  if (blockIdx.x > 0) return clear(zeros, blockIdx.x - 1);
   const int n = (int)a.rows, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, base = wave * 64 * kSmallPer + lane;
   Pair p[kSmallPer];
 #pragma unroll
@@ -280,7 +336,6 @@ struct Sums {
   const int* in_kind;          // [n]: the kind, or ~kind of an entry without a sum
   float* out;                  // [2 nchunk][C]
   int* out_kind;
-  int fill_blocks;             // first level: workgroups that clear the kinds without rows
 };
 
 template <typename T>
@@ -347,98 +402,65 @@ __device__ __forceinline__ int column_of(int at, int C) {
   return c < C ? max(min(c, C - kV), 0) : -1;
 }
 
-// The first pair of the sorted list with that kind or a larger one: the wave looks at 64 places at a time (three steps for 200000
-// pairs, where halving waits for memory 17 times).
-__device__ __forceinline__ int first_of(const Pair* sorted, int n, long long kind) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, count = n;       // it is one of lo .. lo + count
-  while (count > 0) {
-    const int stride = (count + 63) >> 6, at = lane * stride;
-    const bool below = at < count && sorted[lo + at].kind < kind;
-    const int steps = __popcll(__ballot(below));       // a pair that is below has all in front of it below
-    if (steps == 0) return lo;
-    lo += (steps - 1) * stride + 1;
-    count = min(stride - 1, count - (steps - 1) * stride - 1);
-  }
-  return lo;
-}
-// Zeros by one wave, on 16-byte boundaries but for the row's first and last vector.
-template <typename T>
-__device__ __forceinline__ void clear_row(T* row, int C) {
-  const int lane = threadIdx.x & 63;
-  const u32x4 zero = {0, 0, 0, 0};
-  if (C < kVector<T>) {
-    if (lane < C) row[lane] = 0;
-    return;
-  }
-  const int skip = (int)(-(reinterpret_cast<size_t>(row) / sizeof(T)) & (kVector<T> - 1)), whole = (C - skip) / kVector<T>;
-  u32x4* to = reinterpret_cast<u32x4*>(row + skip);
-  for (int at = lane; at < whole; at += 64) to[at] = zero;
-  if (lane == 0 && skip != 0) *reinterpret_cast<u32x4_any*>(row) = zero;
-  if (lane == 1 && skip + whole * kVector<T> < C) *reinterpret_cast<u32x4_any*>(row + (C - kVector<T>)) = zero;
-}
-// Clears the kinds that have no row: 64 kinds a workgroup, its waves take them in turn.
-constexpr int kClear = 64;
-template <typename T>
-__device__ void clear_unused(const Sums& s, int block) {
-  const EmbedArgs& a = s.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (long long k0 = (long long)block * kClear; k0 < a.kinds; k0 += (long long)s.fill_blocks * kClear) {
-    const long long kind = k0 + lane;
-    int lo = first_of(s.sorted, s.n, k0), hi = first_of(s.sorted, s.n, k0 + kClear);
-    const int end = hi;
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      if (s.sorted[mid].kind < kind) lo = mid + 1;
-      else hi = mid;
-    }
-    const bool none = kind < a.kinds && (lo >= end || s.sorted[lo].kind != kind);
-    int turn = 0;
-    for (u64 left = __ballot(none); left; left &= left - 1, ++turn)
-      if (turn % 4 == wave) clear_row<T>(static_cast<T*>(a.dtable) + (k0 + __builtin_ctzll(left)) * a.lddt, a.C);
+// A pair of the sorted list.  kWave: the same for all lanes, by a scalar load, so that what follows from it takes no vector registers.
+template <bool kWave>
+__device__ __forceinline__ Pair sorted_at(const Sums& s, int i) {
+  if constexpr (kWave) {
+    const u64 w = ((const __attribute__((address_space(4))) u64*)reinterpret_cast<size_t>(s.sorted))[i];
+    return Pair{(int)w, (int)(w >> 32)};
+  } else {
+    return s.sorted[i];
   }
 }
-
-// First level: chunks of the sorted rows, of up to 64 of them: one sum in fp32 a kind.
-template <typename T>
+// First level: chunks of the sorted rows.  kWave: a wave each, of rows or slabs of more than 32 vectors.
+template <typename T, bool kWave>
 __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
-  constexpr int kV = kVector<T>, kAhead = 8;
+  constexpr int kV = kVector<T>, kAhead = kWave ? 8 : 4;
   const EmbedArgs& a = s.a;
-  if ((int)blockIdx.x < s.fill_blocks) return clear_unused<T>(s, blockIdx.x);
-  const int block = blockIdx.x - s.fill_blocks;
-  const int t = threadIdx.x & (s.lanes - 1), seats = 256 / s.lanes;
-  const long long item = (long long)block * seats + threadIdx.x / s.lanes;
+  const int lanes = kWave ? 64 : s.lanes, t = threadIdx.x & (lanes - 1), seat = threadIdx.x / lanes;
+  const long long item = (long long)blockIdx.x * (256 / lanes) + (kWave ? __builtin_amdgcn_readfirstlane(seat) : seat);
   if (item >= (long long)s.nchunk * s.nslab) return;
   Close close;
   close.chunk = (int)(item / s.nslab);
   const int c = t < s.used ? column_of<kV>((int)(item - (long long)close.chunk * s.nslab) * s.used + t, a.C) : -1;
   if (c < 0) return;
-  const long long p0l = (long long)close.chunk * s.chunk;
-  const int p0 = (int)p0l, p1 = (int)min(p0l + s.chunk, (long long)s.n), len = p1 - p0;
+  const int p0 = (int)((long long)close.chunk * s.chunk), p1 = (int)min((long long)p0 + s.chunk, (long long)s.n), len = p1 - p0;
   const T* dY = static_cast<const T*>(a.dY);
-  int kind = s.sorted[p0].kind;
-  close.from_before = p0 > 0 && s.sorted[p0 - 1].kind == kind;
-  const int past = p1 < s.n ? s.sorted[p1].kind : -1;
-  auto write = [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c, x); };
-  float sum[kV];
+  Pair e[kAhead];
 #pragma unroll
-  for (int k = 0; k < kV; ++k) sum[k] = 0.f;
+  for (int u = 0; u < kAhead; ++u) e[u] = sorted_at<kWave>(s, p0 + min(u, len - 1));
+  int kind = e[0].kind;
+  close.from_before = p0 > 0 && sorted_at<kWave>(s, max(p0 - 1, 0)).kind == kind;
+  const int past = p1 < s.n ? sorted_at<kWave>(s, min(p1, s.n - 1)).kind : -1;
+  auto write = [&](int of, const float (&x)[kV]) { write_kind<T>(a, of, c, x); };
+  float sum[kV], runs[kV];     // of up to kRun rows; of the kind's runs
+#pragma unroll
+  for (int k = 0; k < kV; ++k) sum[k] = runs[k] = 0.f;
+  auto join = [&]() {
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      runs[k] += sum[k];
+      sum[k] = 0.f;
+    }
+  };
   bool first = true;
   for (int q = 0; q < len; q += kAhead) {
-    Pair e[kAhead];
+    if (e[0].kind >= a.kinds) break;                     // only rows that stand for nothing are left
     u32x4 v[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) e[u] = s.sorted[p0 + min(q + u, len - 1)];
-    if (e[0].kind >= a.kinds) break;                     // only rows that stand for nothing are left
-#pragma unroll
     for (int u = 0; u < kAhead; ++u) v[u] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c, a.C);
+    Pair next[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) next[u] = sorted_at<kWave>(s, p0 + min(q + kAhead + u, len - 1));
+    if (q > 0 && q % kRun == 0) join();
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (q + u >= len || e[u].kind >= a.kinds) break;
       if (e[u].kind != kind) {
-        close_kind(s, close, kind, c, sum, true, first, false, write);
+        join();
+        close_kind(s, close, kind, c, runs, true, first, false, write);
 #pragma unroll
-        for (int k = 0; k < kV; ++k) sum[k] = 0.f;
+        for (int k = 0; k < kV; ++k) runs[k] = 0.f;
         first = false;
         kind = e[u].kind;
       }
@@ -447,9 +469,12 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
 #pragma unroll
       for (int k = 0; k < kV; ++k) sum[k] += x[k];
     }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) e[u] = next[u];
   }
+  join();
   close.goes_on = past == kind;
-  close_kind(s, close, kind, c, sum, kind < a.kinds, first, true, write);
+  close_kind(s, close, kind, c, runs, kind < a.kinds, first, true, write);
 }
 
 __device__ __forceinline__ int kind_of_entry(int k) { return k < 0 ? ~k : k; }
@@ -550,8 +575,8 @@ __global__ __launch_bounds__(64 * kLastWaves) void last_sums_kernel(const Sums s
   if (any) write_kind4(a, kind, c, x);
 }
 
-constexpr int kLastMost = 2048;        // entries that the last launch takes
-constexpr int kEntryChunk = 32;
+constexpr int kLastMost = 1024;        // entries that the last launch takes
+constexpr int kEntryChunk = 16;        // by 32, and 2048: 100000 rows of 1024 to 50000 kinds 112 us for 108, 1 M of 16 131 for 120
 
 int lanes_of(int vectors) {
   int l = 1;
@@ -579,9 +604,10 @@ Plan plan(long long rows, int kinds, int C, int bytes) {
   const int vectors = (C * bytes + 15) / 16;
   p.lanes = lanes_of(vectors);
   p.nslab = (vectors + p.lanes - 1) / p.lanes;
-  // eight thousand waves, but 16 to 64 rows a chunk
-  const long long seats = 8192LL * (64 / p.lanes), chunk = (rows * p.nslab + seats - 1) / seats;
-  p.chunk = (int)(chunk < 16 ? 16 : (chunk > 64 ? 64 : (chunk + 7) / 8 * 8));
+  // Two waves a SIMD, eight rows on their way each, but 16 to 256 rows a chunk (474011 rows of 256 in fp32 to 97 kinds, the whole call:
+  // 123 us by 2048 waves, 131 by 2560, 130 by 4096, 137 by 8192; 1024 make 65521 rows of 1031 in bf16 slower, 140 us for 127).
+  const long long seats = 2048LL * (64 / p.lanes), chunk = (rows * p.nslab + seats - 1) / seats;
+  p.chunk = (int)(chunk < 16 ? 16 : (chunk > 4 * kRun ? 4 * kRun : (chunk + 7) / 8 * 8));
   p.nchunk = (int)((rows + p.chunk - 1) / p.chunk);
   long long e = p.nchunk > 1 ? 2LL * p.nchunk : 0;           // of one chunk nothing is left to sum
   while (e > 0) {
@@ -628,15 +654,14 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
   m.lanes = p.lanes;
   m.nslab = p.nslab;
   m.used = ((a.C + kVector<T> - 1) / kVector<T> + p.nslab - 1) / p.nslab;
-  const long long fill = ((long long)a.kinds + kClear - 1) / kClear, fill_most = 1 << 20;
-  m.fill_blocks = (int)(fill < fill_most ? fill : fill_most);
   if (p.levels > 0) {
     m.out = reinterpret_cast<float*>(a.workspace + r.sum[0]);
     m.out_kind = reinterpret_cast<int*>(a.workspace + r.kind[0]);
   }
   const long long seats = 256 / p.lanes, items = (long long)p.nchunk * p.nslab;
-  const dim3 grid((unsigned)(m.fill_blocks + (items + seats - 1) / seats));
-  hipLaunchKernelGGL((sum_rows_kernel<T>), grid, dim3(256), 0, s, m);
+  const dim3 grid((unsigned)((items + seats - 1) / seats));
+  if (p.lanes == 64) hipLaunchKernelGGL((sum_rows_kernel<T, true>), grid, dim3(256), 0, s, m);
+  else hipLaunchKernelGGL((sum_rows_kernel<T, false>), grid, dim3(256), 0, s, m);
   // entries: four columns a thread
   const int fours = (a.C + 3) / 4;
   m.lanes = lanes_of(fours);
@@ -665,16 +690,24 @@ const Pair* sort(const EmbedArgs& a, const Plan& p, const Room& r, hipStream_t s
   int* count = reinterpret_cast<int*>(a.workspace + r.count);
   int* total = reinterpret_cast<int*>(a.workspace + r.total);
   if (p.tiles == 0) {
-    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSmallThreads), 0, s, a, p.all_bits, pair[0]);
+    const Part all = part_of(zeros_of(a), 0, 1, kSmallWaves);
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1 + all.blocks), dim3(kSmallThreads), 0, s, a, p.all_bits, pair[0], all);
     return pair[0];
   }
+  const Zeros zeros = zeros_of(a);
+  int launch = 0;
+  auto next = [&]() { return part_of(zeros, launch++, 3 * p.passes, kSortWaves); };
   const Pair* in = nullptr;
   for (int k = 0; k < p.passes; ++k) {
     const int shift = k * p.bits;
     Pair* out = pair[k & 1];
-    hipLaunchKernelGGL((count_kernel<kPer>), dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, count);
-    hipLaunchKernelGGL(scan_kernel, dim3(1 << p.bits), dim3(256), 0, s, count, p.tiles, total);
-    hipLaunchKernelGGL((scatter_kernel<kPer>), dim3(p.tiles), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, (const int*)count, (const int*)total, out);
+    Part z = next();
+    hipLaunchKernelGGL((count_kernel<kPer>), dim3(p.tiles + z.blocks), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, count, z);
+    z = next();
+    hipLaunchKernelGGL(scan_kernel, dim3((1 << p.bits) + z.blocks), dim3(256), 0, s, count, 1 << p.bits, p.tiles, total, z);
+    z = next();
+    hipLaunchKernelGGL((scatter_kernel<kPer>), dim3(p.tiles + z.blocks), dim3(kSortThreads), 0, s, a, in, shift, p.bits, p.tiles, (const int*)count,
+                       (const int*)total, out, z);
     in = out;
   }
   return in;
@@ -713,7 +746,8 @@ hipError_t launch_embed_rows(const EmbedArgs& a, hipStream_t s) {
 hipError_t launch_embed_rows_back(const EmbedArgs& a, hipStream_t s) {
   const Plan p = plan(a.rows, a.kinds, a.C, a.bf16 ? 2 : 4);
   const Room r = room(p, a.rows, a.C);
-  const Pair* sorted = a.rows == 0 ? nullptr : p.per == 1 ? sort<1>(a, p, r, s) : p.per == 4 ? sort<4>(a, p, r, s) : sort<16>(a, p, r, s);
+  const Pair* sorted = p.per == 1 ? sort<1>(a, p, r, s) : p.per == 4 ? sort<4>(a, p, r, s) : sort<16>(a, p, r, s);
+  if (a.rows == 0) return hipGetLastError();
   if (a.bf16) gradient<u16>(a, p, r, sorted, s);
   else gradient<float>(a, p, r, sorted, s);
   return hipGetLastError();
