@@ -1017,7 +1017,7 @@ class Evaluator:
         pb = 0 if beta is None else self._vector(beta, "beta", channels)
         pm, ps = self._vector(mean, "mean", rows), self._vector(rstd, "rstd", rows)
         if out is None:
-            out, lddx = self.torch.empty((rows, channels), dtype=dy.dtype, device=self.device), channels
+            out, lddx = dy.new_empty(rows, channels), channels
         else:
             lddx = self._like(out, "out", rows, channels, dtype)
         px, ldx, kept = 0, 0, None
@@ -1026,9 +1026,9 @@ class Evaluator:
         else:
             px, ldx = x.data_ptr(), self._like(x, "x", rows, channels, dtype)
         pr, ldr = (residual.data_ptr(), self._like(residual, "residual", rows, channels, dtype)) if residual is not None else (0, 0)
-        dgamma, dbeta = self.torch.empty((2, channels), dtype=self.torch.float32, device=self.device).unbind(0)
+        dgamma, dbeta = dy.new_empty(channels, dtype=self.torch.float32), dy.new_empty(channels, dtype=self.torch.float32)
         size = lib().dc_row_norm_bytes(self.ctx, rows, channels)
-        ws = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+        ws = dy.new_empty(size, dtype=self.torch.uint8)
         a = _ROW_NORM.pack(dtype, self._act(act), rows, channels, 0.0, px, ldx, pg, pb, pm, ps, 0, 0,
                            0 if kept is None else C.addressof(kept), dy.data_ptr(), lddy, pr, ldr, out.data_ptr(), lddx,
                            dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), size)
@@ -1063,11 +1063,11 @@ class Evaluator:
             raise ValueError("kinds: need at least one")
         pid = self._ids(ids, rows)
         if out is None:
-            out, ldt = self.torch.empty((kinds, channels), dtype=dy.dtype, device=self.device), channels
+            out, ldt = dy.new_empty(kinds, channels), channels
         else:
             ldt = self._like(out, "out", kinds, channels, dtype)
         size = lib().dc_embed_rows_bytes(self.ctx, rows, kinds, channels)
-        ws = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+        ws = dy.new_empty(size, dtype=self.torch.uint8)
         a = _EMBED.pack(dtype, rows, kinds, channels, scale, pid, 0, 0, 0, 0, dy.data_ptr(), lddy, out.data_ptr(), ldt, ws.data_ptr(), size)
         st = lib().dc_embed_rows_backward(self.ctx, a, self._raw_stream())
         if st:
