@@ -572,6 +572,34 @@ def test_adamw(ev, states, p, sizes, g):
 
 
 @pytest.mark.parametrize("states", ["f32", "8bit"])
+@pytest.mark.parametrize("sizes", [[2048 * 3], [2048 * 4], [2048 * 4, 1], [2048 * 2047, 2048], [2048 * 2047, 2048, 1], [2048 * 2046 + 1] * 2])
+def test_adamw_of_whole_chunks(ev, states, sizes):
+    """Around the sizes at which workgroups are full and calls are small."""
+    params = tensors_of(sizes, "mixed")
+    args = dict(lr=3e-3, betas=(0.9, 0.98), eps=1e-7)
+    o, plain = ev.adamw(params, **args, weight_decay=0.1, states=states, seed=3), Plain(params, [0.1] * len(sizes), states, 3, **args)
+    for k in range(2):
+        grads = grads_of(params, k)
+        o.step(grads)
+        plain.step(grads)
+        check_state(o, plain, params)
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_adamw_of_nothing(ev, states):
+    """A step without elements is one all the same."""
+    none = torch.zeros(0, device="cuda")
+    for params, grads in [([], []), ([none], [none]), (tensors_of([300, 2049], "mixed"), [None, None]), ([none] * 100, [none] * 100)]:
+        was = [p.clone() for p in params]
+        o = ev.adamw(params, states=states)
+        for _ in range(3):
+            o.step(grads)
+        assert o.steps.tolist() == [3, 0] and all(torch.equal(a, b) for a, b in zip(was, params))
+        w, m, v = o.values()
+        assert w.numel() == o.total and not m.any() and not v.any()
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit"])
 @pytest.mark.parametrize("first", [1, 3, 8])
 def test_adamw_of_parts_of_a_buffer(ev, states, first):
     """Parameters and gradients off every boundary, between others that stay as they are; gradients times a device number."""
@@ -846,11 +874,31 @@ def test_offsets_beyond_32_bits(ev):
         v = x[lo:lo + 1_000_000].double()
         want.index_add_(0, ids[lo:lo + 1_000_000].long(), v)
         size.index_add_(0, ids[lo:lo + 1_000_000].long(), v.abs())
-    # 64 rows of a chunk in fp32, five lists rounded to fp32
-    close(dt, want.cpu(), (70 * U * size + 2 * U * want.abs()).cpu(), "dtable")
+    # 64 rows of a run and four runs of a chunk in fp32, five lists rounded to fp32
+    close(dt, want.cpu(), ((64 + 4 + 5) * U * size + 2 * U * want.abs()).cpu(), "dtable")
     y.fill_(7)
     ev.embed_rows_backward(x[:3], far, rows, out=y)
     assert torch.equal(y[far.long()], x[:3]) and not y[last][:per - 77].any() and int((y != 0).any(1).sum()) == 3
+
+
+@pytest.mark.parametrize("rows", [1, 4096, 4097, 70001])
+def test_the_most_kinds(ev, rows):
+    """Kinds up to the largest number of them, of which most have no row."""
+    kinds, C = 2 ** 31 - 1, 1
+    g = torch.Generator().manual_seed(rows)
+    ids = torch.randint(0, kinds, (rows,), generator=g)
+    ids[0], ids[rows // 2], ids[-1] = kinds - 1, 0, kinds - 1
+    if rows > 1:
+        ids[1] = -1
+    dy = rand(3, rows, C).bfloat16()
+    dt = ev.embed_rows_backward(dy.cuda(), ids.int().cuda(), kinds)
+    used, back = ids[ids >= 0].unique(return_inverse=True)
+    want, size = (torch.zeros(used.numel(), C, dtype=torch.float64).index_add_(0, back, v[ids >= 0]) for v in (dy.double(), dy.double().abs()))
+    close(dt[used.cuda()], want, 4 * U * size + (R(torch.bfloat16) + 3 * U) * want.abs(), "dtable")
+    assert sum(int(part.count_nonzero()) for part in dt.split(2 ** 29)) == int((want != 0).sum())
+    y = ev.embed_rows(ids.int().cuda(), dt, 2.0)
+    assert torch.equal(y, torch.where(ids.cuda()[:, None] >= 0, 2 * dt[ids.cuda().clamp(min=0)], 0))
+    assert ev.check() == 0
 
 
 @pytest.mark.parametrize("states,n", [("f32", 2 ** 30 + 131 * 128 + 5), ("8bit", 2 ** 31 + 131 * 128 + 5)])
