@@ -488,12 +488,17 @@ Plan forward_plan(long long rows, int C, bool bf16) {
   if (p.blocks > most) p.blocks = most;
   return p;
 }
-// What a CU works on at a time, as each workgroup sums gradients of gamma and beta: 512 threads, or 1024 that read less than 40 bytes
-// of a row each (1000000 x 64 in fp32 142 us by 512, 160 by 1024; 2000000 x 64 in bf16 193 and 150).
-Plan back_plan(long long rows, int C, int n_cu, bool few) {
+// What a CU works on at a time, as each workgroup sums gradients of gamma and beta: rows of together 40 KB read and written, by 1024
+// threads at most (60000 x 1536 in bf16 with dres by 2, 3 and 5 workgroups a CU 181, 143 and 155 us; 1000000 x 256 in fp32 with dres by
+// 1 and 2 714 and 778; 2000003 x 256 in bf16 by 3 and 4 575 and 607).  bytes: of eight values of a row, read and written.
+constexpr int kAtWork = 40000;
+Plan back_plan(long long rows, int C, int n_cu, int bytes) {
   Plan p = plan(rows, C, C > 8192 ? 16 : 8);
-  const int each = (few ? 512 : 1024) / p.threads;
-  const long long most = (long long)n_cu * (each < 1 ? 1 : each);
+  const int work = p.wide ? C * bytes / 8 : 256 * bytes;         // of a workgroup's rows
+  int each = (kAtWork + work / 2) / work;
+  if (each > 1024 / p.threads) each = 1024 / p.threads;
+  if (each < 1) each = 1;
+  const long long most = (long long)n_cu * each;
   if (p.blocks > most) p.blocks = most;
   return p;
 }
@@ -552,7 +557,7 @@ void backward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
 
 }  // namespace
 
-size_t row_norm_floats(long long rows, int C, int n_cu) { return (size_t)back_plan(rows, C, n_cu, false).blocks * 2 * C; }
+size_t row_norm_floats(long long rows, int C, int n_cu) { return (size_t)back_plan(rows, C, n_cu, 8 + 16 + 16).blocks * 2 * C; }
 
 hipError_t launch_row_norm(const RowNormArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
@@ -563,7 +568,7 @@ hipError_t launch_row_norm(const RowNormArgs& a, hipStream_t s) {
 
 hipError_t launch_row_norm_back(const RowNormArgs& a, hipStream_t s) {
   const int bytes = a.bf16 ? 16 : 32;              // of eight values
-  const Plan p = back_plan(a.rows, a.C, a.n_cu, (a.kept.code ? 8 : bytes) + bytes + (a.dRes ? bytes : 0) >= 40);
+  const Plan p = back_plan(a.rows, a.C, a.n_cu, (a.kept.code ? 8 : bytes) + 2 * bytes + (a.dRes ? bytes : 0));
   if (a.rows > 0) {
     if (a.kept.code) {
       if (a.bf16) backward<u16, Kept8>(a, p, s);
