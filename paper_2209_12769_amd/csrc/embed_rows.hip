@@ -11,7 +11,7 @@
 // in fp32, the chunks' in 64 bits, rounded to fp32 from list to list.  The table is cleared by the sort's launches, kinds that have
 // rows are written after that.  Bound by memory in the rows' sums, which read rows at the sorted list's places, and by launches in
 // the rest (474011 rows of 256 in fp32 to 97 kinds: 120 us, of them 89 the rows' sums, 5.4 TB/s; 65521 rows of 1031 in bf16 to
-// 128001 kinds: 126 us, of them 52 the sort and the zeros, 56 the rows' sums).
+// 128001 kinds: 103 us, of them 51 the sort and the zeros, 37 the rows' sums).
 #include "row_vectors.h"
 
 namespace dc {
@@ -103,8 +103,8 @@ __device__ __forceinline__ void in_order() {
 
 // ---- zeros ----
 // The launches of the sort wait for memory most of the time.  They clear the table besides, a part of it each, by further workgroups
-// (65521 rows of 1031 in bf16 to 128001 kinds, half of them without a row: the call 136 us, and 144 where the sums' launch looks for
-// those and clears no others; 3000 rows of 1024 to 250000 kinds 99 and 120; 65536 rows of 1024, one of each kind, 99 and 90).
+// (3000 rows of 1024 in bf16 to 250000 kinds: the call 98 us, and 120 where the sums' launch looks for kinds without rows and clears no
+// others; 65536 rows of 1024, one of each kind, 88 and 90).
 struct Zeros {
   u16* table;                  // in halves of a word: rows of `width`, the last of `last`, `stride` from one to the next
   long long stride, rows;
@@ -116,7 +116,9 @@ struct Part {
   int blocks;
 };
 constexpr int kClear = 8192;   // halves of a word that a wave clears
-// A row by one wave, on 16-byte boundaries but for its first and last vector.
+// A row by one wave, on 16-byte boundaries but for its first and last vector.  Zeros, and rows of kinds that lie inside one chunk, are
+// stored as not used again soon: left in L2 they would be in the way of the rows that are summed (65521 rows of 1031 in bf16 to 128001
+// kinds 125 -> 103 us; 100000 of 1024 to 100000 kinds 136 -> 114; tables of few kinds the same).
 __device__ __forceinline__ void clear_row(u16* row, int n) {
   const int lane = threadIdx.x & 63;
   const u32x4 zero = {0, 0, 0, 0};
@@ -126,7 +128,7 @@ __device__ __forceinline__ void clear_row(u16* row, int n) {
   }
   const int skip = (int)(-(reinterpret_cast<size_t>(row) / 2) & 7), whole = (n - skip) / 8;
   u32x4* to = reinterpret_cast<u32x4*>(row + skip);
-  for (int at = lane; at < whole; at += 64) to[at] = zero;
+  for (int at = lane; at < whole; at += 64) __builtin_nontemporal_store(zero, to + at);
   if (lane == 0 && skip != 0) *reinterpret_cast<u32x4_any*>(row) = zero;
   if (lane == 1 && skip + whole * 8 < n) *reinterpret_cast<u32x4_any*>(row + (n - 8)) = zero;
 }
@@ -343,7 +345,9 @@ __device__ __forceinline__ void write_kind(const EmbedArgs& a, int kind, int c, 
   float y[kVector<T>];
 #pragma unroll
   for (int k = 0; k < kVector<T>; ++k) y[k] = x[k] * a.scale;
-  store_vector<T, false>(static_cast<T*>(a.dtable) + (long long)kind * a.lddt, c, a.C, pack(y, T()));
+  T* to = static_cast<T*>(a.dtable) + (long long)kind * a.lddt;
+  if (c + kVector<T> <= a.C) __builtin_nontemporal_store(pack(y, T()), reinterpret_cast<u32x4_any*>(to + c));
+  else store_vector<T, false>(to, c, a.C, pack(y, T()));
 }
 // Four columns of an entry from c.
 __device__ __forceinline__ void read_entry(float (&x)[4], const float* row, int c, int C) { unpack(x, load_vector<float, false>(row, c, C), 0.f); }
