@@ -10,7 +10,7 @@
 // enough for one workgroup a kind.  No atomics: the same call gives the same bits.  Sums: up to 64 rows in fp32, up to four such runs
 // in fp32, the chunks' in 64 bits, rounded to fp32 from list to list.  The table is cleared by the sort's launches, kinds that have
 // rows are written after that.  Bound by memory in the rows' sums, which read rows at the sorted list's places, and by launches in
-// the rest (474011 rows of 256 in fp32 to 97 kinds: 120 us, of them 89 the rows' sums, 5.4 TB/s; 65521 rows of 1031 in bf16 to
+// the rest (474011 rows of 256 in fp32 to 97 kinds: 107 us, of them 77 the rows' sums, 6.3 TB/s; 65521 rows of 1031 in bf16 to
 // 128001 kinds: 103 us, of them 51 the sort and the zeros, 37 the rows' sums).
 #include "row_vectors.h"
 
@@ -416,8 +416,10 @@ __device__ __forceinline__ Pair sorted_at(const Sums& s, int i) {
     return s.sorted[i];
   }
 }
-// First level: chunks of the sorted rows.  kWave: a wave each, of rows or slabs of more than 32 vectors.
-template <typename T, bool kWave>
+// First level: chunks of the sorted rows.  kWave: a wave each, of rows or slabs of more than 32 vectors.  kOnce: dY is read as not used
+// again soon.
+constexpr long long kCached = 256 << 20;       // bytes that the memory's cache holds
+template <typename T, bool kWave, bool kOnce>
 __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
   constexpr int kV = kVector<T>, kAhead = kWave ? 8 : 4;
   const EmbedArgs& a = s.a;
@@ -452,7 +454,11 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
     if (e[0].kind >= a.kinds) break;                     // only rows that stand for nothing are left
     u32x4 v[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = load_vector<T, false>(dY + (long long)e[u].row * a.lddy, c, a.C);
+    for (int u = 0; u < kAhead; ++u) {
+      const T* row = dY + (long long)e[u].row * a.lddy;
+      if constexpr (kOnce) v[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + c));
+      else v[u] = load_vector<T, kWave>(row, c, a.C);
+    }
     Pair next[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) next[u] = sorted_at<kWave>(s, p0 + min(q + kAhead + u, len - 1));
@@ -664,8 +670,12 @@ void gradient(const EmbedArgs& a, const Plan& p, const Room& r, const Pair* sort
   }
   const long long seats = 256 / p.lanes, items = (long long)p.nchunk * p.nslab;
   const dim3 grid((unsigned)((items + seats - 1) / seats));
-  if (p.lanes == 64) hipLaunchKernelGGL((sum_rows_kernel<T, true>), grid, dim3(256), 0, s, m);
-  else hipLaunchKernelGGL((sum_rows_kernel<T, false>), grid, dim3(256), 0, s, m);
+  // A dY that the memory's cache cannot hold goes past the others: 474011 rows of 256 in fp32 to 97 kinds 122 -> 109 us, 2 M of 512 in
+  // bf16 to 200000 623 -> 582.  A smaller one, which may be there from the launch that wrote it, does not: 100000 rows of 1024 in bf16
+  // to 50000 kinds, read again and again, 93 us, past the caches 107.
+  if (p.lanes < 64) hipLaunchKernelGGL((sum_rows_kernel<T, false, false>), grid, dim3(256), 0, s, m);
+  else if (a.rows * a.C * (long long)sizeof(T) > kCached) hipLaunchKernelGGL((sum_rows_kernel<T, true, true>), grid, dim3(256), 0, s, m);
+  else hipLaunchKernelGGL((sum_rows_kernel<T, true, false>), grid, dim3(256), 0, s, m);
   // entries: four columns a thread
   const int fours = (a.C + 3) / 4;
   m.lanes = lanes_of(fours);
