@@ -8,9 +8,9 @@
 // power of two of a wave's lanes, several rows a wave, wider rows a workgroup.  The forward pass is one launch of as many
 // workgroups as there are rows for, two rows a seat: they are handed out in the order of the addresses, and a copy of that kind
 // gets 6.1 TB/s where one by resident workgroups that go on in strides gets 4.7.  (5.7 M rows of 256 in bf16 with SiLU, 5.8 GB:
-// 1025 us, 5.7 TB/s; 1235 by resident workgroups that request a row ahead.)  The gradients keep to what is resident, since each
-// workgroup hands on sums of 2 C numbers (2 M rows of 256 in bf16 with GELU and dres, 4.1 GB: 800 us, 5.1 TB/s; 474011 rows of 256
-// in fp32, x in 8 bits: 1.1 GB, 202 us, 5.4 TB/s).
+// 982 us, 6.0 TB/s; by resident workgroups that request a row ahead a fifth more.)  The gradients keep to what is resident, since
+// each workgroup hands on sums of 2 C numbers (2 M rows of 256 in bf16 with GELU and dres, 4.1 GB: 770 us, 5.3 TB/s; 474011 rows of
+// 256 in fp32, x in 8 bits: 1.1 GB, 197 us, 5.6 TB/s).
 // The variance is that of d = x - m, m the row's sum over C as fp32 has it: mean d is what m lacks, v = mean d^2 - (mean d)^2.
 // So neither loses digits for values far from zero, and mu is m + mean d, rounded once where it is returned.
 // Gradients of gamma and beta: 64 rows of a thread in fp32, these sums in fp32 again, a workgroup's rows and the workgroups
@@ -70,23 +70,29 @@ struct Fetched<float, Kept8, NV> {
   unsigned v[NV];
   unsigned e[NV], e2[NV];
 };
+// kOnce: as not used again soon.
+template <bool kOnce, typename V>
+__device__ __forceinline__ V read(const V* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(p);
+  else return *p;
+}
 // `row` elements from p on: p is the same for the wave, so that only 32 bits are the lane's own.
-template <typename T, int NV, Fit kFit>
+template <bool kOnce, typename T, int NV, Fit kFit>
 __device__ __forceinline__ void fetch(Fetched<T, T, NV>& f, const T* p, unsigned row, const Columns<T, NV>& q, int C) {
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     if constexpr (kFit == kShort) f.v[j] = load_vector<T, false>(p + row, q.at[j], C);
-    else f.v[j] = *reinterpret_cast<const u32x4_any*>(p + (row + (unsigned)q.at[j]));
+    else f.v[j] = read<kOnce>(reinterpret_cast<const u32x4_any*>(p + (row + (unsigned)q.at[j])));
   }
 }
 // A row of codes goes up to a multiple of 32, so a short one has a whole vector too.
-template <typename T, int NV, Fit kFit>
+template <bool kOnce, typename T, int NV, Fit kFit>
 __device__ __forceinline__ void fetch(Fetched<T, Kept8, NV>& f, const signed char* p, unsigned row, const unsigned char* e, unsigned row_e, const Columns<T, NV>& q) {
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const unsigned at = q.at[j];
-    if constexpr (sizeof(T) == 2) f.v[j] = *reinterpret_cast<const u32x2_any*>(p + (row + at));
-    else f.v[j] = *reinterpret_cast<const u32_any*>(p + (row + at));
+    if constexpr (sizeof(T) == 2) f.v[j] = read<kOnce>(reinterpret_cast<const u32x2_any*>(p + (row + at)));
+    else f.v[j] = read<kOnce>(reinterpret_cast<const u32_any*>(p + (row + at)));
     f.e[j] = e[row_e + at / kKeptBlock];
     f.e2[j] = kFit == kBack ? e[row_e + (at + kVector<T> - 1) / kKeptBlock] : 0;
   }
@@ -142,7 +148,7 @@ __device__ __forceinline__ void vectors_at(float (&g)[NV * kVector<T>], const fl
   }
 }
 // kOwn: a vector that ends with the row writes only what is its own, so that its neighbour's may be read until then.
-template <typename T, int NV, Fit kFit, bool kOwn = false>
+template <bool kOnce, typename T, int NV, Fit kFit, bool kOwn = false>
 __device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], T* p, unsigned row, const Columns<T, NV>& q, int C) {
   constexpr int kV = kVector<T>;
 #pragma unroll
@@ -157,7 +163,11 @@ __device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], T* p, uns
 #pragma unroll
         for (int k = 0; k < kV; ++k)
           if (k >= q.skip[j]) narrow(w[k], p[row + (unsigned)(q.at[j] + k)]);
-      } else *reinterpret_cast<u32x4_any*>(p + (row + (unsigned)q.at[j])) = pack(w, T());
+      } else if constexpr (kOnce) {
+        __builtin_nontemporal_store(pack(w, T()), reinterpret_cast<u32x4_any*>(p + (row + (unsigned)q.at[j])));
+      } else {
+        *reinterpret_cast<u32x4_any*>(p + (row + (unsigned)q.at[j])) = pack(w, T());
+      }
     }
   }
 }
@@ -228,7 +238,7 @@ __device__ __forceinline__ unsigned rows_on(int seat, long long ld) { return (un
 // Rows of a seat in the forward pass, whose requests go out together (5.7 M rows of 256 in bf16 with SiLU: one 1090 us, two 995,
 // four 1018; 20000 rows of 8192 in bf16 177, 136 and 135; 20011 of 5003 in fp32 186, 157 and 194).
 constexpr int kSeatRows = 2;
-template <typename T, int NV, int kLanes, Fit kFit>
+template <typename T, int NV, int kLanes, Fit kFit, bool kOnce>
 __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel(const RowNormArgs a, int row_lanes) {
   constexpr int kV = kVector<T>, kN = NV * kV, kRows = kSeatRows;
   __shared__ float red[kLanes == kGroup ? 3 * kMostWaves : 1];
@@ -245,7 +255,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const bool there = u * s.seats + s.seat < left;
-      fetch<T, NV, kFit>(f[u], u * s.seats < left ? X + u * s.seats * a.ldx : X, there ? x_on : 0u, q, a.C);
+      fetch<kOnce, T, NV, kFit>(f[u], u * s.seats < left ? X + u * s.seats * a.ldx : X, there ? x_on : 0u, q, a.C);
     }
     float gamma[kN], beta[kN];
     vectors_at<T, NV, kFit>(gamma, a.gamma, 1.f, q, a.C);
@@ -281,7 +291,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel
 #pragma unroll
       for (int k = 0; k < kN; ++k) x[k] = fmaf(fmaf(x[k], r, shift), gamma[k], beta[k]);
       activate<kN>(x, a.act);
-      put<T, NV, kFit>(x, Y + u * s.seats * a.ldy, y_on, q, a.C);
+      put<kOnce, T, NV, kFit>(x, Y + u * s.seats * a.ldy, y_on, q, a.C);
       if (a.mean && s.t == 0) {
         a.mean[row0 + u * s.seats + s.seat] = m + lacks;
         a.rstd[row0 + u * s.seats + s.seat] = r;
@@ -290,7 +300,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_kernel
   }
 }
 
-template <typename T, typename X, int NV, int kLanes, Fit kFit>
+template <typename T, typename X, int NV, int kLanes, Fit kFit, bool kOnce>
 __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_kernel(const RowNormArgs a, int row_lanes) {
   constexpr int kV = kVector<T>, kN = NV * kV;
   constexpr bool kKept = !std::is_same<T, X>::value, kWide = kLanes == kGroup;
@@ -338,10 +348,10 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
   for (long long row0 = (long long)blockIdx.x * s.seats; row0 + s.seat < a.rows; row0 += (long long)gridDim.x * s.seats) {
     Fetched<T, X, NV> f;
     Fetched<T, T, NV> fd, fr;
-    if constexpr (kKept) fetch<T, NV, kFit>(f, a.kept.code + row0 * a.kept.ld_code, x_on, a.kept.exponent + row0 * a.kept.ld_exponent, e_on, q);
-    else fetch<T, NV, kFit>(f, static_cast<const T*>(a.X) + row0 * a.ldx, x_on, q, a.C);
-    fetch<T, NV, kFit>(fd, static_cast<const T*>(a.dY) + row0 * a.lddy, dy_on, q, a.C);
-    if (!kLds && a.dRes) fetch<T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
+    if constexpr (kKept) fetch<kOnce, T, NV, kFit>(f, a.kept.code + row0 * a.kept.ld_code, x_on, a.kept.exponent + row0 * a.kept.ld_exponent, e_on, q);
+    else fetch<kOnce, T, NV, kFit>(f, static_cast<const T*>(a.X) + row0 * a.ldx, x_on, q, a.C);
+    fetch<kOnce, T, NV, kFit>(fd, static_cast<const T*>(a.dY) + row0 * a.lddy, dy_on, q, a.C);
+    if (!kLds && a.dRes) fetch<kOnce, T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
     const float m = a.mean[row0 + s.seat], r = a.rstd[row0 + s.seat];
     float xh[kN], dz[kN];
     values<T, NV, kFit>(xh, f, q);
@@ -404,7 +414,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
     parity ^= 1;
     s1 *= share;
     s2 *= share;
-    if (kLds && a.dRes) fetch<T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
+    if (kLds && a.dRes) fetch<kOnce, T, NV, kFit>(fr, static_cast<const T*>(a.dRes) + row0 * a.lddres, res_on, q, a.C);
 #pragma unroll
     for (int k = 0; k < kN; ++k) dz[k] = r * (dz[k] - s1 - xh[k] * s2);
     if (a.dRes) {
@@ -413,7 +423,7 @@ __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_k
 #pragma unroll
       for (int k = 0; k < kN; ++k) dz[k] += add[k];
     }
-    put<T, NV, kFit, kLds>(dz, static_cast<T*>(a.dX) + row0 * a.lddx, dx_on, q, a.C);
+    put<kOnce, T, NV, kFit, kLds>(dz, static_cast<T*>(a.dX) + row0 * a.lddx, dx_on, q, a.C);
     if (++run == kRun) {
       run = 0;
       join(false);
@@ -520,6 +530,12 @@ void each_fit(const Plan& p, int C, F f) {
   else if (C >= kVector<T>) fit(Number<0>());
   else f(Number<0>(), std::integral_constant<Fit, kShort>());
 }
+// Whether rows go past the caches: whole ones (parts of lines are put together there) of which the memory's cache cannot hold all.
+// 5.7 M rows of 256 in bf16, forward, 1025 -> 983 us; gradients of 2 M of them with dres 800 -> 768, of 474011 in fp32, x in 8 bits, 204 -> 197.
+// Smaller ones may be there for the next operator: behind 200000 rows of 256 in bf16 past the caches a dense layer made it 102 us for 95.
+constexpr long long kCached = 256 << 20;
+template <Fit kFit>
+bool once(const RowNormArgs& a) { return kFit == kWhole && a.rows * a.C * (a.bf16 ? 2LL : 4LL) > kCached; }
 template <typename T>
 void forward(const RowNormArgs& a, hipStream_t s) {
   constexpr int NV = 8 / kVector<T>;
@@ -528,14 +544,20 @@ void forward(const RowNormArgs& a, hipStream_t s) {
   each_fit<T>(p, a.C, [&](auto lanes, auto fit) {
     constexpr int kLanes = decltype(lanes)::value;
     constexpr Fit kFit = decltype(fit)::value;
-    // sixteen values: a workgroup's rows, and a whole wave's in bf16
-    if constexpr (kLanes == kGroup || (kLanes == 64 && sizeof(T) == 2)) {
-      if (p.per == 16) {
-        hipLaunchKernelGGL((row_norm_kernel<T, 2 * NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
-        return;
+    auto launch = [&](auto vectors, auto past) {
+      hipLaunchKernelGGL((row_norm_kernel<T, decltype(vectors)::value, kLanes, kFit, decltype(past)::value != 0>), g, b, 0, s, a, p.lanes);
+    };
+    auto vectors = [&](auto past) {
+      // sixteen values: a workgroup's rows, and a whole wave's in bf16
+      if constexpr (kLanes == kGroup || (kLanes == 64 && sizeof(T) == 2)) {
+        if (p.per == 16) return launch(Number<2 * NV>(), past);
       }
+      launch(Number<NV>(), past);
+    };
+    if constexpr (kFit == kWhole) {
+      if (once<kFit>(a)) return vectors(Number<1>());
     }
-    hipLaunchKernelGGL((row_norm_kernel<T, NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
+    vectors(Number<0>());
   });
 }
 template <typename T, typename X>
@@ -545,13 +567,19 @@ void backward(const RowNormArgs& a, const Plan& p, hipStream_t s) {
   each_fit<T>(p, a.C, [&](auto lanes, auto fit) {
     constexpr int kLanes = decltype(lanes)::value;
     constexpr Fit kFit = decltype(fit)::value;
-    if constexpr (kLanes == kGroup) {
-      if (p.per == 16) {
-        hipLaunchKernelGGL((row_norm_back_kernel<T, X, 2 * NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
-        return;
+    auto launch = [&](auto vectors, auto past) {
+      hipLaunchKernelGGL((row_norm_back_kernel<T, X, decltype(vectors)::value, kLanes, kFit, decltype(past)::value != 0>), g, b, 0, s, a, p.lanes);
+    };
+    auto vectors = [&](auto past) {
+      if constexpr (kLanes == kGroup) {
+        if (p.per == 16) return launch(Number<2 * NV>(), past);
       }
+      launch(Number<NV>(), past);
+    };
+    if constexpr (kFit == kWhole) {
+      if (once<kFit>(a)) return vectors(Number<1>());
     }
-    hipLaunchKernelGGL((row_norm_back_kernel<T, X, NV, kLanes, kFit>), g, b, 0, s, a, p.lanes);
+    vectors(Number<0>());
   });
 }
 

@@ -839,6 +839,40 @@ def test_calls_on_two_streams_at_once(ev):
     assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
 
 
+@pytest.mark.parametrize("dtype,C", [("bf16", 64), ("f32", 128), ("bf16", 256), ("f32", 256), ("bf16", 512), ("f32", 512), ("bf16", 1024), ("f32", 1024), ("f32", 8192),
+                                     ("bf16", 16384), ("f32", 16384)])
+def test_row_norm_of_more_than_the_caches(ev, dtype, C):
+    """Rows of together more than 256 MiB: each the same as among few, and gamma's and beta's gradients by 64 bits."""
+    t = TYPES[dtype]
+    rows = 2 ** 28 // (C * (2 if dtype == "bf16" else 4)) + 5
+    g = torch.Generator(device="cuda").manual_seed(C)
+    x, dy = torch.randn(rows, C, generator=g, device="cuda").to(t), torch.randn(rows, C, generator=g, device="cuda").to(t)
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g, device="cuda"), 0.3 * torch.randn(C, generator=g, device="cuda")
+    y, mean, rstd = ev.row_norm(x, gamma, beta, EPS, "silu")
+    step = rows // 3
+    for rest, past in ((x, dy), (ev.keep_rows(x), None)):
+        dx, dgamma, dbeta = ev.row_norm_backward(dy, rest, gamma, beta, mean, rstd, "silu", past)
+        back = x if rest is x else ev.restore_rows(rest, torch.float32)
+        sums = torch.zeros(4, C, dtype=torch.float64, device="cuda")
+        for lo in range(0, rows, step):
+            at = slice(lo, min(lo + step, rows))
+            few = ev.row_norm(x[at], gamma, beta, EPS, "silu")
+            assert torch.equal(few[0], y[at]) and torch.equal(few[1], mean[at]) and torch.equal(few[2], rstd[at])
+            # codes go by rows, so those of a part are the part's own
+            part = x[at] if rest is x else ev.keep_rows(x[at])
+            assert torch.equal(ev.row_norm_backward(dy[at], part, gamma, beta, mean[at], rstd[at], "silu", None if past is None else past[at])[0], dx[at])
+            for lo2 in range(at.start, at.stop, 1 << 24 >> (C.bit_length() - 1)):
+                to = slice(lo2, min(lo2 + (1 << 24 >> (C.bit_length() - 1)), at.stop))
+                xh = (back[to].double() - mean[to, None]) * rstd[to, None]
+                dz = dy[to].double() * slope(xh * gamma + beta, "silu")
+                sums += torch.stack([(dz * xh).sum(0), dz.sum(0), (dz * xh).abs().sum(0), dz.abs().sum(0)])
+        # 64 rows of a thread, its runs (of at most 256 workgroups' rows a run, here fewer than 70), 64 bits twice; the terms' own 30
+        n = 64 + 70 + 6 + 30
+        size = 1 + gamma.abs().double() + beta.abs()
+        close(dgamma, sums[0].cpu(), (n * U * (sums[2] + sums[3] * size)).cpu(), "dgamma")
+        close(dbeta, sums[1].cpu(), (n * U * sums[3] * size).cpu(), "dbeta")
+
+
 def test_offsets_beyond_32_bits(ev):
     """Arrays of more than 4 GiB: the last rows against 64 bits, everything that is summed over all rows too."""
     rows, C, per, kinds = 8_600_000, 128, 500, 1000
