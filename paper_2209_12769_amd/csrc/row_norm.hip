@@ -70,11 +70,21 @@ struct Fetched<float, Kept8, NV> {
   unsigned v[NV];
   unsigned e[NV], e2[NV];
 };
-// kOnce: as not used again soon.
-template <bool kOnce, typename V>
-__device__ __forceinline__ V read(const V* p) {
-  if constexpr (kOnce) return __builtin_nontemporal_load(p);
-  else return *p;
+// 16, 8 and 4 bytes from anywhere.  kOnce: as not used again soon.
+template <bool kOnce>
+__device__ __forceinline__ u32x4 read16(const void* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(static_cast<const u32x4_any*>(p));
+  else return *static_cast<const u32x4_any*>(p);
+}
+template <bool kOnce>
+__device__ __forceinline__ u32x2 read8(const void* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(static_cast<const u32x2_any*>(p));
+  else return *static_cast<const u32x2_any*>(p);
+}
+template <bool kOnce>
+__device__ __forceinline__ unsigned read4(const void* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(static_cast<const u32_any*>(p));
+  else return *static_cast<const u32_any*>(p);
 }
 // `row` elements from p on: p is the same for the wave, so that only 32 bits are the lane's own.
 template <bool kOnce, typename T, int NV, Fit kFit>
@@ -82,7 +92,7 @@ __device__ __forceinline__ void fetch(Fetched<T, T, NV>& f, const T* p, unsigned
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     if constexpr (kFit == kShort) f.v[j] = load_vector<T, false>(p + row, q.at[j], C);
-    else f.v[j] = read<kOnce>(reinterpret_cast<const u32x4_any*>(p + (row + (unsigned)q.at[j])));
+    else f.v[j] = read16<kOnce>(p + (row + (unsigned)q.at[j]));
   }
 }
 // A row of codes goes up to a multiple of 32, so a short one has a whole vector too.
@@ -91,8 +101,8 @@ __device__ __forceinline__ void fetch(Fetched<T, Kept8, NV>& f, const signed cha
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const unsigned at = q.at[j];
-    if constexpr (sizeof(T) == 2) f.v[j] = read<kOnce>(reinterpret_cast<const u32x2_any*>(p + (row + at)));
-    else f.v[j] = read<kOnce>(reinterpret_cast<const u32_any*>(p + (row + at)));
+    if constexpr (sizeof(T) == 2) f.v[j] = read8<kOnce>(p + (row + at));
+    else f.v[j] = read4<kOnce>(p + (row + at));
     f.e[j] = e[row_e + at / kKeptBlock];
     f.e2[j] = kFit == kBack ? e[row_e + (at + kVector<T> - 1) / kKeptBlock] : 0;
   }
