@@ -542,7 +542,7 @@ class AdamW:
         self.total = total
         self._shapes, self._dtypes = [p.shape for p in self.params], [p.dtype for p in self.params]
         # what the table holds of the tensors' places and the gradients' types, as lists; `_held` keeps that memory theirs, so that a
-        # place that is still the same needs no further look
+        # place that is still the same is the same tensor's
         self._ptrs, self._g_dtypes = [p.data_ptr() for p in self.params], None
         self._held = [p.detach() for p in self.params]
         eight = states == "8bit"
@@ -559,8 +559,11 @@ class AdamW:
             raise ValueError(f"tensor {k}: need contiguous float32 or bfloat16 on {self.ev.device}")
 
     def _args(self, grad_scale: int) -> bytes:
-        ptrs = list(map(self.ev.torch.Tensor.data_ptr, self.params))
-        if ptrs != self._ptrs:                             # tensors whose owner gave them other memory
+        T = self.ev.torch.Tensor
+        ptrs = list(map(T.data_ptr, self.params))
+        # tensors whose owner gave them other memory, or let the same memory stand in another order, type or shape
+        if (ptrs != self._ptrs or list(map(T.dtype.__get__, self.params)) != self._dtypes
+                or list(map(T.shape.__get__, self.params)) != self._shapes or not all(map(T.is_contiguous, self.params))):
             for k, p in enumerate(self.params):
                 self._check(k, p)
                 if p.shape != self._shapes[k] or p.dtype != self._dtypes[k]:

@@ -138,3 +138,28 @@ def test_adamw_looks_at_every_gradient(ev):
                    (2, torch.zeros(1))]:
         for rest in (good, [None] * 4):
             refused(f"gradient {k}", o.step, [bad if i == k else g for i, g in enumerate(rest)])
+
+
+def test_adamw_looks_at_the_layout_of_parameters(ev):
+    """A parameter whose order, type or shape changed while its memory is the same: refused, and taken again once it is as it was."""
+    def changed(p):
+        yield "transposed", lambda: p.t_(), lambda: p.t_()
+        was = p.data
+        for name, other in [("transposed data", was.t()), ("overlapping rows", was.as_strided((16, 16), (8, 1))), ("another type", was.flatten().view(torch.bfloat16)[:256].view(16, 16)),
+                            ("no type of a parameter", was.view(torch.int32)), ("fewer rows", was[:9]), ("another shape", was.view(8, 32)), ("a vector", was.view(256))]:
+            assert other.data_ptr() == was.data_ptr()
+            yield name, lambda: setattr(p, "data", other), lambda: setattr(p, "data", was)
+    params = [torch.zeros(7), torch.arange(256.0).view(16, 16)]
+    o = ev.adamw(params)
+    grads = [torch.zeros_like(p) for p in params]
+    without_context(o.step, grads)
+    for name, change, undo in changed(params[1]):
+        change()
+        for call, args in ((o.step, [grads]), (o.step, [[None, grads[1]]]), (o.values, ["w"])):
+            try:
+                refused("tensor 1", call, *args)
+            except B.DiscoError:
+                pytest.fail(f"{name}: {call.__name__} went on to the library")
+        undo()
+        without_context(o.step, grads)
+        without_context(o.values, "w")
