@@ -564,6 +564,8 @@ class AdamW:
         # tensors whose owner gave them other memory, or let the same memory stand in another order, type or shape
         if (ptrs != self._ptrs or list(map(T.dtype.__get__, self.params)) != self._dtypes
                 or list(map(T.shape.__get__, self.params)) != self._shapes or not all(map(T.is_contiguous, self.params))):
+            if len(ptrs) != len(self._shapes):
+                raise ValueError(f"params: made of {len(self._shapes)} tensors, not {len(ptrs)}")
             for k, p in enumerate(self.params):
                 self._check(k, p)
                 if p.shape != self._shapes[k] or p.dtype != self._dtypes[k]:
@@ -577,8 +579,8 @@ class AdamW:
         """One step with a gradient for every tensor (float32 or bfloat16, contiguous, its shape), None for tensors that stay as
         they are.  grad_scale: a float32 device tensor of one number that the gradients are multiplied by."""
         ev, T = self.ev, self.ev.torch.Tensor
-        if len(grads) != len(self.params):
-            raise ValueError(f"need {len(self.params)} gradients, not {len(grads)}")
+        if len(grads) != len(self._shapes):
+            raise ValueError(f"need {len(self._shapes)} gradients, not {len(grads)}")
         which, have, shapes = slice(None), grads, self._shapes
         if any(map(operator.is_, grads, itertools.repeat(None))):
             which = [k for k, g in enumerate(grads) if g is not None]

@@ -163,3 +163,14 @@ def test_adamw_looks_at_the_layout_of_parameters(ev):
         undo()
         without_context(o.step, grads)
         without_context(o.values, "w")
+
+
+def test_adamw_has_the_parameters_that_it_was_made_of(ev):
+    """The list of them is no place to add or to take away any."""
+    params = [torch.zeros(7), torch.zeros(7)]
+    for change in (lambda ps: ps.append(torch.zeros(7)), lambda ps: ps.pop(), lambda ps: ps.pop(0)):
+        o = ev.adamw(params)
+        change(o.params)
+        refused("2 tensors", o.step, [torch.zeros(7)] * 2)
+        refused("2 gradients", o.step, [torch.zeros(7)] * len(o.params))
+        refused("2 tensors", o.values, "w")
