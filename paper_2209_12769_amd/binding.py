@@ -514,10 +514,11 @@ class AdamW:
     at[k] .. at[k] + its elements.  Saved, and copied back into them (copy_), they go on where they were.  lr, betas, eps and seed
     may be changed between steps.  A parameter may be given other memory (data) of its shape and type."""
 
-    _STATE = frozenset(("m", "v", "m_exponent", "v_exponent", "low", "steps", "params", "at", "total", "states"))
+    _PARTS = ("m", "v", "m_exponent", "v_exponent", "low", "steps")
+    _FIXED = frozenset(_PARTS + ("params", "at", "total", "states"))
 
     def __setattr__(self, name, value):
-        if name in self._STATE and name in self.__dict__:              # the calls go by where they lie
+        if name in self._FIXED and name in self.__dict__:              # the calls go by where they lie
             raise AttributeError(f"{name} is kept where it is: copy_ into it")
         object.__setattr__(self, name, value)
 
@@ -551,8 +552,12 @@ class AdamW:
             self.m_exponent, self.v_exponent = (torch.zeros(total // 128, dtype=torch.uint8, device=ev.device) if eight else None for _ in range(2))
             self.low = torch.zeros(total, dtype=torch.int16, device=ev.device) if half else None
             self.steps = torch.zeros(2, dtype=torch.int32, device=ev.device)
-        self._where = (total, self.m.data_ptr(), self.v.data_ptr(), self.m_exponent.data_ptr() if eight else 0,
-                       self.v_exponent.data_ptr() if eight else 0, self.low.data_ptr() if half else 0, self.steps.data_ptr())
+        # the state and where it lies; that memory is kept too
+        self._state = {name: getattr(self, name) for name in self._PARTS if getattr(self, name) is not None}
+        self._state_ptrs = list(map(torch.Tensor.data_ptr, self._state.values()))
+        at = dict(zip(self._state, self._state_ptrs))
+        self._where = (total, *(at.get(name, 0) for name in self._PARTS))
+        self._held_state = [t.detach() for t in self._state.values()]
 
     def _check(self, k: int, p):
         if p.device != self.ev.device or p.dtype not in self.ev._types or not p.is_contiguous():
@@ -560,6 +565,9 @@ class AdamW:
 
     def _args(self, grad_scale: int) -> bytes:
         T = self.ev.torch.Tensor
+        if list(map(T.data_ptr, self._state.values())) != self._state_ptrs:
+            moved = [name for name, was in zip(self._state, self._state_ptrs) if self._state[name].data_ptr() != was]
+            raise ValueError(f"{', '.join(moved)}: given other memory; copy_ into the state")
         ptrs = list(map(T.data_ptr, self.params))
         # tensors whose owner gave them other memory, or let the same memory stand in another order, type or shape
         if (ptrs != self._ptrs or list(map(T.dtype.__get__, self.params)) != self._dtypes

@@ -174,3 +174,23 @@ def test_adamw_has_the_parameters_that_it_was_made_of(ev):
         refused("2 tensors", o.step, [torch.zeros(7)] * 2)
         refused("2 gradients", o.step, [torch.zeros(7)] * len(o.params))
         refused("2 tensors", o.values, "w")
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_adamw_state_given_other_memory(ev, states):
+    """The calls go by where the state lies: a part of it that has other memory, or none, is refused, and what it had is not
+    another tensor's while the calls would write there."""
+    q = torch.zeros(300, dtype=torch.bfloat16)
+    o = ev.adamw([q], states=states)
+    for name in ["m", "v", "low", "steps"] + (["m_exponent", "v_exponent"] if states == "8bit" else []):
+        part = getattr(o, name)
+        was, memory = part.data_ptr(), part.data
+        for other in (part.clone(), part.data[1:], torch.zeros(0, dtype=part.dtype)):
+            part.data = other
+            refused(name, o.step, [q.clone()])
+            refused(name, o.values, "w")
+        del memory
+        taken = [torch.zeros_like(part) for _ in range(20)] + [torch.zeros(n, dtype=part.dtype) for n in (2, 4, 384, 768)]
+        assert all(t.data_ptr() != was for t in taken), name
+        o = ev.adamw([q], states=states)
+    without_context(o.step, [q.clone()])
