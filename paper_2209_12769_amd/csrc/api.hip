@@ -2213,6 +2213,7 @@ dc_status dc_check(dc_ctx* ctx, void* stream) {
     ctx->err = code == DC_ERR_BAD_PARTITION ? "device: label out of range or candidate/base-graph mismatch"
              : code == DC_ERR_CAPACITY      ? "device: sizes exceed the configured or provided capacity"
              : code == DC_ERR_BAD_GRAPH     ? "device: batch malformed (offsets, row pointers or a neighbour out of its graph)"
+             : code == DC_ERR_INVALID_ARG   ? "device: an id outside [-1, kinds), or a target that is not positive and finite"
                                             : "device: error";
   }
   return static_cast<dc_status>(code);

@@ -1086,3 +1086,10 @@ def test_adamw_refuses(B, ev):
         assert call([{}], values(w)) == B.DC_ERR_INVALID_ARG
     torch.cuda.synchronize()
     assert ev.check() == B.DC_OK and not p.any() and steps.tolist() == [3, 0]
+
+
+def test_embed_rows_says_what_was_wrong_with_an_id(B, ev):
+    assert ev.check() == B.DC_OK
+    ev.embed_rows(torch.tensor([0, 9], dtype=torch.int32, device="cuda"), torch.ones(9, 8, device="cuda"))
+    assert ev.check() == B.DC_ERR_INVALID_ARG and "id outside [-1, kinds)" in B.dc_last_error(ev.ctx)
+    assert ev.check() == B.DC_OK
