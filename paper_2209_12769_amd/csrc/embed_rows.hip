@@ -20,10 +20,10 @@ namespace {
 typedef unsigned long long u64;
 
 // ---- forward ----
-__device__ __forceinline__ int kind_of(const EmbedArgs& a, long long row) {
-  const int k = a.id[row];
-  if (k >= 0 && k < a.kinds) return k;
-  if (k != -1) atomicCAS(&a.status[1], 0, (int)DC_ERR_INVALID_ARG);
+// The kind that an id names, -1 for none.
+__device__ __forceinline__ int kind_of(const EmbedArgs& a, int id) {
+  if (id >= 0 && id < a.kinds) return id;
+  if (id != -1) atomicCAS(&a.status[1], 0, (int)DC_ERR_INVALID_ARG);
   return -1;
 }
 
@@ -51,10 +51,7 @@ __global__ __launch_bounds__(1024) void embed_kernel(const EmbedArgs a, int used
     for (int u = 0; u < kAtOnce; ++u) kind[u] = id[min(u * across + seat, left - 1)];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      if (kind[u] < 0 || kind[u] >= a.kinds) {
-        if (kind[u] != -1) atomicCAS(&a.status[1], 0, (int)DC_ERR_INVALID_ARG);
-        kind[u] = -1;
-      }
+      kind[u] = kind_of(a, kind[u]);
       v[u] = load_vector<T, false>(table + (long long)max(kind[u], 0) * a.ldt, (int)c, a.C);
     }
 #pragma unroll
@@ -66,7 +63,7 @@ __global__ __launch_bounds__(1024) void embed_kernel(const EmbedArgs a, int used
       for (int k = 0; k < kV; ++k) x[k] = kind[u] < 0 ? 0.f : x[k] * a.scale;
       T* to = Y + (long long)(u * across) * a.ldy;
       if (a.C >= kV) *reinterpret_cast<u32x4_any*>(to + y_on) = pack(x, T());
-      else store_vector<T, false>(to + y_on, 0, a.C, pack(x, T()));
+      else store_vector<T>(to + y_on, 0, a.C, pack(x, T()));
     }
   }
 }
@@ -82,7 +79,7 @@ struct Pair {
 // Rows that stand for nothing, or for no kind of the table, come last, as kind `kinds`.
 __device__ __forceinline__ Pair pair_at(const EmbedArgs& a, const Pair* in, int i) {
   if (in) return in[i];
-  const int k = kind_of(a, i);
+  const int k = kind_of(a, a.id[i]);
   return Pair{k < 0 ? a.kinds : k, i};
 }
 // The lanes of the wave, among `active`, whose digit is the same.
@@ -347,7 +344,7 @@ __device__ __forceinline__ void write_kind(const EmbedArgs& a, int kind, int c, 
   for (int k = 0; k < kVector<T>; ++k) y[k] = x[k] * a.scale;
   T* to = static_cast<T*>(a.dtable) + (long long)kind * a.lddt;
   if (c + kVector<T> <= a.C) __builtin_nontemporal_store(pack(y, T()), reinterpret_cast<u32x4_any*>(to + c));
-  else store_vector<T, false>(to, c, a.C, pack(y, T()));
+  else store_vector<T>(to, c, a.C, pack(y, T()));
 }
 // Four columns of an entry from c.
 __device__ __forceinline__ void read_entry(float (&x)[4], const float* row, int c, int C) { unpack(x, load_vector<float, false>(row, c, C), 0.f); }
@@ -356,7 +353,7 @@ __device__ __forceinline__ void write_entry(float* row, int c, int C, const floa
 #pragma unroll
   for (int k = 0; k < kV; k += 4) {
     const float y[4] = {x[k], x[k + 1], x[k + 2], x[k + 3]};
-    if (c + k < C) store_vector<float, false>(row, c + k, C, pack(y, 0.f));
+    if (c + k < C) store_vector<float>(row, c + k, C, pack(y, 0.f));
   }
 }
 // Four columns of a kind.
@@ -365,7 +362,7 @@ __device__ __forceinline__ void write_kind4(const EmbedArgs& a, int kind, int c,
 #pragma unroll
   for (int k = 0; k < 4; ++k) y[k] = x[k] * a.scale;
   if (!a.bf16) {
-    store_vector<float, false>(static_cast<float*>(a.dtable) + (long long)kind * a.lddt, c, a.C, pack(y, 0.f));
+    store_vector<float>(static_cast<float*>(a.dtable) + (long long)kind * a.lddt, c, a.C, pack(y, 0.f));
     return;
   }
   u16* row = static_cast<u16*>(a.dtable) + (long long)kind * a.lddt;

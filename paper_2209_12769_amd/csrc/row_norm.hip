@@ -168,7 +168,7 @@ __device__ __forceinline__ void put(const float (&y)[NV * kVector<T>], T* p, uns
     for (int k = 0; k < kV; ++k) w[k] = y[j * kV + k];
     if (kFit == kWhole || q.skip[j] < kV) {
       if constexpr (kFit == kShort) {
-        store_vector<T, false>(p + row, q.at[j], C, pack(w, T()));
+        store_vector<T>(p + row, q.at[j], C, pack(w, T()));
       } else if (kOwn && kFit == kBack && q.skip[j] > 0) {
 #pragma unroll
         for (int k = 0; k < kV; ++k)

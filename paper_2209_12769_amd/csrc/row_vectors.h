@@ -16,8 +16,6 @@ typedef unsigned u32_any __attribute__((aligned(1), may_alias));
 template <typename T>
 constexpr int kVector = 16 / (int)sizeof(T);     // values of 16 bytes
 
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(u16 x) { return __uint_as_float((unsigned)x << 16); }
 __device__ __forceinline__ void narrow(float x, float& y) { y = x; }
 __device__ __forceinline__ void narrow(float x, u16& y) { y = to_bf16(x); }
 
@@ -36,10 +34,10 @@ __device__ __forceinline__ u32x4 load_vector(const T* row, int c, int C) {
     }
   return v;
 }
-template <typename T, bool kFull>
+template <typename T>
 __device__ __forceinline__ void store_vector(T* row, int c, int C, u32x4 v) {
   constexpr int kV = kVector<T>;
-  if (kFull || c + kV <= C) {
+  if (c + kV <= C) {
     *reinterpret_cast<u32x4_any*>(row + c) = v;
     return;
   }
