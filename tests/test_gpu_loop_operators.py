@@ -1093,3 +1093,109 @@ def test_embed_rows_says_what_was_wrong_with_an_id(B, ev):
     ev.embed_rows(torch.tensor([0, 9], dtype=torch.int32, device="cuda"), torch.ones(9, 8, device="cuda"))
     assert ev.check() == B.DC_ERR_INVALID_ARG and "id outside [-1, kinds)" in B.dc_last_error(ev.ctx)
     assert ev.check() == B.DC_OK
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("C", [40, 256, 600, 9001])
+@pytest.mark.parametrize("where", ["x", "dy", "residual"])
+def test_row_norm_backward_of_a_row_that_is_not_finite(ev, dtype, bad, C, where):
+    """The other rows have the bits that they have where that row is finite."""
+    x, gamma, beta = (v.cuda() for v in norm_inputs(50, C, dtype))
+    t = {"x": x, "dy": rand(9, 50, C).to(x.dtype).cuda(), "residual": rand(10, 50, C).to(x.dtype).cuda()}
+
+    def back():
+        _, mean, rstd = ev.row_norm(t["x"], gamma, beta, EPS, "silu")
+        return ev.row_norm_backward(t["dy"], t["x"], gamma, beta, mean, rstd, "silu", t["residual"])
+    clean = back()
+    t[where][7, C // 2] = bad
+    dx, dgamma, dbeta = back()
+    fine = torch.arange(50, device="cuda") != 7
+    assert torch.equal(dx[fine], clean[0][fine]) and not torch.isfinite(dx[7, C // 2])
+    if where == "residual":                                # which is added behind everything else
+        assert torch.equal(dgamma, clean[1]) and torch.equal(dbeta, clean[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset,spread", [(1e5, 1.0), (1e6, 0.1), (-1e8, 8.0), (0.0, 1e-6), (3e12, 1e9)])
+@pytest.mark.parametrize("C", [5, 200, 3000, 9001])
+@pytest.mark.parametrize("name", ["none", "silu"])
+def test_row_norm_backward_far_from_zero(ev, dtype, offset, spread, C, name):
+    """Gradients by the mean and rstd that are given: those of the forward pass, which are rounded."""
+    rows, t = 40, TYPES[dtype]
+    x, dy = (offset + spread * rand(3, rows, C)).to(t), rand(4, rows, C).to(t)
+    _, gamma, beta = norm_inputs(1, C, dtype)
+    _, mean, rstd = ev.row_norm(x.cuda(), gamma.cuda(), beta.cuda(), EPS, name)
+    got = ev.row_norm_backward(dy.cuda(), x.cuda(), gamma.cuda(), beta.cuda(), mean, rstd, name)
+    for g, (w, tol), what in zip(got, norm_back_reference(x, dy, None, gamma, beta, mean.cpu(), rstd.cpu(), name, t), ("dx", "dgamma", "dbeta")):
+        close(g, w, tol, what)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,ld,first", [(64, 65, 1), (128, 131, 3), (256, 257, 1), (256, 259, 2), (512, 513, 7), (1024, 1025, 1), (4096, 4099, 1), (8192, 8195, 5), (16384, 16387, 1)])
+def test_row_norm_of_more_than_the_caches_anywhere(ev, dtype, C, ld, first):
+    """Rows of together more than 256 MiB that begin at any element have the bits of rows on 16-byte boundaries, both ways, from
+    kept rows and in place, and nothing between them is touched."""
+    t = TYPES[dtype]
+    rows = 2 ** 28 // (C * (2 if dtype == "bf16" else 4)) + 5
+    g = torch.Generator(device="cuda").manual_seed(C + ld)
+
+    def spread_out(v, fill, cols=C):
+        apart = ld - C + cols
+        buf = torch.full((first + v.shape[0] * apart,), fill, dtype=v.dtype, device="cuda")
+        w = buf[first:].view(v.shape[0], apart)[:, :cols]
+        w.copy_(v)
+        return w, buf
+
+    def untouched(w, buf, fill):
+        w.fill_(fill)
+        return bool((buf == fill).all())
+    x, dy, past = (torch.randn(rows, C, generator=g, device="cuda").to(t) for _ in range(3))
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g, device="cuda"), 0.3 * torch.randn(C, generator=g, device="cuda")
+    want = ev.row_norm(x, gamma, beta, EPS, "silu")
+    xa, _ = spread_out(x, 3)
+    ya, buf = spread_out(x, 5)
+    got = ev.row_norm(xa, gamma, beta, EPS, "silu", out=ya)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and untouched(ya, buf, 5)
+    del ya, buf, got
+    mean, rstd = want[1:]
+    want = ev.row_norm_backward(dy, x, gamma, beta, mean, rstd, "silu", past)
+    da, _ = spread_out(dy, 3)
+    pa, buf = spread_out(past, 5)
+    got = ev.row_norm_backward(da, xa, gamma, beta, mean, rstd, "silu", pa, out=pa)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and untouched(pa, buf, 5)
+    del pa, buf, got, xa
+    kept = ev.keep_rows(x)
+    want = ev.row_norm_backward(dy, kept, gamma, beta, mean, rstd, "silu")
+    off = type(kept)(spread_out(kept.code, 3)[0], spread_out(kept.exponent, 3, C // 32)[0], C)
+    ya, buf = spread_out(x, 5)
+    got = ev.row_norm_backward(da, off, gamma, beta, mean, rstd, "silu", out=ya)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and untouched(ya, buf, 5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kinds,how", [(97, "skewed"), (20011, "even")])
+@pytest.mark.parametrize("C,ld,first", [(1031, 1033, 1), (2057, 2058, 3), (264, 265, 1), (520, 520, 1)])
+def test_embed_rows_backward_of_more_than_the_caches_anywhere(ev, dtype, kinds, how, C, ld, first):
+    """Rows of together more than 256 MiB that begin at any element, to a table that does: against sums in 64 bits, and the bits
+    of rows one behind the other."""
+    t = TYPES[dtype]
+    rows = 2 ** 28 // (C * (2 if dtype == "bf16" else 4)) + 5
+    print(rows, kinds, C, ld, first, flush=True)
+    dy = torch.randn(rows, C, generator=torch.Generator(device="cuda").manual_seed(C + ld), device="cuda").to(t)
+    ids = ids_of(rows, kinds, how).cuda()
+    da = torch.full((first + rows * ld,), math.nan, dtype=t, device="cuda")[first:].view(rows, ld)[:, :C]
+    da.copy_(dy)
+    buf = torch.full((first + kinds * ld,), 5, dtype=t, device="cuda")
+    table = buf[first:].view(kinds, ld)[:, :C]
+    ev.embed_rows_backward(da, ids, kinds, 0.7, out=table)
+    assert torch.equal(table, ev.embed_rows_backward(dy, ids, kinds, 0.7))
+    want, size = (torch.zeros(kinds, C, dtype=torch.float64, device="cuda") for _ in range(2))
+    for lo in range(0, rows, 30000):
+        v = dy[lo:lo + 30000].double()
+        want.index_add_(0, ids[lo:lo + 30000].long(), v)
+        size.index_add_(0, ids[lo:lo + 30000].long(), v.abs())
+    # 64 rows of a run and four runs of a chunk in fp32, three lists rounded to fp32, the scale as fp32 and its product
+    close(table, (0.7 * want).cpu(), ((64 + 4 + 3) * U * 0.7 * size + (R(t) + 3 * U) * 0.7 * want.abs()).cpu(), "dtable")
+    table.fill_(5)
+    assert (buf == 5).all()
