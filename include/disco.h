@@ -580,7 +580,8 @@ typedef struct {
   int64_t ldy;
   /* backward only: u = gamma dY act'(.), xh = (x - mean) rstd,
    * dX = rstd (u - mean u - xh mean(u xh)) + dres, dgamma = sum dY act'(.) xh, dbeta = sum dY act'(.)
-   * by mean and rstd as they are given                                                   */
+   * by mean and rstd as they are given: a mean that was rounded to fp32 moves xh of its row by up to 2^-24 |mean| rstd (0.3 for
+   * values around 10^6 that spread by 0.1), and the gradients with it                    */
   const dc_kept_rows* kept; /* x as kept rows, or null                                    */
   const void* dY;
   int64_t lddy;
@@ -642,8 +643,15 @@ dc_status dc_embed_rows_backward(dc_ctx* ctx, const dc_embed_rows_args* args, vo
  *                     state takes from mix(mix(seed ^ mix(t)) + (q / 2) 0xD1342543DE82EF95) the low 32 bits (q even) or the high
  *                     ones, of them the low half for m and the high half for v.  m, v and g^2 (1 - beta2) are formed by
  *                     operations of fp32 rounded one by one, w from m and v before they are rounded to codes.
+ * A number that is not finite in a gradient makes the element's m, v and w NaN or infinite for good, with 8-bit moments m and v of
+ * its 128 places: a caller whose gradients may have one looks at them before the step.
+ * t is one number for all tensors: one whose gradient is null keeps its moments, and its next step is corrected by the t of that
+ * call.  (A first gradient at a late step moves a parameter by up to (1 - beta1) / sqrt(1 - beta2) lr, 3.2 lr by 0.9 and 0.999.)
+ * t and *grad_scale are read on the device, everything else is part of the call: replayed from a graph it counts t on and has lr,
+ * betas, eps, weight decay and seed as they were captured.
  * Tensors and states may not overlap, gradients may be each other.  `tensors` is read before the call returns.  All
- * tensors are one launch per 96 of them.                                                                             */
+ * tensors are one launch per 96 of them; where the last of these has more than 2048 chunks of 2048 elements (a tensor's last chunk
+ * may be a part of one), or none, one more counts the step.                                                         */
 enum { DC_MOMENTS_F32 = 0, DC_MOMENTS_8BIT = 1 };
 typedef struct {
   void* p;                  /* dev [n], neighbours                                        */

@@ -512,7 +512,9 @@ class AdamW:
     The state, device tensors of `total` places: m, v (float32, or uint8 codes with m_exponent and v_exponent for each 128
     places), low (int16: the low halves of bfloat16 parameters), steps (int32: steps done, 0).  Tensor k has the places
     at[k] .. at[k] + its elements.  Saved, and copied back into them (copy_), they go on where they were.  lr, betas, eps and seed
-    may be changed between steps.  A parameter may be given other memory (data) of its shape and type."""
+    may be changed between steps.  A parameter may be given other memory (data) of its shape and type, contiguous as it was.  A
+    bfloat16 parameter that is written anew keeps its low halves, up to half a rounding of it, until they are cleared
+    (low[at[k]:at[k] + p.numel()] = 0)."""
 
     _PARTS = ("m", "v", "m_exponent", "v_exponent", "low", "steps")
     _FIXED = frozenset(_PARTS + ("params", "at", "total", "states"))
@@ -585,7 +587,9 @@ class AdamW:
 
     def step(self, grads, grad_scale=None):
         """One step with a gradient for every tensor (float32 or bfloat16, contiguous, its shape), None for tensors that stay as
-        they are.  grad_scale: a float32 device tensor of one number that the gradients are multiplied by."""
+        they are.  grad_scale: a float32 device tensor of one number that the gradients are multiplied by.  `steps` counts for
+        all tensors: the corrections of one that had no gradient go on.  Captured in a graph, a step counts on when it is replayed and keeps
+        lr, betas, eps and seed of its capture.  A gradient that is not finite stays in the moments for good."""
         ev, T = self.ev, self.ev.torch.Tensor
         if len(grads) != len(self._shapes):
             raise ValueError(f"need {len(self._shapes)} gradients, not {len(grads)}")
@@ -594,7 +598,8 @@ class AdamW:
             which = [k for k, g in enumerate(grads) if g is not None]
             have, shapes = [grads[k] for k in which], [shapes[k] for k in which]
             self._table["g"] = 0
-        # A small step is bound by what happens here: one look at all of them after the other takes a quarter less than all at one.
+        # A small step is bound by what happens here and in _args: one look at all of them after the other takes a quarter less than
+        # all at one (28 parameters: 19.7 us, 4.5 of them for what _args looks at besides addresses).
         dtypes = list(map(T.dtype.__get__, have))
         if (not ev._types.keys() >= set(dtypes) or list(map(T.shape.__get__, have)) != shapes
                 or list(map(T.get_device, have)).count(ev.device.index) != len(have)
@@ -1024,7 +1029,7 @@ class Evaluator:
 
     def row_norm_backward(self, dy, x, gamma, beta, mean, rstd, act: str = "none", residual=None, out=None):
         """(dx, dgamma, dbeta) for the gradient dy at the result; `residual` is added to dx.  x: the rows, or KeptRows of
-        them; mean, rstd: what row_norm returned."""
+        them; mean, rstd: what row_norm returned, taken as they are (mean as rounded: see dc_row_norm_args for rows far from zero)."""
         rows, channels, lddy, dtype = self._rows(dy, "dy")
         pg = 0 if gamma is None else self._vector(gamma, "gamma", channels)
         pb = 0 if beta is None else self._vector(beta, "beta", channels)
@@ -1056,7 +1061,7 @@ class Evaluator:
         return self._vector(ids, "ids", ids.shape[0], self.torch.int32)
 
     def embed_rows(self, ids, table, scale: float = 1.0, out=None):
-        """scale * table[ids], rows of zeros where an id is -1.  check() reports ids that are neither."""
+        """scale * table[ids], rows of zeros where an id is -1; ids: int32.  check() reports ids that are neither."""
         kinds, channels, ldt, dtype = self._rows(table, "table")
         pid, rows = self._ids(ids), ids.shape[0]
         if out is None:

@@ -2108,7 +2108,7 @@ dc_status adamw_call(dc_ctx* ctx, const dc_adamw_args* a, bool step, float* cons
     }
     k.t[k.tensors++] = AdamwTensor{t.p, t.g, (long long)t.n, (unsigned)(t.at / kMomentBlock), (float)t.weight_decay, k.chunks,
                                    (t.p_dtype == DC_BF16 ? 1 : 0) | (t.g_dtype == DC_BF16 ? 2 : 0)};
-    k.chunks += (int)adamw_chunks(t.n);          // 2^26 of all tensors at most
+    k.chunks += (int)adamw_chunks(t.n);          // 2^27 of all tensors at most, and a part of one of each
   }
   k.count_up = step;
   if (step || k.chunks > 0) return enqueue_result(ctx, launch(), "AdamW launch");

@@ -11,7 +11,9 @@
 // in fp32, the chunks' in 64 bits, rounded to fp32 from list to list.  The table is cleared by the sort's launches, kinds that have
 // rows are written after that.  Bound by memory in the rows' sums, which read rows at the sorted list's places, and by launches in
 // the rest (474011 rows of 256 in fp32 to 97 kinds: 107 us, of them 77 the rows' sums, 6.3 TB/s; 65521 rows of 1031 in bf16 to
-// 128001 kinds: 103 us, of them 51 the sort and the zeros, 37 the rows' sums).
+// 128001 kinds, by dY that take turns: 109 us, of them 52 the sort and the zeros, 35 the rows' sums).  Rows of up to 32 vectors, to 97
+// kinds: 474011 rows of 256 in bf16 80 us, of them 45 the rows' sums (5.4 TB/s), of 128 in fp32 76 and 41 (5.9), of 128 in bf16 60 and
+// 26 (4.6).
 #include "row_vectors.h"
 
 namespace dc {
@@ -413,8 +415,10 @@ __device__ __forceinline__ Pair sorted_at(const Sums& s, int i) {
     return s.sorted[i];
   }
 }
-// First level: chunks of the sorted rows.  kWave: a wave each, of rows or slabs of more than 32 vectors.  kOnce: dY is read as not used
-// again soon.
+// First level: chunks of the sorted rows.  kWave: a wave each, of rows or slabs of more than 32 vectors, so that the list comes by scalar
+// loads and eight rows are on their way in the registers that this leaves (the whole call with and without: 65521 rows of 1031 in bf16 to
+// 128001 kinds 103 and 111 us, 100000 of 1024 to 50000 93 and 95; 474011 of 256 in fp32 to 97 110 and 108.5).  kOnce: dY is read as not
+// used again soon.
 constexpr long long kCached = 256 << 20;       // bytes that the memory's cache holds
 template <typename T, bool kWave, bool kOnce>
 __global__ __launch_bounds__(256) void sum_rows_kernel(const Sums s) {
@@ -605,7 +609,9 @@ Plan plan(long long rows, int kinds, int C, int bytes) {
   while (p.all_bits < 31 && (kinds >> p.all_bits) != 0) ++p.all_bits;          // values 0 .. kinds
   p.passes = rows <= kSmall ? 1 : (p.all_bits + kBits - 1) / kBits;
   p.bits = (p.all_bits + p.passes - 1) / p.passes;
-  // Small tiles until there are some hundred of them (65521 rows by tiles of 4096: 16 us a kernel, by tiles of 256: 5).
+  // Small tiles until there are some hundred of them (65521 rows by tiles of 4096: 16 us a kernel, by tiles of 256: 5).  The whole call,
+  // rows of 32 in bf16 to 100000 kinds, by tiles of 256, 1024 and 4096 pairs: 65521 rows 50, 53 and 84 us, 131072 65, 65 and 95, 262144
+  // 81, 70 and 100, 1 M 155, 109 and 122, 3 M 372, 212 and 191.
   p.per = rows <= 65536 ? 1 : (rows <= 1048576 ? 4 : 16);
   p.tiles = rows <= kSmall ? 0 : (int)((rows + kSortThreads * p.per - 1) / (kSortThreads * p.per));
   const int vectors = (C * bytes + 15) / 16;

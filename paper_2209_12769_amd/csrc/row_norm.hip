@@ -12,7 +12,8 @@
 // each workgroup hands on sums of 2 C numbers (2 M rows of 256 in bf16 with GELU and dres, 4.1 GB: 770 us, 5.3 TB/s; 474011 rows of
 // 256 in fp32, x in 8 bits: 1.1 GB, 197 us, 5.6 TB/s).
 // The variance is that of d = x - m, m the row's sum over C as fp32 has it: mean d is what m lacks, v = mean d^2 - (mean d)^2.
-// So neither loses digits for values far from zero, and mu is m + mean d, rounded once where it is returned.
+// So neither loses digits for values far from zero, and mu is m + mean d, rounded once where it is returned.  The gradients go by that
+// rounded mu: their xh is off by up to 2^-24 |mu| r, the same for a whole row.
 // Gradients of gamma and beta: 64 rows of a thread in fp32, these sums in fp32 again, a workgroup's rows and the workgroups
 // in 64 bits and a fixed order.
 #include <type_traits>
@@ -314,7 +315,9 @@ template <typename T, typename X, int NV, int kLanes, Fit kFit, bool kOnce>
 __global__ __launch_bounds__(kLanes == kGroup ? 1024 : 256) void row_norm_back_kernel(const RowNormArgs a, int row_lanes) {
   constexpr int kV = kVector<T>, kN = NV * kV;
   constexpr bool kKept = !std::is_same<T, X>::value, kWide = kLanes == kGroup;
-  // of sixteen values a thread the sums over rows stay in LDS, a thread's fours of both 1024 fours apart
+  // Of sixteen values a thread the sums over rows stay in LDS, a thread's fours of both 1024 fours apart.  That is one workgroup a CU, of
+  // which nothing covers the waits at its barrier, and in fp32 128 registers do not suffice (3 to 26 words of a thread in scratch memory):
+  // with dres 20000 x 16384 in bf16 653 us, 4.0 TB/s, in fp32 935, 5.6; 20011 x 16383 833 and 1206; rows of 8192 in fp32 5.7 TB/s.
   constexpr bool kLds = kN > 8;
   __shared__ float red[kWide ? 4 * kMostWaves : 2 * 256 * kN];
   __shared__ float4 sums[kLds ? 1024 * kN / 2 : 1];
@@ -500,7 +503,8 @@ Plan plan(long long rows, int C, int per) {
 }
 // A row a seat at a time, in the order in which the workgroups are handed out (a launch has less than 2^32 threads).  Wide rows in
 // bf16 take sixteen values a thread, two requests, as rows in fp32 do with eight, and go faster by a tenth
-// (50000 x 4096 in bf16, one row a seat: 211 us by eight, 189 by sixteen).
+// (50000 x 4096 in bf16, one row a seat: 211 us by eight, 189 by sixteen).  Rows beyond 8192 channels are one workgroup a CU (1024
+// threads of 92 to 114 registers): 20000 x 16384 in bf16 350 us, 3.7 TB/s, in fp32 497, 5.3.
 Plan forward_plan(long long rows, int C, bool bf16) {
   Plan p = plan(rows, C, C > 8192 || (bf16 && C > kNarrow) ? 16 : 8);
   p.blocks = (p.blocks + kSeatRows - 1) / kSeatRows;
